@@ -457,6 +457,131 @@ mkv_status mkv_kvquant_step(const mkv_config* cfg, const mkv_quant_params* qpara
 mkv_status mkv_rocket_step(const mkv_config* cfg, const void* q, const void* k_new, const void* v_new,
                            mkv_cache* cache, int32_t* page_idx_out, void* out, void* stream);
 
+/* ------------------------------------------------- trees of drafted tokens */
+
+/* Speculative decoding: a draft proposes n tokens per batch entry that form a
+ * tree behind the cached tokens; one pass attends with all of them, the
+ * verifier accepts one path, and that path's rows join the cache.  The paper
+ * (Table 1) runs one token a step; these calls are the same decode step for
+ * several.  The drafted tokens' keys and values stay outside the cache until
+ * they are accepted, so a rejected token never has to be taken out of it.
+ *
+ * mask uint64 [B][n]: drafted token i of entry b attends to every cached token
+ * 0..T_len[b]-1 and to drafted token j iff bit j of mask[b][i] is set (its
+ * ancestors and itself; bits n and above are ignored).  A token that sees
+ * nothing (empty cache, no bit) gets zeros.  What a token does not see does
+ * not reach its output, whatever bits (infinities, NaN) it holds.
+ */
+
+/* Bytes of workspace mkv_tree_attention needs for n drafted tokens over caches
+ * of T_cap slots (laid out as mkv_workspace_size describes).  Host only. */
+mkv_status mkv_tree_workspace_size(const mkv_config* cfg, int64_t T_cap, int32_t n, size_t* bytes);
+
+/* Attention of the drafted tokens of an FP16 cache.  q, out fp16
+ * [B][n][Hq][D]; k_tree, v_tree fp16 [B][n][Hkv][D] (keys already rotated by
+ * the tokens' positions); 1 <= n <= 64.  cfg->method must be MKV_FP16
+ * (MKV_ERR_UNSUPPORTED otherwise).  q, k_tree, v_tree, out and the cache's k
+ * and v must be 16-byte aligned and ws 256-byte aligned (MKV_ERR_INVALID_ARG);
+ * T_cap < 2^31 - 256 (MKV_ERR_UNSUPPORTED).  The cache is only read.  A bounded
+ * wait that ran out sets MKV_FLAG_WAIT_TIMEOUT. */
+mkv_status mkv_tree_attention(const mkv_config* cfg, const void* q, const mkv_cache* cache, const void* k_tree,
+                              const void* v_tree, const uint64_t* mask, int32_t n, void* out, void* ws,
+                              size_t ws_bytes, void* stream);
+
+/* Append the accepted path to an FP16 cache: for i < n_path[b], the rows of
+ * drafted token path[b][i] go to slot T_len[b] + i; then T_len[b] += n_path[b].
+ * k_tree, v_tree fp16 [B][n][Hkv][D], 16-byte aligned; path int32 [B][n]
+ * (entries at n_path[b] and above are not read; NULL: tokens 0, 1, ..), n_path
+ * int32 [B] (NULL: n for every entry); n >= 1 of any size.  An entry whose
+ * path does not fit its cache, is longer than n, negative, or names a token
+ * outside [0, n) gets no row, keeps T_len and sets MKV_FLAG_CACHE_FULL (read
+ * by mkv_get_status). */
+mkv_status mkv_tree_commit(const mkv_config* cfg, const void* k_tree, const void* v_tree, const int32_t* path,
+                           const int32_t* n_path, int32_t n, mkv_cache* cache, void* stream);
+
+/* -------------------------------------------------------- latent attention */
+
+/* A cache of one shared latent row a token: compression by the architecture,
+ * beside the paper's four by algorithm (Table 1).  Token t holds a row
+ * c_t of rank + rope_dim values, [latent | rotated key shared by all heads].
+ * Head h's key and value are linear in the latent part,
+ *   key_t,h = [W_uk[h] c_t[0:rank] | c_t[rank:]],  value_t,h = W_uv[h] c_t[0:rank],
+ * with the weights of a head stacked as w_kv [H][nope_dim + v_dim][rank]
+ * (W_uk[h] first).  Two forms of the same attention:
+ *   expanded (prompts): mkv_latent_expand writes every token's keys and values,
+ *     mkv_latent_prefill attends to them;
+ *   absorbed (decode): mkv_latent_absorb carries the queries into the latent
+ *     space, qa = [W_uk[h]^T q_nope | q_rope]; mkv_latent_attention attends to
+ *     the rows themselves, s = qa . c_t, o = sum_t p_t c_t[0:rank], reading each
+ *     row once for all heads; mkv_latent_project carries o out, W_uv[h] o. */
+typedef enum { MKV_F16 = 0, MKV_BF16 = 1 } mkv_dtype;
+
+typedef struct {
+  uint32_t abi_version;   /* must equal MKV_ABI_VERSION                      */
+  int32_t dtype;          /* mkv_dtype of every tensor of the call           */
+  int32_t B, H;           /* batch entries, query heads (1..256)             */
+  int32_t rank;           /* 256 or 512                                      */
+  int32_t rope_dim;       /* 64                                              */
+  int32_t nope_dim;       /* unrotated dims of a head's query/key: 64 or 128 */
+  int32_t v_dim;          /* dims of a head's value: 64 or 128               */
+  float softmax_scale;    /* 0 -> 1/sqrt(nope_dim + rope_dim)                */
+} mkv_latent_config;
+
+/* Device memory owned by the caller: T_len int32 [B] tokens held, rows
+ * [B][T_cap][rank + rope_dim], 16-byte aligned; token t in slot t. */
+typedef struct {
+  int64_t T_cap;
+  int32_t* T_len;
+  void* rows;
+} mkv_latent_cache;
+
+/* Bytes of workspace mkv_latent_attention needs for n tokens per entry over
+ * caches of T_cap slots.  Host only. */
+mkv_status mkv_latent_workspace_size(const mkv_latent_config* cfg, int64_t T_cap, int32_t n, size_t* bytes);
+
+/* q [B][n][H][nope_dim + rope_dim] -> q_abs [B][n][H][rank + rope_dim]:
+ * W_uk[h]^T q_nope, then the rotated part as it is.  n >= 1 of any size;
+ * pointers 16-byte aligned (as in every latent call: MKV_ERR_INVALID_ARG). */
+mkv_status mkv_latent_absorb(const mkv_latent_config* cfg, const void* q, const void* w_kv, int32_t n, void* q_abs,
+                             void* stream);
+
+/* o_lat [B][n][H][rank] -> out [B][n][H][v_dim]: W_uv[h] o_lat. */
+mkv_status mkv_latent_project(const mkv_latent_config* cfg, const void* o_lat, const void* w_kv, int32_t n, void* out,
+                              void* stream);
+
+/* Absorbed attention.  q_abs [B][n][H][rank + rope_dim], o_lat [B][n][H][rank],
+ * 1 <= n <= 64.  rows_tree [B][n][rank + rope_dim] and mask [B][n]: the drafted
+ * tokens and who sees them, as for mkv_tree_attention; rows_tree NULL (mask is
+ * then not read): every query sees exactly the T_len[b] cached tokens, as in a
+ * plain decode step whose token was committed first.  The cache is only read.
+ * ws must be 256-byte aligned. */
+mkv_status mkv_latent_attention(const mkv_latent_config* cfg, const void* q_abs, const mkv_latent_cache* cache,
+                                const void* rows_tree, const uint64_t* mask, int32_t n, void* o_lat, void* ws,
+                                size_t ws_bytes, void* stream);
+
+/* Keys and values of the cached tokens: kv [B][H][T_max][nope_dim + v_dim],
+ * kv[b][h][t] = w_kv[h] c_t[0:rank] for t < min(T_len[b], T_max); later rows
+ * are not written.  1 <= T_max <= T_cap. */
+mkv_status mkv_latent_expand(const mkv_latent_config* cfg, const mkv_latent_cache* cache, const void* w_kv,
+                             int64_t T_max, void* kv, void* stream);
+
+/* Expanded attention of a prompt, or of its next chunk.  q, out
+ * [B][n][H][nope_dim + rope_dim] and [B][n][H][v_dim]; kv [B][H][T_max][..] from
+ * mkv_latent_expand; the shared rotated keys are read from the cache, which
+ * holds the prompt's rows already.  Query i of entry b (i < q_len[b]; q_len NULL:
+ * n for every entry) is at position T_len[b] - q_len[b] + i and attends to the
+ * tokens up to its own; queries past q_len[b], and those before position 0, get
+ * zeros.  T_len[b] <= T_max (tokens past T_max are not attended to). */
+mkv_status mkv_latent_prefill(const mkv_latent_config* cfg, const void* q, const void* kv, int64_t T_max,
+                              const mkv_latent_cache* cache, const int32_t* q_len, int32_t n, void* out,
+                              void* stream);
+
+/* The accepted path's rows join the cache, as mkv_tree_commit; rows_new
+ * [B][n][rank + rope_dim].  With path and n_path NULL, a plain append of n rows
+ * (a prompt's, or a step's). */
+mkv_status mkv_latent_commit(const mkv_latent_config* cfg, const void* rows_new, const int32_t* path,
+                             const int32_t* n_path, int32_t n, mkv_latent_cache* cache, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

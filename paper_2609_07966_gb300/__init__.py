@@ -19,6 +19,7 @@ MKV_OK, MKV_ERR_INVALID_ARG, MKV_ERR_UNSUPPORTED, MKV_ERR_CUDA, MKV_ERR_CAPACITY
     MKV_ERR_TIMEOUT = range(7)
 MKV_FP16, MKV_KVQUANT, MKV_H2O, MKV_ROCKET = range(4)
 MKV_QUANT_UNIFORM, MKV_QUANT_NUQ = range(2)
+MKV_F16, MKV_BF16 = range(2)
 MKV_FLAG_K_OUTLIER_OVERFLOW = 0x1
 MKV_FLAG_CACHE_FULL = 0x2
 MKV_FLAG_WAIT_TIMEOUT = 0x4
@@ -51,6 +52,16 @@ class mkv_cache(ctypes.Structure):
                 ("k_out_cap", ctypes.c_int64)]
 
 
+class mkv_latent_config(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("B", ctypes.c_int32),
+                ("H", ctypes.c_int32), ("rank", ctypes.c_int32), ("rope_dim", ctypes.c_int32),
+                ("nope_dim", ctypes.c_int32), ("v_dim", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+class mkv_latent_cache(ctypes.Structure):
+    _fields_ = [("T_cap", ctypes.c_int64), ("T_len", ctypes.c_void_p), ("rows", ctypes.c_void_p)]
+
+
 class mkv_quant_params(ctypes.Structure):
     _fields_ = [("t_lo", ctypes.c_void_p), ("t_hi", ctypes.c_void_p), ("k_lo", ctypes.c_void_p),
                 ("k_scale", ctypes.c_void_p), ("k_cb", ctypes.c_void_p), ("v_cb", ctypes.c_void_p),
@@ -71,6 +82,9 @@ _P = ctypes.c_void_p
 _CFG = ctypes.POINTER(mkv_config)
 _CACHE = ctypes.POINTER(mkv_cache)
 _QP = ctypes.POINTER(mkv_quant_params)
+_LCFG = ctypes.POINTER(mkv_latent_config)
+_LCACHE = ctypes.POINTER(mkv_latent_cache)
+_SIZE = ctypes.POINTER(ctypes.c_size_t)
 _SIGS = {
     "mkv_workspace_size": [_CFG, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)],
     "mkv_cache_bytes": [_CFG, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t)],
@@ -93,6 +107,16 @@ _SIGS = {
     "mkv_select_config": [ctypes.POINTER(mkv_candidate), ctypes.c_int32, ctypes.c_double, ctypes.c_double,
                           ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)],
     "mkv_decode_attention_noalloc": [_CFG, _P, _CACHE, _P, _P],
+    "mkv_tree_workspace_size": [_CFG, ctypes.c_int64, ctypes.c_int32, _SIZE],
+    "mkv_tree_attention": [_CFG, _P, _CACHE, _P, _P, _P, ctypes.c_int32, _P, _P, ctypes.c_size_t, _P],
+    "mkv_tree_commit": [_CFG, _P, _P, _P, _P, ctypes.c_int32, _CACHE, _P],
+    "mkv_latent_workspace_size": [_LCFG, ctypes.c_int64, ctypes.c_int32, _SIZE],
+    "mkv_latent_absorb": [_LCFG, _P, _P, ctypes.c_int32, _P, _P],
+    "mkv_latent_project": [_LCFG, _P, _P, ctypes.c_int32, _P, _P],
+    "mkv_latent_attention": [_LCFG, _P, _LCACHE, _P, _P, ctypes.c_int32, _P, _P, ctypes.c_size_t, _P],
+    "mkv_latent_expand": [_LCFG, _LCACHE, _P, ctypes.c_int64, _P, _P],
+    "mkv_latent_prefill": [_LCFG, _P, _P, ctypes.c_int64, _LCACHE, _P, ctypes.c_int32, _P, _P],
+    "mkv_latent_commit": [_LCFG, _P, _P, _P, ctypes.c_int32, _LCACHE, _P],
 }
 
 
@@ -249,6 +273,64 @@ def mkv_kvquant_step(cfg, qparams, q: int, k_new: int, v_new: int, cache: mkv_ca
 
 def mkv_rocket_step(cfg, q: int, k_new: int, v_new: int, cache: mkv_cache, page_idx_out, out: int, stream=None):
     _call("mkv_rocket_step", ctypes.byref(cfg), q, k_new, v_new, ctypes.byref(cache), page_idx_out or None, out,
+          _stream(stream))
+
+
+def mkv_tree_workspace_size(cfg: mkv_config, T_cap: int, n: int) -> int:
+    b = ctypes.c_size_t(0)
+    _call("mkv_tree_workspace_size", ctypes.byref(cfg), T_cap, n, ctypes.byref(b))
+    return b.value
+
+
+def mkv_tree_attention(cfg, q: int, cache: mkv_cache, k_tree: int, v_tree: int, mask: int, n: int, out: int, ws: int,
+                       ws_bytes: int, stream=None):
+    _call("mkv_tree_attention", ctypes.byref(cfg), q, ctypes.byref(cache), k_tree, v_tree, mask, n, out, ws,
+          ws_bytes, _stream(stream))
+
+
+def mkv_tree_commit(cfg, k_tree: int, v_tree: int, path, n_path, n: int, cache: mkv_cache, stream=None):
+    _call("mkv_tree_commit", ctypes.byref(cfg), k_tree, v_tree, path or None, n_path or None, n, ctypes.byref(cache),
+          _stream(stream))
+
+
+def latent_config(dtype: int, B: int, H: int, rank: int = 512, rope_dim: int = 64, nope_dim: int = 128,
+                  v_dim: int = 128, softmax_scale: float = 0.0) -> mkv_latent_config:
+    """An mkv_latent_config with the ABI version set; fields as in mkv.h."""
+    return mkv_latent_config(MKV_ABI_VERSION, dtype, B, H, rank, rope_dim, nope_dim, v_dim, softmax_scale)
+
+
+def mkv_latent_workspace_size(cfg: mkv_latent_config, T_cap: int, n: int) -> int:
+    b = ctypes.c_size_t(0)
+    _call("mkv_latent_workspace_size", ctypes.byref(cfg), T_cap, n, ctypes.byref(b))
+    return b.value
+
+
+def mkv_latent_absorb(cfg, q: int, w_kv: int, n: int, q_abs: int, stream=None):
+    _call("mkv_latent_absorb", ctypes.byref(cfg), q, w_kv, n, q_abs, _stream(stream))
+
+
+def mkv_latent_project(cfg, o_lat: int, w_kv: int, n: int, out: int, stream=None):
+    _call("mkv_latent_project", ctypes.byref(cfg), o_lat, w_kv, n, out, _stream(stream))
+
+
+def mkv_latent_attention(cfg, q_abs: int, cache: mkv_latent_cache, rows_tree, mask, n: int, o_lat: int, ws: int,
+                         ws_bytes: int, stream=None):
+    _call("mkv_latent_attention", ctypes.byref(cfg), q_abs, ctypes.byref(cache), rows_tree or None, mask or None, n,
+          o_lat, ws, ws_bytes, _stream(stream))
+
+
+def mkv_latent_expand(cfg, cache: mkv_latent_cache, w_kv: int, T_max: int, kv: int, stream=None):
+    _call("mkv_latent_expand", ctypes.byref(cfg), ctypes.byref(cache), w_kv, T_max, kv, _stream(stream))
+
+
+def mkv_latent_prefill(cfg, q: int, kv: int, T_max: int, cache: mkv_latent_cache, q_len, n: int, out: int,
+                       stream=None):
+    _call("mkv_latent_prefill", ctypes.byref(cfg), q, kv, T_max, ctypes.byref(cache), q_len or None, n, out,
+          _stream(stream))
+
+
+def mkv_latent_commit(cfg, rows_new: int, path, n_path, n: int, cache: mkv_latent_cache, stream=None):
+    _call("mkv_latent_commit", ctypes.byref(cfg), rows_new, path or None, n_path or None, n, ctypes.byref(cache),
           _stream(stream))
 
 

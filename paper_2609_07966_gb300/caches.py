@@ -7,7 +7,8 @@ from __future__ import annotations
 
 import dataclasses
 
-from . import (MKV_FP16, MKV_H2O, MKV_KVQUANT, MKV_ROCKET, mkv_cache, mkv_quant_params, mkv_workspace_size,
+from . import (MKV_BF16, MKV_FP16, MKV_H2O, MKV_KVQUANT, MKV_ROCKET, mkv_cache, mkv_latent_cache,
+               mkv_latent_workspace_size, mkv_quant_params, mkv_tree_workspace_size, mkv_workspace_size,
                n_value_outliers)
 
 
@@ -95,3 +96,52 @@ def workspace(cfg, T_cap: int, device="cuda"):
     import torch
     n = mkv_workspace_size(cfg, T_cap)
     return torch.zeros(n, dtype=torch.uint8, device=device), n
+
+
+def wrap_cache(cfg, T_len, k, v) -> Cache:
+    """An FP16 cache over tensors the caller already has: k, v [B][Hkv][T_cap][D], T_len int32 [B]."""
+    c = mkv_cache()
+    c.T_cap, c.T_len, c.k, c.v = k.shape[2], _ptr(T_len), _ptr(k), _ptr(v)
+    return Cache(cfg, k.shape[2], {"T_len": T_len, "k": k, "v": v}, c)
+
+
+def tree_workspace(cfg, T_cap: int, n: int, device="cuda"):
+    """(tensor, nbytes) of the workspace of mkv_tree_attention for n drafted tokens, zero-filled."""
+    import torch
+    b = mkv_tree_workspace_size(cfg, T_cap, n)
+    return torch.zeros(b, dtype=torch.uint8, device=device), b
+
+
+@dataclasses.dataclass
+class LatentCache:
+    """One layer's latent cache: torch tensors plus the mkv_latent_cache struct over them."""
+    cfg: object
+    T_cap: int
+    t: dict
+    c: mkv_latent_cache
+
+
+def latent_dtype(cfg):
+    import torch
+    return torch.bfloat16 if cfg.dtype == MKV_BF16 else torch.float16
+
+
+def wrap_latent_cache(cfg, T_len, rows) -> LatentCache:
+    """A latent cache over tensors the caller already has: rows [B][T_cap][rank + rope_dim], T_len int32 [B]."""
+    return LatentCache(cfg, rows.shape[1], {"T_len": T_len, "rows": rows},
+                       mkv_latent_cache(rows.shape[1], _ptr(T_len), _ptr(rows)))
+
+
+def alloc_latent_cache(cfg, T_cap: int, device="cuda") -> LatentCache:
+    """Zeroed latent cache of T_cap slots (T_len = 0)."""
+    import torch
+    return wrap_latent_cache(cfg, torch.zeros(cfg.B, dtype=torch.int32, device=device),
+                             torch.zeros((cfg.B, T_cap, cfg.rank + cfg.rope_dim), dtype=latent_dtype(cfg),
+                                         device=device))
+
+
+def latent_workspace(cfg, T_cap: int, n: int, device="cuda"):
+    """(tensor, nbytes) of the workspace of mkv_latent_attention for n tokens per entry, zero-filled."""
+    import torch
+    b = mkv_latent_workspace_size(cfg, T_cap, n)
+    return torch.zeros(b, dtype=torch.uint8, device=device), b

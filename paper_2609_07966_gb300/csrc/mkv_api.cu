@@ -9,6 +9,7 @@
 
 #include "mkv_common.cuh"
 #include "mkv_internal.h"
+#include "mkv_rows.h"
 
 namespace mkv {
 
@@ -128,25 +129,6 @@ using namespace mkv;
 
 namespace {
 
-#define MKV_CUDA(expr)                                                          \
-  do {                                                                          \
-    cudaError_t e_ = (expr);                                                    \
-    if (e_ != cudaSuccess) {                                                    \
-      set_error("%s: %s", #expr, cudaGetErrorString(e_));                       \
-      return MKV_ERR_CUDA;                                                      \
-    }                                                                           \
-  } while (0)
-
-#define MKV_REQUIRE(cond, code, ...) \
-  do {                               \
-    if (!(cond)) {                   \
-      set_error(__VA_ARGS__);        \
-      return code;                   \
-    }                                \
-  } while (0)
-
-inline cudaStream_t as_stream(void* s) { return static_cast<cudaStream_t>(s); }
-
 mkv_status check_config(const mkv_config* c) {
   MKV_REQUIRE(c != nullptr, MKV_ERR_INVALID_ARG, "config is NULL");
   MKV_REQUIRE(c->abi_version == MKV_ABI_VERSION, MKV_ERR_INVALID_ARG, "abi_version %u != %u",
@@ -235,12 +217,6 @@ mkv_status check_qparams(const mkv_config* c, const mkv_quant_params* p, bool ne
   return MKV_OK;
 }
 
-#define MKV_TRY(expr)              \
-  do {                             \
-    mkv_status s_ = (expr);        \
-    if (s_ != MKV_OK) return s_;   \
-  } while (0)
-
 size_t workspace_bytes(const mkv_config* c, int64_t T_cap) {
   size_t b = decode_ws(*c, T_cap, nullptr).bytes;
   if (c->method == MKV_H2O || c->method == MKV_ROCKET) b = std::max(b, prefill_ws(*c, T_cap, nullptr).bytes);
@@ -326,6 +302,8 @@ mkv_status mkv_get_status(void* stream, uint32_t* flags) {
   MKV_CUDA(take_status_decode(flags, as_stream(stream)));
   MKV_CUDA(take_status_prefill(flags, as_stream(stream)));
   MKV_CUDA(take_status_kvq_step(flags, as_stream(stream)));
+  MKV_CUDA(take_status_rows(flags, as_stream(stream)));
+  MKV_CUDA(take_status_commit(flags, as_stream(stream)));
   if (*flags & MKV_FLAG_WAIT_TIMEOUT) {
     set_error("device status flags 0x%x (a bounded wait ran out)", *flags);
     return MKV_ERR_TIMEOUT;
