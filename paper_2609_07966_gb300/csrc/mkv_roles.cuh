@@ -1,0 +1,188 @@
+// Pieces shared by the warp-specialised tcgen05 attention and product kernels: bounded waits, operand
+// descriptors for both majors, tensor-memory loads and stores of a thread's columns, tensor maps.
+#pragma once
+
+#include <cuda.h>   // CUtensorMap and its enums; the encoder is fetched from the driver at run time
+#include <cuda_bf16.h>
+
+#include "mkv_tc.cuh"
+
+namespace mkv {
+
+constexpr uint64_t kRoleWaitNs = 1000000000ull;   // a bounded wait gives up after 1 s
+
+// Bounded wait of one role: false when it ran out (the flag is raised and MKV_FLAG_WAIT_TIMEOUT set in
+// *status) or another role's did.
+__device__ __forceinline__ bool wait_or_fail(uint64_t* bar, uint32_t parity, volatile int* fail, uint32_t* status) {
+  if (tc_mbar_try(bar, parity)) return true;
+  const uint64_t t0 = globaltimer_ns();
+  for (;;) {
+    if (tc_mbar_try(bar, parity)) return true;
+    if (*fail) return false;
+    if (globaltimer_ns() - t0 > kRoleWaitNs) break;
+  }
+  *fail = 1;
+  atomicOr(status, MKV_FLAG_WAIT_TIMEOUT);
+  return false;
+}
+
+// Instruction descriptor of kind::f16 with an fp32 accumulator: D format f32 in [4,6), A and B formats
+// (0 fp16, 1 bf16) in [7,10) and [10,13), A / B stored with M / N contiguous in bits 15 / 16, N >> 3 in
+// [17,23), M >> 4 in [24,29).
+__host__ __device__ constexpr uint32_t tc_idesc(bool bf16, int M, int N, bool a_mn, bool b_mn) {
+  return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((a_mn ? 1u : 0u) << 15) |
+         ((b_mn ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// Shared-memory descriptor of an operand whose M (or N) index is contiguous: `width` elements of it per
+// row (64, 32 or 16: the 128-, 64- or 32-byte swizzle), one row per K index, 8 rows a group; groups follow
+// one another every 8 rows, blocks of `width` every `block` bytes.  A K step of 16 advances by 16 rows.
+template <int width>
+__device__ __forceinline__ uint64_t tc_desc_mn(uint32_t start, uint32_t block) {
+  static_assert(width == 64 || width == 32 || width == 16, "row width");
+  constexpr uint64_t layout = width == 64 ? 2 : width == 32 ? 4 : 6;
+  return (uint64_t)((start >> 4) & 0x3fffu) | ((uint64_t)((block >> 4) & 0x3fffu) << 16) |
+         ((uint64_t)(8 * width * 2 >> 4) << 32) | ((uint64_t)1u << 46) | (layout << 61);
+}
+
+// Byte offset of 16-byte piece `c` of row `r` in such a tile (the swizzle XORs the piece with the row's
+// 128-byte line).
+template <int width>
+__device__ __forceinline__ uint32_t mn_offset(int r, int c) {
+  if (width == 64) return (uint32_t)(r * 128 + ((c ^ (r & 7)) << 4));
+  if (width == 32) return (uint32_t)(r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
+  return (uint32_t)(r * 32 + ((c ^ ((r >> 2) & 1)) << 4));
+}
+
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void prefetch_map(const void* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// Named barrier over `count` threads: with and without an OR of a predicate.
+__device__ __forceinline__ void bar_sync(int id, int count) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
+}
+__device__ __forceinline__ bool bar_or(int id, int count, bool p) {
+  uint32_t r;
+  asm volatile(
+      "{ .reg .pred p, q; setp.ne.u32 p, %1, 0; barrier.cta.red.or.pred q, %2, %3, p; selp.u32 %0, 1, 0, q; }"
+      : "=r"(r)
+      : "r"((uint32_t)p), "r"(id), "r"(count)
+      : "memory");
+  return r != 0;
+}
+
+// C consecutive fp32 columns of the thread's tensor-memory lane; the wait names the registers, so no use is
+// ordered before it.
+template <int C>
+__device__ __forceinline__ void tm_load(uint32_t addr, float (&v)[C]);
+template <>
+__device__ __forceinline__ void tm_load<8>(uint32_t addr, float (&v)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+               : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7])
+               :
+               : "memory");
+}
+#define MKV_OUT16(m, v, o)                                                                                      \
+  m(v[o + 0]), m(v[o + 1]), m(v[o + 2]), m(v[o + 3]), m(v[o + 4]), m(v[o + 5]), m(v[o + 6]), m(v[o + 7]),       \
+      m(v[o + 8]), m(v[o + 9]), m(v[o + 10]), m(v[o + 11]), m(v[o + 12]), m(v[o + 13]), m(v[o + 14]), m(v[o + 15])
+#define MKV_EQF(x) "=f"(x)
+#define MKV_PLF(x) "+f"(x)
+#define MKV_INF(x) "f"(x)
+template <>
+__device__ __forceinline__ void tm_load<16>(uint32_t addr, float (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+      : MKV_OUT16(MKV_EQF, v, 0)
+      : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : MKV_OUT16(MKV_PLF, v, 0) : : "memory");
+}
+template <>
+__device__ __forceinline__ void tm_load<32>(uint32_t addr, float (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+      : MKV_OUT16(MKV_EQF, v, 0), MKV_OUT16(MKV_EQF, v, 16)
+      : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : MKV_OUT16(MKV_PLF, v, 0), MKV_OUT16(MKV_PLF, v, 16) : : "memory");
+}
+// The stores complete at tm_store_wait().
+template <int C>
+__device__ __forceinline__ void tm_store(uint32_t addr, const float (&v)[C]);
+template <>
+__device__ __forceinline__ void tm_store<8>(uint32_t addr, const float (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};\n" ::"f"(v[0]), "f"(v[1]),
+               "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "r"(addr)
+               : "memory");
+}
+template <>
+__device__ __forceinline__ void tm_store<16>(uint32_t addr, const float (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};\n" ::
+          MKV_OUT16(MKV_INF, v, 0),
+      "r"(addr)
+      : "memory");
+}
+template <>
+__device__ __forceinline__ void tm_store<32>(uint32_t addr, const float (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};\n" ::MKV_OUT16(MKV_INF, v, 0),
+      MKV_OUT16(MKV_INF, v, 16), "r"(addr)
+      : "memory");
+}
+#undef MKV_OUT16
+#undef MKV_EQF
+#undef MKV_PLF
+#undef MKV_INF
+__device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Two fp32 values rounded to the type and packed (lo in the low half).
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if (BF16)
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <bool BF16>
+__device__ __forceinline__ float widen(uint16_t x) {
+  return BF16 ? __uint_as_float((uint32_t)x << 16) : __half2float(__ushort_as_half(x));
+}
+// Whether a 16-bit value is an infinity or NaN: its exponent bits are all ones.
+template <bool BF16>
+__device__ __forceinline__ bool non_finite(uint16_t x) {
+  constexpr uint16_t e = BF16 ? 0x7f80 : 0x7c00;
+  return (x & e) == e;
+}
+
+// A reduction of each of C columns over the warp's 32 lanes: on return v[0] of lane i holds column
+// i / (32 / C).
+template <int C, typename Op>
+__device__ __forceinline__ void reduce_columns(float (&v)[C], int lane, Op op) {
+  int lb = 16;
+#pragma unroll
+  for (int w = C / 2; w >= 1; w >>= 1) {
+    const bool up = (lane & lb) != 0;
+#pragma unroll
+    for (int i = 0; i < w; ++i) {
+      const float keep = up ? v[i + w] : v[i], send = up ? v[i] : v[i + w];
+      v[i] = op(keep, __shfl_xor_sync(0xffffffffu, send, lb));
+    }
+    lb >>= 1;
+  }
+  for (; lb >= 1; lb >>= 1) v[0] = op(v[0], __shfl_xor_sync(0xffffffffu, v[0], lb));
+}
+
+// A 4-D tensor map of 16-bit elements: dims and strides in elements (innermost stride 1), a box of
+// 64 x box1 x box2 x 1 with the 128-byte swizzle; what lies outside reads as zero.
+cudaError_t encode_map(CUtensorMap* m, const void* base, const int64_t (&dims)[4], const int64_t (&strides)[3],
+                       int box1, int box2);
+
+}  // namespace mkv
