@@ -1,53 +1,416 @@
-// Causal attention of a prompt's queries over expanded latent keys and values.
+// Causal attention of a prompt's queries over expanded latent keys and values:
+//   out_i = sum_{j <= pos_i} p_ij v_j / sum p_ij,  p_ij = 2^(scale log2(e) (q_i[:nope] . k_j + q_i[nope:] . r_j) - m_i)
+// with a head's own key part k_j and value v_j (mkv_latent_expand) and the rotated part r_j that all heads share,
+// which is read from the cache's rows: a key tile is assembled in shared memory from the two.
+//
+// Bound by the tensor cores (640 flops a pair at 192 / 128 dims against 2 exponentials' worth of special-function
+// time).  A CTA takes 256 queries of one head as two blocks of 128 rows and streams 128-key tiles past both, so the
+// tensor cores work on one block while the other is in its softmax:
+//   S_i [128 x 128] = Q_i K^T    operands in shared memory, accumulator in tensor memory
+//   O_i [128 x dv] += P_i V      P_i from tensor memory (it overwrites the S_i it came from), V from shared memory,
+//                                read along its other index
+// Tensor memory is full: 2 x (128 columns S / P + 128 columns O).  Warps 0..3 and 4..7 are the two softmax groups (a
+// thread holds one row: its maximum and sum need no exchange), then one warp loads tiles by TMA and one issues the
+// products in the order PV_0(t), QK_0(t + 1), PV_1(t), QK_1(t + 1).
+//
+// As in rows_attn.cu a row's maximum is raised only when a score passes it by 2^8, so O is almost never rescaled;
+// statistics and accumulators are fp32, the weights are rounded once to the type the tensor cores take.
 #include <algorithm>
 
+#include "mkv_roles.cuh"
 #include "mkv_rows.h"
-#include "row_attention.cuh"
 
 namespace mkv {
 
-namespace {
+__device__ uint32_t g_status_latent_prefill;   // MKV_FLAG_* bits raised here
 
-template <typename T, int DN, int DV>
-__global__ void __launch_bounds__(kRowWarps * 32) prefill_kernel(const PrefillCall a) {
-  constexpr int DK = DN + 64;
-  const int64_t row = blockIdx.x;                     // (b n + i) H + h
-  const int h = (int)(row % a.H);
-  const int64_t b = row / a.H / a.n, i = row / a.H % a.n;
-  const int64_t len = std::min<int64_t>(std::max(a.T_len[b], 0), a.T_max);
-  const int64_t ql = a.q_len != nullptr ? std::min(std::max(a.q_len[b], 0), a.n) : a.n;
-  const int64_t seen = i < ql ? std::min<int64_t>(len, (int64_t)a.T_len[b] - ql + i + 1) : 0;
-  const T* kv = static_cast<const T*>(a.kv) + (b * a.H + h) * a.T_max * (DN + DV);
-  const T* rows = static_cast<const T*>(a.rows) + b * a.T_cap * (a.rank + 64) + a.rank;
-  row_attention<T, DN, DK, DV>(
-      static_cast<const T*>(a.q) + row * DK, seen, a.scale * kLog2e,
-      [&](int64_t j, const T*& k0, const T*& k1, const T*& v) {
-        k0 = kv + j * (DN + DV);
-        v = k0 + DN;
-        k1 = rows + j * (a.rank + 64);
-        return true;
-      },
-      static_cast<T*>(a.out) + row * DV);
+cudaError_t take_status_latent_prefill(uint32_t* flags, cudaStream_t st) {
+  uint32_t v = 0, zero = 0;
+  cudaError_t e = cudaMemcpyFromSymbolAsync(&v, g_status_latent_prefill, sizeof(v), 0, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess)
+    e = cudaMemcpyToSymbolAsync(g_status_latent_prefill, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  *flags |= v;
+  return e;
 }
 
-template <typename T>
-cudaError_t launch_t(const PrefillCall& c, cudaStream_t st) {
-  const unsigned grid = (unsigned)((int64_t)c.B * c.n * c.H);
-  if (c.nope == 128 && c.v_dim == 128)
-    prefill_kernel<T, 128, 128><<<grid, kRowWarps * 32, 0, st>>>(c);
-  else if (c.nope == 128)
-    prefill_kernel<T, 128, 64><<<grid, kRowWarps * 32, 0, st>>>(c);
-  else if (c.v_dim == 128)
-    prefill_kernel<T, 64, 128><<<grid, kRowWarps * 32, 0, st>>>(c);
-  else
-    prefill_kernel<T, 64, 64><<<grid, kRowWarps * 32, 0, st>>>(c);
+namespace {
+
+constexpr int kBR = 128;            // rows a block, keys a tile
+constexpr float kRaise = 8.f;       // a score may pass the running maximum by this (log2) before it is raised
+constexpr float kOffset = 6.f;      // weights carry 2^kOffset (fp16: full precision down to 2^-20 of the maximum)
+constexpr float kNoMax = -1e30f;    // running maximum of a row that has seen nothing
+
+struct PrefillArgs {
+  int n, H;
+  int64_t T_max;
+  float scale_log2;
+  const int32_t *T_len, *q_len;
+  const uint16_t* kv;               // values, for non-finite ones
+  uint16_t* out;
+  int rank;
+};
+
+template <bool BF16_, int DN_, int DV_>
+struct PShape {
+  static constexpr bool BF16 = BF16_;
+  static constexpr int DN = DN_, DV = DV_, DK = DN + 64;
+  static constexpr int KA = DK / 64, VA = DV / 64;
+  static constexpr int ATOM = kBR * 128;                    // 128 rows of 64 dims
+  static constexpr int QBLK = KA * ATOM, KST = KA * ATOM, VST = VA * ATOM;
+  static constexpr int NSK = 2;
+  static constexpr int NSV = (2 * QBLK + NSK * KST + 2 * VST <= 224 * 1024 - 2048) ? 2 : 1;
+  static constexpr int Q_OFF = 0, K_OFF = 2 * QBLK, V_OFF = K_OFF + NSK * KST;
+  static constexpr int CTL_OFF = V_OFF + NSV * VST;
+  static constexpr int ALLOC = CTL_OFF + 512 + 1024;
+  static_assert(ALLOC <= 227 * 1024, "shared memory");
+};
+// Two softmax warpgroups, loads and products (and two idle warps); registers a thread at launch (168, what 384
+// threads get) split 2 x 208 + 88.
+constexpr int kPThreads = 384, kPRegsSoftmax = 208, kPRegsOther = 88;
+static_assert(2 * kPRegsSoftmax + kPRegsOther <= 3 * 168, "register shares");
+constexpr int kFixWords = 16;       // flags of the keys of the tiles that some row sees only in part
+
+struct PCtl {
+  uint64_t qfull[2], kfull[2], kempty[2], vfull[2], vempty[2], sfull[2], pfull[2], pvdone[2];
+  uint32_t tslot;
+  int fail, k_loaded, v_loaded, issued[2];
+  uint32_t nonfinite[kFixWords];    // keys (from the first partial tile) whose value holds a non-finite number
+};
+static_assert(sizeof(PCtl) <= 512, "control block");
+
+template <class S>
+__global__ void __launch_bounds__(kPThreads, 1)
+    latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kvmap,
+                          const __grid_constant__ CUtensorMap rmap, const PrefillArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+  PCtl* ctl = reinterpret_cast<PCtl*>(sm + S::CTL_OFF);
+  const int h = blockIdx.x % a.H, b = blockIdx.x / a.H;
+  const int i0 = (int)(gridDim.y - 1 - blockIdx.y) * 2 * kBR;    // the queries with the most keys first
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  const int tl = a.T_len[b];
+  const int len = (int)std::min<int64_t>(std::max(tl, 0), a.T_max);
+  const int ql = a.q_len != nullptr ? std::min(std::max(a.q_len[b], 0), a.n) : a.n;
+  // tokens that query i sees
+  auto seen_by = [&](int i) { return i < ql ? (int)std::min<int64_t>(len, std::max<int64_t>(0, (int64_t)tl - ql + i + 1)) : 0; };
+  int nt[2];                                             // tiles of each block
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int first = i0 + k * kBR, last = std::min(first + kBR, ql) - 1;
+    nt[k] = last >= first ? (seen_by(last) + kBR - 1) / kBR : 0;
+  }
+  const int ntiles = std::max(nt[0], nt[1]);
+  if (ntiles == 0) {
+    const int rows = std::min(2 * kBR, a.n - i0);
+    for (int e = threadIdx.x; e < rows * (S::DV / 8); e += kPThreads)
+      reinterpret_cast<uint4*>(a.out + (((int64_t)b * a.n + i0 + e / (S::DV / 8)) * a.H + h) * S::DV)[e % (S::DV / 8)] =
+          make_uint4(0, 0, 0, 0);
+    return;
+  }
+  const int td = seen_by(i0) / kBR;                      // first tile that the first row does not see whole
+
+  if (warp == 8) tc_alloc(&ctl->tslot, 512);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < 2; ++s) {
+      tc_mbar_init(&ctl->qfull[s], 1);
+      tc_mbar_init(&ctl->kfull[s], 1);
+      tc_mbar_init(&ctl->kempty[s], 1);
+      tc_mbar_init(&ctl->vfull[s], 1);
+      tc_mbar_init(&ctl->vempty[s], 1);
+      tc_mbar_init(&ctl->sfull[s], 1);
+      tc_mbar_init(&ctl->pfull[s], 4);
+      tc_mbar_init(&ctl->pvdone[s], 1);
+    }
+    tc_fence_mbar_init();
+    ctl->fail = ctl->k_loaded = ctl->v_loaded = ctl->issued[0] = ctl->issued[1] = 0;
+    for (int w = 0; w < kFixWords; ++w) ctl->nonfinite[w] = 0;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tbase = ctl->tslot;
+  volatile int* fail = &ctl->fail;
+  uint32_t* status = &g_status_latent_prefill;
+
+  if (warp >= 8) {
+    regs_down<kPRegsOther>();
+    if (warp == 8) {
+      // ---------------------------------------------------------------- loads: Q0 K0 Q1 V0 K1 V1 ..
+      if (lane == 0) {
+        auto load_q = [&](int k) {
+          tc_mbar_expect_tx(&ctl->qfull[k], S::QBLK);
+          for (int at = 0; at < S::KA; ++at)
+            tma_load_4d(sm + S::Q_OFF + k * S::QBLK + at * S::ATOM, &qmap, at * 64, i0 + k * kBR, h, b, &ctl->qfull[k]);
+        };
+        auto load_k = [&](int t) {
+          const int s = t % S::NSK, u = t / S::NSK;
+          if (u > 0 && !wait_or_fail(&ctl->kempty[s], (uint32_t)((u - 1) & 1), fail, status)) return false;
+          uint8_t* dst = sm + S::K_OFF + s * S::KST;
+          tc_mbar_expect_tx(&ctl->kfull[s], S::KST);
+          for (int at = 0; at < S::DN / 64; ++at)
+            tma_load_4d(dst + at * S::ATOM, &kvmap, at * 64, t * kBR, h, b, &ctl->kfull[s]);
+          tma_load_4d(dst + (S::DN / 64) * S::ATOM, &rmap, a.rank, t * kBR, b, 0, &ctl->kfull[s]);
+          ctl->k_loaded = t + 1;
+          return true;
+        };
+        auto load_v = [&](int t) {
+          const int s = t % S::NSV, u = t / S::NSV;
+          if (u > 0 && !wait_or_fail(&ctl->vempty[s], (uint32_t)((u - 1) & 1), fail, status)) return false;
+          tc_mbar_expect_tx(&ctl->vfull[s], S::VST);
+          for (int at = 0; at < S::VA; ++at)
+            tma_load_4d(sm + S::V_OFF + s * S::VST + at * S::ATOM, &kvmap, S::DN + at * 64, t * kBR, h, b,
+                        &ctl->vfull[s]);
+          ctl->v_loaded = t + 1;
+          return true;
+        };
+        load_q(0);
+        bool ok = load_k(0);
+        load_q(1);
+        for (int t = 0; ok && t < ntiles; ++t) {
+          if (t + 1 < ntiles) ok = load_k(t + 1);
+          if (ok) ok = load_v(t);
+        }
+      }
+    } else if (warp == 9) {
+      // ---------------------------------------------------------------- products
+      if (lane == 0) {
+        constexpr uint32_t idS = tc_idesc(S::BF16, kBR, kBR, false, false);
+        constexpr uint32_t idO = tc_idesc(S::BF16, kBR, S::DV, false, true);
+        const Desc qd = tc_desc_sw128(smem_addr(sm + S::Q_OFF));
+        const Desc kd = tc_desc_sw128(smem_addr(sm + S::K_OFF));
+        const Desc vd = tc_desc_mn<64>(smem_addr(sm + S::V_OFF), S::ATOM);
+        auto wait = [&](uint64_t* bar, uint32_t parity) {
+          const bool ok = wait_or_fail(bar, parity, fail, status);
+          tc_fence_after();
+          return ok;
+        };
+        auto scores = [&](int k, int t) {     // S_k of tile t
+          const Desc q0 = qd.at(k * S::QBLK).opaque(), k0 = kd.at(t % S::NSK * S::KST).opaque();
+  #pragma unroll
+          for (int kk = 0; kk < S::KA * 4; ++kk) {
+            const uint32_t o = (kk >> 2) * S::ATOM + (kk & 3) * 32;
+            tc_mma_ss(tbase + (uint32_t)(k * kBR), q0.at(o), k0.at(o), idS, kk > 0 ? 1u : 0u);
+          }
+          tc_commit(&ctl->sfull[k]);
+        };
+        auto values = [&](int k, int t) {     // O_k += P_k V of tile t
+          const Desc v0 = vd.at(t % S::NSV * S::VST).opaque();
+  #pragma unroll
+          for (int kk = 0; kk < kBR / 16; ++kk)
+            tc_mma_ts(tbase + (uint32_t)(2 * kBR + k * kBR), tbase + (uint32_t)(k * kBR + kk * 8), v0.at(kk * 2048), idO,
+                      t > 0 || kk > 0 ? 1u : 0u);
+          tc_commit(&ctl->pvdone[k]);
+          ctl->issued[k] = t + 1;
+        };
+        bool ok = wait(&ctl->kfull[0], 0);
+        for (int k = 0; ok && k < 2; ++k) {
+          ok = wait(&ctl->qfull[k], 0);
+          if (ok && nt[k] > 0) scores(k, 0);
+        }
+        if (ok) tc_commit(&ctl->kempty[0]);
+        for (int t = 0; ok && t < ntiles; ++t) {
+          ok = wait(&ctl->vfull[t % S::NSV], (uint32_t)((t / S::NSV) & 1));
+          if (ok && t + 1 < ntiles) ok = wait(&ctl->kfull[(t + 1) % S::NSK], (uint32_t)(((t + 1) / S::NSK) & 1));
+          for (int k = 0; ok && k < 2; ++k) {
+            if (t < nt[k]) {
+              ok = wait(&ctl->pfull[k], (uint32_t)(t & 1));
+              if (!ok) break;
+              values(k, t);
+            }
+            if (k == 1) tc_commit(&ctl->vempty[t % S::NSV]);
+            if (t + 1 < nt[k]) scores(k, t + 1);
+            if (k == 1 && t + 1 < ntiles) tc_commit(&ctl->kempty[(t + 1) % S::NSK]);
+          }
+        }
+      }
+    }
+  } else {
+    regs_up<kPRegsSoftmax>();
+    // ---------------------------------------------------------------- softmax: group k, row 32 (warp % 4) + lane
+    const int k = warp >> 2;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t tS = tbase + lanes + (uint32_t)(k * kBR), tO = tbase + lanes + (uint32_t)(2 * kBR + k * kBR);
+    const int row = (warp & 3) * 32 + lane, i = i0 + k * kBR + row;
+    const int seen = seen_by(i);
+    float m = kNoMax, l = 0.f;
+    bool dead = false;      // this warp's waits ran out: no barrier but mbarriers joins warps here, so it just stops
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (!dead) dead = !__all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status));
+      tc_fence_after();
+      return !dead;
+    };
+    for (int t = 0; t < nt[k]; ++t) {
+      if (!wait(&ctl->sfull[k], (uint32_t)(t & 1))) break;
+      float v[kBR];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tm_issue<32>(tS + c * 32, *reinterpret_cast<float(*)[32]>(&v[c * 32]));
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tm_wait<32>(*reinterpret_cast<float(*)[32]>(&v[c * 32]));
+      if (t >= td) {                         // a tile that some row sees only in part
+        const int lim = seen - t * kBR;
+#pragma unroll
+        for (int c = 0; c < kBR; ++c) v[c] = c < lim ? v[c] : -INFINITY;
+      }
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int c = 0; c < kBR / 2; ++c) mx[c & 3] = fmax3(mx[c & 3], v[2 * c], v[2 * c + 1]);
+      const float mt = fmax3(mx[0], mx[1], fmaxf(mx[2], mx[3])) * a.scale_log2;   // (the scale is positive)
+      if (__any_sync(0xffffffffu, mt > m + kRaise)) {
+        const float nm = fmaxf(m, mt), w = ex2_approx(m - nm);
+        m = nm;
+        l *= w;
+        if (t > 0) {
+          if (!wait(&ctl->pvdone[k], (uint32_t)((t - 1) & 1))) break;
+#pragma unroll 1
+          for (int c = 0; c < S::DV / 32; ++c) {
+            float o[32];
+            tm_load<32>(tO + c * 32, o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] *= w;
+            tm_store<32>(tO + c * 32, o);
+          }
+        }
+      }
+      const uint64_t sc2 = pk2(a.scale_log2, a.scale_log2), off2 = pk2(kOffset - m, kOffset - m);
+      uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {          // 64 keys = 32 packed columns
+        float pk[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const float2 x = upk2(ffma2(pk2(v[c * 64 + 2 * e], v[c * 64 + 2 * e + 1]), sc2, off2));
+          const float p0 = ex2_approx(x.x), p1 = ex2_approx(x.y);
+          sum2[e & 1] = fadd2(sum2[e & 1], pk2(p0, p1));
+          pk[e] = __uint_as_float(pack2<S::BF16>(p0, p1));
+        }
+        tm_store<32>(tS + c * 32, pk);
+      }
+      const float2 s0 = upk2(sum2[0]), s1 = upk2(sum2[1]);
+      l += (s0.x + s0.y) + (s1.x + s1.y);
+      if (t >= td && (k == 0 || t >= nt[0])) {
+        // Values that some row of the CTA does not see must not meet its zero weight (0 x NaN): slots past the
+        // length become zeros; a token's non-finite values become zeros here and are added to the rows that see it
+        // at the end.  Done by the first block that meets the tile, before its product.
+        if (!wait(&ctl->vfull[t % S::NSV], (uint32_t)((t / S::NSV) & 1))) break;
+        uint8_t* vt = sm + S::V_OFF + (t % S::NSV) * S::VST;
+        for (int e = threadIdx.x & 127; e < kBR * 8 * S::VA; e += 128) {
+          const int r = e / (8 * S::VA), x = e % (8 * S::VA);
+          uint4* p8 = reinterpret_cast<uint4*>(vt + (x >> 3) * S::ATOM + r * 128 + ((x & 7) << 4));
+          if (t * kBR + r >= len) {
+            *p8 = make_uint4(0, 0, 0, 0);
+            continue;
+          }
+          uint4 raw = *p8;
+          if (bad_pairs<S::BF16>(raw)) {
+            *p8 = raw;
+            const int key = (t - td) * kBR + r;
+            atomicOr(&ctl->nonfinite[key >> 5], 1u << (key & 31));
+          }
+        }
+        fence_async_smem();
+      }
+      tm_store_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc_mbar_arrive(&ctl->pfull[k]);
+    }
+    // ---------------------------------------------------------------- output
+    // the other block's last tile may hold values zeroed for this one: its flags are complete once both are done
+    if (nt[k] > 0) wait(&ctl->pvdone[k], (uint32_t)((nt[k] - 1) & 1));
+    if (!dead) {
+      const float inv = l == 0.f || i >= ql ? 0.f : 1.f / l;
+      uint16_t* dst = a.out + (((int64_t)b * a.n + i) * a.H + h) * S::DV;
+      uint32_t any = 0;
+      for (int w = 0; w < kFixWords; ++w) any |= ctl->nonfinite[w];
+#pragma unroll 1
+      for (int c = 0; c < S::DV / 32; ++c) {
+        float o[32];
+        if (nt[k] > 0) {
+          tm_load<32>(tO + c * 32, o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+        }
+        if (any != 0) {                      // the non-finite values that this row sees
+          for (int key = td * kBR; key < seen; ++key) {
+            const int f = key - td * kBR;
+            if (!(ctl->nonfinite[f >> 5] >> (f & 31) & 1)) continue;
+            const uint16_t* y = a.kv + (((int64_t)b * a.H + h) * a.T_max + key) * (S::DN + S::DV) + S::DN + c * 32;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] += non_finite<S::BF16>(y[e]) ? widen<S::BF16>(y[e]) : 0.f;
+          }
+        }
+        if (i < a.n) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint4 x;
+            x.x = pack2<S::BF16>(inv == 0.f ? 0.f : o[8 * e] * inv, inv == 0.f ? 0.f : o[8 * e + 1] * inv);
+            x.y = pack2<S::BF16>(inv == 0.f ? 0.f : o[8 * e + 2] * inv, inv == 0.f ? 0.f : o[8 * e + 3] * inv);
+            x.z = pack2<S::BF16>(inv == 0.f ? 0.f : o[8 * e + 4] * inv, inv == 0.f ? 0.f : o[8 * e + 5] * inv);
+            x.w = pack2<S::BF16>(inv == 0.f ? 0.f : o[8 * e + 6] * inv, inv == 0.f ? 0.f : o[8 * e + 7] * inv);
+            reinterpret_cast<uint4*>(dst + c * 32)[e] = x;
+          }
+        }
+      }
+    }
+  }
+  // teardown: on a failure wait (bounded) for the copies and products already issued
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && ctl->fail) {
+    tc_mbar_wait(&ctl->qfull[0], 0, kRoleWaitNs);
+    tc_mbar_wait(&ctl->qfull[1], 0, kRoleWaitNs);
+    for (int t = std::max(0, ctl->k_loaded - S::NSK); t < ctl->k_loaded; ++t)
+      tc_mbar_wait(&ctl->kfull[t % S::NSK], (uint32_t)((t / S::NSK) & 1), kRoleWaitNs);
+    for (int t = std::max(0, ctl->v_loaded - S::NSV); t < ctl->v_loaded; ++t)
+      tc_mbar_wait(&ctl->vfull[t % S::NSV], (uint32_t)((t / S::NSV) & 1), kRoleWaitNs);
+    for (int k = 0; k < 2; ++k)
+      if (ctl->issued[k] > 0) tc_mbar_wait(&ctl->pvdone[k], (uint32_t)((ctl->issued[k] - 1) & 1), kRoleWaitNs);
+  }
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8) tc_dealloc(tbase, 512);
+}
+
+template <class S>
+cudaError_t launch_shape(const PrefillCall& c, const PrefillArgs& a, cudaStream_t st) {
+  CUtensorMap qm, kvm, rm;
+  const int64_t dk = S::DK, n = c.n, H = c.H, B = c.B, d = S::DN + S::DV, T = c.T_max, row = c.rank + c.rope;
+  cudaError_t e = encode_map(&qm, c.q, {dk, n, H, B}, {H * dk, dk, n * H * dk}, kBR, 1);
+  if (e == cudaSuccess) e = encode_map(&kvm, c.kv, {d, T, H, B}, {d, T * d, H * T * d}, kBR, 1);
+  if (e == cudaSuccess) e = encode_map(&rm, c.rows, {row, c.T_cap, B, 1}, {row, c.T_cap * row, B * c.T_cap * row}, kBR, 1);
+  if (e != cudaSuccess) return e;
+  constexpr int smem = std::max(S::ALLOC, 116 * 1024);      // one CTA an SM: it takes all of the tensor memory
+  e = cudaFuncSetAttribute(latent_prefill_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  latent_prefill_kernel<S><<<dim3((unsigned)(H * B), (unsigned)ceil_div(n, 2 * kBR)), kPThreads, smem, st>>>(qm, kvm, rm, a);
   return cudaPeekAtLastError();
+}
+
+template <bool BF16>
+cudaError_t launch_t(const PrefillCall& c, const PrefillArgs& a, cudaStream_t st) {
+  if (c.nope == 128 && c.v_dim == 128) return launch_shape<PShape<BF16, 128, 128>>(c, a, st);
+  if (c.nope == 128) return launch_shape<PShape<BF16, 128, 64>>(c, a, st);
+  if (c.v_dim == 128) return launch_shape<PShape<BF16, 64, 128>>(c, a, st);
+  return launch_shape<PShape<BF16, 64, 64>>(c, a, st);
 }
 
 }  // namespace
 
 cudaError_t launch_latent_prefill(const PrefillCall& c, cudaStream_t st) {
-  return c.dtype == MKV_BF16 ? launch_t<__nv_bfloat16>(c, st) : launch_t<__half>(c, st);
+  PrefillArgs a{};
+  a.n = c.n;
+  a.H = c.H;
+  a.T_max = c.T_max;
+  a.scale_log2 = c.scale * kLog2e;
+  a.T_len = c.T_len;
+  a.q_len = c.q_len;
+  a.kv = static_cast<const uint16_t*>(c.kv);
+  a.out = static_cast<uint16_t*>(c.out);
+  a.rank = c.rank;
+  return c.dtype == MKV_BF16 ? launch_t<true>(c, a, st) : launch_t<false>(c, a, st);
 }
 
 }  // namespace mkv

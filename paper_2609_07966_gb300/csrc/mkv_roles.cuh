@@ -54,9 +54,50 @@ __device__ __forceinline__ uint32_t mn_offset(int r, int c) {
   return (uint32_t)(r * 32 + ((c ^ ((r >> 2) & 1)) << 4));
 }
 
+// An operand descriptor as its two words: a product's offsets only touch the low one.  opaque() hides the low
+// word's value from the compiler, which would otherwise keep every k step's sum in a register across tiles.
+struct Desc {
+  uint32_t lo, hi;
+  __device__ __forceinline__ Desc(uint64_t d) : lo((uint32_t)d), hi((uint32_t)(d >> 32)) {}
+  __device__ __forceinline__ Desc(uint32_t l, uint32_t h) : lo(l), hi(h) {}
+  __device__ __forceinline__ Desc at(uint32_t bytes) const { return Desc(lo + (bytes >> 4), hi); }
+  __device__ __forceinline__ Desc opaque() const {
+    uint32_t x = lo;
+    asm volatile("" : "+r"(x));
+    return Desc(x, hi);
+  }
+};
+// D[tmem] (+)= A[smem] B[smem], one K step of 16
+__device__ __forceinline__ void tc_mma_ss(uint32_t d_tmem, Desc a, Desc b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{ .reg .pred p; .reg .b64 da, db; setp.ne.b32 p, %6, 0; mov.b64 da, {%1, %2}; mov.b64 db, {%3, %4};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p; }" ::"r"(d_tmem),
+      "r"(a.lo), "r"(a.hi), "r"(b.lo), "r"(b.hi), "r"(idesc), "r"(acc)
+      : "memory");
+}
+// the same with A in tensor memory: its rows are lanes, two 16-bit values of K a column
+__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, Desc b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{ .reg .pred p; .reg .b64 db; setp.ne.b32 p, %5, 0; mov.b64 db, {%2, %3};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p; }" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b.lo), "r"(b.hi), "r"(idesc), "r"(acc)
+      : "memory");
+}
+
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void prefetch_map(const void* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// This warpgroup's registers per thread; every warp of it takes part, and the block's shares have to add up to no
+// more than it was launched with.
+template <int R>
+__device__ __forceinline__ void regs_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R));
+}
+template <int R>
+__device__ __forceinline__ void regs_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R));
 }
 
 // Named barrier over `count` threads: with and without an OR of a predicate.
@@ -73,15 +114,20 @@ __device__ __forceinline__ bool bar_or(int id, int count, bool p) {
   return r != 0;
 }
 
-// C consecutive fp32 columns of the thread's tensor-memory lane; the wait names the registers, so no use is
-// ordered before it.
+// C consecutive fp32 columns of the thread's tensor-memory lane.  The registers are valid after tm_wait, which
+// names them, so no use is ordered before it (a second wait, already satisfied, covers more registers).
 template <int C>
-__device__ __forceinline__ void tm_load(uint32_t addr, float (&v)[C]);
+__device__ __forceinline__ void tm_issue(uint32_t addr, float (&v)[C]);
+template <int C>
+__device__ __forceinline__ void tm_wait(float (&v)[C]);
 template <>
-__device__ __forceinline__ void tm_load<8>(uint32_t addr, float (&v)[8]) {
+__device__ __forceinline__ void tm_issue<8>(uint32_t addr, float (&v)[8]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
                : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
                : "r"(addr));
+}
+template <>
+__device__ __forceinline__ void tm_wait<8>(float (&v)[8]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
                : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7])
                :
@@ -94,21 +140,32 @@ __device__ __forceinline__ void tm_load<8>(uint32_t addr, float (&v)[8]) {
 #define MKV_PLF(x) "+f"(x)
 #define MKV_INF(x) "f"(x)
 template <>
-__device__ __forceinline__ void tm_load<16>(uint32_t addr, float (&v)[16]) {
+__device__ __forceinline__ void tm_issue<16>(uint32_t addr, float (&v)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
       : MKV_OUT16(MKV_EQF, v, 0)
       : "r"(addr));
+}
+template <>
+__device__ __forceinline__ void tm_wait<16>(float (&v)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : MKV_OUT16(MKV_PLF, v, 0) : : "memory");
 }
 template <>
-__device__ __forceinline__ void tm_load<32>(uint32_t addr, float (&v)[32]) {
+__device__ __forceinline__ void tm_issue<32>(uint32_t addr, float (&v)[32]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
       "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
       : MKV_OUT16(MKV_EQF, v, 0), MKV_OUT16(MKV_EQF, v, 16)
       : "r"(addr));
+}
+template <>
+__device__ __forceinline__ void tm_wait<32>(float (&v)[32]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : MKV_OUT16(MKV_PLF, v, 0), MKV_OUT16(MKV_PLF, v, 16) : : "memory");
+}
+template <int C>
+__device__ __forceinline__ void tm_load(uint32_t addr, float (&v)[C]) {
+  tm_issue<C>(addr, v);
+  tm_wait<C>(v);
 }
 // The stores complete at tm_store_wait().
 template <int C>
@@ -160,6 +217,22 @@ template <bool BF16>
 __device__ __forceinline__ bool non_finite(uint16_t x) {
   constexpr uint16_t e = BF16 ? 0x7f80 : 0x7c00;
   return (x & e) == e;
+}
+
+// Zeroes the non-finite values among eight packed ones; whether there were any.
+template <bool BF16>
+__device__ __forceinline__ bool bad_pairs(uint4& x) {
+  constexpr uint32_t e = BF16 ? 0x7f80u : 0x7c00u;
+  uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool lo = (w[i] & e) == e, hi = (w[i] & (e << 16)) == (e << 16);
+    any |= lo | hi;
+    w[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+  }
+  x = make_uint4(w[0], w[1], w[2], w[3]);
+  return any;
 }
 
 // A reduction of each of C columns over the warp's 32 lanes: on return v[0] of lane i holds column

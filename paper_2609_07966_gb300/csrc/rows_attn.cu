@@ -75,7 +75,10 @@ struct Shape {
   static constexpr int NB = DV / MV;                       // O^T blocks
   static constexpr int NG = N > 64 ? 4 : 2;                // softmax groups of 128 threads
   static constexpr int C = N / NG;                         // rows a softmax thread holds
-  static constexpr int THREADS = NG * 128 + 64;
+  static constexpr int THREADS = NG * 128 + 128;           // softmax groups; loads, products (and two idle warps)
+  // registers a thread: what a launch of THREADS gets, and its split between softmax and the others
+  static constexpr int RL = NG == 2 ? 168 : 96, RS = NG == 2 ? 208 : 104, RO = NG == 2 ? 88 : 64;
+  static_assert(NG * RS + RO <= (NG + 1) * RL, "register shares");
   static constexpr int PW = N >= 64 ? 64 : N;              // row width of a weight tile (elements)
   static constexpr int ATOM = KT * 128;                    // bytes of 64 dims of a tile
   static constexpr int QATOM = N * 128;
@@ -163,71 +166,75 @@ __global__ void __launch_bounds__(S::THREADS, 1)
   const uint32_t tO = tbase + 2 * N;
   volatile int* fail = &ctl->fail;
 
-  if (warp == S::NG * 4) {
-    // ---------------------------------------------------------------- loads
-    if (lane == 0) {
-      tc_mbar_expect_tx(&ctl->qfull, S::KA * S::QATOM);
-      for (int at = 0; at < S::KA; ++at)
-        if (S::SHARED)
-          tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, row0, b, 0, &ctl->qfull);
-        else
-          tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, kvh * a.G, row0 / a.G, b, &ctl->qfull);
-      for (int t = 0; t < nt; ++t) {
-        const int s = t % S::NS, u = t / S::NS;
-        if (u > 0 && !wait_or_fail(&ctl->kempty[s], (uint32_t)((u - 1) & 1), fail, &g_status_rows)) break;
-        const bool tr = t_begin + t >= ctiles;
-        const int key = tr ? 0 : (t_begin + t) * KT;
-        uint8_t* dst = sm + S::KV_OFF + s * S::STAGE;
-        tc_mbar_expect_tx(&ctl->kfull[s], S::STAGE);
+  if (warp >= S::NG * 4) {
+    regs_down<S::RO>();
+    if (warp == S::NG * 4) {
+      // ---------------------------------------------------------------- loads
+      if (lane == 0) {
+        tc_mbar_expect_tx(&ctl->qfull, S::KA * S::QATOM);
         for (int at = 0; at < S::KA; ++at)
-          tma_load_4d(dst + at * S::ATOM, tr ? &ktmap : &kmap, at * 64, key, S::SHARED ? b : kvh, S::SHARED ? 0 : b,
-                      &ctl->kfull[s]);
-        if (!S::SHARED)
-          for (int at = 0; at < S::VA; ++at)
-            tma_load_4d(dst + S::V_OFF + at * S::ATOM, tr ? &vtmap : &vmap, at * 64, key, kvh, b, &ctl->kfull[s]);
-        ctl->loaded = t + 1;
+          if (S::SHARED)
+            tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, row0, b, 0, &ctl->qfull);
+          else
+            tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, kvh * a.G, row0 / a.G, b, &ctl->qfull);
+        for (int t = 0; t < nt; ++t) {
+          const int s = t % S::NS, u = t / S::NS;
+          if (u > 0 && !wait_or_fail(&ctl->kempty[s], (uint32_t)((u - 1) & 1), fail, &g_status_rows)) break;
+          const bool tr = t_begin + t >= ctiles;
+          const int key = tr ? 0 : (t_begin + t) * KT;
+          uint8_t* dst = sm + S::KV_OFF + s * S::STAGE;
+          tc_mbar_expect_tx(&ctl->kfull[s], S::STAGE);
+          for (int at = 0; at < S::KA; ++at)
+            tma_load_4d(dst + at * S::ATOM, tr ? &ktmap : &kmap, at * 64, key, S::SHARED ? b : kvh, S::SHARED ? 0 : b,
+                        &ctl->kfull[s]);
+          if (!S::SHARED)
+            for (int at = 0; at < S::VA; ++at)
+              tma_load_4d(dst + S::V_OFF + at * S::ATOM, tr ? &vtmap : &vmap, at * 64, key, kvh, b, &ctl->kfull[s]);
+          ctl->loaded = t + 1;
+        }
       }
-    }
-  } else if (warp == S::NG * 4 + 1) {
-    // ---------------------------------------------------------------- products
-    if (lane == 0) {
-      constexpr uint32_t idS = tc_idesc(S::BF16, KT, N, false, false);
-      constexpr uint32_t idO = tc_idesc(S::BF16, S::MV, N, true, true);
-      const uint64_t qd = tc_desc_sw128(smem_addr(sm + S::Q_OFF));
-      const uint64_t kd = tc_desc_sw128(smem_addr(sm + S::KV_OFF));
-      const uint64_t vd = tc_desc_mn<64>(smem_addr(sm + S::KV_OFF + S::V_OFF), S::ATOM);
-      const uint64_t pd = tc_desc_mn<S::PW>(smem_addr(sm + S::P_OFF), KT * S::PW * 2);
-      auto scores = [&](int t) {        // S^T of tile t
-        const int s = t % S::NS;
-        if (!wait_or_fail(&ctl->kfull[s], (uint32_t)((t / S::NS) & 1), fail, &g_status_rows)) return false;
-        tc_fence_after();
-        const uint64_t ks = kd + (uint64_t)((s * S::STAGE) >> 4);
-#pragma unroll
-        for (int kk = 0; kk < S::KA * 4; ++kk)
-          tc_mma(tbase + (uint32_t)((t & 1) * N), ks + (uint64_t)(((kk >> 2) * S::ATOM + (kk & 3) * 32) >> 4),
-                 qd + (uint64_t)(((kk >> 2) * S::QATOM + (kk & 3) * 32) >> 4), idS, kk > 0 ? 1u : 0u);
-        tc_commit(&ctl->sfull[t & 1]);
-        return true;
-      };
-      bool ok = wait_or_fail(&ctl->qfull, 0, fail, &g_status_rows) && scores(0);
-      for (int t = 0; ok && t < nt; ++t) {
-        if (t + 1 < nt && !scores(t + 1)) break;
-        const int s = t % S::NS, pb = t % S::NP;
-        if (!wait_or_fail(&ctl->pfull[pb], (uint32_t)((t / S::NP) & 1), fail, &g_status_rows)) break;
-        tc_fence_after();
-        const uint64_t vs = vd + (uint64_t)((s * S::STAGE) >> 4), ps = pd + (uint64_t)((pb * S::PBUF) >> 4);
-#pragma unroll
-        for (int mb = 0; mb < S::NB; ++mb)
-#pragma unroll
-          for (int kk = 0; kk < KT / 16; ++kk)
-            tc_mma(tO + (uint32_t)(mb * N), vs + (uint64_t)((mb * (S::MV / 64) * S::ATOM + kk * 2048) >> 4),
-                   ps + (uint64_t)((kk * 16 * S::PW * 2) >> 4), idO, t > 0 || kk > 0 ? 1u : 0u);
-        tc_commit(&ctl->kempty[s]);
-        tc_commit(&ctl->pvdone[pb]);
-        ctl->issued = t + 1;
+    } else if (warp == S::NG * 4 + 1) {
+      // ---------------------------------------------------------------- products
+      if (lane == 0) {
+        constexpr uint32_t idS = tc_idesc(S::BF16, KT, N, false, false);
+        constexpr uint32_t idO = tc_idesc(S::BF16, S::MV, N, true, true);
+        const Desc qd = tc_desc_sw128(smem_addr(sm + S::Q_OFF));
+        const Desc kd = tc_desc_sw128(smem_addr(sm + S::KV_OFF));
+        const Desc vd = tc_desc_mn<64>(smem_addr(sm + S::KV_OFF + S::V_OFF), S::ATOM);
+        const Desc pd = tc_desc_mn<S::PW>(smem_addr(sm + S::P_OFF), KT * S::PW * 2);
+        auto scores = [&](int t) {        // S^T of tile t
+          const int s = t % S::NS;
+          if (!wait_or_fail(&ctl->kfull[s], (uint32_t)((t / S::NS) & 1), fail, &g_status_rows)) return false;
+          tc_fence_after();
+          const Desc ks = kd.at(s * S::STAGE).opaque(), qs = qd.opaque();
+  #pragma unroll
+          for (int kk = 0; kk < S::KA * 4; ++kk)
+            tc_mma_ss(tbase + (uint32_t)((t & 1) * N), ks.at((kk >> 2) * S::ATOM + (kk & 3) * 32),
+                      qs.at((kk >> 2) * S::QATOM + (kk & 3) * 32), idS, kk > 0 ? 1u : 0u);
+          tc_commit(&ctl->sfull[t & 1]);
+          return true;
+        };
+        bool ok = wait_or_fail(&ctl->qfull, 0, fail, &g_status_rows) && scores(0);
+        for (int t = 0; ok && t < nt; ++t) {
+          if (t + 1 < nt && !scores(t + 1)) break;
+          const int s = t % S::NS, pb = t % S::NP;
+          if (!wait_or_fail(&ctl->pfull[pb], (uint32_t)((t / S::NP) & 1), fail, &g_status_rows)) break;
+          tc_fence_after();
+          const Desc vs = vd.at(s * S::STAGE).opaque(), ps = pd.at(pb * S::PBUF).opaque();
+  #pragma unroll
+          for (int mb = 0; mb < S::NB; ++mb)
+  #pragma unroll
+            for (int kk = 0; kk < KT / 16; ++kk)
+              tc_mma_ss(tO + (uint32_t)(mb * N), vs.at(mb * (S::MV / 64) * S::ATOM + kk * 2048),
+                        ps.at(kk * 16 * S::PW * 2), idO, t > 0 || kk > 0 ? 1u : 0u);
+          tc_commit(&ctl->kempty[s]);
+          tc_commit(&ctl->pvdone[pb]);
+          ctl->issued = t + 1;
+        }
       }
     }
   } else {
+    regs_up<S::RS>();
     // ---------------------------------------------------------------- softmax
     const int q = warp & 3, grp = warp >> 2;             // lane quarter (keys), rows grp C .. + C - 1
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
@@ -332,18 +339,10 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         uint8_t* vt = sm + S::KV_OFF + s * S::STAGE + S::V_OFF;
         for (int e = threadIdx.x; e < valid * 8 * S::VA; e += S::NG * 128) {
           const int r = e / (8 * S::VA), x = e % (8 * S::VA);
-          uint16_t* p8 = reinterpret_cast<uint16_t*>(vt + (x >> 3) * S::ATOM + r * 128 + ((x & 7) << 4));
-          uint4 raw = *reinterpret_cast<uint4*>(p8);
-          uint16_t* h = reinterpret_cast<uint16_t*>(&raw);
-          bool bad = false;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (non_finite<S::BF16>(h[i])) {
-              bad = true;
-              h[i] = 0;
-            }
-          if (bad) {
-            *reinterpret_cast<uint4*>(p8) = raw;
+          uint4* p8 = reinterpret_cast<uint4*>(vt + (x >> 3) * S::ATOM + r * 128 + ((x & 7) << 4));
+          uint4 raw = *p8;
+          if (bad_pairs<S::BF16>(raw)) {
+            *p8 = raw;
             atomicOr(reinterpret_cast<unsigned long long*>(&ctl->nonfinite), 1ull << r);
           }
         }
