@@ -90,6 +90,7 @@ cudaError_t launch_commit(const CommitCall& c, cudaStream_t st);
 // Status words of these units (as take_status_append).
 cudaError_t take_status_rows(uint32_t* flags, cudaStream_t st);
 cudaError_t take_status_latent_prefill(uint32_t* flags, cudaStream_t st);
+cudaError_t take_status_product(uint32_t* flags, cudaStream_t st);
 cudaError_t take_status_commit(uint32_t* flags, cudaStream_t st);
 
 }  // namespace mkv
