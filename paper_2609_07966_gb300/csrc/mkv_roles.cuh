@@ -26,6 +26,17 @@ __device__ __forceinline__ bool wait_or_fail(uint64_t* bar, uint32_t parity, vol
   return false;
 }
 
+// One non-blocking test of phase `parity` of `bar`.
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{ .reg .pred p; mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+      : "=r"(ok)
+      : "r"(smem_addr(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // Instruction descriptor of kind::f16 with an fp32 accumulator: D format f32 in [4,6), A and B formats
 // (0 fp16, 1 bf16) in [7,10) and [10,13), A / B stored with M / N contiguous in bits 15 / 16, N >> 3 in
 // [17,23), M >> 4 in [24,29).

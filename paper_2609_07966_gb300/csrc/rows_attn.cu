@@ -12,9 +12,14 @@
 // (its first dv dims): one load of a row serves both products.  Accumulators live in tensor memory: S^T twice
 // (tile t + 1's scores are computed under tile t's softmax), O^T as dv / 128 blocks of N columns.
 //
-// A CTA takes one (batch entry, key head), one block of N rows and a run of key tiles (the drafted tokens are
-// one more tile at the end); runs of one block are joined by join_kernel.  Warps 0..4g-1 are the softmax
-// (a thread holds one key and N / g rows), then one warp loads tiles by TMA and one issues the products.
+// Work: the key tiles of all (entry, key head, row block) units, the drafted tokens as one more tile at the end of
+// each unit, are laid end to end and every CTA takes an equal run (the lengths are read on the device, so unequal
+// entries balance too).  A unit inside one run is written directly; the pieces of a unit that several runs share go
+// to the workspace and join_kernel adds them up.
+//
+// Roles: warps 0..4g-1 are the softmax (a thread holds one key and N / g rows), then one warp loads chunks by TMA
+// into a ring of slots and one issues products, taking whichever is ready: a finished tile's second product
+// first (it frees slots), else the next chunk of the scores.
 //
 // The running maximum m is only raised when some score of a tile passes it by 2^8 (weights then stay below
 // 2^14 with the offset below), which a group-wide vote finds: after the first tiles almost never, so the O^T
@@ -50,8 +55,8 @@ constexpr float kNoMax = -1e30f;    // running maximum of a row that has seen no
 
 struct RowsArgs {
   int B, n, H, Hkv, G;              // G: query heads per key head (latent: H)
-  int R;                            // rows per unit: n G
-  int n_split;
+  int R, row_blocks;                // rows per (entry, key head): n G; their blocks of N
+  int log_g;                        // FP16 caches: log2 G
   bool tree;
   int64_t T_cap;
   float scale_log2;
@@ -59,427 +64,657 @@ struct RowsArgs {
   const uint64_t* mask;             // [B][n]
   const uint16_t* v_tree;           // values of the drafted tokens (for non-finite ones)
   int64_t v_tok, v_head;            // their strides: token, key head
-  void* out;
-  float* part_o;                    // [units][R][n_split][DV]
-  float2* part_ml;                  // [units][R][n_split]
+  uint16_t* out;
+  float* part_o;                    // [CTAs][2][N][DV]: a run's pieces of units that other runs share
+  float2* part_ml;                  // [CTAs][2][N]
 };
 
 // KA / VA: 64-dim atoms of a key / value; SHARED: values are the keys' first atoms; KT keys a tile, N rows a
-// block, NS stages, NP weight buffers.
-template <bool BF16_, int KA_, int VA_, bool SHARED_, int KT_, int N_, int NS_, int NP_>
+// block, SLOTS ring slots, ROPE slots of the last key atom (SHARED), NP weight buffers.
+template <bool BF16_, int KA_, int VA_, bool SHARED_, int KT_, int N_, int SLOTS_, int ROPE_, int NP_>
 struct Shape {
   static constexpr bool BF16 = BF16_, SHARED = SHARED_;
-  static constexpr int KA = KA_, VA = VA_, KT = KT_, N = N_, NS = NS_, NP = NP_;
+  static constexpr int KA = KA_, VA = VA_, KT = KT_, N = N_, SLOTS = SLOTS_, ROPE = ROPE_, NP = NP_;
   static constexpr int DV = VA * 64;
   static constexpr int MV = DV >= 128 ? 128 : 64;          // value dims per product (its M)
   static constexpr int NB = DV / MV;                       // O^T blocks
   static constexpr int NG = N > 64 ? 4 : 2;                // softmax groups of 128 threads
   static constexpr int C = N / NG;                         // rows a softmax thread holds
-  static constexpr int THREADS = NG * 128 + 128;           // softmax groups; loads, products (and two idle warps)
+  static constexpr int SOFT = NG * 128, THREADS = SOFT + 128;   // (two of the last four warps idle)
   // registers a thread: what a launch of THREADS gets, and its split between softmax and the others
   static constexpr int RL = NG == 2 ? 168 : 96, RS = NG == 2 ? 208 : 104, RO = NG == 2 ? 88 : 64;
   static_assert(NG * RS + RO <= (NG + 1) * RL, "register shares");
   static constexpr int PW = N >= 64 ? 64 : N;              // row width of a weight tile (elements)
   static constexpr int ATOM = KT * 128;                    // bytes of 64 dims of a tile
   static constexpr int QATOM = N * 128;
-  static constexpr int STAGE = (KA + (SHARED ? 0 : VA)) * ATOM;
-  static constexpr int V_OFF = SHARED ? 0 : KA * ATOM;     // of the values within a stage
+  // a tile's ring chunks: SHARED: its value blocks (MV dims each, the last key atom apart); else keys, values
+  static constexpr int CH = SHARED ? NB : 2;
+  static constexpr int SLOT = SHARED ? (MV / 64) * ATOM : KA * ATOM;
+  static_assert(SHARED || KA == VA, "keys and values of one size");
+  static_assert(!SHARED || KA == VA + 1, "one key atom past the values");
   static constexpr int PBUF = KT * N * 2;
   static constexpr int Q_OFF = 0;
   static constexpr int KV_OFF = KA * QATOM;
-  static constexpr int P_OFF = KV_OFF + NS * STAGE;
-  static constexpr int CTL_OFF = P_OFF + NP * PBUF;
-  static constexpr int RED_OFF = CTL_OFF + 768;            // [4][N] floats
-  static constexpr int BYTES = RED_OFF + 4 * N * 4;
-  static constexpr int ALLOC = BYTES + 1024;               // slack to align the base to 1024 B
+  static constexpr int R_OFF = KV_OFF + SLOTS * SLOT;
+  static constexpr int P_OFF = R_OFF + ROPE * ATOM;
+  static constexpr int VIS_OFF = P_OFF + NP * PBUF;        // [kMaxTree][VW] words: rows that see a drafted token
+  static constexpr int VW = (N + 31) / 32;
+  static constexpr int RED_OFF = VIS_OFF + kMaxTree * VW * 4;   // [4][N] floats
+  static constexpr int CTL_OFF = RED_OFF + 4 * N * 4;
+  static constexpr int ALLOC = CTL_OFF + 512 + 1024;       // slack to align the base to 1024 B
   static constexpr int COLS = (2 + NB) * N;
-  static constexpr int TMEM = COLS <= 32 ? 32 : COLS <= 64 ? 64 : COLS <= 128 ? 128 : COLS <= 256 ? 256 : 512;
+  static constexpr int TMEM = COLS <= 64 ? 64 : COLS <= 128 ? 128 : COLS <= 256 ? 256 : 512;
   static_assert(COLS <= 512 && ALLOC <= 227 * 1024, "does not fit an SM");
 };
 
+constexpr int kMaxSlotsRing = 12;
 struct RowsCtl {
-  uint64_t qfull, kfull[4], kempty[4], sfull[2], pfull[2], pvdone[2];
+  uint64_t qfull, qempty, ofree, full[kMaxSlotsRing], empty[kMaxSlotsRing], rfull[4], rempty[4], sfull[2], pfull[2],
+      pvdone[2];
   uint64_t nonfinite;     // drafted tokens that hold a non-finite value
+  int64_t run0, run1, base;   // this CTA's run of tiles, first tile of entry b0
   uint32_t tslot;
-  int fail, loaded, issued;
-  uint64_t mask[kMaxTree];
+  int fail, b0;
+  int q_loads, chunks, ropes, scores, values;   // issued so far (read after a failure)
 };
-static_assert(sizeof(RowsCtl) <= 768, "control block");
+static_assert(sizeof(RowsCtl) <= 512, "control block");
+
+__device__ __forceinline__ int entry_len(const RowsArgs& a, int b) {
+  return (int)std::min<int64_t>(std::max(a.T_len[b], 0), a.T_cap);
+}
+// Tiles of one unit of entry b.
+template <int KT>
+__device__ __forceinline__ int entry_tiles(const RowsArgs& a, int b) {
+  return (entry_len(a, b) + KT - 1) / KT + (a.tree ? 1 : 0);
+}
+
+// A run's pieces, one unit at a time.
+template <int KT>
+struct Pieces {
+  const RowsArgs& a;
+  int64_t cur, end, base;   // next tile of the run, its end, first tile of entry b
+  int b, per;               // units per entry
+  // the current piece: unit `u` of entry b, its tiles t0 .. t1 - 1 of `tiles`
+  int u, t0, t1, tiles, len, index;
+  __device__ __forceinline__ Pieces(const RowsArgs& args, const RowsCtl* c)
+      : a(args), cur(c->run0), end(c->run1), base(c->base), b(c->b0), per(args.Hkv * args.row_blocks), index(-1) {}
+  __device__ __forceinline__ bool next() {
+    if (cur >= end) return false;
+    for (;;) {
+      len = entry_len(a, b);
+      tiles = (len + KT - 1) / KT + (a.tree ? 1 : 0);
+      if (cur < base + (int64_t)tiles * per) break;
+      base += (int64_t)tiles * per;
+      ++b;
+    }
+    const int64_t rel = cur - base;
+    u = (int)(rel / tiles);
+    t0 = (int)(rel - (int64_t)u * tiles);
+    t1 = (int)std::min<int64_t>(tiles, t0 + (end - cur));
+    cur += t1 - t0;
+    ++index;
+    return true;
+  }
+};
 
 template <class S>
 __global__ void __launch_bounds__(S::THREADS, 1)
     rows_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                 const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap ktmap,
                 const __grid_constant__ CUtensorMap vtmap, const RowsArgs a) {
-  constexpr int KT = S::KT, N = S::N, C = S::C;
+  constexpr int KT = S::KT, N = S::N, C = S::C, CH = S::CH;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
   RowsCtl* ctl = reinterpret_cast<RowsCtl*>(sm + S::CTL_OFF);
-  float* red = reinterpret_cast<float*>(sm + S::RED_OFF);
-  const int split = blockIdx.x, rb = blockIdx.y, unit = blockIdx.z;
-  const int b = unit / a.Hkv, kvh = unit % a.Hkv;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int kLoad = S::NG * 4, kMma = kLoad + 1;      // their warps
 
-  // this CTA's tiles: the entry's cached tiles, then the drafted tokens' tile
-  const int len = (int)std::min<int64_t>(std::max(a.T_len[b], 0), a.T_cap);
-  const int ctiles = (len + KT - 1) / KT, tiles = ctiles + (a.tree ? 1 : 0);
-  const int t_begin = (int)((int64_t)tiles * split / a.n_split);
-  const int t_end = (int)((int64_t)tiles * (split + 1) / a.n_split);
-  const int nt = t_end - t_begin;
-  const int row0 = rb * N;
-  const int rows = std::min(N, a.R - row0);
-  if (nt == 0) {
-    for (int r = threadIdx.x; r < rows; r += S::THREADS)
-      if (a.n_split > 1) a.part_ml[((int64_t)unit * a.R + row0 + r) * a.n_split + split] = make_float2(-INFINITY, 0.f);
-    if (a.n_split == 1)
-      for (int e = threadIdx.x; e < rows * S::DV; e += S::THREADS) {
-        const int r = row0 + e / S::DV;
-        const int64_t o = ((int64_t)b * a.n + r / a.G) * a.H + (int64_t)kvh * a.G + r % a.G;
-        static_cast<uint16_t*>(a.out)[o * S::DV + e % S::DV] = 0;
+  // ---- setup: barriers, tensor memory; then (after the stream's previous kernel) this CTA's run of tiles
+  if (warp == kMma) tc_alloc(&ctl->tslot, S::TMEM);
+  if (warp == kLoad) {
+    if (lane == 0) {
+      prefetch_map(&qmap);
+      prefetch_map(&kmap);
+      tc_mbar_init(&ctl->qfull, 1);
+      tc_mbar_init(&ctl->qempty, 1);
+      tc_mbar_init(&ctl->ofree, S::NG * 4);
+      for (int s = 0; s < S::SLOTS; ++s) {
+        tc_mbar_init(&ctl->full[s], 1);
+        tc_mbar_init(&ctl->empty[s], 1);
       }
-    return;
-  }
-
-  if (warp == S::NG * 4) tc_alloc(&ctl->tslot, S::TMEM);
-  if (threadIdx.x == 0) {
-    tc_mbar_init(&ctl->qfull, 1);
-    for (int s = 0; s < S::NS; ++s) {
-      tc_mbar_init(&ctl->kfull[s], 1);
-      tc_mbar_init(&ctl->kempty[s], 1);
+      for (int s = 0; s < S::ROPE; ++s) {
+        tc_mbar_init(&ctl->rfull[s], 1);
+        tc_mbar_init(&ctl->rempty[s], 1);
+      }
+      for (int s = 0; s < 2; ++s) {
+        tc_mbar_init(&ctl->sfull[s], 1);
+        tc_mbar_init(&ctl->pfull[s], S::NG * 4);
+        tc_mbar_init(&ctl->pvdone[s], 1);
+      }
+      tc_fence_mbar_init();
+      ctl->fail = ctl->q_loads = ctl->chunks = ctl->ropes = ctl->scores = ctl->values = 0;
     }
-    for (int s = 0; s < 2; ++s) {
-      tc_mbar_init(&ctl->sfull[s], 1);
-      tc_mbar_init(&ctl->pfull[s], S::NG * 4);
-      tc_mbar_init(&ctl->pvdone[s], 1);
+    pdl_wait_and_trigger();
+    const int per = a.Hkv * a.row_blocks;
+    int64_t total = 0;
+    for (int b = lane; b < a.B; b += 32) total += entry_tiles<KT>(a, b);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    total *= per;
+    const int64_t runs = std::min<int64_t>(gridDim.x, total);   // none of them empty
+    const int64_t run0 = blockIdx.x < runs ? total * blockIdx.x / runs : 0;
+    const int64_t run1 = blockIdx.x < runs ? total * (blockIdx.x + 1) / runs : 0;
+    // the entry that holds tile run0
+    int64_t base = 0;
+    int b0 = 0;
+    for (int c = 0; c < a.B && run0 < run1; c += 32) {
+      const int64_t mine = c + lane < a.B ? (int64_t)entry_tiles<KT>(a, c + lane) * per : 0;
+      int64_t upto = mine;                                // inclusive prefix within the 32
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += x;
+      }
+      const unsigned past = __ballot_sync(0xffffffffu, c + lane < a.B && base + upto > run0);
+      if (past) {
+        const int w = __ffs(past) - 1;
+        b0 = c + w;
+        base += __shfl_sync(0xffffffffu, upto - mine, w);
+        break;
+      }
+      base += __shfl_sync(0xffffffffu, upto, 31);
     }
-    tc_fence_mbar_init();
-    ctl->nonfinite = 0;
-    ctl->fail = 0;
-    ctl->loaded = 0;
-    ctl->issued = 0;
+    if (lane == 0) {
+      ctl->run0 = run0;
+      ctl->run1 = run1;
+      ctl->base = base;
+      ctl->b0 = b0;
+    }
+  } else {
+    pdl_wait_and_trigger();
   }
-  if (a.tree && threadIdx.x < a.n) ctl->mask[threadIdx.x] = a.mask[(int64_t)b * a.n + threadIdx.x];
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tbase = ctl->tslot;
   const uint32_t tO = tbase + 2 * N;
   volatile int* fail = &ctl->fail;
+  uint32_t* status = &g_status_rows;
 
-  if (warp >= S::NG * 4) {
+  if (warp >= kLoad) {
     regs_down<S::RO>();
-    if (warp == S::NG * 4) {
+    if (warp == kLoad && lane == 0) {
       // ---------------------------------------------------------------- loads
-      if (lane == 0) {
+      Pieces<KT> p(a, ctl);
+      int g = 0;                                          // tiles loaded by this CTA so far
+      bool ok = true;
+      while (ok && p.next()) {
+        const int kvh = p.u / a.row_blocks, row0 = p.u % a.row_blocks * N;
+        if (p.index > 0) ok = wait_or_fail(&ctl->qempty, (uint32_t)((p.index - 1) & 1), fail, status);
+        if (!ok) break;
         tc_mbar_expect_tx(&ctl->qfull, S::KA * S::QATOM);
         for (int at = 0; at < S::KA; ++at)
           if (S::SHARED)
-            tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, row0, b, 0, &ctl->qfull);
+            tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, row0, p.b, 0, &ctl->qfull);
           else
-            tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, kvh * a.G, row0 / a.G, b, &ctl->qfull);
-        for (int t = 0; t < nt; ++t) {
-          const int s = t % S::NS, u = t / S::NS;
-          if (u > 0 && !wait_or_fail(&ctl->kempty[s], (uint32_t)((u - 1) & 1), fail, &g_status_rows)) break;
-          const bool tr = t_begin + t >= ctiles;
-          const int key = tr ? 0 : (t_begin + t) * KT;
-          uint8_t* dst = sm + S::KV_OFF + s * S::STAGE;
-          tc_mbar_expect_tx(&ctl->kfull[s], S::STAGE);
-          for (int at = 0; at < S::KA; ++at)
-            tma_load_4d(dst + at * S::ATOM, tr ? &ktmap : &kmap, at * 64, key, S::SHARED ? b : kvh, S::SHARED ? 0 : b,
-                        &ctl->kfull[s]);
-          if (!S::SHARED)
-            for (int at = 0; at < S::VA; ++at)
-              tma_load_4d(dst + S::V_OFF + at * S::ATOM, tr ? &vtmap : &vmap, at * 64, key, kvh, b, &ctl->kfull[s]);
-          ctl->loaded = t + 1;
+            tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, kvh * a.G, row0 >> a.log_g, p.b, &ctl->qfull);
+        ctl->q_loads = p.index + 1;
+        for (int t = p.t0; ok && t < p.t1; ++t, ++g) {
+          const bool tr = a.tree && t == p.tiles - 1;
+          const int key = tr ? 0 : t * KT;
+          const CUtensorMap* km = tr ? &ktmap : &kmap;
+          const CUtensorMap* vm = tr ? &vtmap : &vmap;
+#pragma unroll
+          for (int j = 0; j < CH; ++j) {
+            const int c = g * CH + j, s = c % S::SLOTS, w = c / S::SLOTS;
+            if (w > 0 && !wait_or_fail(&ctl->empty[s], (uint32_t)((w - 1) & 1), fail, status)) {
+              ok = false;
+              break;
+            }
+            uint8_t* dst = sm + S::KV_OFF + s * S::SLOT;
+            tc_mbar_expect_tx(&ctl->full[s], S::SLOT);
+            for (int x = 0; x < S::SLOT / S::ATOM; ++x)
+              if (S::SHARED)
+                tma_load_4d(dst + x * S::ATOM, km, (j * (S::MV / 64) + x) * 64, key, p.b, 0, &ctl->full[s]);
+              else
+                tma_load_4d(dst + x * S::ATOM, j == 0 ? km : vm, x * 64, key, kvh, p.b, &ctl->full[s]);
+            ctl->chunks = c + 1;
+          }
+          if constexpr (S::SHARED) {
+            if (!ok) break;
+            const int s = g % S::ROPE, w = g / S::ROPE;
+            ok = w == 0 || wait_or_fail(&ctl->rempty[s], (uint32_t)((w - 1) & 1), fail, status);
+            if (!ok) break;
+            tc_mbar_expect_tx(&ctl->rfull[s], S::ATOM);
+            tma_load_4d(sm + S::R_OFF + s * S::ATOM, km, S::VA * 64, key, p.b, 0, &ctl->rfull[s]);
+            ctl->ropes = g + 1;
+          }
         }
       }
-    } else if (warp == S::NG * 4 + 1) {
+    } else if (warp == kMma && lane == 0) {
       // ---------------------------------------------------------------- products
-      if (lane == 0) {
-        constexpr uint32_t idS = tc_idesc(S::BF16, KT, N, false, false);
-        constexpr uint32_t idO = tc_idesc(S::BF16, S::MV, N, true, true);
-        const Desc qd = tc_desc_sw128(smem_addr(sm + S::Q_OFF));
-        const Desc kd = tc_desc_sw128(smem_addr(sm + S::KV_OFF));
-        const Desc vd = tc_desc_mn<64>(smem_addr(sm + S::KV_OFF + S::V_OFF), S::ATOM);
-        const Desc pd = tc_desc_mn<S::PW>(smem_addr(sm + S::P_OFF), KT * S::PW * 2);
-        auto scores = [&](int t) {        // S^T of tile t
-          const int s = t % S::NS;
-          if (!wait_or_fail(&ctl->kfull[s], (uint32_t)((t / S::NS) & 1), fail, &g_status_rows)) return false;
-          tc_fence_after();
-          const Desc ks = kd.at(s * S::STAGE).opaque(), qs = qd.opaque();
-  #pragma unroll
-          for (int kk = 0; kk < S::KA * 4; ++kk)
-            tc_mma_ss(tbase + (uint32_t)((t & 1) * N), ks.at((kk >> 2) * S::ATOM + (kk & 3) * 32),
-                      qs.at((kk >> 2) * S::QATOM + (kk & 3) * 32), idS, kk > 0 ? 1u : 0u);
-          tc_commit(&ctl->sfull[t & 1]);
-          return true;
-        };
-        bool ok = wait_or_fail(&ctl->qfull, 0, fail, &g_status_rows) && scores(0);
-        for (int t = 0; ok && t < nt; ++t) {
-          if (t + 1 < nt && !scores(t + 1)) break;
-          const int s = t % S::NS, pb = t % S::NP;
-          if (!wait_or_fail(&ctl->pfull[pb], (uint32_t)((t / S::NP) & 1), fail, &g_status_rows)) break;
-          tc_fence_after();
-          const Desc vs = vd.at(s * S::STAGE).opaque(), ps = pd.at(pb * S::PBUF).opaque();
-  #pragma unroll
-          for (int mb = 0; mb < S::NB; ++mb)
-  #pragma unroll
-            for (int kk = 0; kk < KT / 16; ++kk)
-              tc_mma_ss(tO + (uint32_t)(mb * N), vs.at(mb * (S::MV / 64) * S::ATOM + kk * 2048),
-                        ps.at(kk * 16 * S::PW * 2), idO, t > 0 || kk > 0 ? 1u : 0u);
-          tc_commit(&ctl->kempty[s]);
-          tc_commit(&ctl->pvdone[pb]);
-          ctl->issued = t + 1;
+      constexpr uint32_t idS = tc_idesc(S::BF16, KT, N, false, false);
+      constexpr uint32_t idO = tc_idesc(S::BF16, S::MV, N, true, true);
+      const Desc qd = tc_desc_sw128(smem_addr(sm + S::Q_OFF));
+      const Desc kd = tc_desc_sw128(smem_addr(sm + S::KV_OFF));
+      const Desc rd = tc_desc_sw128(smem_addr(sm + S::R_OFF));
+      const Desc vd = tc_desc_mn<64>(smem_addr(sm + S::KV_OFF), S::ATOM);
+      const Desc pd = tc_desc_mn<S::PW>(smem_addr(sm + S::P_OFF), KT * S::PW * 2);
+      Pieces<KT> p(a, ctl);
+      int g0 = 0;                                         // tiles of the earlier pieces
+      bool ok = true;
+      while (ok && p.next()) {
+        const int nt = p.t1 - p.t0;
+        ok = wait_or_fail(&ctl->qfull, (uint32_t)(p.index & 1), fail, status);
+        int ts = 0, js = 0, tv = 0;                       // next scores (tile, step), next second product
+        // steps of a tile's scores: its ring chunks that hold keys, then (SHARED) the last key atom
+        constexpr int kSteps = S::SHARED ? CH + 1 : 1;
+        uint64_t since = 0;                               // when it last found nothing ready
+        int idle = 0;
+        while (ok && tv < nt) {
+          const int gs = g0 + ts, gv = g0 + tv;
+          bool ready = tv < ts && mbar_test(&ctl->pfull[gv % S::NP], (uint32_t)((gv / S::NP) & 1));
+          if (!S::SHARED && ready) {
+            const int c = gv * CH + 1;
+            ready = mbar_test(&ctl->full[c % S::SLOTS], (uint32_t)((c / S::SLOTS) & 1));
+          }
+          if (ready) {
+            if (tv == 0 && p.index > 0)                   // the previous piece's outputs have been read
+              ok = wait_or_fail(&ctl->ofree, (uint32_t)((p.index - 1) & 1), fail, status);
+            if (!ok) break;
+            tc_fence_after();
+            const Desc ps = pd.at(gv % S::NP * S::PBUF).opaque();
+#pragma unroll
+            for (int mb = 0; mb < S::NB; ++mb) {
+              const int s = (gv * CH + (S::SHARED ? mb : 1)) % S::SLOTS;
+              const Desc vs = vd.at(s * S::SLOT).opaque();
+#pragma unroll
+              for (int kk = 0; kk < KT / 16; ++kk)
+                tc_mma_ss(tO + (uint32_t)(mb * N), vs.at(kk * 2048), ps.at(kk * 16 * S::PW * 2), idO,
+                          tv > 0 || kk > 0 ? 1u : 0u);
+              tc_commit(&ctl->empty[s]);
+            }
+            tc_commit(&ctl->pvdone[gv % S::NP]);
+            ctl->values = gv + 1;
+            ++tv;
+            idle = 0;
+            continue;
+          }
+          if (ts < nt && ts <= tv + 1) {                  // S^T buffer gs & 1 has been read (tile ts - 2 is past its softmax)
+            const bool rope = S::SHARED && js == CH;
+            const int c = gs * CH + js, s = c % S::SLOTS, r = S::SHARED ? gs % S::ROPE : 0;
+            if (rope ? mbar_test(&ctl->rfull[r], (uint32_t)((gs / (S::SHARED ? S::ROPE : 1)) & 1))
+                     : mbar_test(&ctl->full[s], (uint32_t)((c / S::SLOTS) & 1))) {
+              tc_fence_after();
+              const uint32_t d = tbase + (uint32_t)((gs & 1) * N);
+              if (rope) {
+                const Desc ks = rd.at(r * S::ATOM).opaque(), qs = qd.at(S::VA * S::QATOM).opaque();
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) tc_mma_ss(d, ks.at(kk * 32), qs.at(kk * 32), idS, 1u);
+                tc_commit(&ctl->rempty[r]);
+              } else {
+                constexpr int kAtoms = S::SLOT / S::ATOM;
+                const Desc ks = kd.at(s * S::SLOT).opaque(), qs = qd.at(js * kAtoms * S::QATOM).opaque();
+#pragma unroll
+                for (int kk = 0; kk < kAtoms * 4; ++kk)
+                  tc_mma_ss(d, ks.at((kk >> 2) * S::ATOM + (kk & 3) * 32), qs.at((kk >> 2) * S::QATOM + (kk & 3) * 32),
+                            idS, js > 0 || kk > 0 ? 1u : 0u);
+                if (!S::SHARED) tc_commit(&ctl->empty[s]);
+              }
+              if (++js == kSteps) {
+                tc_commit(&ctl->sfull[gs & 1]);
+                js = 0;
+                ++ts;
+                ctl->scores = gs + 1;
+                if (ts == nt) tc_commit(&ctl->qempty);
+              }
+              idle = 0;
+              continue;
+            }
+          }
+          // nothing is ready: a bounded wait for either, its clock read now and then
+          if ((++idle & 63) == 0) {
+            const uint64_t now = globaltimer_ns();
+            if (idle == 64) since = now;
+            if (now - since > kRoleWaitNs) {
+              *fail = 1;
+              atomicOr(status, MKV_FLAG_WAIT_TIMEOUT);
+            }
+            ok = *fail == 0;
+            if (idle > (1 << 30)) idle = 128;
+          }
         }
+        g0 += nt;
       }
     }
   } else {
     regs_up<S::RS>();
     // ---------------------------------------------------------------- softmax
+    float* red = reinterpret_cast<float*>(sm + S::RED_OFF);
+    uint32_t* vis = reinterpret_cast<uint32_t*>(sm + S::VIS_OFF);
     const int q = warp & 3, grp = warp >> 2;             // lane quarter (keys), rows grp C .. + C - 1
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
     // a tile of 64 keys takes lanes 0..15 of each quarter, one of 128 all of them
     const bool live = KT == 128 || lane < 16;
     const int key = KT == 128 ? q * 32 + lane : q * 16 + (lane & 15);
-    float m[C], l[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      m[c] = kNoMax;
-      l[c] = 0.f;
-    }
-    // A warp whose wait ran out stops waiting but still meets its group's barriers, so none is left waiting.
+    // A warp whose wait ran out stops waiting but still meets the barriers, so none is left waiting.
     bool dead = false;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (!dead) dead = !__all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, &g_status_rows));
+      if (!dead) dead = !__all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status));
       tc_fence_after();
     };
-    for (int t = 0; t < nt; ++t) {
-      const int s = t % S::NS, pb = t % S::NP;
-      const bool tr = t_begin + t >= ctiles;
-      const int valid = tr ? a.n : std::min(KT, len - (t_begin + t) * KT);   // keys of the tile that exist
-      wait(&ctl->sfull[t & 1], (uint32_t)((t >> 1) & 1));
-      float v[C];
-      tm_load<C>(tbase + lanes + (uint32_t)((t & 1) * N + grp * C), v);
-      const bool exists = live && key < valid;
-      bool over = false;
-      if (tr) {
+    Pieces<KT> p(a, ctl);
+    int g = 0;                                            // tiles met by this CTA so far
+    while (p.next()) {
+      const int nt = p.t1 - p.t0, kvh = p.u / a.row_blocks, row0 = p.u % a.row_blocks * N;
+      const int rows = std::min(N, a.R - row0);
+      const bool has_tree = a.tree && p.t1 == p.tiles;
+      if (has_tree) {                                     // for every drafted token, the rows that see it
+        bar_sync(5, S::SOFT);                             // (the previous piece's reads are done)
+        if (threadIdx.x == 0) ctl->nonfinite = 0;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int tok = (row0 + grp * C + c) / a.G;
-          const bool see = exists && tok < a.n && (ctl->mask[tok] >> key & 1);
-          v[c] = see ? v[c] * a.scale_log2 : -INFINITY;
-          over |= v[c] > m[c] + kRaise;
+        for (int w = 0; w < S::VW; ++w) {
+          const int r = w * 32 + lane, tok = (row0 + r) / a.G;
+          const uint64_t bits = r < rows ? a.mask[(int64_t)p.b * a.n + tok] : 0;
+          for (int j = warp; j < a.n; j += S::SOFT / 32) {
+            const unsigned word = __ballot_sync(0xffffffffu, (bits >> j & 1) != 0);
+            if (lane == 0) vis[j * S::VW + w] = word;
+          }
         }
-      } else {
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          v[c] = exists ? v[c] * a.scale_log2 : -INFINITY;
-          over |= v[c] > m[c] + kRaise;
-        }
+        bar_sync(5, S::SOFT);
       }
-      if (bar_or(1 + grp, 128, over)) {
-        // some score passed its row's maximum: raise the maxima to the tile's, rescale sums and outputs
-        float w[C];
+      float m[C], l[C];
 #pragma unroll
-        for (int c = 0; c < C; ++c) w[c] = v[c];
-        reduce_columns<C>(w, lane, [](float x, float y) { return fmaxf(x, y); });
-        if ((lane & (32 / C - 1)) == 0) red[q * N + grp * C + lane / (32 / C)] = w[0];
-        bar_sync(1 + grp, 128);
+      for (int c = 0; c < C; ++c) {
+        m[c] = kNoMax;
+        l[c] = 0.f;
+      }
+      for (int t = 0; t < nt; ++t, ++g) {
+        const int pb = g % S::NP;
+        const bool tr = has_tree && t == nt - 1;
+        const int valid = tr ? a.n : std::min(KT, p.len - (p.t0 + t) * KT);   // keys of the tile that exist
+        wait(&ctl->sfull[g & 1], (uint32_t)((g >> 1) & 1));
+        float v[C];
+        tm_load<C>(tbase + lanes + (uint32_t)((g & 1) * N + grp * C), v);
+        const bool exists = live && key < valid;
+        // the rows of this thread that see its key
+        uint32_t see = exists ? 0xffffffffu : 0u;
+        if (tr && exists) see = vis[key * S::VW + grp * C / 32] >> (grp * C % 32);
+        bool over = false;
+        if (valid == KT && !tr && KT == 128) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int x = grp * C + c;
-          const float mx = fmaxf(fmaxf(red[x], red[N + x]), fmaxf(red[2 * N + x], red[3 * N + x]));
-          const float nm = fmaxf(m[c], mx);
-          w[c] = ex2_approx(m[c] - nm);
-          m[c] = nm;
-          l[c] *= w[c];
+          for (int c = 0; c < C; ++c) {
+            v[c] *= a.scale_log2;
+            over |= v[c] > m[c] + kRaise;
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            v[c] = see >> c & 1 ? v[c] * a.scale_log2 : -INFINITY;
+            over |= v[c] > m[c] + kRaise;
+          }
         }
-        if (t > 0) {
-          wait(&ctl->pvdone[(t - 1) % S::NP], (uint32_t)(((t - 1) / S::NP) & 1));
+        if (bar_or(1 + grp, 128, over)) {
+          // some score passed its row's maximum: raise the maxima to the tile's, rescale sums and outputs
+          float w[C];
+#pragma unroll
+          for (int c = 0; c < C; ++c) w[c] = v[c];
+          reduce_columns<C>(w, lane, [](float x, float y) { return fmaxf(x, y); });
+          if ((lane & (32 / C - 1)) == 0) red[q * N + grp * C + lane / (32 / C)] = w[0];
+          bar_sync(1 + grp, 128);
+          const float4* r4 = reinterpret_cast<const float4*>(red + grp * C);
+#pragma unroll
+          for (int c = 0; c < C / 4; ++c) {
+            const float4 x0 = r4[c], x1 = r4[N / 4 + c], x2 = r4[2 * N / 4 + c], x3 = r4[3 * N / 4 + c];
+            const float mx[4] = {fmax3(x0.x, x1.x, fmaxf(x2.x, x3.x)), fmax3(x0.y, x1.y, fmaxf(x2.y, x3.y)),
+                                 fmax3(x0.z, x1.z, fmaxf(x2.z, x3.z)), fmax3(x0.w, x1.w, fmaxf(x2.w, x3.w))};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float nm = fmaxf(m[4 * c + e], mx[e]);
+              w[4 * c + e] = ex2_approx(m[4 * c + e] - nm);
+              m[4 * c + e] = nm;
+              l[4 * c + e] *= w[4 * c + e];
+            }
+          }
+          if (t > 0) {
+            wait(&ctl->pvdone[(g - 1) % S::NP], (uint32_t)(((g - 1) / S::NP) & 1));
 #pragma unroll 1
-          for (int mb = 0; mb < S::NB; ++mb) {
-            float o[C];
-            tm_load<C>(tO + lanes + (uint32_t)(mb * N + grp * C), o);
+            for (int mb = 0; mb < S::NB; ++mb) {
+              float o[C];
+              tm_load<C>(tO + lanes + (uint32_t)(mb * N + grp * C), o);
 #pragma unroll
-            for (int c = 0; c < C; ++c) o[c] *= w[c];
-            tm_store<C>(tO + lanes + (uint32_t)(mb * N + grp * C), o);
-          }
-          tm_store_wait();
-        }
-      }
-      // weights, their sums, and the rounded weights for the second product
-      uint32_t pk[C / 2];
-#pragma unroll
-      for (int c = 0; c < C; c += 2) {
-        const float p0 = ex2_approx(v[c] - m[c] + kOffset), p1 = ex2_approx(v[c + 1] - m[c + 1] + kOffset);
-        l[c] += p0;
-        l[c + 1] += p1;
-        pk[c / 2] = pack2<S::BF16>(p0, p1);
-      }
-      if (t >= S::NP) wait(&ctl->pvdone[pb], (uint32_t)((t / S::NP - 1) & 1));
-      if (live) {
-        const int col = grp * C;
-        uint8_t* pt = sm + S::P_OFF + pb * S::PBUF + (col / S::PW) * (KT * S::PW * 2);
-#pragma unroll
-        for (int i = 0; i < C / 8; ++i)
-          *reinterpret_cast<uint4*>(pt + mn_offset<S::PW>(key, (col % S::PW) / 8 + i)) =
-              make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
-      }
-      // Values that no row may meet must not meet a zero weight either (0 x NaN): slots past the length become
-      // zeros; a drafted token's non-finite values become zeros here and are added to the rows that see it at
-      // the end.  (Latent: the scores of this tile are complete, so its keys may be overwritten.)
-      if (valid < KT && !tr) {
-        uint8_t* vt = sm + S::KV_OFF + s * S::STAGE + S::V_OFF;
-        for (int e = threadIdx.x; e < (KT - valid) * 8 * S::VA; e += S::NG * 128) {
-          const int r = valid + e / (8 * S::VA), x = e % (8 * S::VA);
-          *reinterpret_cast<uint4*>(vt + (x >> 3) * S::ATOM + r * 128 + ((x & 7) << 4)) = make_uint4(0, 0, 0, 0);
-        }
-      }
-      if (tr) {
-        uint8_t* vt = sm + S::KV_OFF + s * S::STAGE + S::V_OFF;
-        for (int e = threadIdx.x; e < valid * 8 * S::VA; e += S::NG * 128) {
-          const int r = e / (8 * S::VA), x = e % (8 * S::VA);
-          uint4* p8 = reinterpret_cast<uint4*>(vt + (x >> 3) * S::ATOM + r * 128 + ((x & 7) << 4));
-          uint4 raw = *p8;
-          if (bad_pairs<S::BF16>(raw)) {
-            *p8 = raw;
-            atomicOr(reinterpret_cast<unsigned long long*>(&ctl->nonfinite), 1ull << r);
+              for (int c = 0; c < C; ++c) o[c] *= w[c];
+              tm_store<C>(tO + lanes + (uint32_t)(mb * N + grp * C), o);
+            }
+            tm_store_wait();
           }
         }
+        // weights, their sums, and the rounded weights for the second product
+        uint32_t pk[C / 2];
+#pragma unroll
+        for (int c = 0; c < C; c += 2) {
+          const float p0 = ex2_approx(v[c] - m[c] + kOffset), p1 = ex2_approx(v[c + 1] - m[c + 1] + kOffset);
+          l[c] += p0;
+          l[c + 1] += p1;
+          pk[c / 2] = pack2<S::BF16>(p0, p1);
+        }
+        if (g >= S::NP) wait(&ctl->pvdone[pb], (uint32_t)((g / S::NP - 1) & 1));
+        if (live) {
+          const int col = grp * C;
+          uint8_t* pt = sm + S::P_OFF + pb * S::PBUF + (col / S::PW) * (KT * S::PW * 2);
+#pragma unroll
+          for (int i = 0; i < C / 8; ++i)
+            *reinterpret_cast<uint4*>(pt + mn_offset<S::PW>(key, (col % S::PW) / 8 + i)) =
+                make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
+        }
+        // Values that no row may meet must not meet a zero weight either (0 x NaN): slots past the length become
+        // zeros; a drafted token's non-finite values become zeros here and are added to the rows that see it at
+        // the end.  (Latent: the scores of this tile are complete, so its keys may be overwritten.)
+        if (tr || valid < KT) {
+          if (!S::SHARED) {
+            const int c = g * CH + 1;
+            wait(&ctl->full[c % S::SLOTS], (uint32_t)((c / S::SLOTS) & 1));
+          }
+          const int r0 = tr ? 0 : valid, r1 = tr ? a.n : KT;
+          for (int e = threadIdx.x; e < (r1 - r0) * 8 * S::VA; e += S::SOFT) {
+            const int r = r0 + e / (8 * S::VA), x = e % (8 * S::VA), at = x >> 3;
+            const int s = (g * CH + (S::SHARED ? at / (S::MV / 64) : 1)) % S::SLOTS;
+            uint4* p8 = reinterpret_cast<uint4*>(sm + S::KV_OFF + s * S::SLOT +
+                                                 (S::SHARED ? at % (S::MV / 64) : at) * S::ATOM +
+                                                 mn_offset<64>(r, x & 7));
+            uint4 raw = make_uint4(0, 0, 0, 0);
+            bool write = !tr;
+            if (tr) {
+              raw = *p8;
+              write = bad_pairs<S::BF16>(raw);
+              if (write) atomicOr(reinterpret_cast<unsigned long long*>(&ctl->nonfinite), 1ull << r);
+            }
+            if (write) *p8 = raw;
+          }
+        }
+        fence_async_smem();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc_mbar_arrive(&ctl->pfull[pb]);
       }
-      fence_async_smem();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) tc_mbar_arrive(&ctl->pfull[pb]);
-    }
-    // ---------------------------------------------------------------- outputs of this run of tiles
-    wait(&ctl->pvdone[(nt - 1) % S::NP], (uint32_t)(((nt - 1) / S::NP) & 1));
-    if (!bar_or(1 + grp, 128, dead)) {                   // (the group's earlier reads of `red` are done)
+      // -------------------------------------------------------------- this piece's outputs
+      wait(&ctl->pvdone[(g - 1) % S::NP], (uint32_t)(((g - 1) / S::NP) & 1));
+      const bool gone = bar_or(1 + grp, 128, dead);        // (the group's earlier reads of `red` are done)
       float w[C];
 #pragma unroll
       for (int c = 0; c < C; ++c) w[c] = live ? l[c] : 0.f;
       reduce_columns<C>(w, lane, [](float x, float y) { return x + y; });
       if ((lane & (32 / C - 1)) == 0) red[q * N + grp * C + lane / (32 / C)] = w[0];
       bar_sync(1 + grp, 128);
+      const float4* r4 = reinterpret_cast<const float4*>(red + grp * C);
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int x = grp * C + c;
-        l[c] = (red[x] + red[N + x]) + (red[2 * N + x] + red[3 * N + x]);
+      for (int c = 0; c < C / 4; ++c) {
+        const float4 x0 = r4[c], x1 = r4[N / 4 + c], x2 = r4[2 * N / 4 + c], x3 = r4[3 * N / 4 + c];
+        l[4 * c] = (x0.x + x1.x) + (x2.x + x3.x);
+        l[4 * c + 1] = (x0.y + x1.y) + (x2.y + x3.y);
+        l[4 * c + 2] = (x0.z + x1.z) + (x2.z + x3.z);
+        l[4 * c + 3] = (x0.w + x1.w) + (x2.w + x3.w);
       }
-      if (a.n_split > 1 && q == 0 && lane == 0) {
+      if (!gone) {
+        const bool whole = nt == p.tiles;
+        const int64_t slot = (int64_t)blockIdx.x * 2 + (p.index > 0 ? 1 : 0);
+        const uint64_t nf = has_tree ? ctl->nonfinite : 0;
+        const bool dlive = S::MV == 128 || lane < 16;
+        const int dl = S::MV == 128 ? q * 32 + lane : q * 16 + (lane & 15);
+        if (!whole && q == 0 && lane == 0) {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (grp * C + c < rows)
-            a.part_ml[((int64_t)unit * a.R + row0 + grp * C + c) * a.n_split + split] =
-                make_float2(l[c] == 0.f ? -INFINITY : m[c], l[c]);
-      }
-      const uint64_t nf = ctl->nonfinite;
-      const bool dlive = S::MV == 128 || lane < 16;
+          for (int c = 0; c < C; ++c)
+            a.part_ml[slot * N + grp * C + c] = make_float2(l[c] == 0.f ? -INFINITY : m[c], l[c]);
+        }
+        if (whole) {
+#pragma unroll
+          for (int c = 0; c < C; ++c) l[c] = l[c] == 0.f ? 0.f : 1.f / l[c];
+        }
 #pragma unroll 1
-      for (int mb = 0; mb < S::NB; ++mb) {
-        const int d = mb * S::MV + (S::MV == 128 ? q * 32 + lane : q * 16 + (lane & 15));
-        float o[C];
-        tm_load<C>(tO + lanes + (uint32_t)(mb * N + grp * C), o);
+        for (int mb = 0; mb < S::NB; ++mb) {
+          const int d = mb * S::MV + dl;
+          float o[C];
+          tm_load<C>(tO + lanes + (uint32_t)(mb * N + grp * C), o);
+          if (nf != 0) {                                   // the non-finite values that a row sees
+            for (int c = 0; c < C; ++c) {
+              const int r = grp * C + c;
+              if (r >= rows) break;
+              float add = 0.f;
+              for (uint64_t bits = nf & a.mask[(int64_t)p.b * a.n + (row0 + r) / a.G]; bits; bits &= bits - 1) {
+                const int j = __ffsll((long long)bits) - 1;
+                const uint16_t y = j < a.n ? a.v_tree[((int64_t)p.b * a.n + j) * a.v_tok + kvh * a.v_head + d] : 0;
+                if (non_finite<S::BF16>(y)) add += widen<S::BF16>(y);
+              }
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int r = grp * C + c;
-          if (r >= rows || !dlive) continue;
-          const int tok = (row0 + r) / a.G, g = (row0 + r) % a.G;
-          float x = o[c];
-          if (nf != 0) {                                 // the non-finite values that this row sees
-            for (uint64_t bits = nf & ctl->mask[tok]; bits; bits &= bits - 1) {
-              const int j = __ffsll((long long)bits) - 1;
-              const uint16_t y = a.v_tree[((int64_t)b * a.n + j) * a.v_tok + kvh * a.v_head + d];
-              if (non_finite<S::BF16>(y)) x += widen<S::BF16>(y);
+              for (int e = 0; e < C; ++e) o[e] += e == c ? add : 0.f;
             }
           }
-          if (a.n_split > 1) {
-            a.part_o[(((int64_t)unit * a.R + row0 + r) * a.n_split + split) * S::DV + d] = x;
+          if (!whole) {
+            float* po = a.part_o + (slot * N + grp * C) * S::DV + d;
+            if (dlive) {
+#pragma unroll
+              for (int c = 0; c < C; ++c)
+                if (grp * C + c < rows) po[c * S::DV] = o[c];
+            }
           } else {
-            const int64_t at = (((int64_t)b * a.n + tok) * a.H + (int64_t)kvh * a.G + g) * S::DV + d;
-            static_cast<uint16_t*>(a.out)[at] = (uint16_t)pack2<S::BF16>(l[c] == 0.f ? 0.f : x / l[c], 0.f);
+            // neighbouring lanes swap, so that each stores two dims of one row of a pair
+            const bool odd = lane & 1;
+#pragma unroll
+            for (int c = 0; c < C; c += 2) {
+              const float x0 = l[c] == 0.f ? 0.f : o[c] * l[c], x1 = l[c + 1] == 0.f ? 0.f : o[c + 1] * l[c + 1];
+              const float y = __shfl_xor_sync(0xffffffffu, odd ? x0 : x1, 1);
+              const uint32_t h = odd ? pack2<S::BF16>(y, x1) : pack2<S::BF16>(x0, y);
+              const int r = grp * C + c + (odd ? 1 : 0), row = row0 + r;
+              const int64_t at = S::SHARED ? (int64_t)p.b * a.R + row
+                                           : ((int64_t)p.b * a.n + (row >> a.log_g)) * a.H + kvh * a.G + (row & (a.G - 1));
+              if (r < rows && dlive) *reinterpret_cast<uint32_t*>(a.out + at * S::DV + (d & ~1)) = h;
+            }
           }
         }
       }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc_mbar_arrive(&ctl->ofree);
     }
   }
   // teardown: on a failure wait (bounded) for the copies and products already issued
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && ctl->fail) {
-    tc_mbar_wait(&ctl->qfull, 0, kRoleWaitNs);
-    for (int t = std::max(0, ctl->loaded - S::NS); t < ctl->loaded; ++t)
-      tc_mbar_wait(&ctl->kfull[t % S::NS], (uint32_t)((t / S::NS) & 1), kRoleWaitNs);
-    if (ctl->issued > 0) {
-      const int t = ctl->issued - 1;
-      tc_mbar_wait(&ctl->pvdone[t % S::NP], (uint32_t)((t / S::NP) & 1), kRoleWaitNs);
-    }
+    if (ctl->q_loads > 0) tc_mbar_wait(&ctl->qfull, (uint32_t)((ctl->q_loads - 1) & 1), kRoleWaitNs);
+    for (int c = std::max(0, ctl->chunks - S::SLOTS); c < ctl->chunks; ++c)
+      tc_mbar_wait(&ctl->full[c % S::SLOTS], (uint32_t)((c / S::SLOTS) & 1), kRoleWaitNs);
+    for (int c = std::max(0, ctl->ropes - S::ROPE); S::SHARED && c < ctl->ropes; ++c)
+      tc_mbar_wait(&ctl->rfull[c % std::max(1, S::ROPE)], (uint32_t)((c / std::max(1, S::ROPE)) & 1), kRoleWaitNs);
+    if (ctl->scores > 0)
+      tc_mbar_wait(&ctl->sfull[(ctl->scores - 1) & 1], (uint32_t)(((ctl->scores - 1) >> 1) & 1), kRoleWaitNs);
+    if (ctl->values > 0)
+      tc_mbar_wait(&ctl->pvdone[(ctl->values - 1) % S::NP], (uint32_t)(((ctl->values - 1) / S::NP) & 1), kRoleWaitNs);
   }
   __syncthreads();
   tc_fence_after();
-  if (warp == S::NG * 4) tc_dealloc(tbase, S::TMEM);
+  if (warp == kMma) tc_dealloc(tbase, S::TMEM);
 }
 
-// out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over the splits of one row.  A thread takes four dims.
-template <bool BF16>
-__global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int DV) {
+// The units that several runs share: out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over their pieces; zeros for
+// the units of an entry without any token.  DV / 4 threads a row, each four dims.
+template <bool BF16, int KT, int DV>
+__global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N, int ctas) {
   pdl_wait_and_trigger();
-  const int64_t row = blockIdx.x;                        // unit R + r
-  const int64_t unit = row / a.R;
-  const int r = (int)(row % a.R), b = (int)(unit / a.Hkv), kvh = (int)(unit % a.Hkv);
-  const float2* ml = a.part_ml + row * a.n_split;
-  float M = -INFINITY;
-  for (int s = 0; s < a.n_split; ++s) M = fmaxf(M, ml[s].x);
-  const int64_t at = (((int64_t)b * a.n + r / a.G) * a.H + (int64_t)kvh * a.G + r % a.G) * DV;
-  for (int d = threadIdx.x * 4; d < DV; d += 512) {
-    float L = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < a.n_split; ++s) {
-      const float2 x = ml[s];
-      if (x.x == -INFINITY) continue;                    // nothing seen: its output was not written
-      const float w = ex2_approx(x.x - M);
-      const float4 y = *reinterpret_cast<const float4*>(a.part_o + (row * a.n_split + s) * DV + d);
-      L += w * x.y;
-      o.x += w * y.x;
-      o.y += w * y.y;
-      o.z += w * y.z;
-      o.w += w * y.w;
-    }
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    uint2 h;
-    h.x = pack2<BF16>(o.x * inv, o.y * inv);
-    h.y = pack2<BF16>(o.z * inv, o.w * inv);
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at + d) = h;
+  constexpr int kPer = 512 / DV;                         // rows a CTA
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * kPer + threadIdx.x / (DV / 4);   // (b Hkv + kvh) R + r
+  const bool live = row < (int64_t)a.B * a.Hkv * a.R;
+  const int64_t bh = (live ? row : 0) / a.R;
+  const int r = (int)((live ? row : 0) % a.R), b = (int)(bh / a.Hkv), kvh = (int)(bh % a.Hkv), d = threadIdx.x % (DV / 4) * 4;
+  // tiles before entry b, and of all entries (rows of one warp may be of different entries: summed per thread group)
+  const int per = a.Hkv * a.row_blocks;
+  int64_t before = 0, total = 0;
+  constexpr int kGrp = DV / 4 < 32 ? DV / 4 : 32;        // threads of a row within a warp
+  for (int e = lane % kGrp; e < a.B; e += kGrp) {
+    const int x = entry_tiles<KT>(a, e);
+    total += x;
+    before += e < b ? x : 0;
   }
+#pragma unroll
+  for (int k = kGrp / 2; k; k >>= 1) {
+    total += __shfl_xor_sync(0xffffffffu, total, k);
+    before += __shfl_xor_sync(0xffffffffu, before, k);
+  }
+  if (!live) return;
+  const int tiles = entry_tiles<KT>(a, b);
+  const int64_t at = (a.log_g < 0 ? row : ((int64_t)b * a.n + (r >> a.log_g)) * a.H + kvh * a.G + (r & (a.G - 1))) * DV + d;
+  if (tiles == 0) {
+    *reinterpret_cast<uint2*>(a.out + at) = make_uint2(0, 0);
+    return;
+  }
+  total *= per;
+  const int64_t runs = std::min<int64_t>(ctas, total);
+  const int64_t u0 = before * per + (int64_t)(kvh * a.row_blocks + r / N) * tiles;   // the unit's first tile
+  const int64_t c0 = cta_of_chunk(u0, total, runs), c1 = cta_of_chunk(u0 + tiles - 1, total, runs);
+  if (c0 == c1) return;                                  // one run held the whole unit
+  const int64_t first = c0 * 2 + (total * c0 / runs < u0 ? 1 : 0);   // its first piece: not the first of its run?
+  float M = -INFINITY;
+  for (int64_t c = c0; c <= c1; ++c) M = fmaxf(M, a.part_ml[(c == c0 ? first : c * 2) * N + r % N].x);
+  float L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int64_t c = c0; c <= c1; ++c) {
+    const int64_t s = (c == c0 ? first : c * 2) * N + r % N;
+    const float2 x = a.part_ml[s];
+    const float4 y = *reinterpret_cast<const float4*>(a.part_o + s * DV + d);
+    const float w = x.x == -INFINITY ? 0.f : ex2_approx(x.x - M);
+    L += w * x.y;
+    o.x += w * y.x;
+    o.y += w * y.y;
+    o.z += w * y.z;
+    o.w += w * y.w;
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  uint2 h;
+  h.x = pack2<BF16>(inv == 0.f ? 0.f : o.x * inv, inv == 0.f ? 0.f : o.y * inv);
+  h.y = pack2<BF16>(inv == 0.f ? 0.f : o.z * inv, inv == 0.f ? 0.f : o.w * inv);
+  *reinterpret_cast<uint2*>(a.out + at) = h;
 }
 
 // ---------------------------------------------------------------- host side
 struct Plan {
-  int N, KT, R, row_blocks, n_split;
+  int N, KT, R, row_blocks, ctas;
   size_t ml_off, o_off, bytes;
 };
 
 Plan plan_rows(const RowsCall& c) {
   Plan p{};
   p.R = c.n * (c.H / c.Hkv);
-  p.N = 64;
+  p.N = p.R <= 16 ? 16 : p.R <= 32 ? 32 : 64;
   p.KT = c.latent ? 64 : 128;
   p.row_blocks = (int)ceil_div(p.R, p.N);
-  // the run length that leaves the busiest SM least to do; a run costs a few tiles' time by itself
-  const int64_t tiles = ceil_div(c.T_cap, p.KT) + 1, blocks = (int64_t)c.B * c.Hkv * p.row_blocks;
-  int64_t best = 1, cost = INT64_MAX;
-  for (int64_t n = 1; n <= std::min<int64_t>(tiles, kNumSMs); ++n) {
-    const int64_t x = ceil_div(blocks * n, kNumSMs) * (ceil_div(tiles, n) + 4);
-    if (x < cost) {
-      cost = x;
-      best = n;
-    }
-  }
-  p.n_split = (int)best;
-  const size_t parts = (size_t)c.B * c.Hkv * p.R * p.n_split;
+  const int64_t tiles = (ceil_div(c.T_cap, p.KT) + 1) * c.B * c.Hkv * p.row_blocks;
+  p.ctas = (int)std::min<int64_t>(tiles, kNumSMs);
+  const size_t parts = (size_t)p.ctas * 2 * p.N;
   p.ml_off = kCounterBytes;
   p.o_off = p.ml_off + align256(parts * sizeof(float2));
-  p.bytes = p.n_split > 1 ? p.o_off + align256(parts * c.dv * sizeof(float)) : kCounterBytes;
+  p.bytes = p.o_off + align256(parts * c.dv * sizeof(float));
   return p;
 }
 
@@ -508,17 +743,30 @@ cudaError_t launch_shape(const RowsCall& c, const Plan& p, RowsArgs a, cudaStrea
   constexpr int smem = std::max(S::ALLOC, 116 * 1024);
   e = cudaFuncSetAttribute(rows_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  rows_kernel<S><<<dim3(p.n_split, p.row_blocks, (unsigned)(B * Hkv)), S::THREADS, smem, st>>>(qm, km, vm, ktm, vtm, a);
-  e = cudaPeekAtLastError();
-  if (e != cudaSuccess || p.n_split == 1) return e;
-  return launch_pdl(join_kernel<S::BF16>, dim3((unsigned)(B * Hkv * p.R)), dim3(std::min(128, S::DV / 4)), 0, st, a,
-                    (int)S::DV);
+  e = launch_pdl(rows_kernel<S>, dim3(p.ctas), dim3(S::THREADS), smem, st, qm, km, vm, ktm, vtm, a);
+  if (e != cudaSuccess) return e;
+  const unsigned grid = (unsigned)ceil_div(B * Hkv * p.R, 512 / S::DV);
+  return launch_pdl(join_kernel<S::BF16, S::KT, S::DV>, dim3(grid), dim3(128), 0, st, a, (int)S::N, p.ctas);
 }
 
+// rows a block, ring slots, last-key-atom slots, weight buffers: what an SM's shared memory holds
 template <bool BF16>
 cudaError_t launch_latent(const RowsCall& c, const Plan& p, const RowsArgs& a, cudaStream_t st) {
-  if (c.dv == 512) return launch_shape<Shape<BF16, 9, 8, true, 64, 64, 2, 1>>(c, p, a, st);
-  return launch_shape<Shape<BF16, 5, 4, true, 64, 64, 3, 2>>(c, p, a, st);
+  if (c.dv == 512) {
+    if (p.N == 16) return launch_shape<Shape<BF16, 9, 8, true, 64, 16, 10, 3, 2>>(c, p, a, st);
+    if (p.N == 32) return launch_shape<Shape<BF16, 9, 8, true, 64, 32, 9, 3, 2>>(c, p, a, st);
+    return launch_shape<Shape<BF16, 9, 8, true, 64, 64, 8, 2, 1>>(c, p, a, st);
+  }
+  if (p.N == 16) return launch_shape<Shape<BF16, 5, 4, true, 64, 16, 10, 4, 2>>(c, p, a, st);
+  if (p.N == 32) return launch_shape<Shape<BF16, 5, 4, true, 64, 32, 9, 4, 2>>(c, p, a, st);
+  return launch_shape<Shape<BF16, 5, 4, true, 64, 64, 8, 4, 2>>(c, p, a, st);
+}
+
+template <int KA, int SL>
+cudaError_t launch_tree(const RowsCall& c, const Plan& p, const RowsArgs& a, cudaStream_t st) {
+  if (p.N == 16) return launch_shape<Shape<false, KA, KA, false, 128, 16, SL, 0, 2>>(c, p, a, st);
+  if (p.N == 32) return launch_shape<Shape<false, KA, KA, false, 128, 32, SL, 0, 2>>(c, p, a, st);
+  return launch_shape<Shape<false, KA, KA, false, 128, 64, KA == 2 ? 5 : SL, 0, 2>>(c, p, a, st);
 }
 
 }  // namespace
@@ -534,7 +782,10 @@ cudaError_t launch_rows_attention(const RowsCall& c, void* ws, cudaStream_t st) 
   a.Hkv = c.Hkv;
   a.G = c.H / c.Hkv;
   a.R = p.R;
-  a.n_split = p.n_split;
+  a.row_blocks = p.row_blocks;
+  a.log_g = -1;
+  if (!c.latent)
+    for (a.log_g = 0; (1 << a.log_g) < a.G;) ++a.log_g;
   a.tree = c.k_tree != nullptr;
   a.T_cap = c.T_cap;
   a.scale_log2 = c.scale * kLog2e;
@@ -543,12 +794,11 @@ cudaError_t launch_rows_attention(const RowsCall& c, void* ws, cudaStream_t st) 
   a.v_tree = static_cast<const uint16_t*>(c.latent ? c.k_tree : c.v_tree);
   a.v_tok = c.latent ? c.dk : (int64_t)c.Hkv * c.dv;
   a.v_head = c.latent ? 0 : c.dv;
-  a.out = c.out;
+  a.out = static_cast<uint16_t*>(c.out);
   a.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + p.ml_off);
   a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.o_off);
   if (c.latent) return c.dtype == MKV_BF16 ? launch_latent<true>(c, p, a, st) : launch_latent<false>(c, p, a, st);
-  if (c.dv == 128) return launch_shape<Shape<false, 2, 2, false, 128, 64, 2, 2>>(c, p, a, st);
-  return launch_shape<Shape<false, 1, 1, false, 128, 64, 3, 2>>(c, p, a, st);
+  return c.dv == 128 ? launch_tree<2, 6>(c, p, a, st) : launch_tree<1, 10>(c, p, a, st);
 }
 
 }  // namespace mkv
