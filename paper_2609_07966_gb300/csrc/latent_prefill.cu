@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
     regs_down<kPRegsOther>();
     if (warp == 8) {
       // ---------------------------------------------------------------- loads: Q0 K0 Q1 V0 K1 V1 ..
-      if (lane == 0) {
+      if (elect_one()) {
         auto load_q = [&](int k) {
           tc_mbar_expect_tx(&ctl->qfull[k], S::QBLK);
           for (int at = 0; at < S::KA; ++at)
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
       }
     } else if (warp == 9) {
       // ---------------------------------------------------------------- products
-      if (lane == 0) {
+      if (elect_one()) {
         constexpr uint32_t idS = tc_idesc(S::BF16, kBR, kBR, false, false);
         constexpr uint32_t idO = tc_idesc(S::BF16, kBR, S::DV, false, true);
         const Desc qd = tc_desc_sw128(smem_addr(sm + S::Q_OFF));

@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   uint32_t* status = &g_status_product;
 
   if (warp == 4) {
-    if (lane == 0) {
+    if (elect_one()) {
       int64_t held = -1;
       int c = 0, w = 0;
       for (int64_t i = first; i < last; ++i) {
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       }
     }
   } else if (warp == 5) {
-    if (lane == 0) {
+    if (elect_one()) {
       constexpr uint32_t id = tc_idesc(S::BF16, kTok, NT, false, S::W_MN);
       const Desc ad = tc_desc_sw128(smem_addr(sa));
       const Desc wd = S::W_MN ? tc_desc_mn<64>(smem_addr(sm), (uint32_t)a.K * 128) : tc_desc_sw128(smem_addr(sm));

@@ -26,6 +26,14 @@ __device__ __forceinline__ bool wait_or_fail(uint64_t* bar, uint32_t parity, vol
   return false;
 }
 
+// One thread of a converged warp.  (Code behind this choice is known to run in a single thread, which matters for
+// the instructions that take their operands from uniform registers: TMA copies and tensor-core products.)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(p));
+  return p != 0;
+}
+
 // One non-blocking test of phase `parity` of `bar`.
 __device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
   uint32_t ok;

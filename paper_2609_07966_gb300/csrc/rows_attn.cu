@@ -243,7 +243,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
 
   if (warp >= kLoad) {
     regs_down<S::RO>();
-    if (warp == kLoad && lane == 0) {
+    if (warp == kLoad) {
+     if (elect_one()) {
       // ---------------------------------------------------------------- loads
       Pieces<KT> p(a, ctl);
       int g = 0;                                          // tiles loaded by this CTA so far
@@ -291,7 +292,9 @@ __global__ void __launch_bounds__(S::THREADS, 1)
           }
         }
       }
-    } else if (warp == kMma && lane == 0) {
+     }
+    } else if (warp == kMma) {
+     if (elect_one()) {
       // ---------------------------------------------------------------- products
       constexpr uint32_t idS = tc_idesc(S::BF16, KT, N, false, false);
       constexpr uint32_t idO = tc_idesc(S::BF16, S::MV, N, true, true);
@@ -386,6 +389,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         }
         g0 += nt;
       }
+     }
     }
   } else {
     regs_up<S::RS>();
