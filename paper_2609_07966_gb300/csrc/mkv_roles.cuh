@@ -17,7 +17,9 @@ __device__ __forceinline__ bool wait_or_fail(uint64_t* bar, uint32_t parity, vol
   if (tc_mbar_try(bar, parity)) return true;
   const uint64_t t0 = globaltimer_ns();
   for (;;) {
-    if (tc_mbar_try(bar, parity)) return true;
+#pragma unroll 1
+    for (int i = 0; i < 16; ++i)
+      if (tc_mbar_try(bar, parity)) return true;
     if (*fail) return false;
     if (globaltimer_ns() - t0 > kRoleWaitNs) break;
   }

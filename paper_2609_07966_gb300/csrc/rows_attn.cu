@@ -67,6 +67,7 @@ struct RowsArgs {
   uint16_t* out;
   float* part_o;                    // [CTAs][2][N][DV]: a run's pieces of units that other runs share
   float2* part_ml;                  // [CTAs][2][N]
+  struct Joint* joint;              // [B][Hkv][row_blocks]
 };
 
 // KA / VA: 64-dim atoms of a key / value; SHARED: values are the keys' first atoms; KT keys a tile, N rows a
@@ -112,9 +113,10 @@ struct RowsCtl {
   uint64_t qfull, qempty, ofree, full[kMaxSlotsRing], empty[kMaxSlotsRing], rfull[4], rempty[4], sfull[2], pfull[2],
       pvdone[2];
   uint64_t nonfinite;     // drafted tokens that hold a non-finite value
-  int64_t run0, run1, base;   // this CTA's run of tiles, first tile of entry b0
   uint32_t tslot;
-  int fail, b0;
+  int runs, run_len, longer;  // (Runs)
+  int run0, run1, base, b0;   // this CTA's run of tiles; first tile of entry b0, which holds run0
+  int fail;
   int q_loads, chunks, ropes, scores, values;   // issued so far (read after a failure)
 };
 static_assert(sizeof(RowsCtl) <= 512, "control block");
@@ -128,11 +130,32 @@ __device__ __forceinline__ int entry_tiles(const RowsArgs& a, int b) {
   return (entry_len(a, b) + KT - 1) / KT + (a.tree ? 1 : 0);
 }
 
+// `total` tiles in `runs` runs, the first total % runs of them one tile longer: run i starts at tile run_start(i).
+struct Runs {
+  int runs, len, longer;
+  __device__ __forceinline__ Runs(int total, int ctas) {
+    runs = std::max(1, std::min(ctas, total));           // none of them empty
+    len = total / runs;
+    longer = total - len * runs;
+  }
+  __device__ __forceinline__ int start(int i) const { return i * len + std::min(i, longer); }
+  __device__ __forceinline__ int of(int tile) const {    // the run that holds a tile
+    const int split = longer * (len + 1);
+    return tile < split ? tile / (len + 1) : longer + (tile - split) / len;
+  }
+};
+
+// Where the pieces of a unit that several runs share are: run `run` holds the first one, in its slot `slot`
+// (0: its first piece, 1: its last), the runs after it the others in slot 0.
+struct Joint {
+  int run, slot, count;     // count 1: written directly
+};
+
 // A run's pieces, one unit at a time.
 template <int KT>
 struct Pieces {
   const RowsArgs& a;
-  int64_t cur, end, base;   // next tile of the run, its end, first tile of entry b
+  int cur, end, base;       // next tile of the run, its end, first tile of entry b
   int b, per;               // units per entry
   // the current piece: unit `u` of entry b, its tiles t0 .. t1 - 1 of `tiles`
   int u, t0, t1, tiles, len, index;
@@ -143,14 +166,13 @@ struct Pieces {
     for (;;) {
       len = entry_len(a, b);
       tiles = (len + KT - 1) / KT + (a.tree ? 1 : 0);
-      if (cur < base + (int64_t)tiles * per) break;
-      base += (int64_t)tiles * per;
+      if (cur < base + tiles * per) break;
+      base += tiles * per;
       ++b;
     }
-    const int64_t rel = cur - base;
-    u = (int)(rel / tiles);
-    t0 = (int)(rel - (int64_t)u * tiles);
-    t1 = (int)std::min<int64_t>(tiles, t0 + (end - cur));
+    u = (cur - base) / tiles;
+    t0 = cur - base - u * tiles;
+    t1 = std::min(tiles, t0 + (end - cur));
     cur += t1 - t0;
     ++index;
     return true;
@@ -196,23 +218,22 @@ __global__ void __launch_bounds__(S::THREADS, 1)
     }
     pdl_wait_and_trigger();
     const int per = a.Hkv * a.row_blocks;
-    int64_t total = 0;
-    for (int b = lane; b < a.B; b += 32) total += entry_tiles<KT>(a, b);
+    const int mine0 = lane < a.B ? entry_tiles<KT>(a, lane) * per : 0;
+    int total = mine0;
+    for (int b = lane + 32; b < a.B; b += 32) total += entry_tiles<KT>(a, b) * per;
 #pragma unroll
     for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-    total *= per;
-    const int64_t runs = std::min<int64_t>(gridDim.x, total);   // none of them empty
-    const int64_t run0 = blockIdx.x < runs ? total * blockIdx.x / runs : 0;
-    const int64_t run1 = blockIdx.x < runs ? total * (blockIdx.x + 1) / runs : 0;
+    const Runs rs(total, gridDim.x);
+    const int i = blockIdx.x, run0 = i < rs.runs ? rs.start(i) : 0;
+    const int run1 = i < rs.runs && total > 0 ? rs.start(i + 1) : 0;
     // the entry that holds tile run0
-    int64_t base = 0;
-    int b0 = 0;
+    int base = 0, b0 = 0;
     for (int c = 0; c < a.B && run0 < run1; c += 32) {
-      const int64_t mine = c + lane < a.B ? (int64_t)entry_tiles<KT>(a, c + lane) * per : 0;
-      int64_t upto = mine;                                // inclusive prefix within the 32
+      const int mine = c == 0 ? mine0 : c + lane < a.B ? entry_tiles<KT>(a, c + lane) * per : 0;
+      int upto = mine;                                    // inclusive prefix within the 32
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
-        const int64_t x = __shfl_up_sync(0xffffffffu, upto, d);
+        const int x = __shfl_up_sync(0xffffffffu, upto, d);
         if (lane >= d) upto += x;
       }
       const unsigned past = __ballot_sync(0xffffffffu, c + lane < a.B && base + upto > run0);
@@ -225,6 +246,9 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       base += __shfl_sync(0xffffffffu, upto, 31);
     }
     if (lane == 0) {
+      ctl->runs = rs.runs;
+      ctl->run_len = rs.len;
+      ctl->longer = rs.longer;
       ctl->run0 = run0;
       ctl->run1 = run1;
       ctl->base = base;
@@ -293,6 +317,20 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         }
       }
      }
+    } else if (warp == kMma + 1) {
+      // ---------------------------------------------------------------- for join_kernel: the units that start here
+      if (elect_one()) {
+        Pieces<KT> p(a, ctl);
+        Runs rs(1, 1);
+        rs.runs = ctl->runs;
+        rs.len = ctl->run_len;
+        rs.longer = ctl->longer;
+        while (p.next())
+          if (p.t0 == 0) {
+            const int u0 = p.base + p.u * p.tiles;
+            a.joint[p.b * p.per + p.u] = Joint{(int)blockIdx.x, p.index > 0 ? 1 : 0, rs.of(u0 + p.tiles - 1) - (int)blockIdx.x + 1};
+          }
+      }
     } else if (warp == kMma) {
      if (elect_one()) {
       // ---------------------------------------------------------------- products
@@ -327,7 +365,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
             if (!ok) break;
             tc_fence_after();
             const Desc ps = pd.at(gv % S::NP * S::PBUF).opaque();
-#pragma unroll
+            // (loops stay rolled: this thread's code has to stay in the instruction cache beside the others')
+#pragma unroll 1
             for (int mb = 0; mb < S::NB; ++mb) {
               const int s = (gv * CH + (S::SHARED ? mb : 1)) % S::SLOTS;
               const Desc vs = vd.at(s * S::SLOT).opaque();
@@ -350,20 +389,20 @@ __global__ void __launch_bounds__(S::THREADS, 1)
                      : mbar_test(&ctl->full[s], (uint32_t)((c / S::SLOTS) & 1))) {
               tc_fence_after();
               const uint32_t d = tbase + (uint32_t)((gs & 1) * N);
-              if (rope) {
-                const Desc ks = rd.at(r * S::ATOM).opaque(), qs = qd.at(S::VA * S::QATOM).opaque();
+              constexpr int kAtoms = S::SLOT / S::ATOM;
+              Desc ks = rope ? rd.at(r * S::ATOM) : kd.at(s * S::SLOT), qs = qd.at(js * kAtoms * S::QATOM);
+#pragma unroll 1
+              for (int x = 0; x < (rope ? 1 : kAtoms); ++x) {
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) tc_mma_ss(d, ks.at(kk * 32), qs.at(kk * 32), idS, 1u);
-                tc_commit(&ctl->rempty[r]);
-              } else {
-                constexpr int kAtoms = S::SLOT / S::ATOM;
-                const Desc ks = kd.at(s * S::SLOT).opaque(), qs = qd.at(js * kAtoms * S::QATOM).opaque();
-#pragma unroll
-                for (int kk = 0; kk < kAtoms * 4; ++kk)
-                  tc_mma_ss(d, ks.at((kk >> 2) * S::ATOM + (kk & 3) * 32), qs.at((kk >> 2) * S::QATOM + (kk & 3) * 32),
-                            idS, js > 0 || kk > 0 ? 1u : 0u);
-                if (!S::SHARED) tc_commit(&ctl->empty[s]);
+                for (int kk = 0; kk < 4; ++kk)
+                  tc_mma_ss(d, ks.at(kk * 32), qs.at(kk * 32), idS, js > 0 || x > 0 || kk > 0 ? 1u : 0u);
+                ks = ks.at(S::ATOM);
+                qs = qs.at(S::QATOM);
               }
+              if (rope)
+                tc_commit(&ctl->rempty[r]);
+              else if (!S::SHARED)
+                tc_commit(&ctl->empty[s]);
               if (++js == kSteps) {
                 tc_commit(&ctl->sfull[gs & 1]);
                 js = 0;
@@ -641,70 +680,85 @@ __global__ void __launch_bounds__(S::THREADS, 1)
 }
 
 // The units that several runs share: out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over their pieces; zeros for
-// the units of an entry without any token.  DV / 4 threads a row, each four dims.
+// the units of an entry without any token.  A CTA takes 512 / DV rows, a thread four dims of one; the weights of a
+// row's pieces are worked out side by side first, so that the pieces' loads do not wait for one another.
+constexpr int kJoinWeights = 160;      // at most one piece per run
 template <bool BF16, int KT, int DV>
-__global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N, int ctas) {
+__global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
+  constexpr int kPer = 512 / DV, kGrp = DV / 4;          // rows a CTA, threads a row
+  __shared__ float sw[kPer][kJoinWeights], sred[4][2];
   pdl_wait_and_trigger();
-  constexpr int kPer = 512 / DV;                         // rows a CTA
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * kPer + threadIdx.x / (DV / 4);   // (b Hkv + kvh) R + r
-  const bool live = row < (int64_t)a.B * a.Hkv * a.R;
-  const int64_t bh = (live ? row : 0) / a.R;
-  const int r = (int)((live ? row : 0) % a.R), b = (int)(bh / a.Hkv), kvh = (int)(bh % a.Hkv), d = threadIdx.x % (DV / 4) * 4;
-  // tiles before entry b, and of all entries (rows of one warp may be of different entries: summed per thread group)
-  const int per = a.Hkv * a.row_blocks;
-  int64_t before = 0, total = 0;
-  constexpr int kGrp = DV / 4 < 32 ? DV / 4 : 32;        // threads of a row within a warp
-  for (int e = lane % kGrp; e < a.B; e += kGrp) {
-    const int x = entry_tiles<KT>(a, e);
-    total += x;
-    before += e < b ? x : 0;
-  }
-#pragma unroll
-  for (int k = kGrp / 2; k; k >>= 1) {
-    total += __shfl_xor_sync(0xffffffffu, total, k);
-    before += __shfl_xor_sync(0xffffffffu, before, k);
-  }
-  if (!live) return;
+  const int g = threadIdx.x / kGrp, x = threadIdx.x % kGrp;
+  const int64_t rows = (int64_t)a.B * a.Hkv * a.R, want = (int64_t)blockIdx.x * kPer + g;
+  const int64_t row = want < rows ? want : rows - 1;     // (b Hkv + kvh) R + r
+  const int64_t bh = row / a.R;
+  const int r = (int)(row - bh * a.R), b = (int)(bh / a.Hkv), kvh = (int)(bh - (int64_t)b * a.Hkv);
   const int tiles = entry_tiles<KT>(a, b);
+  const Joint jt = tiles > 0 ? a.joint[bh * a.row_blocks + r / N] : Joint{0, 0, 1};
+  const int count = jt.count;
+  // a piece's place in the workspace; piece i is of run jt.run + i
+  auto place = [&](int i) { return ((int64_t)(jt.run + i) * 2 + (i == 0 ? jt.slot : 0)) * N + r % N; };
+  // threads of one row: a maximum and a sum over all of its pieces (all threads of the CTA take part)
+  auto all = [&](float v, bool maximum, int slot) {
+#pragma unroll
+    for (int d = (kGrp < 32 ? kGrp : 32) / 2; d; d >>= 1) {
+      const float y = __shfl_xor_sync(0xffffffffu, v, d);
+      v = maximum ? fmaxf(v, y) : v + y;
+    }
+    if constexpr (kGrp > 32) {                           // a row of several warps
+      const int w = threadIdx.x >> 5, w0 = w / (kGrp / 32) * (kGrp / 32);
+      if ((threadIdx.x & 31) == 0) sred[w][slot] = v;
+      __syncthreads();
+      v = sred[w0][slot];
+      for (int k = 1; k < kGrp / 32; ++k) v = maximum ? fmaxf(v, sred[w0 + k][slot]) : v + sred[w0 + k][slot];
+    }
+    return v;
+  };
+  float2 ml[(kJoinWeights + kGrp - 1) / kGrp];
+  float M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int k = 0; k < (kJoinWeights + kGrp - 1) / kGrp; ++k) {
+    const int i = k * kGrp + x;
+    ml[k] = count > 1 && i < count ? a.part_ml[place(i)] : make_float2(-INFINITY, 0.f);
+    M = fmaxf(M, ml[k].x);
+  }
+  M = all(M, true, 0);
+#pragma unroll
+  for (int k = 0; k < (kJoinWeights + kGrp - 1) / kGrp; ++k) {
+    const int i = k * kGrp + x;
+    const float w = ml[k].x == -INFINITY ? 0.f : ex2_approx(ml[k].x - M);
+    if (i < kJoinWeights) sw[g][i] = w;
+    L += w * ml[k].y;
+  }
+  L = all(L, false, 1);
+  __syncthreads();
+  if (want >= rows || (count <= 1 && tiles > 0)) return;   // one run held the whole unit
+  const int d = x * 4;
   const int64_t at = (a.log_g < 0 ? row : ((int64_t)b * a.n + (r >> a.log_g)) * a.H + kvh * a.G + (r & (a.G - 1))) * DV + d;
-  if (tiles == 0) {
-    *reinterpret_cast<uint2*>(a.out + at) = make_uint2(0, 0);
-    return;
-  }
-  total *= per;
-  const int64_t runs = std::min<int64_t>(ctas, total);
-  const int64_t u0 = before * per + (int64_t)(kvh * a.row_blocks + r / N) * tiles;   // the unit's first tile
-  const int64_t c0 = cta_of_chunk(u0, total, runs), c1 = cta_of_chunk(u0 + tiles - 1, total, runs);
-  if (c0 == c1) return;                                  // one run held the whole unit
-  const int64_t first = c0 * 2 + (total * c0 / runs < u0 ? 1 : 0);   // its first piece: not the first of its run?
-  float M = -INFINITY;
-  for (int64_t c = c0; c <= c1; ++c) M = fmaxf(M, a.part_ml[(c == c0 ? first : c * 2) * N + r % N].x);
-  float L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int64_t c = c0; c <= c1; ++c) {
-    const int64_t s = (c == c0 ? first : c * 2) * N + r % N;
-    const float2 x = a.part_ml[s];
-    const float4 y = *reinterpret_cast<const float4*>(a.part_o + s * DV + d);
-    const float w = x.x == -INFINITY ? 0.f : ex2_approx(x.x - M);
-    L += w * x.y;
-    o.x += w * y.x;
-    o.y += w * y.y;
-    o.z += w * y.z;
-    o.w += w * y.w;
-  }
   const float inv = L == 0.f ? 0.f : 1.f / L;
+  if (tiles > 0 && inv != 0.f) {
+#pragma unroll 8
+    for (int i = 0; i < count; ++i) {
+      const float4 y = *reinterpret_cast<const float4*>(a.part_o + place(i) * DV + d);
+      const float w = sw[g][i] * inv;
+      o.x += w * y.x;
+      o.y += w * y.y;
+      o.z += w * y.z;
+      o.w += w * y.w;
+    }
+  }
   uint2 h;
-  h.x = pack2<BF16>(inv == 0.f ? 0.f : o.x * inv, inv == 0.f ? 0.f : o.y * inv);
-  h.y = pack2<BF16>(inv == 0.f ? 0.f : o.z * inv, inv == 0.f ? 0.f : o.w * inv);
+  h.x = pack2<BF16>(o.x, o.y);
+  h.y = pack2<BF16>(o.z, o.w);
   *reinterpret_cast<uint2*>(a.out + at) = h;
 }
 
 // ---------------------------------------------------------------- host side
 struct Plan {
   int N, KT, R, row_blocks, ctas;
-  size_t ml_off, o_off, bytes;
+  int64_t tiles;               // of all units when every entry is full
+  size_t joint_off, ml_off, o_off, bytes;
 };
 
 Plan plan_rows(const RowsCall& c) {
@@ -713,10 +767,11 @@ Plan plan_rows(const RowsCall& c) {
   p.N = p.R <= 16 ? 16 : p.R <= 32 ? 32 : 64;
   p.KT = c.latent ? 64 : 128;
   p.row_blocks = (int)ceil_div(p.R, p.N);
-  const int64_t tiles = (ceil_div(c.T_cap, p.KT) + 1) * c.B * c.Hkv * p.row_blocks;
-  p.ctas = (int)std::min<int64_t>(tiles, kNumSMs);
+  p.tiles = (ceil_div(c.T_cap, p.KT) + 1) * c.B * c.Hkv * p.row_blocks;
+  p.ctas = (int)std::min<int64_t>(p.tiles, kNumSMs);
   const size_t parts = (size_t)p.ctas * 2 * p.N;
-  p.ml_off = kCounterBytes;
+  p.joint_off = kCounterBytes;
+  p.ml_off = p.joint_off + align256((size_t)c.B * c.Hkv * p.row_blocks * sizeof(Joint));
   p.o_off = p.ml_off + align256(parts * sizeof(float2));
   p.bytes = p.o_off + align256(parts * c.dv * sizeof(float));
   return p;
@@ -750,7 +805,7 @@ cudaError_t launch_shape(const RowsCall& c, const Plan& p, RowsArgs a, cudaStrea
   e = launch_pdl(rows_kernel<S>, dim3(p.ctas), dim3(S::THREADS), smem, st, qm, km, vm, ktm, vtm, a);
   if (e != cudaSuccess) return e;
   const unsigned grid = (unsigned)ceil_div(B * Hkv * p.R, 512 / S::DV);
-  return launch_pdl(join_kernel<S::BF16, S::KT, S::DV>, dim3(grid), dim3(128), 0, st, a, (int)S::N, p.ctas);
+  return launch_pdl(join_kernel<S::BF16, S::KT, S::DV>, dim3(grid), dim3(128), 0, st, a, (int)S::N);
 }
 
 // rows a block, ring slots, last-key-atom slots, weight buffers: what an SM's shared memory holds
@@ -799,6 +854,8 @@ cudaError_t launch_rows_attention(const RowsCall& c, void* ws, cudaStream_t st) 
   a.v_tok = c.latent ? c.dk : (int64_t)c.Hkv * c.dv;
   a.v_head = c.latent ? 0 : c.dv;
   a.out = static_cast<uint16_t*>(c.out);
+  if (p.tiles > INT32_MAX / 2) return cudaErrorInvalidConfiguration;   // more than any GPU's memory holds
+  a.joint = reinterpret_cast<Joint*>(static_cast<uint8_t*>(ws) + p.joint_off);
   a.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + p.ml_off);
   a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.o_off);
   if (c.latent) return c.dtype == MKV_BF16 ? launch_latent<true>(c, p, a, st) : launch_latent<false>(c, p, a, st);
