@@ -91,6 +91,10 @@ struct Shape {
   // a tile's ring chunks: SHARED: its value blocks (MV dims each, the last key atom apart); else keys, values
   static constexpr int CH = SHARED ? NB : 2;
   static constexpr int SLOT = SHARED ? (MV / 64) * ATOM : KA * ATOM;
+  // "Loaded" barriers (a tile's keys; not SHARED: its values apart), one per tile whose loads may be under way: tile
+  // g + AHEAD is only begun once tile g's products are issued (SHARED: its last key atom's slot is free; else its
+  // ring slots are).
+  static constexpr int AHEAD = SHARED ? ROPE : SLOTS / 2 + 1;
   static_assert(SHARED || KA == VA, "keys and values of one size");
   static_assert(!SHARED || KA == VA + 1, "one key atom past the values");
   static constexpr int PBUF = KT * N * 2;
@@ -110,14 +114,13 @@ struct Shape {
 
 constexpr int kMaxSlotsRing = 12;
 struct RowsCtl {
-  uint64_t qfull, qempty, ofree, full[kMaxSlotsRing], empty[kMaxSlotsRing], rfull[4], rempty[4], sfull[2], pfull[2],
-      pvdone[2];
+  uint64_t qfull, qempty, ofree, kfull[8], vfull[8], empty[kMaxSlotsRing], rempty[4], sfull[2], pfull[2], pvdone[2];
   uint64_t nonfinite;     // drafted tokens that hold a non-finite value
   uint32_t tslot;
   int runs, run_len, longer;  // (Runs)
   int run0, run1, base, b0;   // this CTA's run of tiles; first tile of entry b0, which holds run0
   int fail;
-  int q_loads, chunks, ropes, scores, values;   // issued so far (read after a failure)
+  int q_loads, loaded, scores, values;   // pieces' queries, tiles issued so far (read after a failure)
 };
 static_assert(sizeof(RowsCtl) <= 512, "control block");
 
@@ -200,21 +203,19 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       tc_mbar_init(&ctl->qfull, 1);
       tc_mbar_init(&ctl->qempty, 1);
       tc_mbar_init(&ctl->ofree, S::NG * 4);
-      for (int s = 0; s < S::SLOTS; ++s) {
-        tc_mbar_init(&ctl->full[s], 1);
-        tc_mbar_init(&ctl->empty[s], 1);
+      for (int s = 0; s < S::AHEAD; ++s) {
+        tc_mbar_init(&ctl->kfull[s], S::SHARED ? CH + 1 : 1);
+        tc_mbar_init(&ctl->vfull[s], 1);
       }
-      for (int s = 0; s < S::ROPE; ++s) {
-        tc_mbar_init(&ctl->rfull[s], 1);
-        tc_mbar_init(&ctl->rempty[s], 1);
-      }
+      for (int s = 0; s < S::SLOTS; ++s) tc_mbar_init(&ctl->empty[s], 1);
+      for (int s = 0; s < S::ROPE; ++s) tc_mbar_init(&ctl->rempty[s], 1);
       for (int s = 0; s < 2; ++s) {
         tc_mbar_init(&ctl->sfull[s], 1);
         tc_mbar_init(&ctl->pfull[s], S::NG * 4);
         tc_mbar_init(&ctl->pvdone[s], 1);
       }
       tc_fence_mbar_init();
-      ctl->fail = ctl->q_loads = ctl->chunks = ctl->ropes = ctl->scores = ctl->values = 0;
+      ctl->fail = ctl->q_loads = ctl->loaded = ctl->scores = ctl->values = 0;
     }
     pdl_wait_and_trigger();
     const int per = a.Hkv * a.row_blocks;
@@ -271,7 +272,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
      if (elect_one()) {
       // ---------------------------------------------------------------- loads
       Pieces<KT> p(a, ctl);
-      int g = 0;                                          // tiles loaded by this CTA so far
+      int g = 0, slot = 0, lap = 0;                       // tiles loaded so far; next ring slot, times around
       bool ok = true;
       while (ok && p.next()) {
         const int kvh = p.u / a.row_blocks, row0 = p.u % a.row_blocks * N;
@@ -289,31 +290,35 @@ __global__ void __launch_bounds__(S::THREADS, 1)
           const int key = tr ? 0 : t * KT;
           const CUtensorMap* km = tr ? &ktmap : &kmap;
           const CUtensorMap* vm = tr ? &vtmap : &vmap;
+          if constexpr (S::SHARED) {
+            // the last key atom first: its slot bounds the tiles under way, and so the use of kfull
+            const int r = g % S::ROPE, w = g / S::ROPE;
+            ok = w == 0 || wait_or_fail(&ctl->rempty[r], (uint32_t)((w - 1) & 1), fail, status);
+            if (!ok) break;
+            tc_mbar_expect_tx(&ctl->kfull[r], S::ATOM);
+            tma_load_4d(sm + S::R_OFF + r * S::ATOM, km, S::VA * 64, key, p.b, 0, &ctl->kfull[r]);
+          }
 #pragma unroll
           for (int j = 0; j < CH; ++j) {
-            const int c = g * CH + j, s = c % S::SLOTS, w = c / S::SLOTS;
-            if (w > 0 && !wait_or_fail(&ctl->empty[s], (uint32_t)((w - 1) & 1), fail, status)) {
+            uint64_t* bar = S::SHARED || j == 0 ? &ctl->kfull[g % S::AHEAD] : &ctl->vfull[g % S::AHEAD];
+            if (lap > 0 && !wait_or_fail(&ctl->empty[slot], (uint32_t)((lap - 1) & 1), fail, status)) {
               ok = false;
               break;
             }
-            uint8_t* dst = sm + S::KV_OFF + s * S::SLOT;
-            tc_mbar_expect_tx(&ctl->full[s], S::SLOT);
+            uint8_t* dst = sm + S::KV_OFF + slot * S::SLOT;
+            tc_mbar_expect_tx(bar, S::SLOT);
+#pragma unroll
             for (int x = 0; x < S::SLOT / S::ATOM; ++x)
               if (S::SHARED)
-                tma_load_4d(dst + x * S::ATOM, km, (j * (S::MV / 64) + x) * 64, key, p.b, 0, &ctl->full[s]);
+                tma_load_4d(dst + x * S::ATOM, km, (j * (S::MV / 64) + x) * 64, key, p.b, 0, bar);
               else
-                tma_load_4d(dst + x * S::ATOM, j == 0 ? km : vm, x * 64, key, kvh, p.b, &ctl->full[s]);
-            ctl->chunks = c + 1;
+                tma_load_4d(dst + x * S::ATOM, j == 0 ? km : vm, x * 64, key, kvh, p.b, bar);
+            if (++slot == S::SLOTS) {
+              slot = 0;
+              ++lap;
+            }
           }
-          if constexpr (S::SHARED) {
-            if (!ok) break;
-            const int s = g % S::ROPE, w = g / S::ROPE;
-            ok = w == 0 || wait_or_fail(&ctl->rempty[s], (uint32_t)((w - 1) & 1), fail, status);
-            if (!ok) break;
-            tc_mbar_expect_tx(&ctl->rfull[s], S::ATOM);
-            tma_load_4d(sm + S::R_OFF + s * S::ATOM, km, S::VA * 64, key, p.b, 0, &ctl->rfull[s]);
-            ctl->ropes = g + 1;
-          }
+          if (ok) ctl->loaded = g + 1;
         }
       }
      }
@@ -343,77 +348,78 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       const Desc pd = tc_desc_mn<S::PW>(smem_addr(sm + S::P_OFF), KT * S::PW * 2);
       Pieces<KT> p(a, ctl);
       int g0 = 0;                                         // tiles of the earlier pieces
+      int kslot = 0, vslot = 0;                           // ring slots of the next scores' and values' tile
       bool ok = true;
       while (ok && p.next()) {
         const int nt = p.t1 - p.t0;
         ok = wait_or_fail(&ctl->qfull, (uint32_t)(p.index & 1), fail, status);
-        int ts = 0, js = 0, tv = 0;                       // next scores (tile, step), next second product
-        // steps of a tile's scores: its ring chunks that hold keys, then (SHARED) the last key atom
-        constexpr int kSteps = S::SHARED ? CH + 1 : 1;
+        int ts = 0, tv = 0;                               // next tile's scores, next tile's second product
         uint64_t since = 0;                               // when it last found nothing ready
         int idle = 0;
         while (ok && tv < nt) {
           const int gs = g0 + ts, gv = g0 + tv;
-          bool ready = tv < ts && mbar_test(&ctl->pfull[gv % S::NP], (uint32_t)((gv / S::NP) & 1));
-          if (!S::SHARED && ready) {
-            const int c = gv * CH + 1;
-            ready = mbar_test(&ctl->full[c % S::SLOTS], (uint32_t)((c / S::SLOTS) & 1));
-          }
-          if (ready) {
+          // what is ready is looked up together: a product should not wait for more than one look
+          // (S^T buffer gs & 1 has been read once tile ts - 2 is past its softmax, that is once ts <= tv + 1)
+          const bool can_s = ts < nt && ts <= tv + 1 &&
+                             mbar_test(&ctl->kfull[gs % S::AHEAD], (uint32_t)((gs / S::AHEAD) & 1));
+          bool can_v = tv < ts && mbar_test(&ctl->pfull[gv % S::NP], (uint32_t)((gv / S::NP) & 1));
+          if (!S::SHARED)
+            can_v = can_v && mbar_test(&ctl->vfull[gv % S::AHEAD], (uint32_t)((gv / S::AHEAD) & 1));
+          if (can_v) {
             if (tv == 0 && p.index > 0)                   // the previous piece's outputs have been read
               ok = wait_or_fail(&ctl->ofree, (uint32_t)((p.index - 1) & 1), fail, status);
             if (!ok) break;
             tc_fence_after();
             const Desc ps = pd.at(gv % S::NP * S::PBUF).opaque();
-            // (loops stay rolled: this thread's code has to stay in the instruction cache beside the others')
-#pragma unroll 1
+            int s = S::SHARED ? vslot : vslot + 1 == S::SLOTS ? 0 : vslot + 1;
+#pragma unroll
             for (int mb = 0; mb < S::NB; ++mb) {
-              const int s = (gv * CH + (S::SHARED ? mb : 1)) % S::SLOTS;
               const Desc vs = vd.at(s * S::SLOT).opaque();
 #pragma unroll
               for (int kk = 0; kk < KT / 16; ++kk)
                 tc_mma_ss(tO + (uint32_t)(mb * N), vs.at(kk * 2048), ps.at(kk * 16 * S::PW * 2), idO,
                           tv > 0 || kk > 0 ? 1u : 0u);
               tc_commit(&ctl->empty[s]);
+              if (++s == S::SLOTS) s = 0;
             }
             tc_commit(&ctl->pvdone[gv % S::NP]);
+            vslot = s;
             ctl->values = gv + 1;
             ++tv;
             idle = 0;
-            continue;
           }
-          if (ts < nt && ts <= tv + 1) {                  // S^T buffer gs & 1 has been read (tile ts - 2 is past its softmax)
-            const bool rope = S::SHARED && js == CH;
-            const int c = gs * CH + js, s = c % S::SLOTS, r = S::SHARED ? gs % S::ROPE : 0;
-            if (rope ? mbar_test(&ctl->rfull[r], (uint32_t)((gs / (S::SHARED ? S::ROPE : 1)) & 1))
-                     : mbar_test(&ctl->full[s], (uint32_t)((c / S::SLOTS) & 1))) {
-              tc_fence_after();
-              const uint32_t d = tbase + (uint32_t)((gs & 1) * N);
-              constexpr int kAtoms = S::SLOT / S::ATOM;
-              Desc ks = rope ? rd.at(r * S::ATOM) : kd.at(s * S::SLOT), qs = qd.at(js * kAtoms * S::QATOM);
-#pragma unroll 1
-              for (int x = 0; x < (rope ? 1 : kAtoms); ++x) {
+          if (can_s) {
+            tc_fence_after();
+            const uint32_t d = tbase + (uint32_t)((gs & 1) * N);
+            constexpr int kAtoms = S::SLOT / S::ATOM, kChunks = S::SHARED ? CH : 1;
+            int s = kslot;
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk)
-                  tc_mma_ss(d, ks.at(kk * 32), qs.at(kk * 32), idS, js > 0 || x > 0 || kk > 0 ? 1u : 0u);
-                ks = ks.at(S::ATOM);
-                qs = qs.at(S::QATOM);
-              }
-              if (rope)
-                tc_commit(&ctl->rempty[r]);
-              else if (!S::SHARED)
-                tc_commit(&ctl->empty[s]);
-              if (++js == kSteps) {
-                tc_commit(&ctl->sfull[gs & 1]);
-                js = 0;
-                ++ts;
-                ctl->scores = gs + 1;
-                if (ts == nt) tc_commit(&ctl->qempty);
-              }
-              idle = 0;
-              continue;
+            for (int j = 0; j < kChunks; ++j) {
+              const Desc ks = kd.at(s * S::SLOT).opaque(), qs = qd.at(j * kAtoms * S::QATOM).opaque();
+#pragma unroll
+              for (int kk = 0; kk < kAtoms * 4; ++kk)
+                tc_mma_ss(d, ks.at((kk >> 2) * S::ATOM + (kk & 3) * 32), qs.at((kk >> 2) * S::QATOM + (kk & 3) * 32),
+                          idS, j > 0 || kk > 0 ? 1u : 0u);
+              if (!S::SHARED) tc_commit(&ctl->empty[s]);
+              if (++s == S::SLOTS) s = 0;
             }
+            if constexpr (S::SHARED) {
+              const int r = gs % S::ROPE;
+              const Desc ks = rd.at(r * S::ATOM).opaque(), qs = qd.at(S::VA * S::QATOM).opaque();
+#pragma unroll
+              for (int kk = 0; kk < 4; ++kk) tc_mma_ss(d, ks.at(kk * 32), qs.at(kk * 32), idS, 1u);
+              tc_commit(&ctl->rempty[r]);
+              kslot = s;
+            } else {
+              kslot = s + 1 == S::SLOTS ? 0 : s + 1;      // past the tile's values
+            }
+            tc_commit(&ctl->sfull[gs & 1]);
+            ++ts;
+            ctl->scores = gs + 1;
+            if (ts == nt) tc_commit(&ctl->qempty);
+            idle = 0;
           }
+          if (can_s || can_v) continue;
           // nothing is ready: a bounded wait for either, its clock read now and then
           if ((++idle & 63) == 0) {
             const uint64_t now = globaltimer_ns();
@@ -554,10 +560,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         // zeros; a drafted token's non-finite values become zeros here and are added to the rows that see it at
         // the end.  (Latent: the scores of this tile are complete, so its keys may be overwritten.)
         if (tr || valid < KT) {
-          if (!S::SHARED) {
-            const int c = g * CH + 1;
-            wait(&ctl->full[c % S::SLOTS], (uint32_t)((c / S::SLOTS) & 1));
-          }
+          if (!S::SHARED) wait(&ctl->vfull[g % S::AHEAD], (uint32_t)((g / S::AHEAD) & 1));
           const int r0 = tr ? 0 : valid, r1 = tr ? a.n : KT;
           for (int e = threadIdx.x; e < (r1 - r0) * 8 * S::VA; e += S::SOFT) {
             const int r = r0 + e / (8 * S::VA), x = e % (8 * S::VA), at = x >> 3;
@@ -665,10 +668,12 @@ __global__ void __launch_bounds__(S::THREADS, 1)
   __syncthreads();
   if (threadIdx.x == 0 && ctl->fail) {
     if (ctl->q_loads > 0) tc_mbar_wait(&ctl->qfull, (uint32_t)((ctl->q_loads - 1) & 1), kRoleWaitNs);
-    for (int c = std::max(0, ctl->chunks - S::SLOTS); c < ctl->chunks; ++c)
-      tc_mbar_wait(&ctl->full[c % S::SLOTS], (uint32_t)((c / S::SLOTS) & 1), kRoleWaitNs);
-    for (int c = std::max(0, ctl->ropes - S::ROPE); S::SHARED && c < ctl->ropes; ++c)
-      tc_mbar_wait(&ctl->rfull[c % std::max(1, S::ROPE)], (uint32_t)((c / std::max(1, S::ROPE)) & 1), kRoleWaitNs);
+    // (a tile whose loads were only begun when its wait ran out: nothing says when those end but time)
+    for (int g = std::max(0, ctl->loaded - S::AHEAD); g <= ctl->loaded; ++g) {
+      tc_mbar_wait(&ctl->kfull[g % S::AHEAD], (uint32_t)((g / S::AHEAD) & 1), g < ctl->loaded ? kRoleWaitNs : 10000000ull);
+      if (!S::SHARED && g < ctl->loaded)
+        tc_mbar_wait(&ctl->vfull[g % S::AHEAD], (uint32_t)((g / S::AHEAD) & 1), kRoleWaitNs);
+    }
     if (ctl->scores > 0)
       tc_mbar_wait(&ctl->sfull[(ctl->scores - 1) & 1], (uint32_t)(((ctl->scores - 1) >> 1) & 1), kRoleWaitNs);
     if (ctl->values > 0)
