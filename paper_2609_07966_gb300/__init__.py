@@ -147,7 +147,7 @@ def mkv_last_error() -> str:
 
 
 def _call(name, *args):
-    st = getattr(lib(), name)(*args)
+    st = getattr(_lib or lib(), name)(*args)
     if st != MKV_OK:
         raise MkvError(st, name, mkv_last_error())
 
@@ -167,11 +167,22 @@ def config(method: int, B: int, Hq: int, Hkv: int, D: int, **kw) -> mkv_config:
     return c
 
 
+_current_stream = None
+
+
 def _stream(stream):
-    if stream is None:
+    """The stream handle of a call: the given one, or torch's current stream on the current device."""
+    if stream is not None:
+        return int(stream)
+    global _current_stream
+    if _current_stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
-    return int(stream)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:          # the handle alone: building a Stream object costs more than a launch
+            _current_stream = lambda: raw(torch.cuda.current_device())      # noqa: E731
+        else:
+            _current_stream = lambda: torch.cuda.current_stream().cuda_stream      # noqa: E731
+    return _current_stream()
 
 
 def mkv_workspace_size(cfg: mkv_config, T_cap: int) -> int:

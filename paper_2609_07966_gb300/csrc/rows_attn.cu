@@ -118,7 +118,7 @@ struct RowsCtl {
   uint64_t nonfinite;     // drafted tokens that hold a non-finite value
   uint32_t tslot;
   int runs, run_len, longer;  // (Runs)
-  int run0, run1, base, b0;   // this CTA's run of tiles; first tile of entry b0, which holds run0
+  int run0, run1, base, b0, len0;   // this CTA's run of tiles; first tile of entry b0, which holds run0; its length
   int fail;
   int q_loads, loaded, scores, values;   // pieces' queries, tiles issued so far (read after a failure)
 };
@@ -129,8 +129,12 @@ __device__ __forceinline__ int entry_len(const RowsArgs& a, int b) {
 }
 // Tiles of one unit of entry b.
 template <int KT>
+__device__ __forceinline__ int unit_tiles(const RowsArgs& a, int len) {
+  return (len + KT - 1) / KT + (a.tree ? 1 : 0);
+}
+template <int KT>
 __device__ __forceinline__ int entry_tiles(const RowsArgs& a, int b) {
-  return (entry_len(a, b) + KT - 1) / KT + (a.tree ? 1 : 0);
+  return unit_tiles<KT>(a, entry_len(a, b));
 }
 
 // `total` tiles in `runs` runs, the first total % runs of them one tile longer: run i starts at tile run_start(i).
@@ -163,15 +167,15 @@ struct Pieces {
   // the current piece: unit `u` of entry b, its tiles t0 .. t1 - 1 of `tiles`
   int u, t0, t1, tiles, len, index;
   __device__ __forceinline__ Pieces(const RowsArgs& args, const RowsCtl* c)
-      : a(args), cur(c->run0), end(c->run1), base(c->base), b(c->b0), per(args.Hkv * args.row_blocks), index(-1) {}
+      : a(args), cur(c->run0), end(c->run1), base(c->base), b(c->b0), per(args.Hkv * args.row_blocks), len(c->len0),
+        index(-1) {}
   __device__ __forceinline__ bool next() {
     if (cur >= end) return false;
     for (;;) {
-      len = entry_len(a, b);
-      tiles = (len + KT - 1) / KT + (a.tree ? 1 : 0);
+      tiles = unit_tiles<KT>(a, len);
       if (cur < base + tiles * per) break;
       base += tiles * per;
-      ++b;
+      len = entry_len(a, ++b);
     }
     u = (cur - base) / tiles;
     t0 = cur - base - u * tiles;
@@ -219,7 +223,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
     }
     pdl_wait_and_trigger();
     const int per = a.Hkv * a.row_blocks;
-    const int mine0 = lane < a.B ? entry_tiles<KT>(a, lane) * per : 0;
+    const int len_mine = lane < a.B ? entry_len(a, lane) : 0;
+    const int mine0 = lane < a.B ? unit_tiles<KT>(a, len_mine) * per : 0;
     int total = mine0;
     for (int b = lane + 32; b < a.B; b += 32) total += entry_tiles<KT>(a, b) * per;
 #pragma unroll
@@ -246,7 +251,9 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       }
       base += __shfl_sync(0xffffffffu, upto, 31);
     }
+    const int len0 = b0 < 32 ? __shfl_sync(0xffffffffu, len_mine, b0) : entry_len(a, b0);
     if (lane == 0) {
+      ctl->len0 = len0;
       ctl->runs = rs.runs;
       ctl->run_len = rs.len;
       ctl->longer = rs.longer;
@@ -699,8 +706,8 @@ __global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
   const int64_t bh = row / a.R;
   const int r = (int)(row - bh * a.R), b = (int)(bh / a.Hkv), kvh = (int)(bh - (int64_t)b * a.Hkv);
   const int tiles = entry_tiles<KT>(a, b);
-  const Joint jt = tiles > 0 ? a.joint[bh * a.row_blocks + r / N] : Joint{0, 0, 1};
-  const int count = jt.count;
+  const Joint jt = a.joint[bh * a.row_blocks + r / N];     // (not written for an entry without tiles)
+  const int count = tiles > 0 ? jt.count : 1;
   // a piece's place in the workspace; piece i is of run jt.run + i
   auto place = [&](int i) { return ((int64_t)(jt.run + i) * 2 + (i == 0 ? jt.slot : 0)) * N + r % N; };
   // threads of one row: a maximum and a sum over all of its pieces (all threads of the CTA take part)
@@ -743,14 +750,21 @@ __global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   const float inv = L == 0.f ? 0.f : 1.f / L;
   if (tiles > 0 && inv != 0.f) {
-#pragma unroll 8
-    for (int i = 0; i < count; ++i) {
-      const float4 y = *reinterpret_cast<const float4*>(a.part_o + place(i) * DV + d);
-      const float w = sw[g][i] * inv;
-      o.x += w * y.x;
-      o.y += w * y.y;
-      o.z += w * y.z;
-      o.w += w * y.w;
+    constexpr int kAt = 12;                              // pieces whose loads are under way together
+    for (int i0 = 0; i0 < count; i0 += kAt) {
+      float4 y[kAt];
+#pragma unroll
+      for (int k = 0; k < kAt; ++k)
+        if (i0 + k < count) y[k] = *reinterpret_cast<const float4*>(a.part_o + place(i0 + k) * DV + d);
+#pragma unroll
+      for (int k = 0; k < kAt; ++k)
+        if (i0 + k < count) {
+          const float w = sw[g][i0 + k] * inv;
+          o.x += w * y[k].x;
+          o.y += w * y[k].y;
+          o.z += w * y[k].z;
+          o.w += w * y[k].w;
+        }
     }
   }
   uint2 h;
