@@ -1,9 +1,11 @@
 // The accepted path of a tree of drafted tokens joins a cache: for i < n_path[b] the rows of token
-// path[b][i] are copied to slot T_len[b] + i, then T_len[b] += n_path[b].  Bound by memory latency (a few
-// tens of KB an entry) and, for a whole prompt's rows, by bandwidth.
+// path[b][i] are copied to slot T_len[b] + i, then T_len[b] += n_path[b].  A step's few tens of KB an entry are bound
+// by latency, a whole prompt's rows by bandwidth; a warp moves one token's row of one cache at a time (its heads lie
+// together in the source), four 16-byte pieces a lane in flight.
 //
-// A cluster of CTAs per entry shares the copies; every CTA reads the length and checks the whole path, a
-// cluster barrier separates those reads from the first CTA's store of the new length.
+// Every CTA that reads an entry's length has to do so before it changes.  A step's rows are shared by a cluster of
+// CTAs per entry, whose barrier separates the reads from the first CTA's store of the new length: one launch.  A
+// prompt's rows are shared by as many CTAs as the GPU holds, and a second launch stores the lengths.
 #include <algorithm>
 
 #include "mkv_common.cuh"
@@ -26,40 +28,64 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");
 }
 
-__global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitCall a) {
-  const int b = blockIdx.y, parts = gridDim.x;
-  const int t0 = a.T_len[b];
-  const int np = a.n_path != nullptr ? a.n_path[b] : a.n;
+// Whether entry b's path fits (all threads of the CTA take part); its length and path length.
+__device__ __forceinline__ bool path_fits(const CommitCall& a, int b, int& t0, int& np) {
+  t0 = a.T_len[b];
+  np = a.n_path != nullptr ? a.n_path[b] : a.n;
   bool ok = t0 >= 0 && np >= 0 && np <= a.n && (int64_t)t0 + np <= a.T_cap;
   if (ok && a.path != nullptr)
     for (int i = threadIdx.x; i < np; i += kCommitThreads) {
       const int p = a.path[(int64_t)b * a.n + i];
       ok = ok && p >= 0 && p < a.n;
     }
-  ok = __syncthreads_and(ok);
-  cluster_sync();                                       // every CTA of the entry has read its length
-  if (cluster_rank() == 0 && threadIdx.x == 0) {
-    if (ok)
-      a.T_len[b] = t0 + np;
-    else
-      atomicOr(&g_status_commit, MKV_FLAG_CACHE_FULL);
+  return __syncthreads_and(ok);
+}
+
+__device__ __forceinline__ void store_length(const CommitCall& a, int b, bool ok, int t) {
+  if (threadIdx.x != 0) return;
+  if (ok)
+    a.T_len[b] = t;
+  else
+    atomicOr(&g_status_commit, MKV_FLAG_CACHE_FULL);
+}
+
+template <bool kCluster>
+__global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitCall a) {
+  const int b = blockIdx.y;
+  int t0, np;
+  const bool ok = path_fits(a, b, t0, np);
+  if (kCluster) {
+    cluster_sync();                                     // every CTA of the entry has read its length
+    if (cluster_rank() == 0) store_length(a, b, ok, t0 + np);
   }
   if (!ok) return;
-  // (cache, token, head, 16-byte piece), pieces fastest
-  const int per = a.row_bytes / 16;
-  const int64_t one = (int64_t)np * a.heads * per, total = a.src1 != nullptr ? 2 * one : one;
-  for (int64_t e = (int64_t)blockIdx.x * kCommitThreads + threadIdx.x; e < total;
-       e += (int64_t)parts * kCommitThreads) {
-    const bool second = e >= one;
-    const int64_t x = second ? e - one : e;
-    const int c = (int)(x % per), h = (int)(x / per % a.heads);
-    const int64_t i = x / per / a.heads;
-    const int64_t tok = a.path != nullptr ? a.path[(int64_t)b * a.n + i] : i;
-    const uint4* src = static_cast<const uint4*>(second ? a.src1 : a.src0);
-    uint4* dst = static_cast<uint4*>(second ? a.dst1 : a.dst0);
-    dst[(((int64_t)b * a.heads + h) * a.T_cap + t0 + i) * per + c] =
-        src[(((int64_t)b * a.n + tok) * a.heads + h) * per + c];
+  const int lane = threadIdx.x & 31, per = a.row_bytes / 16, row = a.heads * per;   // pieces of a token's row
+  const int64_t jobs = a.src1 != nullptr ? 2 * (int64_t)np : np;
+  for (int64_t j = (int64_t)blockIdx.x * (kCommitThreads / 32) + (threadIdx.x >> 5); j < jobs;
+       j += (int64_t)gridDim.x * (kCommitThreads / 32)) {
+    const bool second = j >= np;
+    const int i = (int)(second ? j - np : j);
+    const int tok = a.path != nullptr ? a.path[(int64_t)b * a.n + i] : i;
+    const uint4* src = static_cast<const uint4*>(second ? a.src1 : a.src0) + ((int64_t)b * a.n + tok) * row;
+    uint4* dst = static_cast<uint4*>(second ? a.dst1 : a.dst0) + ((int64_t)b * a.heads * a.T_cap + t0 + i) * per;
+    for (int e0 = lane; e0 < row; e0 += 128) {
+      uint4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (e0 + 32 * k < row) x[k] = src[e0 + 32 * k];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int e = e0 + 32 * k, h = e / per;
+        if (e < row) dst[(int64_t)h * a.T_cap * per + (e - h * per)] = x[k];
+      }
+    }
   }
+}
+
+__global__ void __launch_bounds__(kCommitThreads) length_kernel(const CommitCall a) {
+  int t0, np;
+  const bool ok = path_fits(a, blockIdx.x, t0, np);
+  store_length(a, blockIdx.x, ok, t0 + np);
 }
 
 }  // namespace
@@ -75,6 +101,17 @@ cudaError_t take_status_commit(uint32_t* flags, cudaStream_t st) {
 
 cudaError_t launch_commit(const CommitCall& c, cudaStream_t st) {
   constexpr int kParts = 8;                             // the largest portable cluster
+  // One launch up to 1 MiB an entry (measured, 16 rows of 4 KB x 8 entries: 4.2 us; 9.4 MB of one entry: 86 us through
+  // one cluster, against the two launches' time below).
+  const int64_t bytes = (int64_t)c.n * c.heads * c.row_bytes * (c.src1 != nullptr ? 2 : 1);
+  if (bytes > (1 << 20)) {
+    const int64_t want = ceil_div((int64_t)4 * kNumSMs, (int64_t)c.B), most = ceil_div(c.n, kCommitThreads / 32);
+    commit_kernel<false><<<dim3((unsigned)std::min(want, most), c.B), kCommitThreads, 0, st>>>(c);
+    const cudaError_t e = cudaPeekAtLastError();
+    if (e != cudaSuccess) return e;
+    length_kernel<<<c.B, kCommitThreads, 0, st>>>(c);
+    return cudaPeekAtLastError();
+  }
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim = {kParts, 1, 1};
@@ -84,7 +121,7 @@ cudaError_t launch_commit(const CommitCall& c, cudaStream_t st) {
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, commit_kernel, c);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, commit_kernel<true>, c);
   return e != cudaSuccess ? e : cudaPeekAtLastError();
 }
 

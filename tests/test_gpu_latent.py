@@ -292,11 +292,12 @@ def test_expanded_and_absorbed_forms_agree():
 
 
 # ------------------------------------------------------------------------------------------- commit
-@pytest.mark.parametrize("dtype,rank,n", [("fp16", 512, 1), ("bf16", 256, 33), ("fp16", 512, 700)])
+@pytest.mark.parametrize("dtype,rank,n", [("fp16", 512, 1), ("bf16", 256, 33), ("fp16", 512, 700), ("bf16", 512, 2000)])
 def test_latent_commit(dtype, rank, n):
+    """Short paths go in one launch, a prompt's rows in two."""
     torch = torch_cuda()
     rng = np.random.default_rng(n)
-    B, T_cap, lens = 3, 1500, [0, 800, 1499]
+    B, T_cap, lens = 3, 2500, [0, 800, 2499]
     cfg = mkv.latent_config(KINDS[dtype], B, 4, rank=rank)
     cache = caches.alloc_latent_cache(cfg, T_cap)
     cache.t["T_len"].copy_(torch.tensor(lens, dtype=torch.int32))
