@@ -49,6 +49,7 @@ struct PrefillArgs {
   const uint16_t* kv;               // values, for non-finite ones
   uint16_t* out;
   int rank;
+  int units, group;                 // (entry, head) pairs; how many of them are worked on together
 };
 
 template <bool BF16_, int DN_, int DV_>
@@ -57,14 +58,21 @@ struct PShape {
   static constexpr int DN = DN_, DV = DV_, DK = DN + 64;
   static constexpr int KA = DK / 64, VA = DV / 64;
   static constexpr int ATOM = kBR * 128;                    // 128 rows of 64 dims
-  static constexpr int QBLK = KA * ATOM, KST = KA * ATOM, VST = VA * ATOM;
-  static constexpr int NSK = 2;
-  static constexpr int NSV = (2 * QBLK + NSK * KST + 2 * VST <= 224 * 1024 - 2048) ? 2 : 1;
-  static constexpr int Q_OFF = 0, K_OFF = 2 * QBLK, V_OFF = K_OFF + NSK * KST;
-  static constexpr int CTL_OFF = V_OFF + NSV * VST;
+  static constexpr int QBLK = KA * ATOM;
+  // Key and value atoms pass through one ring in the order K0 V0 K1 V1 .., which is the order they are done with.  What
+  // shared memory holds beside the queries (8 atoms of 16 KB at 192 / 128 dims) is a tile's keys, the values of the
+  // tile before it, and the next values: with a fixed pair of key stages the single value stage left was waited for
+  // (a fifth of the tile time).
+  static constexpr int TA = KA + VA;                        // atoms of a tile
+  static constexpr int RING = (227 * 1024 - 1536 - 2 * QBLK) / ATOM;
+  static_assert(RING >= TA + VA, "shared memory");
+  static constexpr int Q_OFF = 0, R_OFF = 2 * QBLK;
+  static constexpr int CTL_OFF = R_OFF + RING * ATOM;
   static constexpr int ALLOC = CTL_OFF + 512 + 1024;
   static_assert(ALLOC <= 227 * 1024, "shared memory");
 };
+constexpr int64_t kGroupBytes = 32 << 20;
+constexpr int kBars = 4;            // tiles whose barriers are told apart: more than the ring holds
 // Two softmax warpgroups, loads and products (and two idle warps); registers a thread at launch (168, what 384
 // threads get) split 2 x 208 + 88.
 constexpr int kPThreads = 384, kPRegsSoftmax = 208, kPRegsOther = 88;
@@ -72,7 +80,7 @@ static_assert(2 * kPRegsSoftmax + kPRegsOther <= 3 * 168, "register shares");
 constexpr int kFixWords = 16;       // flags of the keys of the tiles that some row sees only in part
 
 struct PCtl {
-  uint64_t qfull[2], kfull[2], kempty[2], vfull[2], vempty[2], sfull[2], pfull[2], pvdone[2];
+  uint64_t qfull[2], kfull[kBars], kempty[kBars], vfull[kBars], vempty[kBars], sfull[2], pfull[2][2], pvdone[2];
   uint32_t tslot;
   int fail, k_loaded, v_loaded, issued[2];
   uint32_t nonfinite[kFixWords];    // keys (from the first partial tile) whose value holds a non-finite number
@@ -86,8 +94,13 @@ __global__ void __launch_bounds__(kPThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
   PCtl* ctl = reinterpret_cast<PCtl*>(sm + S::CTL_OFF);
-  const int h = blockIdx.x % a.H, b = blockIdx.x / a.H;
-  const int i0 = (int)(gridDim.y - 1 - blockIdx.y) * 2 * kBR;    // the queries with the most keys first
+  // Launch order: groups of a.group (entry, head) units whose keys and values fit L2 together; within a group the
+  // query blocks with the most keys first, so that the last blocks to start are short.
+  const int nblk = (a.n + 2 * kBR - 1) / (2 * kBR);
+  const int grp = (int)(blockIdx.x / ((unsigned)a.group * nblk)), in = (int)(blockIdx.x - (unsigned)grp * a.group * nblk);
+  const int size = std::min(a.group, a.units - grp * a.group), unit = grp * a.group + in % size;
+  const int h = unit % a.H, b = unit / a.H;
+  const int i0 = (nblk - 1 - in / size) * 2 * kBR;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   const int tl = a.T_len[b];
@@ -113,14 +126,17 @@ __global__ void __launch_bounds__(kPThreads, 1)
 
   if (warp == 8) tc_alloc(&ctl->tslot, 512);
   if (threadIdx.x == 0) {
-    for (int s = 0; s < 2; ++s) {
-      tc_mbar_init(&ctl->qfull[s], 1);
+    for (int s = 0; s < kBars; ++s) {
       tc_mbar_init(&ctl->kfull[s], 1);
       tc_mbar_init(&ctl->kempty[s], 1);
       tc_mbar_init(&ctl->vfull[s], 1);
       tc_mbar_init(&ctl->vempty[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      tc_mbar_init(&ctl->qfull[s], 1);
       tc_mbar_init(&ctl->sfull[s], 1);
-      tc_mbar_init(&ctl->pfull[s], 4);
+      tc_mbar_init(&ctl->pfull[s][0], 4);
+      tc_mbar_init(&ctl->pfull[s][1], 4);
       tc_mbar_init(&ctl->pvdone[s], 1);
     }
     tc_fence_mbar_init();
@@ -144,24 +160,37 @@ __global__ void __launch_bounds__(kPThreads, 1)
           for (int at = 0; at < S::KA; ++at)
             tma_load_4d(sm + S::Q_OFF + k * S::QBLK + at * S::ATOM, &qmap, at * 64, i0 + k * kBR, h, b, &ctl->qfull[k]);
         };
+        // the ring slot of atom j of tile t, free once its last atom is done with
+        auto slot_for = [&](int t, int j, uint8_t*& dst) {
+          const int x = t * S::TA + j, was = x - S::RING;
+          dst = sm + S::R_OFF + x % S::RING * S::ATOM;
+          if (was < 0) return true;
+          const int pt = was / S::TA;
+          return wait_or_fail(was % S::TA < S::KA ? &ctl->kempty[pt % kBars] : &ctl->vempty[pt % kBars],
+                              (uint32_t)((pt / kBars) & 1), fail, status);
+        };
         auto load_k = [&](int t) {
-          const int s = t % S::NSK, u = t / S::NSK;
-          if (u > 0 && !wait_or_fail(&ctl->kempty[s], (uint32_t)((u - 1) & 1), fail, status)) return false;
-          uint8_t* dst = sm + S::K_OFF + s * S::KST;
-          tc_mbar_expect_tx(&ctl->kfull[s], S::KST);
-          for (int at = 0; at < S::DN / 64; ++at)
-            tma_load_4d(dst + at * S::ATOM, &kvmap, at * 64, t * kBR, h, b, &ctl->kfull[s]);
-          tma_load_4d(dst + (S::DN / 64) * S::ATOM, &rmap, a.rank, t * kBR, b, 0, &ctl->kfull[s]);
+          uint64_t* bar = &ctl->kfull[t % kBars];
+          for (int j = 0; j < S::KA; ++j) {
+            uint8_t* dst;
+            if (!slot_for(t, j, dst)) return false;
+            if (j == 0) tc_mbar_expect_tx(bar, S::KA * S::ATOM);
+            if (j < S::DN / 64)
+              tma_load_4d(dst, &kvmap, j * 64, t * kBR, h, b, bar);
+            else
+              tma_load_4d(dst, &rmap, a.rank, t * kBR, b, 0, bar);
+          }
           ctl->k_loaded = t + 1;
           return true;
         };
         auto load_v = [&](int t) {
-          const int s = t % S::NSV, u = t / S::NSV;
-          if (u > 0 && !wait_or_fail(&ctl->vempty[s], (uint32_t)((u - 1) & 1), fail, status)) return false;
-          tc_mbar_expect_tx(&ctl->vfull[s], S::VST);
-          for (int at = 0; at < S::VA; ++at)
-            tma_load_4d(sm + S::V_OFF + s * S::VST + at * S::ATOM, &kvmap, S::DN + at * 64, t * kBR, h, b,
-                        &ctl->vfull[s]);
+          uint64_t* bar = &ctl->vfull[t % kBars];
+          for (int j = 0; j < S::VA; ++j) {
+            uint8_t* dst;
+            if (!slot_for(t, S::KA + j, dst)) return false;
+            if (j == 0) tc_mbar_expect_tx(bar, S::VA * S::ATOM);
+            tma_load_4d(dst, &kvmap, S::DN + j * 64, t * kBR, h, b, bar);
+          }
           ctl->v_loaded = t + 1;
           return true;
         };
@@ -169,40 +198,47 @@ __global__ void __launch_bounds__(kPThreads, 1)
         bool ok = load_k(0);
         load_q(1);
         for (int t = 0; ok && t < ntiles; ++t) {
-          if (t + 1 < ntiles) ok = load_k(t + 1);
-          if (ok) ok = load_v(t);
+          ok = load_v(t);
+          if (ok && t + 1 < ntiles) ok = load_k(t + 1);
         }
       }
     } else if (warp == 9) {
       // ---------------------------------------------------------------- products
       if (elect_one()) {
         constexpr uint32_t idS = tc_idesc(S::BF16, kBR, kBR, false, false);
-        constexpr uint32_t idO = tc_idesc(S::BF16, kBR, S::DV, false, true);
+        constexpr uint32_t idO = tc_idesc(S::BF16, kBR, 64, false, true);
         const Desc qd = tc_desc_sw128(smem_addr(sm + S::Q_OFF));
-        const Desc kd = tc_desc_sw128(smem_addr(sm + S::K_OFF));
-        const Desc vd = tc_desc_mn<64>(smem_addr(sm + S::V_OFF), S::ATOM);
+        const Desc kd = tc_desc_sw128(smem_addr(sm + S::R_OFF));
+        const Desc vd = tc_desc_mn<64>(smem_addr(sm + S::R_OFF), S::ATOM);
         auto wait = [&](uint64_t* bar, uint32_t parity) {
           const bool ok = wait_or_fail(bar, parity, fail, status);
           tc_fence_after();
           return ok;
         };
         auto scores = [&](int k, int t) {     // S_k of tile t
-          const Desc q0 = qd.at(k * S::QBLK).opaque(), k0 = kd.at(t % S::NSK * S::KST).opaque();
-  #pragma unroll
-          for (int kk = 0; kk < S::KA * 4; ++kk) {
-            const uint32_t o = (kk >> 2) * S::ATOM + (kk & 3) * 32;
-            tc_mma_ss(tbase + (uint32_t)(k * kBR), q0.at(o), k0.at(o), idS, kk > 0 ? 1u : 0u);
+          int slot = t * S::TA % S::RING;
+#pragma unroll
+          for (int j = 0; j < S::KA; ++j) {
+            const Desc q0 = qd.at(k * S::QBLK + j * S::ATOM).opaque(), k0 = kd.at(slot * S::ATOM).opaque();
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              tc_mma_ss(tbase + (uint32_t)(k * kBR), q0.at(kk * 32), k0.at(kk * 32), idS, j > 0 || kk > 0 ? 1u : 0u);
+            if (++slot == S::RING) slot = 0;
           }
           tc_commit(&ctl->sfull[k]);
         };
-        auto values = [&](int k, int t) {     // O_k += P_k V of tile t
-          const Desc v0 = vd.at(t % S::NSV * S::VST).opaque();
-  #pragma unroll
-          for (int kk = 0; kk < kBR / 16; ++kk)
-            tc_mma_ts(tbase + (uint32_t)(2 * kBR + k * kBR), tbase + (uint32_t)(k * kBR + kk * 8), v0.at(kk * 2048), idO,
-                      t > 0 || kk > 0 ? 1u : 0u);
-          tc_commit(&ctl->pvdone[k]);
-          ctl->issued[k] = t + 1;
+        auto values = [&](int k, int t, int half) {     // O_k += P_k V over half of tile t's keys
+          int slot = (t * S::TA + S::KA) % S::RING;      // (64 dims a product: a tile's value atoms need not be neighbours)
+#pragma unroll
+          for (int j = 0; j < S::VA; ++j) {
+            const Desc v0 = vd.at(slot * S::ATOM + half * (kBR / 2) * 128).opaque();
+            const uint32_t p0 = tbase + (uint32_t)(k * kBR + half * (kBR / 4));
+#pragma unroll
+            for (int kk = 0; kk < kBR / 32; ++kk)
+              tc_mma_ts(tbase + (uint32_t)(2 * kBR + k * kBR + j * 64), p0 + (uint32_t)(kk * 8), v0.at(kk * 2048), idO,
+                        t > 0 || half > 0 || kk > 0 ? 1u : 0u);
+            if (++slot == S::RING) slot = 0;
+          }
         };
         bool ok = wait(&ctl->kfull[0], 0);
         for (int k = 0; ok && k < 2; ++k) {
@@ -211,17 +247,23 @@ __global__ void __launch_bounds__(kPThreads, 1)
         }
         if (ok) tc_commit(&ctl->kempty[0]);
         for (int t = 0; ok && t < ntiles; ++t) {
-          ok = wait(&ctl->vfull[t % S::NSV], (uint32_t)((t / S::NSV) & 1));
-          if (ok && t + 1 < ntiles) ok = wait(&ctl->kfull[(t + 1) % S::NSK], (uint32_t)(((t + 1) / S::NSK) & 1));
+          ok = wait(&ctl->vfull[t % kBars], (uint32_t)((t / kBars) & 1));
+          if (ok && t + 1 < ntiles) ok = wait(&ctl->kfull[(t + 1) % kBars], (uint32_t)(((t + 1) / kBars) & 1));
           for (int k = 0; ok && k < 2; ++k) {
             if (t < nt[k]) {
-              ok = wait(&ctl->pfull[k], (uint32_t)(t & 1));
+              // (the first half's weights arrive while the softmax works on the second)
+              ok = wait(&ctl->pfull[k][0], (uint32_t)(t & 1));
               if (!ok) break;
-              values(k, t);
+              values(k, t, 0);
+              ok = wait(&ctl->pfull[k][1], (uint32_t)(t & 1));
+              if (!ok) break;
+              values(k, t, 1);
+              tc_commit(&ctl->pvdone[k]);
+              ctl->issued[k] = t + 1;
             }
-            if (k == 1) tc_commit(&ctl->vempty[t % S::NSV]);
+            if (k == 1) tc_commit(&ctl->vempty[t % kBars]);
             if (t + 1 < nt[k]) scores(k, t + 1);
-            if (k == 1 && t + 1 < ntiles) tc_commit(&ctl->kempty[(t + 1) % S::NSK]);
+            if (k == 1 && t + 1 < ntiles) tc_commit(&ctl->kempty[(t + 1) % kBars]);
           }
         }
       }
@@ -273,31 +315,15 @@ __global__ void __launch_bounds__(kPThreads, 1)
           }
         }
       }
-      const uint64_t sc2 = pk2(a.scale_log2, a.scale_log2), off2 = pk2(kOffset - m, kOffset - m);
-      uint64_t sum2[2] = {0ull, 0ull};
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {          // 64 keys = 32 packed columns
-        float pk[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const float2 x = upk2(ffma2(pk2(v[c * 64 + 2 * e], v[c * 64 + 2 * e + 1]), sc2, off2));
-          const float p0 = ex2_approx(x.x), p1 = ex2_approx(x.y);
-          sum2[e & 1] = fadd2(sum2[e & 1], pk2(p0, p1));
-          pk[e] = __uint_as_float(pack2<S::BF16>(p0, p1));
-        }
-        tm_store<32>(tS + c * 32, pk);
-      }
-      const float2 s0 = upk2(sum2[0]), s1 = upk2(sum2[1]);
-      l += (s0.x + s0.y) + (s1.x + s1.y);
       if (t >= td && (k == 0 || t >= nt[0])) {
         // Values that some row of the CTA does not see must not meet its zero weight (0 x NaN): slots past the
         // length become zeros; a token's non-finite values become zeros here and are added to the rows that see it
         // at the end.  Done by the first block that meets the tile, before its product.
-        if (!wait(&ctl->vfull[t % S::NSV], (uint32_t)((t / S::NSV) & 1))) break;
-        uint8_t* vt = sm + S::V_OFF + (t % S::NSV) * S::VST;
+        if (!wait(&ctl->vfull[t % kBars], (uint32_t)((t / kBars) & 1))) break;
         for (int e = threadIdx.x & 127; e < kBR * 8 * S::VA; e += 128) {
           const int r = e / (8 * S::VA), x = e % (8 * S::VA);
-          uint4* p8 = reinterpret_cast<uint4*>(vt + (x >> 3) * S::ATOM + r * 128 + ((x & 7) << 4));
+          uint4* p8 = reinterpret_cast<uint4*>(sm + S::R_OFF + (t * S::TA + S::KA + (x >> 3)) % S::RING * S::ATOM +
+                                               mn_offset<64>(r, x & 7));
           if (t * kBR + r >= len) {
             *p8 = make_uint4(0, 0, 0, 0);
             continue;
@@ -311,10 +337,26 @@ __global__ void __launch_bounds__(kPThreads, 1)
         }
         fence_async_smem();
       }
-      tm_store_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) tc_mbar_arrive(&ctl->pfull[k]);
+      const uint64_t sc2 = pk2(a.scale_log2, a.scale_log2), off2 = pk2(kOffset - m, kOffset - m);
+      uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {          // 64 keys = 32 packed columns
+        float pk[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const float2 x = upk2(ffma2(pk2(v[c * 64 + 2 * e], v[c * 64 + 2 * e + 1]), sc2, off2));
+          const float p0 = ex2_approx(x.x), p1 = ex2_approx(x.y);
+          sum2[e & 1] = fadd2(sum2[e & 1], pk2(p0, p1));
+          pk[e] = __uint_as_float(pack2<S::BF16>(p0, p1));
+        }
+        tm_store<32>(tS + c * 32, pk);
+        tm_store_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc_mbar_arrive(&ctl->pfull[k][c]);
+      }
+      const float2 s0 = upk2(sum2[0]), s1 = upk2(sum2[1]);
+      l += (s0.x + s0.y) + (s1.x + s1.y);
     }
     // ---------------------------------------------------------------- output
     // the other block's last tile may hold values zeroed for this one: its flags are complete once both are done
@@ -362,10 +404,11 @@ __global__ void __launch_bounds__(kPThreads, 1)
   if (threadIdx.x == 0 && ctl->fail) {
     tc_mbar_wait(&ctl->qfull[0], 0, kRoleWaitNs);
     tc_mbar_wait(&ctl->qfull[1], 0, kRoleWaitNs);
-    for (int t = std::max(0, ctl->k_loaded - S::NSK); t < ctl->k_loaded; ++t)
-      tc_mbar_wait(&ctl->kfull[t % S::NSK], (uint32_t)((t / S::NSK) & 1), kRoleWaitNs);
-    for (int t = std::max(0, ctl->v_loaded - S::NSV); t < ctl->v_loaded; ++t)
-      tc_mbar_wait(&ctl->vfull[t % S::NSV], (uint32_t)((t / S::NSV) & 1), kRoleWaitNs);
+    // (a tile whose loads were only begun when a wait ran out: nothing says when those end but time)
+    for (int t = std::max(0, ctl->k_loaded - kBars + 1); t <= ctl->k_loaded; ++t)
+      tc_mbar_wait(&ctl->kfull[t % kBars], (uint32_t)((t / kBars) & 1), t < ctl->k_loaded ? kRoleWaitNs : 10000000ull);
+    for (int t = std::max(0, ctl->v_loaded - kBars + 1); t <= ctl->v_loaded; ++t)
+      tc_mbar_wait(&ctl->vfull[t % kBars], (uint32_t)((t / kBars) & 1), t < ctl->v_loaded ? kRoleWaitNs : 10000000ull);
     for (int k = 0; k < 2; ++k)
       if (ctl->issued[k] > 0) tc_mbar_wait(&ctl->pvdone[k], (uint32_t)((ctl->issued[k] - 1) & 1), kRoleWaitNs);
   }
@@ -375,17 +418,21 @@ __global__ void __launch_bounds__(kPThreads, 1)
 }
 
 template <class S>
-cudaError_t launch_shape(const PrefillCall& c, const PrefillArgs& a, cudaStream_t st) {
+cudaError_t launch_shape(const PrefillCall& c, PrefillArgs a, cudaStream_t st) {
   CUtensorMap qm, kvm, rm;
   const int64_t dk = S::DK, n = c.n, H = c.H, B = c.B, d = S::DN + S::DV, T = c.T_max, row = c.rank + c.rope;
   cudaError_t e = encode_map(&qm, c.q, {dk, n, H, B}, {H * dk, dk, n * H * dk}, kBR, 1);
   if (e == cudaSuccess) e = encode_map(&kvm, c.kv, {d, T, H, B}, {d, T * d, H * T * d}, kBR, 1);
   if (e == cudaSuccess) e = encode_map(&rm, c.rows, {row, c.T_cap, B, 1}, {row, c.T_cap * row, B * c.T_cap * row}, kBR, 1);
   if (e != cudaSuccess) return e;
+  a.units = c.B * c.H;
+  a.group = (int)std::max<int64_t>(1, std::min<int64_t>(a.units, kGroupBytes / (T * d * 2)));
+  const int64_t grid = ceil_div(n, 2 * kBR) * a.units;
+  if (grid > INT32_MAX) return cudaErrorInvalidConfiguration;
   constexpr int smem = std::max(S::ALLOC, 116 * 1024);      // one CTA an SM: it takes all of the tensor memory
   e = cudaFuncSetAttribute(latent_prefill_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  latent_prefill_kernel<S><<<dim3((unsigned)(H * B), (unsigned)ceil_div(n, 2 * kBR)), kPThreads, smem, st>>>(qm, kvm, rm, a);
+  latent_prefill_kernel<S><<<(unsigned)grid, kPThreads, smem, st>>>(qm, kvm, rm, a);
   return cudaPeekAtLastError();
 }
 

@@ -276,59 +276,59 @@ __global__ void __launch_bounds__(S::THREADS, 1)
   if (warp >= kLoad) {
     regs_down<S::RO>();
     if (warp == kLoad) {
-     if (elect_one()) {
-      // ---------------------------------------------------------------- loads
-      Pieces<KT> p(a, ctl);
-      int g = 0, slot = 0, lap = 0;                       // tiles loaded so far; next ring slot, times around
-      bool ok = true;
-      while (ok && p.next()) {
-        const int kvh = p.u / a.row_blocks, row0 = p.u % a.row_blocks * N;
-        if (p.index > 0) ok = wait_or_fail(&ctl->qempty, (uint32_t)((p.index - 1) & 1), fail, status);
-        if (!ok) break;
-        tc_mbar_expect_tx(&ctl->qfull, S::KA * S::QATOM);
-        for (int at = 0; at < S::KA; ++at)
-          if (S::SHARED)
-            tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, row0, p.b, 0, &ctl->qfull);
-          else
-            tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, kvh * a.G, row0 >> a.log_g, p.b, &ctl->qfull);
-        ctl->q_loads = p.index + 1;
-        for (int t = p.t0; ok && t < p.t1; ++t, ++g) {
-          const bool tr = a.tree && t == p.tiles - 1;
-          const int key = tr ? 0 : t * KT;
-          const CUtensorMap* km = tr ? &ktmap : &kmap;
-          const CUtensorMap* vm = tr ? &vtmap : &vmap;
-          if constexpr (S::SHARED) {
-            // the last key atom first: its slot bounds the tiles under way, and so the use of kfull
-            const int r = g % S::ROPE, w = g / S::ROPE;
-            ok = w == 0 || wait_or_fail(&ctl->rempty[r], (uint32_t)((w - 1) & 1), fail, status);
-            if (!ok) break;
-            tc_mbar_expect_tx(&ctl->kfull[r], S::ATOM);
-            tma_load_4d(sm + S::R_OFF + r * S::ATOM, km, S::VA * 64, key, p.b, 0, &ctl->kfull[r]);
-          }
-#pragma unroll
-          for (int j = 0; j < CH; ++j) {
-            uint64_t* bar = S::SHARED || j == 0 ? &ctl->kfull[g % S::AHEAD] : &ctl->vfull[g % S::AHEAD];
-            if (lap > 0 && !wait_or_fail(&ctl->empty[slot], (uint32_t)((lap - 1) & 1), fail, status)) {
-              ok = false;
-              break;
+      if (elect_one()) {
+        // ---------------------------------------------------------------- loads
+        Pieces<KT> p(a, ctl);
+        int g = 0, slot = 0, lap = 0;                       // tiles loaded so far; next ring slot, times around
+        bool ok = true;
+        while (ok && p.next()) {
+          const int kvh = p.u / a.row_blocks, row0 = p.u % a.row_blocks * N;
+          if (p.index > 0) ok = wait_or_fail(&ctl->qempty, (uint32_t)((p.index - 1) & 1), fail, status);
+          if (!ok) break;
+          tc_mbar_expect_tx(&ctl->qfull, S::KA * S::QATOM);
+          for (int at = 0; at < S::KA; ++at)
+            if (S::SHARED)
+              tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, row0, p.b, 0, &ctl->qfull);
+            else
+              tma_load_4d(sm + S::Q_OFF + at * S::QATOM, &qmap, at * 64, kvh * a.G, row0 >> a.log_g, p.b, &ctl->qfull);
+          ctl->q_loads = p.index + 1;
+          for (int t = p.t0; ok && t < p.t1; ++t, ++g) {
+            const bool tr = a.tree && t == p.tiles - 1;
+            const int key = tr ? 0 : t * KT;
+            const CUtensorMap* km = tr ? &ktmap : &kmap;
+            const CUtensorMap* vm = tr ? &vtmap : &vmap;
+            if constexpr (S::SHARED) {
+              // the last key atom first: its slot bounds the tiles under way, and so the use of kfull
+              const int r = g % S::ROPE, w = g / S::ROPE;
+              ok = w == 0 || wait_or_fail(&ctl->rempty[r], (uint32_t)((w - 1) & 1), fail, status);
+              if (!ok) break;
+              tc_mbar_expect_tx(&ctl->kfull[r], S::ATOM);
+              tma_load_4d(sm + S::R_OFF + r * S::ATOM, km, S::VA * 64, key, p.b, 0, &ctl->kfull[r]);
             }
-            uint8_t* dst = sm + S::KV_OFF + slot * S::SLOT;
-            tc_mbar_expect_tx(bar, S::SLOT);
 #pragma unroll
-            for (int x = 0; x < S::SLOT / S::ATOM; ++x)
-              if (S::SHARED)
-                tma_load_4d(dst + x * S::ATOM, km, (j * (S::MV / 64) + x) * 64, key, p.b, 0, bar);
-              else
-                tma_load_4d(dst + x * S::ATOM, j == 0 ? km : vm, x * 64, key, kvh, p.b, bar);
-            if (++slot == S::SLOTS) {
-              slot = 0;
-              ++lap;
+            for (int j = 0; j < CH; ++j) {
+              uint64_t* bar = S::SHARED || j == 0 ? &ctl->kfull[g % S::AHEAD] : &ctl->vfull[g % S::AHEAD];
+              if (lap > 0 && !wait_or_fail(&ctl->empty[slot], (uint32_t)((lap - 1) & 1), fail, status)) {
+                ok = false;
+                break;
+              }
+              uint8_t* dst = sm + S::KV_OFF + slot * S::SLOT;
+              tc_mbar_expect_tx(bar, S::SLOT);
+#pragma unroll
+              for (int x = 0; x < S::SLOT / S::ATOM; ++x)
+                if (S::SHARED)
+                  tma_load_4d(dst + x * S::ATOM, km, (j * (S::MV / 64) + x) * 64, key, p.b, 0, bar);
+                else
+                  tma_load_4d(dst + x * S::ATOM, j == 0 ? km : vm, x * 64, key, kvh, p.b, bar);
+              if (++slot == S::SLOTS) {
+                slot = 0;
+                ++lap;
+              }
             }
+            if (ok) ctl->loaded = g + 1;
           }
-          if (ok) ctl->loaded = g + 1;
         }
       }
-     }
     } else if (warp == kMma + 1) {
       // ---------------------------------------------------------------- for join_kernel: the units that start here
       if (elect_one()) {
@@ -344,104 +344,104 @@ __global__ void __launch_bounds__(S::THREADS, 1)
           }
       }
     } else if (warp == kMma) {
-     if (elect_one()) {
-      // ---------------------------------------------------------------- products
-      constexpr uint32_t idS = tc_idesc(S::BF16, KT, N, false, false);
-      constexpr uint32_t idO = tc_idesc(S::BF16, S::MV, N, true, true);
-      const Desc qd = tc_desc_sw128(smem_addr(sm + S::Q_OFF));
-      const Desc kd = tc_desc_sw128(smem_addr(sm + S::KV_OFF));
-      const Desc rd = tc_desc_sw128(smem_addr(sm + S::R_OFF));
-      const Desc vd = tc_desc_mn<64>(smem_addr(sm + S::KV_OFF), S::ATOM);
-      const Desc pd = tc_desc_mn<S::PW>(smem_addr(sm + S::P_OFF), KT * S::PW * 2);
-      Pieces<KT> p(a, ctl);
-      int g0 = 0;                                         // tiles of the earlier pieces
-      int kslot = 0, vslot = 0;                           // ring slots of the next scores' and values' tile
-      bool ok = true;
-      while (ok && p.next()) {
-        const int nt = p.t1 - p.t0;
-        ok = wait_or_fail(&ctl->qfull, (uint32_t)(p.index & 1), fail, status);
-        int ts = 0, tv = 0;                               // next tile's scores, next tile's second product
-        uint64_t since = 0;                               // when it last found nothing ready
-        int idle = 0;
-        while (ok && tv < nt) {
-          const int gs = g0 + ts, gv = g0 + tv;
-          // what is ready is looked up together: a product should not wait for more than one look
-          // (S^T buffer gs & 1 has been read once tile ts - 2 is past its softmax, that is once ts <= tv + 1)
-          const bool can_s = ts < nt && ts <= tv + 1 &&
-                             mbar_test(&ctl->kfull[gs % S::AHEAD], (uint32_t)((gs / S::AHEAD) & 1));
-          bool can_v = tv < ts && mbar_test(&ctl->pfull[gv % S::NP], (uint32_t)((gv / S::NP) & 1));
-          if (!S::SHARED)
-            can_v = can_v && mbar_test(&ctl->vfull[gv % S::AHEAD], (uint32_t)((gv / S::AHEAD) & 1));
-          if (can_v) {
-            if (tv == 0 && p.index > 0)                   // the previous piece's outputs have been read
-              ok = wait_or_fail(&ctl->ofree, (uint32_t)((p.index - 1) & 1), fail, status);
-            if (!ok) break;
-            tc_fence_after();
-            const Desc ps = pd.at(gv % S::NP * S::PBUF).opaque();
-            int s = S::SHARED ? vslot : vslot + 1 == S::SLOTS ? 0 : vslot + 1;
+      if (elect_one()) {
+        // ---------------------------------------------------------------- products
+        constexpr uint32_t idS = tc_idesc(S::BF16, KT, N, false, false);
+        constexpr uint32_t idO = tc_idesc(S::BF16, S::MV, N, true, true);
+        const Desc qd = tc_desc_sw128(smem_addr(sm + S::Q_OFF));
+        const Desc kd = tc_desc_sw128(smem_addr(sm + S::KV_OFF));
+        const Desc rd = tc_desc_sw128(smem_addr(sm + S::R_OFF));
+        const Desc vd = tc_desc_mn<64>(smem_addr(sm + S::KV_OFF), S::ATOM);
+        const Desc pd = tc_desc_mn<S::PW>(smem_addr(sm + S::P_OFF), KT * S::PW * 2);
+        Pieces<KT> p(a, ctl);
+        int g0 = 0;                                         // tiles of the earlier pieces
+        int kslot = 0, vslot = 0;                           // ring slots of the next scores' and values' tile
+        bool ok = true;
+        while (ok && p.next()) {
+          const int nt = p.t1 - p.t0;
+          ok = wait_or_fail(&ctl->qfull, (uint32_t)(p.index & 1), fail, status);
+          int ts = 0, tv = 0;                               // next tile's scores, next tile's second product
+          uint64_t since = 0;                               // when it last found nothing ready
+          int idle = 0;
+          while (ok && tv < nt) {
+            const int gs = g0 + ts, gv = g0 + tv;
+            // what is ready is looked up together: a product should not wait for more than one look
+            // (S^T buffer gs & 1 has been read once tile ts - 2 is past its softmax, that is once ts <= tv + 1)
+            const bool can_s = ts < nt && ts <= tv + 1 &&
+                               mbar_test(&ctl->kfull[gs % S::AHEAD], (uint32_t)((gs / S::AHEAD) & 1));
+            bool can_v = tv < ts && mbar_test(&ctl->pfull[gv % S::NP], (uint32_t)((gv / S::NP) & 1));
+            if (!S::SHARED)
+              can_v = can_v && mbar_test(&ctl->vfull[gv % S::AHEAD], (uint32_t)((gv / S::AHEAD) & 1));
+            if (can_v) {
+              if (tv == 0 && p.index > 0)                   // the previous piece's outputs have been read
+                ok = wait_or_fail(&ctl->ofree, (uint32_t)((p.index - 1) & 1), fail, status);
+              if (!ok) break;
+              tc_fence_after();
+              const Desc ps = pd.at(gv % S::NP * S::PBUF).opaque();
+              int s = S::SHARED ? vslot : vslot + 1 == S::SLOTS ? 0 : vslot + 1;
 #pragma unroll
-            for (int mb = 0; mb < S::NB; ++mb) {
-              const Desc vs = vd.at(s * S::SLOT).opaque();
+              for (int mb = 0; mb < S::NB; ++mb) {
+                const Desc vs = vd.at(s * S::SLOT).opaque();
 #pragma unroll
-              for (int kk = 0; kk < KT / 16; ++kk)
-                tc_mma_ss(tO + (uint32_t)(mb * N), vs.at(kk * 2048), ps.at(kk * 16 * S::PW * 2), idO,
-                          tv > 0 || kk > 0 ? 1u : 0u);
-              tc_commit(&ctl->empty[s]);
-              if (++s == S::SLOTS) s = 0;
+                for (int kk = 0; kk < KT / 16; ++kk)
+                  tc_mma_ss(tO + (uint32_t)(mb * N), vs.at(kk * 2048), ps.at(kk * 16 * S::PW * 2), idO,
+                            tv > 0 || kk > 0 ? 1u : 0u);
+                tc_commit(&ctl->empty[s]);
+                if (++s == S::SLOTS) s = 0;
+              }
+              tc_commit(&ctl->pvdone[gv % S::NP]);
+              vslot = s;
+              ctl->values = gv + 1;
+              ++tv;
+              idle = 0;
             }
-            tc_commit(&ctl->pvdone[gv % S::NP]);
-            vslot = s;
-            ctl->values = gv + 1;
-            ++tv;
-            idle = 0;
+            if (can_s) {
+              tc_fence_after();
+              const uint32_t d = tbase + (uint32_t)((gs & 1) * N);
+              constexpr int kAtoms = S::SLOT / S::ATOM, kChunks = S::SHARED ? CH : 1;
+              int s = kslot;
+#pragma unroll
+              for (int j = 0; j < kChunks; ++j) {
+                const Desc ks = kd.at(s * S::SLOT).opaque(), qs = qd.at(j * kAtoms * S::QATOM).opaque();
+#pragma unroll
+                for (int kk = 0; kk < kAtoms * 4; ++kk)
+                  tc_mma_ss(d, ks.at((kk >> 2) * S::ATOM + (kk & 3) * 32), qs.at((kk >> 2) * S::QATOM + (kk & 3) * 32),
+                            idS, j > 0 || kk > 0 ? 1u : 0u);
+                if (!S::SHARED) tc_commit(&ctl->empty[s]);
+                if (++s == S::SLOTS) s = 0;
+              }
+              if constexpr (S::SHARED) {
+                const int r = gs % S::ROPE;
+                const Desc ks = rd.at(r * S::ATOM).opaque(), qs = qd.at(S::VA * S::QATOM).opaque();
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) tc_mma_ss(d, ks.at(kk * 32), qs.at(kk * 32), idS, 1u);
+                tc_commit(&ctl->rempty[r]);
+                kslot = s;
+              } else {
+                kslot = s + 1 == S::SLOTS ? 0 : s + 1;      // past the tile's values
+              }
+              tc_commit(&ctl->sfull[gs & 1]);
+              ++ts;
+              ctl->scores = gs + 1;
+              if (ts == nt) tc_commit(&ctl->qempty);
+              idle = 0;
+            }
+            if (can_s || can_v) continue;
+            // nothing is ready: a bounded wait for either, its clock read now and then
+            if ((++idle & 63) == 0) {
+              const uint64_t now = globaltimer_ns();
+              if (idle == 64) since = now;
+              if (now - since > kRoleWaitNs) {
+                *fail = 1;
+                atomicOr(status, MKV_FLAG_WAIT_TIMEOUT);
+              }
+              ok = *fail == 0;
+              if (idle > (1 << 30)) idle = 128;
+            }
           }
-          if (can_s) {
-            tc_fence_after();
-            const uint32_t d = tbase + (uint32_t)((gs & 1) * N);
-            constexpr int kAtoms = S::SLOT / S::ATOM, kChunks = S::SHARED ? CH : 1;
-            int s = kslot;
-#pragma unroll
-            for (int j = 0; j < kChunks; ++j) {
-              const Desc ks = kd.at(s * S::SLOT).opaque(), qs = qd.at(j * kAtoms * S::QATOM).opaque();
-#pragma unroll
-              for (int kk = 0; kk < kAtoms * 4; ++kk)
-                tc_mma_ss(d, ks.at((kk >> 2) * S::ATOM + (kk & 3) * 32), qs.at((kk >> 2) * S::QATOM + (kk & 3) * 32),
-                          idS, j > 0 || kk > 0 ? 1u : 0u);
-              if (!S::SHARED) tc_commit(&ctl->empty[s]);
-              if (++s == S::SLOTS) s = 0;
-            }
-            if constexpr (S::SHARED) {
-              const int r = gs % S::ROPE;
-              const Desc ks = rd.at(r * S::ATOM).opaque(), qs = qd.at(S::VA * S::QATOM).opaque();
-#pragma unroll
-              for (int kk = 0; kk < 4; ++kk) tc_mma_ss(d, ks.at(kk * 32), qs.at(kk * 32), idS, 1u);
-              tc_commit(&ctl->rempty[r]);
-              kslot = s;
-            } else {
-              kslot = s + 1 == S::SLOTS ? 0 : s + 1;      // past the tile's values
-            }
-            tc_commit(&ctl->sfull[gs & 1]);
-            ++ts;
-            ctl->scores = gs + 1;
-            if (ts == nt) tc_commit(&ctl->qempty);
-            idle = 0;
-          }
-          if (can_s || can_v) continue;
-          // nothing is ready: a bounded wait for either, its clock read now and then
-          if ((++idle & 63) == 0) {
-            const uint64_t now = globaltimer_ns();
-            if (idle == 64) since = now;
-            if (now - since > kRoleWaitNs) {
-              *fail = 1;
-              atomicOr(status, MKV_FLAG_WAIT_TIMEOUT);
-            }
-            ok = *fail == 0;
-            if (idle > (1 << 30)) idle = 128;
-          }
+          g0 += nt;
         }
-        g0 += nt;
       }
-     }
     }
   } else {
     regs_up<S::RS>();
