@@ -248,7 +248,6 @@ __global__ void __launch_bounds__(kPThreads, 1)
         if (ok) tc_commit(&ctl->kempty[0]);
         for (int t = 0; ok && t < ntiles; ++t) {
           ok = wait(&ctl->vfull[t % kBars], (uint32_t)((t / kBars) & 1));
-          if (ok && t + 1 < ntiles) ok = wait(&ctl->kfull[(t + 1) % kBars], (uint32_t)(((t + 1) / kBars) & 1));
           for (int k = 0; ok && k < 2; ++k) {
             if (t < nt[k]) {
               // (the first half's weights arrive while the softmax works on the second)
@@ -262,6 +261,10 @@ __global__ void __launch_bounds__(kPThreads, 1)
               ctl->issued[k] = t + 1;
             }
             if (k == 1) tc_commit(&ctl->vempty[t % kBars]);
+            if (k == 0 && t + 1 < ntiles) {
+              ok = wait(&ctl->kfull[(t + 1) % kBars], (uint32_t)(((t + 1) / kBars) & 1));
+              if (!ok) break;
+            }
             if (t + 1 < nt[k]) scores(k, t + 1);
             if (k == 1 && t + 1 < ntiles) tc_commit(&ctl->kempty[(t + 1) % kBars]);
           }
