@@ -3,12 +3,16 @@
 //   project  W = W_uv[h]    (rank -> v)
 //   expand   W = [W_uk[h]; W_uv[h]] on a cached row's latent part (rank -> nope + v)
 // For a decode step's few tokens they are bound by reading the weights once (and by the launch), for a prompt's by the
-// tensor cores.  One kernel: a CTA holds a tile of one head's weights (NT output dims x all of K) in shared memory and
-// streams 128-token blocks past it,
-//   D [128 tokens x NT] = X [128 x K] W [K x NT]
-// with the accumulator in tensor memory twice, so a block's stores run under the next one's products.  CTAs take
-// equal runs of the (weight tile, token block) pairs, token blocks fastest, so a weight tile is loaded once or twice.
-// W is used as it is stored: along K for project and expand, along the output dims for absorb.
+// tensor cores and the shared memory that feeds them.  Both kernels hold a tile of one head's weights (all of K) in
+// shared memory and stream token blocks past it, the accumulator in tensor memory twice, so that a block's stores run
+// under the next one's products.  CTAs take equal runs of the (weight tile, token block) pairs, token blocks fastest,
+// so a weight tile is loaded once or twice.
+//
+// product_kernel (absorb, project): D [128 tokens x NT] = X [128 x K] W [K x NT]; a thread stores a token's dims.  W is
+//   used as it is stored: along K for project, along the output dims for absorb.
+// expand_kernel: D^T [128 dims x 256 tokens] = W [128 x K] X^T [K x 256].  The narrow side is as wide as the tensor core
+//   takes it, because a 128 x 256 product reads 12 KB of operands in 128 cycles where a 128 x 128 one reads 8 KB in 64:
+//   the copies that refill shared memory need the difference.
 #include <algorithm>
 
 #include "mkv_roles.cuh"
@@ -36,8 +40,8 @@ struct ProductArgs {
   int n_dim;                   // output dims per head, dims per output row
   int out_row;
   int64_t rows;                // tokens (expand: of each entry)
-  int64_t blocks;              // 128-token blocks (expand: of each entry)
-  int64_t items;               // H x dim tiles x blocks (x B)
+  int64_t blocks;              // their blocks of 128 (expand: of each entry, of 256)
+  int64_t items;               // H x dim tiles x blocks (expand: x B)
   int dim_tiles;
   const int32_t* T_len;        // expand
   const uint16_t* x;           // absorb: the queries, for their rotated part
@@ -83,19 +87,14 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   const int kc = a.K / 64;
 
   struct Item {
-    int64_t wt, b, t0;          // weight tile (h, dims), entry, first token of the block
+    int64_t wt, t0;             // weight tile (h, dims), first token of the block
     int limit;                  // tokens of the block that exist
   };
-  const int64_t per_wt = S::KIND == Product::kExpand ? a.B * a.blocks : a.blocks;
   auto item = [&](int64_t i) {
     Item x;
-    x.wt = i / per_wt;
-    const int64_t r = i % per_wt;
-    x.b = S::KIND == Product::kExpand ? r / a.blocks : 0;
-    x.t0 = (S::KIND == Product::kExpand ? r % a.blocks : r) * kTok;
-    int64_t n = a.rows;
-    if (S::KIND == Product::kExpand) n = std::min<int64_t>(n, a.T_len[x.b]);
-    x.limit = (int)std::max<int64_t>(0, std::min<int64_t>(kTok, n - x.t0));
+    x.wt = i / a.blocks;
+    x.t0 = i % a.blocks * kTok;
+    x.limit = (int)std::min<int64_t>(kTok, a.rows - x.t0);
     return x;
   };
 
@@ -127,7 +126,6 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       int c = 0, w = 0;
       for (int64_t i = first; i < last; ++i) {
         const Item x = item(i);
-        if (x.limit == 0) continue;
         const int h = (int)(x.wt / a.dim_tiles), d0 = (int)(x.wt % a.dim_tiles) * NT;
         if (x.wt != held) {
           if (w > 0 && !wait_or_fail(&ctl->wempty, (uint32_t)((w - 1) & 1), fail, status)) break;
@@ -149,10 +147,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
             break;
           }
           tc_mbar_expect_tx(&ctl->afull[s], kAtomA);
-          if (S::KIND == Product::kExpand)
-            tma_load_4d(sa + s * kAtomA, &xmap, j * 64, (int)x.t0, (int)x.b, 0, &ctl->afull[s]);
-          else
-            tma_load_4d(sa + s * kAtomA, &xmap, j * 64, h, (int)x.t0, 0, &ctl->afull[s]);
+          tma_load_4d(sa + s * kAtomA, &xmap, j * 64, h, (int)x.t0, 0, &ctl->afull[s]);
           ctl->loaded = c + 1;
         }
         if (!ok) break;
@@ -168,7 +163,6 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       bool ok = true;
       for (int64_t i = first; ok && i < last; ++i) {
         const Item x = item(i);
-        if (x.limit == 0) continue;
         if (x.wt != held) {
           if (w > 0) tc_commit(&ctl->wempty);             // the products with the old weights
           ok = wait_or_fail(&ctl->wfull, (uint32_t)(w & 1), fail, status);
@@ -200,14 +194,13 @@ __global__ void __launch_bounds__(kPrThreads, 1)
     int n = 0;
     for (int64_t i = first; i < last; ++i) {
       const Item x = item(i);
-      if (x.limit == 0) continue;
       const int h = (int)(x.wt / a.dim_tiles), d0 = (int)(x.wt % a.dim_tiles) * NT, buf = n & 1;
       const bool ok = wait_or_fail(&ctl->tfull[buf], (uint32_t)((n / 2) & 1), fail, status);
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after();
       const int r = warp * 32 + lane;
       const bool live = r < x.limit;
-      const int64_t orow = S::KIND == Product::kExpand ? (x.b * a.H + h) * a.rows + x.t0 + r : (x.t0 + r) * a.H + h;
+      const int64_t orow = (x.t0 + r) * a.H + h;
       uint4* dst = reinterpret_cast<uint4*>(a.out + orow * a.out_row + d0);
 #pragma unroll
       for (int c = 0; c < NT / 32; ++c) {
@@ -245,20 +238,211 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   if (warp == 4) tc_dealloc(tbase, S::TMEM);
 }
 
+// ------------------------------------------------------------------------------------------------ expand
+constexpr int kExTok = 256, kExStages = 3, kExThreads = 320;   // eight warps of stores, one of loads, one of products
+constexpr int kExAtomW = 128 * 128, kExAtomX = kExTok * 128;
+
+struct ExCtl {
+  uint64_t wfull, wempty, xfull[kExStages], xempty[kExStages], tfull[2], tempty[2];
+  uint32_t tslot;
+  int fail, loaded, weights, issued;
+};
+static_assert(sizeof(ExCtl) <= 256, "control block");
+
+template <bool BF16>
+__global__ void __launch_bounds__(kExThreads, 1)
+    expand_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap,
+                  const ProductArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+  const int kc = a.K / 64;
+  uint8_t* sx = sm + kc * kExAtomW;                       // [kExStages] 256 tokens x 64 of K
+  ExCtl* ctl = reinterpret_cast<ExCtl*>(sx + kExStages * kExAtomX);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t first = a.items * blockIdx.x / gridDim.x, last = a.items * (blockIdx.x + 1) / gridDim.x;
+
+  // the items of this CTA's run whose tokens exist
+  struct Items {
+    const ProductArgs& a;
+    int64_t i, last;
+    int wt, b, h, d0, limit;    // weight tile, entry, head, first dim, tokens of the block that exist
+    int64_t t0;
+    __device__ Items(const ProductArgs& args, int64_t f, int64_t l) : a(args), i(f), last(l) {}
+    __device__ bool next() {
+      for (; i < last; ++i) {
+        const int64_t per = a.B * a.blocks, r = i % per;
+        wt = (int)(i / per);
+        b = (int)(r / a.blocks);
+        t0 = r % a.blocks * kExTok;
+        const int64_t n = std::min<int64_t>(a.rows, a.T_len[b]) - t0;
+        if (n <= 0) continue;
+        limit = (int)std::min<int64_t>(kExTok, n);
+        h = wt / a.dim_tiles;
+        d0 = wt % a.dim_tiles * 128;
+        ++i;
+        return true;
+      }
+      return false;
+    }
+  };
+
+  if (warp == 8) tc_alloc(&ctl->tslot, 512);
+  if (threadIdx.x == 0) {
+    tc_mbar_init(&ctl->wfull, 1);
+    tc_mbar_init(&ctl->wempty, 1);
+    for (int s = 0; s < kExStages; ++s) {
+      tc_mbar_init(&ctl->xfull[s], 1);
+      tc_mbar_init(&ctl->xempty[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      tc_mbar_init(&ctl->tfull[s], 1);
+      tc_mbar_init(&ctl->tempty[s], 8);
+    }
+    tc_fence_mbar_init();
+    ctl->fail = ctl->loaded = ctl->weights = ctl->issued = 0;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tbase = ctl->tslot;
+  volatile int* fail = &ctl->fail;
+  uint32_t* status = &g_status_product;
+  Items it(a, first, last);
+
+  if (warp == 8) {
+    if (elect_one()) {
+      int held = -1, w = 0, s = 0, lap = 0;
+      bool ok = true;
+      while (ok && it.next()) {
+        if (it.wt != held) {
+          if (w > 0 && !wait_or_fail(&ctl->wempty, (uint32_t)((w - 1) & 1), fail, status)) break;
+          tc_mbar_expect_tx(&ctl->wfull, kc * kExAtomW);
+          for (int j = 0; j < kc; ++j) tma_load_4d(sm + j * kExAtomW, &wmap, j * 64, it.d0, it.h, 0, &ctl->wfull);
+          held = it.wt;
+          ctl->weights = ++w;
+        }
+        for (int j = 0; j < kc; ++j) {
+          if (lap > 0 && !wait_or_fail(&ctl->xempty[s], (uint32_t)((lap - 1) & 1), fail, status)) {
+            ok = false;
+            break;
+          }
+          tc_mbar_expect_tx(&ctl->xfull[s], kExAtomX);
+          tma_load_4d(sx + s * kExAtomX, &xmap, j * 64, (int)it.t0, it.b, 0, &ctl->xfull[s]);
+          ctl->loaded = lap * kExStages + s + 1;
+          if (++s == kExStages) {
+            s = 0;
+            ++lap;
+          }
+        }
+      }
+    }
+  } else if (warp == 9) {
+    if (elect_one()) {
+      constexpr uint32_t id = tc_idesc(BF16, 128, kExTok, false, false);
+      const Desc wd = tc_desc_sw128(smem_addr(sm)), xd = tc_desc_sw128(smem_addr(sx));
+      int held = -1, w = 0, n = 0, s = 0, lap = 0;
+      bool ok = true;
+      while (ok && it.next()) {
+        if (it.wt != held) {
+          if (w > 0) tc_commit(&ctl->wempty);             // the products with the old weights
+          ok = wait_or_fail(&ctl->wfull, (uint32_t)(w & 1), fail, status);
+          held = it.wt;
+          ++w;
+        }
+        const int buf = n & 1;
+        if (ok && n >= 2) ok = wait_or_fail(&ctl->tempty[buf], (uint32_t)((n / 2 - 1) & 1), fail, status);
+        for (int j = 0; ok && j < kc; ++j) {
+          ok = wait_or_fail(&ctl->xfull[s], (uint32_t)(lap & 1), fail, status);
+          if (!ok) break;
+          tc_fence_after();
+          const Desc ws = wd.at(j * kExAtomW).opaque(), xs = xd.at(s * kExAtomX).opaque();
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            tc_mma_ss(tbase + (uint32_t)(buf * kExTok), ws.at(kk * 32), xs.at(kk * 32), id, j > 0 || kk > 0 ? 1u : 0u);
+          tc_commit(&ctl->xempty[s]);
+          if (++s == kExStages) {
+            s = 0;
+            ++lap;
+          }
+        }
+        if (!ok) break;
+        tc_commit(&ctl->tfull[buf]);
+        ctl->issued = ++n;
+      }
+    }
+  } else {
+    // stores: lane = dim, half of the block's tokens; neighbouring lanes swap, so that each holds two dims of every
+    // other token
+    const int q = warp & 3, half = warp >> 2;
+    const uint32_t lanes = (uint32_t)(q * 32) << 16;
+    const bool odd = lane & 1;
+    int n = 0;
+    while (it.next()) {
+      const int buf = n & 1;
+      const bool ok = wait_or_fail(&ctl->tfull[buf], (uint32_t)((n / 2) & 1), fail, status);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      tc_fence_after();
+      const int dim = it.d0 + q * 32 + lane;
+      uint16_t* dst = a.out + (((int64_t)it.b * a.H + it.h) * a.rows + it.t0 + half * 128 + (odd ? 1 : 0)) * a.out_row + (dim & ~1);
+      const int left = dim < a.n_dim ? it.limit - half * 128 - (odd ? 1 : 0) : 0;   // its tokens c with c < left exist
+#pragma unroll 1
+      for (int c0 = 0; c0 < 128; c0 += 32) {
+        float v[32];
+        tm_load<32>(tbase + lanes + (uint32_t)(buf * kExTok + half * 128 + c0), v);
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+          const float y = __shfl_xor_sync(0xffffffffu, odd ? v[c] : v[c + 1], 1);
+          const uint32_t x = odd ? pack2<BF16>(y, v[c + 1]) : pack2<BF16>(v[c], y);
+          if (c0 + c < left) *reinterpret_cast<uint32_t*>(dst + (int64_t)(c0 + c) * a.out_row) = x;
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc_mbar_arrive(&ctl->tempty[buf]);
+      ++n;
+    }
+  }
+  // teardown: on a failure wait (bounded) for the copies and products already issued
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && ctl->fail) {
+    if (ctl->weights > 0) tc_mbar_wait(&ctl->wfull, (uint32_t)((ctl->weights - 1) & 1), kRoleWaitNs);
+    for (int c = std::max(0, ctl->loaded - kExStages); c < ctl->loaded; ++c)
+      tc_mbar_wait(&ctl->xfull[c % kExStages], (uint32_t)((c / kExStages) & 1), kRoleWaitNs);
+    if (ctl->issued > 0)
+      tc_mbar_wait(&ctl->tfull[(ctl->issued - 1) & 1], (uint32_t)(((ctl->issued - 1) / 2) & 1), kRoleWaitNs);
+  }
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8) tc_dealloc(tbase, 512);
+}
+
+template <bool BF16>
+cudaError_t launch_expand(const ProductCall& c, ProductArgs a, cudaStream_t st) {
+  const int64_t H = c.H, d = c.nope + c.v_dim, r = c.rank, row = r + c.rope;
+  a.dim_tiles = (int)ceil_div(d, 128);
+  a.blocks = ceil_div(a.rows, kExTok);
+  a.items = H * a.dim_tiles * a.blocks * c.B;
+  CUtensorMap xm, wm;
+  cudaError_t e = encode_map(&xm, c.x, {row, c.T_cap, c.B, 1}, {row, c.T_cap * row, c.B * c.T_cap * row}, kExTok, 1);
+  if (e == cudaSuccess) e = encode_map(&wm, c.w, {r, d, H, 1}, {r, d * r, H * d * r}, 128, 1);
+  if (e != cudaSuccess) return e;
+  constexpr int smem = 8 * kExAtomW + kExStages * kExAtomX + 256 + 1024;   // one CTA an SM, at either rank
+  static_assert(smem <= 227 * 1024 && smem >= 116 * 1024, "shared memory");
+  e = cudaFuncSetAttribute(expand_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  expand_kernel<BF16><<<(unsigned)std::min<int64_t>(a.items, kNumSMs), kExThreads, smem, st>>>(xm, wm, a);
+  return cudaPeekAtLastError();
+}
+
 template <class S>
 cudaError_t launch_shape(const ProductCall& c, ProductArgs a, cudaStream_t st) {
   const int64_t H = c.H, d = c.nope + c.v_dim, r = c.rank;
   a.dim_tiles = a.n_dim / S::NT;
-  a.items = H * a.dim_tiles * a.blocks * (S::KIND == Product::kExpand ? c.B : 1);
+  a.items = H * a.dim_tiles * a.blocks;
   CUtensorMap xm, wm;
-  cudaError_t e;
-  if (S::KIND == Product::kExpand) {
-    const int64_t row = r + c.rope;
-    e = encode_map(&xm, c.x, {row, c.T_cap, c.B, 1}, {row, c.T_cap * row, c.B * c.T_cap * row}, kTok, 1);
-  } else {
-    const int64_t row = a.x_row;
-    e = encode_map(&xm, c.x, {row, H, a.rows, 1}, {row, H * row, a.rows * H * row}, 1, kTok);
-  }
+  const int64_t row = a.x_row;
+  cudaError_t e = encode_map(&xm, c.x, {row, H, a.rows, 1}, {row, H * row, a.rows * H * row}, 1, kTok);
   if (e == cudaSuccess)
     e = encode_map(&wm, c.w, {r, d, H, 1}, {r, d * r, H * d * r}, S::W_MN ? a.K : S::NT, 1);
   if (e != cudaSuccess) return e;
@@ -273,7 +457,7 @@ cudaError_t launch_shape(const ProductCall& c, ProductArgs a, cudaStream_t st) {
 template <bool BF16, Product KIND>
 cudaError_t launch_kind(const ProductCall& c, const ProductArgs& a, cudaStream_t st) {
   // 64-dim tiles where 128 would not divide the dims, or would leave SMs without work
-  const int64_t wide = (int64_t)c.H * (a.n_dim / 128) * a.blocks * (KIND == Product::kExpand ? c.B : 1);
+  const int64_t wide = (int64_t)c.H * (a.n_dim / 128) * a.blocks;
   if (a.n_dim % 128 != 0 || wide < kNumSMs) return launch_shape<PrShape<BF16, KIND, 64>>(c, a, st);
   return launch_shape<PrShape<BF16, KIND, 128>>(c, a, st);
 }
@@ -305,7 +489,7 @@ cudaError_t launch_t(const ProductCall& c, cudaStream_t st) {
     case Product::kExpand:
       a.K = c.rank;
       a.n_dim = a.out_row = c.nope + c.v_dim;
-      return launch_kind<BF16, Product::kExpand>(c, a, st);
+      return launch_expand<BF16>(c, a, st);
   }
   return cudaErrorInvalidValue;
 }
