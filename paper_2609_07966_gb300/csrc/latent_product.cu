@@ -317,7 +317,8 @@ __global__ void __launch_bounds__(kExThreads, 1)
         if (it.wt != held) {
           if (w > 0 && !wait_or_fail(&ctl->wempty, (uint32_t)((w - 1) & 1), fail, status)) break;
           tc_mbar_expect_tx(&ctl->wfull, kc * kExAtomW);
-          for (int j = 0; j < kc; ++j) tma_load_4d(sm + j * kExAtomW, &wmap, j * 64, it.d0, it.h, 0, &ctl->wfull);
+          for (int j = 0; j < kc; ++j)
+            tma_load_4d(sm + j * kExAtomW, &wmap, j * 64, 0, 0, (it.h * a.out_row + it.d0) / 32, &ctl->wfull);
           held = it.wt;
           ctl->weights = ++w;
         }
@@ -371,34 +372,37 @@ __global__ void __launch_bounds__(kExThreads, 1)
       }
     }
   } else {
-    // stores: lane = dim, half of the block's tokens; neighbouring lanes swap, so that each holds two dims of every
-    // other token
+    // stores: lane = dim (in the order of the weights' rows), half of the block's tokens; the lanes exchange values, so
+    // that each stores eight dims of a token
     const int q = warp & 3, half = warp >> 2;
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
-    const bool odd = lane & 1;
     int n = 0;
     while (it.next()) {
       const int buf = n & 1;
       const bool ok = wait_or_fail(&ctl->tfull[buf], (uint32_t)((n / 2) & 1), fail, status);
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after();
-      const int dim = it.d0 + q * 32 + lane;
-      uint16_t* dst = a.out + (((int64_t)it.b * a.H + it.h) * a.rows + it.t0 + half * 128 + (odd ? 1 : 0)) * a.out_row + (dim & ~1);
-      const int left = dim < a.n_dim ? it.limit - half * 128 - (odd ? 1 : 0) : 0;   // its tokens c with c < left exist
-#pragma unroll 1
-      for (int c0 = 0; c0 < 128; c0 += 32) {
-        float v[32];
-        tm_load<32>(tbase + lanes + (uint32_t)(buf * kExTok + half * 128 + c0), v);
+      // the accumulator is given back before the stores, not behind them
+      float v[128];
 #pragma unroll
-        for (int c = 0; c < 32; c += 2) {
-          const float y = __shfl_xor_sync(0xffffffffu, odd ? v[c] : v[c + 1], 1);
-          const uint32_t x = odd ? pack2<BF16>(y, v[c + 1]) : pack2<BF16>(v[c], y);
-          if (c0 + c < left) *reinterpret_cast<uint32_t*>(dst + (int64_t)(c0 + c) * a.out_row) = x;
-        }
-      }
+      for (int c = 0; c < 4; ++c)
+        tm_issue<32>(tbase + lanes + (uint32_t)(buf * kExTok + half * 128 + c * 32), *reinterpret_cast<float(*)[32]>(&v[c * 32]));
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tm_wait<32>(*reinterpret_cast<float(*)[32]>(&v[c * 32]));
       tc_fence_before();
       __syncwarp();
       if (lane == 0) tc_mbar_arrive(&ctl->tempty[buf]);
+      const int dim = it.d0 + q * 32 + (lane & 3) * 8, tok = half * 128 + (lane >> 2);   // of its first store
+      uint16_t* dst = a.out + (((int64_t)it.b * a.H + it.h) * a.rows + it.t0 + tok) * a.out_row + dim;
+      const int left = dim < a.n_dim ? it.limit - tok : 0;         // its tokens c with c < left exist
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint4 x[4];
+        gather_rows<BF16>(*reinterpret_cast<float(*)[32]>(&v[c * 32]), lane, x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (c * 32 + 8 * k < left) *reinterpret_cast<uint4*>(dst + (int64_t)(c * 32 + 8 * k) * a.out_row) = x[k];
+      }
       ++n;
     }
   }
@@ -425,7 +429,9 @@ cudaError_t launch_expand(const ProductCall& c, ProductArgs a, cudaStream_t st) 
   a.items = H * a.dim_tiles * a.blocks * c.B;
   CUtensorMap xm, wm;
   cudaError_t e = encode_map(&xm, c.x, {row, c.T_cap, c.B, 1}, {row, c.T_cap * row, c.B * c.T_cap * row}, kExTok, 1);
-  if (e == cudaSuccess) e = encode_map(&wm, c.w, {r, d, H, 1}, {r, d * r, H * d * r}, 128, 1);
+  // a tile's rows in the order that gather_rows wants: row 4 s + g of 32 is dim 8 g + s (past a head's dims it reads
+  // the next head's, whose outputs are not stored)
+  if (e == cudaSuccess) e = encode_map(&wm, c.w, {r, 4, 8, H * d / 32}, {8 * r, r, 32 * r}, 4, 8, 4);
   if (e != cudaSuccess) return e;
   constexpr int smem = 8 * kExAtomW + kExStages * kExAtomX + 256 + 1024;   // one CTA an SM, at either rank
   static_assert(smem <= 227 * 1024 && smem >= 116 * 1024, "shared memory");

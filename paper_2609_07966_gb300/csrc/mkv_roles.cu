@@ -25,13 +25,13 @@ EncodeTiled encoder() {
 
 // fp16 and bf16 tensors alike: a map only moves 16-bit elements, and zero fill is the same bits.
 cudaError_t encode_map(CUtensorMap* m, const void* base, const int64_t (&dims)[4], const int64_t (&strides)[3],
-                       int box1, int box2) {
+                       int box1, int box2, int box3) {
   const EncodeTiled enc = encoder();
   if (enc == nullptr) return cudaErrorNotSupported;
   cuuint64_t d[4], s[3];
   for (int i = 0; i < 4; ++i) d[i] = (cuuint64_t)dims[i];
   for (int i = 0; i < 3; ++i) s[i] = (cuuint64_t)strides[i] * 2;
-  const cuuint32_t box[4] = {64, (cuuint32_t)box1, (cuuint32_t)box2, 1};
+  const cuuint32_t box[4] = {64, (cuuint32_t)box1, (cuuint32_t)box2, (cuuint32_t)box3};
   const cuuint32_t es[4] = {1, 1, 1, 1};
   const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base), d, s, box, es,
                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,

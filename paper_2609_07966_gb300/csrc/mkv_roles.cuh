@@ -256,6 +256,32 @@ __device__ __forceinline__ bool bad_pairs(uint4& x) {
   return any;
 }
 
+// 32 columns of a warp whose lane i holds output value 8 (i % 4) + i / 4 of each: rounded and exchanged between lanes so
+// that lane i holds the eight values 8 (i % 4) .. + 7 of column 8 k + i / 4 in out[k] (three rounds of pairwise swaps);
+// four neighbouring lanes then store 64 neighbouring bytes.
+template <bool BF16>
+__device__ __forceinline__ void gather_rows(const float (&v)[32], int lane, uint4 (&out)[4]) {
+  const bool b0 = lane & 4, b1 = lane & 8, b2 = lane & 16;
+  uint32_t h[16];                 // two values of column 2 p + b0
+#pragma unroll
+  for (int p = 0; p < 16; ++p) {
+    const float y = __shfl_xor_sync(0xffffffffu, b0 ? v[2 * p] : v[2 * p + 1], 4);
+    h[p] = b0 ? pack2<BF16>(y, v[2 * p + 1]) : pack2<BF16>(v[2 * p], y);
+  }
+  uint2 w[8];                     // four values of column 4 p + 2 b1 + b0
+#pragma unroll
+  for (int p = 0; p < 8; ++p) {
+    const uint32_t y = __shfl_xor_sync(0xffffffffu, b1 ? h[2 * p] : h[2 * p + 1], 8);
+    w[p] = b1 ? make_uint2(y, h[2 * p + 1]) : make_uint2(h[2 * p], y);
+  }
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const uint2 s = b2 ? w[2 * p] : w[2 * p + 1];
+    const uint32_t y0 = __shfl_xor_sync(0xffffffffu, s.x, 16), y1 = __shfl_xor_sync(0xffffffffu, s.y, 16);
+    out[p] = b2 ? make_uint4(y0, y1, w[2 * p + 1].x, w[2 * p + 1].y) : make_uint4(w[2 * p].x, w[2 * p].y, y0, y1);
+  }
+}
+
 // A reduction of each of C columns over the warp's 32 lanes: on return v[0] of lane i holds column
 // i / (32 / C).
 template <int C, typename Op>
@@ -275,8 +301,8 @@ __device__ __forceinline__ void reduce_columns(float (&v)[C], int lane, Op op) {
 }
 
 // A 4-D tensor map of 16-bit elements: dims and strides in elements (innermost stride 1), a box of
-// 64 x box1 x box2 x 1 with the 128-byte swizzle; what lies outside reads as zero.
+// 64 x box1 x box2 x box3 with the 128-byte swizzle; what lies outside reads as zero.
 cudaError_t encode_map(CUtensorMap* m, const void* base, const int64_t (&dims)[4], const int64_t (&strides)[3],
-                       int box1, int box2);
+                       int box1, int box2, int box3 = 1);
 
 }  // namespace mkv
