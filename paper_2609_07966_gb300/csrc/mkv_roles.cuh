@@ -188,6 +188,32 @@ __device__ __forceinline__ void tm_load(uint32_t addr, float (&v)[C]) {
   tm_issue<C>(addr, v);
   tm_wait<C>(v);
 }
+// 16 tensor-memory lanes (an accumulator of 64 rows has 16 in each warp's quarter): lanes 0..15 of the warp get
+// columns 0 .. C - 1 of them, lanes 16..31 columns C .. 2 C - 1.
+template <int C>
+__device__ __forceinline__ void tm_load_halves(uint32_t addr, float (&v)[C]);
+template <>
+__device__ __forceinline__ void tm_load_halves<4>(uint32_t addr, float (&v)[4]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x32bx2.x4.b32 {%0,%1,%2,%3}, [%4], 4;\n"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3])
+               : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]) : : "memory");
+}
+template <>
+__device__ __forceinline__ void tm_load_halves<8>(uint32_t addr, float (&v)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.16x32bx2.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8], 8;\n"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+               : "r"(addr));
+  tm_wait<8>(v);
+}
+template <>
+__device__ __forceinline__ void tm_load_halves<16>(uint32_t addr, float (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x32bx2.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16], 16;\n"
+      : MKV_OUT16(MKV_EQF, v, 0)
+      : "r"(addr));
+  tm_wait<16>(v);
+}
 // The stores complete at tm_store_wait().
 template <int C>
 __device__ __forceinline__ void tm_store(uint32_t addr, const float (&v)[C]);
@@ -282,11 +308,12 @@ __device__ __forceinline__ void gather_rows(const float (&v)[32], int lane, uint
   }
 }
 
-// A reduction of each of C columns over the warp's 32 lanes: on return v[0] of lane i holds column
-// i / (32 / C).
-template <int C, typename Op>
+// A reduction of each of C columns over each L neighbouring lanes: on return v[0] of lane i holds column
+// (i % L) / (L / C).
+template <int L, int C, typename Op>
 __device__ __forceinline__ void reduce_columns(float (&v)[C], int lane, Op op) {
-  int lb = 16;
+  static_assert(C <= L, "a column for every lane at most");
+  int lb = L / 2;
 #pragma unroll
   for (int w = C / 2; w >= 1; w >>= 1) {
     const bool up = (lane & lb) != 0;

@@ -17,7 +17,7 @@
 // entries balance too).  A unit inside one run is written directly; the pieces of a unit that several runs share go
 // to the workspace and join_kernel adds them up.
 //
-// Roles: warps 0..4g-1 are the softmax (a thread holds one key and N / g rows), then one warp loads chunks by TMA
+// Roles: warps 0..4g-1 are the softmax (a thread holds one key and some rows), then one warp loads chunks by TMA
 // into a ring of slots and one issues products, taking whichever is ready: a finished tile's second product
 // first (it frees slots), else the next chunk of the scores.
 //
@@ -80,7 +80,10 @@ struct Shape {
   static constexpr int MV = DV >= 128 ? 128 : 64;          // value dims per product (its M)
   static constexpr int NB = DV / MV;                       // O^T blocks
   static constexpr int NG = N > 64 ? 4 : 2;                // softmax groups of 128 threads
-  static constexpr int C = N / NG;                         // rows a softmax thread holds
+  static constexpr int C = N / NG;                         // rows of a softmax group
+  // A tile of 64 keys takes 16 tensor-memory lanes of each warp's quarter: the warp's halves then share its rows, so
+  // that no lane idles.  L lanes hold one set of CS rows.
+  static constexpr int L = KT == 64 ? 16 : 32, CS = C * L / 32;
   static constexpr int SOFT = NG * 128, THREADS = SOFT + 128;   // (two of the last four warps idle)
   // registers a thread: what a launch of THREADS gets, and its split between softmax and the others
   static constexpr int RL = NG == 2 ? 168 : 96, RS = NG == 2 ? 208 : 104, RO = NG == 2 ? 88 : 64;
@@ -186,12 +189,27 @@ struct Pieces {
   }
 };
 
+struct MaxOp {
+  __device__ __forceinline__ float operator()(float x, float y) const { return fmaxf(x, y); }
+};
+struct AddOp {
+  __device__ __forceinline__ float operator()(float x, float y) const { return x + y; }
+};
+// A reduction over one warp quarter's keys: its results for the thread's rows in red[0 .. CS - 1], visible to the
+// softmax group on return.
+template <class S, typename Op>
+__device__ __forceinline__ void group_reduce(float (&w)[S::CS], float* red, int lane, int grp, Op op) {
+  reduce_columns<S::L>(w, lane, op);
+  if ((lane & (S::L / S::CS - 1)) == 0) red[(lane & (S::L - 1)) / (S::L / S::CS)] = w[0];
+  bar_sync(1 + grp, 128);
+}
+
 template <class S>
 __global__ void __launch_bounds__(S::THREADS, 1)
     rows_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                 const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap ktmap,
                 const __grid_constant__ CUtensorMap vtmap, const RowsArgs a) {
-  constexpr int KT = S::KT, N = S::N, C = S::C, CH = S::CH;
+  constexpr int KT = S::KT, N = S::N, C = S::C, CH = S::CH, CS = S::CS, L = S::L;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
   RowsCtl* ctl = reinterpret_cast<RowsCtl*>(sm + S::CTL_OFF);
@@ -450,9 +468,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
     uint32_t* vis = reinterpret_cast<uint32_t*>(sm + S::VIS_OFF);
     const int q = warp & 3, grp = warp >> 2;             // lane quarter (keys), rows grp C .. + C - 1
     const uint32_t lanes = (uint32_t)(q * 32) << 16;
-    // a tile of 64 keys takes lanes 0..15 of each quarter, one of 128 all of them
-    const bool live = KT == 128 || lane < 16;
-    const int key = KT == 128 ? q * 32 + lane : q * 16 + (lane & 15);
+    const int key = q * L + (lane & (L - 1));            // this thread's key of a tile, and its first row
+    const int col0 = grp * C + (L == 16 ? (lane >> 4) * CS : 0);
     // A warp whose wait ran out stops waiting but still meets the barriers, so none is left waiting.
     bool dead = false;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -479,48 +496,48 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         }
         bar_sync(5, S::SOFT);
       }
-      float m[C], l[C];
+      float m[CS], l[CS];
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
+      for (int c = 0; c < CS; ++c) {
         m[c] = kNoMax;
         l[c] = 0.f;
       }
+      const float4* r4 = reinterpret_cast<const float4*>(red + col0);
       for (int t = 0; t < nt; ++t, ++g) {
         const int pb = g % S::NP;
         const bool tr = has_tree && t == nt - 1;
         const int valid = tr ? a.n : std::min(KT, p.len - (p.t0 + t) * KT);   // keys of the tile that exist
         wait(&ctl->sfull[g & 1], (uint32_t)((g >> 1) & 1));
-        float v[C];
-        tm_load<C>(tbase + lanes + (uint32_t)((g & 1) * N + grp * C), v);
-        const bool exists = live && key < valid;
-        // the rows of this thread that see its key
-        uint32_t see = exists ? 0xffffffffu : 0u;
-        if (tr && exists) see = vis[key * S::VW + grp * C / 32] >> (grp * C % 32);
+        float v[CS];
+        if constexpr (L == 16)
+          tm_load_halves<CS>(tbase + lanes + (uint32_t)((g & 1) * N + grp * C), v);
+        else
+          tm_load<CS>(tbase + lanes + (uint32_t)((g & 1) * N + grp * C), v);
         bool over = false;
-        if (valid == KT && !tr && KT == 128) {
+        if (valid == KT && !tr) {
 #pragma unroll
-          for (int c = 0; c < C; ++c) {
+          for (int c = 0; c < CS; ++c) {
             v[c] *= a.scale_log2;
             over |= v[c] > m[c] + kRaise;
           }
         } else {
+          // the rows of this thread that see its key
+          uint32_t see = key < valid ? 0xffffffffu : 0u;
+          if (tr && key < valid) see = vis[key * S::VW + col0 / 32] >> (col0 % 32);
 #pragma unroll
-          for (int c = 0; c < C; ++c) {
+          for (int c = 0; c < CS; ++c) {
             v[c] = see >> c & 1 ? v[c] * a.scale_log2 : -INFINITY;
             over |= v[c] > m[c] + kRaise;
           }
         }
         if (bar_or(1 + grp, 128, over)) {
           // some score passed its row's maximum: raise the maxima to the tile's, rescale sums and outputs
-          float w[C];
+          float w[CS];
 #pragma unroll
-          for (int c = 0; c < C; ++c) w[c] = v[c];
-          reduce_columns<C>(w, lane, [](float x, float y) { return fmaxf(x, y); });
-          if ((lane & (32 / C - 1)) == 0) red[q * N + grp * C + lane / (32 / C)] = w[0];
-          bar_sync(1 + grp, 128);
-          const float4* r4 = reinterpret_cast<const float4*>(red + grp * C);
+          for (int c = 0; c < CS; ++c) w[c] = v[c];
+          group_reduce<S>(w, red + q * N + col0, lane, grp, MaxOp());
 #pragma unroll
-          for (int c = 0; c < C / 4; ++c) {
+          for (int c = 0; c < CS / 4; ++c) {
             const float4 x0 = r4[c], x1 = r4[N / 4 + c], x2 = r4[2 * N / 4 + c], x3 = r4[3 * N / 4 + c];
             const float mx[4] = {fmax3(x0.x, x1.x, fmaxf(x2.x, x3.x)), fmax3(x0.y, x1.y, fmaxf(x2.y, x3.y)),
                                  fmax3(x0.z, x1.z, fmaxf(x2.z, x3.z)), fmax3(x0.w, x1.w, fmaxf(x2.w, x3.w))};
@@ -533,35 +550,44 @@ __global__ void __launch_bounds__(S::THREADS, 1)
             }
           }
           if (t > 0) {
+            // every thread needs its whole group's factors here: passed round through `red`
+            bar_sync(1 + grp, 128);
+            if (q == 0 && (lane & (L - 1)) == 0) {
+#pragma unroll
+              for (int c = 0; c < CS; ++c) red[col0 + c] = w[c];
+            }
+            bar_sync(1 + grp, 128);
             wait(&ctl->pvdone[(g - 1) % S::NP], (uint32_t)(((g - 1) / S::NP) & 1));
 #pragma unroll 1
             for (int mb = 0; mb < S::NB; ++mb) {
               float o[C];
               tm_load<C>(tO + lanes + (uint32_t)(mb * N + grp * C), o);
 #pragma unroll
-              for (int c = 0; c < C; ++c) o[c] *= w[c];
+              for (int c = 0; c < C; ++c) o[c] *= red[grp * C + c];
               tm_store<C>(tO + lanes + (uint32_t)(mb * N + grp * C), o);
             }
             tm_store_wait();
           }
         }
         // weights, their sums, and the rounded weights for the second product
-        uint32_t pk[C / 2];
+        uint32_t pk[CS / 2];
 #pragma unroll
-        for (int c = 0; c < C; c += 2) {
+        for (int c = 0; c < CS; c += 2) {
           const float p0 = ex2_approx(v[c] - m[c] + kOffset), p1 = ex2_approx(v[c + 1] - m[c + 1] + kOffset);
           l[c] += p0;
           l[c + 1] += p1;
           pk[c / 2] = pack2<S::BF16>(p0, p1);
         }
         if (g >= S::NP) wait(&ctl->pvdone[pb], (uint32_t)((g / S::NP - 1) & 1));
-        if (live) {
-          const int col = grp * C;
-          uint8_t* pt = sm + S::P_OFF + pb * S::PBUF + (col / S::PW) * (KT * S::PW * 2);
+        uint8_t* pt = sm + S::P_OFF + pb * S::PBUF + (col0 / S::PW) * (KT * S::PW * 2);
+        if constexpr (CS >= 8) {
 #pragma unroll
-          for (int i = 0; i < C / 8; ++i)
-            *reinterpret_cast<uint4*>(pt + mn_offset<S::PW>(key, (col % S::PW) / 8 + i)) =
+          for (int i = 0; i < CS / 8; ++i)
+            *reinterpret_cast<uint4*>(pt + mn_offset<S::PW>(key, (col0 % S::PW) / 8 + i)) =
                 make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
+        } else {
+          *reinterpret_cast<uint2*>(pt + mn_offset<S::PW>(key, (col0 % S::PW) / 8) + (col0 % 8) * 2) =
+              make_uint2(pk[0], pk[1]);
         }
         // Values that no row may meet must not meet a zero weight either (0 x NaN): slots past the length become
         // zeros; a drafted token's non-finite values become zeros here and are added to the rows that see it at
@@ -593,20 +619,16 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       // -------------------------------------------------------------- this piece's outputs
       wait(&ctl->pvdone[(g - 1) % S::NP], (uint32_t)(((g - 1) / S::NP) & 1));
       const bool gone = bar_or(1 + grp, 128, dead);        // (the group's earlier reads of `red` are done)
-      float w[C];
-#pragma unroll
-      for (int c = 0; c < C; ++c) w[c] = live ? l[c] : 0.f;
-      reduce_columns<C>(w, lane, [](float x, float y) { return x + y; });
-      if ((lane & (32 / C - 1)) == 0) red[q * N + grp * C + lane / (32 / C)] = w[0];
-      bar_sync(1 + grp, 128);
-      const float4* r4 = reinterpret_cast<const float4*>(red + grp * C);
+      group_reduce<S>(l, red + q * N + col0, lane, grp, AddOp());
+      float sum[C];
+      const float4* s4 = reinterpret_cast<const float4*>(red + grp * C);
 #pragma unroll
       for (int c = 0; c < C / 4; ++c) {
-        const float4 x0 = r4[c], x1 = r4[N / 4 + c], x2 = r4[2 * N / 4 + c], x3 = r4[3 * N / 4 + c];
-        l[4 * c] = (x0.x + x1.x) + (x2.x + x3.x);
-        l[4 * c + 1] = (x0.y + x1.y) + (x2.y + x3.y);
-        l[4 * c + 2] = (x0.z + x1.z) + (x2.z + x3.z);
-        l[4 * c + 3] = (x0.w + x1.w) + (x2.w + x3.w);
+        const float4 x0 = s4[c], x1 = s4[N / 4 + c], x2 = s4[2 * N / 4 + c], x3 = s4[3 * N / 4 + c];
+        sum[4 * c] = (x0.x + x1.x) + (x2.x + x3.x);
+        sum[4 * c + 1] = (x0.y + x1.y) + (x2.y + x3.y);
+        sum[4 * c + 2] = (x0.z + x1.z) + (x2.z + x3.z);
+        sum[4 * c + 3] = (x0.w + x1.w) + (x2.w + x3.w);
       }
       if (!gone) {
         const bool whole = nt == p.tiles;
@@ -614,14 +636,17 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         const uint64_t nf = has_tree ? ctl->nonfinite : 0;
         const bool dlive = S::MV == 128 || lane < 16;
         const int dl = S::MV == 128 ? q * 32 + lane : q * 16 + (lane & 15);
-        if (!whole && q == 0 && lane == 0) {
+        if (!whole && q == 0 && (lane & (L - 1)) == 0) {
 #pragma unroll
-          for (int c = 0; c < C; ++c)
-            a.part_ml[slot * N + grp * C + c] = make_float2(l[c] == 0.f ? -INFINITY : m[c], l[c]);
+          for (int c = 0; c < CS; ++c) {
+            const int x = col0 + c;
+            const float all = (red[x] + red[N + x]) + (red[2 * N + x] + red[3 * N + x]);
+            a.part_ml[slot * N + x] = make_float2(all == 0.f ? -INFINITY : m[c], all);
+          }
         }
         if (whole) {
 #pragma unroll
-          for (int c = 0; c < C; ++c) l[c] = l[c] == 0.f ? 0.f : 1.f / l[c];
+          for (int c = 0; c < C; ++c) sum[c] = sum[c] == 0.f ? 0.f : 1.f / sum[c];
         }
 #pragma unroll 1
         for (int mb = 0; mb < S::NB; ++mb) {
@@ -654,7 +679,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
             const bool odd = lane & 1;
 #pragma unroll
             for (int c = 0; c < C; c += 2) {
-              const float x0 = l[c] == 0.f ? 0.f : o[c] * l[c], x1 = l[c + 1] == 0.f ? 0.f : o[c + 1] * l[c + 1];
+              const float x0 = sum[c] == 0.f ? 0.f : o[c] * sum[c];
+              const float x1 = sum[c + 1] == 0.f ? 0.f : o[c + 1] * sum[c + 1];
               const float y = __shfl_xor_sync(0xffffffffu, odd ? x0 : x1, 1);
               const uint32_t h = odd ? pack2<S::BF16>(y, x1) : pack2<S::BF16>(x0, y);
               const int r = grp * C + c + (odd ? 1 : 0), row = row0 + r;
