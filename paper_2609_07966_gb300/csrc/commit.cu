@@ -8,7 +8,7 @@
 // prompt's rows are shared by as many CTAs as the GPU holds, and a second launch stores the lengths.
 #include <algorithm>
 
-#include "mkv_common.cuh"
+#include "mkv_roles.cuh"
 #include "mkv_rows.h"
 
 namespace mkv {
@@ -18,15 +18,6 @@ namespace {
 __device__ uint32_t g_status_commit;
 
 constexpr int kCommitThreads = 512;
-
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");
-}
 
 // Whether entry b's path fits (all threads of the CTA take part); its length and path length.
 __device__ __forceinline__ bool path_fits(const CommitCall& a, int b, int& t0, int& np) {

@@ -12,10 +12,13 @@
 // (its first dv dims): one load of a row serves both products.  Accumulators live in tensor memory: S^T twice
 // (tile t + 1's scores are computed under tile t's softmax), O^T as dv / 128 blocks of N columns.
 //
-// Work: the key tiles of all (entry, key head, row block) units, the drafted tokens as one more tile at the end of
-// each unit, are laid end to end and every CTA takes an equal run (the lengths are read on the device, so unequal
-// entries balance too).  A unit inside one run is written directly; the pieces of a unit that several runs share go
-// to the workspace and join_kernel adds them up.
+// Work: a unit is one (entry, key head, row block); its key tiles are the entry's cached ones and, last, the drafted
+// tokens'.  The lengths are read on the device.  Two ways to share the units out, chosen by plan_rows:
+//   clusters  a cluster of CTAs per unit, each an equal run of its tiles; the pieces are joined through distributed
+//             shared memory (each CTA sums a slice of the dims over the others'), so one launch does it all;
+//   runs      the tiles of all units laid end to end, an equal run for every CTA, whatever the entries' lengths; a unit
+//             inside one run is written directly, the pieces of a unit that several runs share go to the workspace
+//             and join_kernel adds them up.
 //
 // Roles: warps 0..4g-1 are the softmax (a thread holds one key and some rows), then one warp loads chunks by TMA
 // into a ring of slots and one issues products, taking whichever is ready: a finished tile's second product
@@ -57,6 +60,7 @@ struct RowsArgs {
   int B, n, H, Hkv, G;              // G: query heads per key head (latent: H)
   int R, row_blocks;                // rows per (entry, key head): n G; their blocks of N
   int log_g;                        // FP16 caches: log2 G
+  int cluster, log_cluster;         // CTAs a unit, joined in the kernel (a power of two); 0: runs over all units
   bool tree;
   int64_t T_cap;
   float scale_log2;
@@ -115,6 +119,7 @@ struct Shape {
   static_assert(COLS <= 512 && ALLOC <= 227 * 1024, "does not fit an SM");
 };
 
+constexpr int kMaxCluster = 8;      // CTAs of a cluster: the largest portable size
 constexpr int kMaxSlotsRing = 12;
 struct RowsCtl {
   uint64_t qfull, qempty, ofree, kfull[8], vfull[8], empty[kMaxSlotsRing], rempty[4], sfull[2], pfull[2], pvdone[2];
@@ -204,6 +209,26 @@ __device__ __forceinline__ void group_reduce(float (&w)[S::CS], float* red, int 
   bar_sync(1 + grp, 128);
 }
 
+// Adds to dim d of each of C rows (the first `rows` of them from row `row` of the unit on) the non-finite values of the
+// drafted tokens `nf` that it sees.
+template <class S>
+__device__ __forceinline__ void add_non_finite(const RowsArgs& a, uint64_t nf, int b, int kvh, int row, int rows, int d,
+                                            float (&o)[S::C]) {
+  for (int c = 0; c < S::C && c < rows; ++c) {
+    float add = 0.f;
+    for (uint64_t bits = nf & a.mask[(int64_t)b * a.n + (row + c) / a.G]; bits; bits &= bits - 1) {
+      const int j = __ffsll((long long)bits) - 1;
+      const uint16_t y = j < a.n ? a.v_tree[((int64_t)b * a.n + j) * a.v_tok + kvh * a.v_head + d] : 0;
+      if (non_finite<S::BF16>(y)) add += widen<S::BF16>(y);
+    }
+#pragma unroll
+    for (int e = 0; e < S::C; ++e) o[e] += e == c ? add : 0.f;
+  }
+}
+
+// First tile of CTA i of the 2^k that share a unit of `tiles`.
+__device__ __forceinline__ int cluster_tile(int tiles, int i, int k) { return (int)((int64_t)tiles * i >> k); }
+
 template <class S>
 __global__ void __launch_bounds__(S::THREADS, 1)
     rows_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
@@ -241,44 +266,56 @@ __global__ void __launch_bounds__(S::THREADS, 1)
     }
     pdl_wait_and_trigger();
     const int per = a.Hkv * a.row_blocks;
-    const int len_mine = lane < a.B ? entry_len(a, lane) : 0;
-    const int mine0 = lane < a.B ? unit_tiles<KT>(a, len_mine) * per : 0;
-    int total = mine0;
-    for (int b = lane + 32; b < a.B; b += 32) total += entry_tiles<KT>(a, b) * per;
-#pragma unroll
-    for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-    const Runs rs(total, gridDim.x);
-    const int i = blockIdx.x, run0 = i < rs.runs ? rs.start(i) : 0;
-    const int run1 = i < rs.runs && total > 0 ? rs.start(i + 1) : 0;
-    // the entry that holds tile run0
-    int base = 0, b0 = 0;
-    for (int c = 0; c < a.B && run0 < run1; c += 32) {
-      const int mine = c == 0 ? mine0 : c + lane < a.B ? entry_tiles<KT>(a, c + lane) * per : 0;
-      int upto = mine;                                    // inclusive prefix within the 32
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += x;
+    if (a.cluster > 0) {
+      if (lane == 0) {
+        const int unit = blockIdx.x >> a.log_cluster, i = blockIdx.x & (a.cluster - 1), b = unit / per, u = unit - b * per;
+        const int len = entry_len(a, b), tiles = unit_tiles<KT>(a, len);
+        ctl->len0 = len;
+        ctl->b0 = b;
+        ctl->base = 0;
+        ctl->run0 = u * tiles + cluster_tile(tiles, i, a.log_cluster);
+        ctl->run1 = u * tiles + cluster_tile(tiles, i + 1, a.log_cluster);
       }
-      const unsigned past = __ballot_sync(0xffffffffu, c + lane < a.B && base + upto > run0);
-      if (past) {
-        const int w = __ffs(past) - 1;
-        b0 = c + w;
-        base += __shfl_sync(0xffffffffu, upto - mine, w);
-        break;
+    } else {
+      const int len_mine = lane < a.B ? entry_len(a, lane) : 0;
+      const int mine0 = lane < a.B ? unit_tiles<KT>(a, len_mine) * per : 0;
+      int total = mine0;
+      for (int b = lane + 32; b < a.B; b += 32) total += entry_tiles<KT>(a, b) * per;
+#pragma unroll
+      for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+      const Runs rs(total, gridDim.x);
+      const int i = blockIdx.x, run0 = i < rs.runs ? rs.start(i) : 0;
+      const int run1 = i < rs.runs && total > 0 ? rs.start(i + 1) : 0;
+      // the entry that holds tile run0
+      int base = 0, b0 = 0;
+      for (int c = 0; c < a.B && run0 < run1; c += 32) {
+        const int mine = c == 0 ? mine0 : c + lane < a.B ? entry_tiles<KT>(a, c + lane) * per : 0;
+        int upto = mine;                                    // inclusive prefix within the 32
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int x = __shfl_up_sync(0xffffffffu, upto, d);
+          if (lane >= d) upto += x;
+        }
+        const unsigned past = __ballot_sync(0xffffffffu, c + lane < a.B && base + upto > run0);
+        if (past) {
+          const int w = __ffs(past) - 1;
+          b0 = c + w;
+          base += __shfl_sync(0xffffffffu, upto - mine, w);
+          break;
+        }
+        base += __shfl_sync(0xffffffffu, upto, 31);
       }
-      base += __shfl_sync(0xffffffffu, upto, 31);
-    }
-    const int len0 = b0 < 32 ? __shfl_sync(0xffffffffu, len_mine, b0) : entry_len(a, b0);
-    if (lane == 0) {
-      ctl->len0 = len0;
-      ctl->runs = rs.runs;
-      ctl->run_len = rs.len;
-      ctl->longer = rs.longer;
-      ctl->run0 = run0;
-      ctl->run1 = run1;
-      ctl->base = base;
-      ctl->b0 = b0;
+      const int len0 = b0 < 32 ? __shfl_sync(0xffffffffu, len_mine, b0) : entry_len(a, b0);
+      if (lane == 0) {
+        ctl->len0 = len0;
+        ctl->runs = rs.runs;
+        ctl->run_len = rs.len;
+        ctl->longer = rs.longer;
+        ctl->run0 = run0;
+        ctl->run1 = run1;
+        ctl->base = base;
+        ctl->b0 = b0;
+      }
     }
   } else {
     pdl_wait_and_trigger();
@@ -349,7 +386,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       }
     } else if (warp == kMma + 1) {
       // ---------------------------------------------------------------- for join_kernel: the units that start here
-      if (elect_one()) {
+      if (a.cluster == 0 && elect_one()) {
         Pieces<KT> p(a, ctl);
         Runs rs(1, 1);
         rs.runs = ctl->runs;
@@ -620,6 +657,18 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       wait(&ctl->pvdone[(g - 1) % S::NP], (uint32_t)(((g - 1) / S::NP) & 1));
       const bool gone = bar_or(1 + grp, 128, dead);        // (the group's earlier reads of `red` are done)
       group_reduce<S>(l, red + q * N + col0, lane, grp, AddOp());
+      if (a.cluster > 0) {                                 // its one piece: joined with the other CTAs' below
+        if (q == 0 && (lane & (L - 1)) == 0) {
+          float2* ml = reinterpret_cast<float2*>(sm + S::VIS_OFF);
+#pragma unroll
+          for (int c = 0; c < CS; ++c) {
+            const int x = col0 + c;
+            const float all = (red[x] + red[N + x]) + (red[2 * N + x] + red[3 * N + x]);
+            ml[x] = make_float2(all == 0.f ? -INFINITY : m[c], all);
+          }
+        }
+        break;
+      }
       float sum[C];
       const float4* s4 = reinterpret_cast<const float4*>(red + grp * C);
 #pragma unroll
@@ -653,20 +702,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
           const int d = mb * S::MV + dl;
           float o[C];
           tm_load<C>(tO + lanes + (uint32_t)(mb * N + grp * C), o);
-          if (nf != 0) {                                   // the non-finite values that a row sees
-            for (int c = 0; c < C; ++c) {
-              const int r = grp * C + c;
-              if (r >= rows) break;
-              float add = 0.f;
-              for (uint64_t bits = nf & a.mask[(int64_t)p.b * a.n + (row0 + r) / a.G]; bits; bits &= bits - 1) {
-                const int j = __ffsll((long long)bits) - 1;
-                const uint16_t y = j < a.n ? a.v_tree[((int64_t)p.b * a.n + j) * a.v_tok + kvh * a.v_head + d] : 0;
-                if (non_finite<S::BF16>(y)) add += widen<S::BF16>(y);
-              }
-#pragma unroll
-              for (int e = 0; e < C; ++e) o[e] += e == c ? add : 0.f;
-            }
-          }
+          if (nf != 0) add_non_finite<S>(a, nf, p.b, kvh, row0 + grp * C, rows - grp * C, d, o);
           if (!whole) {
             float* po = a.part_o + (slot * N + grp * C) * S::DV + d;
             if (dlive) {
@@ -696,9 +732,77 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       if (lane == 0) tc_mbar_arrive(&ctl->ofree);
     }
   }
-  // teardown: on a failure wait (bounded) for the copies and products already issued
   tc_fence_before();
   __syncthreads();
+  if (a.cluster > 0) {
+    // ---------------------------------------------------------------- the cluster's pieces joined
+    const int per = a.Hkv * a.row_blocks, b = ctl->b0, u = (int)(blockIdx.x >> a.log_cluster) - b * per;
+    const int kvh = u / a.row_blocks, row0 = u % a.row_blocks * N, rows = std::min(N, a.R - row0);
+    const int tiles = unit_tiles<KT>(a, ctl->len0), rank = (int)cluster_rank();
+    auto has = [&](int i) { return cluster_tile(tiles, i, a.log_cluster) < cluster_tile(tiles, i + 1, a.log_cluster); };
+    float2* ml = reinterpret_cast<float2*>(sm + S::VIS_OFF);      // [N] (maximum, sum) of this CTA's piece
+    float* weight = reinterpret_cast<float*>(sm + S::RED_OFF);    // [N] what its output counts for
+    float* out = reinterpret_cast<float*>(sm + S::KV_OFF);        // [N][DV] its weighted output (the ring is idle now)
+    static_assert(N * S::DV * 4 <= S::SLOTS * S::SLOT && N * 8 <= kMaxTree * S::VW * 4, "room for the join");
+    tc_fence_after();
+    cluster_sync();
+    if (warp < kLoad) {
+      const int q = warp & 3, grp = warp >> 2;
+      if (threadIdx.x < N && has(rank)) {
+        float2 x[kMaxCluster];
+        float M = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kMaxCluster; ++i) {
+          x[i] = i < a.cluster && has(i) ? ld_cluster2(cluster_addr(ml + threadIdx.x, i)) : make_float2(-INFINITY, 0.f);
+          M = fmaxf(M, x[i].x);
+        }
+#pragma unroll
+        for (int i = 0; i < kMaxCluster; ++i)
+          if (x[i].x != -INFINITY) sum += ex2_approx(x[i].x - M) * x[i].y;
+        const float mine = ml[threadIdx.x].x;
+        weight[threadIdx.x] = sum == 0.f || mine == -INFINITY ? 0.f : ex2_approx(mine - M) / sum;
+      }
+      bar_sync(5, S::SOFT);
+      if (has(rank)) {
+        const uint64_t nf = a.tree && cluster_tile(tiles, rank + 1, a.log_cluster) == tiles ? ctl->nonfinite : 0;
+#pragma unroll 1
+        for (int mb = 0; mb < S::NB; ++mb) {
+          const int d = mb * S::MV + (S::MV == 128 ? q * 32 + lane : q * 16 + (lane & 15));
+          float o[C];
+          tm_load<C>(tO + ((uint32_t)(q * 32) << 16) + (uint32_t)(mb * N + grp * C), o);
+          if (nf != 0) add_non_finite<S>(a, nf, b, kvh, row0 + grp * C, rows - grp * C, d, o);
+          if (S::MV == 128 || lane < 16) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) out[(grp * C + c) * S::DV + d] = o[c] * weight[grp * C + c];
+          }
+        }
+      }
+    }
+    cluster_sync();
+    if (warp < kLoad && *fail == 0) {
+      const int quads = (S::DV / 4) >> a.log_cluster;              // this CTA's dims: rank DV / cluster .., four a thread
+      const int log_q = 31 - __clz(quads);
+      for (int e = threadIdx.x; e < rows * quads; e += S::SOFT) {
+        const int r = e >> log_q, d = (rank * quads + (e & (quads - 1))) * 4, row = row0 + r;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < kMaxCluster; ++i)
+          if (i < a.cluster && has(i)) {
+            const float4 y = ld_cluster4(cluster_addr(out + r * S::DV + d, i));
+            o.x += y.x;
+            o.y += y.y;
+            o.z += y.z;
+            o.w += y.w;
+          }
+        const int64_t at = S::SHARED ? (int64_t)b * a.R + row
+                                     : ((int64_t)b * a.n + (row >> a.log_g)) * a.H + kvh * a.G + (row & (a.G - 1));
+        *reinterpret_cast<uint2*>(a.out + at * S::DV + d) =
+            make_uint2(pack2<S::BF16>(o.x, o.y), pack2<S::BF16>(o.z, o.w));
+      }
+    }
+    cluster_sync();                                                // no CTA leaves while another reads its memory
+  }
+  // teardown: on a failure wait (bounded) for the copies and products already issued
   if (threadIdx.x == 0 && ctl->fail) {
     if (ctl->q_loads > 0) tc_mbar_wait(&ctl->qfull, (uint32_t)((ctl->q_loads - 1) & 1), kRoleWaitNs);
     // (a tile whose loads were only begun when its wait ran out: nothing says when those end but time)
@@ -802,6 +906,7 @@ __global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
 // ---------------------------------------------------------------- host side
 struct Plan {
   int N, KT, R, row_blocks, ctas;
+  int cluster;                 // CTAs a unit; 0: runs
   int64_t tiles;               // of all units when every entry is full
   size_t joint_off, ml_off, o_off, bytes;
 };
@@ -814,7 +919,16 @@ Plan plan_rows(const RowsCall& c) {
   p.row_blocks = (int)ceil_div(p.R, p.N);
   p.tiles = (ceil_div(c.T_cap, p.KT) + 1) * c.B * c.Hkv * p.row_blocks;
   p.ctas = (int)std::min<int64_t>(p.tiles, kNumSMs);
-  const size_t parts = (size_t)p.ctas * 2 * p.N;
+  // Clusters where as many as there are units run beside each other (one CTA an SM: 76 of 2, 36 of 4, 15 of 8) and no
+  // CTA's share is much longer than an equal one: joining through the workspace costs about four tiles' time and a
+  // seventh of a long run's.  Measured, clusters against runs: 16 drafted tokens over 8 x 8K (64 units) 49 against 54 us,
+  // 8 over 3000 tokens (8 units) 11 against 17, one latent token over 8 x 1000 (8 units) 12.0 against 13.7; but 28 (runs)
+  // against 34 for one latent token over 8 x 8K.
+  const int64_t units = (int64_t)c.B * c.Hkv * p.row_blocks, per_unit = ceil_div(c.T_cap, p.KT) + 1;
+  const int64_t equal = ceil_div(per_unit * units, kNumSMs);
+  const int k = units <= 15 ? 8 : units <= 36 ? 4 : units <= 76 ? 2 : 0;
+  p.cluster = k > 0 && ceil_div(per_unit, k) <= equal + equal / 7 + 4 ? k : 0;
+  const size_t parts = (size_t)p.ctas * 2 * p.N;       // (of the runs, so that the size does not fall with T_cap or n)
   p.joint_off = kCounterBytes;
   p.ml_off = p.joint_off + align256((size_t)c.B * c.Hkv * p.row_blocks * sizeof(Joint));
   p.o_off = p.ml_off + align256(parts * sizeof(float2));
@@ -847,8 +961,21 @@ cudaError_t launch_shape(const RowsCall& c, const Plan& p, RowsArgs a, cudaStrea
   constexpr int smem = std::max(S::ALLOC, 116 * 1024);
   e = cudaFuncSetAttribute(rows_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(rows_kernel<S>, dim3(p.ctas), dim3(S::THREADS), smem, st, qm, km, vm, ktm, vtm, a);
-  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {(unsigned)std::max(1, p.cluster), 1, 1};
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.cluster > 0 ? (unsigned)(B * Hkv * p.row_blocks * p.cluster) : (unsigned)p.ctas);
+  cfg.blockDim = dim3(S::THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.cluster > 0 ? 2 : 1;
+  e = cudaLaunchKernelEx(&cfg, rows_kernel<S>, qm, km, vm, ktm, vtm, a);
+  if (e == cudaSuccess) e = cudaPeekAtLastError();
+  if (e != cudaSuccess || p.cluster > 0) return e;
   const unsigned grid = (unsigned)ceil_div(B * Hkv * p.R, 512 / S::DV);
   return launch_pdl(join_kernel<S::BF16, S::KT, S::DV>, dim3(grid), dim3(128), 0, st, a, (int)S::N);
 }
@@ -887,6 +1014,8 @@ cudaError_t launch_rows_attention(const RowsCall& c, void* ws, cudaStream_t st) 
   a.G = c.H / c.Hkv;
   a.R = p.R;
   a.row_blocks = p.row_blocks;
+  a.cluster = p.cluster;
+  for (a.log_cluster = 0; (1 << a.log_cluster) < a.cluster;) ++a.log_cluster;
   a.log_g = -1;
   if (!c.latent)
     for (a.log_g = 0; (1 << a.log_g) < a.G;) ++a.log_g;
