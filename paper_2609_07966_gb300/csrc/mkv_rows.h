@@ -49,6 +49,7 @@ struct RowsCall {
   void* out;                       // [B][n][H][dv]
 };
 size_t rows_ws_bytes(const RowsCall& c);
+bool rows_countable(const RowsCall& c);   // its key tiles fit the kernel's 32-bit counts
 cudaError_t launch_rows_attention(const RowsCall& c, void* ws, cudaStream_t st);
 
 // Causal attention over expanded keys and values (latent_prefill.cu).

@@ -1003,6 +1003,7 @@ cudaError_t launch_tree(const RowsCall& c, const Plan& p, const RowsArgs& a, cud
 }  // namespace
 
 size_t rows_ws_bytes(const RowsCall& c) { return plan_rows(c).bytes; }
+bool rows_countable(const RowsCall& c) { return plan_rows(c).tiles <= INT32_MAX / 2; }
 
 cudaError_t launch_rows_attention(const RowsCall& c, void* ws, cudaStream_t st) {
   const Plan p = plan_rows(c);
@@ -1028,7 +1029,6 @@ cudaError_t launch_rows_attention(const RowsCall& c, void* ws, cudaStream_t st) 
   a.v_tok = c.latent ? c.dk : (int64_t)c.Hkv * c.dv;
   a.v_head = c.latent ? 0 : c.dv;
   a.out = static_cast<uint16_t*>(c.out);
-  if (p.tiles > INT32_MAX / 2) return cudaErrorInvalidConfiguration;   // more than any GPU's memory holds
   a.joint = reinterpret_cast<Joint*>(static_cast<uint8_t*>(ws) + p.joint_off);
   a.part_ml = reinterpret_cast<float2*>(static_cast<uint8_t*>(ws) + p.ml_off);
   a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.o_off);

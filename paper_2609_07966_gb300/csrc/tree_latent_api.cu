@@ -51,6 +51,11 @@ mkv_status check_ws(const void* ws, size_t have, size_t need) {
   return MKV_OK;
 }
 
+mkv_status check_rows(const RowsCall& r) {
+  MKV_REQUIRE(rows_countable(r), MKV_ERR_UNSUPPORTED, "too many key tiles (T_cap x entries x rows) for one call");
+  return MKV_OK;
+}
+
 float latent_scale(const mkv_latent_config* c) {
   return c->softmax_scale > 0.f ? c->softmax_scale : 1.0f / sqrtf((float)(c->nope_dim + c->rope_dim));
 }
@@ -118,7 +123,9 @@ extern "C" {
 mkv_status mkv_tree_workspace_size(const mkv_config* cfg, int64_t T_cap, int32_t n, size_t* bytes) {
   MKV_REQUIRE(bytes != nullptr, MKV_ERR_INVALID_ARG, "bytes is NULL");
   MKV_TRY(check_tree_cfg(cfg, T_cap, n));
-  *bytes = rows_ws_bytes(rows_of_tree(cfg, T_cap, n));
+  const RowsCall r = rows_of_tree(cfg, T_cap, n);
+  MKV_TRY(check_rows(r));
+  *bytes = rows_ws_bytes(r);
   return MKV_OK;
 }
 
@@ -132,6 +139,7 @@ mkv_status mkv_tree_attention(const mkv_config* cfg, const void* q, const mkv_ca
                   aligned16(cache->v),
               MKV_ERR_INVALID_ARG, "q, out, k_tree, v_tree and the cache must be 16-byte aligned");
   RowsCall r = rows_of_tree(cfg, cache->T_cap, n);
+  MKV_TRY(check_rows(r));
   MKV_TRY(check_ws(ws, ws_bytes, rows_ws_bytes(r)));
   r.q = q;
   r.k = cache->k;
@@ -173,7 +181,9 @@ mkv_status mkv_latent_workspace_size(const mkv_latent_config* cfg, int64_t T_cap
   MKV_REQUIRE(bytes != nullptr && T_cap >= 1, MKV_ERR_INVALID_ARG, "bytes NULL or T_cap < 1");
   MKV_REQUIRE(T_cap < kMaxSlots, MKV_ERR_UNSUPPORTED, "T_cap %lld too large", (long long)T_cap);
   MKV_TRY(check_tree_n(n));
-  *bytes = rows_ws_bytes(rows_of_latent(cfg, T_cap, n));
+  const RowsCall r = rows_of_latent(cfg, T_cap, n);
+  MKV_TRY(check_rows(r));
+  *bytes = rows_ws_bytes(r);
   return MKV_OK;
 }
 
@@ -225,6 +235,7 @@ mkv_status mkv_latent_attention(const mkv_latent_config* cfg, const void* q_abs,
   MKV_REQUIRE(aligned16(q_abs) && aligned16(o_lat) && aligned16(rows_tree), MKV_ERR_INVALID_ARG,
               "q_abs, o_lat and rows_tree must be 16-byte aligned");
   RowsCall r = rows_of_latent(cfg, cache->T_cap, n);
+  MKV_TRY(check_rows(r));
   MKV_TRY(check_ws(ws, ws_bytes, rows_ws_bytes(r)));
   r.q = q_abs;
   r.k = r.v = cache->rows;

@@ -77,6 +77,21 @@ def test_absorbed_long_contexts_split(T):
     _check(c, _run(c), f"T{T}")
 
 
+@pytest.mark.parametrize("H,n,tree", [(8, 1, False), (32, 5, True)])
+def test_absorbed_many_ragged_units(H, n, tree):
+    """More units than SMs, of unequal lengths: runs of tiles that hold whole units and parts of others; then all empty."""
+    lens = [(29 * b * b) % 300 if b % 5 else 0 for b in range(80)]
+    c = _case("bf16", 80, H, 256, n, 320, lens, seed=H, tree=tree, junk=float("nan"))
+    _check(c, _run(c), f"H{H} n{n}")
+    c["cache"].t["T_len"].zero_()
+    c["lens"] = [0] * 80
+    out = _run(c)
+    if tree:
+        _check(c, out, "empty cache")
+    else:
+        assert (f64(out) == 0).all()
+
+
 def test_absorbed_empty_rows_are_zero():
     masks = np.array([[0b10, 0, 0b100]], dtype=np.uint64)
     c = _case("bf16", 1, 8, 512, 3, 64, [0], seed=2, masks=masks, junk=float("nan"))

@@ -74,6 +74,14 @@ def test_long_contexts_split(T):
     _check(c, _run(c), f"T{T}")
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_ragged_units(D):
+    """More units than SMs, of unequal lengths, some empty: runs of tiles that hold whole units and parts of others."""
+    lens = [(37 * b * b) % 500 if b % 7 else 0 for b in range(45)]
+    c = _case(45, 4, 2, D, 3, 512, lens, seed=D, junk=float("nan"))
+    _check(c, _run(c), f"D{D}", entries=range(0, 45, 4))
+
+
 def test_empty_rows_are_zero():
     masks = np.array([[0, 0b10, 0], [0, 0, 0]], dtype=np.uint64)
     c = _case(2, 2, 4, 64, 3, 64, [0, 0], seed=3, masks=masks, junk=float("inf"))

@@ -93,6 +93,7 @@ def test_latent_config_refusals(L):
         assert size(_lat(**bad)) == uns, bad
     assert size(_lat(), T=0) == inv and size(_lat(), k=0) == inv and size(_lat(), k=65) == uns
     assert size(_lat(), T=1 << 31) == uns
+    assert size(_lat(B=4096, H=256), T=1 << 20, k=64) == uns and "tiles" in mkv.mkv_last_error()
     c = _lat()
     c.abi_version = 7
     assert size(c) == inv
