@@ -42,6 +42,7 @@ __device__ __forceinline__ void store_length(const CommitCall& a, int b, bool ok
 
 template <bool kCluster>
 __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitCall a) {
+  pdl_wait_and_trigger();
   const int b = blockIdx.y;
   int t0, np;
   const bool ok = path_fits(a, b, t0, np);
@@ -74,6 +75,7 @@ __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitCall
 }
 
 __global__ void __launch_bounds__(kCommitThreads) length_kernel(const CommitCall a) {
+  pdl_wait_and_trigger();
   int t0, np;
   const bool ok = path_fits(a, blockIdx.x, t0, np);
   store_length(a, blockIdx.x, ok, t0 + np);
@@ -97,21 +99,21 @@ cudaError_t launch_commit(const CommitCall& c, cudaStream_t st) {
   const int64_t bytes = (int64_t)c.n * c.heads * c.row_bytes * (c.src1 != nullptr ? 2 : 1);
   if (bytes > (1 << 20)) {
     const int64_t want = ceil_div((int64_t)4 * kNumSMs, (int64_t)c.B), most = ceil_div(c.n, kCommitThreads / 32);
-    commit_kernel<false><<<dim3((unsigned)std::min(want, most), c.B), kCommitThreads, 0, st>>>(c);
-    const cudaError_t e = cudaPeekAtLastError();
-    if (e != cudaSuccess) return e;
-    length_kernel<<<c.B, kCommitThreads, 0, st>>>(c);
-    return cudaPeekAtLastError();
+    const cudaError_t e =
+        launch_pdl(commit_kernel<false>, dim3((unsigned)std::min(want, most), c.B), dim3(kCommitThreads), 0, st, c);
+    return e != cudaSuccess ? e : launch_pdl(length_kernel, dim3(c.B), dim3(kCommitThreads), 0, st, c);
   }
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim = {kParts, 1, 1};
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kParts, c.B);
   cfg.blockDim = dim3(kCommitThreads);
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, commit_kernel<true>, c);
   return e != cudaSuccess ? e : cudaPeekAtLastError();
 }

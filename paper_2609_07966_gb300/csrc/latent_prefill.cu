@@ -103,6 +103,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
   const int i0 = (nblk - 1 - in / size) * 2 * kBR;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+  pdl_wait_and_trigger();                                // (from here on memory that the stream's previous kernel wrote)
   const int tl = a.T_len[b];
   const int len = (int)std::min<int64_t>(std::max(tl, 0), a.T_max);
   const int ql = a.q_len != nullptr ? std::min(std::max(a.q_len[b], 0), a.n) : a.n;
@@ -435,8 +436,7 @@ cudaError_t launch_shape(const PrefillCall& c, PrefillArgs a, cudaStream_t st) {
   constexpr int smem = std::max(S::ALLOC, 116 * 1024);      // one CTA an SM: it takes all of the tensor memory
   e = cudaFuncSetAttribute(latent_prefill_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  latent_prefill_kernel<S><<<(unsigned)grid, kPThreads, smem, st>>>(qm, kvm, rm, a);
-  return cudaPeekAtLastError();
+  return launch_pdl(latent_prefill_kernel<S>, dim3((unsigned)grid), dim3(kPThreads), smem, st, qm, kvm, rm, a);
 }
 
 template <bool BF16>
