@@ -15,7 +15,7 @@
 // Work: a unit is one (entry, key head, row block); its key tiles are the entry's cached ones and, last, the drafted
 // tokens'.  The lengths are read on the device.  Two ways to share the units out, chosen by plan_rows:
 //   clusters  a cluster of CTAs per unit, each an equal run of its tiles; the pieces are joined through distributed
-//             shared memory (each CTA sums a slice of the dims over the others'), so one launch does it all;
+//             shared memory (each CTA gets every piece's slice of its dims), so one launch does it all;
 //   runs      the tiles of all units laid end to end, an equal run for every CTA, whatever the entries' lengths; a unit
 //             inside one run is written directly, the pieces of a unit that several runs share go to the workspace
 //             and join_kernel adds them up.
@@ -127,6 +127,7 @@ struct RowsCtl {
   uint32_t tslot;
   int runs, run_len, longer;  // (Runs)
   int run0, run1, base, b0, len0;   // this CTA's run of tiles; first tile of entry b0, which holds run0; its length
+  int u0;                           // the unit of that entry that holds run0
   int fail;
   int q_loads, loaded, scores, values;   // pieces' queries, tiles issued so far (read after a failure)
 };
@@ -175,17 +176,19 @@ struct Pieces {
   // the current piece: unit `u` of entry b, its tiles t0 .. t1 - 1 of `tiles`
   int u, t0, t1, tiles, len, index;
   __device__ __forceinline__ Pieces(const RowsArgs& args, const RowsCtl* c)
-      : a(args), cur(c->run0), end(c->run1), base(c->base), b(c->b0), per(args.Hkv * args.row_blocks), len(c->len0),
-        index(-1) {}
+      : a(args), cur(c->run0), end(c->run1), base(c->base), b(c->b0), per(args.Hkv * args.row_blocks), u(c->u0 - 1),
+        len(c->len0), index(-1) {}
   __device__ __forceinline__ bool next() {
     if (cur >= end) return false;
+    ++u;                    // after a piece that ends its unit, the next one
+#pragma unroll 1
     for (;;) {
       tiles = unit_tiles<KT>(a, len);
       if (cur < base + tiles * per) break;
       base += tiles * per;
+      u = 0;
       len = entry_len(a, ++b);
     }
-    u = (cur - base) / tiles;
     t0 = cur - base - u * tiles;
     t1 = std::min(tiles, t0 + (end - cur));
     cur += t1 - t0;
@@ -273,6 +276,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         ctl->len0 = len;
         ctl->b0 = b;
         ctl->base = 0;
+        ctl->u0 = u;
         ctl->run0 = u * tiles + cluster_tile(tiles, i, a.log_cluster);
         ctl->run1 = u * tiles + cluster_tile(tiles, i + 1, a.log_cluster);
       }
@@ -307,6 +311,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       }
       const int len0 = b0 < 32 ? __shfl_sync(0xffffffffu, len_mine, b0) : entry_len(a, b0);
       if (lane == 0) {
+        const int tiles0 = std::max(1, unit_tiles<KT>(a, len0));
+        ctl->u0 = (run0 - base) / tiles0;
         ctl->len0 = len0;
         ctl->runs = rs.runs;
         ctl->run_len = rs.len;
@@ -513,6 +519,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       if (!dead) dead = !__all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status));
       tc_fence_after();
     };
+    bool arrived = false;                                 // at the cluster's barrier
     Pieces<KT> p(a, ctl);
     int g = 0;                                            // tiles met by this CTA so far
     while (p.next()) {
@@ -655,6 +662,10 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       }
       // -------------------------------------------------------------- this piece's outputs
       wait(&ctl->pvdone[(g - 1) % S::NP], (uint32_t)(((g - 1) / S::NP) & 1));
+      if (a.cluster > 0) {
+        cluster_arrive();                                  // (this warp is done with the ring)
+        arrived = true;
+      }
       const bool gone = bar_or(1 + grp, 128, dead);        // (the group's earlier reads of `red` are done)
       group_reduce<S>(l, red + q * N + col0, lane, grp, AddOp());
       if (a.cluster > 0) {                                 // its one piece: joined with the other CTAs' below
@@ -731,76 +742,94 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       __syncwarp();
       if (lane == 0) tc_mbar_arrive(&ctl->ofree);
     }
+    if (a.cluster > 0 && !arrived) cluster_arrive();      // (a CTA without a tile)
+  }
+  if (a.cluster > 0 && warp >= kLoad) {
+    __syncwarp();
+    cluster_arrive();
   }
   tc_fence_before();
   __syncthreads();
   if (a.cluster > 0) {
     // ---------------------------------------------------------------- the cluster's pieces joined
+    // The ring is idle in every CTA past the barrier's wait.  Each sends slice i of its output's dims, unweighted, to
+    // CTA i, its rows' (maximum, sum) to all; each then adds up its own slice.  Loops stay rolled: code that runs once
+    // comes from a cold instruction cache, about 14 cycles an instruction (unrolled, the weights alone took 7000).
     const int per = a.Hkv * a.row_blocks, b = ctl->b0, u = (int)(blockIdx.x >> a.log_cluster) - b * per;
     const int kvh = u / a.row_blocks, row0 = u % a.row_blocks * N, rows = std::min(N, a.R - row0);
     const int tiles = unit_tiles<KT>(a, ctl->len0), rank = (int)cluster_rank();
-    auto has = [&](int i) { return cluster_tile(tiles, i, a.log_cluster) < cluster_tile(tiles, i + 1, a.log_cluster); };
-    float2* ml = reinterpret_cast<float2*>(sm + S::VIS_OFF);      // [N] (maximum, sum) of this CTA's piece
-    float* weight = reinterpret_cast<float*>(sm + S::RED_OFF);    // [N] what its output counts for
-    float* out = reinterpret_cast<float*>(sm + S::KV_OFF);        // [N][DV] its weighted output (the ring is idle now)
-    static_assert(N * S::DV * 4 <= S::SLOTS * S::SLOT && N * 8 <= kMaxTree * S::VW * 4, "room for the join");
+    unsigned has = 0;                                                       // the CTAs that hold a piece
+#pragma unroll 1
+    for (int i = 0; i < a.cluster; ++i)
+      has |= (cluster_tile(tiles, i, a.log_cluster) < cluster_tile(tiles, i + 1, a.log_cluster) ? 1u : 0u) << i;
+    const int slice = S::DV >> a.log_cluster, log_s = 31 - __clz(slice);
+    float* pieces = reinterpret_cast<float*>(sm + S::KV_OFF);               // [cluster][N][slice]
+    float2* stats = reinterpret_cast<float2*>(pieces + N * S::DV);          // [cluster][N]; then x is the weight
+    static_assert(N * S::DV * 4 + kMaxCluster * N * 8 <= S::SLOTS * S::SLOT + S::ROPE * S::ATOM &&
+                      N * 8 <= kMaxTree * S::VW * 4,
+                  "room for the join");
     tc_fence_after();
-    cluster_sync();
-    if (warp < kLoad) {
+    cluster_wait();
+    if (warp < kLoad && (has >> rank & 1)) {
       const int q = warp & 3, grp = warp >> 2;
-      if (threadIdx.x < N && has(rank)) {
-        float2 x[kMaxCluster];
-        float M = -INFINITY, sum = 0.f;
+      const float2* ml = reinterpret_cast<const float2*>(sm + S::VIS_OFF);  // [N]
+      for (int e = threadIdx.x; e < N << a.log_cluster; e += S::SOFT)
+        st_cluster2(cluster_addr(stats + rank * N + e % N, (uint32_t)(e / N)), ml[e % N]);
+      const uint64_t nf = a.tree && cluster_tile(tiles, rank + 1, a.log_cluster) == tiles ? ctl->nonfinite : 0;
+#pragma unroll 1
+      for (int mb = 0; mb < S::NB; ++mb) {
+        const int d = mb * S::MV + (S::MV == 128 ? q * 32 + lane : q * 16 + (lane & 15));
+        float o[C];
+        tm_load<C>(tO + ((uint32_t)(q * 32) << 16) + (uint32_t)(mb * N + grp * C), o);
+        if (nf != 0) add_non_finite<S>(a, nf, b, kvh, row0 + grp * C, rows - grp * C, d, o);
+        const uint32_t to = cluster_addr(pieces + ((rank * N + grp * C) << log_s) + (d & (slice - 1)), (uint32_t)(d >> log_s));
+        if (S::MV == 128 || lane < 16) {
 #pragma unroll
-        for (int i = 0; i < kMaxCluster; ++i) {
-          x[i] = i < a.cluster && has(i) ? ld_cluster2(cluster_addr(ml + threadIdx.x, i)) : make_float2(-INFINITY, 0.f);
-          M = fmaxf(M, x[i].x);
+          for (int c = 0; c < C; ++c)
+            if (grp * C + c < rows) st_cluster(to + ((uint32_t)c << (log_s + 2)), o[c]);
         }
+      }
+    }
+    __syncwarp();
+    cluster_sync();                                                // all pieces are here; none is sent any more
+    if (warp < kLoad) {
+      // eight lanes a row, one piece each
+#pragma unroll 1
+      for (int e = threadIdx.x; e < N * kMaxCluster; e += S::SOFT) {
+        const int i = e % kMaxCluster;
+        float2* x = stats + i * N + e / kMaxCluster;
+        const float2 y = has >> i & 1 ? *x : make_float2(-INFINITY, 0.f);
+        float M = y.x;
 #pragma unroll
-        for (int i = 0; i < kMaxCluster; ++i)
-          if (x[i].x != -INFINITY) sum += ex2_approx(x[i].x - M) * x[i].y;
-        const float mine = ml[threadIdx.x].x;
-        weight[threadIdx.x] = sum == 0.f || mine == -INFINITY ? 0.f : ex2_approx(mine - M) / sum;
+        for (int d = kMaxCluster / 2; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+        const float w = y.x == -INFINITY ? 0.f : ex2_approx(y.x - M);
+        float sum = w * y.y;
+#pragma unroll
+        for (int d = kMaxCluster / 2; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (has >> i & 1) x->x = sum == 0.f ? 0.f : w / sum;
       }
       bar_sync(5, S::SOFT);
-      if (has(rank)) {
-        const uint64_t nf = a.tree && cluster_tile(tiles, rank + 1, a.log_cluster) == tiles ? ctl->nonfinite : 0;
-#pragma unroll 1
-        for (int mb = 0; mb < S::NB; ++mb) {
-          const int d = mb * S::MV + (S::MV == 128 ? q * 32 + lane : q * 16 + (lane & 15));
-          float o[C];
-          tm_load<C>(tO + ((uint32_t)(q * 32) << 16) + (uint32_t)(mb * N + grp * C), o);
-          if (nf != 0) add_non_finite<S>(a, nf, b, kvh, row0 + grp * C, rows - grp * C, d, o);
-          if (S::MV == 128 || lane < 16) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) out[(grp * C + c) * S::DV + d] = o[c] * weight[grp * C + c];
-          }
+      if (*fail == 0) {
+        for (int e = threadIdx.x; e < rows << (log_s - 2); e += S::SOFT) {      // four dims of a row
+          const int r = e >> (log_s - 2), ds = (e & ((slice >> 2) - 1)) * 4, row = row0 + r;
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int i = 0; i < a.cluster; ++i)
+            if (has >> i & 1) {
+              const float4 y = *reinterpret_cast<const float4*>(pieces + ((i * N + r) << log_s) + ds);
+              const float w = stats[i * N + r].x;
+              o.x += w * y.x;
+              o.y += w * y.y;
+              o.z += w * y.z;
+              o.w += w * y.w;
+            }
+          const int64_t at = S::SHARED ? (int64_t)b * a.R + row
+                                       : ((int64_t)b * a.n + (row >> a.log_g)) * a.H + kvh * a.G + (row & (a.G - 1));
+          *reinterpret_cast<uint2*>(a.out + at * S::DV + (rank << log_s) + ds) =
+              make_uint2(pack2<S::BF16>(o.x, o.y), pack2<S::BF16>(o.z, o.w));
         }
       }
     }
-    cluster_sync();
-    if (warp < kLoad && *fail == 0) {
-      const int quads = (S::DV / 4) >> a.log_cluster;              // this CTA's dims: rank DV / cluster .., four a thread
-      const int log_q = 31 - __clz(quads);
-      for (int e = threadIdx.x; e < rows * quads; e += S::SOFT) {
-        const int r = e >> log_q, d = (rank * quads + (e & (quads - 1))) * 4, row = row0 + r;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int i = 0; i < kMaxCluster; ++i)
-          if (i < a.cluster && has(i)) {
-            const float4 y = ld_cluster4(cluster_addr(out + r * S::DV + d, i));
-            o.x += y.x;
-            o.y += y.y;
-            o.z += y.z;
-            o.w += y.w;
-          }
-        const int64_t at = S::SHARED ? (int64_t)b * a.R + row
-                                     : ((int64_t)b * a.n + (row >> a.log_g)) * a.H + kvh * a.G + (row & (a.G - 1));
-        *reinterpret_cast<uint2*>(a.out + at * S::DV + d) =
-            make_uint2(pack2<S::BF16>(o.x, o.y), pack2<S::BF16>(o.z, o.w));
-      }
-    }
-    cluster_sync();                                                // no CTA leaves while another reads its memory
   }
   // teardown: on a failure wait (bounded) for the copies and products already issued
   if (threadIdx.x == 0 && ctl->fail) {
