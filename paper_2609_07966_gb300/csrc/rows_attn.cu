@@ -212,12 +212,13 @@ __device__ __forceinline__ void group_reduce(float (&w)[S::CS], float* red, int 
   bar_sync(1 + grp, 128);
 }
 
-// Adds to dim d of each of C rows (the first `rows` of them from row `row` of the unit on) the non-finite values of the
+// Adds to dim d of each of W rows (the first `rows` of them from row `row` of the unit on) the non-finite values of the
 // drafted tokens `nf` that it sees.
-template <class S>
+template <class S, int W>
 __device__ __forceinline__ void add_non_finite(const RowsArgs& a, uint64_t nf, int b, int kvh, int row, int rows, int d,
-                                            float (&o)[S::C]) {
-  for (int c = 0; c < S::C && c < rows; ++c) {
+                                               float (&o)[W]) {
+#pragma unroll 1
+  for (int c = 0; c < W && c < rows; ++c) {
     float add = 0.f;
     for (uint64_t bits = nf & a.mask[(int64_t)b * a.n + (row + c) / a.G]; bits; bits &= bits - 1) {
       const int j = __ffsll((long long)bits) - 1;
@@ -225,7 +226,7 @@ __device__ __forceinline__ void add_non_finite(const RowsArgs& a, uint64_t nf, i
       if (non_finite<S::BF16>(y)) add += widen<S::BF16>(y);
     }
 #pragma unroll
-    for (int e = 0; e < S::C; ++e) o[e] += e == c ? add : 0.f;
+    for (int e = 0; e < W; ++e) o[e] += e == c ? add : 0.f;
   }
 }
 
@@ -776,17 +777,19 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       for (int e = threadIdx.x; e < N << a.log_cluster; e += S::SOFT)
         st_cluster2(cluster_addr(stats + rank * N + e % N, (uint32_t)(e / N)), ml[e % N]);
       const uint64_t nf = a.tree && cluster_tile(tiles, rank + 1, a.log_cluster) == tiles ? ctl->nonfinite : 0;
+      constexpr int CJ = C > 16 ? 16 : C;                          // rows at a time (few registers are left here)
 #pragma unroll 1
-      for (int mb = 0; mb < S::NB; ++mb) {
+      for (int e = 0; e < S::NB * (C / CJ); ++e) {
+        const int mb = e / (C / CJ), col = grp * C + e % (C / CJ) * CJ;
         const int d = mb * S::MV + (S::MV == 128 ? q * 32 + lane : q * 16 + (lane & 15));
-        float o[C];
-        tm_load<C>(tO + ((uint32_t)(q * 32) << 16) + (uint32_t)(mb * N + grp * C), o);
-        if (nf != 0) add_non_finite<S>(a, nf, b, kvh, row0 + grp * C, rows - grp * C, d, o);
-        const uint32_t to = cluster_addr(pieces + ((rank * N + grp * C) << log_s) + (d & (slice - 1)), (uint32_t)(d >> log_s));
+        float o[CJ];
+        tm_load<CJ>(tO + ((uint32_t)(q * 32) << 16) + (uint32_t)(mb * N + col), o);
+        if (nf != 0) add_non_finite<S>(a, nf, b, kvh, row0 + col, rows - col, d, o);
+        const uint32_t to = cluster_addr(pieces + ((rank * N + col) << log_s) + (d & (slice - 1)), (uint32_t)(d >> log_s));
         if (S::MV == 128 || lane < 16) {
 #pragma unroll
-          for (int c = 0; c < C; ++c)
-            if (grp * C + c < rows) st_cluster(to + ((uint32_t)c << (log_s + 2)), o[c]);
+          for (int c = 0; c < CJ; ++c)
+            if (col + c < rows) st_cluster(to + ((uint32_t)c << (log_s + 2)), o[c]);
         }
       }
     }
