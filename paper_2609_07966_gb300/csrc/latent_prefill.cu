@@ -289,20 +289,30 @@ __global__ void __launch_bounds__(kPThreads, 1)
     };
     for (int t = 0; t < nt[k]; ++t) {
       if (!wait(&ctl->sfull[k], (uint32_t)(t & 1))) break;
+      const int lim = t >= td ? seen - t * kBR : kBR;    // columns of the tile that this row sees
+      const bool part = t >= td;                         // (a tile that some row sees only in part)
       float v[kBR];
+      float mt = -INFINITY;
+      auto raw_max = [&](const float(&x)[32]) {
+        float a0 = fmax3(x[0], x[1], x[2]), a1 = fmax3(x[3], x[4], x[5]);
+#pragma unroll
+        for (int e = 6; e < 30; e += 4) {
+          a0 = fmax3(a0, x[e], x[e + 1]);
+          a1 = fmax3(a1, x[e + 2], x[e + 3]);
+        }
+        mt = fmax3(mt, fmax3(a0, x[30], x[31]), a1);
+      };
 #pragma unroll
       for (int c = 0; c < 4; ++c) tm_issue<32>(tS + c * 32, *reinterpret_cast<float(*)[32]>(&v[c * 32]));
 #pragma unroll
       for (int c = 0; c < 4; ++c) tm_wait<32>(*reinterpret_cast<float(*)[32]>(&v[c * 32]));
-      if (t >= td) {                         // a tile that some row sees only in part
-        const int lim = seen - t * kBR;
+      if (part) {
 #pragma unroll
         for (int c = 0; c < kBR; ++c) v[c] = c < lim ? v[c] : -INFINITY;
       }
-      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-      for (int c = 0; c < kBR / 2; ++c) mx[c & 3] = fmax3(mx[c & 3], v[2 * c], v[2 * c + 1]);
-      const float mt = fmax3(mx[0], mx[1], fmaxf(mx[2], mx[3])) * a.scale_log2;   // (the scale is positive)
+      for (int c = 0; c < 4; ++c) raw_max(*reinterpret_cast<float(*)[32]>(&v[c * 32]));
+      mt *= a.scale_log2;                                // (the scale is positive)
       if (__any_sync(0xffffffffu, mt > m + kRaise)) {
         const float nm = fmaxf(m, mt), w = ex2_approx(m - nm);
         m = nm;
@@ -324,40 +334,52 @@ __global__ void __launch_bounds__(kPThreads, 1)
         // length become zeros; a token's non-finite values become zeros here and are added to the rows that see it
         // at the end.  Done by the first block that meets the tile, before its product.
         if (!wait(&ctl->vfull[t % kBars], (uint32_t)((t / kBars) & 1))) break;
-        for (int e = threadIdx.x & 127; e < kBR * 8 * S::VA; e += 128) {
-          const int r = e / (8 * S::VA), x = e % (8 * S::VA);
-          uint4* p8 = reinterpret_cast<uint4*>(sm + S::R_OFF + (t * S::TA + S::KA + (x >> 3)) % S::RING * S::ATOM +
-                                               mn_offset<64>(r, x & 7));
-          if (t * kBR + r >= len) {
-            *p8 = make_uint4(0, 0, 0, 0);
-            continue;
-          }
-          uint4 raw = *p8;
-          if (bad_pairs<S::BF16>(raw)) {
-            *p8 = raw;
-            const int key = (t - td) * kBR + r;
-            atomicOr(&ctl->nonfinite[key >> 5], 1u << (key & 31));
+        // (a thread's pieces of an atom are 16 rows apart, so the swizzle leaves them 2 KB apart)
+        const int r0 = (threadIdx.x & 127) >> 3;
+#pragma unroll 1
+        for (int j = 0; j < S::VA; ++j) {
+          uint8_t* piece = sm + S::R_OFF + (t * S::TA + S::KA + j) % S::RING * S::ATOM + mn_offset<64>(r0, threadIdx.x & 7);
+          const int tail = len - t * kBR - r0;           // its rows from here on are past the length
+#pragma unroll
+          for (int x = 0; x < kBR; x += 16) {
+            uint4* p8 = reinterpret_cast<uint4*>(piece + x * 128);
+            uint4 raw = *p8;
+            if (x >= tail) {
+              *p8 = make_uint4(0, 0, 0, 0);
+            } else if (any_non_finite<S::BF16>(raw)) {
+              bad_pairs<S::BF16>(raw);
+              *p8 = raw;
+              const int key = (t - td) * kBR + r0 + x;
+              atomicOr(&ctl->nonfinite[key >> 5], 1u << (key & 31));
+            }
           }
         }
         fence_async_smem();
       }
       const uint64_t sc2 = pk2(a.scale_log2, a.scale_log2), off2 = pk2(kOffset - m, kOffset - m);
       uint64_t sum2[2] = {0ull, 0ull};
+      // 32 scores -> 16 columns of packed weights
+      auto weights = [&](const float(&x)[32], float(&pk)[16]) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {          // 64 keys = 32 packed columns
-        float pk[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const float2 x = upk2(ffma2(pk2(v[c * 64 + 2 * e], v[c * 64 + 2 * e + 1]), sc2, off2));
-          const float p0 = ex2_approx(x.x), p1 = ex2_approx(x.y);
+        for (int e = 0; e < 16; ++e) {
+          const float2 y = upk2(ffma2(pk2(x[2 * e], x[2 * e + 1]), sc2, off2));
+          const float p0 = ex2_approx(y.x), p1 = ex2_approx(y.y);
           sum2[e & 1] = fadd2(sum2[e & 1], pk2(p0, p1));
           pk[e] = __uint_as_float(pack2<S::BF16>(p0, p1));
         }
-        tm_store<32>(tS + c * 32, pk);
+      };
+      auto hand_over = [&](int half) {
         tm_store_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) tc_mbar_arrive(&ctl->pfull[k][c]);
+        if (lane == 0) tc_mbar_arrive(&ctl->pfull[k][half]);
+      };
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float pk[16];
+        weights(*reinterpret_cast<float(*)[32]>(&v[c * 32]), pk);
+        tm_store<16>(tS + c * 16, pk);
+        if (c & 1) hand_over(c >> 1);
       }
       const float2 s0 = upk2(sum2[0]), s1 = upk2(sum2[1]);
       l += (s0.x + s0.y) + (s1.x + s1.y);

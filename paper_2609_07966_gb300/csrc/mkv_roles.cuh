@@ -290,6 +290,14 @@ __device__ __forceinline__ bool non_finite(uint16_t x) {
   return (x & e) == e;
 }
 
+// Whether any of eight packed values is an infinity or NaN: adding one to an all-ones exponent carries into the sign.
+template <bool BF16>
+__device__ __forceinline__ bool any_non_finite(const uint4& x) {
+  constexpr uint32_t one = BF16 ? 0x00800080u : 0x04000400u;
+  const uint32_t a = ((x.x & 0x7fff7fffu) + one) | ((x.y & 0x7fff7fffu) + one);
+  const uint32_t b = ((x.z & 0x7fff7fffu) + one) | ((x.w & 0x7fff7fffu) + one);
+  return ((a | b) & 0x80008000u) != 0;
+}
 // Zeroes the non-finite values among eight packed ones; whether there were any.
 template <bool BF16>
 __device__ __forceinline__ bool bad_pairs(uint4& x) {
