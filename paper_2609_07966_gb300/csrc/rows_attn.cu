@@ -639,29 +639,23 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         // the end.  (Latent: the scores of this tile are complete, so its keys may be overwritten.)
         if (tr || valid < KT) {
           if (!S::SHARED) wait(&ctl->vfull[g % S::AHEAD], (uint32_t)((g / S::AHEAD) & 1));
-          // (a thread's pieces of an atom are a multiple of 8 rows apart, so the swizzle leaves them at equal steps)
-          constexpr int kStep = S::SOFT / 8;               // rows between a thread's pieces
-          const int r0 = threadIdx.x >> 3;
+          const int r0 = tr ? 0 : valid, r1 = tr ? a.n : KT;
 #pragma unroll 1
-          for (int at = 0; at < S::VA; ++at) {
+          for (int e = threadIdx.x; e < (r1 - r0) * 8 * S::VA; e += S::SOFT) {
+            const int r = r0 + e / (8 * S::VA), x = e % (8 * S::VA), at = x >> 3;
             const int s = (g * CH + (S::SHARED ? at / (S::MV / 64) : 1)) % S::SLOTS;
-            uint8_t* piece = sm + S::KV_OFF + s * S::SLOT + (S::SHARED ? at % (S::MV / 64) : at) * S::ATOM +
-                             mn_offset<64>(r0, threadIdx.x & 7);
-#pragma unroll
-            for (int x = 0; x < KT; x += kStep) {
-              const int r = r0 + x;
-              uint4* p8 = reinterpret_cast<uint4*>(piece + x * 128);
-              if (r >= KT) break;                          // (more threads than pieces)
-              if (r >= valid) {
-                if (!tr) *p8 = make_uint4(0, 0, 0, 0);     // (the copy left zeros past the drafted tokens)
-              } else if (tr) {
-                uint4 raw = *p8;
-                if (any_non_finite<S::BF16>(raw)) {
-                  bad_pairs<S::BF16>(raw);
-                  *p8 = raw;
-                  atomicOr(reinterpret_cast<unsigned long long*>(&ctl->nonfinite), 1ull << r);
-                }
-              }
+            uint4* p8 = reinterpret_cast<uint4*>(sm + S::KV_OFF + s * S::SLOT +
+                                                 (S::SHARED ? at % (S::MV / 64) : at) * S::ATOM +
+                                                 mn_offset<64>(r, x & 7));
+            if (!tr) {
+              *p8 = make_uint4(0, 0, 0, 0);
+              continue;
+            }
+            uint4 raw = *p8;
+            if (any_non_finite<S::BF16>(raw)) {
+              bad_pairs<S::BF16>(raw);
+              *p8 = raw;
+              atomicOr(reinterpret_cast<unsigned long long*>(&ctl->nonfinite), 1ull << r);
             }
           }
         }
