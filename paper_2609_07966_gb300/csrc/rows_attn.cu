@@ -18,7 +18,8 @@
 //             shared memory (each CTA gets every piece's slice of its dims), so one launch does it all;
 //   runs      the tiles of all units laid end to end, an equal run for every CTA, whatever the entries' lengths; a unit
 //             inside one run is written directly, the pieces of a unit that several runs share go to the workspace
-//             and join_kernel adds them up.
+//             and join_kernel adds them up.  With several row blocks a run belongs to as many CTAs, one block each, that
+//             meet its keys at the same time and so share them in L2.
 //
 // Roles: warps 0..4g-1 are the softmax (a thread holds one key and some rows), then one warp loads chunks by TMA
 // into a ring of slots and one issues products, taking whichever is ready: a finished tile's second product
@@ -59,6 +60,7 @@ constexpr float kNoMax = -1e30f;    // running maximum of a row that has seen no
 struct RowsArgs {
   int B, n, H, Hkv, G;              // G: query heads per key head (latent: H)
   int R, row_blocks;                // rows per (entry, key head): n G; their blocks of N
+  int side, in_run;                 // CTAs that take a run together, a row block each (or 1); row blocks within a run (or 1)
   int log_g;                        // FP16 caches: log2 G
   int cluster, log_cluster;         // CTAs a unit, joined in the kernel (a power of two); 0: runs over all units
   bool tree;
@@ -175,8 +177,9 @@ struct Pieces {
   int b, per;               // units per entry
   // the current piece: unit `u` of entry b, its tiles t0 .. t1 - 1 of `tiles`
   int u, t0, t1, tiles, len, index;
+  int kvh, rb;              // its key head and row block
   __device__ __forceinline__ Pieces(const RowsArgs& args, const RowsCtl* c)
-      : a(args), cur(c->run0), end(c->run1), base(c->base), b(c->b0), per(args.Hkv * args.row_blocks), u(c->u0 - 1),
+      : a(args), cur(c->run0), end(c->run1), base(c->base), b(c->b0), per(args.Hkv * args.in_run), u(c->u0 - 1),
         len(c->len0), index(-1) {}
   __device__ __forceinline__ bool next() {
     if (cur >= end) return false;
@@ -189,6 +192,8 @@ struct Pieces {
       u = 0;
       len = entry_len(a, ++b);
     }
+    kvh = a.in_run == 1 ? u : u / a.in_run;
+    rb = a.side > 1 ? (int)(blockIdx.x % a.side) : u - kvh * a.in_run;
     t0 = cur - base - u * tiles;
     t1 = std::min(tiles, t0 + (end - cur));
     cur += t1 - t0;
@@ -269,7 +274,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       ctl->fail = ctl->q_loads = ctl->loaded = ctl->scores = ctl->values = 0;
     }
     pdl_wait_and_trigger();
-    const int per = a.Hkv * a.row_blocks;
+    const int per = a.Hkv * a.in_run;
     if (a.cluster > 0) {
       if (lane == 0) {
         const int unit = blockIdx.x >> a.log_cluster, i = blockIdx.x & (a.cluster - 1), b = unit / per, u = unit - b * per;
@@ -288,8 +293,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       for (int b = lane + 32; b < a.B; b += 32) total += entry_tiles<KT>(a, b) * per;
 #pragma unroll
       for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-      const Runs rs(total, gridDim.x);
-      const int i = blockIdx.x, run0 = i < rs.runs ? rs.start(i) : 0;
+      const Runs rs(total, a.side == 1 ? gridDim.x : gridDim.x / a.side);
+      const int i = a.side == 1 ? blockIdx.x : blockIdx.x / a.side, run0 = i < rs.runs ? rs.start(i) : 0;
       const int run1 = i < rs.runs && total > 0 ? rs.start(i + 1) : 0;
       // the entry that holds tile run0
       int base = 0, b0 = 0;
@@ -344,7 +349,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         int g = 0, slot = 0, lap = 0;                       // tiles loaded so far; next ring slot, times around
         bool ok = true;
         while (ok && p.next()) {
-          const int kvh = p.u / a.row_blocks, row0 = p.u % a.row_blocks * N;
+          const int kvh = p.kvh, row0 = p.rb * N;
           if (p.index > 0) ok = wait_or_fail(&ctl->qempty, (uint32_t)((p.index - 1) & 1), fail, status);
           if (!ok) break;
           tc_mbar_expect_tx(&ctl->qfull, S::KA * S::QATOM);
@@ -402,7 +407,9 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         while (p.next())
           if (p.t0 == 0) {
             const int u0 = p.base + p.u * p.tiles;
-            a.joint[p.b * p.per + p.u] = Joint{(int)blockIdx.x, p.index > 0 ? 1 : 0, rs.of(u0 + p.tiles - 1) - (int)blockIdx.x + 1};
+            const int run = a.side == 1 ? blockIdx.x : blockIdx.x / a.side;
+            a.joint[((int64_t)p.b * a.Hkv + p.kvh) * a.row_blocks + p.rb] =
+                Joint{run, p.index > 0 ? 1 : 0, rs.of(u0 + p.tiles - 1) - run + 1};
           }
       }
     } else if (warp == kMma) {
@@ -524,7 +531,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
     Pieces<KT> p(a, ctl);
     int g = 0;                                            // tiles met by this CTA so far
     while (p.next()) {
-      const int nt = p.t1 - p.t0, kvh = p.u / a.row_blocks, row0 = p.u % a.row_blocks * N;
+      const int nt = p.t1 - p.t0, kvh = p.kvh, row0 = p.rb * N;
       const int rows = std::min(N, a.R - row0);
       const bool has_tree = a.tree && p.t1 == p.tiles;
       if (has_tree) {                                     // for every drafted token, the rows that see it
@@ -874,7 +881,9 @@ __global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
   const Joint jt = a.joint[bh * a.row_blocks + r / N];     // (not written for an entry without tiles)
   const int count = tiles > 0 ? jt.count : 1;
   // a piece's place in the workspace; piece i is of run jt.run + i
-  auto place = [&](int i) { return ((int64_t)(jt.run + i) * 2 + (i == 0 ? jt.slot : 0)) * N + r % N; };
+  // (a.side CTAs share a run: the row's block tells which of them)
+  const int rn = r % N, step = a.side * 2 * N, at0 = jt.run * step + (a.side > 1 ? r / N : 0) * 2 * N + rn;
+  auto place = [&](int i) { return at0 + i * step + (i == 0 ? jt.slot * N : 0); };
   // threads of one row: a maximum and a sum over all of its pieces (all threads of the CTA take part)
   auto all = [&](float v, bool maximum, int slot) {
 #pragma unroll
@@ -915,21 +924,21 @@ __global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   const float inv = L == 0.f ? 0.f : 1.f / L;
   if (tiles > 0 && inv != 0.f) {
-    constexpr int kAt = 12;                              // pieces whose loads are under way together
+    // kAt pieces' loads under way together, none behind a condition (past the last piece it is loaded again, for nothing)
+    constexpr int kAt = DV >= 256 ? 16 : 8;
     for (int i0 = 0; i0 < count; i0 += kAt) {
       float4 y[kAt];
 #pragma unroll
       for (int k = 0; k < kAt; ++k)
-        if (i0 + k < count) y[k] = *reinterpret_cast<const float4*>(a.part_o + place(i0 + k) * DV + d);
+        y[k] = *reinterpret_cast<const float4*>(a.part_o + (int64_t)place(std::min(i0 + k, count - 1)) * DV + d);
 #pragma unroll
-      for (int k = 0; k < kAt; ++k)
-        if (i0 + k < count) {
-          const float w = sw[g][i0 + k] * inv;
-          o.x += w * y[k].x;
-          o.y += w * y[k].y;
-          o.z += w * y[k].z;
-          o.w += w * y[k].w;
-        }
+      for (int k = 0; k < kAt; ++k) {
+        const float w = i0 + k < count ? sw[g][i0 + k] * inv : 0.f;
+        o.x = w == 0.f ? o.x : o.x + w * y[k].x;
+        o.y = w == 0.f ? o.y : o.y + w * y[k].y;
+        o.z = w == 0.f ? o.z : o.z + w * y[k].z;
+        o.w = w == 0.f ? o.w : o.w + w * y[k].w;
+      }
     }
   }
   uint2 h;
@@ -942,6 +951,7 @@ __global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
 struct Plan {
   int N, KT, R, row_blocks, ctas;
   int cluster;                 // CTAs a unit; 0: runs
+  int side;                    // CTAs that take a run together
   int64_t tiles;               // of all units when every entry is full
   size_t joint_off, ml_off, o_off, bytes;
 };
@@ -963,6 +973,10 @@ Plan plan_rows(const RowsCall& c) {
   const int64_t equal = ceil_div(per_unit * units, kNumSMs);
   const int k = units <= 15 ? 8 : units <= 36 ? 4 : units <= 76 ? 2 : 0;
   p.cluster = k > 0 && ceil_div(per_unit, k) <= equal + equal / 7 + 4 ? k : 0;
+  // A run for all row blocks at once where that leaves few SMs without one (12 tokens of 32 heads over 32K rows, 6
+  // blocks: 25 x 6 CTAs; as 152 runs of single blocks the keys came from HBM 3.6 times).
+  p.side = 1;
+  if (p.cluster == 0 && p.row_blocks > 1 && p.ctas / p.row_blocks * p.row_blocks >= p.ctas * 7 / 8) p.side = p.row_blocks;
   const size_t parts = (size_t)p.ctas * 2 * p.N;       // (of the runs, so that the size does not fall with T_cap or n)
   p.joint_off = kCounterBytes;
   p.ml_off = p.joint_off + align256((size_t)c.B * c.Hkv * p.row_blocks * sizeof(Joint));
@@ -1002,7 +1016,8 @@ cudaError_t launch_shape(const RowsCall& c, const Plan& p, RowsArgs a, cudaStrea
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim = {(unsigned)std::max(1, p.cluster), 1, 1};
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.cluster > 0 ? (unsigned)(B * Hkv * p.row_blocks * p.cluster) : (unsigned)p.ctas);
+  cfg.gridDim = dim3(p.cluster > 0 ? (unsigned)(B * Hkv * p.row_blocks * p.cluster)
+                                    : (unsigned)(p.ctas / p.side * p.side));
   cfg.blockDim = dim3(S::THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -1050,6 +1065,8 @@ cudaError_t launch_rows_attention(const RowsCall& c, void* ws, cudaStream_t st) 
   a.G = c.H / c.Hkv;
   a.R = p.R;
   a.row_blocks = p.row_blocks;
+  a.side = p.side;
+  a.in_run = p.row_blocks / p.side;
   a.cluster = p.cluster;
   for (a.log_cluster = 0; (1 << a.log_cluster) < a.cluster;) ++a.log_cluster;
   a.log_g = -1;
