@@ -18,12 +18,18 @@
 //             shared memory (each CTA gets every piece's slice of its dims), so one launch does it all;
 //   runs      the tiles of all units laid end to end, an equal run for every CTA, whatever the entries' lengths; a unit
 //             inside one run is written directly, the pieces of a unit that several runs share go to the workspace
-//             and join_kernel adds them up.  With several row blocks a run belongs to as many CTAs, one block each, that
-//             meet its keys at the same time and so share them in L2.
+//             and join_kernel adds them up.  With several row blocks a run belongs to as many CTAs, one block each,
+//             that meet its keys at the same time and so share them in L2.
 //
 // Roles: warps 0..4g-1 are the softmax (a thread holds one key and some rows), then one warp loads chunks by TMA
 // into a ring of slots and one issues products, taking whichever is ready: a finished tile's second product
 // first (it frees slots), else the next chunk of the scores.
+//
+// Bound by memory while a block's N rows need fewer tensor cycles a tile than its copy takes (64 keys of 576 dims: 3100
+// cycles at an SM's share of HBM against 1600 at N = 32, 2000 at N = 64), else by a tile's chain of scores, softmax and
+// second product.  Measured (GPU time): 16 drafted tokens over an 8 x 8K FP16 cache (32/8 heads, D 128) 48 us, 5.5
+// TB/s; one latent token over 8 x 8K rows (32 heads, rank 512) 28.6 us, 2.6 TB/s; 12 drafted over 4 x 32K ragged rows
+// 122 us, 0.73 PFLOP/s; one latent token over 777 rows 10.4 us.
 //
 // The running maximum m is only raised when some score of a tile passes it by 2^8 (weights then stay below
 // 2^14 with the offset below), which a group-wide vote finds: after the first tiles almost never, so the O^T
@@ -60,7 +66,8 @@ constexpr float kNoMax = -1e30f;    // running maximum of a row that has seen no
 struct RowsArgs {
   int B, n, H, Hkv, G;              // G: query heads per key head (latent: H)
   int R, row_blocks;                // rows per (entry, key head): n G; their blocks of N
-  int side, in_run;                 // CTAs that take a run together, a row block each (or 1); row blocks within a run (or 1)
+  int side;                         // CTAs that take a run together, a row block each (or 1)
+  int in_run;                       // row blocks within a run (or 1)
   int log_g;                        // FP16 caches: log2 G
   int cluster, log_cluster;         // CTAs a unit, joined in the kernel (a power of two); 0: runs over all units
   bool tree;
@@ -277,7 +284,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
     const int per = a.Hkv * a.in_run;
     if (a.cluster > 0) {
       if (lane == 0) {
-        const int unit = blockIdx.x >> a.log_cluster, i = blockIdx.x & (a.cluster - 1), b = unit / per, u = unit - b * per;
+        const int unit = blockIdx.x >> a.log_cluster, i = blockIdx.x & (a.cluster - 1);
+        const int b = unit / per, u = unit - b * per;
         const int len = entry_len(a, b), tiles = unit_tiles<KT>(a, len);
         ctl->len0 = len;
         ctl->b0 = b;
@@ -742,8 +750,9 @@ __global__ void __launch_bounds__(S::THREADS, 1)
               const float y = __shfl_xor_sync(0xffffffffu, odd ? x0 : x1, 1);
               const uint32_t h = odd ? pack2<S::BF16>(y, x1) : pack2<S::BF16>(x0, y);
               const int r = grp * C + c + (odd ? 1 : 0), row = row0 + r;
-              const int64_t at = S::SHARED ? (int64_t)p.b * a.R + row
-                                           : ((int64_t)p.b * a.n + (row >> a.log_g)) * a.H + kvh * a.G + (row & (a.G - 1));
+              const int64_t at =
+                  S::SHARED ? (int64_t)p.b * a.R + row
+                            : ((int64_t)p.b * a.n + (row >> a.log_g)) * a.H + kvh * a.G + (row & (a.G - 1));
               if (r < rows && dlive) *reinterpret_cast<uint32_t*>(a.out + at * S::DV + (d & ~1)) = h;
             }
           }
@@ -795,7 +804,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         float o[CJ];
         tm_load<CJ>(tO + ((uint32_t)(q * 32) << 16) + (uint32_t)(mb * N + col), o);
         if (nf != 0) add_non_finite<S>(a, nf, b, kvh, row0 + col, rows - col, d, o);
-        const uint32_t to = cluster_addr(pieces + ((rank * N + col) << log_s) + (d & (slice - 1)), (uint32_t)(d >> log_s));
+        const uint32_t to =
+            cluster_addr(pieces + ((rank * N + col) << log_s) + (d & (slice - 1)), (uint32_t)(d >> log_s));
         if (S::MV == 128 || lane < 16) {
 #pragma unroll
           for (int c = 0; c < CJ; ++c)
@@ -849,7 +859,8 @@ __global__ void __launch_bounds__(S::THREADS, 1)
     if (ctl->q_loads > 0) tc_mbar_wait(&ctl->qfull, (uint32_t)((ctl->q_loads - 1) & 1), kRoleWaitNs);
     // (a tile whose loads were only begun when its wait ran out: nothing says when those end but time)
     for (int g = std::max(0, ctl->loaded - S::AHEAD); g <= ctl->loaded; ++g) {
-      tc_mbar_wait(&ctl->kfull[g % S::AHEAD], (uint32_t)((g / S::AHEAD) & 1), g < ctl->loaded ? kRoleWaitNs : 10000000ull);
+      tc_mbar_wait(&ctl->kfull[g % S::AHEAD], (uint32_t)((g / S::AHEAD) & 1),
+                   g < ctl->loaded ? kRoleWaitNs : 10000000ull);
       if (!S::SHARED && g < ctl->loaded)
         tc_mbar_wait(&ctl->vfull[g % S::AHEAD], (uint32_t)((g / S::AHEAD) & 1), kRoleWaitNs);
     }
@@ -920,11 +931,12 @@ __global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
   __syncthreads();
   if (want >= rows || (count <= 1 && tiles > 0)) return;   // one run held the whole unit
   const int d = x * 4;
-  const int64_t at = (a.log_g < 0 ? row : ((int64_t)b * a.n + (r >> a.log_g)) * a.H + kvh * a.G + (r & (a.G - 1))) * DV + d;
+  const int64_t at =
+      (a.log_g < 0 ? row : ((int64_t)b * a.n + (r >> a.log_g)) * a.H + kvh * a.G + (r & (a.G - 1))) * DV + d;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   const float inv = L == 0.f ? 0.f : 1.f / L;
   if (tiles > 0 && inv != 0.f) {
-    // kAt pieces' loads under way together, none behind a condition (past the last piece it is loaded again, for nothing)
+    // kAt pieces' loads under way together, none behind a condition (past the last piece it is loaded again, unused)
     constexpr int kAt = DV >= 256 ? 16 : 8;
     for (int i0 = 0; i0 < count; i0 += kAt) {
       float4 y[kAt];
@@ -966,17 +978,21 @@ Plan plan_rows(const RowsCall& c) {
   p.ctas = (int)std::min<int64_t>(p.tiles, kNumSMs);
   // Clusters where as many as there are units run beside each other (one CTA an SM: 76 of 2, 36 of 4, 15 of 8) and no
   // CTA's share is much longer than an equal one: joining through the workspace costs about four tiles' time and a
-  // seventh of a long run's.  Measured, clusters against runs: 16 drafted tokens over 8 x 8K (64 units) 49 against 54 us,
-  // 8 over 3000 tokens (8 units) 11 against 17, one latent token over 8 x 1000 (8 units) 12.0 against 13.7; but 28 (runs)
-  // against 34 for one latent token over 8 x 8K.
+  // seventh of a long run's.  Measured, clusters against runs: 16 drafted tokens over 8 x 8K (64 units) 49 against 56
+  // us, 8 over 3000 tokens (8 units) 10 against 16, one latent token over 8 x 1000 (8 units) 10.9 against 13.4; but 32
+  // against 28 for one latent token over 8 x 8K.  One entry's FP16 key heads wait for the runs' join longer than for a
+  // share twice as long (8 units: 12000 tokens 17.8 against 21.3, 26000 28.8 against 30.8; 4 units, 8000 tokens 13.1
+  // against 18.2; latent 4000 rows 17.5 against 13.4); with more entries, unequal lengths are better off in runs.
   const int64_t units = (int64_t)c.B * c.Hkv * p.row_blocks, per_unit = ceil_div(c.T_cap, p.KT) + 1;
   const int64_t equal = ceil_div(per_unit * units, kNumSMs);
   const int k = units <= 15 ? 8 : units <= 36 ? 4 : units <= 76 ? 2 : 0;
-  p.cluster = k > 0 && ceil_div(per_unit, k) <= equal + equal / 7 + 4 ? k : 0;
+  const int64_t most = !c.latent && c.B == 1 ? 2 * equal + 6 : equal + equal / 7 + 4;
+  p.cluster = k > 0 && ceil_div(per_unit, k) <= most ? k : 0;
   // A run for all row blocks at once where that leaves few SMs without one (12 tokens of 32 heads over 32K rows, 6
   // blocks: 25 x 6 CTAs; as 152 runs of single blocks the keys came from HBM 3.6 times).
   p.side = 1;
-  if (p.cluster == 0 && p.row_blocks > 1 && p.ctas / p.row_blocks * p.row_blocks >= p.ctas * 7 / 8) p.side = p.row_blocks;
+  if (p.cluster == 0 && p.row_blocks > 1 && p.ctas / p.row_blocks * p.row_blocks >= p.ctas * 7 / 8)
+    p.side = p.row_blocks;
   const size_t parts = (size_t)p.ctas * 2 * p.N;       // (of the runs, so that the size does not fall with T_cap or n)
   p.joint_off = kCounterBytes;
   p.ml_off = p.joint_off + align256((size_t)c.B * c.Hkv * p.row_blocks * sizeof(Joint));

@@ -74,6 +74,13 @@ def test_long_contexts_split(T):
     _check(c, _run(c), f"T{T}")
 
 
+@pytest.mark.parametrize("Hkv,T,T_cap", [(8, 9001, 12000), (8, 100, 12000), (4, 7999, 8000), (2, 33000, 33008)])
+def test_one_long_entry(Hkv, T, T_cap):
+    """One entry alone, with capacity to spare: a key head's keys are split over a cluster or over runs."""
+    c = _case(1, Hkv, 4, 128, 6, T_cap, [T], seed=T, junk=float("nan"))
+    _check(c, _run(c), f"T{T} of {T_cap}")
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_many_ragged_units(D):
     """More units than SMs, of unequal lengths, some empty: runs of tiles that hold whole units and parts of others."""
