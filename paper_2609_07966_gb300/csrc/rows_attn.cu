@@ -876,14 +876,18 @@ __global__ void __launch_bounds__(S::THREADS, 1)
 
 // The units that several runs share: out = sum_s 2^(m_s - M) o_s / sum_s 2^(m_s - M) l_s over their pieces; zeros for
 // the units of an entry without any token.  A CTA takes 512 / DV rows, a thread four dims of one; the weights of a
-// row's pieces are worked out side by side first, so that the pieces' loads do not wait for one another.
+// row's pieces are worked out side by side first, so that the pieces' loads do not wait for one another.  With many
+// pieces a row PARTS groups of 128 threads take kAt pieces in turn, and their sums are added in the groups' order.
 constexpr int kJoinWeights = 160;      // at most one piece per run
-template <bool BF16, int KT, int DV>
-__global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
+constexpr int kJoinThreads = 128;      // of a group
+template <bool BF16, int KT, int DV, int PARTS>
+__global__ void __launch_bounds__(kJoinThreads * PARTS) join_kernel(const RowsArgs a, int N) {
   constexpr int kPer = 512 / DV, kGrp = DV / 4;          // rows a CTA, threads a row
-  __shared__ float sw[kPer][kJoinWeights], sred[4][2];
+  __shared__ float sw[kPer][kJoinWeights], sred[4 * PARTS][2];
+  __shared__ float4 ssum[PARTS > 1 ? PARTS - 1 : 1][kJoinThreads];
   pdl_wait_and_trigger();
-  const int g = threadIdx.x / kGrp, x = threadIdx.x % kGrp;
+  const int part = threadIdx.x / kJoinThreads, tid = threadIdx.x % kJoinThreads;
+  const int g = tid / kGrp, x = tid % kGrp;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.R, want = (int64_t)blockIdx.x * kPer + g;
   const int64_t row = want < rows ? want : rows - 1;     // (b Hkv + kvh) R + r
   const int64_t bh = row / a.R;
@@ -895,7 +899,7 @@ __global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
   // (a.side CTAs share a run: the row's block tells which of them)
   const int rn = r % N, step = a.side * 2 * N, at0 = jt.run * step + (a.side > 1 ? r / N : 0) * 2 * N + rn;
   auto place = [&](int i) { return at0 + i * step + (i == 0 ? jt.slot * N : 0); };
-  // threads of one row: a maximum and a sum over all of its pieces (all threads of the CTA take part)
+  // a group's threads of one row: a maximum and a sum over all of its pieces (all threads of the CTA take part)
   auto all = [&](float v, bool maximum, int slot) {
 #pragma unroll
     for (int d = (kGrp < 32 ? kGrp : 32) / 2; d; d >>= 1) {
@@ -924,21 +928,21 @@ __global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
   for (int k = 0; k < (kJoinWeights + kGrp - 1) / kGrp; ++k) {
     const int i = k * kGrp + x;
     const float w = ml[k].x == -INFINITY ? 0.f : ex2_approx(ml[k].x - M);
-    if (i < kJoinWeights) sw[g][i] = w;
+    if (part == 0 && i < kJoinWeights) sw[g][i] = w;
     L += w * ml[k].y;
   }
   L = all(L, false, 1);
   __syncthreads();
-  if (want >= rows || (count <= 1 && tiles > 0)) return;   // one run held the whole unit
+  const bool live = want < rows && (count > 1 || tiles <= 0);   // (else one run held the whole unit)
   const int d = x * 4;
   const int64_t at =
       (a.log_g < 0 ? row : ((int64_t)b * a.n + (r >> a.log_g)) * a.H + kvh * a.G + (r & (a.G - 1))) * DV + d;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  if (tiles > 0 && inv != 0.f) {
+  if (live && tiles > 0 && inv != 0.f) {
     // kAt pieces' loads under way together, none behind a condition (past the last piece it is loaded again, unused)
-    constexpr int kAt = DV >= 256 ? 16 : 8;
-    for (int i0 = 0; i0 < count; i0 += kAt) {
+    constexpr int kAt = DV >= 256 && PARTS == 1 ? 16 : 8;
+    for (int i0 = part * kAt; i0 < count; i0 += kAt * PARTS) {
       float4 y[kAt];
 #pragma unroll
       for (int k = 0; k < kAt; ++k)
@@ -953,6 +957,17 @@ __global__ void __launch_bounds__(128) join_kernel(const RowsArgs a, int N) {
       }
     }
   }
+  if constexpr (PARTS > 1) {
+    if (part > 0) ssum[part - 1][tid] = o;
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int k = 0; k < PARTS - 1; ++k) {
+      const float4 y = ssum[k][tid];
+      o = make_float4(o.x + y.x, o.y + y.y, o.z + y.z, o.w + y.w);
+    }
+  }
+  if (!live) return;
   uint2 h;
   h.x = pack2<BF16>(o.x, o.y);
   h.y = pack2<BF16>(o.z, o.w);
@@ -977,17 +992,16 @@ Plan plan_rows(const RowsCall& c) {
   p.tiles = (ceil_div(c.T_cap, p.KT) + 1) * c.B * c.Hkv * p.row_blocks;
   p.ctas = (int)std::min<int64_t>(p.tiles, kNumSMs);
   // Clusters where as many as there are units run beside each other (one CTA an SM: 76 of 2, 36 of 4, 15 of 8) and no
-  // CTA's share is much longer than an equal one: joining through the workspace costs about four tiles' time and a
-  // seventh of a long run's.  Measured, clusters against runs: 16 drafted tokens over 8 x 8K (64 units) 49 against 56
-  // us, 8 over 3000 tokens (8 units) 10 against 16, one latent token over 8 x 1000 (8 units) 10.9 against 13.4; but 32
-  // against 28 for one latent token over 8 x 8K.  One entry's FP16 key heads wait for the runs' join longer than for a
-  // share twice as long (8 units: 12000 tokens 17.8 against 21.3, 26000 28.8 against 30.8; 4 units, 8000 tokens 13.1
-  // against 18.2; latent 4000 rows 17.5 against 13.4); with more entries, unequal lengths are better off in runs.
+  // CTA's share is much longer than an equal one: joining through the workspace costs about four tiles' time (two of
+  // the 64-row tiles, which take longer), and a seventh of a long run's where HBM is the bound.  Measured, clusters
+  // against runs: 16 drafted tokens over 8 x 8K (64 units) 49 against 53 us, 8 over 3000 tokens (8 units) 10.1 against
+  // 13.5, one latent token over 8 x 1000 (8 units) 11.0 against 12.4; but 32 against 27 for one latent token over 8 x
+  // 8K, and 36.6 against 31.9 for 5 over 8 x 4K (24 units, ragged); 32 x 8K (32 units) 59 against 62.
   const int64_t units = (int64_t)c.B * c.Hkv * p.row_blocks, per_unit = ceil_div(c.T_cap, p.KT) + 1;
   const int64_t equal = ceil_div(per_unit * units, kNumSMs);
+  const int64_t spare = (p.N <= 32 ? 4 : 2) + (p.row_blocks == 1 ? equal / 7 : 0);
   const int k = units <= 15 ? 8 : units <= 36 ? 4 : units <= 76 ? 2 : 0;
-  const int64_t most = !c.latent && c.B == 1 ? 2 * equal + 6 : equal + equal / 7 + 4;
-  p.cluster = k > 0 && ceil_div(per_unit, k) <= most ? k : 0;
+  p.cluster = k > 0 && ceil_div(per_unit, k) <= equal + spare ? k : 0;
   // A run for all row blocks at once where that leaves few SMs without one (12 tokens of 32 heads over 32K rows, 6
   // blocks: 25 x 6 CTAs; as 152 runs of single blocks the keys came from HBM 3.6 times).
   p.side = 1;
@@ -1043,7 +1057,11 @@ cudaError_t launch_shape(const RowsCall& c, const Plan& p, RowsArgs a, cudaStrea
   if (e == cudaSuccess) e = cudaPeekAtLastError();
   if (e != cudaSuccess || p.cluster > 0) return e;
   const unsigned grid = (unsigned)ceil_div(B * Hkv * p.R, 512 / S::DV);
-  return launch_pdl(join_kernel<S::BF16, S::KT, S::DV>, dim3(grid), dim3(128), 0, st, a, (int)S::N);
+  // Four groups where a unit has more pieces (about) than one takes at a time and the CTAs fit beside each other (one
+  // latent token over 32000 rows 35.5 -> 25.6 us, over 8 x 8K 28.7 -> 26.8; but 16 x 4K, 512 CTAs, 26.8 -> 28.8).
+  if (p.ctas / (B * Hkv * p.row_blocks) >= 8 && grid <= 2 * kNumSMs)
+    return launch_pdl(join_kernel<S::BF16, S::KT, S::DV, 4>, dim3(grid), dim3(4 * kJoinThreads), 0, st, a, (int)S::N);
+  return launch_pdl(join_kernel<S::BF16, S::KT, S::DV, 1>, dim3(grid), dim3(kJoinThreads), 0, st, a, (int)S::N);
 }
 
 // rows a block, ring slots, last-key-atom slots, weight buffers: what an SM's shared memory holds
