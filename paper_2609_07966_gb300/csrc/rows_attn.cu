@@ -28,7 +28,7 @@
 // Bound by memory while a block's N rows need fewer tensor cycles a tile than its copy takes (64 keys of 576 dims: 3100
 // cycles at an SM's share of HBM against 1600 at N = 32, 2000 at N = 64), else by a tile's chain of scores, softmax and
 // second product.  Measured (GPU time): 16 drafted tokens over an 8 x 8K FP16 cache (32/8 heads, D 128) 48 us, 5.5
-// TB/s; one latent token over 8 x 8K rows (32 heads, rank 512) 28.6 us, 2.6 TB/s; 12 drafted over 4 x 32K ragged rows
+// TB/s; one latent token over 8 x 8K rows (32 heads, rank 512) 26.5 us, 2.9 TB/s; 12 drafted over 4 x 32K ragged rows
 // 122 us, 0.73 PFLOP/s; one latent token over 777 rows 10.4 us.
 //
 // The running maximum m is only raised when some score of a tile passes it by 2^8 (weights then stay below
