@@ -43,6 +43,8 @@ constexpr int kBR = 128;            // rows a block, keys a tile
 constexpr float kRaise = 8.f;       // a score may pass the running maximum by this (log2) before it is raised
 constexpr float kOffset = 6.f;      // weights carry 2^kOffset (fp16: full precision down to 2^-20 of the maximum)
 constexpr float kNoMax = -1e30f;    // running maximum of a row that has seen nothing
+// Up to this maximum (log2) an unrounded product of score and scale is within a half of the rounded one.
+constexpr float kFused = 16777216.f;
 
 struct PrefillArgs {
   int n, H;
@@ -365,7 +367,17 @@ __global__ void __launch_bounds__(kPThreads, 1)
         }
         fence_async_smem();
       }
-      const uint64_t sc2 = pk2(a.scale_log2, a.scale_log2), off2 = pk2(kOffset - m, kOffset - m);
+      // A weight's exponent is one fused product and sum, score x scale - m, in which the product is not rounded but the
+      // maximum it meets is: a factor that all of a row's weights share, unless the maximum is so large that its
+      // rounding alone passes the exponent's range.  Then the product is rounded too, as the maximum was.
+      float sc = a.scale_log2, off = kOffset - m;
+      if (__any_sync(0xffffffffu, fabsf(m) > kFused && m != kNoMax)) {
+#pragma unroll
+        for (int c = 0; c < kBR; ++c) v[c] = __fsub_rn(__fmul_rn(v[c], sc), m);
+        sc = 1.f;
+        off = kOffset;
+      }
+      const uint64_t sc2 = pk2(sc, sc), off2 = pk2(off, off);
       uint64_t sum2[2] = {0ull, 0ull};
       // 32 scores -> 16 columns of packed weights
       auto weights = [&](const float(&x)[32], float(&pk)[16]) {
