@@ -42,7 +42,7 @@ namespace {
 constexpr int kBR = 128;            // rows a block, keys a tile
 constexpr float kRaise = 8.f;       // a score may pass the running maximum by this (log2) before it is raised
 constexpr float kOffset = 6.f;      // weights carry 2^kOffset (fp16: full precision down to 2^-20 of the maximum)
-constexpr float kNoMax = -1e30f;    // running maximum of a row that has seen nothing
+constexpr float kNoMax = -3.402823466e+38f;   // running maximum of a row that has seen nothing: no score is below it
 // Up to this maximum (log2) an unrounded product of score and scale is within a half of the rounded one.
 constexpr float kFused = 16777216.f;
 

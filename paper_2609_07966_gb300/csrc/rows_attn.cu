@@ -61,7 +61,7 @@ constexpr float kRaise = 8.f;       // a score may pass the running maximum by t
 // Weights carry 2^kOffset, so that those far below the maximum keep full precision in fp16 (normal down to
 // 2^-20 of the maximum); it cancels in the division by their sum.
 constexpr float kOffset = 6.f;
-constexpr float kNoMax = -1e30f;    // running maximum of a row that has seen nothing
+constexpr float kNoMax = -3.402823466e+38f;   // running maximum of a row that has seen nothing: no score is below it
 
 struct RowsArgs {
   int B, n, H, Hkv, G;              // G: query heads per key head (latent: H)

@@ -40,3 +40,37 @@ def test_prefill_large_scores(dtype, q0, k0, better):
     """Past 2^31 a score times the scale, unrounded, is hundreds away from the rounded maximum."""
     torch_cuda()
     _prefill(dtype, q0, k0, better)
+
+
+# Negative scores near the end of the bf16 range's products: below -1e30.
+FAR = [("bf16", 2.0 ** 60, -2.0 ** 50, -2.0 ** 49), ("bf16", 2.0 ** 60, 2.0 ** 50, 2.0 ** 51)]
+
+
+@pytest.mark.parametrize("dtype,q0,k0,better", FAR)
+def test_prefill_far_scores(dtype, q0, k0, better):
+    torch_cuda()
+    _prefill(dtype, q0, k0, better)
+
+
+@pytest.mark.parametrize("dtype,q0,k0,better", SCORES + FAR)
+@pytest.mark.parametrize("T_cap", [320, 9000])
+def test_latent_far_scores(dtype, q0, k0, better, T_cap):
+    import torch
+    torch_cuda()
+    rng = np.random.default_rng(6)
+    B, n, H, lens, at, rank = 2, 2, 8, [300, 210], 170, 256
+    q = torch.zeros((B, n, H, rank + 64), device="cuda")
+    q[..., rank:] = q0
+    rows = randn(rng, (B, T_cap, rank + 64), dtype)
+    new = randn(rng, (B, n, rank + 64), dtype)
+    rows[..., rank:] = k0
+    new[..., rank:] = k0
+    rows[1, at, rank:] = better
+    q = q.to(rows.dtype)
+    masks = np.array([[0b01, 0b11]] * B, dtype=np.uint64)
+    out = calls.latent(dtype, q, rows, lens, new, masks)
+    for b, t in enumerate(lens):
+        keys = np.concatenate([f64(rows[b, :t]), f64(new[b])])
+        vis = np.repeat(L.tree_visible(masks[b], n, t), H, axis=0)
+        ref, mag = L.attend_visible(f64(q[b]).reshape(n * H, -1), keys, keys[:, :rank], vis, 192 ** -0.5)
+        check_attention(out[b].reshape(n * H, rank), ref, mag, dtype, f"b{b}")
