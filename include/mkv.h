@@ -469,8 +469,10 @@ mkv_status mkv_rocket_step(const mkv_config* cfg, const void* q, const void* k_n
  * mask uint64 [B][n]: drafted token i of entry b attends to every cached token
  * 0..T_len[b]-1 and to drafted token j iff bit j of mask[b][i] is set (its
  * ancestors and itself; bits n and above are ignored).  A token that sees
- * nothing (empty cache, no bit) gets zeros.  What a token does not see does
- * not reach its output, whatever bits (infinities, NaN) it holds.
+ * nothing (empty cache, no bit) gets zeros; one whose scores are all minus
+ * infinity gets NaN, as softmax has it (so in every call below).  What a token
+ * does not see does not reach its output, whatever bits (infinities, NaN) it
+ * holds.
  */
 
 /* Bytes of workspace mkv_tree_attention needs for n drafted tokens over caches

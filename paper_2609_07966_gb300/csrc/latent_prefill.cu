@@ -409,7 +409,8 @@ __global__ void __launch_bounds__(kPThreads, 1)
     // the other block's last tile may hold values zeroed for this one: its flags are complete once both are done
     if (nt[k] > 0) wait(&ctl->pvdone[k], (uint32_t)((nt[k] - 1) & 1));
     if (!dead) {
-      const float inv = l == 0.f || i >= ql ? 0.f : 1.f / l;
+      // zeros for a row that sees nothing; NaN for one whose scores are all minus infinity
+      const float inv = seen <= 0 ? 0.f : l == 0.f ? NAN : 1.f / l;
       uint16_t* dst = a.out + (((int64_t)b * a.n + i) * a.H + h) * S::DV;
       uint32_t any = 0;
       for (int w = 0; w < kFixWords; ++w) any |= ctl->nonfinite[w];

@@ -242,6 +242,21 @@ __device__ __forceinline__ void add_non_finite(const RowsArgs& a, uint64_t nf, i
   }
 }
 
+// Bit c: row `row + c` of the unit sees nothing (its entry holds no token and none of its drafted bits is set).  Such a
+// row gives zeros; a row that does see tokens, but with scores of minus infinity only, has no weights to divide by: NaN.
+template <int W>
+__device__ __forceinline__ uint32_t blind_rows(const RowsArgs& a, int len, int b, int row) {
+  if (len > 0) return 0;
+  uint32_t blind = 0;
+#pragma unroll 1
+  for (int c = 0; c < W; ++c) {
+    const int tok = (row + c) / a.G;
+    const uint64_t bits = a.tree && tok < a.n ? a.mask[(int64_t)b * a.n + tok] : 0;
+    if (bits << (kMaxTree - a.n) == 0) blind |= 1u << c;
+  }
+  return blind;
+}
+
 // First tile of CTA i of the 2^k that share a unit of `tiles`.
 __device__ __forceinline__ int cluster_tile(int tiles, int i, int k) { return (int)((int64_t)tiles * i >> k); }
 
@@ -723,9 +738,10 @@ __global__ void __launch_bounds__(S::THREADS, 1)
             a.part_ml[slot * N + x] = make_float2(all == 0.f ? -INFINITY : m[c], all);
           }
         }
+        const uint32_t blind = whole ? blind_rows<C>(a, p.len, p.b, row0 + grp * C) : 0;
         if (whole) {
 #pragma unroll
-          for (int c = 0; c < C; ++c) sum[c] = sum[c] == 0.f ? 0.f : 1.f / sum[c];
+          for (int c = 0; c < C; ++c) sum[c] = blind >> c & 1 ? 0.f : sum[c] == 0.f ? NAN : 1.f / sum[c];
         }
 #pragma unroll 1
         for (int mb = 0; mb < S::NB; ++mb) {
@@ -777,7 +793,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
     // comes from a cold instruction cache, about 14 cycles an instruction (unrolled, the weights alone took 7000).
     const int per = a.Hkv * a.row_blocks, b = ctl->b0, u = (int)(blockIdx.x >> a.log_cluster) - b * per;
     const int kvh = u / a.row_blocks, row0 = u % a.row_blocks * N, rows = std::min(N, a.R - row0);
-    const int tiles = unit_tiles<KT>(a, ctl->len0), rank = (int)cluster_rank();
+    const int len = ctl->len0, tiles = unit_tiles<KT>(a, len), rank = (int)cluster_rank();
     unsigned has = 0;                                                       // the CTAs that hold a piece
 #pragma unroll 1
     for (int i = 0; i < a.cluster; ++i)
@@ -829,7 +845,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         float sum = w * y.y;
 #pragma unroll
         for (int d = kMaxCluster / 2; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (has >> i & 1) x->x = sum == 0.f ? 0.f : w / sum;
+        if (has >> i & 1) x->x = sum == 0.f ? NAN : w / sum;
       }
       bar_sync(5, S::SOFT);
       if (*fail == 0) {
@@ -846,6 +862,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
               o.z += w * y.z;
               o.w += w * y.w;
             }
+          if (len <= 0 && blind_rows<1>(a, len, b, row)) o = make_float4(0.f, 0.f, 0.f, 0.f);
           const int64_t at = S::SHARED ? (int64_t)b * a.R + row
                                        : ((int64_t)b * a.n + (row >> a.log_g)) * a.H + kvh * a.G + (row & (a.G - 1));
           *reinterpret_cast<uint2*>(a.out + at * S::DV + (rank << log_s) + ds) =
@@ -938,8 +955,8 @@ __global__ void __launch_bounds__(kJoinThreads * PARTS) join_kernel(const RowsAr
   const int64_t at =
       (a.log_g < 0 ? row : ((int64_t)b * a.n + (r >> a.log_g)) * a.H + kvh * a.G + (r & (a.G - 1))) * DV + d;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  if (live && tiles > 0 && inv != 0.f) {
+  const float inv = L == 0.f ? NAN : 1.f / L;            // (a unit of several pieces has cached tokens: its rows see them)
+  if (live && tiles > 0) {
     // kAt pieces' loads under way together, none behind a condition (past the last piece it is loaded again, unused)
     constexpr int kAt = DV >= 256 && PARTS == 1 ? 16 : 8;
     for (int i0 = part * kAt; i0 < count; i0 += kAt * PARTS) {
