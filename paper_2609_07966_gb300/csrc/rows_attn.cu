@@ -966,11 +966,13 @@ __global__ void __launch_bounds__(kJoinThreads * PARTS) join_kernel(const RowsAr
         y[k] = *reinterpret_cast<const float4*>(a.part_o + (int64_t)place(std::min(i0 + k, count - 1)) * DV + d);
 #pragma unroll
       for (int k = 0; k < kAt; ++k) {
-        const float w = i0 + k < count ? sw[g][i0 + k] * inv : 0.f;
-        o.x = w == 0.f ? o.x : o.x + w * y[k].x;
-        o.y = w == 0.f ? o.y : o.y + w * y[k].y;
-        o.z = w == 0.f ? o.z : o.z + w * y[k].z;
-        o.w = w == 0.f ? o.w : o.w + w * y[k].w;
+        // (every piece that exists counts, also with a weight that rounds to zero: 0 x infinity has to show)
+        const bool is = i0 + k < count;
+        const float w = is ? sw[g][i0 + k] * inv : 0.f;
+        o.x = is ? o.x + w * y[k].x : o.x;
+        o.y = is ? o.y + w * y[k].y : o.y;
+        o.z = is ? o.z + w * y[k].z : o.z;
+        o.w = is ? o.w + w * y[k].w : o.w;
       }
     }
   }
