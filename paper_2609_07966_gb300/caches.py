@@ -98,8 +98,23 @@ def workspace(cfg, T_cap: int, device="cuda"):
     return torch.zeros(n, dtype=torch.uint8, device=device), n
 
 
+def _check(name, t, dtype, shape, device):
+    """ValueError unless t is a contiguous tensor of the type, of the shape (at least as many entries: its first
+    dimension) and on the device: the kernels get its address alone."""
+    want = f"{name} must be contiguous {dtype} of shape {list(shape)} (or more entries) on {device}"
+    if t.dtype != dtype or t.device != device or t.dim() != len(shape) or not t.is_contiguous() or \
+            t.shape[0] < shape[0] or tuple(t.shape[1:]) != tuple(shape[1:]):
+        raise ValueError(f"{want}, not {t.dtype} of shape {list(t.shape)}, strides {list(t.stride())} on {t.device}")
+
+
 def wrap_cache(cfg, T_len, k, v) -> Cache:
-    """An FP16 cache over tensors the caller already has: k, v [B][Hkv][T_cap][D], T_len int32 [B]."""
+    """An FP16 cache over tensors the caller already has: k, v fp16 [B][Hkv][T_cap][D], T_len int32 [B], all
+    contiguous and on one device; ValueError otherwise."""
+    import torch
+    shape = (cfg.B, cfg.Hkv, k.shape[2] if k.dim() == 4 else 0, cfg.D)
+    _check("k", k, torch.float16, shape, k.device)
+    _check("v", v, torch.float16, shape, k.device)
+    _check("T_len", T_len, torch.int32, (cfg.B,), k.device)
     c = mkv_cache()
     c.T_cap, c.T_len, c.k, c.v = k.shape[2], _ptr(T_len), _ptr(k), _ptr(v)
     return Cache(cfg, k.shape[2], {"T_len": T_len, "k": k, "v": v}, c)
@@ -127,7 +142,12 @@ def latent_dtype(cfg):
 
 
 def wrap_latent_cache(cfg, T_len, rows) -> LatentCache:
-    """A latent cache over tensors the caller already has: rows [B][T_cap][rank + rope_dim], T_len int32 [B]."""
+    """A latent cache over tensors the caller already has: rows [B][T_cap][rank + rope_dim] of the configuration's type,
+    T_len int32 [B], contiguous and on one device; ValueError otherwise."""
+    import torch
+    _check("rows", rows, latent_dtype(cfg), (cfg.B, rows.shape[1] if rows.dim() == 3 else 0, cfg.rank + cfg.rope_dim),
+           rows.device)
+    _check("T_len", T_len, torch.int32, (cfg.B,), rows.device)
     return LatentCache(cfg, rows.shape[1], {"T_len": T_len, "rows": rows},
                        mkv_latent_cache(rows.shape[1], _ptr(T_len), _ptr(rows)))
 
