@@ -483,7 +483,8 @@ mkv_status mkv_tree_workspace_size(const mkv_config* cfg, int64_t T_cap, int32_t
  * [B][n][Hq][D]; k_tree, v_tree fp16 [B][n][Hkv][D] (keys already rotated by
  * the tokens' positions); 1 <= n <= 64.  cfg->method must be MKV_FP16
  * (MKV_ERR_UNSUPPORTED otherwise).  q, k_tree, v_tree, out and the cache's k
- * and v must be 16-byte aligned and ws 256-byte aligned (MKV_ERR_INVALID_ARG);
+ * and v must be 16-byte aligned, ws 256-byte, mask 8-byte and T_len 4-byte
+ * aligned (MKV_ERR_INVALID_ARG; path, n_path and q_len of the calls below: 4);
  * T_cap < 2^31 - 256 (MKV_ERR_UNSUPPORTED).  The cache is only read.  A bounded
  * wait that ran out sets MKV_FLAG_WAIT_TIMEOUT. */
 mkv_status mkv_tree_attention(const mkv_config* cfg, const void* q, const mkv_cache* cache, const void* k_tree,
@@ -529,8 +530,9 @@ typedef struct {
   float softmax_scale;    /* 0 -> 1/sqrt(nope_dim + rope_dim)                */
 } mkv_latent_config;
 
-/* Device memory owned by the caller: T_len int32 [B] tokens held, rows
- * [B][T_cap][rank + rope_dim], 16-byte aligned; token t in slot t. */
+/* Device memory owned by the caller: T_len int32 [B] tokens held, 4-byte
+ * aligned; rows [B][T_cap][rank + rope_dim], 16-byte aligned; token t in slot
+ * t. */
 typedef struct {
   int64_t T_cap;
   int32_t* T_len;

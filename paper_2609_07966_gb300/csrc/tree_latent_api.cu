@@ -9,7 +9,8 @@ using namespace mkv;
 
 namespace {
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+inline bool aligned16(const void* p) { return aligned(p, 16); }
 
 // Slots are 32-bit coordinates of the copies, a tile past the end included.
 constexpr int64_t kMaxSlots = (int64_t)INT32_MAX - 256;
@@ -36,6 +37,12 @@ mkv_status check_latent_cache(const mkv_latent_cache* k) {
   MKV_REQUIRE(k->T_cap >= 1 && k->T_len && k->rows, MKV_ERR_INVALID_ARG, "cache T_cap/T_len/rows invalid");
   MKV_REQUIRE(k->T_cap < kMaxSlots, MKV_ERR_UNSUPPORTED, "T_cap %lld too large", (long long)k->T_cap);
   MKV_REQUIRE(aligned16(k->rows), MKV_ERR_INVALID_ARG, "cache rows must be 16-byte aligned");
+  MKV_REQUIRE(aligned(k->T_len, 4), MKV_ERR_INVALID_ARG, "T_len must be 4-byte aligned");
+  return MKV_OK;
+}
+
+mkv_status check_path(const int32_t* path, const int32_t* n_path) {
+  MKV_REQUIRE(aligned(path, 4) && aligned(n_path, 4), MKV_ERR_INVALID_ARG, "path and n_path must be 4-byte aligned");
   return MKV_OK;
 }
 
@@ -138,6 +145,8 @@ mkv_status mkv_tree_attention(const mkv_config* cfg, const void* q, const mkv_ca
   MKV_REQUIRE(aligned16(q) && aligned16(out) && aligned16(k_tree) && aligned16(v_tree) && aligned16(cache->k) &&
                   aligned16(cache->v),
               MKV_ERR_INVALID_ARG, "q, out, k_tree, v_tree and the cache must be 16-byte aligned");
+  MKV_REQUIRE(aligned(mask, 8), MKV_ERR_INVALID_ARG, "mask must be 8-byte aligned");
+  MKV_REQUIRE(aligned(cache->T_len, 4), MKV_ERR_INVALID_ARG, "T_len must be 4-byte aligned");
   RowsCall r = rows_of_tree(cfg, cache->T_cap, n);
   MKV_TRY(check_rows(r));
   MKV_TRY(check_ws(ws, ws_bytes, rows_ws_bytes(r)));
@@ -159,6 +168,8 @@ mkv_status mkv_tree_commit(const mkv_config* cfg, const void* k_tree, const void
   MKV_REQUIRE(n >= 1, MKV_ERR_INVALID_ARG, "n = %d must be positive", n);
   MKV_REQUIRE(aligned16(k_tree) && aligned16(v_tree) && aligned16(cache->k) && aligned16(cache->v),
               MKV_ERR_INVALID_ARG, "k_tree, v_tree and the cache must be 16-byte aligned");
+  MKV_REQUIRE(aligned(cache->T_len, 4), MKV_ERR_INVALID_ARG, "T_len must be 4-byte aligned");
+  MKV_TRY(check_path(path, n_path));
   CommitCall c{};
   c.B = cfg->B;
   c.n = n;
@@ -234,6 +245,7 @@ mkv_status mkv_latent_attention(const mkv_latent_config* cfg, const void* q_abs,
   MKV_REQUIRE(rows_tree == nullptr || mask != nullptr, MKV_ERR_INVALID_ARG, "rows_tree needs a mask");
   MKV_REQUIRE(aligned16(q_abs) && aligned16(o_lat) && aligned16(rows_tree), MKV_ERR_INVALID_ARG,
               "q_abs, o_lat and rows_tree must be 16-byte aligned");
+  MKV_REQUIRE(rows_tree == nullptr || aligned(mask, 8), MKV_ERR_INVALID_ARG, "mask must be 8-byte aligned");
   RowsCall r = rows_of_latent(cfg, cache->T_cap, n);
   MKV_TRY(check_rows(r));
   MKV_TRY(check_ws(ws, ws_bytes, rows_ws_bytes(r)));
@@ -257,6 +269,7 @@ mkv_status mkv_latent_prefill(const mkv_latent_config* cfg, const void* q, const
               (long long)T_max);
   MKV_REQUIRE(aligned16(q) && aligned16(kv) && aligned16(out), MKV_ERR_INVALID_ARG,
               "q, kv and out must be 16-byte aligned");
+  MKV_REQUIRE(aligned(q_len, 4), MKV_ERR_INVALID_ARG, "q_len must be 4-byte aligned");
   MKV_REQUIRE((int64_t)cfg->B * cfg->H <= 65535, MKV_ERR_UNSUPPORTED, "B * H above 65535");
   PrefillCall p{};
   p.dtype = cfg->dtype;
@@ -286,6 +299,7 @@ mkv_status mkv_latent_commit(const mkv_latent_config* cfg, const void* rows_new,
   MKV_TRY(check_latent_cache(cache));
   MKV_REQUIRE(rows_new && n >= 1, MKV_ERR_INVALID_ARG, "rows_new NULL or n < 1");
   MKV_REQUIRE(aligned16(rows_new), MKV_ERR_INVALID_ARG, "rows_new must be 16-byte aligned");
+  MKV_TRY(check_path(path, n_path));
   CommitCall c{};
   c.B = cfg->B;
   c.n = n;
