@@ -4,12 +4,13 @@
 
 #include "mkv_common.cuh"
 #include "mkv_internal.h"
+#include "mkv_rows.h"
 
 namespace mkv {
 
 namespace {
 
-__device__ uint32_t g_status_append;   // MKV_FLAG_* bits raised by this unit
+__device__ uint32_t g_status_append;   // MKV_FLAG_* bits raised by this unit and those that status_word serves
 
 struct AppendArgs {
   const uint4* k_new;   // [B][Hkv][D] fp16, as 16-byte chunks
@@ -122,6 +123,10 @@ cudaError_t launch_rope_table(int D, float theta, int64_t T_max, float* table, c
   const int blocks = (int)std::min<int64_t>(ceil_div(n, 256), 4 * kNumSMs * 8);
   rope_table_kernel<<<blocks, 256, 0, st>>>(D, (double)theta, T_max, reinterpret_cast<float2*>(table));
   return cudaPeekAtLastError();
+}
+
+cudaError_t status_word(uint32_t** word) {
+  return cudaGetSymbolAddress(reinterpret_cast<void**>(word), g_status_append);
 }
 
 cudaError_t take_status_append(uint32_t* flags, cudaStream_t st) {

@@ -15,8 +15,6 @@ namespace mkv {
 
 namespace {
 
-__device__ uint32_t g_status_commit;
-
 constexpr int kCommitThreads = 512;
 
 // Whether entry b's path fits (all threads of the CTA take part); its length and path length.
@@ -37,7 +35,7 @@ __device__ __forceinline__ void store_length(const CommitCall& a, int b, bool ok
   if (ok)
     a.T_len[b] = t;
   else
-    atomicOr(&g_status_commit, MKV_FLAG_CACHE_FULL);
+    atomicOr(a.status, MKV_FLAG_CACHE_FULL);
 }
 
 template <bool kCluster>
@@ -83,24 +81,17 @@ __global__ void __launch_bounds__(kCommitThreads) length_kernel(const CommitCall
 
 }  // namespace
 
-cudaError_t take_status_commit(uint32_t* flags, cudaStream_t st) {
-  uint32_t v = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbolAsync(&v, g_status_commit, sizeof(v), 0, cudaMemcpyDeviceToHost, st);
-  if (e == cudaSuccess) e = cudaMemcpyToSymbolAsync(g_status_commit, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, st);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  *flags |= v;
-  return e;
-}
-
-cudaError_t launch_commit(const CommitCall& c, cudaStream_t st) {
+cudaError_t launch_commit(const CommitCall& call, cudaStream_t st) {
+  CommitCall c = call;
+  cudaError_t e = status_word(&c.status);
+  if (e != cudaSuccess) return e;
   constexpr int kParts = 8;                             // the largest portable cluster
   // One launch up to 1 MiB an entry (measured: 16 rows of 4 KB x 8 entries 4.2 us; but 9.4 MB of one entry 86 us through
   // one cluster and 7.9 us in two launches, each with a copy of the length before it).
   const int64_t bytes = (int64_t)c.n * c.heads * c.row_bytes * (c.src1 != nullptr ? 2 : 1);
   if (bytes > (1 << 20)) {
     const int64_t want = ceil_div((int64_t)4 * kNumSMs, (int64_t)c.B), most = ceil_div(c.n, kCommitThreads / 32);
-    const cudaError_t e =
-        launch_pdl(commit_kernel<false>, dim3((unsigned)std::min(want, most), c.B), dim3(kCommitThreads), 0, st, c);
+    e = launch_pdl(commit_kernel<false>, dim3((unsigned)std::min(want, most), c.B), dim3(kCommitThreads), 0, st, c);
     return e != cudaSuccess ? e : launch_pdl(length_kernel, dim3(c.B), dim3(kCommitThreads), 0, st, c);
   }
   cudaLaunchAttribute attr[2];
@@ -114,7 +105,7 @@ cudaError_t launch_commit(const CommitCall& c, cudaStream_t st) {
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, commit_kernel<true>, c);
+  e = cudaLaunchKernelEx(&cfg, commit_kernel<true>, c);
   return e != cudaSuccess ? e : cudaPeekAtLastError();
 }
 

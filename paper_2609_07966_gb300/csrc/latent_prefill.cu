@@ -25,18 +25,6 @@
 
 namespace mkv {
 
-__device__ uint32_t g_status_latent_prefill;   // MKV_FLAG_* bits raised here
-
-cudaError_t take_status_latent_prefill(uint32_t* flags, cudaStream_t st) {
-  uint32_t v = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbolAsync(&v, g_status_latent_prefill, sizeof(v), 0, cudaMemcpyDeviceToHost, st);
-  if (e == cudaSuccess)
-    e = cudaMemcpyToSymbolAsync(g_status_latent_prefill, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, st);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  *flags |= v;
-  return e;
-}
-
 namespace {
 
 constexpr int kBR = 128;            // rows a block, keys a tile
@@ -55,6 +43,7 @@ struct PrefillArgs {
   uint16_t* out;
   int rank;
   int units, group;                 // (entry, head) pairs; how many of them are worked on together
+  uint32_t* status;                 // MKV_FLAG_* bits
 };
 
 template <bool BF16_, int DN_, int DV_>
@@ -159,7 +148,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
   tc_fence_after();
   const uint32_t tbase = ctl->tslot;
   volatile int* fail = &ctl->fail;
-  uint32_t* status = &g_status_latent_prefill;
+  uint32_t* status = a.status;
 
   if (warp >= 8) {
     regs_down<kPRegsOther>();
@@ -496,6 +485,8 @@ cudaError_t launch_t(const PrefillCall& c, const PrefillArgs& a, cudaStream_t st
 
 cudaError_t launch_latent_prefill(const PrefillCall& c, cudaStream_t st) {
   PrefillArgs a{};
+  const cudaError_t e = status_word(&a.status);
+  if (e != cudaSuccess) return e;
   a.n = c.n;
   a.H = c.H;
   a.T_max = c.T_max;

@@ -22,18 +22,6 @@
 
 namespace mkv {
 
-__device__ uint32_t g_status_product;   // MKV_FLAG_* bits raised here
-
-cudaError_t take_status_product(uint32_t* flags, cudaStream_t st) {
-  uint32_t v = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbolAsync(&v, g_status_product, sizeof(v), 0, cudaMemcpyDeviceToHost, st);
-  if (e == cudaSuccess)
-    e = cudaMemcpyToSymbolAsync(g_status_product, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, st);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  *flags |= v;
-  return e;
-}
-
 namespace {
 
 struct ProductArgs {
@@ -49,6 +37,7 @@ struct ProductArgs {
   const uint16_t* x;           // absorb: the queries, for their rotated part
   int x_row, rope_at;
   uint16_t* out;
+  uint32_t* status;            // MKV_FLAG_* bits
 };
 
 constexpr int kTok = 128;
@@ -124,7 +113,7 @@ __global__ void __launch_bounds__(kPrThreads, 1)
   tc_fence_after();
   const uint32_t tbase = ctl->tslot;
   volatile int* fail = &ctl->fail;
-  uint32_t* status = &g_status_product;
+  uint32_t* status = a.status;
 
   if (warp == 4) {
     if (elect_one()) {
@@ -315,7 +304,7 @@ __global__ void __launch_bounds__(kExThreads, 1)
   tc_fence_after();
   const uint32_t tbase = ctl->tslot;
   volatile int* fail = &ctl->fail;
-  uint32_t* status = &g_status_product;
+  uint32_t* status = a.status;
   Items it(a, first, last);
 
   if (warp == 8) {
@@ -482,6 +471,8 @@ cudaError_t launch_kind(const ProductCall& c, const ProductArgs& a, cudaStream_t
 template <bool BF16>
 cudaError_t launch_t(const ProductCall& c, cudaStream_t st) {
   ProductArgs a{};
+  const cudaError_t e = status_word(&a.status);
+  if (e != cudaSuccess) return e;
   a.B = c.B;
   a.H = c.H;
   a.T_len = c.T_len;

@@ -302,10 +302,6 @@ mkv_status mkv_get_status(void* stream, uint32_t* flags) {
   MKV_CUDA(take_status_decode(flags, as_stream(stream)));
   MKV_CUDA(take_status_prefill(flags, as_stream(stream)));
   MKV_CUDA(take_status_kvq_step(flags, as_stream(stream)));
-  MKV_CUDA(take_status_rows(flags, as_stream(stream)));
-  MKV_CUDA(take_status_latent_prefill(flags, as_stream(stream)));
-  MKV_CUDA(take_status_product(flags, as_stream(stream)));
-  MKV_CUDA(take_status_commit(flags, as_stream(stream)));
   if (*flags & MKV_FLAG_WAIT_TIMEOUT) {
     set_error("device status flags 0x%x (a bounded wait ran out)", *flags);
     return MKV_ERR_TIMEOUT;

@@ -85,13 +85,12 @@ struct CommitCall {
   const int32_t *path, *n_path;
   int64_t T_cap;
   int32_t* T_len;
+  uint32_t* status;                // MKV_FLAG_* bits (filled in by the launch)
 };
 cudaError_t launch_commit(const CommitCall& c, cudaStream_t st);
 
-// Status words of these units (as take_status_append).
-cudaError_t take_status_rows(uint32_t* flags, cudaStream_t st);
-cudaError_t take_status_latent_prefill(uint32_t* flags, cudaStream_t st);
-cudaError_t take_status_product(uint32_t* flags, cudaStream_t st);
-cudaError_t take_status_commit(uint32_t* flags, cudaStream_t st);
+// The word (on the current device) that these units' kernels raise MKV_FLAG_* bits in.  It is append.cu's, which
+// mkv_get_status reads anyway: a word of each unit would cost its callers a round trip each.
+cudaError_t status_word(uint32_t** word);
 
 }  // namespace mkv

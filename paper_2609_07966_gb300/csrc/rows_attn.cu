@@ -44,17 +44,6 @@
 
 namespace mkv {
 
-__device__ uint32_t g_status_rows;   // MKV_FLAG_* bits raised here
-
-cudaError_t take_status_rows(uint32_t* flags, cudaStream_t st) {
-  uint32_t v = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbolAsync(&v, g_status_rows, sizeof(v), 0, cudaMemcpyDeviceToHost, st);
-  if (e == cudaSuccess) e = cudaMemcpyToSymbolAsync(g_status_rows, &zero, sizeof(zero), 0, cudaMemcpyHostToDevice, st);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  *flags |= v;
-  return e;
-}
-
 namespace {
 
 constexpr float kRaise = 8.f;       // a score may pass the running maximum by this (log2) before it is raised
@@ -81,6 +70,7 @@ struct RowsArgs {
   float* part_o;                    // [CTAs][2][N][DV]: a run's pieces of units that other runs share
   float2* part_ml;                  // [CTAs][2][N]
   struct Joint* joint;              // [B][Hkv][row_blocks]
+  uint32_t* status;                 // MKV_FLAG_* bits
 };
 
 // KA / VA: 64-dim atoms of a key / value; SHARED: values are the keys' first atoms; KT keys a tile, N rows a
@@ -361,7 +351,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
   const uint32_t tbase = ctl->tslot;
   const uint32_t tO = tbase + 2 * N;
   volatile int* fail = &ctl->fail;
-  uint32_t* status = &g_status_rows;
+  uint32_t* status = a.status;
 
   if (warp >= kLoad) {
     regs_down<S::RO>();
@@ -1111,6 +1101,8 @@ bool rows_countable(const RowsCall& c) { return plan_rows(c).tiles <= INT32_MAX 
 cudaError_t launch_rows_attention(const RowsCall& c, void* ws, cudaStream_t st) {
   const Plan p = plan_rows(c);
   RowsArgs a{};
+  const cudaError_t e = status_word(&a.status);
+  if (e != cudaSuccess) return e;
   a.B = c.B;
   a.n = c.n;
   a.H = c.H;
