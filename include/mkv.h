@@ -229,12 +229,14 @@ mkv_status mkv_rope_table(int32_t D, float theta, int64_t T_max, float* table, v
 mkv_status mkv_get_status(void* stream, uint32_t* flags);
 
 /* Diagnostic of the device wait-timeout path (no counterpart in the paper):
- * launches one CTA whose bounded mbarrier wait, the routine the prefill
+ * launches a CTA whose bounded mbarrier wait, the routine the prefill
  * scoring's waits use, can never complete (nothing arrives on its barrier);
  * after about `ms` milliseconds (1..1000, else MKV_ERR_INVALID_ARG) it gives
  * up and sets MKV_FLAG_WAIT_TIMEOUT, so the next mkv_get_status returns
- * MKV_ERR_TIMEOUT with that bit, and the context stays usable.  Asynchronous
- * on `stream`; it reads and writes no caller memory. */
+ * MKV_ERR_TIMEOUT with that bit, and the context stays usable.  A second CTA
+ * does the same behind it with the routine of the tree and latent calls, with
+ * a copy and tensor-core products under way, and waits for those before it
+ * ends.  Asynchronous on `stream`; it reads and writes no caller memory. */
 mkv_status mkv_wait_timeout_selftest(int32_t ms, void* stream);
 
 /* Thread-local description of the last error (never NULL). */

@@ -76,9 +76,9 @@ static_assert(2 * kPRegsSoftmax + kPRegsOther <= 3 * 168, "register shares");
 constexpr int kFixWords = 16;       // flags of the keys of the tiles that some row sees only in part
 
 struct PCtl {
-  uint64_t qfull[2], kfull[kBars], kempty[kBars], vfull[kBars], vempty[kBars], sfull[2], pfull[2][2], pvdone[2];
+  uint64_t drained, qfull[2], kfull[kBars], kempty[kBars], vfull[kBars], vempty[kBars], sfull[2], pfull[2][2], pvdone[2];
   uint32_t tslot;
-  int fail, k_loaded, v_loaded, issued[2];
+  int fail, k_loads, v_loads;       // tiles whose keys or values were asked for (read after a failure)
   uint32_t nonfinite[kFixWords];    // keys (from the first partial tile) whose value holds a non-finite number
 };
 static_assert(sizeof(PCtl) <= 512, "control block");
@@ -127,9 +127,9 @@ __global__ void __launch_bounds__(kPThreads, 1)
   if (warp == 8) tc_alloc(&ctl->tslot, 512);
   if (threadIdx.x == 0) {
     for (int s = 0; s < kBars; ++s) {
-      tc_mbar_init(&ctl->kfull[s], 1);
+      tc_mbar_init(&ctl->kfull[s], S::KA);
       tc_mbar_init(&ctl->kempty[s], 1);
-      tc_mbar_init(&ctl->vfull[s], 1);
+      tc_mbar_init(&ctl->vfull[s], S::VA);
       tc_mbar_init(&ctl->vempty[s], 1);
     }
     for (int s = 0; s < 2; ++s) {
@@ -139,8 +139,9 @@ __global__ void __launch_bounds__(kPThreads, 1)
       tc_mbar_init(&ctl->pfull[s][1], 4);
       tc_mbar_init(&ctl->pvdone[s], 1);
     }
+    tc_mbar_init(&ctl->drained, 1);
     tc_fence_mbar_init();
-    ctl->fail = ctl->k_loaded = ctl->v_loaded = ctl->issued[0] = ctl->issued[1] = 0;
+    ctl->fail = ctl->k_loads = ctl->v_loads = 0;
     for (int w = 0; w < kFixWords; ++w) ctl->nonfinite[w] = 0;
   }
   tc_fence_before();
@@ -173,25 +174,31 @@ __global__ void __launch_bounds__(kPThreads, 1)
           uint64_t* bar = &ctl->kfull[t % kBars];
           for (int j = 0; j < S::KA; ++j) {
             uint8_t* dst;
-            if (!slot_for(t, j, dst)) return false;
-            if (j == 0) tc_mbar_expect_tx(bar, S::KA * S::ATOM);
+            if (!slot_for(t, j, dst)) {
+              if (j > 0) give_up(bar, S::KA - j);
+              return false;
+            }
+            tc_mbar_expect_tx(bar, S::ATOM);
             if (j < S::DN / 64)
               tma_load_4d(dst, &kvmap, j * 64, t * kBR, h, b, bar);
             else
               tma_load_4d(dst, &rmap, a.rank, t * kBR, b, 0, bar);
+            ctl->k_loads = t + 1;
           }
-          ctl->k_loaded = t + 1;
           return true;
         };
         auto load_v = [&](int t) {
           uint64_t* bar = &ctl->vfull[t % kBars];
           for (int j = 0; j < S::VA; ++j) {
             uint8_t* dst;
-            if (!slot_for(t, S::KA + j, dst)) return false;
-            if (j == 0) tc_mbar_expect_tx(bar, S::VA * S::ATOM);
+            if (!slot_for(t, S::KA + j, dst)) {
+              if (j > 0) give_up(bar, S::VA - j);
+              return false;
+            }
+            tc_mbar_expect_tx(bar, S::ATOM);
             tma_load_4d(dst, &kvmap, S::DN + j * 64, t * kBR, h, b, bar);
+            ctl->v_loads = t + 1;
           }
-          ctl->v_loaded = t + 1;
           return true;
         };
         load_q(0);
@@ -258,7 +265,6 @@ __global__ void __launch_bounds__(kPThreads, 1)
               if (!ok) break;
               values(k, t, 1);
               tc_commit(&ctl->pvdone[k]);
-              ctl->issued[k] = t + 1;
             }
             if (k == 1) tc_commit(&ctl->vempty[t % kBars]);
             if (k == 0 && t + 1 < ntiles) {
@@ -269,6 +275,7 @@ __global__ void __launch_bounds__(kPThreads, 1)
             if (k == 1 && t + 1 < ntiles) tc_commit(&ctl->kempty[(t + 1) % kBars]);
           }
         }
+        tc_commit(&ctl->drained);
       }
     }
   } else {
@@ -435,19 +442,19 @@ __global__ void __launch_bounds__(kPThreads, 1)
       }
     }
   }
-  // teardown: on a failure wait (bounded) for the copies and products already issued
+  // teardown: the products issued are complete; after a failure so are the copies (each wait bounded)
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && ctl->fail) {
-    tc_mbar_wait(&ctl->qfull[0], 0, kRoleWaitNs);
-    tc_mbar_wait(&ctl->qfull[1], 0, kRoleWaitNs);
-    // (a tile whose loads were only begun when a wait ran out: nothing says when those end but time)
-    for (int t = std::max(0, ctl->k_loaded - kBars + 1); t <= ctl->k_loaded; ++t)
-      tc_mbar_wait(&ctl->kfull[t % kBars], (uint32_t)((t / kBars) & 1), t < ctl->k_loaded ? kRoleWaitNs : 10000000ull);
-    for (int t = std::max(0, ctl->v_loaded - kBars + 1); t <= ctl->v_loaded; ++t)
-      tc_mbar_wait(&ctl->vfull[t % kBars], (uint32_t)((t / kBars) & 1), t < ctl->v_loaded ? kRoleWaitNs : 10000000ull);
-    for (int k = 0; k < 2; ++k)
-      if (ctl->issued[k] > 0) tc_mbar_wait(&ctl->pvdone[k], (uint32_t)((ctl->issued[k] - 1) & 1), kRoleWaitNs);
+  if (threadIdx.x == 0) {
+    tc_mbar_wait(&ctl->drained, 0, kRoleWaitNs);
+    if (ctl->fail) {
+      tc_mbar_wait(&ctl->qfull[0], 0, kRoleWaitNs);
+      tc_mbar_wait(&ctl->qfull[1], 0, kRoleWaitNs);
+      for (int t = std::max(0, ctl->k_loads - kBars); t < ctl->k_loads; ++t)
+        tc_mbar_wait(&ctl->kfull[t % kBars], (uint32_t)((t / kBars) & 1), kRoleWaitNs);
+      for (int t = std::max(0, ctl->v_loads - kBars); t < ctl->v_loads; ++t)
+        tc_mbar_wait(&ctl->vfull[t % kBars], (uint32_t)((t / kBars) & 1), kRoleWaitNs);
+    }
   }
   __syncthreads();
   tc_fence_after();

@@ -55,9 +55,9 @@ struct PrShape {
 };
 
 struct PrCtl {
-  uint64_t wfull, wempty, afull[kStagesA], aempty[kStagesA], tfull[2], tempty[2];
+  uint64_t wfull, wempty, afull[kStagesA], aempty[kStagesA], tfull[2], tempty[2], drained;
   uint32_t tslot;
-  int fail, loaded, weights, issued;
+  int fail, loaded, weights;   // token stages, weight tiles asked for (read after a failure)
 };
 static_assert(sizeof(PrCtl) <= 256, "control block");
 
@@ -104,8 +104,9 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       tc_mbar_init(&ctl->tfull[s], 1);
       tc_mbar_init(&ctl->tempty[s], 4);
     }
+    tc_mbar_init(&ctl->drained, 1);
     tc_fence_mbar_init();
-    ctl->fail = ctl->loaded = ctl->weights = ctl->issued = 0;
+    ctl->fail = ctl->loaded = ctl->weights = 0;
   }
   pdl_wait_and_trigger();
   tc_fence_before();
@@ -180,8 +181,9 @@ __global__ void __launch_bounds__(kPrThreads, 1)
         }
         if (!ok) break;
         tc_commit(&ctl->tfull[buf]);
-        ctl->issued = ++n;
+        ++n;
       }
+      tc_commit(&ctl->drained);
     }
   } else {
     // stores: thread = token of the block
@@ -220,15 +222,16 @@ __global__ void __launch_bounds__(kPrThreads, 1)
       ++n;
     }
   }
-  // teardown: on a failure wait (bounded) for the copies and products already issued
+  // teardown: the products issued are complete; after a failure so are the copies (each wait bounded)
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && ctl->fail) {
-    if (ctl->weights > 0) tc_mbar_wait(&ctl->wfull, (uint32_t)((ctl->weights - 1) & 1), kRoleWaitNs);
-    for (int c = std::max(0, ctl->loaded - kStagesA); c < ctl->loaded; ++c)
-      tc_mbar_wait(&ctl->afull[c % kStagesA], (uint32_t)((c / kStagesA) & 1), kRoleWaitNs);
-    if (ctl->issued > 0)
-      tc_mbar_wait(&ctl->tfull[(ctl->issued - 1) & 1], (uint32_t)(((ctl->issued - 1) / 2) & 1), kRoleWaitNs);
+  if (threadIdx.x == 0) {
+    tc_mbar_wait(&ctl->drained, 0, kRoleWaitNs);
+    if (ctl->fail) {
+      if (ctl->weights > 0) tc_mbar_wait(&ctl->wfull, (uint32_t)((ctl->weights - 1) & 1), kRoleWaitNs);
+      for (int c = std::max(0, ctl->loaded - kStagesA); c < ctl->loaded; ++c)
+        tc_mbar_wait(&ctl->afull[c % kStagesA], (uint32_t)((c / kStagesA) & 1), kRoleWaitNs);
+    }
   }
   __syncthreads();
   tc_fence_after();
@@ -240,9 +243,9 @@ constexpr int kExTok = 256, kExStages = 3, kExThreads = 320;   // eight warps of
 constexpr int kExAtomW = 128 * 128, kExAtomX = kExTok * 128;
 
 struct ExCtl {
-  uint64_t wfull, wempty, xfull[kExStages], xempty[kExStages], tfull[2], tempty[2];
+  uint64_t wfull, wempty, xfull[kExStages], xempty[kExStages], tfull[2], tempty[2], drained;
   uint32_t tslot;
-  int fail, loaded, weights, issued;
+  int fail, loaded, weights;   // token stages, weight tiles asked for (read after a failure)
 };
 static_assert(sizeof(ExCtl) <= 256, "control block");
 
@@ -295,8 +298,9 @@ __global__ void __launch_bounds__(kExThreads, 1)
       tc_mbar_init(&ctl->tfull[s], 1);
       tc_mbar_init(&ctl->tempty[s], 8);
     }
+    tc_mbar_init(&ctl->drained, 1);
     tc_fence_mbar_init();
-    ctl->fail = ctl->loaded = ctl->weights = ctl->issued = 0;
+    ctl->fail = ctl->loaded = ctl->weights = 0;
   }
   pdl_wait_and_trigger();
   tc_fence_before();
@@ -366,8 +370,9 @@ __global__ void __launch_bounds__(kExThreads, 1)
         }
         if (!ok) break;
         tc_commit(&ctl->tfull[buf]);
-        ctl->issued = ++n;
+        ++n;
       }
+      tc_commit(&ctl->drained);
     }
   } else {
     // stores: lane = dim (in the order of the weights' rows), half of the block's tokens; the lanes exchange values, so
@@ -405,15 +410,16 @@ __global__ void __launch_bounds__(kExThreads, 1)
       ++n;
     }
   }
-  // teardown: on a failure wait (bounded) for the copies and products already issued
+  // teardown: the products issued are complete; after a failure so are the copies (each wait bounded)
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0 && ctl->fail) {
-    if (ctl->weights > 0) tc_mbar_wait(&ctl->wfull, (uint32_t)((ctl->weights - 1) & 1), kRoleWaitNs);
-    for (int c = std::max(0, ctl->loaded - kExStages); c < ctl->loaded; ++c)
-      tc_mbar_wait(&ctl->xfull[c % kExStages], (uint32_t)((c / kExStages) & 1), kRoleWaitNs);
-    if (ctl->issued > 0)
-      tc_mbar_wait(&ctl->tfull[(ctl->issued - 1) & 1], (uint32_t)(((ctl->issued - 1) / 2) & 1), kRoleWaitNs);
+  if (threadIdx.x == 0) {
+    tc_mbar_wait(&ctl->drained, 0, kRoleWaitNs);
+    if (ctl->fail) {
+      if (ctl->weights > 0) tc_mbar_wait(&ctl->wfull, (uint32_t)((ctl->weights - 1) & 1), kRoleWaitNs);
+      for (int c = std::max(0, ctl->loaded - kExStages); c < ctl->loaded; ++c)
+        tc_mbar_wait(&ctl->xfull[c % kExStages], (uint32_t)((c / kExStages) & 1), kRoleWaitNs);
+    }
   }
   __syncthreads();
   tc_fence_after();

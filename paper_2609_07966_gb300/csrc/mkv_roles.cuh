@@ -11,9 +11,14 @@ namespace mkv {
 
 constexpr uint64_t kRoleWaitNs = 1000000000ull;   // a bounded wait gives up after 1 s
 
+// How a CTA ends, failed or not: the role that issues products commits them all to a barrier of their own as it leaves,
+// wherever it stopped, and nothing of the CTA's is given back before that phase ends; on a failure the copies under way
+// are waited for too, which end a phase each because the role that loads gives up the rest of a tile that it began.
+//
 // Bounded wait of one role: false when it ran out (the flag is raised and MKV_FLAG_WAIT_TIMEOUT set in
 // *status) or another role's did.
-__device__ __forceinline__ bool wait_or_fail(uint64_t* bar, uint32_t parity, volatile int* fail, uint32_t* status) {
+__device__ __forceinline__ bool wait_or_fail(uint64_t* bar, uint32_t parity, volatile int* fail, uint32_t* status,
+                                             uint64_t ns = kRoleWaitNs) {
   if (tc_mbar_try(bar, parity)) return true;
   const uint64_t t0 = globaltimer_ns();
   for (;;) {
@@ -21,11 +26,16 @@ __device__ __forceinline__ bool wait_or_fail(uint64_t* bar, uint32_t parity, vol
     for (int i = 0; i < 16; ++i)
       if (tc_mbar_try(bar, parity)) return true;
     if (*fail) return false;
-    if (globaltimer_ns() - t0 > kRoleWaitNs) break;
+    if (globaltimer_ns() - t0 > ns) break;
   }
   *fail = 1;
   atomicOr(status, MKV_FLAG_WAIT_TIMEOUT);
   return false;
+}
+
+// Arrives for the `left` pieces of a tile that will not be asked for: its phase ends with the copies that were.
+__device__ __forceinline__ void give_up(uint64_t* bar, int left) {
+  for (; left > 0; --left) tc_mbar_arrive(bar);
 }
 
 // One thread of a converged warp.  (Code behind this choice is known to run in a single thread, which matters for

@@ -93,4 +93,7 @@ cudaError_t launch_commit(const CommitCall& c, cudaStream_t st);
 // mkv_get_status reads anyway: a word of each unit would cost its callers a round trip each.
 cudaError_t status_word(uint32_t** word);
 
+// One CTA whose roles' waits run out after ms (mkv_roles.cu).
+cudaError_t launch_role_wait_selftest(int ms, cudaStream_t st);
+
 }  // namespace mkv

@@ -121,14 +121,14 @@ struct Shape {
 constexpr int kMaxCluster = 8;      // CTAs of a cluster: the largest portable size
 constexpr int kMaxSlotsRing = 12;
 struct RowsCtl {
-  uint64_t qfull, qempty, ofree, kfull[8], vfull[8], empty[kMaxSlotsRing], rempty[4], sfull[2], pfull[2], pvdone[2];
+  uint64_t qfull, qempty, ofree, drained, kfull[8], vfull[8], empty[kMaxSlotsRing], rempty[4], sfull[2], pfull[2], pvdone[2];
   uint64_t nonfinite;     // drafted tokens that hold a non-finite value
   uint32_t tslot;
   int runs, run_len, longer;  // (Runs)
   int run0, run1, base, b0, len0;   // this CTA's run of tiles; first tile of entry b0, which holds run0; its length
   int u0;                           // the unit of that entry that holds run0
   int fail;
-  int q_loads, loaded, scores, values;   // pieces' queries, tiles issued so far (read after a failure)
+  int q_loads, k_loads, v_loads;    // pieces' queries, tiles whose keys or values were asked for (read after a failure)
 };
 static_assert(sizeof(RowsCtl) <= 512, "control block");
 
@@ -271,6 +271,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       tc_mbar_init(&ctl->qfull, 1);
       tc_mbar_init(&ctl->qempty, 1);
       tc_mbar_init(&ctl->ofree, S::NG * 4);
+      tc_mbar_init(&ctl->drained, 1);
       for (int s = 0; s < S::AHEAD; ++s) {
         tc_mbar_init(&ctl->kfull[s], S::SHARED ? CH + 1 : 1);
         tc_mbar_init(&ctl->vfull[s], 1);
@@ -283,7 +284,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
         tc_mbar_init(&ctl->pvdone[s], 1);
       }
       tc_fence_mbar_init();
-      ctl->fail = ctl->q_loads = ctl->loaded = ctl->scores = ctl->values = 0;
+      ctl->fail = ctl->q_loads = ctl->k_loads = ctl->v_loads = 0;
     }
     pdl_wait_and_trigger();
     const int per = a.Hkv * a.in_run;
@@ -384,12 +385,14 @@ __global__ void __launch_bounds__(S::THREADS, 1)
               if (!ok) break;
               tc_mbar_expect_tx(&ctl->kfull[r], S::ATOM);
               tma_load_4d(sm + S::R_OFF + r * S::ATOM, km, S::VA * 64, key, p.b, 0, &ctl->kfull[r]);
+              ctl->k_loads = g + 1;
             }
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
               uint64_t* bar = S::SHARED || j == 0 ? &ctl->kfull[g % S::AHEAD] : &ctl->vfull[g % S::AHEAD];
               if (lap > 0 && !wait_or_fail(&ctl->empty[slot], (uint32_t)((lap - 1) & 1), fail, status)) {
                 ok = false;
+                if (S::SHARED) give_up(bar, CH - j);
                 break;
               }
               uint8_t* dst = sm + S::KV_OFF + slot * S::SLOT;
@@ -400,12 +403,12 @@ __global__ void __launch_bounds__(S::THREADS, 1)
                   tma_load_4d(dst + x * S::ATOM, km, (j * (S::MV / 64) + x) * 64, key, p.b, 0, bar);
                 else
                   tma_load_4d(dst + x * S::ATOM, j == 0 ? km : vm, x * 64, key, kvh, p.b, bar);
+              if (!S::SHARED) (j == 0 ? ctl->k_loads : ctl->v_loads) = g + 1;
               if (++slot == S::SLOTS) {
                 slot = 0;
                 ++lap;
               }
             }
-            if (ok) ctl->loaded = g + 1;
           }
         }
       }
@@ -473,7 +476,6 @@ __global__ void __launch_bounds__(S::THREADS, 1)
               }
               tc_commit(&ctl->pvdone[gv % S::NP]);
               vslot = s;
-              ctl->values = gv + 1;
               ++tv;
               idle = 0;
             }
@@ -504,7 +506,6 @@ __global__ void __launch_bounds__(S::THREADS, 1)
               }
               tc_commit(&ctl->sfull[gs & 1]);
               ++ts;
-              ctl->scores = gs + 1;
               if (ts == nt) tc_commit(&ctl->qempty);
               idle = 0;
             }
@@ -523,6 +524,7 @@ __global__ void __launch_bounds__(S::THREADS, 1)
           }
           g0 += nt;
         }
+        tc_commit(&ctl->drained);
       }
     }
   } else {
@@ -861,20 +863,16 @@ __global__ void __launch_bounds__(S::THREADS, 1)
       }
     }
   }
-  // teardown: on a failure wait (bounded) for the copies and products already issued
-  if (threadIdx.x == 0 && ctl->fail) {
-    if (ctl->q_loads > 0) tc_mbar_wait(&ctl->qfull, (uint32_t)((ctl->q_loads - 1) & 1), kRoleWaitNs);
-    // (a tile whose loads were only begun when its wait ran out: nothing says when those end but time)
-    for (int g = std::max(0, ctl->loaded - S::AHEAD); g <= ctl->loaded; ++g) {
-      tc_mbar_wait(&ctl->kfull[g % S::AHEAD], (uint32_t)((g / S::AHEAD) & 1),
-                   g < ctl->loaded ? kRoleWaitNs : 10000000ull);
-      if (!S::SHARED && g < ctl->loaded)
+  // teardown: the products issued are complete; after a failure so are the copies (each wait bounded)
+  if (threadIdx.x == 0) {
+    tc_mbar_wait(&ctl->drained, 0, kRoleWaitNs);
+    if (ctl->fail) {
+      if (ctl->q_loads > 0) tc_mbar_wait(&ctl->qfull, (uint32_t)((ctl->q_loads - 1) & 1), kRoleWaitNs);
+      for (int g = std::max(0, ctl->k_loads - S::AHEAD); g < ctl->k_loads; ++g)
+        tc_mbar_wait(&ctl->kfull[g % S::AHEAD], (uint32_t)((g / S::AHEAD) & 1), kRoleWaitNs);
+      for (int g = std::max(0, ctl->v_loads - S::AHEAD); g < ctl->v_loads; ++g)
         tc_mbar_wait(&ctl->vfull[g % S::AHEAD], (uint32_t)((g / S::AHEAD) & 1), kRoleWaitNs);
     }
-    if (ctl->scores > 0)
-      tc_mbar_wait(&ctl->sfull[(ctl->scores - 1) & 1], (uint32_t)(((ctl->scores - 1) >> 1) & 1), kRoleWaitNs);
-    if (ctl->values > 0)
-      tc_mbar_wait(&ctl->pvdone[(ctl->values - 1) % S::NP], (uint32_t)(((ctl->values - 1) / S::NP) & 1), kRoleWaitNs);
   }
   __syncthreads();
   tc_fence_after();
