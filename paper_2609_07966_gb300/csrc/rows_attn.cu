@@ -77,21 +77,22 @@ struct RowsArgs {
 // block, SLOTS ring slots, ROPE slots of the last key atom (SHARED), NP weight buffers.
 template <bool BF16_, int KA_, int VA_, bool SHARED_, int KT_, int N_, int SLOTS_, int ROPE_, int NP_>
 struct Shape {
+  static_assert(N_ == 16 || N_ == 32 || N_ == 64, "rows a block (plan_rows)");
   static constexpr bool BF16 = BF16_, SHARED = SHARED_;
   static constexpr int KA = KA_, VA = VA_, KT = KT_, N = N_, SLOTS = SLOTS_, ROPE = ROPE_, NP = NP_;
   static constexpr int DV = VA * 64;
   static constexpr int MV = DV >= 128 ? 128 : 64;          // value dims per product (its M)
   static constexpr int NB = DV / MV;                       // O^T blocks
-  static constexpr int NG = N > 64 ? 4 : 2;                // softmax groups of 128 threads
+  static constexpr int NG = 2;                             // softmax groups of 128 threads
   static constexpr int C = N / NG;                         // rows of a softmax group
   // A tile of 64 keys takes 16 tensor-memory lanes of each warp's quarter: the warp's halves then share its rows, so
   // that no lane idles.  L lanes hold one set of CS rows.
   static constexpr int L = KT == 64 ? 16 : 32, CS = C * L / 32;
   static constexpr int SOFT = NG * 128, THREADS = SOFT + 128;   // (two of the last four warps idle)
   // registers a thread: what a launch of THREADS gets, and its split between softmax and the others
-  static constexpr int RL = NG == 2 ? 168 : 96, RS = NG == 2 ? 208 : 104, RO = NG == 2 ? 88 : 64;
+  static constexpr int RL = 168, RS = 208, RO = 88;
   static_assert(NG * RS + RO <= (NG + 1) * RL, "register shares");
-  static constexpr int PW = N >= 64 ? 64 : N;              // row width of a weight tile (elements)
+  static constexpr int PW = N;                             // row width of a weight tile (elements)
   static constexpr int ATOM = KT * 128;                    // bytes of 64 dims of a tile
   static constexpr int QATOM = N * 128;
   // a tile's ring chunks: SHARED: its value blocks (MV dims each, the last key atom apart); else keys, values
