@@ -14,7 +14,9 @@
 //   takes it, because a 128 x 256 product reads 12 KB of operands in 128 cycles where a 128 x 128 one reads 8 KB in 64:
 //   the copies that refill shared memory need the difference.
 // Measured (GPU time): 8192 rows for 32 heads (rank 512, 128 + 128 dims) 61 us, 1.12 PFLOP/s, 0.57 of cuBLAS's rate; a
-// step's absorb for 8 tokens 4.3 us, project for 48 tokens 4.0 us.
+// step's absorb for 8 tokens 4.3 us, project for 48 tokens 4.0 us; for 8 tokens of 128 heads 8.1 us (one weight tile after
+// another) and 5.0 us.  Expand's runs are equal in T_max, not in the entries' lengths: one of 8192 rows beside three of 100
+// takes 132 us.
 #include <algorithm>
 
 #include "mkv_roles.cuh"

@@ -28,8 +28,9 @@
 // Bound by memory while a block's N rows need fewer tensor cycles a tile than its copy takes (64 keys of 576 dims: 3100
 // cycles at an SM's share of HBM against 1600 at N = 32, 2000 at N = 64), else by a tile's chain of scores, softmax and
 // second product.  Measured (GPU time): 16 drafted tokens over an 8 x 8K FP16 cache (32/8 heads, D 128) 48 us, 5.5
-// TB/s; one latent token over 8 x 8K rows (32 heads, rank 512) 26.5 us, 2.9 TB/s; 12 drafted over 4 x 32K ragged rows
-// 122 us, 0.73 PFLOP/s; one latent token over 777 rows 10.4 us.
+// TB/s; one latent token over 8 x 8K rows (rank 512) 26.6 us at 32 heads, 2.9 TB/s, and 40 us at 128; 12 drafted over 4
+// x 32K ragged rows 123 us, 0.73 PFLOP/s; one latent token over 777 rows 10.5 us where the cache's capacity is near the
+// length, 11.1 at 32K slots (the plan goes by the capacity).
 //
 // The running maximum m is only raised when some score of a tile passes it by 2^8 (weights then stay below
 // 2^14 with the offset below), which a group-wide vote finds: after the first tiles almost never, so the O^T
@@ -1003,8 +1004,11 @@ Plan plan_rows(const RowsCall& c) {
   // CTA's share is much longer than an equal one: joining through the workspace costs about four tiles' time (two of
   // the 64-row tiles, which take longer), and a seventh of a long run's where HBM is the bound.  Measured, clusters
   // against runs: 16 drafted tokens over 8 x 8K (64 units) 49 against 53 us, 8 over 3000 tokens (8 units) 10.1 against
-  // 13.5, one latent token over 8 x 1000 (8 units) 11.0 against 12.4; but 32 against 27 for one latent token over 8 x
-  // 8K, and 36.6 against 31.9 for 5 over 8 x 4K (24 units, ragged); 32 x 8K (32 units) 59 against 62.
+  // 13.5, one latent token over 8 x 1000 (8 units) 11.2 against 12.2, 8 x 4K 20.9 against 21.8; but 32 against 27 for one
+  // latent token over 8 x 8K, and 36.6 against 31.9 for 5 over 8 x 4K (24 units, ragged).  The rule is a rough one: on
+  // the side of the crossing that it takes for clusters', one latent token over 2000 tokens 12.9 against 11.2, over 32 x
+  // 16K 105.9 against 104.3 (32 x 8K 59.3 against 61.0); on the other, 16 drafted over 3 x 8K 27.1 against 29.9, 5 over
+  // 24 x 1000 (16 heads) 24.5 against 29.7 (24 x 4K 62 against 54).
   const int64_t units = (int64_t)c.B * c.Hkv * p.row_blocks, per_unit = ceil_div(c.T_cap, p.KT) + 1;
   const int64_t equal = ceil_div(per_unit * units, kNumSMs);
   const int64_t spare = (p.N <= 32 ? 4 : 2) + (p.row_blocks == 1 ? equal / 7 : 0);
@@ -1066,7 +1070,8 @@ cudaError_t launch_shape(const RowsCall& c, const Plan& p, RowsArgs a, cudaStrea
   if (e != cudaSuccess || p.cluster > 0) return e;
   const unsigned grid = (unsigned)ceil_div(B * Hkv * p.R, 512 / S::DV);
   // Four groups where a unit has more pieces (about) than one takes at a time and the CTAs fit beside each other (one
-  // latent token over 32000 rows 35.5 -> 25.6 us, over 8 x 8K 28.7 -> 26.8; but 16 x 4K, 512 CTAs, 26.8 -> 28.8).
+  // latent token over 32000 rows 35.5 -> 25.6 us, over 8 x 8K 28.7 -> 26.8, 16 x 4K of 16 heads, 256 CTAs, 24.5 -> 23.5;
+  // but of 32 heads, 512 CTAs, 26.8 -> 28.8, and with six pieces a unit, 16 drafted over 3 x 8K, 29.8 -> 31.1).
   if (p.ctas / (B * Hkv * p.row_blocks) >= 8 && grid <= 2 * kNumSMs)
     return launch_pdl(join_kernel<S::BF16, S::KT, S::DV, 4>, dim3(grid), dim3(4 * kJoinThreads), 0, st, a, (int)S::N);
   return launch_pdl(join_kernel<S::BF16, S::KT, S::DV, 1>, dim3(grid), dim3(kJoinThreads), 0, st, a, (int)S::N);
