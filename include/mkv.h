@@ -71,6 +71,9 @@ typedef enum { MKV_QUANT_UNIFORM = 0, MKV_QUANT_NUQ = 1 } mkv_quant_mode;
 #define MKV_FLAG_CACHE_FULL 0x2u          /* an append found no free slot; dropped */
 #define MKV_FLAG_WAIT_TIMEOUT 0x4u        /* a prefill-scoring CTA gave up waiting on the
                                              tensor core; that call's scores are invalid */
+#define MKV_FLAG_BAD_INDEX 0x8u           /* a page outside its pool, a position outside its table,
+                                             or an entry with more rows than max_rows */
+#define MKV_FLAG_NOT_FINITE 0x10u         /* an infinity or NaN was stored in 8 bits */
 
 /* One configuration (a row of Table 1, with its parameters).  Host POD. */
 typedef struct {
@@ -587,6 +590,153 @@ mkv_status mkv_latent_prefill(const mkv_latent_config* cfg, const void* q, const
  * (a prompt's, or a step's). */
 mkv_status mkv_latent_commit(const mkv_latent_config* cfg, const void* rows_new, const int32_t* path,
                              const int32_t* n_path, int32_t n, mkv_latent_cache* cache, void* stream);
+
+/* --------------------------------------------------------- rotary positions */
+
+/* Rotary positions of queries and keys: the first rot_dim dims of a head are
+ * rot_dim / 2 pairs (x, y), and at position p pair i becomes
+ *   (x c - y s, y c + x s),  (c, s) = magnitude (cos, sin)(p f_i),
+ * with f_i = theta^(-2i / rot_dim) radians a position, changed for contexts
+ * longer than those trained on by `scaling`.  mkv_rope_table is the table of
+ * the whole-head, half-layout, unscaled case; every path above takes queries
+ * and keys that are rotated already, and these calls rotate them.  Each
+ * product and the sum are rounded to fp32, the result once to the type. */
+typedef enum {
+  MKV_ROPE_HALF = 0,   /* pair i: dims i and i + rot_dim / 2 */
+  MKV_ROPE_PAIRS = 1   /* pair i: dims 2i and 2i + 1         */
+} mkv_rope_layout;
+
+typedef enum {
+  MKV_ROPE_PLAIN = 0,  /* f_i                                                  */
+  MKV_ROPE_LINEAR = 1, /* f_i / factor                                         */
+  MKV_ROPE_BANDS = 2,  /* t_i = context f_i / 2 pi turns within the context: f_i
+                          from `high` turns up, f_i / factor up to `low`, mixed
+                          in proportion to t_i between them                    */
+  MKV_ROPE_RAMP = 3    /* f_i up to the pair that makes `high` turns within the
+                          context, f_i / factor from the one that makes `low`,
+                          mixed in proportion to i between them (the bounds
+                          rounded outwards to whole pairs, and taken within
+                          0..rot_dim - 1)                                      */
+} mkv_rope_scaling;
+
+typedef struct {
+  uint32_t abi_version;   /* must equal MKV_ABI_VERSION                       */
+  int32_t D;              /* dims of a head: even, 2..256                     */
+  int32_t rot_dim;        /* its first rot_dim dims are rotated: even, 2..D   */
+  int32_t layout;         /* mkv_rope_layout                                  */
+  int32_t scaling;        /* mkv_rope_scaling                                 */
+  float theta;            /* > 1                                              */
+  float factor;           /* LINEAR, BANDS, RAMP: >= 1                        */
+  float low, high;        /* BANDS, RAMP: turns, 0 < low < high               */
+  int64_t context;        /* BANDS, RAMP: tokens trained on, >= 1             */
+  float magnitude;        /* 0 -> 1 (RAMP: 0.1 ln(factor) + 1)                */
+} mkv_rope_config;
+
+/* table fp32 [T_max][rot_dim/2][2]: (c, s) of positions 0..T_max-1, computed
+ * in fp64 on the device and rounded once. */
+mkv_status mkv_rope_scaled_table(const mkv_rope_config* cfg, int64_t T_max, float* table, void* stream);
+
+/* Rotates `heads` heads of n tokens: token i's are [heads][D] at x + i *
+ * x_stride (in elements; 0: heads * D), its position is pos[i], and the
+ * rotated heads (with their other dims as they are) go to out + i *
+ * out_stride.  dtype is an mkv_dtype, pos int32 [n], n >= 1.  transposed != 0
+ * applies the transpose instead, which takes the gradient of the output to
+ * that of the input.  out may be x itself (then with the same stride), but
+ * must not overlap it otherwise.  Pointers 2-byte aligned (pos 4, table 8);
+ * with 16-byte aligned rows and rot_dim a multiple of 16 it runs fastest.  A
+ * position outside the table is taken as the nearest one in it and sets
+ * MKV_FLAG_BAD_INDEX. */
+mkv_status mkv_rope_apply(const mkv_rope_config* cfg, int32_t dtype, const void* x, int64_t x_stride,
+                          const int32_t* pos, int64_t n, int32_t heads, const float* table, int64_t T_max,
+                          int32_t transposed, void* out, int64_t out_stride, void* stream);
+
+/* ------------------------------------------------------------ 8-bit pages */
+
+/* A paged cache held in 8 bits, with one scale for each page and key head:
+ * compression that needs no calibration, beside KVQuant's below 4 bits (Table
+ * 1).  Entry b's token t lies in row t % page_size of page
+ * page_table[b][t / page_size]; a key or value is its code times the page's
+ * scale for that head.  An entry's newest tokens, its rows, are flattened over
+ * the entries: entry b has rows start[b]..start[b+1]-1 of n (start int32
+ * [B + 1], ascending from 0 to at most n; NULL: n / B rows for every entry,
+ * and B must divide n).  What lies behind start[B] is neither read nor
+ * written. */
+typedef enum {
+  MKV_E4M3 = 0,   /* 8-bit floats, largest 448; the two NaN codes are never
+                     written and stand for +-480 where they are read        */
+  MKV_I8 = 1      /* two's complement, -127..127                             */
+} mkv_code_format;
+
+typedef struct {
+  uint32_t abi_version;   /* must equal MKV_ABI_VERSION                       */
+  int32_t dtype;          /* mkv_dtype of queries, new keys, values, outputs  */
+  int32_t format;         /* mkv_code_format                                  */
+  int32_t B, Hq, Hkv;     /* Hq a multiple of Hkv, at most 32 times it        */
+  int32_t D;              /* 64 or 128                                        */
+  int32_t page_size;      /* 16, 32, 64 or 128 tokens                         */
+  float softmax_scale;    /* 0 -> 1/sqrt(D)                                   */
+} mkv_paged_config;
+
+/* Device memory owned by the caller.  The pages of an entry differ from one
+ * another, and those that an append writes into belong to no other entry. */
+typedef struct {
+  int64_t num_pages;            /* pages in the pool                          */
+  int64_t max_pages;            /* pages an entry may hold                    */
+  const int32_t* page_table;    /* int32 [B][max_pages]                       */
+  int32_t* T_len;               /* int32 [B]: tokens held                     */
+  int32_t* tickets;             /* int32 [B]: zero-filled by the caller once;
+                                   every call leaves them zero                */
+  void* k;                      /* codes [num_pages][Hkv][page_size][D],      */
+  void* v;                      /*   16-byte aligned                          */
+  float* k_scale;               /* fp32 [num_pages][Hkv], positive and finite */
+  float* v_scale;
+} mkv_paged_cache;
+
+/* The rows of an append.  Row i's heads are contiguous at k + i * k_stride and
+ * so on (strides in elements; 0: the heads' dims), so that parts of a fused
+ * projection's rows can be taken as they are.  Pointers 16-byte aligned,
+ * strides multiples of 8. */
+typedef struct {
+  int64_t n;
+  const int32_t* start;         /* int32 [B + 1] or NULL                      */
+  const int32_t* pos;           /* int32 [n] or NULL: row i of entry b is at
+                                   position T_len[b] + i                      */
+  const void* q;                /* [n][Hq][D] or NULL: no queries             */
+  const void* k;                /* [n][Hkv][D]                                */
+  const void* v;
+  void* q_out;                  /* rotated queries; q itself if in place      */
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+} mkv_paged_rows;
+
+/* One launch that rotates the rows' queries and keys (rope, table and T_max as
+ * for mkv_rope_apply, rot_dim a multiple of 16; rope NULL: taken as they are),
+ * quantizes keys and values into the pages behind T_len[b], and adds the rows
+ * to T_len.  A page's scale is the least power of two (2^-100..2^120) with
+ * which its largest magnitude is at most 448 or 127 codes; a page that held
+ * tokens keeps its scale if the new ones fit it, else it takes the larger one
+ * and the codes that it held are rounded again.  Codes are rounded to nearest
+ * even.  An infinity is stored as the largest code and NaN as zero, which sets
+ * MKV_FLAG_NOT_FINITE.  An entry whose rows do not fit max_pages
+ * (MKV_FLAG_CACHE_FULL) or need a page outside the pool (MKV_FLAG_BAD_INDEX)
+ * gets no key or value and keeps its T_len; its queries are rotated. */
+mkv_status mkv_paged_append(const mkv_paged_config* cfg, const mkv_rope_config* rope, const float* table, int64_t T_max,
+                            const mkv_paged_rows* rows, mkv_paged_cache* cache, void* stream);
+
+/* Bytes of workspace mkv_paged_attention needs for n rows, at most max_rows of
+ * an entry (laid out as mkv_workspace_size describes).  Host only. */
+mkv_status mkv_paged_workspace_size(const mkv_paged_config* cfg, int64_t n, int64_t max_rows, size_t* bytes);
+
+/* Causal attention of the entries' newest rows, which the cache holds already:
+ * row i of entry b's m is at position T_len[b] - m + i and attends to the
+ * tokens up to its own; a row before position 0 gets zeros.  q [n][Hq][D] (row
+ * stride q_stride elements; 0: Hq * D), out likewise, 16-byte aligned, strides
+ * multiples of 8.  No entry has more than max_rows rows (1..n); one that does
+ * is left out and sets MKV_FLAG_BAD_INDEX.  Tokens of a page outside the pool
+ * are not seen (MKV_FLAG_BAD_INDEX).  The cache is only read.  ws must be
+ * 256-byte aligned. */
+mkv_status mkv_paged_attention(const mkv_paged_config* cfg, const void* q, int64_t q_stride, const int32_t* start,
+                               int64_t n, int64_t max_rows, const mkv_paged_cache* cache, void* out,
+                               int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -20,9 +20,14 @@ MKV_OK, MKV_ERR_INVALID_ARG, MKV_ERR_UNSUPPORTED, MKV_ERR_CUDA, MKV_ERR_CAPACITY
 MKV_FP16, MKV_KVQUANT, MKV_H2O, MKV_ROCKET = range(4)
 MKV_QUANT_UNIFORM, MKV_QUANT_NUQ = range(2)
 MKV_F16, MKV_BF16 = range(2)
+MKV_ROPE_HALF, MKV_ROPE_PAIRS = range(2)
+MKV_ROPE_PLAIN, MKV_ROPE_LINEAR, MKV_ROPE_BANDS, MKV_ROPE_RAMP = range(4)
+MKV_E4M3, MKV_I8 = range(2)
 MKV_FLAG_K_OUTLIER_OVERFLOW = 0x1
 MKV_FLAG_CACHE_FULL = 0x2
 MKV_FLAG_WAIT_TIMEOUT = 0x4
+MKV_FLAG_BAD_INDEX = 0x8
+MKV_FLAG_NOT_FINITE = 0x10
 
 _STATUS_NAMES = {0: "MKV_OK", 1: "MKV_ERR_INVALID_ARG", 2: "MKV_ERR_UNSUPPORTED", 3: "MKV_ERR_CUDA",
                  4: "MKV_ERR_CAPACITY", 5: "MKV_ERR_WORKSPACE", 6: "MKV_ERR_TIMEOUT"}
@@ -62,6 +67,32 @@ class mkv_latent_cache(ctypes.Structure):
     _fields_ = [("T_cap", ctypes.c_int64), ("T_len", ctypes.c_void_p), ("rows", ctypes.c_void_p)]
 
 
+class mkv_rope_config(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_uint32), ("D", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32), ("theta", ctypes.c_float),
+                ("factor", ctypes.c_float), ("low", ctypes.c_float), ("high", ctypes.c_float),
+                ("context", ctypes.c_int64), ("magnitude", ctypes.c_float)]
+
+
+class mkv_paged_config(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("format", ctypes.c_int32),
+                ("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+class mkv_paged_cache(ctypes.Structure):
+    _fields_ = [("num_pages", ctypes.c_int64), ("max_pages", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+                ("T_len", ctypes.c_void_p), ("tickets", ctypes.c_void_p), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class mkv_paged_rows(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("start", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("q", ctypes.c_void_p),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_out", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("q_out_stride", ctypes.c_int64)]
+
+
 class mkv_quant_params(ctypes.Structure):
     _fields_ = [("t_lo", ctypes.c_void_p), ("t_hi", ctypes.c_void_p), ("k_lo", ctypes.c_void_p),
                 ("k_scale", ctypes.c_void_p), ("k_cb", ctypes.c_void_p), ("v_cb", ctypes.c_void_p),
@@ -84,6 +115,10 @@ _CACHE = ctypes.POINTER(mkv_cache)
 _QP = ctypes.POINTER(mkv_quant_params)
 _LCFG = ctypes.POINTER(mkv_latent_config)
 _LCACHE = ctypes.POINTER(mkv_latent_cache)
+_ROPE = ctypes.POINTER(mkv_rope_config)
+_PCFG = ctypes.POINTER(mkv_paged_config)
+_PCACHE = ctypes.POINTER(mkv_paged_cache)
+_I32, _I64 = ctypes.c_int32, ctypes.c_int64
 _SIZE = ctypes.POINTER(ctypes.c_size_t)
 _SIGS = {
     "mkv_workspace_size": [_CFG, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)],
@@ -117,6 +152,11 @@ _SIGS = {
     "mkv_latent_expand": [_LCFG, _LCACHE, _P, ctypes.c_int64, _P, _P],
     "mkv_latent_prefill": [_LCFG, _P, _P, ctypes.c_int64, _LCACHE, _P, ctypes.c_int32, _P, _P],
     "mkv_latent_commit": [_LCFG, _P, _P, _P, ctypes.c_int32, _LCACHE, _P],
+    "mkv_rope_scaled_table": [_ROPE, _I64, _P, _P],
+    "mkv_rope_apply": [_ROPE, _I32, _P, _I64, _P, _I64, _I32, _P, _I64, _I32, _P, _I64, _P],
+    "mkv_paged_append": [_PCFG, _ROPE, _P, _I64, ctypes.POINTER(mkv_paged_rows), _PCACHE, _P],
+    "mkv_paged_workspace_size": [_PCFG, _I64, _I64, _SIZE],
+    "mkv_paged_attention": [_PCFG, _P, _I64, _P, _I64, _I64, _PCACHE, _P, _I64, _P, ctypes.c_size_t, _P],
 }
 
 
@@ -343,6 +383,55 @@ def mkv_latent_prefill(cfg, q: int, kv: int, T_max: int, cache: mkv_latent_cache
 def mkv_latent_commit(cfg, rows_new: int, path, n_path, n: int, cache: mkv_latent_cache, stream=None):
     _call("mkv_latent_commit", ctypes.byref(cfg), rows_new, path or None, n_path or None, n, ctypes.byref(cache),
           _stream(stream))
+
+
+def rope_config(D: int, rot_dim: int | None = None, layout: int = MKV_ROPE_HALF, scaling: int = MKV_ROPE_PLAIN,
+                theta: float = 10000.0, factor: float = 1.0, low: float = 1.0, high: float = 4.0, context: int = 0,
+                magnitude: float = 0.0) -> mkv_rope_config:
+    """An mkv_rope_config with the ABI version set (rot_dim: the whole head unless given); fields as in mkv.h."""
+    return mkv_rope_config(MKV_ABI_VERSION, D, D if rot_dim is None else rot_dim, layout, scaling, theta, factor, low,
+                           high, context, magnitude)
+
+
+def mkv_rope_scaled_table(cfg: mkv_rope_config, T_max: int, table: int, stream=None):
+    _call("mkv_rope_scaled_table", ctypes.byref(cfg), T_max, table, _stream(stream))
+
+
+def mkv_rope_apply(cfg: mkv_rope_config, dtype: int, x: int, x_stride: int, pos: int, n: int, heads: int, table: int,
+                   T_max: int, transposed, out: int, out_stride: int, stream=None):
+    _call("mkv_rope_apply", ctypes.byref(cfg), dtype, x, x_stride, pos, n, heads, table, T_max, int(transposed), out,
+          out_stride, _stream(stream))
+
+
+def paged_config(dtype: int, format: int, B: int, Hq: int, Hkv: int, D: int, page_size: int,
+                 softmax_scale: float = 0.0) -> mkv_paged_config:
+    """An mkv_paged_config with the ABI version set; fields as in mkv.h."""
+    return mkv_paged_config(MKV_ABI_VERSION, dtype, format, B, Hq, Hkv, D, page_size, softmax_scale)
+
+
+def paged_rows(n: int, start=None, pos=None, q=None, k=None, v=None, q_out=None, q_stride: int = 0, k_stride: int = 0,
+               v_stride: int = 0, q_out_stride: int = 0) -> mkv_paged_rows:
+    """An mkv_paged_rows; fields as in mkv.h."""
+    return mkv_paged_rows(n, start or None, pos or None, q or None, k or None, v or None, q_out or None, q_stride,
+                          k_stride, v_stride, q_out_stride)
+
+
+def mkv_paged_append(cfg: mkv_paged_config, rope, table, T_max: int, rows: mkv_paged_rows, cache: mkv_paged_cache,
+                     stream=None):
+    _call("mkv_paged_append", ctypes.byref(cfg), ctypes.byref(rope) if rope is not None else None, table or None, T_max,
+          ctypes.byref(rows), ctypes.byref(cache), _stream(stream))
+
+
+def mkv_paged_workspace_size(cfg: mkv_paged_config, n: int, max_rows: int) -> int:
+    b = ctypes.c_size_t(0)
+    _call("mkv_paged_workspace_size", ctypes.byref(cfg), n, max_rows, ctypes.byref(b))
+    return b.value
+
+
+def mkv_paged_attention(cfg: mkv_paged_config, q: int, q_stride: int, start, n: int, max_rows: int,
+                        cache: mkv_paged_cache, out: int, out_stride: int, ws: int, ws_bytes: int, stream=None):
+    _call("mkv_paged_attention", ctypes.byref(cfg), q, q_stride, start or None, n, max_rows, ctypes.byref(cache), out,
+          out_stride, ws, ws_bytes, _stream(stream))
 
 
 def n_value_outliers(D: int, frac: float) -> int:

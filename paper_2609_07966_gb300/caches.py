@@ -7,9 +7,9 @@ from __future__ import annotations
 
 import dataclasses
 
-from . import (MKV_BF16, MKV_FP16, MKV_H2O, MKV_KVQUANT, MKV_ROCKET, mkv_cache, mkv_latent_cache,
-               mkv_latent_workspace_size, mkv_quant_params, mkv_tree_workspace_size, mkv_workspace_size,
-               n_value_outliers)
+from . import (MKV_BF16, MKV_E4M3, MKV_FP16, MKV_H2O, MKV_KVQUANT, MKV_ROCKET, mkv_cache, mkv_latent_cache,
+               mkv_latent_workspace_size, mkv_paged_cache, mkv_paged_workspace_size, mkv_quant_params,
+               mkv_rope_scaled_table, mkv_tree_workspace_size, mkv_workspace_size, n_value_outliers)
 
 
 @dataclasses.dataclass
@@ -164,4 +164,64 @@ def latent_workspace(cfg, T_cap: int, n: int, device="cuda"):
     """(tensor, nbytes) of the workspace of mkv_latent_attention for n tokens per entry, zero-filled."""
     import torch
     b = mkv_latent_workspace_size(cfg, T_cap, n)
+    return torch.zeros(b, dtype=torch.uint8, device=device), b
+
+
+def rope_table(cfg, T_max: int, device="cuda", stream=None):
+    """fp32 [T_max][rot_dim / 2][2]: the table of mkv_rope_scaled_table, filled on the device's current stream."""
+    import torch
+    t = torch.empty((T_max, cfg.rot_dim // 2, 2), dtype=torch.float32, device=device)
+    with torch.cuda.device(t.device):
+        mkv_rope_scaled_table(cfg, T_max, _ptr(t), stream)
+    return t
+
+
+@dataclasses.dataclass
+class PagedCache:
+    """One layer's 8-bit pages: torch tensors plus the mkv_paged_cache struct over them."""
+    cfg: object
+    t: dict
+    c: mkv_paged_cache
+
+
+def code_dtype(cfg):
+    import torch
+    return torch.float8_e4m3fn if cfg.format == MKV_E4M3 else torch.int8
+
+
+def wrap_paged_cache(cfg, page_table, T_len, k, v, k_scale, v_scale, tickets=None) -> PagedCache:
+    """A paged cache over tensors the caller already has: k, v [num_pages][Hkv][page_size][D] of code_dtype(cfg), k_scale,
+    v_scale fp32 [num_pages][Hkv], page_table int32 [B][max_pages], T_len int32 [B], all contiguous and on one device;
+    ValueError otherwise.  tickets int32 [B] zeros (allocated unless given)."""
+    import torch
+    num = k.shape[0] if k.dim() == 4 else 0
+    shape = (num, cfg.Hkv, cfg.page_size, cfg.D)
+    _check("k", k, code_dtype(cfg), shape, k.device)
+    _check("v", v, code_dtype(cfg), shape, k.device)
+    _check("k_scale", k_scale, torch.float32, (num, cfg.Hkv), k.device)
+    _check("v_scale", v_scale, torch.float32, (num, cfg.Hkv), k.device)
+    _check("page_table", page_table, torch.int32, (cfg.B, page_table.shape[1] if page_table.dim() == 2 else 0), k.device)
+    _check("T_len", T_len, torch.int32, (cfg.B,), k.device)
+    if tickets is None:
+        tickets = torch.zeros(cfg.B, dtype=torch.int32, device=k.device)
+    _check("tickets", tickets, torch.int32, (cfg.B,), k.device)
+    t = {"page_table": page_table, "T_len": T_len, "tickets": tickets, "k": k, "v": v, "k_scale": k_scale,
+         "v_scale": v_scale}
+    return PagedCache(cfg, t, mkv_paged_cache(num, page_table.shape[1], **{x: _ptr(y) for x, y in t.items()}))
+
+
+def alloc_paged_cache(cfg, num_pages: int, max_pages: int, device="cuda") -> PagedCache:
+    """Zeroed pool of num_pages pages, empty entries, and a page table that names no page (-1) yet."""
+    import torch
+    shape = (num_pages, cfg.Hkv, cfg.page_size, cfg.D)
+    k, v = (torch.zeros(shape, dtype=torch.int8, device=device).view(code_dtype(cfg)) for _ in range(2))
+    ks, vs = (torch.ones(shape[:2], dtype=torch.float32, device=device) for _ in range(2))
+    return wrap_paged_cache(cfg, torch.full((cfg.B, max_pages), -1, dtype=torch.int32, device=device),
+                            torch.zeros(cfg.B, dtype=torch.int32, device=device), k, v, ks, vs)
+
+
+def paged_workspace(cfg, n: int, max_rows: int, device="cuda"):
+    """(tensor, nbytes) of the workspace of mkv_paged_attention for n rows, at most max_rows an entry, zero-filled."""
+    import torch
+    b = mkv_paged_workspace_size(cfg, n, max_rows)
     return torch.zeros(b, dtype=torch.uint8, device=device), b

@@ -40,6 +40,19 @@ cudaError_t encode_map(CUtensorMap* m, const void* base, const int64_t (&dims)[4
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+cudaError_t encode_code_map(CUtensorMap* m, const void* base, int width, int64_t rows, int64_t heads, int box_rows) {
+  const EncodeTiled enc = encoder();
+  if (enc == nullptr) return cudaErrorNotSupported;
+  const cuuint64_t d[4] = {(cuuint64_t)width, (cuuint64_t)rows, (cuuint64_t)heads, 1};
+  const cuuint64_t s[3] = {(cuuint64_t)width, (cuuint64_t)(rows * width), (cuuint64_t)(heads * rows * width)};
+  const cuuint32_t box[4] = {(cuuint32_t)width, (cuuint32_t)box_rows, 1, 1}, es[4] = {1, 1, 1, 1};
+  const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), d, s, box, es,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 namespace {
 
 // The roles of a CTA that fails: one has asked for half of a tile, one has products under way, and both wait for what

@@ -373,5 +373,7 @@ __device__ __forceinline__ void reduce_columns(float (&v)[C], int lane, Op op) {
 // 64 x box1 x box2 x box3 with the 128-byte swizzle; what lies outside reads as zero.
 cudaError_t encode_map(CUtensorMap* m, const void* base, const int64_t (&dims)[4], const int64_t (&strides)[3],
                        int box1, int box2, int box3 = 1);
+// A map of bytes [heads][rows][width], width 64 or 128: boxes of width x box_rows of one head, the swizzle of that width.
+cudaError_t encode_code_map(CUtensorMap* m, const void* base, int width, int64_t rows, int64_t heads, int box_rows);
 
 }  // namespace mkv

@@ -1,0 +1,362 @@
+// New tokens join an 8-bit paged cache, and their queries and keys are rotated on the way, in one launch:
+//   e = least integer with max |x| <= top 2^e over a page's tokens of one head,  code = round(x 2^-e)
+// (x a rotated key or a value, top 448 or 127).  A page that holds tokens already keeps its scale if the new ones fit it;
+// else the codes that it holds are rounded again to the larger scale.
+//
+// Bound by memory: every row is read once, queries are written in 16 bits and keys and values in 8.  A slot is one page of
+// one entry that the call writes into, with the rows that fall into it; its keys and values are units of one head each.
+// A unit's values stay in registers, in fp32, between its maximum and its codes, so that rows are read and rotated once:
+//   warps   a unit a warp, eight units a CTA: decode steps, and pages of 16 tokens (128 work columns);
+//   blocks  a unit a CTA of 256 threads: larger pages filled by prompts.
+// Other CTAs of the slot rotate its rows' queries, a thread the same dims of several heads.
+//
+// Every CTA reads its entry's length, and the last one to have read it (a ticket an entry) stores the new one.
+#include <algorithm>
+
+#include "mkv_paged.cuh"
+
+namespace mkv {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kKeep = 4;            // columns of 16 dims that a thread holds
+constexpr int kExpMin = -100, kExpMax = 120;
+
+struct AppendArgs {
+  PagedAppendCall c;
+  uint32_t* status;
+  int cap;                          // start null: slots of an entry
+  int kv_ctas, q_ctas, q_heads;     // CTAs of a slot; heads of a query CTA
+};
+
+// Slots lie entry after entry: entry b's from slot_base(b) on, enough of them for m rows that begin anywhere in a page.
+__device__ __forceinline__ int64_t slot_base(const AppendArgs& a, int b) {
+  const int64_t r0 = min(max((int64_t)a.c.s.start[b], (int64_t)0), a.c.s.n);
+  return (r0 + (int64_t)b * (2 * a.c.s.page - 2)) / a.c.s.page;
+}
+// The entry of a slot: the last one whose slots begin at or before it (32 entries looked up at a time).
+__device__ __forceinline__ int slot_entry(const AppendArgs& a, int64_t slot, int lane) {
+  int lo = 0, count = a.c.s.B;
+  for (;;) {
+    const int step = (count + 31) / 32, at = lane * step;
+    const unsigned upto = __ballot_sync(0xffffffffu, at < count && slot_base(a, lo + at) <= slot);
+    const int last = max(0, __popc(upto) - 1);
+    lo += last * step;
+    if (step == 1) return lo;
+    count = min(step, count - last * step);
+  }
+}
+
+template <int FMT>
+__device__ __forceinline__ constexpr float top_code() { return FMT == MKV_E4M3 ? 448.f : 127.f; }
+
+// 2^e with e the least integer such that `most` <= top 2^e (its bits; finite and not negative).
+template <int FMT>
+__device__ __forceinline__ float least_scale(uint32_t most) {
+  // most = m 2^x, 1/2 <= m < 1; top = 0.875 2^9 or (127/128) 2^7
+  const int x = (int)(most >> 23) - 126;
+  const uint32_t mant = most & 0x7fffffu;
+  const bool over = FMT == MKV_E4M3 ? mant > 0x600000u : mant > 0x7e0000u;
+  const int e = x - (FMT == MKV_E4M3 ? 9 : 7) + (over ? 1 : 0);
+  return __uint_as_float((uint32_t)(127 + min(max(e, kExpMin), kExpMax)) << 23);
+}
+
+// x / scale rounded to codes (x finite or infinite).  A power of two's reciprocal is exact.
+struct Divide {
+  float scale, inv;
+  __device__ __forceinline__ explicit Divide(float s) : scale(s), inv(0.f) {
+    const uint32_t u = __float_as_uint(s), e = u >> 23;
+    if ((u & 0x7fffffu) == 0 && e >= 1 && e <= 253) inv = __uint_as_float((254u - e) << 23);
+  }
+  __device__ __forceinline__ float operator()(float x) const { return inv != 0.f ? x * inv : __fdiv_rn(x, scale); }
+};
+// Eight codes (rounded to nearest even, the largest ones beyond the range).
+template <int FMT>
+__device__ __forceinline__ uint2 encode8(const float* x) {
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (FMT == MKV_E4M3) {
+      uint16_t lo, hi;
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x[4 * i + 1]), "f"(x[4 * i]));
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x[4 * i + 3]), "f"(x[4 * i + 2]));
+      w[i] = (uint32_t)lo | (uint32_t)hi << 16;
+    } else {
+      w[i] = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        w[i] |= ((uint32_t)min(max(__float2int_rn(x[4 * i + k]), -127), 127) & 0xffu) << (8 * k);
+    }
+  }
+  return make_uint2(w[0], w[1]);
+}
+// Four codes as their values.
+template <int FMT>
+__device__ __forceinline__ void decode4(uint32_t w, float* x) {
+  uint32_t even, odd;
+  widen_codes<FMT>(w, even, odd);
+  const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&even));
+  const float2 o = __half22float2(*reinterpret_cast<const __half2*>(&odd));
+  constexpr float up = FMT == MKV_E4M3 ? kE4m3Up : 1.f;
+  x[0] = e.x * up;
+  x[1] = o.x * up;
+  x[2] = e.y * up;
+  x[3] = o.y * up;
+}
+
+// The rows of a slot: rows row0 .. row0 + count - 1 of the call, tokens at .. of page `pid`, which holds `held` tokens.
+struct Slot {
+  int64_t row0, token0;
+  int count, at, held;
+  int64_t pid;
+};
+
+// One column of 16 dims of a unit's row: its two runs of eight dims, rotated.
+template <int D, bool BF16>
+__device__ __forceinline__ void load_column(const AppendArgs& a, const Slot& s, bool key, int h, int e, float (&x)[16], int& lo,
+                                            int& hi) {
+  constexpr int kCols = D / 16;
+  const int i = e / kCols, col = e % kCols;
+  const int64_t row = s.row0 + i;
+  const bool turn = key && col < a.c.rope.rot / 16;
+  lo = turn ? turn_lo(col, a.c.rope.pairs) : 16 * col;
+  hi = turn ? turn_hi(col, a.c.rope.rot, a.c.rope.pairs) : 16 * col + 8;
+  const uint16_t* p = (key ? a.c.k_new + row * a.c.k_stride : a.c.v_new + row * a.c.v_stride) + h * D;
+  const uint4 p0 = *reinterpret_cast<const uint4*>(p + lo), p1 = *reinterpret_cast<const uint4*>(p + hi);
+  Turn8 t;
+  if (turn) t.load(turn_row(a.c.rope, a.c.pos != nullptr ? a.c.pos[row] : s.token0 + i, a.status), 8 * col);
+  widen8<BF16>(p0, x);
+  widen8<BF16>(p1, x + 8);
+  if (turn) rotate16(x, t, a.c.rope.pairs, 1.f);
+}
+
+template <int FMT, int D>
+__device__ __forceinline__ void store_column(uint8_t* page, const Slot& s, int e, float (&x)[16], int lo, int hi,
+                                             const Divide& div) {
+  constexpr int kCols = D / 16;
+  uint8_t* row = page + (int64_t)(s.at + e / kCols) * D;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = x[i] == x[i] ? div(x[i]) : 0.f;
+  *reinterpret_cast<uint2*>(row + lo) = encode8<FMT>(x);
+  *reinterpret_cast<uint2*>(row + hi) = encode8<FMT>(x + 8);
+}
+
+// GROUP threads (a warp or the CTA) quantize one head's keys or values of a slot.
+template <int FMT, int D, bool BF16, int GROUP>
+__device__ __forceinline__ void quantize_unit(const AppendArgs& a, const Slot& s, bool key, int h) {
+  constexpr int kCols = D / 16;
+  const int tid = threadIdx.x % GROUP, items = s.count * kCols;
+  const int64_t head = s.pid * a.c.s.Hkv + h;
+  float* scale = (key ? a.c.k_scale : a.c.v_scale) + head;
+  uint8_t* page = (key ? a.c.k : a.c.v) + head * a.c.s.page * D;
+  const float was = s.held > 0 ? *scale : 0.f;
+  float x[kKeep][16];
+  int lo[kKeep], hi[kKeep];
+  uint32_t most = 0;
+  bool bad = false;
+  auto measure = [&](const float(&y)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t u = __float_as_uint(y[i]) & 0x7fffffffu;
+      const bool no = u >= 0x7f800000u;
+      bad |= no;
+      most = max(most, no ? 0u : u);
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < kKeep; ++k)
+    if (tid + k * GROUP < items) {
+      load_column<D, BF16>(a, s, key, h, tid + k * GROUP, x[k], lo[k], hi[k]);
+      measure(x[k]);
+    }
+  // (warps: more than 16 tokens of an entry that the others do not have; they are read again below)
+  if (GROUP == 32)
+    for (int e = tid + kKeep * GROUP; e < items; e += GROUP) {
+      float y[16];
+      int l, g;
+      load_column<D, BF16>(a, s, key, h, e, y, l, g);
+      measure(y);
+    }
+  if (bad) atomicOr(a.status, MKV_FLAG_NOT_FINITE);
+  most = __reduce_max_sync(0xffffffffu, most);
+  if constexpr (GROUP > 32) {
+    __shared__ uint32_t of_warp[GROUP / 32];
+    if ((tid & 31) == 0) of_warp[tid >> 5] = most;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < GROUP / 32; ++w) most = max(most, of_warp[w]);
+  }
+  const bool fits = s.held > 0 && __uint_as_float(most) <= top_code<FMT>() * was;
+  const float now = fits ? was : least_scale<FMT>(most);
+  if (!fits) {
+    if (tid == 0) *scale = now;
+    if (s.held > 0) {
+      const float less = __fdiv_rn(was, now);
+      for (int e = tid; e < s.held * kCols; e += GROUP) {
+        uint4* p = reinterpret_cast<uint4*>(page) + e;
+        const uint4 old = *p;
+        float y[16];
+        decode4<FMT>(old.x, y);
+        decode4<FMT>(old.y, y + 4);
+        decode4<FMT>(old.z, y + 8);
+        decode4<FMT>(old.w, y + 12);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] *= less;
+        const uint2 n0 = encode8<FMT>(y), n1 = encode8<FMT>(y + 8);
+        *p = make_uint4(n0.x, n0.y, n1.x, n1.y);
+      }
+    }
+  }
+  const Divide div(now);
+#pragma unroll
+  for (int k = 0; k < kKeep; ++k)
+    if (tid + k * GROUP < items) store_column<FMT, D>(page, s, tid + k * GROUP, x[k], lo[k], hi[k], div);
+  if (GROUP == 32)
+    for (int e = tid + kKeep * GROUP; e < items; e += GROUP) {
+      float y[16];
+      int l, g;
+      load_column<D, BF16>(a, s, key, h, e, y, l, g);
+      store_column<FMT, D>(page, s, e, y, l, g, div);
+    }
+}
+
+// The queries of a slot's rows, heads h0 .. h1 - 1.
+template <int D, bool BF16>
+__device__ __forceinline__ void rotate_queries(const AppendArgs& a, const Slot& s, int h0, int h1) {
+  constexpr int kCols = D / 16;
+  const PagedAppendCall& c = a.c;
+  const int items = s.count * kCols, side = max(1, min(h1 - h0, kThreads / items));   // heads side by side
+  for (int e = threadIdx.x; e < items * side; e += kThreads) {
+    const int sh = e / items, item = e - sh * items, i = item / kCols, col = item % kCols;
+    const int64_t row = s.row0 + i;
+    const bool turn = col < c.rope.rot / 16;
+    const int lo = turn ? turn_lo(col, c.rope.pairs) : 16 * col, hi = turn ? turn_hi(col, c.rope.rot, c.rope.pairs) : 16 * col + 8;
+    Turn8 t;
+    if (turn) t.load(turn_row(c.rope, c.pos != nullptr ? c.pos[row] : s.token0 + i, a.status), 8 * col);
+    const uint16_t* x = c.q + row * c.q_stride;
+    uint16_t* out = c.q_out + row * c.q_out_stride;
+    constexpr int U = 4;                                  // heads whose loads are under way together
+    for (int h = h0 + sh; h < h1; h += U * side) {
+      uint4 p0[U], p1[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (h + u * side < h1) {
+          p0[u] = *reinterpret_cast<const uint4*>(x + (h + u * side) * D + lo);
+          p1[u] = *reinterpret_cast<const uint4*>(x + (h + u * side) * D + hi);
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (h + u * side >= h1) break;
+        if (turn) {
+          float v[16];
+          widen8<BF16>(p0[u], v);
+          widen8<BF16>(p1[u], v + 8);
+          rotate16(v, t, c.rope.pairs, 1.f);
+          p0[u] = narrow8<BF16>(v);
+          p1[u] = narrow8<BF16>(v + 8);
+        }
+        *reinterpret_cast<uint4*>(out + (h + u * side) * D + lo) = p0[u];
+        *reinterpret_cast<uint4*>(out + (h + u * side) * D + hi) = p1[u];
+      }
+    }
+  }
+}
+
+template <int FMT, int D, bool BF16, int GROUP>
+__global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a) {
+  pdl_wait_and_trigger();
+  const PagedAppendCall& c = a.c;
+  const int page = c.s.page;
+  int b, j;                                                // the slot's entry; its page, counted from the entry's first
+  int64_t slots;                                           // of the entry
+  if (c.s.start == nullptr) {
+    b = blockIdx.x / a.cap;
+    j = blockIdx.x - b * a.cap;
+    slots = a.cap;
+  } else {
+    b = slot_entry(a, blockIdx.x, threadIdx.x & 31);
+    const int64_t base = slot_base(a, b);
+    j = (int)((int64_t)blockIdx.x - base);
+    slots = slot_base(a, b + 1) - base;
+    if (j < 0 || j >= slots) return;                       // (behind the last entry's)
+  }
+  const EntryRows rows = entry_rows(c.s, b);
+  if (rows.count == 0) return;
+  const int t = c.T_len[b];
+  const int64_t t0 = max(t, 0);
+  bool ok = t >= 0, pages = true;
+  ok = ok && t0 + rows.count <= c.s.max_pages * page;
+  if (ok)
+    for (int64_t p = t0 / page + threadIdx.x; p <= (t0 + rows.count - 1) / page; p += kThreads) {
+      const int pid = c.s.page_table[b * c.s.max_pages + p];
+      pages = pages && pid >= 0 && pid < c.s.num_pages;
+    }
+  pages = __syncthreads_and(pages);
+  if (threadIdx.x == 0) {
+    const int all = (int)(slots * (a.kv_ctas + a.q_ctas));
+    if (atomicAdd(c.tickets + b, 1) == all - 1) {          // every CTA of the entry has read its length
+      c.tickets[b] = 0;
+      if (!ok || !pages)
+        atomicOr(a.status, ok ? MKV_FLAG_BAD_INDEX : MKV_FLAG_CACHE_FULL);
+      else
+        c.T_len[b] = (int)(t0 + rows.count);
+    }
+  }
+  Slot s;
+  const int off = (int)(t0 % page);
+  const int64_t i0 = max((int64_t)0, (int64_t)j * page - off), i1 = min(rows.count, (int64_t)(j + 1) * page - off);
+  if (i0 >= i1) return;
+  s.row0 = rows.first + i0;
+  s.token0 = (int64_t)t + i0;
+  s.count = (int)(i1 - i0);
+  s.at = j == 0 ? off : 0;
+  s.held = s.at;
+  if ((int)blockIdx.y >= a.kv_ctas) {
+    const int h0 = ((int)blockIdx.y - a.kv_ctas) * a.q_heads;
+    rotate_queries<D, BF16>(a, s, h0, min(h0 + a.q_heads, c.s.Hq));
+    return;
+  }
+  if (!ok || !pages) return;
+  s.pid = c.s.page_table[b * c.s.max_pages + t0 / page + j];
+  const int unit = blockIdx.y * (kThreads / GROUP) + threadIdx.x / GROUP;
+  if (unit < 2 * c.s.Hkv) quantize_unit<FMT, D, BF16, GROUP>(a, s, unit < c.s.Hkv, unit < c.s.Hkv ? unit : unit - c.s.Hkv);
+}
+
+template <int FMT, int D, bool BF16>
+cudaError_t launch_d(const AppendArgs& args, int64_t slots, bool warps, cudaStream_t st) {
+  AppendArgs a = args;
+  a.kv_ctas = warps ? (int)ceil_div(2 * a.c.s.Hkv, kThreads / 32) : 2 * a.c.s.Hkv;
+  const dim3 grid((unsigned)slots, (unsigned)(a.kv_ctas + a.q_ctas));
+  if (warps) return launch_pdl(append_kernel<FMT, D, BF16, 32>, grid, dim3(kThreads), 0, st, a);
+  return launch_pdl(append_kernel<FMT, D, BF16, kThreads>, grid, dim3(kThreads), 0, st, a);
+}
+template <int FMT>
+cudaError_t launch_f(const AppendArgs& a, int64_t slots, bool warps, cudaStream_t st) {
+  const bool bf16 = a.c.s.dtype == MKV_BF16;
+  if (a.c.s.D == 128)
+    return bf16 ? launch_d<FMT, 128, true>(a, slots, warps, st) : launch_d<FMT, 128, false>(a, slots, warps, st);
+  return bf16 ? launch_d<FMT, 64, true>(a, slots, warps, st) : launch_d<FMT, 64, false>(a, slots, warps, st);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_append(const PagedAppendCall& c, cudaStream_t st) {
+  AppendArgs a{};
+  const cudaError_t e = status_word(&a.status);
+  if (e != cudaSuccess) return e;
+  a.c = c;
+  const int64_t m = ceil_div(c.s.n, c.s.B), page = c.s.page;
+  a.cap = (int)((m + page - 2) / page + 1);
+  const int64_t slots = c.s.start == nullptr ? c.s.B * (int64_t)a.cap : (c.s.n + c.s.B * (2 * page - 2)) / page;
+  if (slots > INT32_MAX) return cudaErrorInvalidConfiguration;
+  // A warp holds 128 columns: a page of 16 tokens, or the few tokens an entry of a decode step.
+  const bool warps = std::min(m, page) * (c.s.D / 16) <= 32 * kKeep;
+  // (without a rotation, queries that stay where they are need nothing)
+  const bool queries = c.q != nullptr && !(c.rope.rot == 0 && c.q_out == c.q);
+  a.q_heads = warps ? std::min(c.s.Hq, 32) : std::min(c.s.Hq, 8);
+  a.q_ctas = queries ? (int)ceil_div(c.s.Hq, a.q_heads) : 0;
+  return c.s.format == MKV_E4M3 ? launch_f<MKV_E4M3>(a, slots, warps, st) : launch_f<MKV_I8>(a, slots, warps, st);
+}
+
+}  // namespace mkv
