@@ -77,6 +77,21 @@ __device__ __forceinline__ EntryRows entry_rows(const PagedShape& s, int b) {
   return {r0, min(max((int64_t)s.start[b + 1], r0), s.n) - r0};
 }
 
+// The last entry of B that begins at or before what is looked for (`begins(b)`, true up to it; 32 entries at a time, by a
+// whole warp).
+template <typename F>
+__device__ __forceinline__ int find_entry(int B, int lane, F begins) {
+  int lo = 0, count = B;
+  for (;;) {
+    const int step = (count + 31) / 32, at = lane * step;
+    const unsigned upto = __ballot_sync(0xffffffffu, at < count && begins(lo + at));
+    const int last = max(0, __popc(upto) - 1);
+    lo += last * step;
+    if (step == 1) return lo;
+    count = min(step, count - last * step);
+  }
+}
+
 // Four 8-bit codes as two pairs of fp16: even holds bytes 0 and 2, odd bytes 1 and 3.  E4M3: an e4m3 code's sign,
 // exponent and mantissa moved into fp16's places read as the code's value times 2^-8 (the two formats' exponent biases
 // differ by 8), zero and subnormal codes alike; the NaN codes read as +-480, so no bits of a page give a non-finite

@@ -69,8 +69,12 @@ struct PagedAttnCall {
   const uint8_t *k, *v;
   const float *k_scale, *v_scale;
 };
-constexpr int kPagedRows = 32;     // query rows of a key head up to which paged_decode.cu takes a call
+// Calls of up to kPagedRows query rows a key head (max_rows x heads of a group) go to paged_decode.cu, others to
+// paged_prefill.cu.
+constexpr int kPagedRows = 32;
 size_t paged_decode_ws_bytes(const PagedAttnCall& c);
 cudaError_t launch_paged_decode(const PagedAttnCall& c, void* ws, cudaStream_t st);
+size_t paged_prefill_ws_bytes(const PagedAttnCall& c);
+cudaError_t launch_paged_prefill(const PagedAttnCall& c, void* ws, cudaStream_t st);
 
 }  // namespace mkv

@@ -131,9 +131,12 @@ PagedShape shape_of(const mkv_paged_config* c, int64_t n, const int32_t* start, 
 mkv_status check_attention_rows(const mkv_paged_config* c, int64_t n, int64_t max_rows) {
   MKV_REQUIRE(n >= 1 && max_rows >= 1 && max_rows <= n, MKV_ERR_INVALID_ARG, "rows must be 1 <= max_rows <= n");
   MKV_REQUIRE(n <= INT32_MAX, MKV_ERR_UNSUPPORTED, "n = %lld too large", (long long)n);
-  MKV_REQUIRE(max_rows * (c->Hq / c->Hkv) <= kPagedRows, MKV_ERR_UNSUPPORTED,
-              "max_rows x query heads a key head above %d", kPagedRows);
   return MKV_OK;
+}
+
+bool few_rows(const PagedAttnCall& c) { return c.max_rows * (c.s.Hq / c.s.Hkv) <= kPagedRows; }
+size_t attention_ws_bytes(const PagedAttnCall& c) {
+  return few_rows(c) ? paged_decode_ws_bytes(c) : paged_prefill_ws_bytes(c);
 }
 
 }  // namespace
@@ -248,7 +251,7 @@ mkv_status mkv_paged_workspace_size(const mkv_paged_config* cfg, int64_t n, int6
   PagedAttnCall c{};
   c.s = shape_of(cfg, n, nullptr, nullptr);
   c.max_rows = max_rows;
-  *bytes = paged_decode_ws_bytes(c);
+  *bytes = attention_ws_bytes(c);
   return MKV_OK;
 }
 
@@ -267,7 +270,7 @@ mkv_status mkv_paged_attention(const mkv_paged_config* cfg, const void* q, int64
   MKV_TRY(check_row("out", out, dims, &c.out_stride));
   c.s = shape_of(cfg, n, start, cache);
   c.max_rows = max_rows;
-  const size_t need = paged_decode_ws_bytes(c);
+  const size_t need = attention_ws_bytes(c);
   MKV_REQUIRE(ws != nullptr && ws_bytes >= need, MKV_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
   MKV_REQUIRE(aligned(ws, 256), MKV_ERR_INVALID_ARG, "ws must be 256-byte aligned");
   c.scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / sqrtf((float)cfg->D);
@@ -278,7 +281,7 @@ mkv_status mkv_paged_attention(const mkv_paged_config* cfg, const void* q, int64
   c.v = static_cast<const uint8_t*>(cache->v);
   c.k_scale = cache->k_scale;
   c.v_scale = cache->v_scale;
-  MKV_CUDA(launch_paged_decode(c, ws, as_stream(stream)));
+  MKV_CUDA(few_rows(c) ? launch_paged_decode(c, ws, as_stream(stream)) : launch_paged_prefill(c, ws, as_stream(stream)));
   return MKV_OK;
 }
 

@@ -35,19 +35,6 @@ __device__ __forceinline__ int64_t slot_base(const AppendArgs& a, int b) {
   const int64_t r0 = min(max((int64_t)a.c.s.start[b], (int64_t)0), a.c.s.n);
   return (r0 + (int64_t)b * (2 * a.c.s.page - 2)) / a.c.s.page;
 }
-// The entry of a slot: the last one whose slots begin at or before it (32 entries looked up at a time).
-__device__ __forceinline__ int slot_entry(const AppendArgs& a, int64_t slot, int lane) {
-  int lo = 0, count = a.c.s.B;
-  for (;;) {
-    const int step = (count + 31) / 32, at = lane * step;
-    const unsigned upto = __ballot_sync(0xffffffffu, at < count && slot_base(a, lo + at) <= slot);
-    const int last = max(0, __popc(upto) - 1);
-    lo += last * step;
-    if (step == 1) return lo;
-    count = min(step, count - last * step);
-  }
-}
-
 template <int FMT>
 __device__ __forceinline__ constexpr float top_code() { return FMT == MKV_E4M3 ? 448.f : 127.f; }
 
@@ -275,7 +262,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a) {
     j = blockIdx.x - b * a.cap;
     slots = a.cap;
   } else {
-    b = slot_entry(a, blockIdx.x, threadIdx.x & 31);
+    b = find_entry(c.s.B, threadIdx.x & 31, [&](int e) { return slot_base(a, e) <= (int64_t)blockIdx.x; });
     const int64_t base = slot_base(a, b);
     j = (int)((int64_t)blockIdx.x - base);
     slots = slot_base(a, b + 1) - base;
