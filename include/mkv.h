@@ -663,7 +663,8 @@ mkv_status mkv_rope_apply(const mkv_rope_config* cfg, int32_t dtype, const void*
  * written. */
 typedef enum {
   MKV_E4M3 = 0,   /* 8-bit floats, largest 448; the two NaN codes are never
-                     written and stand for +-480 where they are read        */
+                     written, and are NaN where a token holds them (what lies
+                     behind an entry's last token may be anything)          */
   MKV_I8 = 1      /* two's complement, -127..127                             */
 } mkv_code_format;
 

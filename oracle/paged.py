@@ -61,7 +61,7 @@ def _e4m3_values():
     return v
 
 
-E4M3 = _e4m3_values()          # the two NaN codes read as +-480
+E4M3 = _e4m3_values()          # (of the two NaN codes: what their bits would be)
 
 
 def decode(codes, fmt):

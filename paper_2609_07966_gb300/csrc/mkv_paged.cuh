@@ -92,27 +92,42 @@ __device__ __forceinline__ int find_entry(int B, int lane, F begins) {
   }
 }
 
-// Four 8-bit codes as two pairs of fp16: even holds bytes 0 and 2, odd bytes 1 and 3.  E4M3: an e4m3 code's sign,
-// exponent and mantissa moved into fp16's places read as the code's value times 2^-8 (the two formats' exponent biases
-// differ by 8), zero and subnormal codes alike; the NaN codes read as +-480, so no bits of a page give a non-finite
-// number, which a weight of zero would not mask.  I8: 1024 + 128 + x by placing the biased byte in the mantissa, less
-// 1152.  All exact.
-constexpr float kE4m3Up = 256.f;    // what an e4m3 code's fp16 form is short of
+// Four 8-bit codes as two pairs of fp16, bytes 0 and 1 and bytes 2 and 3; exact.  E4M3: one conversion a pair (shifting
+// sign, exponent and mantissa into place takes 10 issue cycles of a scheduler for four codes, this 6); the NaN codes become
+// NaN.  I8: 1024 + 128 + x by placing the biased byte in the mantissa, less 1152.
 template <int FMT>
-__device__ __forceinline__ void widen_codes(uint32_t w, uint32_t& even, uint32_t& odd) {
+__device__ __forceinline__ void widen_codes(uint32_t w, uint32_t& lo, uint32_t& hi) {
   if (FMT == MKV_E4M3) {
-    const uint32_t u = w << 7;
-    even = ((w << 8) & 0x80008000u) | (u & 0x3f803f80u);
-    odd = (w & 0x80008000u) | ((w >> 1) & 0x3f803f80u);
+    asm("{ .reg .b16 a, b; mov.b32 {a, b}, %2; cvt.rn.f16x2.e4m3x2 %0, a; cvt.rn.f16x2.e4m3x2 %1, b; }"
+        : "=r"(lo), "=r"(hi)
+        : "r"(w));
   } else {
     const uint32_t u = w ^ 0x80808080u;
-    const uint32_t e = (u & 0x00ff00ffu) | 0x64006400u, o = __byte_perm(u, 0x64646464u, 0x4341);
+    const uint32_t l = __byte_perm(u, 0x64646464u, 0x4140), h = __byte_perm(u, 0x64646464u, 0x4342);
     const __half2 k = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
-    const __half2 he = __hsub2(*reinterpret_cast<const __half2*>(&e), k);
-    const __half2 ho = __hsub2(*reinterpret_cast<const __half2*>(&o), k);
-    even = *reinterpret_cast<const uint32_t*>(&he);
-    odd = *reinterpret_cast<const uint32_t*>(&ho);
+    const __half2 hl = __hsub2(*reinterpret_cast<const __half2*>(&l), k);
+    const __half2 hh = __hsub2(*reinterpret_cast<const __half2*>(&h), k);
+    lo = *reinterpret_cast<const uint32_t*>(&hl);
+    hi = *reinterpret_cast<const uint32_t*>(&hh);
   }
+}
+
+// Softmax over 8-bit pages.  Two running maxima a row: m of the scores s (log2), for the sum of the weights p = 2^(s - m),
+// and m2 of s + log2 vs, for the weights p vs 2^(m - m2 + 6) that the tensor cores take in fp16: pages of any value scales
+// then keep full precision.  Either is only raised once a score passes it by 2^8, so accumulators are almost never rescaled
+// and a weight stays below 2^14 (vs is taken as mantissa and exponent, 2^(e - 1) <= vs < 2^e).
+constexpr float kRaise = 8.f;
+constexpr float kOffset = 6.f;      // (full precision in fp16 down to 2^-20 of the maximum)
+constexpr float kNoMax = -3.402823466e+38f;   // the maxima of a row that has seen nothing: no score is below it
+// An output is o / sum 2^(m2 - m - 6): the power's square root, applied twice after 1 / sum (it could pass fp32's range).
+__device__ __forceinline__ float half_power(float m, float m2) { return ex2_approx(0.5f * (m2 - m - kOffset)); }
+
+// What an fp32 power of two of `exponent` (within -126 .. 127) is.
+__device__ __forceinline__ float power_of_two(int exponent) { return __uint_as_float((uint32_t)(127 + exponent) << 23); }
+// The exponent of the power of two that a bf16 row is scaled by, so that it fits fp16: its largest finite magnitude comes to
+// lie within 2^14 .. 2^15 (what that rounds away is 2^-39 of it).
+__device__ __forceinline__ int row_exponent(float most) {
+  return most > 0.f ? max(-113, min(126, 14 + 127 - (int)(__float_as_uint(most) >> 23))) : 0;
 }
 
 }  // namespace mkv

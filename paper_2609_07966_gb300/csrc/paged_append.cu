@@ -81,15 +81,14 @@ __device__ __forceinline__ uint2 encode8(const float* x) {
 // Four codes as their values.
 template <int FMT>
 __device__ __forceinline__ void decode4(uint32_t w, float* x) {
-  uint32_t even, odd;
-  widen_codes<FMT>(w, even, odd);
-  const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&even));
-  const float2 o = __half22float2(*reinterpret_cast<const __half2*>(&odd));
-  constexpr float up = FMT == MKV_E4M3 ? kE4m3Up : 1.f;
-  x[0] = e.x * up;
-  x[1] = o.x * up;
-  x[2] = e.y * up;
-  x[3] = o.y * up;
+  uint32_t lo, hi;
+  widen_codes<FMT>(w, lo, hi);
+  const float2 l = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+  const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  x[0] = l.x;
+  x[1] = l.y;
+  x[2] = h.x;
+  x[3] = h.y;
 }
 
 // The rows of a slot: rows row0 .. row0 + count - 1 of the call, tokens at .. of page `pid`, which holds `held` tokens.

@@ -8,8 +8,7 @@
 //   O_i [128 x D]  += W_i V      W_i (the weights, fp16) from tensor memory, over the S_i they came from
 // The tensor cores have no product of 16-bit queries with 8-bit codes, so one warpgroup widens every tile's codes to fp16
 // (exactly) on their way into shared memory: plain 16-byte loads, eight of the next operand always under way, then the
-// swizzled layout that the products read.  Four dims of a code word come out in the order 0, 2, 1, 3; queries are stored in
-// that order too, and the outputs put back.  Once a tile serves 256 rows its conversion is an eighth of the products' time.
+// swizzled layout that the products read.  Once a tile serves 256 rows its conversion is an eighth of the products' time.
 //
 // A tile's pages have scales of their own: within 16 columns both are constant, so a score's is part of the factor of its
 // exponent, the maxima are kept per 16 columns until they are scaled, and a weight is p vs 2^(m - m2 + 6).
@@ -27,8 +26,6 @@ namespace {
 
 constexpr int kBR = 128;            // rows a block, tokens a tile
 constexpr int kRows = 2 * kBR;      // rows a unit
-constexpr float kRaise = 8.f, kOffset = 6.f;   // as in paged_decode.cu
-constexpr float kNoMax = -3.402823466e+38f;
 // Up to this maximum (log2) an unrounded product of score and scale is within a half of the rounded one.
 constexpr float kFused = 16777216.f;
 constexpr int kThreads = 512;       // two softmax warpgroups, one that converts, one whose first warp issues products
@@ -40,7 +37,7 @@ struct PrefillArgs {
   PagedAttnCall c;
   uint32_t* status;
   int G;
-  float scale_log2;                 // (e4m3: with the 2^8 that the widened codes lack)
+  float scale_log2;
   int64_t slots;                    // units of all entries, a key head's
   int per;                          // start null: units of an entry
   int splits;                       // parts of a unit's tokens
@@ -106,12 +103,6 @@ __device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
-}
-
-// o / sum 2^(m2 - m - 6) (e4m3: + 8), as a factor applied twice after 1 / sum (the power could pass fp32's range)
-template <int FMT>
-__device__ __forceinline__ float half_power(float m, float m2) {
-  return ex2_approx(0.5f * (m2 - m - kOffset + (FMT == MKV_E4M3 ? 8.f : 0.f)));
 }
 
 template <class S, bool BF16>
@@ -259,8 +250,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       x[i] = o < 0 ? make_uint4(0, 0, 0, 0)
                    : __ldg(reinterpret_cast<const uint4*>(codes + o + (row & 15) * D + piece * 16));
     };
-    auto store = [&](int i, uint8_t* tile) {
-      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+    auto store = [&](int i, uint8_t* tile, bool zero) {
+      const uint32_t w[4] = {zero ? 0u : x[i].x, zero ? 0u : x[i].y, zero ? 0u : x[i].z, zero ? 0u : x[i].w};
       uint32_t e[8];
 #pragma unroll
       for (int k = 0; k < 4; ++k) widen_codes<S::FMT>(w[k], e[2 * k], e[2 * k + 1]);
@@ -292,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       if (!ok) break;
 #pragma unroll
       for (int i = 0; i < STEP; ++i) {
-        store(i, tile);
+        store(i, tile, false);
         load(i, off, c.v);
       }
       if (warp == 8 && lane < 8) {
@@ -304,11 +295,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       hand_over(&ctl->kfull[s]);
       pid = check(t + 1, next);
       off = offset(t + 1, pid);
+      const int tail = u.len - (c0 + t) * kBR;             // rows of the tile that exist
       if (t > 1) ok = __all_sync(0xffffffffu, wait_or_fail(&ctl->vempty[s], (uint32_t)(((t >> 1) - 1) & 1), fail, status));
       if (!ok) break;
 #pragma unroll
       for (int i = 0; i < STEP; ++i) {
-        store(i, tile + S::TILE);
+        // (what lies behind the length, whatever it is, must not meet a zero weight as NaN)
+        store(i, tile + S::TILE, i * ROWS + row >= tail);
         load(i, off, c.k);
       }
       hand_over(&ctl->vfull[s]);
@@ -344,16 +337,15 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
             for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(v[i]) < INFINITY ? fabsf(v[i]) : 0.f);
 #pragma unroll
             for (int d = 1; d < LN; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-            const int e = most > 0.f ? max(-113, min(126, 14 + 127 - (int)(__float_as_uint(most) >> 23))) : 0;
-            const float f = __uint_as_float((uint32_t)(127 + e) << 23);
+            const int e = row_exponent(most);
+            const float f = power_of_two(e);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] *= f;
             y[q] = narrow8<false>(v);
-            if (ch == 0) qs[r] = __uint_as_float((uint32_t)(127 - e) << 23);
+            if (ch == 0) qs[r] = power_of_two(-e);
           }
           *reinterpret_cast<uint4*>(sm + S::Q_OFF + (r / kBR) * S::QBLK + (ch >> 3) * S::ATOM + mn_offset<64>(r % kBR, ch & 7)) =
-              make_uint4(__byte_perm(y[q].x, y[q].y, 0x5410), __byte_perm(y[q].x, y[q].y, 0x7632),
-                         __byte_perm(y[q].z, y[q].w, 0x5410), __byte_perm(y[q].z, y[q].w, 0x7632));
+              y[q];
         }
       }
       fence_async_smem();
@@ -472,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     if (!dead) {
       const bool whole = a.splits == 1;
       // zeros for a row that sees nothing; NaN for one whose scores are all minus infinity
-      const float inv = seen <= 0 ? 0.f : l == 0.f ? NAN : 1.f / l, hp = half_power<S::FMT>(m, m2);
+      const float inv = seen <= 0 ? 0.f : l == 0.f ? NAN : 1.f / l, hp = half_power(m, m2);
       if (!whole) a.part_st[part + rin] = make_float4(m, l, m2, 0.f);
       uint16_t* dst = c.out + (u.row0 + row / u.G) * c.out_stride + (int64_t)(u.kvh * u.G + row % u.G) * D;
       float* po = a.part_o + (part + rin) * D;
@@ -482,19 +474,18 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
           float o[32];
           tm_load<32>(tO + i * 32, o);
           if (row >= u.rows) continue;
-          // (dims come in the order 0, 2, 1, 3)
           if (whole) {
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = inv == 0.f ? 0.f : o[e] * inv * hp * hp;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               reinterpret_cast<uint4*>(dst + i * 32)[e] =
-                  make_uint4(pack2<BF16>(o[8 * e], o[8 * e + 2]), pack2<BF16>(o[8 * e + 1], o[8 * e + 3]),
-                             pack2<BF16>(o[8 * e + 4], o[8 * e + 6]), pack2<BF16>(o[8 * e + 5], o[8 * e + 7]));
+                  make_uint4(pack2<BF16>(o[8 * e], o[8 * e + 1]), pack2<BF16>(o[8 * e + 2], o[8 * e + 3]),
+                             pack2<BF16>(o[8 * e + 4], o[8 * e + 5]), pack2<BF16>(o[8 * e + 6], o[8 * e + 7]));
           } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              reinterpret_cast<float4*>(po + i * 32)[e] = make_float4(o[4 * e], o[4 * e + 2], o[4 * e + 1], o[4 * e + 3]);
+              reinterpret_cast<float4*>(po + i * 32)[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
           }
         }
       }
@@ -548,7 +539,7 @@ __global__ void __launch_bounds__(256) join_kernel(const PrefillArgs a) {
 #pragma unroll
     for (int k = 0; k < VL; ++k) y[k] += f * po[k];
   }
-  const float inv = u.seen(row) <= 0 ? 0.f : sum == 0.f ? NAN : 1.f / sum, hp = half_power<FMT>(mx, mx2);
+  const float inv = u.seen(row) <= 0 ? 0.f : sum == 0.f ? NAN : 1.f / sum, hp = half_power(mx, mx2);
 #pragma unroll
   for (int k = 0; k < VL; ++k) y[k] = inv == 0.f ? 0.f : y[k] * inv * hp * hp;
   uint16_t* dst = a.c.out + (u.row0 + row / u.G) * a.c.out_stride + (int64_t)(u.kvh * u.G + row % u.G) * D + lane * VL;
@@ -605,7 +596,7 @@ cudaError_t launch_paged_prefill(const PagedAttnCall& c, void* ws, cudaStream_t 
   const Plan p = plan_of(c);
   a.c = c;
   a.G = c.s.Hq / c.s.Hkv;
-  a.scale_log2 = c.scale * kLog2e * (c.s.format == MKV_E4M3 ? kE4m3Up : 1.f);
+  a.scale_log2 = c.scale * kLog2e;
   a.slots = p.slots;
   a.per = p.per;
   a.splits = p.splits;
