@@ -72,6 +72,7 @@ struct PagedAttnCall {
 // Calls of up to kPagedRows query rows a key head (max_rows x heads of a group) go to paged_decode.cu, others to
 // paged_prefill.cu.
 constexpr int kPagedRows = 8;
+bool paged_decode_countable(const PagedAttnCall& c);      // its chunks fit the kernel's 32-bit counts
 size_t paged_decode_ws_bytes(const PagedAttnCall& c);
 cudaError_t launch_paged_decode(const PagedAttnCall& c, void* ws, cudaStream_t st);
 size_t paged_prefill_ws_bytes(const PagedAttnCall& c);

@@ -13,9 +13,10 @@
 // whole 16-byte pieces of its rows.  Queries are fp16 in registers (bf16 ones scaled by a power of two a row).  Statistics
 // and accumulators are fp32.
 //
-// Work: the chunks of all (entry, key head) units end to end, an equal run for every CTA whatever the entries' lengths
-// (read on the device); pieces of a unit that several runs share go to the workspace, and the last CTA of the unit to
-// arrive adds them up in their order.  One warp loads chunks by TMA, a page (or its part of the chunk) a copy.
+// Work: the chunks of all (entry, key head) units end to end, cut into equal runs whatever the entries' lengths (read on the
+// device); a CTA takes one, or several in turn.  Pieces of a unit that several runs share go to the workspace, and the CTA
+// whose piece is the last to arrive adds them up in their order.  One warp finds out the work and loads it by TMA, a page
+// (or its part of the chunk) a copy; what the other warps have to know of a chunk comes with it.
 #include <math.h>
 
 #include <algorithm>
@@ -28,10 +29,14 @@ namespace {
 
 constexpr int N = 8;                // rows
 constexpr int W = 4;                // warps that compute
-constexpr int kChunk = 32 * W;      // tokens
+constexpr int kTokens = 32 * W;     // of a chunk
 constexpr int kComputing = 32 * W, kThreads = kComputing + 32;
 constexpr int kCtas = 2;            // of them an SM
-constexpr size_t kRuns = kCtas * kNumSMs;
+constexpr int kGrid = kCtas * kNumSMs;
+// Long runs are cut into four each, which the CTAs take in turn as they get done: SMs differ by a tenth in what they get of
+// HBM's bandwidth.
+constexpr int kTurns = 4, kLongRun = 32;
+constexpr size_t kRuns = kGrid * kTurns;
 
 struct DecodeArgs {
   PagedAttnCall c;
@@ -39,7 +44,9 @@ struct DecodeArgs {
   int G;
   float scale_log2;
   int box;                          // tokens of a page's copy: min(page, chunk)
+  int log_page;
   int* tickets;                     // [B][Hkv], zero between calls
+  int* next_run;                    // zero between calls
   float* part_o;                    // [kRuns][2][N][D]
   float4* part_st;                  // [kRuns][2][N]: m, sum, m2
 };
@@ -47,22 +54,32 @@ struct DecodeArgs {
 template <int FMT_, int D_>
 struct DShape {
   static constexpr int FMT = FMT_, D = D_, STAGES = D == 128 ? 3 : 6;
-  static constexpr int TILE = kChunk * D, GROUPS = kChunk / 16;
+  static constexpr int TILE = kTokens * D, GROUPS = kTokens / 16;
   static constexpr int KV_OFF = 0;                         // [STAGES][K, V]
   static constexpr int SC_OFF = STAGES * 2 * TILE;         // [STAGES][GROUPS] float4: key factor, mantissa and exponent of vs, seen
   static constexpr int O_OFF = SC_OFF + STAGES * GROUPS * 16;   // [W - 1][N][D] floats
-  static constexpr int ST_OFF = O_OFF + (W - 1) * N * D * 4;    // [W][N] float4
-  static constexpr int CTL_OFF = ST_OFF + W * N * 16;
+  static constexpr int ST_OFF = O_OFF + (W - 1) * N * D * 4;    // [W + 1][N] float4: the warps', the piece's
+  static constexpr int HD_OFF = ST_OFF + (W + 1) * N * 16;      // [STAGES] Head
+  static constexpr int Q_OFF = HD_OFF + STAGES * 48;       // [N][D] queries
+  static constexpr int CTL_OFF = Q_OFF + N * D * 2;
   static constexpr int ALLOC = CTL_OFF + 256 + 1024;       // slack to align the base to 1024 B
   static_assert(kCtas * (ALLOC + 1024) <= 228 * 1024, "shared memory");
 };
 
 struct DecodeCtl {
-  uint64_t full[8], empty[8];
-  int64_t run0, run1, base, total, runs;
-  int b0, fail, loads, last;
+  uint64_t full[6], empty[6], qfull, qempty, meet;
+  int fail, loads, q_loads, last;
 };
 static_assert(sizeof(DecodeCtl) <= 256, "control block");
+
+// What comes with a chunk.
+enum { kFirst = 1, kLast = 2, kWhole = 4, kEnd = 8 };     // of a piece; the piece is the whole unit; nothing comes any more
+struct Head {
+  int flags, chunk, len, tokens;   // tokens: the entry's new ones
+  int unit, kvh, row0, mine;       // mine: this piece's place
+  int first, place0, count, pad;   // the unit's pieces: the run of the first, its place; how many there are
+};
+static_assert(sizeof(Head) == 48, "three 16-byte accesses");
 
 // Byte offset of 16-byte piece c of row r of a tile as TMA writes it (rows of 128 or 64 bytes, that swizzle).
 template <int D>
@@ -70,51 +87,36 @@ __device__ __forceinline__ uint32_t code_offset(int r, int c) {
   return mn_offset<D / 2>(r, c);
 }
 
-__device__ __forceinline__ int entry_tokens(const PagedAttnCall& c, int b) {
-  return (int)min((int64_t)max(c.T_len[b], 0), c.s.max_pages * c.s.page);
-}
 struct Entry {
-  int64_t row0;
-  int rows, len, chunks;           // new tokens, tokens held, chunks of a unit
+  int row0, tokens, len, chunks;   // its first row, new tokens, tokens held, chunks of a unit
 };
 __device__ __forceinline__ Entry entry_of(const DecodeArgs& a, int b, bool report) {
   const EntryRows r = entry_rows(a.c.s, b);
   Entry e;
-  e.row0 = r.first;
-  e.rows = (int)min(r.count, a.c.max_rows + 1);
-  e.len = entry_tokens(a.c, b);
-  if (e.rows > a.c.max_rows) {
+  e.row0 = (int)r.first;
+  e.tokens = (int)min(r.count, a.c.max_rows + 1);
+  e.len = (int)min((int64_t)max(a.c.T_len[b], 0), a.c.s.max_pages << a.log_page);
+  if (e.tokens > a.c.max_rows) {
     if (report) atomicOr(a.status, MKV_FLAG_BAD_INDEX);
-    e.rows = 0;
+    e.tokens = 0;
   }
-  e.chunks = e.rows > 0 ? max(1, (e.len + kChunk - 1) / kChunk) : 0;
+  e.chunks = e.tokens > 0 ? max(1, (e.len + kTokens - 1) / kTokens) : 0;
   return e;
 }
 
-// A run's pieces: chunks c0 .. c1 - 1 of one unit at a time.
-struct Pieces {
-  const DecodeArgs& a;
-  int64_t cur, end, base;          // next chunk of the run, its end, first chunk of entry b
-  int b, index;
-  Entry e;
-  int kvh, c0, c1;
-  __device__ __forceinline__ Pieces(const DecodeArgs& args, const DecodeCtl* c)
-      : a(args), cur(c->run0), end(c->run1), base(c->base), b(c->b0), index(-1) {
-    if (cur < end) e = entry_of(a, b, false);
+// `total` chunks in `runs` runs, the first total % runs of them one longer.
+struct Runs {
+  int runs, len, longer;
+  __device__ __forceinline__ explicit Runs(int total) {
+    runs = min(total, kGrid);
+    if (total >= kGrid * kLongRun) runs = kGrid * kTurns;
+    len = runs > 0 ? total / runs : 0;
+    longer = total - len * runs;
   }
-  __device__ __forceinline__ bool next() {
-    if (cur >= end) return false;
-    while (cur >= base + (int64_t)e.chunks * a.c.s.Hkv) {
-      base += (int64_t)e.chunks * a.c.s.Hkv;
-      e = entry_of(a, ++b, false);
-    }
-    const int64_t in = cur - base;
-    kvh = (int)(in / e.chunks);
-    c0 = (int)(in - (int64_t)kvh * e.chunks);
-    c1 = (int)min((int64_t)e.chunks, c0 + (end - cur));
-    cur += c1 - c0;
-    ++index;
-    return true;
+  __device__ __forceinline__ int start(int i) const { return i * len + min(i, longer); }
+  __device__ __forceinline__ int of(int chunk) const {    // the run that holds a chunk
+    const int split = longer * (len + 1);
+    return chunk < split ? chunk / (len + 1) : longer + (chunk - split) / len;
   }
 };
 
@@ -137,137 +139,214 @@ __global__ void __launch_bounds__(kThreads, kCtas)
   uint32_t* status = a.status;
   volatile int* fail = &ctl->fail;
 
-  if (warp == W) {
-    if (lane == 0) {
-      prefetch_map(&kmap);
-      prefetch_map(&vmap);
-      for (int s = 0; s < S::STAGES; ++s) {
-        tc_mbar_init(&ctl->full[s], 1);
-        tc_mbar_init(&ctl->empty[s], W);
-      }
-      tc_fence_mbar_init();
-      ctl->fail = ctl->loads = 0;
+  if (warp == W && lane == 0) {
+    for (int s = 0; s < S::STAGES; ++s) {
+      tc_mbar_init(&ctl->full[s], 2);                      // (its copies; its head and scales)
+      tc_mbar_init(&ctl->empty[s], W);
     }
-    pdl_wait_and_trigger();
-    // all units' chunks, then this CTA's run of them and the entry that holds its first
-    int64_t total = 0;
-    for (int b = lane; b < c.s.B; b += 32) total += (int64_t)entry_of(a, b, blockIdx.x == 0).chunks * Hkv;
-#pragma unroll
-    for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-    const int64_t runs = max((int64_t)1, min((int64_t)gridDim.x, total));     // none of them empty
-    const int64_t run0 = blockIdx.x < runs ? total * blockIdx.x / runs : 0;
-    const int64_t run1 = blockIdx.x < runs ? total * (blockIdx.x + 1) / runs : 0;
-    int64_t base = 0;
-    int b0 = 0;
-    for (int b = 0; b < c.s.B && run0 < run1; b += 32) {
-      const int64_t mine = b + lane < c.s.B ? (int64_t)entry_of(a, b + lane, false).chunks * Hkv : 0;
-      int64_t upto = mine;                                 // inclusive prefix within the 32
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int64_t x = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += x;
-      }
-      const unsigned past = __ballot_sync(0xffffffffu, base + upto > run0);
-      if (past) {
-        const int w = __ffs(past) - 1;
-        b0 = b + w;
-        base += __shfl_sync(0xffffffffu, upto - mine, w);
-        break;
-      }
-      base += __shfl_sync(0xffffffffu, upto, 31);
-    }
-    if (lane == 0) {
-      ctl->run0 = run0;
-      ctl->run1 = run1;
-      ctl->base = base;
-      ctl->total = total;
-      ctl->runs = runs;
-      ctl->b0 = b0;
-    }
-  } else {
-    pdl_wait_and_trigger();
+    tc_mbar_init(&ctl->qfull, 1);
+    tc_mbar_init(&ctl->qempty, W);
+    tc_mbar_init(&ctl->meet, W);
+    tc_fence_mbar_init();
+    ctl->fail = ctl->loads = ctl->q_loads = 0;
+    prefetch_map(&kmap);
+    prefetch_map(&vmap);
   }
   __syncthreads();
+  pdl_wait_and_trigger();
 
   if (warp == W) {
     // ---------------------------------------------------------------- loads
+    const int B = c.s.B, capacity = B < 32 ? B : 32;
+    Entry held = {0, 0, 0, 0};                             // of entry `lane`
+    if (lane < capacity) held = entry_of(a, lane, blockIdx.x == 0);
+    int upto = held.chunks * Hkv, total = 0;               // inclusive prefix within the first 32 entries
+    for (int b = lane + 32; b < B; b += 32) total += entry_of(a, b, blockIdx.x == 0).chunks * Hkv;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += x;
+    }
+    const int upto32 = __shfl_sync(0xffffffffu, upto, 31);
+    if (B > 32) {
+#pragma unroll
+      for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    }
+    total += upto32;
+    const Runs rs(total);
     // A batch is 32 copies' pages, a lane each: page and scales of the next batch are fetched during this one.
-    const int per = kChunk / a.box, span = 32 / per;        // copies a chunk, chunks a batch
-    const int box16 = a.box / 16;
-    Pieces p(a, ctl);
-    int g = 0;
+    const int per = kTokens / a.box, span = 32 / per;       // copies a chunk, chunks a batch
+    const int log_box = __ffs(a.box) - 1, group_copy = lane < S::GROUPS ? lane >> (log_box - 4) : 0;
+    int g = 0, pieces = 0;
     bool ok = true;
-    while (ok && p.next()) {
-      const int32_t* table = c.s.page_table + (int64_t)p.b * c.s.max_pages;
-      auto page_of = [&](int chunk) {                      // of this lane's copy of the batch from `chunk` on
-        const int64_t t = (int64_t)chunk * kChunk + (int64_t)lane * a.box;
-        if (chunk + lane / per >= p.c1 || t >= p.e.len) return -1;
-        return table[t / c.s.page];
+    // the next stage, once it is free
+    auto stage = [&]() {
+      const int s = g % S::STAGES;
+      if (g >= S::STAGES)
+        ok = __all_sync(0xffffffffu, wait_or_fail(&ctl->empty[s], (uint32_t)((g / S::STAGES - 1) & 1), fail, status));
+      return s;
+    };
+    int r = blockIdx.x;
+    while (ok && r < rs.runs) {
+      // the run after this one, of those that the CTAs take in turn
+      int next_run = rs.runs;
+      if (rs.runs > kGrid) {
+        if (lane == 0) {
+          const int old = atomicAdd(a.next_run, 1);
+          next_run = kGrid + old;
+          if (old == rs.runs - 1) *a.next_run = 0;         // (every CTA takes one too many: that was the last of all)
+        }
+      }
+      int cur = rs.start(r);
+      const int end = rs.start(r + 1);
+      // the entry that holds the run's first chunk, and that entry's first chunk
+      int b = 0, base = 0;
+      if (cur < upto32) {
+        b = __ffs(__ballot_sync(0xffffffffu, upto > cur)) - 1;
+        base = __shfl_sync(0xffffffffu, upto - held.chunks * Hkv, b);
+      } else {
+        base = upto32;
+        for (int b0 = 32;; b0 += 32) {
+          const int mine = b0 + lane < B ? entry_of(a, b0 + lane, false).chunks * Hkv : 0;
+          int in = mine;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, in, d);
+            if (lane >= d) in += x;
+          }
+          const unsigned past = __ballot_sync(0xffffffffu, base + in > cur);
+          if (past || b0 + 32 >= B) {
+            const int w = past ? __ffs(past) - 1 : 0;
+            b = b0 + w;
+            base += __shfl_sync(0xffffffffu, in - mine, w);
+            break;
+          }
+          base += __shfl_sync(0xffffffffu, in, 31);
+        }
+      }
+      auto entry = [&](int i) {
+        if (i >= 32) return entry_of(a, i, false);
+        Entry e;
+        e.row0 = __shfl_sync(0xffffffffu, held.row0, i);
+        e.tokens = __shfl_sync(0xffffffffu, held.tokens, i);
+        e.len = __shfl_sync(0xffffffffu, held.len, i);
+        e.chunks = __shfl_sync(0xffffffffu, held.chunks, i);
+        return e;
       };
-      // (a page outside the pool is not seen)
-      auto check = [&](int chunk, int pid) {
-        const int64_t t = (int64_t)chunk * kChunk + (int64_t)lane * a.box;
-        if (chunk + lane / per >= p.c1 || t >= p.e.len) return -1;
-        if (pid < 0 || pid >= c.s.num_pages) {
+      Entry e = entry(b);
+      while (ok && cur < end) {
+        while (cur >= base + e.chunks * Hkv) {
+          base += e.chunks * Hkv;
+          e = entry(++b);
+        }
+        // -------------------------------------------------------- a piece: chunks c0 .. c1 - 1 of a unit
+        const int kvh = (cur - base) / e.chunks, unit0 = base + kvh * e.chunks;
+        const int c0 = cur - unit0, c1 = min(e.chunks, c0 + (end - cur));
+        cur += c1 - c0;
+        const int32_t* table = c.s.page_table + (int64_t)b * c.s.max_pages;
+        auto exists = [&](int chunk) {                     // this lane's copy of the batch from `chunk` on
+          return chunk + lane / per < c1 && chunk * kTokens + (lane << log_box) < e.len;
+        };
+        auto fetch = [&](int chunk) {
+          return exists(chunk) ? table[(chunk * kTokens + (lane << log_box)) >> a.log_page] : -1;
+        };
+        auto check = [&](int chunk, int id) {              // (a page outside the pool is not seen)
+          if (!exists(chunk)) return -1;
+          if (id >= 0 && id < c.s.num_pages) return id;
           atomicOr(status, MKV_FLAG_BAD_INDEX);
           return -1;
-        }
-        return pid;
-      };
-      int pid = check(p.c0, page_of(p.c0)), next = 0;
-      float ks = 0.f, vs = 1.f, nks = 0.f, nvs = 1.f;
-      if (pid >= 0) {
-        ks = c.k_scale[(int64_t)pid * Hkv + p.kvh];
-        vs = c.v_scale[(int64_t)pid * Hkv + p.kvh];
-      }
-      for (int ch = p.c0; ok && ch < p.c1; ++ch, ++g) {
-        const int in = (ch - p.c0) % span, from = ch - in;
-        if (in == 0 && ch > p.c0) {
-          pid = next;
-          ks = nks;
-          vs = nvs;
-        }
-        if (in == 0) next = page_of(ch + span);
-        if (in == span / 2) {
-          next = check(from + span, next);
-          nks = 0.f;
-          nvs = 1.f;
-          if (next >= 0) {
-            nks = c.k_scale[(int64_t)next * Hkv + p.kvh];
-            nvs = c.v_scale[(int64_t)next * Hkv + p.kvh];
+        };
+        auto scales = [&](int id, float& ks, float& vs) {
+          ks = 0.f;
+          vs = 1.f;
+          if (id >= 0) {
+            ks = c.k_scale[(int64_t)id * Hkv + kvh];
+            vs = c.v_scale[(int64_t)id * Hkv + kvh];
           }
-        }
-        const int s = g % S::STAGES;
-        if (g >= S::STAGES) ok = wait_or_fail(&ctl->empty[s], (uint32_t)((g / S::STAGES - 1) & 1), fail, status);
-        ok = __all_sync(0xffffffffu, ok);
+        };
+        int pid = fetch(c0), next = 0;
+        // queries: one copy a token's heads
+        if (pieces > 0) ok = __all_sync(0xffffffffu, wait_or_fail(&ctl->qempty, (uint32_t)((pieces - 1) & 1), fail, status));
         if (!ok) break;
-        const int mine = in * per + lane;                  // the copy that lane < per makes
-        const int id = __shfl_sync(0xffffffffu, pid, mine & 31);
-        // scales of the chunk's groups of 16 tokens
-        const int owner = in * per + (lane < S::GROUPS ? lane / box16 : 0);
-        const float gk = __shfl_sync(0xffffffffu, ks, owner), gv = __shfl_sync(0xffffffffu, vs, owner);
-        const int gid = __shfl_sync(0xffffffffu, pid, owner);
-        if (lane < S::GROUPS) {
-          int e;
-          const float m = frexpf(gv, &e);
-          reinterpret_cast<float4*>(sm + S::SC_OFF)[s * S::GROUPS + lane] =
-              make_float4(gk * a.scale_log2, m, (float)e, gid >= 0 ? 1.f : 0.f);
-        }
-        const bool copy = lane < per && id >= 0;
-        const int copies = __popc(__ballot_sync(0xffffffffu, copy));
-        __syncwarp();
         if (lane == 0) {
-          tc_mbar_expect_tx(&ctl->full[s], (uint32_t)copies * 2 * a.box * D);
-          ctl->loads = g + 1;
+          tc_mbar_expect_tx(&ctl->qfull, (uint32_t)(e.tokens * a.G * D * 2));
+          ctl->q_loads = pieces + 1;
         }
         __syncwarp();
-        if (copy) {
-          uint8_t* dst = sm + S::KV_OFF + s * 2 * S::TILE + lane * a.box * D;
-          const int64_t t = (int64_t)ch * kChunk + (int64_t)lane * a.box;
-          const int y = (int)(t % c.s.page), z = id * Hkv + p.kvh;
-          tma_load_4d(dst, &kmap, 0, y, z, 0, &ctl->full[s]);
-          tma_load_4d(dst + S::TILE, &vmap, 0, y, z, 0, &ctl->full[s]);
+        if (lane < e.tokens)
+          bulk_load(sm + S::Q_OFF + lane * a.G * D * 2,
+                    c.q + (int64_t)(e.row0 + lane) * c.q_stride + (int64_t)kvh * a.G * D, a.G * D * 2, &ctl->qfull);
+        ++pieces;
+        pid = check(c0, pid);
+        float ks, vs, nks = 0.f, nvs = 1.f;
+        scales(pid, ks, vs);
+        Head hd;
+        hd.len = e.len;
+        hd.tokens = e.tokens;
+        hd.unit = b * Hkv + kvh;
+        hd.kvh = kvh;
+        hd.row0 = e.row0;
+        const bool whole = c1 - c0 == e.chunks;
+        hd.first = hd.place0 = hd.count = hd.mine = hd.pad = 0;
+        if (!whole) {                                      // a run's places: its first piece, and its last
+          hd.first = rs.of(unit0);
+          hd.place0 = 2 * hd.first + (rs.start(hd.first) < unit0 ? 1 : 0);
+          hd.count = rs.of(unit0 + e.chunks - 1) - hd.first + 1;
+          hd.mine = r == hd.first ? hd.place0 : 2 * r;
         }
+        for (int ch = c0; ch < c1; ++ch, ++g) {
+          const int in = (ch - c0) % span, from = ch - in;
+          if (in == 0 && ch > c0) {
+            pid = next;
+            ks = nks;
+            vs = nvs;
+          }
+          if (in == 0) next = fetch(ch + span);
+          if (in == span / 2) {
+            next = check(from + span, next);
+            scales(next, nks, nvs);
+          }
+          const int s = stage();
+          if (!ok) break;
+          const int id = __shfl_sync(0xffffffffu, pid, (in * per + lane) & 31);
+          const bool copy = lane < per && id >= 0;
+          const int copies = __popc(__ballot_sync(0xffffffffu, copy));
+          if (lane == 0) {
+            tc_mbar_expect_tx(&ctl->full[s], (uint32_t)copies * 2 * a.box * D);
+            ctl->loads = g + 1;
+          }
+          __syncwarp();
+          if (copy) {
+            uint8_t* dst = sm + S::KV_OFF + s * 2 * S::TILE + (lane << log_box) * D;
+            const int y = (ch * kTokens + (lane << log_box)) & (c.s.page - 1), z = id * Hkv + kvh;
+            tma_load_4d(dst, &kmap, 0, y, z, 0, &ctl->full[s]);
+            tma_load_4d(dst + S::TILE, &vmap, 0, y, z, 0, &ctl->full[s]);
+          }
+          // scales of the chunk's groups of 16 tokens
+          const int owner = in * per + group_copy;
+          const float gk = __shfl_sync(0xffffffffu, ks, owner), gv = __shfl_sync(0xffffffffu, vs, owner);
+          const int gid = __shfl_sync(0xffffffffu, pid, owner);
+          if (lane < S::GROUPS) {
+            int x;
+            const float mant = frexpf(gv, &x);
+            reinterpret_cast<float4*>(sm + S::SC_OFF)[s * S::GROUPS + lane] =
+                make_float4(gk * a.scale_log2, mant, (float)x, gid >= 0 ? 1.f : 0.f);
+          }
+          hd.flags = (ch == c0 ? kFirst : 0) | (ch == c1 - 1 ? kLast : 0) | (whole ? kWhole : 0);
+          hd.chunk = ch;
+          if (lane == 31) *reinterpret_cast<Head*>(sm + S::HD_OFF + s * 48) = hd;
+          __syncwarp();
+          if (lane == 0) tc_mbar_arrive(&ctl->full[s]);
+        }
+      }
+      r = __shfl_sync(0xffffffffu, next_run, 0);
+    }
+    if (ok) {
+      const int s = stage();
+      if (ok && lane == 0) {
+        reinterpret_cast<Head*>(sm + S::HD_OFF + s * 48)->flags = kEnd;
+        tc_mbar_arrive(&ctl->full[s]);
+        tc_mbar_arrive(&ctl->full[s]);
       }
     }
   } else {
@@ -276,25 +355,122 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     float* ob = reinterpret_cast<float*>(sm + S::O_OFF);
     float4* stat = reinterpret_cast<float4*>(sm + S::ST_OFF);
     const bool bf16 = c.s.dtype == MKV_BF16;
-    Pieces p(a, ctl);
-    int g = 0;
+    const int G = a.G;
     bool dead = false;
-    while (p.next()) {
-      const int G = a.G, R = p.e.rows * G;
-      // ------------------------------------------------------------ queries: row lg, dims D / 4 lr ..
-      uint32_t qf[2 * KS];
-      float back[2] = {1.f, 1.f};                          // what scores of rows 2 lr and 2 lr + 1 were scaled by
-      {
-        const uint4* src = reinterpret_cast<const uint4*>(c.q + (p.e.row0 + lg / G) * c.q_stride +
-                                                          (int64_t)(p.kvh * G + lg % G) * D + lr * (D / 4));
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (!dead) dead = !__all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status));
+    };
+    // A barrier of the computing warps whose waits are bounded too: one that gave up does not leave the others waiting.
+    uint32_t met = 0;
+    auto meet = [&]() {
+      __syncwarp();
+      if (lane == 0) tc_mbar_arrive(&ctl->meet);
+      wait(&ctl->meet, met);
+      met ^= 1;
+    };
+    // An output is o / sum 2^(m2 - m - 6); zeros for a row before position 0, which sees nothing; NaN where no score leaves a
+    // weight.
+    auto out_row = [&](const Head& h, int row) {
+      return c.out + (int64_t)(h.row0 + row / G) * c.out_stride + (int64_t)(h.kvh * G + row % G) * D;
+    };
+    auto finish = [&](const Head& h, int row, float4 x, float mm, float sum, float mm2) {
+      const float f = half_power(mm, mm2), inv = sum == 0.f ? NAN : 1.f / sum;
+      x = make_float4(x.x * inv * f * f, x.y * inv * f * f, x.z * inv * f * f, x.w * inv * f * f);
+      if (h.len - h.tokens + row / G < 0) x = make_float4(0.f, 0.f, 0.f, 0.f);
+      return bf16 ? make_uint2(pack2<true>(x.x, x.y), pack2<true>(x.z, x.w))
+                  : make_uint2(pack2<false>(x.x, x.y), pack2<false>(x.z, x.w));
+    };
+    // A piece was handed in and the unit's ticket taken (by thread 0, which looks at it only here): the CTA that took the
+    // unit's last one adds the pieces up.
+    Head owed;
+    owed.count = 0;
+    int ticket = 0;
+    auto settle = [&]() {
+      if (owed.count == 0 || dead) return;
+      if (threadIdx.x == 0) {
+        ctl->last = ticket == owed.count - 1;
+        if (ctl->last) a.tickets[owed.unit] = 0;
+      }
+      meet();
+      if (dead) return;
+      if (ctl->last) {
+        constexpr int VL = D / 32;                         // dims a lane
+        auto place = [&](int i) { return (int64_t)(i == 0 ? owed.place0 : 2 * (owed.first + i)) * N; };
+        auto load = [&](int64_t at) {
+          const float* po = a.part_o + at * D + lane * VL;
+          if constexpr (VL == 4) return __ldcg(reinterpret_cast<const float4*>(po));
+          const float2 f = __ldcg(reinterpret_cast<const float2*>(po));
+          return make_float4(f.x, f.y, 0.f, 0.f);
+        };
+        for (int row = warp; row < owed.tokens * G; row += W) {   // a row a warp
+          float mx = kNoMax, mx2 = kNoMax, sum = 0.f;
+          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+          // eight pieces at a time, their loads under way together
+          for (int i0 = 0; i0 < owed.count; i0 += 8) {
+            float4 st[8], z[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const int64_t at = place(min(i0 + k, owed.count - 1)) + row;
+              st[k] = __ldcg(a.part_st + at);
+              z[k] = load(at);
+              if (i0 + k >= owed.count) st[k] = make_float4(kNoMax, 0.f, kNoMax, 0.f);
+            }
+            float nm = mx, nm2 = mx2;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              nm = fmaxf(nm, st[k].x);
+              nm2 = fmaxf(nm2, st[k].z);
+            }
+            sum *= ex2_approx(mx - nm);
+            const float back = ex2_approx(mx2 - nm2);
+            y = make_float4(y.x * back, y.y * back, y.z * back, y.w * back);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float w = i0 + k < owed.count ? ex2_approx(st[k].z - nm2) : 0.f;
+              sum += st[k].y * ex2_approx(st[k].x - nm);
+              y = make_float4(y.x + w * z[k].x, y.y + w * z[k].y, y.z + w * z[k].z, y.w + w * z[k].w);
+            }
+            mx = nm;
+            mx2 = nm2;
+          }
+          const uint2 h = finish(owed, row, y, mx, sum, mx2);
+          uint16_t* dst = out_row(owed, row) + lane * VL;
+          if constexpr (VL == 4)
+            *reinterpret_cast<uint2*>(dst) = h;
+          else
+            *reinterpret_cast<uint32_t*>(dst) = h.x;
+        }
+      }
+      meet();                                              // (before `last` is set again)
+      owed.count = 0;
+    };
+
+    uint32_t qf[2 * KS];
+    float back[2], o[MB][4], m[2], m2[2], l[2];
+    int pos0 = 0, pieces = 0;
+    for (int g = 0;; ++g) {
+      const int s = g % S::STAGES;
+      wait(&ctl->full[s], (uint32_t)((g / S::STAGES) & 1));
+      if (dead) break;
+      const Head hd = *reinterpret_cast<const Head*>(sm + S::HD_OFF + s * 48);
+      if (hd.flags & kEnd) break;
+      if (hd.flags & kFirst) {
+        // ---------------------------------------------------------- queries: row lg, dims D / 4 lr ..
+        wait(&ctl->qfull, (uint32_t)(pieces & 1));
+        if (dead) break;
+        ++pieces;
+        const uint4* src = reinterpret_cast<const uint4*>(sm + S::Q_OFF + lg * D * 2 + lr * (D / 2));
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
-          const uint4 y = lg < R ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+          const uint4 y = lg < hd.tokens * G ? src[i] : make_uint4(0u, 0u, 0u, 0u);
           qf[4 * i] = y.x;
           qf[4 * i + 1] = y.y;
           qf[4 * i + 2] = y.z;
           qf[4 * i + 3] = y.w;
         }
+        __syncwarp();
+        if (lane == 0) tc_mbar_arrive(&ctl->qempty);
+        back[0] = back[1] = 1.f;                           // what scores of rows 2 lr and 2 lr + 1 were scaled by
         if (bf16) {
           float most = 0.f;
 #pragma unroll
@@ -312,19 +488,21 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 #pragma unroll
           for (int j = 0; j < 2; ++j) back[j] = power_of_two(-__shfl_sync(0xffffffffu, e, (2 * lr + j) * 4));
         }
-      }
-      float o[MB][4], m[2] = {kNoMax, kNoMax}, m2[2] = {kNoMax, kNoMax}, l[2] = {0.f, 0.f};
 #pragma unroll
-      for (int mb = 0; mb < MB; ++mb) o[mb][0] = o[mb][1] = o[mb][2] = o[mb][3] = 0.f;
-      const int pos0 = p.e.len - p.e.rows;                 // the first new token's position
-      for (int ch = p.c0; ch < p.c1; ++ch, ++g) {
-        const int s = g % S::STAGES;
-        if (!dead) dead = !__all_sync(0xffffffffu, wait_or_fail(&ctl->full[s], (uint32_t)((g / S::STAGES) & 1), fail, status));
-        if (dead) break;
-        const int t0 = ch * kChunk + warp * 32;
+        for (int mb = 0; mb < MB; ++mb) o[mb][0] = o[mb][1] = o[mb][2] = o[mb][3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          m[j] = m2[j] = kNoMax;
+          l[j] = 0.f;
+        }
+        pos0 = hd.len - hd.tokens;                         // the first new token's position
+      }
+      {
+        const int ch = hd.chunk;
+        const int t0 = ch * kTokens + warp * 32;
         const float4* scales = reinterpret_cast<const float4*>(sm + S::SC_OFF) + s * S::GROUPS + warp * 2;
         const float4 sc[2] = {scales[0], scales[1]};
-        const bool in[2] = {sc[0].w != 0.f && t0 < p.e.len, sc[1].w != 0.f && t0 + 16 < p.e.len};
+        const bool in[2] = {sc[0].w != 0.f && t0 < hd.len, sc[1].w != 0.f && t0 + 16 < hd.len};
         if (in[0] || in[1]) {
           const uint8_t* K = sm + S::KV_OFF + s * 2 * S::TILE + warp * 32 * D;
           const uint8_t* V = K + S::TILE;
@@ -371,7 +549,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
                 v[u][i][1] = y.y;
               }
               // (a token that no row may meet must not meet a zero weight as NaN)
-              if (!in[u] || t0 + row >= p.e.len)
+              if (!in[u] || t0 + row >= hd.len)
 #pragma unroll
                 for (int k = 0; k < D / 32; ++k) v[u][i][k] = 0u;
             }
@@ -446,6 +624,8 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         __syncwarp();
         if (lane == 0) tc_mbar_arrive(&ctl->empty[s]);
       }
+      if (!(hd.flags & kLast)) continue;
+      settle();                                            // (the piece before this one's unit)
       // ------------------------------------------------------------ the warps' parts joined, in their order
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -454,7 +634,8 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         for (int d = 4; d < 32; d <<= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
         if (lg == 0) stat[warp * N + 2 * lr + j] = make_float4(m[j], t, m2[j], 0.f);
       }
-      bar_sync(1, kComputing);
+      meet();
+      if (dead) break;
       float M[2], M2[2], L[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -480,7 +661,8 @@ __global__ void __launch_bounds__(kThreads, kCtas)
                 make_float2(o[mb][j], o[mb][2 + j]);
         }
       }
-      bar_sync(1, kComputing);
+      meet();
+      if (dead) break;
       if (warp == 0) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -495,130 +677,50 @@ __global__ void __launch_bounds__(kThreads, kCtas)
             }
             *x = y;
           }
-          if (lg == 0) stat[2 * lr + j] = make_float4(M[j], L[j], M2[j], 0.f);
+          if (lg == 0) stat[W * N + 2 * lr + j] = make_float4(M[j], L[j], M2[j], 0.f);
         }
       }
-      const bool gone = bar_or(1, kComputing, dead);
+      meet();
+      if (dead) break;
       // ------------------------------------------------------------ outputs, or a piece for the unit's last CTA
+      const int R = hd.tokens * G;
       constexpr int V4 = D / 4;
-      auto finish = [&](int row, float4 x, float mm, float sum, float mm2) {
-        const bool blind = pos0 + row / G < 0;             // before position 0: it sees nothing
-        const float h = half_power(mm, mm2);
-        const float inv = sum == 0.f ? NAN : 1.f / sum;
-        const float y[4] = {x.x * inv * h * h, x.y * inv * h * h, x.z * inv * h * h, x.w * inv * h * h};
-        uint2 r;
-        if (bf16)
-          r = make_uint2(pack2<true>(y[0], y[1]), pack2<true>(y[2], y[3]));
-        else
-          r = make_uint2(pack2<false>(y[0], y[1]), pack2<false>(y[2], y[3]));
-        return blind ? make_uint2(0u, 0u) : r;
-      };
-      auto out_row = [&](int row) {
-        return c.out + (p.e.row0 + row / G) * c.out_stride + (int64_t)(p.kvh * G + row % G) * D;
-      };
-      if (p.c1 - p.c0 == p.e.chunks) {
-        if (!gone)
-          for (int e = threadIdx.x; e < R * V4; e += kComputing) {
-            const int row = e / V4, d = e % V4 * 4;
-            const float4 st = stat[row];
-            *reinterpret_cast<uint2*>(out_row(row) + d) =
-                finish(row, *reinterpret_cast<const float4*>(ob + row * D + d), st.x, st.y, st.z);
-          }
+      if (hd.flags & kWhole) {
+        for (int e = threadIdx.x; e < R * V4; e += kComputing) {
+          const int row = e / V4, d = e % V4 * 4;
+          const float4 st = stat[W * N + row];
+          *reinterpret_cast<uint2*>(out_row(hd, row) + d) =
+              finish(hd, row, *reinterpret_cast<const float4*>(ob + row * D + d), st.x, st.y, st.z);
+        }
       } else {
-        const int64_t unit0 = p.base + (int64_t)p.kvh * p.e.chunks;
-        auto run_start = [&](int64_t i) { return ctl->total * i / ctl->runs; };
-        auto run_of = [&](int64_t x) { return (int)(((x + 1) * ctl->runs - 1) / ctl->total); };
-        const int first = run_of(unit0), count = run_of(unit0 + p.e.chunks - 1) - first + 1;
-        auto place = [&](int i) {                          // of the unit's piece i: the run's first piece or its last
-          return ((int64_t)(first + i) * 2 + (i == 0 && run_start(first) < unit0 ? 1 : 0)) * N;
-        };
-        const int64_t mine = place((int)blockIdx.x - first);
+        const int64_t mine = (int64_t)hd.mine * N;
         for (int e = threadIdx.x; e < R * V4; e += kComputing)
-          reinterpret_cast<float4*>(a.part_o + mine * D)[e] = reinterpret_cast<const float4*>(ob)[e];
-        if (threadIdx.x < R) a.part_st[mine + threadIdx.x] = stat[threadIdx.x];
-        __threadfence();
-        bar_sync(1, kComputing);
-        if (threadIdx.x == 0) {
-          int* ticket = a.tickets + (int64_t)p.b * Hkv + p.kvh;
-          ctl->last = atomicAdd(ticket, 1) == count - 1;
-          if (ctl->last) *ticket = 0;
-        }
-        bar_sync(1, kComputing);
-        if (ctl->last) {
-          __threadfence();
-          constexpr int VL = D / 32;                       // dims a lane
-          for (int row = warp; row < R; row += W) {        // a row a warp: its pieces' statistics, then their outputs
-            float mx = kNoMax, mx2 = kNoMax, sum = 0.f, y[VL];
-            for (int i = lane; i < count; i += 32) {
-              const float4 st = __ldcg(a.part_st + place(i) + row);
-              mx = fmaxf(mx, st.x);
-              mx2 = fmaxf(mx2, st.z);
-            }
-#pragma unroll
-            for (int d = 16; d; d >>= 1) {
-              mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-              mx2 = fmaxf(mx2, __shfl_xor_sync(0xffffffffu, mx2, d));
-            }
-#pragma unroll
-            for (int k = 0; k < VL; ++k) y[k] = 0.f;
-            for (int i0 = 0; i0 < count; i0 += 32) {
-              float w2 = 0.f;
-              int64_t at = 0;
-              if (i0 + lane < count) {
-                at = place(i0 + lane) + row;
-                const float4 st = __ldcg(a.part_st + at);
-                sum += st.y * ex2_approx(st.x - mx);
-                w2 = ex2_approx(st.z - mx2);
-              }
-              const int most = min(32, count - i0);
-#pragma unroll 8
-              for (int k = 0; k < most; ++k) {
-                const float w = __shfl_sync(0xffffffffu, w2, k);
-                const float* po = a.part_o + __shfl_sync(0xffffffffu, at, k) * D + lane * VL;
-                float z[VL];
-                if constexpr (VL == 4) {
-                  const float4 f = __ldcg(reinterpret_cast<const float4*>(po));
-                  z[0] = f.x;
-                  z[1] = f.y;
-                  z[2] = f.z;
-                  z[3] = f.w;
-                } else {
-                  const float2 f = __ldcg(reinterpret_cast<const float2*>(po));
-                  z[0] = f.x;
-                  z[1] = f.y;
-                }
-#pragma unroll
-                for (int q = 0; q < VL; ++q) y[q] += w * z[q];
-              }
-            }
-#pragma unroll
-            for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            const uint2 r = finish(row, make_float4(y[0], y[1], VL == 4 ? y[VL - 2] : 0.f, VL == 4 ? y[VL - 1] : 0.f), mx, sum, mx2);
-            uint16_t* dst = out_row(row) + lane * VL;
-            if (!gone) {
-              if constexpr (VL == 4)
-                *reinterpret_cast<uint2*>(dst) = r;
-              else
-                *reinterpret_cast<uint32_t*>(dst) = r.x;
-            }
-          }
-        }
+          __stcg(reinterpret_cast<float4*>(a.part_o + mine * D) + e, reinterpret_cast<const float4*>(ob)[e]);
+        if (threadIdx.x < R) __stcg(a.part_st + mine + threadIdx.x, stat[W * N + threadIdx.x]);
+        meet();
+        if (dead) break;
+        if (threadIdx.x == 0)
+          asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(ticket) : "l"(a.tickets + hd.unit) : "memory");
+        owed = hd;
       }
-      bar_sync(1, kComputing);                                   // (before the next piece's queries and sums)
+      // (`ob` and the piece's statistics are written again only behind the next piece's first barrier)
     }
+    settle();
   }
   // teardown: after a failure the copies under way end first (each wait bounded)
   __syncthreads();
-  if (threadIdx.x == 0 && ctl->fail)
+  if (threadIdx.x == 0 && ctl->fail) {
+    if (ctl->q_loads > 0) tc_mbar_wait(&ctl->qfull, (uint32_t)((ctl->q_loads - 1) & 1), kRoleWaitNs);
     for (int x = std::max(0, ctl->loads - S::STAGES); x < ctl->loads; ++x)
       tc_mbar_wait(&ctl->full[x % S::STAGES], (uint32_t)((x / S::STAGES) & 1), kRoleWaitNs);
+  }
   __syncthreads();
 }
 
 // ---------------------------------------------------------------- host side
 template <class S>
 cudaError_t launch_shape(const PagedAttnCall& c, DecodeArgs a, cudaStream_t st) {
-  a.box = std::min(c.s.page, kChunk);
+  a.box = std::min(c.s.page, kTokens);
   const int64_t heads = c.s.num_pages * c.s.Hkv;
   CUtensorMap km, vm;
   cudaError_t e = encode_code_map(&km, c.k, S::D, c.s.page, heads, a.box);
@@ -626,10 +728,14 @@ cudaError_t launch_shape(const PagedAttnCall& c, DecodeArgs a, cudaStream_t st) 
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(decode_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::ALLOC);
   if (e != cudaSuccess) return e;
-  return launch_pdl(decode_kernel<S>, dim3(kRuns), dim3(kThreads), S::ALLOC, st, km, vm, a);
+  return launch_pdl(decode_kernel<S>, dim3(kGrid), dim3(kThreads), S::ALLOC, st, km, vm, a);
 }
 
 }  // namespace
+
+bool paged_decode_countable(const PagedAttnCall& c) {
+  return (int64_t)c.s.B * c.s.Hkv * (ceil_div(c.s.max_pages * c.s.page, kTokens) + 1) <= INT32_MAX / 2;
+}
 
 size_t paged_decode_ws_bytes(const PagedAttnCall& c) {
   return kCounterBytes + align256(kRuns * 2 * N * sizeof(float4)) + align256((size_t)kRuns * 2 * N * c.s.D * sizeof(float));
@@ -641,9 +747,11 @@ cudaError_t launch_paged_decode(const PagedAttnCall& c, void* ws, cudaStream_t s
   if (e != cudaSuccess) return e;
   a.c = c;
   a.G = c.s.Hq / c.s.Hkv;
+  for (a.log_page = 0; (1 << a.log_page) < c.s.page;) ++a.log_page;
   a.scale_log2 = c.scale * kLog2e;
   uint8_t* base = static_cast<uint8_t*>(ws);
   a.tickets = reinterpret_cast<int*>(base);
+  a.next_run = a.tickets + kMaxUnits - 1;
   a.part_st = reinterpret_cast<float4*>(base + kCounterBytes);
   a.part_o = reinterpret_cast<float*>(base + kCounterBytes + align256(kRuns * 2 * N * sizeof(float4)));
   if (c.s.format == MKV_E4M3)
