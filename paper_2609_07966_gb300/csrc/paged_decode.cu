@@ -288,12 +288,6 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         hd.row0 = e.row0;
         const bool whole = c1 - c0 == e.chunks;
         hd.first = hd.place0 = hd.count = hd.mine = hd.pad = 0;
-        if (!whole) {                                      // a run's places: its first piece, and its last
-          hd.first = rs.of(unit0);
-          hd.place0 = 2 * hd.first + (rs.start(hd.first) < unit0 ? 1 : 0);
-          hd.count = rs.of(unit0 + e.chunks - 1) - hd.first + 1;
-          hd.mine = r == hd.first ? hd.place0 : 2 * r;
-        }
         for (int ch = c0; ch < c1; ++ch, ++g) {
           const int in = (ch - c0) % span, from = ch - in;
           if (in == 0 && ch > c0) {
@@ -321,6 +315,12 @@ __global__ void __launch_bounds__(kThreads, kCtas)
             const int y = (ch * kTokens + (lane << log_box)) & (c.s.page - 1), z = id * Hkv + kvh;
             tma_load_4d(dst, &kmap, 0, y, z, 0, &ctl->full[s]);
             tma_load_4d(dst + S::TILE, &vmap, 0, y, z, 0, &ctl->full[s]);
+          }
+          if (ch == c0 && !whole) {                        // a run's places: its first piece, and its last
+            hd.first = rs.of(unit0);
+            hd.place0 = 2 * hd.first + (rs.start(hd.first) < unit0 ? 1 : 0);
+            hd.count = rs.of(unit0 + e.chunks - 1) - hd.first + 1;
+            hd.mine = r == hd.first ? hd.place0 : 2 * r;
           }
           // scales of the chunk's groups of 16 tokens
           const int owner = in * per + group_copy;
@@ -448,6 +448,13 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     uint32_t qf[2 * KS];
     float back[2], o[MB][4], m[2], m2[2], l[2];
     int pos0 = 0, pieces = 0;
+    // where this lane's pieces of a key row and of two value rows lie; further rows are whole swizzle periods away
+    uint32_t kofs[D / 64], vofs[2];
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h) kofs[h] = code_offset<D>(lg, lr * (D / 64) + h);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      vofs[i] = D == 128 ? code_offset<D>(2 * lr + i, lg) : code_offset<D>(2 * lr + i, lg >> 1) + (lg & 1) * 8;
     for (int g = 0;; ++g) {
       const int s = g % S::STAGES;
       wait(&ctl->full[s], (uint32_t)((g / S::STAGES) & 1));
@@ -514,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
             for (int i = 0; i < 2; ++i)
 #pragma unroll
               for (int h = 0; h < D / 64; ++h) {
-                const uint4 y = *reinterpret_cast<const uint4*>(K + code_offset<D>(16 * u + 8 * i + lg, lr * (D / 64) + h));
+                const uint4 y = *reinterpret_cast<const uint4*>(K + kofs[h] + (16 * u + 8 * i) * D);
                 kw[u][i][4 * h] = y.x;
                 kw[u][i][4 * h + 1] = y.y;
                 kw[u][i][4 * h + 2] = y.z;
@@ -536,23 +543,28 @@ __global__ void __launch_bounds__(kThreads, kCtas)
           for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int row = 16 * u + 2 * lr + (i & 1) + 8 * (i >> 1);
+              const uint8_t* src = V + vofs[i & 1] + (16 * u + 8 * (i >> 1)) * D;
               if constexpr (D == 128) {
-                const uint4 y = *reinterpret_cast<const uint4*>(V + code_offset<D>(row, lg));
+                const uint4 y = *reinterpret_cast<const uint4*>(src);
                 v[u][i][0] = y.x;
                 v[u][i][1] = y.y;
                 v[u][i][2] = y.z;
                 v[u][i][3] = y.w;
               } else {
-                const uint2 y = *reinterpret_cast<const uint2*>(V + code_offset<D>(row, lg >> 1) + (lg & 1) * 8);
+                const uint2 y = *reinterpret_cast<const uint2*>(src);
                 v[u][i][0] = y.x;
                 v[u][i][1] = y.y;
               }
-              // (a token that no row may meet must not meet a zero weight as NaN)
-              if (!in[u] || t0 + row >= hd.len)
-#pragma unroll
-                for (int k = 0; k < D / 32; ++k) v[u][i][k] = 0u;
             }
+          if (!in[0] || !in[1] || t0 + 32 > hd.len) {      // (what no row may meet must not meet a zero weight as NaN)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (!in[u] || t0 + 16 * u + 2 * lr + (i & 1) + 8 * (i >> 1) >= hd.len)
+#pragma unroll
+                  for (int k = 0; k < D / 32; ++k) v[u][i][k] = 0u;
+          }
           // -------------------------------------------------------- weights
           bool over = false;
 #pragma unroll
