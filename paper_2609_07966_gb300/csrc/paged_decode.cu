@@ -45,6 +45,7 @@ struct DecodeArgs {
   float scale_log2;
   int box;                          // tokens of a page's copy: min(page, chunk)
   int log_page;
+  int parts;                        // CTAs a unit if each gets as many, or 0: more units than CTAs
   int* tickets;                     // [B][Hkv], zero between calls
   int* next_run;                    // zero between calls
   float* part_o;                    // [kRuns][2][N][D]
@@ -57,13 +58,14 @@ struct DShape {
   static constexpr int TILE = kTokens * D, GROUPS = kTokens / 16;
   static constexpr int KV_OFF = 0;                         // [STAGES][K, V]
   static constexpr int SC_OFF = STAGES * 2 * TILE;         // [STAGES][GROUPS] float4: key factor, mantissa and exponent of vs, seen
-  static constexpr int O_OFF = SC_OFF + STAGES * GROUPS * 16;   // [W - 1][N][D] floats
-  static constexpr int ST_OFF = O_OFF + (W - 1) * N * D * 4;    // [W + 1][N] float4: the warps', the piece's
+  static constexpr int ST_OFF = SC_OFF + STAGES * GROUPS * 16;  // [W + 1][N] float4: the warps', the piece's
   static constexpr int HD_OFF = ST_OFF + (W + 1) * N * 16;      // [STAGES] Head
   static constexpr int Q_OFF = HD_OFF + STAGES * 48;       // [N][D] queries
   static constexpr int CTL_OFF = Q_OFF + N * D * 2;
   static constexpr int ALLOC = CTL_OFF + 256 + 1024;       // slack to align the base to 1024 B
+  static constexpr int OROW = D + 16;                      // floats between rows of the warps' sums
   static_assert(kCtas * (ALLOC + 1024) <= 228 * 1024, "shared memory");
+  static_assert(W * N * OROW * 4 <= 2 * TILE, "room for the warps' sums in a stage");
 };
 
 struct DecodeCtl {
@@ -173,10 +175,17 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
     }
     total += upto32;
-    const Runs rs(total);
+    // Entries of one length (and of few chunks): the same parts of every unit, so that no CTA has pieces of two.
+    const int chunks0 = __shfl_sync(0xffffffffu, held.chunks, 0);
+    const bool even = B <= 32 && a.parts > 0 && total < kGrid * kLongRun &&
+                      __all_sync(0xffffffffu, lane >= B || held.chunks == chunks0);
+    const int part = even ? (chunks0 + a.parts - 1) / a.parts : 0;       // chunks of each
+    Runs rs(total);
+    if (even) rs.runs = B * Hkv * a.parts;
     // A batch is 32 copies' pages, a lane each: page and scales of the next batch are fetched during this one.
-    const int per = kTokens / a.box, span = 32 / per;       // copies a chunk, chunks a batch
-    const int log_box = __ffs(a.box) - 1, group_copy = lane < S::GROUPS ? lane >> (log_box - 4) : 0;
+    const int log_box = __ffs(a.box) - 1, log_per = __ffs(kTokens) - 1 - log_box, log_span = 5 - log_per;
+    const int per = 1 << log_per, span = 1 << log_span;    // copies a chunk, chunks a batch
+    const int group_copy = lane < S::GROUPS ? lane >> (log_box - 4) : 0;
     int g = 0, pieces = 0;
     bool ok = true;
     // the next stage, once it is free
@@ -197,11 +206,15 @@ __global__ void __launch_bounds__(kThreads, kCtas)
           if (old == rs.runs - 1) *a.next_run = 0;         // (every CTA takes one too many: that was the last of all)
         }
       }
-      int cur = rs.start(r);
-      const int end = rs.start(r + 1);
-      // the entry that holds the run's first chunk, and that entry's first chunk
-      int b = 0, base = 0;
-      if (cur < upto32) {
+      // the run's chunks, the entry that holds the first of them, and that entry's first chunk
+      int b = 0, base = 0, cur = rs.start(r), end = rs.start(r + 1);
+      if (even) {
+        const int unit = r / a.parts, first = (r - unit * a.parts) * part;
+        cur = unit * chunks0 + min(first, chunks0);
+        end = unit * chunks0 + min(first + part, chunks0);
+        b = unit / Hkv;
+        base = b * Hkv * chunks0;
+      } else if (cur < upto32) {
         b = __ffs(__ballot_sync(0xffffffffu, upto > cur)) - 1;
         base = __shfl_sync(0xffffffffu, upto - held.chunks * Hkv, b);
       } else {
@@ -245,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         cur += c1 - c0;
         const int32_t* table = c.s.page_table + (int64_t)b * c.s.max_pages;
         auto exists = [&](int chunk) {                     // this lane's copy of the batch from `chunk` on
-          return chunk + lane / per < c1 && chunk * kTokens + (lane << log_box) < e.len;
+          return chunk + (lane >> log_per) < c1 && chunk * kTokens + (lane << log_box) < e.len;
         };
         auto fetch = [&](int chunk) {
           return exists(chunk) ? table[(chunk * kTokens + (lane << log_box)) >> a.log_page] : -1;
@@ -289,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         const bool whole = c1 - c0 == e.chunks;
         hd.first = hd.place0 = hd.count = hd.mine = hd.pad = 0;
         for (int ch = c0; ch < c1; ++ch, ++g) {
-          const int in = (ch - c0) % span, from = ch - in;
+          const int in = (ch - c0) & (span - 1), from = ch - in;
           if (in == 0 && ch > c0) {
             pid = next;
             ks = nks;
@@ -302,7 +315,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
           }
           const int s = stage();
           if (!ok) break;
-          const int id = __shfl_sync(0xffffffffu, pid, (in * per + lane) & 31);
+          const int id = __shfl_sync(0xffffffffu, pid, ((in << log_per) + lane) & 31);
           const bool copy = lane < per && id >= 0;
           const int copies = __popc(__ballot_sync(0xffffffffu, copy));
           if (lane == 0) {
@@ -317,13 +330,19 @@ __global__ void __launch_bounds__(kThreads, kCtas)
             tma_load_4d(dst + S::TILE, &vmap, 0, y, z, 0, &ctl->full[s]);
           }
           if (ch == c0 && !whole) {                        // a run's places: its first piece, and its last
-            hd.first = rs.of(unit0);
-            hd.place0 = 2 * hd.first + (rs.start(hd.first) < unit0 ? 1 : 0);
-            hd.count = rs.of(unit0 + e.chunks - 1) - hd.first + 1;
+            if (even) {
+              hd.first = (b * Hkv + kvh) * a.parts;
+              hd.place0 = 2 * hd.first;
+              hd.count = (chunks0 + part - 1) / part;
+            } else {
+              hd.first = rs.of(unit0);
+              hd.place0 = 2 * hd.first + (rs.start(hd.first) < unit0 ? 1 : 0);
+              hd.count = rs.of(unit0 + e.chunks - 1) - hd.first + 1;
+            }
             hd.mine = r == hd.first ? hd.place0 : 2 * r;
           }
           // scales of the chunk's groups of 16 tokens
-          const int owner = in * per + group_copy;
+          const int owner = (in << log_per) + group_copy;
           const float gk = __shfl_sync(0xffffffffu, ks, owner), gv = __shfl_sync(0xffffffffu, vs, owner);
           const int gid = __shfl_sync(0xffffffffu, pid, owner);
           if (lane < S::GROUPS) {
@@ -352,7 +371,6 @@ __global__ void __launch_bounds__(kThreads, kCtas)
   } else {
     // ---------------------------------------------------------------- attention
     const int lg = lane >> 2, lr = lane & 3;
-    float* ob = reinterpret_cast<float*>(sm + S::O_OFF);
     float4* stat = reinterpret_cast<float4*>(sm + S::ST_OFF);
     const bool bf16 = c.s.dtype == MKV_BF16;
     const int G = a.G;
@@ -634,11 +652,12 @@ __global__ void __launch_bounds__(kThreads, kCtas)
               }
         }
         __syncwarp();
-        if (lane == 0) tc_mbar_arrive(&ctl->empty[s]);
+        if (lane == 0 && !(hd.flags & kLast)) tc_mbar_arrive(&ctl->empty[s]);
       }
       if (!(hd.flags & kLast)) continue;
       settle();                                            // (the piece before this one's unit)
       // ------------------------------------------------------------ the warps' parts joined, in their order
+      // (As few instructions as will do: code that runs once a piece comes from a cold instruction cache.)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         float t = l[j];
@@ -648,7 +667,9 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       }
       meet();
       if (dead) break;
-      float M[2], M2[2], L[2];
+      // The last chunk's stage, which no warp reads any more, takes the warps' sums: [W][N] rows, the dims that a lane holds
+      // of each two 16 floats apart (lanes of a row then store 64 neighbouring bytes).
+      float* ob = reinterpret_cast<float*>(sm + S::KV_OFF + s * 2 * S::TILE);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const float4* x = stat + 2 * lr + j;
@@ -660,62 +681,47 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         }
 #pragma unroll
         for (int w = 0; w < W; ++w) sum += x[w * N].y * ex2_approx(x[w * N].x - mx);
-        M[j] = mx;
-        M2[j] = mx2;
-        L[j] = sum;
         const float f = ex2_approx(m2[j] - mx2);
+        if (warp == 0 && lg == 0) stat[W * N + 2 * lr + j] = make_float4(mx, sum, mx2, 0.f);
+        float* y = ob + (warp * N + 2 * lr + j) * S::OROW + 2 * lg;
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb) {
-          o[mb][j] *= f;
-          o[mb][2 + j] *= f;
-          if (warp > 0)
-            *reinterpret_cast<float2*>(ob + ((warp - 1) * N + 2 * lr + j) * D + (D / 8) * lg + 2 * mb) =
-                make_float2(o[mb][j], o[mb][2 + j]);
-        }
-      }
-      meet();
-      if (dead) break;
-      if (warp == 0) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-#pragma unroll
-          for (int mb = 0; mb < MB; ++mb) {
-            float2* x = reinterpret_cast<float2*>(ob + (2 * lr + j) * D + (D / 8) * lg + 2 * mb);
-            float2 y = make_float2(o[mb][j], o[mb][2 + j]);
-#pragma unroll
-            for (int w = 0; w < W - 1; ++w) {
-              y.x += x[w * N * D / 2].x;
-              y.y += x[w * N * D / 2].y;
-            }
-            *x = y;
-          }
-          if (lg == 0) stat[W * N + 2 * lr + j] = make_float4(M[j], L[j], M2[j], 0.f);
-        }
+        for (int mb = 0; mb < MB; ++mb)
+          *reinterpret_cast<float2*>(y + 16 * mb) = make_float2(o[mb][j] * f, o[mb][2 + j] * f);
       }
       meet();
       if (dead) break;
       // ------------------------------------------------------------ outputs, or a piece for the unit's last CTA
       const int R = hd.tokens * G;
-      constexpr int V4 = D / 4;
-      if (hd.flags & kWhole) {
-        for (int e = threadIdx.x; e < R * V4; e += kComputing) {
-          const int row = e / V4, d = e % V4 * 4;
-          const float4 st = stat[W * N + row];
-          *reinterpret_cast<uint2*>(out_row(hd, row) + d) =
-              finish(hd, row, *reinterpret_cast<const float4*>(ob + row * D + d), st.x, st.y, st.z);
+      const bool whole = hd.flags & kWhole;
+      const int64_t mine = (int64_t)hd.mine * N;
+#pragma unroll 1
+      for (int e = threadIdx.x; e < R * (D / 4); e += kComputing) {
+        const int row = e / (D / 4), d = e % (D / 4) * 4;
+        const float* y = ob + row * S::OROW + d / (D / 8) * 2 + d % (D / 8) * 8;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          const float2 y0 = *reinterpret_cast<const float2*>(y + w * N * S::OROW);
+          const float2 y1 = *reinterpret_cast<const float2*>(y + w * N * S::OROW + 16);
+          x = make_float4(x.x + y0.x, x.y + y0.y, x.z + y1.x, x.w + y1.y);
         }
-      } else {
-        const int64_t mine = (int64_t)hd.mine * N;
-        for (int e = threadIdx.x; e < R * V4; e += kComputing)
-          __stcg(reinterpret_cast<float4*>(a.part_o + mine * D) + e, reinterpret_cast<const float4*>(ob)[e]);
-        if (threadIdx.x < R) __stcg(a.part_st + mine + threadIdx.x, stat[W * N + threadIdx.x]);
-        meet();
-        if (dead) break;
+        const float4 st = stat[W * N + row];
+        if (whole) {
+          *reinterpret_cast<uint2*>(out_row(hd, row) + d) = finish(hd, row, x, st.x, st.y, st.z);
+        } else {
+          __stcg(reinterpret_cast<float4*>(a.part_o + (mine + row) * D + d), x);
+          if (d == 0) __stcg(a.part_st + mine + row, st);
+        }
+      }
+      fence_async_smem();                                  // (before the stage is loaded again)
+      meet();
+      if (dead) break;
+      if (lane == 0) tc_mbar_arrive(&ctl->empty[s]);
+      if (!whole) {
         if (threadIdx.x == 0)
           asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(ticket) : "l"(a.tickets + hd.unit) : "memory");
         owed = hd;
       }
-      // (`ob` and the piece's statistics are written again only behind the next piece's first barrier)
     }
     settle();
   }
@@ -759,6 +765,7 @@ cudaError_t launch_paged_decode(const PagedAttnCall& c, void* ws, cudaStream_t s
   if (e != cudaSuccess) return e;
   a.c = c;
   a.G = c.s.Hq / c.s.Hkv;
+  a.parts = kGrid / (c.s.B * c.s.Hkv);
   for (a.log_page = 0; (1 << a.log_page) < c.s.page;) ++a.log_page;
   a.scale_log2 = c.scale * kLog2e;
   uint8_t* base = static_cast<uint8_t*>(ws);
