@@ -64,8 +64,8 @@ mkv_status check_paged(const mkv_paged_config* c) {
   MKV_REQUIRE(c->format == MKV_E4M3 || c->format == MKV_I8, MKV_ERR_INVALID_ARG, "unknown code format %d", c->format);
   MKV_REQUIRE(c->B >= 1 && c->Hq >= 1 && c->Hkv >= 1, MKV_ERR_INVALID_ARG, "B, Hq and Hkv must be positive");
   MKV_REQUIRE(c->Hq % c->Hkv == 0, MKV_ERR_INVALID_ARG, "Hq = %d not a multiple of Hkv = %d", c->Hq, c->Hkv);
-  MKV_REQUIRE((int64_t)c->B * c->Hkv < kMaxUnits, MKV_ERR_UNSUPPORTED, "B * Hkv = %lld above %d",
-              (long long)c->B * c->Hkv, kMaxUnits - 1);
+  MKV_REQUIRE((int64_t)c->B * c->Hkv <= kMaxUnits, MKV_ERR_UNSUPPORTED, "B * Hkv = %lld above %d",
+              (long long)c->B * c->Hkv, kMaxUnits);
   MKV_REQUIRE(c->Hq / c->Hkv <= 32, MKV_ERR_UNSUPPORTED, "%d query heads a key head, above 32", c->Hq / c->Hkv);
   MKV_REQUIRE(c->D == 64 || c->D == 128, MKV_ERR_UNSUPPORTED, "D = %d not built", c->D);
   MKV_REQUIRE(c->page_size == 16 || c->page_size == 32 || c->page_size == 64 || c->page_size == 128,

@@ -14,8 +14,9 @@
 // and accumulators are fp32.
 //
 // Work: the chunks of all (entry, key head) units end to end, cut into equal runs whatever the entries' lengths (read on the
-// device); a CTA takes one, or several in turn.  Pieces of a unit that several runs share go to the workspace, and the CTA
-// whose piece is the last to arrive adds them up in their order.  One warp finds out the work and loads it by TMA, a page
+// device).  Pieces of a unit that several runs share go to the workspace, and the CTA whose piece is the last to arrive adds
+// them up in their order.  (Four times as many runs, taken in turn, even out what SMs get of HBM's bandwidth, but starting a
+// piece costs more: 16 x 17-32K 146 against 130 us.)  One warp finds out the work and loads it by TMA, a page
 // (or its part of the chunk) a copy; what the other warps have to know of a chunk comes with it.
 #include <math.h>
 
@@ -33,10 +34,9 @@ constexpr int kTokens = 32 * W;     // of a chunk
 constexpr int kComputing = 32 * W, kThreads = kComputing + 32;
 constexpr int kCtas = 2;            // of them an SM
 constexpr int kGrid = kCtas * kNumSMs;
-// Long runs are cut into four each, which the CTAs take in turn as they get done: SMs differ by a tenth in what they get of
-// HBM's bandwidth.
-constexpr int kTurns = 4, kLongRun = 32;
-constexpr size_t kRuns = kGrid * kTurns;
+// Up to this many chunks a CTA, equal parts of every unit where entries are equally long; beyond it a CTA's few pieces cost
+// less than the SMs that such a cut leaves without work.
+constexpr int kLongRun = 32;
 
 struct DecodeArgs {
   PagedAttnCall c;
@@ -47,9 +47,8 @@ struct DecodeArgs {
   int log_page;
   int parts;                        // CTAs a unit if each gets as many, or 0: more units than CTAs
   int* tickets;                     // [B][Hkv], zero between calls
-  int* next_run;                    // zero between calls
-  float* part_o;                    // [kRuns][2][N][D]
-  float4* part_st;                  // [kRuns][2][N]: m, sum, m2
+  float* part_o;                    // [kGrid][2][N][D]
+  float4* part_st;                  // [kGrid][2][N]: m, sum, m2
 };
 
 template <int FMT_, int D_>
@@ -111,7 +110,6 @@ struct Runs {
   int runs, len, longer;
   __device__ __forceinline__ explicit Runs(int total) {
     runs = min(total, kGrid);
-    if (total >= kGrid * kLongRun) runs = kGrid * kTurns;
     len = runs > 0 ? total / runs : 0;
     longer = total - len * runs;
   }
@@ -195,17 +193,8 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         ok = __all_sync(0xffffffffu, wait_or_fail(&ctl->empty[s], (uint32_t)((g / S::STAGES - 1) & 1), fail, status));
       return s;
     };
-    int r = blockIdx.x;
-    while (ok && r < rs.runs) {
-      // the run after this one, of those that the CTAs take in turn
-      int next_run = rs.runs;
-      if (rs.runs > kGrid) {
-        if (lane == 0) {
-          const int old = atomicAdd(a.next_run, 1);
-          next_run = kGrid + old;
-          if (old == rs.runs - 1) *a.next_run = 0;         // (every CTA takes one too many: that was the last of all)
-        }
-      }
+    const int r = blockIdx.x;
+    if (r < rs.runs) {
       // the run's chunks, the entry that holds the first of them, and that entry's first chunk
       int b = 0, base = 0, cur = rs.start(r), end = rs.start(r + 1);
       if (even) {
@@ -358,7 +347,6 @@ __global__ void __launch_bounds__(kThreads, kCtas)
           if (lane == 0) tc_mbar_arrive(&ctl->full[s]);
         }
       }
-      r = __shfl_sync(0xffffffffu, next_run, 0);
     }
     if (ok) {
       const int s = stage();
@@ -756,7 +744,7 @@ bool paged_decode_countable(const PagedAttnCall& c) {
 }
 
 size_t paged_decode_ws_bytes(const PagedAttnCall& c) {
-  return kCounterBytes + align256(kRuns * 2 * N * sizeof(float4)) + align256((size_t)kRuns * 2 * N * c.s.D * sizeof(float));
+  return kCounterBytes + align256((size_t)kGrid * 2 * N * sizeof(float4)) + align256((size_t)kGrid * 2 * N * c.s.D * sizeof(float));
 }
 
 cudaError_t launch_paged_decode(const PagedAttnCall& c, void* ws, cudaStream_t st) {
@@ -770,9 +758,8 @@ cudaError_t launch_paged_decode(const PagedAttnCall& c, void* ws, cudaStream_t s
   a.scale_log2 = c.scale * kLog2e;
   uint8_t* base = static_cast<uint8_t*>(ws);
   a.tickets = reinterpret_cast<int*>(base);
-  a.next_run = a.tickets + kMaxUnits - 1;
   a.part_st = reinterpret_cast<float4*>(base + kCounterBytes);
-  a.part_o = reinterpret_cast<float*>(base + kCounterBytes + align256(kRuns * 2 * N * sizeof(float4)));
+  a.part_o = reinterpret_cast<float*>(base + kCounterBytes + align256((size_t)kGrid * 2 * N * sizeof(float4)));
   if (c.s.format == MKV_E4M3)
     return c.s.D == 128 ? launch_shape<DShape<MKV_E4M3, 128>>(c, a, st) : launch_shape<DShape<MKV_E4M3, 64>>(c, a, st);
   return c.s.D == 128 ? launch_shape<DShape<MKV_I8, 128>>(c, a, st) : launch_shape<DShape<MKV_I8, 64>>(c, a, st);
