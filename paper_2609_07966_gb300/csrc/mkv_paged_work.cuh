@@ -1,0 +1,283 @@
+// Which chunks of 128 tokens a CTA of the paged attention kernels takes, found out by the warp that loads them.
+//
+// The chunks of all (entry, key head) units lie end to end and are cut into runs of one length, one a CTA, whatever the
+// entries' lengths (which are read on the device).  A run's chunks of one unit are a piece; pieces of a unit that several
+// runs share are added up by the CTA whose piece arrives last.  The other warps get what they have to know with each chunk.
+#pragma once
+
+#include "mkv_paged.cuh"
+
+namespace mkv {
+
+constexpr int kTokens = 128;        // of a chunk
+constexpr int kGroups = kTokens / 16;
+
+// Up to this many chunks a CTA, equal parts of every unit where entries are equally long; beyond it a CTA's few pieces cost
+// less than the SMs that such a cut leaves without work.
+constexpr int kLongRun = 32;
+
+struct WorkArgs {
+  int log_page, log_box;            // a copy's tokens: a page's, a chunk's at most
+  int parts;                        // CTAs a unit if each gets as many; 0: not to be done
+  int grid;
+  float scale_log2;
+};
+// (equal parts that leave more than a fifth of the CTAs without work are not worth it)
+inline WorkArgs work_args(const PagedAttnCall& c, int grid) {
+  WorkArgs w{};
+  while ((1 << w.log_page) < c.s.page) ++w.log_page;
+  w.log_box = w.log_page;           // (pages are of 16 to 128 tokens)
+  const int units = c.s.B * c.s.Hkv, parts = grid / units;
+  w.parts = parts * units * 5 >= grid * 4 ? parts : 0;
+  w.grid = grid;
+  w.scale_log2 = c.scale * kLog2e;
+  return w;
+}
+
+enum { kFirst = 1, kLast = 2, kWhole = 4, kEnd = 8 };     // of a piece; the piece is the whole unit; nothing comes any more
+struct Head {
+  int flags, chunk, len, tokens;   // tokens: the entry's new ones
+  int unit, kvh, row0, mine;       // mine: this piece's place
+  int first, place0, count, seen;  // the unit's pieces: the run of the first, its place, how many there are; seen: a bit for
+                                   // each 16 tokens of the chunk that are there
+  // place of the unit's piece i: runs have two, for their first piece and for their last
+  __device__ __forceinline__ int place(int i) const { return i == 0 ? place0 : 2 * (first + i); }
+};
+static_assert(sizeof(Head) == 48, "three 16-byte accesses");
+
+struct Entry {
+  int row0, tokens, len, chunks;   // its first row, new tokens, tokens held, chunks of a unit
+};
+__device__ __forceinline__ Entry entry_of(const PagedAttnCall& c, const WorkArgs& w, int b, uint32_t* report) {
+  const EntryRows r = entry_rows(c.s, b);
+  Entry e;
+  e.row0 = (int)r.first;
+  e.tokens = (int)min(r.count, c.max_rows + 1);
+  e.len = (int)min((int64_t)max(c.T_len[b], 0), c.s.max_pages << w.log_page);
+  if (e.tokens > c.max_rows) {
+    if (report != nullptr) atomicOr(report, MKV_FLAG_BAD_INDEX);
+    e.tokens = 0;
+  }
+  e.chunks = e.tokens > 0 ? max(1, (e.len + kTokens - 1) / kTokens) : 0;
+  return e;
+}
+
+// `total` chunks in `runs` runs, the first total % runs of them one longer.
+struct Runs {
+  int runs, len, longer;
+  __device__ __forceinline__ Runs(int total, int grid) {
+    runs = min(total, grid);
+    len = runs > 0 ? total / runs : 0;
+    longer = total - len * runs;
+  }
+  __device__ __forceinline__ int start(int i) const { return i * len + min(i, longer); }
+  __device__ __forceinline__ int of(int chunk) const {    // the run that holds a chunk
+    const int split = longer * (len + 1);
+    return chunk < split ? chunk / (len + 1) : longer + (chunk - split) / len;
+  }
+};
+
+// A whole warp goes through this CTA's chunks.  For each piece it calls piece(head), for each chunk
+//   copies(head, id)   id: page of copy `lane` of the chunk (those of the tokens 2^log_box lane ..), -1 where there is none
+//   publish(head, sc)  sc (lane < kGroups): key factor, value scale as mantissa and exponent, of tokens 16 lane ..
+// which say whether to go on; whether all went through.
+template <typename Piece, typename Copies, typename Publish>
+__device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkArgs& w, uint32_t* status, int lane,
+                                             Piece piece, Copies copies, Publish publish) {
+  const int B = c.s.B, Hkv = c.s.Hkv;
+  uint32_t* report = blockIdx.x == 0 ? status : nullptr;
+  Entry held = {0, 0, 0, 0};                               // of entry `lane`
+  if (lane < B) held = entry_of(c, w, lane, report);
+  int upto = held.chunks * Hkv, total = 0;                 // inclusive prefix within the first 32 entries
+  for (int b = lane + 32; b < B; b += 32) total += entry_of(c, w, b, report).chunks * Hkv;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, upto, d);
+    if (lane >= d) upto += x;
+  }
+  const int upto32 = __shfl_sync(0xffffffffu, upto, 31);
+  if (B > 32) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+  }
+  total += upto32;
+  // Entries of one length (and of few chunks): the same parts of every unit, so that no CTA has pieces of two.
+  const int chunks0 = __shfl_sync(0xffffffffu, held.chunks, 0);
+  const bool even = B <= 32 && w.parts > 0 && total < w.grid * kLongRun &&
+                    __all_sync(0xffffffffu, lane >= B || held.chunks == chunks0);
+  const int part = even ? (chunks0 + w.parts - 1) / w.parts : 0;         // chunks of each
+  Runs rs(total, w.grid);
+  if (even) rs.runs = B * Hkv * w.parts;
+  const int r = blockIdx.x;
+  if (r >= rs.runs) return true;
+  // the run's chunks, the entry that holds the first of them, and that entry's first chunk
+  int b = 0, base = 0, cur = rs.start(r), end = rs.start(r + 1);
+  if (even) {
+    const int unit = r / w.parts, first = (r - unit * w.parts) * part;
+    cur = unit * chunks0 + min(first, chunks0);
+    end = unit * chunks0 + min(first + part, chunks0);
+    b = unit / Hkv;
+    base = b * Hkv * chunks0;
+  } else if (cur < upto32) {
+    b = __ffs(__ballot_sync(0xffffffffu, upto > cur)) - 1;
+    base = __shfl_sync(0xffffffffu, upto - held.chunks * Hkv, b);
+  } else {
+    base = upto32;
+    for (int b0 = 32;; b0 += 32) {
+      const int mine = b0 + lane < B ? entry_of(c, w, b0 + lane, nullptr).chunks * Hkv : 0;
+      int in = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, in, d);
+        if (lane >= d) in += x;
+      }
+      const unsigned past = __ballot_sync(0xffffffffu, base + in > cur);
+      if (past || b0 + 32 >= B) {
+        const int l = past ? __ffs(past) - 1 : 0;
+        b = b0 + l;
+        base += __shfl_sync(0xffffffffu, in - mine, l);
+        break;
+      }
+      base += __shfl_sync(0xffffffffu, in, 31);
+    }
+  }
+  auto entry = [&](int i) {
+    if (i >= 32) return entry_of(c, w, i, nullptr);
+    Entry e;
+    e.row0 = __shfl_sync(0xffffffffu, held.row0, i);
+    e.tokens = __shfl_sync(0xffffffffu, held.tokens, i);
+    e.len = __shfl_sync(0xffffffffu, held.len, i);
+    e.chunks = __shfl_sync(0xffffffffu, held.chunks, i);
+    return e;
+  };
+  // A batch is 32 copies' pages, a lane each: page and scales of the next batch are fetched during this one.
+  const int log_per = 7 - w.log_box, span = 32 >> log_per; // copies a chunk, chunks a batch
+  const int group_copy = lane < kGroups ? lane >> (w.log_box - 4) : 0;
+  Entry e = entry(b);
+  while (cur < end) {
+    while (cur >= base + e.chunks * Hkv) {
+      base += e.chunks * Hkv;
+      e = entry(++b);
+    }
+    const int kvh = (cur - base) / e.chunks, unit0 = base + kvh * e.chunks;
+    const int c0 = cur - unit0, c1 = min(e.chunks, c0 + (end - cur));
+    cur += c1 - c0;
+    const int32_t* table = c.s.page_table + (int64_t)b * c.s.max_pages;
+    auto exists = [&](int chunk) {                         // this lane's copy of the batch from `chunk` on
+      return chunk + (lane >> log_per) < c1 && chunk * kTokens + (lane << w.log_box) < e.len;
+    };
+    auto fetch = [&](int chunk) {
+      return exists(chunk) ? table[(chunk * kTokens + (lane << w.log_box)) >> w.log_page] : -1;
+    };
+    auto check = [&](int chunk, int id) {                  // (a page outside the pool is not seen)
+      if (!exists(chunk)) return -1;
+      if (id >= 0 && id < c.s.num_pages) return id;
+      atomicOr(status, MKV_FLAG_BAD_INDEX);
+      return -1;
+    };
+    auto scales = [&](int id, float& ks, float& vs) {
+      ks = 0.f;
+      vs = 1.f;
+      if (id >= 0) {
+        ks = c.k_scale[(int64_t)id * Hkv + kvh];
+        vs = c.v_scale[(int64_t)id * Hkv + kvh];
+      }
+    };
+    int pid = fetch(c0), next = 0;
+    const bool whole = c1 - c0 == e.chunks;
+    Head hd;
+    hd.len = e.len;
+    hd.tokens = e.tokens;
+    hd.unit = b * Hkv + kvh;
+    hd.kvh = kvh;
+    hd.row0 = e.row0;
+    hd.first = hd.place0 = hd.count = hd.mine = 0;
+    if (!piece(hd)) return false;
+    pid = check(c0, pid);
+    float ks, vs, nks = 0.f, nvs = 1.f;
+    scales(pid, ks, vs);
+    for (int ch = c0; ch < c1; ++ch) {
+      const int in = (ch - c0) & (span - 1);
+      if (in == 0 && ch > c0) {
+        pid = next;
+        ks = nks;
+        vs = nvs;
+      }
+      if (in == 0) next = fetch(ch + span);
+      if (in == span / 2) {
+        next = check(ch - in + span, next);
+        scales(next, nks, nvs);
+      }
+      hd.flags = (ch == c0 ? kFirst : 0) | (ch == c1 - 1 ? kLast : 0) | (whole ? kWhole : 0);
+      hd.chunk = ch;
+      const int id = __shfl_sync(0xffffffffu, pid, ((in << log_per) + lane) & 31);
+      if (!copies(hd, lane < (1 << log_per) ? id : -1)) return false;
+      if (ch == c0 && !whole) {
+        if (even) {
+          hd.first = hd.unit * w.parts;
+          hd.place0 = 2 * hd.first;
+          hd.count = (chunks0 + part - 1) / part;
+        } else {
+          hd.first = rs.of(unit0);
+          hd.place0 = 2 * hd.first + (rs.start(hd.first) < unit0 ? 1 : 0);
+          hd.count = rs.of(unit0 + e.chunks - 1) - hd.first + 1;
+        }
+        hd.mine = r == hd.first ? hd.place0 : 2 * r;
+      }
+      const int owner = (in << log_per) + group_copy;
+      const float gk = __shfl_sync(0xffffffffu, ks, owner), gv = __shfl_sync(0xffffffffu, vs, owner);
+      const int gid = __shfl_sync(0xffffffffu, pid, owner);
+      hd.seen = (int)__ballot_sync(0xffffffffu, lane < kGroups && gid >= 0);
+      int x;
+      const float mant = frexpf(gv, &x);
+      publish(hd, make_float4(gk * w.scale_log2, mant, (float)x, gid >= 0 ? 1.f : 0.f));
+    }
+  }
+  return true;
+}
+
+// The pieces' sums of one row, added up in the pieces' order: out = sum_i 2^(m2_i - M2) o_i, with M, sum and M2 of all.
+// VL neighbouring dims a lane; part_o [place][rows][32 VL], part_st [place][rows].
+template <int VL>
+__device__ __forceinline__ float4 add_pieces(const Head& hd, const float* part_o, const float4* part_st, int rows, int row,
+                                             int lane, float& mx, float& sum, float& mx2) {
+  mx = mx2 = kNoMax;
+  sum = 0.f;
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = 0; i0 < hd.count; i0 += 8) {               // eight pieces' loads under way together
+    float4 st[8], z[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int64_t at = (int64_t)hd.place(min(i0 + k, hd.count - 1)) * rows + row;
+      st[k] = __ldcg(part_st + at);
+      const float* po = part_o + at * (32 * VL) + lane * VL;
+      if constexpr (VL == 4) {
+        z[k] = __ldcg(reinterpret_cast<const float4*>(po));
+      } else {
+        const float2 f = __ldcg(reinterpret_cast<const float2*>(po));
+        z[k] = make_float4(f.x, f.y, 0.f, 0.f);
+      }
+      if (i0 + k >= hd.count) st[k] = make_float4(kNoMax, 0.f, kNoMax, 0.f);
+    }
+    float nm = mx, nm2 = mx2;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      nm = fmaxf(nm, st[k].x);
+      nm2 = fmaxf(nm2, st[k].z);
+    }
+    sum *= ex2_approx(mx - nm);
+    const float back = ex2_approx(mx2 - nm2);
+    y = make_float4(y.x * back, y.y * back, y.z * back, y.w * back);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float f = i0 + k < hd.count ? ex2_approx(st[k].z - nm2) : 0.f;
+      sum += st[k].y * ex2_approx(st[k].x - nm);
+      y = make_float4(y.x + f * z[k].x, y.y + f * z[k].y, y.z + f * z[k].z, y.w + f * z[k].w);
+    }
+    mx = nm;
+    mx2 = nm2;
+  }
+  return y;
+}
+
+}  // namespace mkv

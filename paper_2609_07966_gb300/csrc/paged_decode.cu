@@ -13,16 +13,14 @@
 // whole 16-byte pieces of its rows.  Queries are fp16 in registers (bf16 ones scaled by a power of two a row).  Statistics
 // and accumulators are fp32.
 //
-// Work: the chunks of all (entry, key head) units end to end, cut into equal runs whatever the entries' lengths (read on the
-// device).  Pieces of a unit that several runs share go to the workspace, and the CTA whose piece is the last to arrive adds
-// them up in their order.  (Four times as many runs, taken in turn, even out what SMs get of HBM's bandwidth, but starting a
-// piece costs more: 16 x 17-32K 146 against 130 us.)  One warp finds out the work and loads it by TMA, a page
-// (or its part of the chunk) a copy; what the other warps have to know of a chunk comes with it.
+// Work is shared out in runs of chunks (mkv_paged_work.cuh); one warp finds out its CTA's and loads it by TMA, a page a copy.
+// A unit's pieces go to the workspace, and the CTA whose piece arrives last adds them up.  (Four times as many runs, taken in
+// turn, even out what SMs get of HBM's bandwidth, but starting a piece costs more: 16 x 17-32K 146 against 130 us.)
 #include <math.h>
 
 #include <algorithm>
 
-#include "mkv_paged.cuh"
+#include "mkv_paged_work.cuh"
 
 namespace mkv {
 
@@ -30,22 +28,15 @@ namespace {
 
 constexpr int N = 8;                // rows
 constexpr int W = 4;                // warps that compute
-constexpr int kTokens = 32 * W;     // of a chunk
+static_assert(kTokens == 32 * W, "32 tokens of a chunk a warp");
 constexpr int kComputing = 32 * W, kThreads = kComputing + 32;
 constexpr int kCtas = 2;            // of them an SM
 constexpr int kGrid = kCtas * kNumSMs;
-// Up to this many chunks a CTA, equal parts of every unit where entries are equally long; beyond it a CTA's few pieces cost
-// less than the SMs that such a cut leaves without work.
-constexpr int kLongRun = 32;
-
 struct DecodeArgs {
   PagedAttnCall c;
   uint32_t* status;
   int G;
-  float scale_log2;
-  int box;                          // tokens of a page's copy: min(page, chunk)
-  int log_page;
-  int parts;                        // CTAs a unit if each gets as many, or 0: more units than CTAs
+  WorkArgs w;
   int* tickets;                     // [B][Hkv], zero between calls
   float* part_o;                    // [kGrid][2][N][D]
   float4* part_st;                  // [kGrid][2][N]: m, sum, m2
@@ -54,7 +45,7 @@ struct DecodeArgs {
 template <int FMT_, int D_>
 struct DShape {
   static constexpr int FMT = FMT_, D = D_, STAGES = D == 128 ? 3 : 6;
-  static constexpr int TILE = kTokens * D, GROUPS = kTokens / 16;
+  static constexpr int TILE = kTokens * D, GROUPS = kGroups;
   static constexpr int KV_OFF = 0;                         // [STAGES][K, V]
   static constexpr int SC_OFF = STAGES * 2 * TILE;         // [STAGES][GROUPS] float4: key factor, mantissa and exponent of vs, seen
   static constexpr int ST_OFF = SC_OFF + STAGES * GROUPS * 16;  // [W + 1][N] float4: the warps', the piece's
@@ -73,52 +64,11 @@ struct DecodeCtl {
 };
 static_assert(sizeof(DecodeCtl) <= 256, "control block");
 
-// What comes with a chunk.
-enum { kFirst = 1, kLast = 2, kWhole = 4, kEnd = 8 };     // of a piece; the piece is the whole unit; nothing comes any more
-struct Head {
-  int flags, chunk, len, tokens;   // tokens: the entry's new ones
-  int unit, kvh, row0, mine;       // mine: this piece's place
-  int first, place0, count, pad;   // the unit's pieces: the run of the first, its place; how many there are
-};
-static_assert(sizeof(Head) == 48, "three 16-byte accesses");
-
 // Byte offset of 16-byte piece c of row r of a tile as TMA writes it (rows of 128 or 64 bytes, that swizzle).
 template <int D>
 __device__ __forceinline__ uint32_t code_offset(int r, int c) {
   return mn_offset<D / 2>(r, c);
 }
-
-struct Entry {
-  int row0, tokens, len, chunks;   // its first row, new tokens, tokens held, chunks of a unit
-};
-__device__ __forceinline__ Entry entry_of(const DecodeArgs& a, int b, bool report) {
-  const EntryRows r = entry_rows(a.c.s, b);
-  Entry e;
-  e.row0 = (int)r.first;
-  e.tokens = (int)min(r.count, a.c.max_rows + 1);
-  e.len = (int)min((int64_t)max(a.c.T_len[b], 0), a.c.s.max_pages << a.log_page);
-  if (e.tokens > a.c.max_rows) {
-    if (report) atomicOr(a.status, MKV_FLAG_BAD_INDEX);
-    e.tokens = 0;
-  }
-  e.chunks = e.tokens > 0 ? max(1, (e.len + kTokens - 1) / kTokens) : 0;
-  return e;
-}
-
-// `total` chunks in `runs` runs, the first total % runs of them one longer.
-struct Runs {
-  int runs, len, longer;
-  __device__ __forceinline__ explicit Runs(int total) {
-    runs = min(total, kGrid);
-    len = runs > 0 ? total / runs : 0;
-    longer = total - len * runs;
-  }
-  __device__ __forceinline__ int start(int i) const { return i * len + min(i, longer); }
-  __device__ __forceinline__ int of(int chunk) const {    // the run that holds a chunk
-    const int split = longer * (len + 1);
-    return chunk < split ? chunk / (len + 1) : longer + (chunk - split) / len;
-  }
-};
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   uint32_t r;
@@ -157,200 +107,57 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 
   if (warp == W) {
     // ---------------------------------------------------------------- loads
-    const int B = c.s.B, capacity = B < 32 ? B : 32;
-    Entry held = {0, 0, 0, 0};                             // of entry `lane`
-    if (lane < capacity) held = entry_of(a, lane, blockIdx.x == 0);
-    int upto = held.chunks * Hkv, total = 0;               // inclusive prefix within the first 32 entries
-    for (int b = lane + 32; b < B; b += 32) total += entry_of(a, b, blockIdx.x == 0).chunks * Hkv;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, upto, d);
-      if (lane >= d) upto += x;
-    }
-    const int upto32 = __shfl_sync(0xffffffffu, upto, 31);
-    if (B > 32) {
-#pragma unroll
-      for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-    }
-    total += upto32;
-    // Entries of one length (and of few chunks): the same parts of every unit, so that no CTA has pieces of two.
-    const int chunks0 = __shfl_sync(0xffffffffu, held.chunks, 0);
-    const bool even = B <= 32 && a.parts > 0 && total < kGrid * kLongRun &&
-                      __all_sync(0xffffffffu, lane >= B || held.chunks == chunks0);
-    const int part = even ? (chunks0 + a.parts - 1) / a.parts : 0;       // chunks of each
-    Runs rs(total);
-    if (even) rs.runs = B * Hkv * a.parts;
-    // A batch is 32 copies' pages, a lane each: page and scales of the next batch are fetched during this one.
-    const int log_box = __ffs(a.box) - 1, log_per = __ffs(kTokens) - 1 - log_box, log_span = 5 - log_per;
-    const int per = 1 << log_per, span = 1 << log_span;    // copies a chunk, chunks a batch
-    const int group_copy = lane < S::GROUPS ? lane >> (log_box - 4) : 0;
     int g = 0, pieces = 0;
-    bool ok = true;
-    // the next stage, once it is free
-    auto stage = [&]() {
-      const int s = g % S::STAGES;
-      if (g >= S::STAGES)
-        ok = __all_sync(0xffffffffu, wait_or_fail(&ctl->empty[s], (uint32_t)((g / S::STAGES - 1) & 1), fail, status));
-      return s;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
     };
-    const int r = blockIdx.x;
-    if (r < rs.runs) {
-      // the run's chunks, the entry that holds the first of them, and that entry's first chunk
-      int b = 0, base = 0, cur = rs.start(r), end = rs.start(r + 1);
-      if (even) {
-        const int unit = r / a.parts, first = (r - unit * a.parts) * part;
-        cur = unit * chunks0 + min(first, chunks0);
-        end = unit * chunks0 + min(first + part, chunks0);
-        b = unit / Hkv;
-        base = b * Hkv * chunks0;
-      } else if (cur < upto32) {
-        b = __ffs(__ballot_sync(0xffffffffu, upto > cur)) - 1;
-        base = __shfl_sync(0xffffffffu, upto - held.chunks * Hkv, b);
-      } else {
-        base = upto32;
-        for (int b0 = 32;; b0 += 32) {
-          const int mine = b0 + lane < B ? entry_of(a, b0 + lane, false).chunks * Hkv : 0;
-          int in = mine;
-#pragma unroll
-          for (int d = 1; d < 32; d <<= 1) {
-            const int x = __shfl_up_sync(0xffffffffu, in, d);
-            if (lane >= d) in += x;
-          }
-          const unsigned past = __ballot_sync(0xffffffffu, base + in > cur);
-          if (past || b0 + 32 >= B) {
-            const int w = past ? __ffs(past) - 1 : 0;
-            b = b0 + w;
-            base += __shfl_sync(0xffffffffu, in - mine, w);
-            break;
-          }
-          base += __shfl_sync(0xffffffffu, in, 31);
-        }
-      }
-      auto entry = [&](int i) {
-        if (i >= 32) return entry_of(a, i, false);
-        Entry e;
-        e.row0 = __shfl_sync(0xffffffffu, held.row0, i);
-        e.tokens = __shfl_sync(0xffffffffu, held.tokens, i);
-        e.len = __shfl_sync(0xffffffffu, held.len, i);
-        e.chunks = __shfl_sync(0xffffffffu, held.chunks, i);
-        return e;
-      };
-      Entry e = entry(b);
-      while (ok && cur < end) {
-        while (cur >= base + e.chunks * Hkv) {
-          base += e.chunks * Hkv;
-          e = entry(++b);
-        }
-        // -------------------------------------------------------- a piece: chunks c0 .. c1 - 1 of a unit
-        const int kvh = (cur - base) / e.chunks, unit0 = base + kvh * e.chunks;
-        const int c0 = cur - unit0, c1 = min(e.chunks, c0 + (end - cur));
-        cur += c1 - c0;
-        const int32_t* table = c.s.page_table + (int64_t)b * c.s.max_pages;
-        auto exists = [&](int chunk) {                     // this lane's copy of the batch from `chunk` on
-          return chunk + (lane >> log_per) < c1 && chunk * kTokens + (lane << log_box) < e.len;
-        };
-        auto fetch = [&](int chunk) {
-          return exists(chunk) ? table[(chunk * kTokens + (lane << log_box)) >> a.log_page] : -1;
-        };
-        auto check = [&](int chunk, int id) {              // (a page outside the pool is not seen)
-          if (!exists(chunk)) return -1;
-          if (id >= 0 && id < c.s.num_pages) return id;
-          atomicOr(status, MKV_FLAG_BAD_INDEX);
-          return -1;
-        };
-        auto scales = [&](int id, float& ks, float& vs) {
-          ks = 0.f;
-          vs = 1.f;
-          if (id >= 0) {
-            ks = c.k_scale[(int64_t)id * Hkv + kvh];
-            vs = c.v_scale[(int64_t)id * Hkv + kvh];
-          }
-        };
-        int pid = fetch(c0), next = 0;
-        // queries: one copy a token's heads
-        if (pieces > 0) ok = __all_sync(0xffffffffu, wait_or_fail(&ctl->qempty, (uint32_t)((pieces - 1) & 1), fail, status));
-        if (!ok) break;
-        if (lane == 0) {
-          tc_mbar_expect_tx(&ctl->qfull, (uint32_t)(e.tokens * a.G * D * 2));
-          ctl->q_loads = pieces + 1;
-        }
-        __syncwarp();
-        if (lane < e.tokens)
-          bulk_load(sm + S::Q_OFF + lane * a.G * D * 2,
-                    c.q + (int64_t)(e.row0 + lane) * c.q_stride + (int64_t)kvh * a.G * D, a.G * D * 2, &ctl->qfull);
-        ++pieces;
-        pid = check(c0, pid);
-        float ks, vs, nks = 0.f, nvs = 1.f;
-        scales(pid, ks, vs);
-        Head hd;
-        hd.len = e.len;
-        hd.tokens = e.tokens;
-        hd.unit = b * Hkv + kvh;
-        hd.kvh = kvh;
-        hd.row0 = e.row0;
-        const bool whole = c1 - c0 == e.chunks;
-        hd.first = hd.place0 = hd.count = hd.mine = hd.pad = 0;
-        for (int ch = c0; ch < c1; ++ch, ++g) {
-          const int in = (ch - c0) & (span - 1), from = ch - in;
-          if (in == 0 && ch > c0) {
-            pid = next;
-            ks = nks;
-            vs = nvs;
-          }
-          if (in == 0) next = fetch(ch + span);
-          if (in == span / 2) {
-            next = check(from + span, next);
-            scales(next, nks, nvs);
-          }
-          const int s = stage();
-          if (!ok) break;
-          const int id = __shfl_sync(0xffffffffu, pid, ((in << log_per) + lane) & 31);
-          const bool copy = lane < per && id >= 0;
-          const int copies = __popc(__ballot_sync(0xffffffffu, copy));
+    auto free_stage = [&]() {
+      return g < S::STAGES || wait(&ctl->empty[g % S::STAGES], (uint32_t)((g / S::STAGES - 1) & 1));
+    };
+    const int log_box = a.w.log_box;
+    bool ok = work_through(
+        c, a.w, status, lane,
+        [&](const Head& hd) {                              // a piece's queries: one copy a token's heads
+          if (pieces > 0 && !wait(&ctl->qempty, (uint32_t)((pieces - 1) & 1))) return false;
+          const int bytes = a.G * D * 2;
           if (lane == 0) {
-            tc_mbar_expect_tx(&ctl->full[s], (uint32_t)copies * 2 * a.box * D);
+            tc_mbar_expect_tx(&ctl->qfull, (uint32_t)(hd.tokens * bytes));
+            ctl->q_loads = pieces + 1;
+          }
+          __syncwarp();
+          if (lane < hd.tokens)
+            bulk_load(sm + S::Q_OFF + lane * bytes, c.q + (int64_t)(hd.row0 + lane) * c.q_stride + (int64_t)hd.kvh * a.G * D,
+                      bytes, &ctl->qfull);
+          ++pieces;
+          return true;
+        },
+        [&](const Head& hd, int id) {
+          if (!free_stage()) return false;
+          const int s = g % S::STAGES, copies = __popc(__ballot_sync(0xffffffffu, id >= 0));
+          if (lane == 0) {
+            tc_mbar_expect_tx(&ctl->full[s], (uint32_t)(copies * 2 * D) << log_box);
             ctl->loads = g + 1;
           }
           __syncwarp();
-          if (copy) {
+          if (id >= 0) {
             uint8_t* dst = sm + S::KV_OFF + s * 2 * S::TILE + (lane << log_box) * D;
-            const int y = (ch * kTokens + (lane << log_box)) & (c.s.page - 1), z = id * Hkv + kvh;
+            const int y = (hd.chunk * kTokens + (lane << log_box)) & (c.s.page - 1), z = id * Hkv + hd.kvh;
             tma_load_4d(dst, &kmap, 0, y, z, 0, &ctl->full[s]);
             tma_load_4d(dst + S::TILE, &vmap, 0, y, z, 0, &ctl->full[s]);
           }
-          if (ch == c0 && !whole) {                        // a run's places: its first piece, and its last
-            if (even) {
-              hd.first = (b * Hkv + kvh) * a.parts;
-              hd.place0 = 2 * hd.first;
-              hd.count = (chunks0 + part - 1) / part;
-            } else {
-              hd.first = rs.of(unit0);
-              hd.place0 = 2 * hd.first + (rs.start(hd.first) < unit0 ? 1 : 0);
-              hd.count = rs.of(unit0 + e.chunks - 1) - hd.first + 1;
-            }
-            hd.mine = r == hd.first ? hd.place0 : 2 * r;
-          }
-          // scales of the chunk's groups of 16 tokens
-          const int owner = (in << log_per) + group_copy;
-          const float gk = __shfl_sync(0xffffffffu, ks, owner), gv = __shfl_sync(0xffffffffu, vs, owner);
-          const int gid = __shfl_sync(0xffffffffu, pid, owner);
-          if (lane < S::GROUPS) {
-            int x;
-            const float mant = frexpf(gv, &x);
-            reinterpret_cast<float4*>(sm + S::SC_OFF)[s * S::GROUPS + lane] =
-                make_float4(gk * a.scale_log2, mant, (float)x, gid >= 0 ? 1.f : 0.f);
-          }
-          hd.flags = (ch == c0 ? kFirst : 0) | (ch == c1 - 1 ? kLast : 0) | (whole ? kWhole : 0);
-          hd.chunk = ch;
+          return true;
+        },
+        [&](const Head& hd, const float4& sc) {
+          const int s = g % S::STAGES;
+          if (lane < S::GROUPS) reinterpret_cast<float4*>(sm + S::SC_OFF)[s * S::GROUPS + lane] = sc;
           if (lane == 31) *reinterpret_cast<Head*>(sm + S::HD_OFF + s * 48) = hd;
           __syncwarp();
           if (lane == 0) tc_mbar_arrive(&ctl->full[s]);
-        }
-      }
-    }
-    if (ok) {
-      const int s = stage();
-      if (ok && lane == 0) {
+          ++g;
+        });
+    if (ok && free_stage()) {
+      const int s = g % S::STAGES;
+      if (lane == 0) {
         reinterpret_cast<Head*>(sm + S::HD_OFF + s * 48)->flags = kEnd;
         tc_mbar_arrive(&ctl->full[s]);
         tc_mbar_arrive(&ctl->full[s]);
@@ -401,44 +208,9 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       if (dead) return;
       if (ctl->last) {
         constexpr int VL = D / 32;                         // dims a lane
-        auto place = [&](int i) { return (int64_t)(i == 0 ? owed.place0 : 2 * (owed.first + i)) * N; };
-        auto load = [&](int64_t at) {
-          const float* po = a.part_o + at * D + lane * VL;
-          if constexpr (VL == 4) return __ldcg(reinterpret_cast<const float4*>(po));
-          const float2 f = __ldcg(reinterpret_cast<const float2*>(po));
-          return make_float4(f.x, f.y, 0.f, 0.f);
-        };
         for (int row = warp; row < owed.tokens * G; row += W) {   // a row a warp
-          float mx = kNoMax, mx2 = kNoMax, sum = 0.f;
-          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-          // eight pieces at a time, their loads under way together
-          for (int i0 = 0; i0 < owed.count; i0 += 8) {
-            float4 st[8], z[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const int64_t at = place(min(i0 + k, owed.count - 1)) + row;
-              st[k] = __ldcg(a.part_st + at);
-              z[k] = load(at);
-              if (i0 + k >= owed.count) st[k] = make_float4(kNoMax, 0.f, kNoMax, 0.f);
-            }
-            float nm = mx, nm2 = mx2;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              nm = fmaxf(nm, st[k].x);
-              nm2 = fmaxf(nm2, st[k].z);
-            }
-            sum *= ex2_approx(mx - nm);
-            const float back = ex2_approx(mx2 - nm2);
-            y = make_float4(y.x * back, y.y * back, y.z * back, y.w * back);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float w = i0 + k < owed.count ? ex2_approx(st[k].z - nm2) : 0.f;
-              sum += st[k].y * ex2_approx(st[k].x - nm);
-              y = make_float4(y.x + w * z[k].x, y.y + w * z[k].y, y.z + w * z[k].z, y.w + w * z[k].w);
-            }
-            mx = nm;
-            mx2 = nm2;
-          }
+          float mx, sum, mx2;
+          const float4 y = add_pieces<VL>(owed, a.part_o, a.part_st, N, row, lane, mx, sum, mx2);
           const uint2 h = finish(owed, row, y, mx, sum, mx2);
           uint16_t* dst = out_row(owed, row) + lane * VL;
           if constexpr (VL == 4)
@@ -726,11 +498,10 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 // ---------------------------------------------------------------- host side
 template <class S>
 cudaError_t launch_shape(const PagedAttnCall& c, DecodeArgs a, cudaStream_t st) {
-  a.box = std::min(c.s.page, kTokens);
   const int64_t heads = c.s.num_pages * c.s.Hkv;
   CUtensorMap km, vm;
-  cudaError_t e = encode_code_map(&km, c.k, S::D, c.s.page, heads, a.box);
-  if (e == cudaSuccess) e = encode_code_map(&vm, c.v, S::D, c.s.page, heads, a.box);
+  cudaError_t e = encode_code_map(&km, c.k, S::D, c.s.page, heads, c.s.page);
+  if (e == cudaSuccess) e = encode_code_map(&vm, c.v, S::D, c.s.page, heads, c.s.page);
   if (e == cudaSuccess)
     e = cudaFuncSetAttribute(decode_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::ALLOC);
   if (e != cudaSuccess) return e;
@@ -753,9 +524,7 @@ cudaError_t launch_paged_decode(const PagedAttnCall& c, void* ws, cudaStream_t s
   if (e != cudaSuccess) return e;
   a.c = c;
   a.G = c.s.Hq / c.s.Hkv;
-  a.parts = kGrid / (c.s.B * c.s.Hkv);
-  for (a.log_page = 0; (1 << a.log_page) < c.s.page;) ++a.log_page;
-  a.scale_log2 = c.scale * kLog2e;
+  a.w = work_args(c, kGrid);
   uint8_t* base = static_cast<uint8_t*>(ws);
   a.tickets = reinterpret_cast<int*>(base);
   a.part_st = reinterpret_cast<float4*>(base + kCounterBytes);
