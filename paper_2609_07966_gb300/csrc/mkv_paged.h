@@ -69,12 +69,13 @@ struct PagedAttnCall {
   const uint8_t *k, *v;
   const float *k_scale, *v_scale;
 };
-// Calls of up to kPagedRows query rows a key head (max_rows x heads of a group) go to paged_decode.cu, others to
-// paged_prefill.cu.
-constexpr int kPagedRows = 8;
-bool paged_decode_countable(const PagedAttnCall& c);      // its chunks fit the kernel's 32-bit counts
+// By the query rows of a key head (max_rows x heads of a group): up to kPagedFew paged_decode.cu, up to kPagedBlock
+// paged_block.cu, more paged_prefill.cu.
+constexpr int kPagedFew = 8, kPagedBlock = 128;
 size_t paged_decode_ws_bytes(const PagedAttnCall& c);
 cudaError_t launch_paged_decode(const PagedAttnCall& c, void* ws, cudaStream_t st);
+size_t paged_block_ws_bytes(const PagedAttnCall& c);
+cudaError_t launch_paged_block(const PagedAttnCall& c, void* ws, cudaStream_t st);
 size_t paged_prefill_ws_bytes(const PagedAttnCall& c);
 cudaError_t launch_paged_prefill(const PagedAttnCall& c, void* ws, cudaStream_t st);
 

@@ -134,9 +134,16 @@ mkv_status check_attention_rows(const mkv_paged_config* c, int64_t n, int64_t ma
   return MKV_OK;
 }
 
-bool few_rows(const PagedAttnCall& c) { return c.max_rows * (c.s.Hq / c.s.Hkv) <= kPagedRows; }
+int64_t rows_of(const PagedAttnCall& c) { return c.max_rows * (c.s.Hq / c.s.Hkv); }
 size_t attention_ws_bytes(const PagedAttnCall& c) {
-  return few_rows(c) ? paged_decode_ws_bytes(c) : paged_prefill_ws_bytes(c);
+  return rows_of(c) <= kPagedFew     ? paged_decode_ws_bytes(c)
+         : rows_of(c) <= kPagedBlock ? paged_block_ws_bytes(c)
+                                     : paged_prefill_ws_bytes(c);
+}
+cudaError_t launch_attention(const PagedAttnCall& c, void* ws, cudaStream_t st) {
+  return rows_of(c) <= kPagedFew     ? launch_paged_decode(c, ws, st)
+         : rows_of(c) <= kPagedBlock ? launch_paged_block(c, ws, st)
+                                     : launch_paged_prefill(c, ws, st);
 }
 
 }  // namespace
@@ -270,7 +277,9 @@ mkv_status mkv_paged_attention(const mkv_paged_config* cfg, const void* q, int64
   MKV_TRY(check_row("out", out, dims, &c.out_stride));
   c.s = shape_of(cfg, n, start, cache);
   c.max_rows = max_rows;
-  MKV_REQUIRE(!few_rows(c) || paged_decode_countable(c), MKV_ERR_UNSUPPORTED, "too many tokens (max_pages x B x Hkv) for one call");
+  // (chunks of 128 tokens are counted in 32 bits)
+  MKV_REQUIRE((int64_t)cfg->B * cfg->Hkv * (cache->max_pages * cfg->page_size / 128 + 1) <= INT32_MAX / 2, MKV_ERR_UNSUPPORTED,
+              "too many tokens (max_pages x B x Hkv) for one call");
   const size_t need = attention_ws_bytes(c);
   MKV_REQUIRE(ws != nullptr && ws_bytes >= need, MKV_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
   MKV_REQUIRE(aligned(ws, 256), MKV_ERR_INVALID_ARG, "ws must be 256-byte aligned");
@@ -282,7 +291,7 @@ mkv_status mkv_paged_attention(const mkv_paged_config* cfg, const void* q, int64
   c.v = static_cast<const uint8_t*>(cache->v);
   c.k_scale = cache->k_scale;
   c.v_scale = cache->v_scale;
-  MKV_CUDA(few_rows(c) ? launch_paged_decode(c, ws, as_stream(stream)) : launch_paged_prefill(c, ws, as_stream(stream)));
+  MKV_CUDA(launch_attention(c, ws, as_stream(stream)));
   return MKV_OK;
 }
 

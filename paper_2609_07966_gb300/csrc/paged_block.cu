@@ -1,0 +1,624 @@
+// Attention of an entry's newest tokens over its 8-bit pages, 9 to 128 query rows of a key head (tokens x heads of a group):
+// drafted tokens, short chunks.  The formula, and the two running maxima, are those of paged_decode.cu.
+//
+// Bound by memory, or by shared memory, which every code passes several times: TMA writes a 128-token tile's codes, a
+// warpgroup reads them, widens them to fp16 (exactly) and writes them again in the layout that the tensor cores read:
+//   S [128 x 128] = Q K^T     Q from tensor memory, K from shared memory
+//   O [128 x D]  += W V       W (the weights, fp16) from tensor memory, V from shared memory
+// The products have 128 rows whatever the call has.  With up to 32 (64) rows the queries are there four (two) times, and copy
+// c takes the tile's tokens 128 / copies c .. alone: all lanes have scores to work on, a thread 32 (64) of them, each copy has
+// maxima and sums of its own, its weights for the other copies' tokens are zeros that are written once, and the copies' sums
+// are added up at the end of a piece.
+//
+// Work is shared out in runs of tiles (mkv_paged_work.cuh).  Roles: one warp finds out its CTA's and loads it (a bulk copy a
+// page), four convert, one issues products, whichever is ready (a finished tile's second product first), four do the softmax
+// of a tile while the next one's scores are computed.
+#include <math.h>
+
+#include <algorithm>
+
+#include "mkv_paged_work.cuh"
+
+namespace mkv {
+
+namespace {
+
+constexpr int kThreads = 384;       // softmax, conversion, loads + products (+ two idle warps)
+constexpr int kSoftmax = 128;
+// registers a thread: what a launch of kThreads gets (168), and its split
+constexpr int kRegsSoftmax = 208, kRegsConvert = 128;
+static_assert(kRegsSoftmax + kRegsConvert + 168 <= 3 * 168, "register shares");
+constexpr int kHeads = 8;           // tiles whose heads and scales are held
+constexpr int kSlots = 3;           // widened tiles (K0 V0 K1 V1 ..)
+constexpr int kGrid = kNumSMs;
+
+struct BlockArgs {
+  PagedAttnCall c;
+  WorkArgs w;
+  uint32_t* status;
+  int G;
+  int* tickets;                     // [B][Hkv], zero between calls
+  float* part_o;                    // [kGrid][2][ROWS][D]
+  float4* part_st;                  // [kGrid][2][ROWS]: m, sum, m2
+};
+
+template <int FMT_, int D_, int COPIES_>
+struct BShape {
+  static constexpr int FMT = FMT_, D = D_, COPIES = COPIES_;
+  static constexpr int ROWS = 128 / COPIES, COLS = 128 / COPIES, NG = COLS / 16;   // of a copy; groups of 16 tokens
+  static constexpr int KA = D / 64, ATOM = 128 * 128, TILE = KA * ATOM;
+  static constexpr int RAW = kTokens * D, RAWS = D == 128 ? 6 : 8;
+  static constexpr int OROW = 36;                          // floats between rows of the join's 32 dims
+  static constexpr int T_OFF = 0;                          // [kSlots] widened tiles
+  static constexpr int R_OFF = T_OFF + kSlots * TILE;      // [RAWS] codes
+  static constexpr int O_OFF = R_OFF + RAWS * RAW;         // [128][OROW] floats
+  static constexpr int SC_OFF = O_OFF + 128 * OROW * 4;    // [kHeads][8] float4
+  static constexpr int HD_OFF = SC_OFF + kHeads * kGroups * 16;
+  static constexpr int ST_OFF = HD_OFF + kHeads * 48;      // [128] + [ROWS] float4: the lanes', the piece's
+  static constexpr int CTL_OFF = ST_OFF + (128 + ROWS) * 16;
+  static constexpr int ALLOC = CTL_OFF + 512 + 1024;       // slack to align the base to 1024 B
+  static_assert(ALLOC <= 227 * 1024, "shared memory");
+  // tensor memory columns
+  static constexpr int S = 0, O = 256, P = 384, Q = 448;
+};
+
+struct BlockCtl {
+  uint64_t raw_full[8], raw_empty[8], tile_full[kSlots], tile_empty[kSlots], head[kHeads], sfull[2], pfull, pvdone, qfull, meet,
+      drained;
+  uint32_t tslot;
+  int fail, loads, last;
+};
+static_assert(sizeof(BlockCtl) <= 512, "control block");
+
+__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+template <class S, bool BF16>
+__global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
+  constexpr int D = S::D;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+  BlockCtl* ctl = reinterpret_cast<BlockCtl*>(sm + S::CTL_OFF);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const PagedAttnCall& c = a.c;
+  const int Hkv = c.s.Hkv;
+  volatile int* fail = &ctl->fail;
+  uint32_t* status = a.status;
+  auto head_at = [&](int g) { return reinterpret_cast<Head*>(sm + S::HD_OFF + g % kHeads * 48); };
+
+  if (warp == 9) tc_alloc(&ctl->tslot, 512);
+  if (threadIdx.x == 256) {
+    for (int s = 0; s < S::RAWS; ++s) {
+      tc_mbar_init(&ctl->raw_full[s], 1);
+      tc_mbar_init(&ctl->raw_empty[s], 4);
+    }
+    for (int s = 0; s < kSlots; ++s) {
+      tc_mbar_init(&ctl->tile_full[s], 4);
+      tc_mbar_init(&ctl->tile_empty[s], 1);
+    }
+    for (int s = 0; s < kHeads; ++s) tc_mbar_init(&ctl->head[s], 1);
+    for (int s = 0; s < 2; ++s) tc_mbar_init(&ctl->sfull[s], 1);
+    tc_mbar_init(&ctl->pfull, 4);
+    tc_mbar_init(&ctl->pvdone, 1);
+    tc_mbar_init(&ctl->qfull, 4);
+    tc_mbar_init(&ctl->meet, 4);
+    tc_mbar_init(&ctl->drained, 1);
+    tc_fence_mbar_init();
+    ctl->fail = ctl->loads = 0;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_wait_and_trigger();
+  const uint32_t tbase = ctl->tslot;
+
+  if (warp == 8) {
+    // ---------------------------------------------------------------- loads
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
+    };
+    int g = 0;
+    const int log_box = a.w.log_box;
+    const bool ok = work_through(
+        c, a.w, status, lane, [&](const Head&) { return true; },
+        [&](const Head& hd, int id) {
+          const int copies = __popc(__ballot_sync(0xffffffffu, id >= 0));
+          const int64_t from = (((int64_t)id * Hkv + hd.kvh) * c.s.page + ((hd.chunk * kTokens + (lane << log_box)) & (c.s.page - 1))) * D;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int item = 2 * g + h, s = item % S::RAWS;
+            if (item >= S::RAWS && !wait(&ctl->raw_empty[s], (uint32_t)((item / S::RAWS - 1) & 1))) return false;
+            if (lane == 0) {
+              tc_mbar_expect_tx(&ctl->raw_full[s], (uint32_t)(copies * D) << log_box);
+              ctl->loads = item + 1;
+            }
+            __syncwarp();
+            if (id >= 0)
+              bulk_load(sm + S::R_OFF + s * S::RAW + (lane << log_box) * D, (h == 0 ? c.k : c.v) + from, (uint32_t)D << log_box,
+                        &ctl->raw_full[s]);
+          }
+          return true;
+        },
+        [&](const Head& hd, const float4& sc) {
+          // (its place is free: tile g's codes could only be loaded once tile g - 8 was done with)
+          if (lane < kGroups) reinterpret_cast<float4*>(sm + S::SC_OFF)[g % kHeads * kGroups + lane] = sc;
+          if (lane == 31) *head_at(g) = hd;
+          __syncwarp();
+          if (lane == 0) tc_mbar_arrive(&ctl->head[g % kHeads]);
+          ++g;
+        });
+    if (ok) {
+      // (the last head's place: the same reasoning with no codes to wait for needs the wait itself)
+      const int item = 2 * g, s = item % S::RAWS;
+      if ((item < S::RAWS || wait(&ctl->raw_empty[s], (uint32_t)((item / S::RAWS - 1) & 1))) && lane == 0) {
+        head_at(g)->flags = kEnd;
+        tc_mbar_arrive(&ctl->head[g % kHeads]);
+      }
+    }
+  } else if (warp == 9) {
+    if (elect_one()) {
+      // ---------------------------------------------------------------- products
+      constexpr uint32_t idS = tc_idesc(false, 128, 128, false, false);
+      constexpr uint32_t idO = tc_idesc(false, 128, D, false, true);
+      const Desc kd = tc_desc_sw128(smem_addr(sm + S::T_OFF));
+      const Desc vd = tc_desc_mn<64>(smem_addr(sm + S::T_OFF), S::ATOM);
+      int ts = 0, tv = 0, pieces = 0;                      // next tile's scores, next tile's second product; pieces begun
+      int flags = 0, vflags = 0;                           // of tile ts (0: not looked up yet); of tile tv
+      uint64_t since = 0;
+      int idle = 0;
+      bool ok = true;
+      while (ok) {
+        if (flags == 0 && mbar_test(&ctl->head[ts % kHeads], (uint32_t)((ts / kHeads) & 1))) flags = head_at(ts)->flags | 16;
+        if ((flags & kEnd) && tv == ts) break;
+        const int ki = 2 * ts, vi = 2 * tv + 1;            // their places in the ring of widened tiles
+        const bool can_v = tv < ts && mbar_test(&ctl->pfull, (uint32_t)(tv & 1)) &&
+                           mbar_test(&ctl->tile_full[vi % kSlots], (uint32_t)((vi / kSlots) & 1));
+        const bool can_s = flags != 0 && !(flags & kEnd) && ts <= tv + 1 && (!(flags & kFirst) || tv == ts) &&
+                           (!(flags & kFirst) || mbar_test(&ctl->qfull, (uint32_t)(pieces & 1))) &&
+                           mbar_test(&ctl->tile_full[ki % kSlots], (uint32_t)((ki / kSlots) & 1));
+        if (can_v) {
+          tc_fence_after();
+          const Desc v0 = vd.at(vi % kSlots * S::TILE).opaque();
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk)
+            tc_mma_ts(tbase + S::O, tbase + S::P + (uint32_t)(kk * 8), v0.at(kk * 2048), idO,
+                      !(vflags & kFirst) || kk > 0 ? 1u : 0u);
+          tc_commit(&ctl->tile_empty[vi % kSlots]);
+          tc_commit(&ctl->pvdone);
+          ++tv;
+          vflags = head_at(tv)->flags;                     // (of a tile whose scores are under way, or looked up below)
+        }
+        if (can_s) {
+          tc_fence_after();
+          const Desc k0 = kd.at(ki % kSlots * S::TILE).opaque();
+          const uint32_t d = tbase + S::S + (uint32_t)((ts & 1) * 128);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            tc_mma_ts(d, tbase + S::Q + (uint32_t)(kk * 8), k0.at((kk >> 2) * S::ATOM + (kk & 3) * 32), idS, kk > 0 ? 1u : 0u);
+          tc_commit(&ctl->tile_empty[ki % kSlots]);
+          tc_commit(&ctl->sfull[ts & 1]);
+          if (flags & kFirst) ++pieces;
+          if (ts == tv) vflags = flags;
+          ++ts;
+          flags = 0;
+        }
+        if (can_s || can_v) {
+          idle = 0;
+          continue;
+        }
+        // nothing is ready: a bounded wait for either, its clock read now and then
+        if ((++idle & 63) == 0) {
+          const uint64_t now = globaltimer_ns();
+          if (idle == 64) since = now;
+          if (now - since > kRoleWaitNs) {
+            *fail = 1;
+            atomicOr(status, MKV_FLAG_WAIT_TIMEOUT);
+          }
+          ok = *fail == 0;
+          if (idle > (1 << 30)) idle = 128;
+        }
+      }
+      tc_commit(&ctl->drained);
+    }
+  } else if (warp >= 4 && warp < 8) {
+    regs_down<kRegsConvert>();
+    // ---------------------------------------------------------------- codes to fp16
+    // A thread takes one 16-byte piece of every ROWS'th row.  Eight neighbouring threads read 128 bytes of codes and store
+    // pieces of two atoms, or of two rows, whose banks differ.
+    constexpr int LN = D / 16, STEP = 128 / LN;            // pieces of a row; rows a step
+    const int tid = threadIdx.x - 128, piece = tid % LN, row = tid / LN;
+    // (pieces 4 .. 7 go to the second atom, at the same banks as the first: they store their halves the other way round)
+    const bool swap = piece >= 4;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
+    };
+    for (int g = 0;; ++g) {
+      if (!wait(&ctl->head[g % kHeads], (uint32_t)((g / kHeads) & 1))) break;
+      const int flags = head_at(g)->flags;
+      if (flags & kEnd) break;
+      const int seen = head_at(g)->seen, tail = head_at(g)->len - head_at(g)->chunk * kTokens;
+      const bool clean = seen == 0xff && tail >= kTokens;
+      bool ok = true;
+#pragma unroll 1
+      for (int h = 0; ok && h < 2; ++h) {
+        const int item = 2 * g + h, rs = item % S::RAWS, s = item % kSlots;
+        ok = wait(&ctl->raw_full[rs], (uint32_t)((item / S::RAWS) & 1)) &&
+             (item < kSlots || wait(&ctl->tile_empty[s], (uint32_t)((item / kSlots - 1) & 1)));
+        if (!ok) break;
+        const uint8_t* src = sm + S::R_OFF + rs * S::RAW + row * D + piece * 16;
+        uint8_t* dst = sm + S::T_OFF + s * S::TILE + (piece >> 2) * S::ATOM;
+        const bool zeros = h == 1 && !clean;               // what no row sees must not meet a zero weight as NaN
+#pragma unroll 4
+        for (int r = row; r < 128; r += STEP) {
+          uint4 x = *reinterpret_cast<const uint4*>(src + (r - row) * D);
+          if (zeros && (r >= tail || !(seen >> (r >> 4) & 1))) x = make_uint4(0u, 0u, 0u, 0u);
+          uint32_t e[8];
+          widen_codes<S::FMT>(x.x, e[0], e[1]);
+          widen_codes<S::FMT>(x.y, e[2], e[3]);
+          widen_codes<S::FMT>(x.z, e[4], e[5]);
+          widen_codes<S::FMT>(x.w, e[6], e[7]);
+          const uint32_t at = mn_offset<64>(r, 2 * (piece & 3) + (swap ? 1 : 0));
+          *reinterpret_cast<uint4*>(dst + at) =
+              make_uint4(swap ? e[4] : e[0], swap ? e[5] : e[1], swap ? e[6] : e[2], swap ? e[7] : e[3]);
+          *reinterpret_cast<uint4*>(dst + (at ^ 16u)) =
+              make_uint4(swap ? e[0] : e[4], swap ? e[1] : e[5], swap ? e[2] : e[6], swap ? e[3] : e[7]);
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          tc_mbar_arrive(&ctl->tile_full[s]);
+          tc_mbar_arrive(&ctl->raw_empty[rs]);
+        }
+      }
+      if (!ok) break;
+    }
+  } else if (warp < 4) {
+    regs_up<kRegsSoftmax>();
+    // ---------------------------------------------------------------- softmax: lane 32 warp + lane, row `row` of copy `copy`
+    constexpr int COLS = S::COLS, NG = S::NG;
+    const int at = warp * 32 + lane, copy = at / S::ROWS, row = at % S::ROWS, G = a.G;
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    const uint32_t tO = tbase + lanes + S::O, tP = tbase + lanes + S::P + (uint32_t)(copy * COLS / 2);
+    float* ob = reinterpret_cast<float*>(sm + S::O_OFF);
+    float4* stat = reinterpret_cast<float4*>(sm + S::ST_OFF);
+    float4* fin = stat + 128;
+    bool dead = false;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (!dead) dead = !__all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status));
+      tc_fence_after();
+    };
+    // (a barrier of the four warps whose waits are bounded too)
+    uint32_t met = 0;
+    auto meet = [&]() {
+      __syncwarp();
+      if (lane == 0) tc_mbar_arrive(&ctl->meet);
+      wait(&ctl->meet, met);
+      met ^= 1;
+    };
+    // An output is o / sum 2^(m2 - m - 6); zeros for a row before position 0, which sees nothing; NaN where no score leaves a
+    // weight.
+    auto store_out = [&](const Head& h, int r, int d, float4 x, float mm, float sum, float mm2) {
+      const float f = half_power(mm, mm2), inv = sum == 0.f ? NAN : 1.f / sum;
+      x = make_float4(x.x * inv * f * f, x.y * inv * f * f, x.z * inv * f * f, x.w * inv * f * f);
+      if (h.len - h.tokens + r / G < 0) x = make_float4(0.f, 0.f, 0.f, 0.f);
+      uint16_t* dst = c.out + (int64_t)(h.row0 + r / G) * c.out_stride + (int64_t)(h.kvh * G + r % G) * D + d;
+      *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<BF16>(x.x, x.y), pack2<BF16>(x.z, x.w));
+    };
+    // A piece was handed in and the unit's ticket taken (by thread 0, which looks at it only here): the CTA that took the
+    // unit's last one adds the pieces up.
+    Head owed;
+    owed.count = 0;
+    int ticket = 0;
+    auto settle = [&]() {
+      if (owed.count == 0 || dead) return;
+      if (threadIdx.x == 0) {
+        ctl->last = ticket == owed.count - 1;
+        if (ctl->last) a.tickets[owed.unit] = 0;
+      }
+      meet();
+      if (dead) return;
+      if (ctl->last) {
+        const int R = owed.tokens * G;
+        if (at < R) {                                      // a row a thread: what its pieces' statistics come to
+          float mx = kNoMax, mx2 = kNoMax, sum = 0.f;
+#pragma unroll 4
+          for (int i = 0; i < owed.count; ++i) {
+            const float4 st = __ldcg(a.part_st + (int64_t)owed.place(i) * S::ROWS + at);
+            const float nm = fmaxf(mx, st.x);
+            sum = sum * ex2_approx(mx - nm) + st.y * ex2_approx(st.x - nm);
+            mx = nm;
+            mx2 = fmaxf(mx2, st.z);
+          }
+          fin[at] = make_float4(mx, sum, mx2, 0.f);
+        }
+        meet();
+        if (dead) return;
+#pragma unroll 2
+        for (int e = at; e < R * (D / 4); e += kSoftmax) { // four dims of a row
+          const int r = e / (D / 4), d = e % (D / 4) * 4;
+          const float4 all = fin[r];
+          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int i = 0; i < owed.count; ++i) {
+            const int64_t p = (int64_t)owed.place(i) * S::ROWS + r;
+            const float f = ex2_approx(__ldcg(a.part_st + p).z - all.z);
+            const float4 z = __ldcg(reinterpret_cast<const float4*>(a.part_o + p * D + d));
+            y = make_float4(y.x + f * z.x, y.y + f * z.y, y.z + f * z.z, y.w + f * z.w);
+          }
+          store_out(owed, r, d, y, all.x, all.y, all.z);
+        }
+      }
+      meet();                                              // (before `last` and `fin` are set again)
+      owed.count = 0;
+    };
+    if (S::COPIES > 1) {                                   // the weights that stay zero
+      float z[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[i] = 0.f;
+      for (int i = 0; i < 4; ++i) tm_store<16>(tbase + lanes + S::P + (uint32_t)(16 * i), z);
+      tm_store_wait();
+    }
+
+    float m = kNoMax, m2 = kNoMax, l = 0.f, back = 1.f;
+    int own = 0;                                           // this row's own position: the last that it sees
+    for (int g = 0;; ++g) {
+      wait(&ctl->head[g % kHeads], (uint32_t)((g / kHeads) & 1));
+      if (dead) break;
+      const Head hd = *head_at(g);
+      if (hd.flags & kEnd) break;
+      const int R = hd.tokens * G;
+      if (hd.flags & kFirst) {
+        // ---------------------------------------------------------- queries to tensor memory (the earlier piece's are read)
+        float q[D / 2];
+        const uint4* src = reinterpret_cast<const uint4*>(c.q + (int64_t)(hd.row0 + row / G) * c.q_stride +
+                                                          (int64_t)(hd.kvh * G + row % G) * D);
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          const uint4 y = row < R ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+          q[4 * i] = __uint_as_float(y.x);
+          q[4 * i + 1] = __uint_as_float(y.y);
+          q[4 * i + 2] = __uint_as_float(y.z);
+          q[4 * i + 3] = __uint_as_float(y.w);
+        }
+        back = 1.f;
+        if (BF16) {
+          float most = 0.f;
+#pragma unroll
+          for (int i = 0; i < D / 2; ++i) {
+            const uint32_t y = __float_as_uint(q[i]);
+            const float x0 = fabsf(widen<true>((uint16_t)y)), x1 = fabsf(widen<true>((uint16_t)(y >> 16)));
+            most = fmax3(most, x0 < INFINITY ? x0 : 0.f, x1 < INFINITY ? x1 : 0.f);
+          }
+          const int e = row_exponent(most);
+          const float f = power_of_two(e);
+          back = power_of_two(-e);
+#pragma unroll
+          for (int i = 0; i < D / 2; ++i) {
+            const uint32_t y = __float_as_uint(q[i]);
+            q[i] = __uint_as_float(pack2<false>(widen<true>((uint16_t)y) * f, widen<true>((uint16_t)(y >> 16)) * f));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i)
+          tm_store<32>(tbase + lanes + S::Q + (uint32_t)(32 * i), *reinterpret_cast<float(*)[32]>(&q[32 * i]));
+        tm_store_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc_mbar_arrive(&ctl->qfull);
+        m = m2 = kNoMax;
+        l = 0.f;
+        own = hd.len - hd.tokens + row / G;
+      }
+      const float4* sc = reinterpret_cast<const float4*>(sm + S::SC_OFF) + g % kHeads * kGroups + copy * NG;
+      wait(&ctl->sfull[g & 1], (uint32_t)((g >> 1) & 1));
+      if (dead) break;
+      const uint32_t tS = tbase + lanes + S::S + (uint32_t)((g & 1) * 128 + copy * COLS);
+      float v[COLS];
+#pragma unroll
+      for (int i = 0; i < COLS / 32; ++i) tm_issue<32>(tS + i * 32, *reinterpret_cast<float(*)[32]>(&v[i * 32]));
+#pragma unroll
+      for (int i = 0; i < COLS / 32; ++i) tm_wait<32>(*reinterpret_cast<float(*)[32]>(&v[i * 32]));
+      // the scores; what the row does not see is minus infinity
+      const bool part = hd.seen != 0xff || (hd.chunk + 1) * kTokens > hd.len - hd.tokens + 1;
+      float mt = -INFINITY, mt2 = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const float4 s4 = sc[i];
+        const float f = s4.x * back;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[16 * i + e] *= f;
+        if (part) {
+          const int upto = s4.w != 0.f ? own + 1 - hd.chunk * kTokens - copy * COLS - 16 * i : 0;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[16 * i + e] = e < upto ? v[16 * i + e] : -INFINITY;
+        }
+        const float* y = v + 16 * i;
+        float x0 = fmax3(y[0], y[1], y[2]), x1 = fmax3(y[3], y[4], y[5]);
+        x0 = fmax3(x0, y[6], y[7]);
+        x1 = fmax3(x1, y[8], y[9]);
+        x0 = fmax3(x0, y[10], y[11]);
+        x1 = fmax3(x1, y[12], y[13]);
+        x0 = fmax3(fmaxf(x0, x1), y[14], y[15]);
+        mt = fmaxf(mt, x0);
+        mt2 = fmaxf(mt2, x0 + s4.z);
+      }
+      const bool raise = __any_sync(0xffffffffu, mt > m + kRaise || mt2 > m2 + kRaise);
+      float w = 1.f;
+      if (raise) {
+        const float nm = fmaxf(m, mt), nm2 = fmaxf(m2, mt2);
+        l *= ex2_approx(m - nm);
+        w = ex2_approx(m2 - nm2);
+        m = nm;
+        m2 = nm2;
+      }
+      // weights
+      const uint64_t off2 = pk2(-m, -m);
+      const float up = m - m2 + kOffset;
+      uint64_t sum2[2] = {0ull, 0ull};
+      float pk[COLS / 2];
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const float4 s4 = sc[i];
+        const float f = ex2_approx(up + s4.z) * s4.y;
+        const uint64_t f2 = pk2(f, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 y = upk2(fadd2(pk2(v[16 * i + 2 * e], v[16 * i + 2 * e + 1]), off2));
+          const uint64_t p = pk2(ex2_approx(y.x), ex2_approx(y.y));
+          sum2[e & 1] = fadd2(sum2[e & 1], p);
+          const float2 z = upk2(fmul2(p, f2));
+          pk[8 * i + e] = __uint_as_float(pack2<false>(z.x, z.y));
+        }
+      }
+      const float2 s0 = upk2(sum2[0]), s1 = upk2(sum2[1]);
+      l += (s0.x + s0.y) + (s1.x + s1.y);
+      // (the tile before this one's weights have been read, and its product added)
+      if (g > 0) wait(&ctl->pvdone, (uint32_t)((g - 1) & 1));
+      if (dead) break;
+      if (raise && !(hd.flags & kFirst)) {
+#pragma unroll 1
+        for (int i = 0; i < D / 32; ++i) {
+          float o[32];
+          tm_load<32>(tO + i * 32, o);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] *= w;
+          tm_store<32>(tO + i * 32, o);
+        }
+      }
+      if constexpr (COLS == 32) {
+        tm_store<16>(tP, pk);
+      } else {
+#pragma unroll
+        for (int i = 0; i < COLS / 64; ++i) tm_store<32>(tP + i * 32, *reinterpret_cast<float(*)[32]>(&pk[i * 32]));
+      }
+      tm_store_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc_mbar_arrive(&ctl->pfull);
+      if (!(hd.flags & kLast)) continue;
+
+      // ------------------------------------------------------------ the end of a piece: the copies added up, 32 dims at a time
+      settle();                                            // (the piece before this one's unit)
+      wait(&ctl->pvdone, (uint32_t)(g & 1));
+      stat[at] = make_float4(m, l, m2, 0.f);
+      meet();
+      if (dead) break;
+      float mx = kNoMax, mx2 = kNoMax, sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < S::COPIES; ++i) {
+        mx = fmaxf(mx, stat[i * S::ROWS + row].x);
+        mx2 = fmaxf(mx2, stat[i * S::ROWS + row].z);
+      }
+#pragma unroll
+      for (int i = 0; i < S::COPIES; ++i) sum += stat[i * S::ROWS + row].y * ex2_approx(stat[i * S::ROWS + row].x - mx);
+      const float fo = ex2_approx(m2 - mx2);
+      const bool whole = hd.flags & kWhole;
+      const int64_t mine = (int64_t)hd.mine * S::ROWS;
+      if (copy == 0) {
+        fin[row] = make_float4(mx, sum, mx2, 0.f);
+        if (!whole && row < R) __stcg(a.part_st + mine + row, make_float4(mx, sum, mx2, 0.f));
+      }
+#pragma unroll 1
+      for (int i = 0; i < D / 32; ++i) {
+        float o[32];
+        tm_load<32>(tO + i * 32, o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          *reinterpret_cast<float4*>(ob + at * S::OROW + 4 * e) =
+              make_float4(o[4 * e] * fo, o[4 * e + 1] * fo, o[4 * e + 2] * fo, o[4 * e + 3] * fo);
+        meet();
+        if (dead) break;
+#pragma unroll 1
+        for (int e = at; e < R * 8; e += kSoftmax) {
+          const int r = e >> 3, d = (e & 7) * 4;
+          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int k = 0; k < S::COPIES; ++k) {
+            const float4 y = *reinterpret_cast<const float4*>(ob + (k * S::ROWS + r) * S::OROW + d);
+            x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+          }
+          if (whole) {
+            const float4 st = fin[r];
+            store_out(hd, r, i * 32 + d, x, st.x, st.y, st.z);
+          } else {
+            __stcg(reinterpret_cast<float4*>(a.part_o + (mine + r) * D + i * 32 + d), x);
+          }
+        }
+        meet();
+        if (dead) break;
+      }
+      if (dead) break;
+      if (!whole) {
+        if (threadIdx.x == 0)
+          asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(ticket) : "l"(a.tickets + hd.unit) : "memory");
+        owed = hd;
+      }
+    }
+    settle();
+  }
+  // teardown: the products issued are complete; after a failure so are the copies (each wait bounded)
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    tc_mbar_wait(&ctl->drained, 0, kRoleWaitNs);
+    if (ctl->fail)
+      for (int x = std::max(0, ctl->loads - S::RAWS); x < ctl->loads; ++x)
+        tc_mbar_wait(&ctl->raw_full[x % S::RAWS], (uint32_t)((x / S::RAWS) & 1), kRoleWaitNs);
+  }
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 9) tc_dealloc(tbase, 512);
+}
+
+// ---------------------------------------------------------------- host side
+int copies_of(const PagedAttnCall& c) {
+  const int64_t R = c.max_rows * (c.s.Hq / c.s.Hkv);
+  return R <= 32 ? 4 : R <= 64 ? 2 : 1;
+}
+
+template <class S, bool BF16>
+cudaError_t launch_shape(const BlockArgs& a, cudaStream_t st) {
+  constexpr int smem = std::max(S::ALLOC, 116 * 1024);      // one CTA an SM: it takes all of the tensor memory
+  const cudaError_t e = cudaFuncSetAttribute(block_kernel<S, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  return e != cudaSuccess ? e : launch_pdl(block_kernel<S, BF16>, dim3(kGrid), dim3(kThreads), smem, st, a);
+}
+template <int FMT, int D, bool BF16>
+cudaError_t launch_c(const BlockArgs& a, cudaStream_t st) {
+  const int copies = copies_of(a.c);
+  if (copies == 4) return launch_shape<BShape<FMT, D, 4>, BF16>(a, st);
+  if (copies == 2) return launch_shape<BShape<FMT, D, 2>, BF16>(a, st);
+  return launch_shape<BShape<FMT, D, 1>, BF16>(a, st);
+}
+template <int FMT>
+cudaError_t launch_f(const BlockArgs& a, cudaStream_t st) {
+  const bool bf16 = a.c.s.dtype == MKV_BF16;
+  if (a.c.s.D == 128) return bf16 ? launch_c<FMT, 128, true>(a, st) : launch_c<FMT, 128, false>(a, st);
+  return bf16 ? launch_c<FMT, 64, true>(a, st) : launch_c<FMT, 64, false>(a, st);
+}
+
+}  // namespace
+
+size_t paged_block_ws_bytes(const PagedAttnCall& c) {
+  const size_t rows = (size_t)kGrid * 2 * (128 / copies_of(c));
+  return kCounterBytes + align256(rows * sizeof(float4)) + align256(rows * c.s.D * sizeof(float));
+}
+
+cudaError_t launch_paged_block(const PagedAttnCall& c, void* ws, cudaStream_t st) {
+  BlockArgs a{};
+  const cudaError_t e = status_word(&a.status);
+  if (e != cudaSuccess) return e;
+  a.c = c;
+  a.w = work_args(c, kGrid);
+  a.G = c.s.Hq / c.s.Hkv;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  a.tickets = reinterpret_cast<int*>(base);
+  a.part_st = reinterpret_cast<float4*>(base + kCounterBytes);
+  a.part_o = reinterpret_cast<float*>(base + kCounterBytes +
+                                      align256((size_t)kGrid * 2 * (128 / copies_of(c)) * sizeof(float4)));
+  return c.s.format == MKV_E4M3 ? launch_f<MKV_E4M3>(a, st) : launch_f<MKV_I8>(a, st);
+}
+
+}  // namespace mkv

@@ -510,10 +510,6 @@ cudaError_t launch_shape(const PagedAttnCall& c, DecodeArgs a, cudaStream_t st) 
 
 }  // namespace
 
-bool paged_decode_countable(const PagedAttnCall& c) {
-  return (int64_t)c.s.B * c.s.Hkv * (ceil_div(c.s.max_pages * c.s.page, kTokens) + 1) <= INT32_MAX / 2;
-}
-
 size_t paged_decode_ws_bytes(const PagedAttnCall& c) {
   return kCounterBytes + align256((size_t)kGrid * 2 * N * sizeof(float4)) + align256((size_t)kGrid * 2 * N * c.s.D * sizeof(float));
 }
