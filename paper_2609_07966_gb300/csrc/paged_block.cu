@@ -11,8 +11,9 @@
 // are added up at the end of a piece.
 //
 // Work is shared out in runs of tiles (mkv_paged_work.cuh).  Roles: one warp finds out its CTA's and loads it (a bulk copy a
-// page), four convert, one issues products, whichever is ready (a finished tile's second product first), four do the softmax
-// of a tile while the next one's scores are computed.
+// page), four convert keys and four values (four for both took 1.4 us a tile, twice what its bytes take), one issues products,
+// whichever is ready (a finished tile's second product first), four do the softmax of a tile while the next one's scores are
+// computed.
 #include <math.h>
 
 #include <algorithm>
@@ -23,13 +24,13 @@ namespace mkv {
 
 namespace {
 
-constexpr int kThreads = 384;       // softmax, conversion, loads + products (+ two idle warps)
-constexpr int kSoftmax = 128;
-// registers a thread: what a launch of kThreads gets (168), and its split
-constexpr int kRegsSoftmax = 208, kRegsConvert = 128;
-static_assert(kRegsSoftmax + kRegsConvert + 168 <= 3 * 168, "register shares");
+// Warpgroups: softmax; conversion of keys; of values; loads + products (+ two idle warps).
+constexpr int kThreads = 512, kSoftmax = 128;
+// registers a thread: what a launch of kThreads gets (128), and its split
+constexpr int kRegsSoftmax = 208, kRegsConvert = 104, kRegsOther = 96;
+static_assert(kRegsSoftmax + 2 * kRegsConvert + kRegsOther <= 4 * 128, "register shares");
 constexpr int kHeads = 8;           // tiles whose heads and scales are held
-constexpr int kSlots = 3;           // widened tiles (K0 V0 K1 V1 ..)
+constexpr int kSlots = 4;           // widened tiles (K0 V0 K1 V1 ..; with three, conversion was part of the products' chain: 50 against 4x us)
 constexpr int kGrid = kNumSMs;
 
 struct BlockArgs {
@@ -47,7 +48,7 @@ struct BShape {
   static constexpr int FMT = FMT_, D = D_, COPIES = COPIES_;
   static constexpr int ROWS = 128 / COPIES, COLS = 128 / COPIES, NG = COLS / 16;   // of a copy; groups of 16 tokens
   static constexpr int KA = D / 64, ATOM = 128 * 128, TILE = KA * ATOM;
-  static constexpr int RAW = kTokens * D, RAWS = D == 128 ? 6 : 8;
+  static constexpr int RAW = kTokens * D, RAWS = D == 128 ? 4 : 8;
   static constexpr int OROW = 36;                          // floats between rows of the join's 32 dims
   static constexpr int T_OFF = 0;                          // [kSlots] widened tiles
   static constexpr int R_OFF = T_OFF + kSlots * TILE;      // [RAWS] codes
@@ -89,8 +90,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
   uint32_t* status = a.status;
   auto head_at = [&](int g) { return reinterpret_cast<Head*>(sm + S::HD_OFF + g % kHeads * 48); };
 
-  if (warp == 9) tc_alloc(&ctl->tslot, 512);
-  if (threadIdx.x == 256) {
+  if (warp == 13) tc_alloc(&ctl->tslot, 512);
+  if (threadIdx.x == 384) {
     for (int s = 0; s < S::RAWS; ++s) {
       tc_mbar_init(&ctl->raw_full[s], 1);
       tc_mbar_init(&ctl->raw_empty[s], 4);
@@ -115,7 +116,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
   pdl_wait_and_trigger();
   const uint32_t tbase = ctl->tslot;
 
-  if (warp == 8) {
+  if (warp >= 12) regs_down<kRegsOther>();
+  if (warp == 12) {
     // ---------------------------------------------------------------- loads
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
@@ -158,7 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         tc_mbar_arrive(&ctl->head[g % kHeads]);
       }
     }
-  } else if (warp == 9) {
+  } else if (warp == 13) {
     if (elect_one()) {
       // ---------------------------------------------------------------- products
       constexpr uint32_t idS = tc_idesc(false, 128, 128, false, false);
@@ -223,57 +225,52 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       }
       tc_commit(&ctl->drained);
     }
-  } else if (warp >= 4 && warp < 8) {
+  } else if (warp >= 4 && warp < 12) {
     regs_down<kRegsConvert>();
-    // ---------------------------------------------------------------- codes to fp16
-    // A thread takes one 16-byte piece of every ROWS'th row.  Eight neighbouring threads read 128 bytes of codes and store
-    // pieces of two atoms, or of two rows, whose banks differ.
-    constexpr int LN = D / 16, STEP = 128 / LN;            // pieces of a row; rows a step
-    const int tid = threadIdx.x - 128, piece = tid % LN, row = tid / LN;
-    // (pieces 4 .. 7 go to the second atom, at the same banks as the first: they store their halves the other way round)
-    const bool swap = piece >= 4;
+    // ---------------------------------------------------------------- codes to fp16: keys (h 0), values (h 1)
+    // A thread takes one 16-byte piece of every STEP'th row.  Of eight neighbouring threads four read the first half of one
+    // row and four the second half of the next: different banks, and so are those of the pieces that they store, in an atom
+    // each (two rows of one atom with 64 dims).
+    constexpr int STEP = D == 128 ? 16 : 32;
+    const int h = warp >= 8 ? 1 : 0, tid = threadIdx.x - 128 - 128 * h;
+    const int piece = D == 128 ? tid & 7 : tid & 3;
+    const int row = D == 128 ? (tid >> 4) * 2 + ((tid >> 2 ^ tid >> 3) & 1) : tid >> 2;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
     };
     for (int g = 0;; ++g) {
       if (!wait(&ctl->head[g % kHeads], (uint32_t)((g / kHeads) & 1))) break;
-      const int flags = head_at(g)->flags;
-      if (flags & kEnd) break;
+      if (head_at(g)->flags & kEnd) break;
       const int seen = head_at(g)->seen, tail = head_at(g)->len - head_at(g)->chunk * kTokens;
-      const bool clean = seen == 0xff && tail >= kTokens;
-      bool ok = true;
-#pragma unroll 1
-      for (int h = 0; ok && h < 2; ++h) {
-        const int item = 2 * g + h, rs = item % S::RAWS, s = item % kSlots;
-        ok = wait(&ctl->raw_full[rs], (uint32_t)((item / S::RAWS) & 1)) &&
-             (item < kSlots || wait(&ctl->tile_empty[s], (uint32_t)((item / kSlots - 1) & 1)));
-        if (!ok) break;
-        const uint8_t* src = sm + S::R_OFF + rs * S::RAW + row * D + piece * 16;
-        uint8_t* dst = sm + S::T_OFF + s * S::TILE + (piece >> 2) * S::ATOM;
-        const bool zeros = h == 1 && !clean;               // what no row sees must not meet a zero weight as NaN
-#pragma unroll 4
-        for (int r = row; r < 128; r += STEP) {
-          uint4 x = *reinterpret_cast<const uint4*>(src + (r - row) * D);
-          if (zeros && (r >= tail || !(seen >> (r >> 4) & 1))) x = make_uint4(0u, 0u, 0u, 0u);
-          uint32_t e[8];
-          widen_codes<S::FMT>(x.x, e[0], e[1]);
-          widen_codes<S::FMT>(x.y, e[2], e[3]);
-          widen_codes<S::FMT>(x.z, e[4], e[5]);
-          widen_codes<S::FMT>(x.w, e[6], e[7]);
-          const uint32_t at = mn_offset<64>(r, 2 * (piece & 3) + (swap ? 1 : 0));
-          *reinterpret_cast<uint4*>(dst + at) =
-              make_uint4(swap ? e[4] : e[0], swap ? e[5] : e[1], swap ? e[6] : e[2], swap ? e[7] : e[3]);
-          *reinterpret_cast<uint4*>(dst + (at ^ 16u)) =
-              make_uint4(swap ? e[0] : e[4], swap ? e[1] : e[5], swap ? e[2] : e[6], swap ? e[3] : e[7]);
-        }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          tc_mbar_arrive(&ctl->tile_full[s]);
-          tc_mbar_arrive(&ctl->raw_empty[rs]);
-        }
+      const int item = 2 * g + h, rs = item % S::RAWS, s = item % kSlots;
+      if (!wait(&ctl->raw_full[rs], (uint32_t)((item / S::RAWS) & 1))) break;
+      if (item >= kSlots && !wait(&ctl->tile_empty[s], (uint32_t)((item / kSlots - 1) & 1))) break;
+      const uint8_t* src = sm + S::R_OFF + rs * S::RAW + row * D + piece * 16;
+      uint8_t* dst = sm + S::T_OFF + s * S::TILE + (piece >> 2) * S::ATOM + row * 128;
+      const uint32_t c0 = (uint32_t)((2 * (piece & 3)) ^ (row & 7)) << 4;
+      uint4 x[128 / STEP];
+#pragma unroll
+      for (int i = 0; i < 128 / STEP; ++i) x[i] = *reinterpret_cast<const uint4*>(src + i * STEP * D);
+      if (h == 1 && (seen != 0xff || tail < kTokens))      // what no row sees must not meet a zero weight as NaN
+#pragma unroll
+        for (int i = 0; i < 128 / STEP; ++i)
+          if (row + i * STEP >= tail || !(seen >> ((row + i * STEP) >> 4) & 1)) x[i] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int i = 0; i < 128 / STEP; ++i) {
+        uint32_t e[8];
+        widen_codes<S::FMT>(x[i].x, e[0], e[1]);
+        widen_codes<S::FMT>(x[i].y, e[2], e[3]);
+        widen_codes<S::FMT>(x[i].z, e[4], e[5]);
+        widen_codes<S::FMT>(x[i].w, e[6], e[7]);
+        *reinterpret_cast<uint4*>(dst + i * STEP * 128 + c0) = make_uint4(e[0], e[1], e[2], e[3]);
+        *reinterpret_cast<uint4*>(dst + i * STEP * 128 + (c0 ^ 16u)) = make_uint4(e[4], e[5], e[6], e[7]);
       }
-      if (!ok) break;
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        tc_mbar_arrive(&ctl->tile_full[s]);
+        tc_mbar_arrive(&ctl->raw_empty[rs]);
+      }
     }
   } else if (warp < 4) {
     regs_up<kRegsSoftmax>();
@@ -336,19 +333,37 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         }
         meet();
         if (dead) return;
-#pragma unroll 2
-        for (int e = at; e < R * (D / 4); e += kSoftmax) { // four dims of a row
-          const int r = e / (D / 4), d = e % (D / 4) * 4;
-          const float4 all = fin[r];
-          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+        constexpr int U = 8;                               // (so many rows' loads under way together)
+#pragma unroll 1
+        for (int e0 = at; e0 < R * (D / 4); e0 += U * kSoftmax) {   // four dims of a row
+          float4 y[U];
+#pragma unroll
+          for (int k = 0; k < U; ++k) y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
           for (int i = 0; i < owed.count; ++i) {
-            const int64_t p = (int64_t)owed.place(i) * S::ROWS + r;
-            const float f = ex2_approx(__ldcg(a.part_st + p).z - all.z);
-            const float4 z = __ldcg(reinterpret_cast<const float4*>(a.part_o + p * D + d));
-            y = make_float4(y.x + f * z.x, y.y + f * z.y, y.z + f * z.z, y.w + f * z.w);
+            float f[U];
+            float4 z[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+              const int e = min(e0 + k * kSoftmax, R * (D / 4) - 1);
+              const int64_t p = (int64_t)owed.place(i) * S::ROWS + e / (D / 4);
+              f[k] = __ldcg(a.part_st + p).z - fin[e / (D / 4)].z;
+              z[k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + p * D + e % (D / 4) * 4));
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+              const float w = ex2_approx(f[k]);
+              y[k] = make_float4(y[k].x + w * z[k].x, y[k].y + w * z[k].y, y[k].z + w * z[k].z, y[k].w + w * z[k].w);
+            }
           }
-          store_out(owed, r, d, y, all.x, all.y, all.z);
+#pragma unroll
+          for (int k = 0; k < U; ++k) {
+            const int e = e0 + k * kSoftmax;
+            if (e < R * (D / 4)) {
+              const float4 all = fin[e / (D / 4)];
+              store_out(owed, e / (D / 4), e % (D / 4) * 4, y[k], all.x, all.y, all.z);
+            }
+          }
         }
       }
       meet();                                              // (before `last` and `fin` are set again)
@@ -570,7 +585,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
   }
   __syncthreads();
   tc_fence_after();
-  if (warp == 9) tc_dealloc(tbase, 512);
+  if (warp == 13) tc_dealloc(tbase, 512);
 }
 
 // ---------------------------------------------------------------- host side
