@@ -35,15 +35,26 @@ inline WorkArgs work_args(const PagedAttnCall& c, int grid) {
 }
 
 enum { kFirst = 1, kLast = 2, kWhole = 4, kEnd = 8 };     // of a piece; the piece is the whole unit; nothing comes any more
-struct Head {
-  int flags, chunk, len, tokens;   // tokens: the entry's new ones
-  int unit, kvh, row0, mine;       // mine: this piece's place
-  int first, place0, count, seen;  // the unit's pieces: the run of the first, its place, how many there are; seen: a bit for
-                                   // each 16 tokens of the chunk that are there
+// What comes with a chunk, and what comes with the first one of a piece.
+struct Chunk {
+  int flags, chunk, copies, scales;  // copies: a bit for each page's copy that is there; scales: where the first one's are
+};
+struct Piece {
+  int len, tokens, unit, kvh;      // tokens: the entry's new ones
+  int row0, mine, first, place0;   // mine: this piece's place; the unit's pieces: the run of the first, its place,
+  int count, pad[3];               // how many there are
   // place of the unit's piece i: runs have two, for their first piece and for their last
   __device__ __forceinline__ int place(int i) const { return i == 0 ? place0 : 2 * (first + i); }
 };
-static_assert(sizeof(Head) == 48, "three 16-byte accesses");
+struct Head {
+  Chunk c;
+  Piece p;
+};
+static_assert(sizeof(Head) == 64, "four 16-byte accesses");
+// Scales of a batch of 32 copies lie together: key factor, value scale as mantissa and exponent.  As many batches are kept
+// as chunks can be between the warp that loads and those that compute (a batch may hold one chunk alone).
+constexpr int kBatches = 8;
+constexpr int kScaleBytes = kBatches * 32 * 16;
 
 struct Entry {
   int row0, tokens, len, chunks;   // its first row, new tokens, tokens held, chunks of a unit
@@ -77,13 +88,13 @@ struct Runs {
   }
 };
 
-// A whole warp goes through this CTA's chunks.  For each piece it calls piece(head), for each chunk
-//   copies(head, id)   id: page of copy `lane` of the chunk (those of the tokens 2^log_box lane ..), -1 where there is none
-//   publish(head, sc)  sc (lane < kGroups): key factor, value scale as mantissa and exponent, of tokens 16 lane ..
-// which say whether to go on; whether all went through.
-template <typename Piece, typename Copies, typename Publish>
-__device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkArgs& w, uint32_t* status, int lane,
-                                             Piece piece, Copies copies, Publish publish) {
+// A whole warp goes through this CTA's chunks.  For each piece it calls piece(p), for each chunk
+//   copies(ch, p, mine, id, at)   lane: whether a copy of the chunk is its own, the copy's page, and its place in the chunk
+//   publish(ch, p)                (after the scales are in place)
+// which say whether to go on; whether all went through.  Little is done a chunk: a warp alone takes 6 cycles an instruction.
+template <typename Begin, typename Copies, typename Publish>
+__device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkArgs& w, uint32_t* status, float4* held_scales,
+                                             int lane, Begin piece, Copies copies, Publish publish) {
   const int B = c.s.B, Hkv = c.s.Hkv;
   uint32_t* report = blockIdx.x == 0 ? status : nullptr;
   Entry held = {0, 0, 0, 0};                               // of entry `lane`
@@ -152,7 +163,7 @@ __device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkA
   };
   // A batch is 32 copies' pages, a lane each: page and scales of the next batch are fetched during this one.
   const int log_per = 7 - w.log_box, span = 32 >> log_per; // copies a chunk, chunks a batch
-  const int group_copy = lane < kGroups ? lane >> (w.log_box - 4) : 0;
+  int batch = -1;
   Entry e = entry(b);
   while (cur < end) {
     while (cur >= base + e.chunks * Hkv) {
@@ -185,17 +196,18 @@ __device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkA
     };
     int pid = fetch(c0), next = 0;
     const bool whole = c1 - c0 == e.chunks;
-    Head hd;
-    hd.len = e.len;
-    hd.tokens = e.tokens;
-    hd.unit = b * Hkv + kvh;
-    hd.kvh = kvh;
-    hd.row0 = e.row0;
-    hd.first = hd.place0 = hd.count = hd.mine = 0;
-    if (!piece(hd)) return false;
+    Piece p;
+    p.len = e.len;
+    p.tokens = e.tokens;
+    p.unit = b * Hkv + kvh;
+    p.kvh = kvh;
+    p.row0 = e.row0;
+    p.first = p.place0 = p.count = p.mine = 0;
+    if (!piece(p)) return false;
     pid = check(c0, pid);
     float ks, vs, nks = 0.f, nvs = 1.f;
     scales(pid, ks, vs);
+    unsigned there = 0;                                    // copies of the batch
     for (int ch = c0; ch < c1; ++ch) {
       const int in = (ch - c0) & (span - 1);
       if (in == 0 && ch > c0) {
@@ -208,29 +220,34 @@ __device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkA
         next = check(ch - in + span, next);
         scales(next, nks, nvs);
       }
-      hd.flags = (ch == c0 ? kFirst : 0) | (ch == c1 - 1 ? kLast : 0) | (whole ? kWhole : 0);
-      hd.chunk = ch;
-      const int id = __shfl_sync(0xffffffffu, pid, ((in << log_per) + lane) & 31);
-      if (!copies(hd, lane < (1 << log_per) ? id : -1)) return false;
+      if (in == 0) {
+        there = __ballot_sync(0xffffffffu, pid >= 0);
+        batch = (batch + 1) % kBatches;
+      }
+      Chunk head;
+      head.flags = (ch == c0 ? kFirst : 0) | (ch == c1 - 1 ? kLast : 0) | (whole ? kWhole : 0);
+      head.chunk = ch;
+      head.copies = (int)(there >> (in << log_per)) & ((1 << (1 << log_per)) - 1);
+      head.scales = batch * 32 + (in << log_per);
+      if (!copies(head, p, pid >= 0 && lane >> log_per == in, pid, lane & ((1 << log_per) - 1))) return false;
+      if (in == 0) {
+        int x;
+        const float mant = frexpf(vs, &x);
+        held_scales[batch * 32 + lane] = make_float4(ks * w.scale_log2, mant, (float)x, 0.f);
+      }
       if (ch == c0 && !whole) {
         if (even) {
-          hd.first = hd.unit * w.parts;
-          hd.place0 = 2 * hd.first;
-          hd.count = (chunks0 + part - 1) / part;
+          p.first = p.unit * w.parts;
+          p.place0 = 2 * p.first;
+          p.count = (chunks0 + part - 1) / part;
         } else {
-          hd.first = rs.of(unit0);
-          hd.place0 = 2 * hd.first + (rs.start(hd.first) < unit0 ? 1 : 0);
-          hd.count = rs.of(unit0 + e.chunks - 1) - hd.first + 1;
+          p.first = rs.of(unit0);
+          p.place0 = 2 * p.first + (rs.start(p.first) < unit0 ? 1 : 0);
+          p.count = rs.of(unit0 + e.chunks - 1) - p.first + 1;
         }
-        hd.mine = r == hd.first ? hd.place0 : 2 * r;
+        p.mine = r == p.first ? p.place0 : 2 * r;
       }
-      const int owner = (in << log_per) + group_copy;
-      const float gk = __shfl_sync(0xffffffffu, ks, owner), gv = __shfl_sync(0xffffffffu, vs, owner);
-      const int gid = __shfl_sync(0xffffffffu, pid, owner);
-      hd.seen = (int)__ballot_sync(0xffffffffu, lane < kGroups && gid >= 0);
-      int x;
-      const float mant = frexpf(gv, &x);
-      publish(hd, make_float4(gk * w.scale_log2, mant, (float)x, gid >= 0 ? 1.f : 0.f));
+      publish(head, p);
     }
   }
   return true;
@@ -239,7 +256,7 @@ __device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkA
 // The pieces' sums of one row, added up in the pieces' order: out = sum_i 2^(m2_i - M2) o_i, with M, sum and M2 of all.
 // VL neighbouring dims a lane; part_o [place][rows][32 VL], part_st [place][rows].
 template <int VL>
-__device__ __forceinline__ float4 add_pieces(const Head& hd, const float* part_o, const float4* part_st, int rows, int row,
+__device__ __forceinline__ float4 add_pieces(const Piece& hd, const float* part_o, const float4* part_st, int rows, int row,
                                              int lane, float& mx, float& sum, float& mx2) {
   mx = mx2 = kNoMax;
   sum = 0.f;

@@ -53,11 +53,12 @@ struct BShape {
   static constexpr int T_OFF = 0;                          // [kSlots] widened tiles
   static constexpr int R_OFF = T_OFF + kSlots * TILE;      // [RAWS] codes
   static constexpr int O_OFF = R_OFF + RAWS * RAW;         // [128][OROW] floats
-  static constexpr int SC_OFF = O_OFF + 128 * OROW * 4;    // [kHeads][8] float4
-  static constexpr int HD_OFF = SC_OFF + kHeads * kGroups * 16;
-  static constexpr int ST_OFF = HD_OFF + kHeads * 48;      // [128] + [ROWS] float4: the lanes', the piece's
+  static constexpr int SC_OFF = O_OFF + 128 * OROW * 4;    // scales of kBatches batches
+  static constexpr int HD_OFF = SC_OFF + kScaleBytes;
+  static constexpr int ST_OFF = HD_OFF + kHeads * 64;      // [128] + [ROWS] float4: the lanes', the piece's
   static constexpr int CTL_OFF = ST_OFF + (128 + ROWS) * 16;
   static constexpr int ALLOC = CTL_OFF + 512 + 1024;       // slack to align the base to 1024 B
+  static_assert(kHeads <= kBatches, "scales are kept");
   static_assert(ALLOC <= 227 * 1024, "shared memory");
   // tensor memory columns
   static constexpr int S = 0, O = 256, P = 384, Q = 448;
@@ -88,7 +89,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
   const int Hkv = c.s.Hkv;
   volatile int* fail = &ctl->fail;
   uint32_t* status = a.status;
-  auto head_at = [&](int g) { return reinterpret_cast<Head*>(sm + S::HD_OFF + g % kHeads * 48); };
+  auto head_at = [&](int g) { return reinterpret_cast<Head*>(sm + S::HD_OFF + g % kHeads * 64); };
 
   if (warp == 13) tc_alloc(&ctl->tslot, 512);
   if (threadIdx.x == 384) {
@@ -115,6 +116,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
   tc_fence_after();
   pdl_wait_and_trigger();
   const uint32_t tbase = ctl->tslot;
+  const int all_copies = (1 << (kTokens >> a.w.log_box)) - 1;
 
   if (warp >= 12) regs_down<kRegsOther>();
   if (warp == 12) {
@@ -125,29 +127,29 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
     int g = 0;
     const int log_box = a.w.log_box;
     const bool ok = work_through(
-        c, a.w, status, lane, [&](const Head&) { return true; },
-        [&](const Head& hd, int id) {
-          const int copies = __popc(__ballot_sync(0xffffffffu, id >= 0));
-          const int64_t from = (((int64_t)id * Hkv + hd.kvh) * c.s.page + ((hd.chunk * kTokens + (lane << log_box)) & (c.s.page - 1))) * D;
+        c, a.w, status, reinterpret_cast<float4*>(sm + S::SC_OFF), lane, [&](const Piece&) { return true; },
+        [&](const Chunk& ch, const Piece& p, bool mine, int id, int at) {
+          const uint32_t bytes = (uint32_t)(__popc(ch.copies) * D) << log_box;
+          const int64_t from = (((int64_t)id * Hkv + p.kvh) * c.s.page + ((ch.chunk * kTokens + (at << log_box)) & (c.s.page - 1))) * D;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const int item = 2 * g + h, s = item % S::RAWS;
             if (item >= S::RAWS && !wait(&ctl->raw_empty[s], (uint32_t)((item / S::RAWS - 1) & 1))) return false;
             if (lane == 0) {
-              tc_mbar_expect_tx(&ctl->raw_full[s], (uint32_t)(copies * D) << log_box);
+              tc_mbar_expect_tx(&ctl->raw_full[s], bytes);
               ctl->loads = item + 1;
             }
             __syncwarp();
-            if (id >= 0)
-              bulk_load(sm + S::R_OFF + s * S::RAW + (lane << log_box) * D, (h == 0 ? c.k : c.v) + from, (uint32_t)D << log_box,
+            if (mine)
+              bulk_load(sm + S::R_OFF + s * S::RAW + (at << log_box) * D, (h == 0 ? c.k : c.v) + from, (uint32_t)D << log_box,
                         &ctl->raw_full[s]);
           }
           return true;
         },
-        [&](const Head& hd, const float4& sc) {
+        [&](const Chunk& ch, const Piece& p) {
           // (its place is free: tile g's codes could only be loaded once tile g - 8 was done with)
-          if (lane < kGroups) reinterpret_cast<float4*>(sm + S::SC_OFF)[g % kHeads * kGroups + lane] = sc;
-          if (lane == 31) *head_at(g) = hd;
+          if (lane == 31) head_at(g)->c = ch;
+          if (lane == 31) head_at(g)->p = p;
           __syncwarp();
           if (lane == 0) tc_mbar_arrive(&ctl->head[g % kHeads]);
           ++g;
@@ -156,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       // (the last head's place: the same reasoning with no codes to wait for needs the wait itself)
       const int item = 2 * g, s = item % S::RAWS;
       if ((item < S::RAWS || wait(&ctl->raw_empty[s], (uint32_t)((item / S::RAWS - 1) & 1))) && lane == 0) {
-        head_at(g)->flags = kEnd;
+        head_at(g)->c.flags = kEnd;
         tc_mbar_arrive(&ctl->head[g % kHeads]);
       }
     }
@@ -173,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       int idle = 0;
       bool ok = true;
       while (ok) {
-        if (flags == 0 && mbar_test(&ctl->head[ts % kHeads], (uint32_t)((ts / kHeads) & 1))) flags = head_at(ts)->flags | 16;
+        if (flags == 0 && mbar_test(&ctl->head[ts % kHeads], (uint32_t)((ts / kHeads) & 1))) flags = head_at(ts)->c.flags | 16;
         if ((flags & kEnd) && tv == ts) break;
         const int ki = 2 * ts, vi = 2 * tv + 1;            // their places in the ring of widened tiles
         const bool can_v = tv < ts && mbar_test(&ctl->pfull, (uint32_t)(tv & 1)) &&
@@ -191,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
           tc_commit(&ctl->tile_empty[vi % kSlots]);
           tc_commit(&ctl->pvdone);
           ++tv;
-          vflags = head_at(tv)->flags;                     // (of a tile whose scores are under way, or looked up below)
+          vflags = head_at(tv)->c.flags;                     // (of a tile whose scores are under way, or looked up below)
         }
         if (can_s) {
           tc_fence_after();
@@ -240,8 +242,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
     };
     for (int g = 0;; ++g) {
       if (!wait(&ctl->head[g % kHeads], (uint32_t)((g / kHeads) & 1))) break;
-      if (head_at(g)->flags & kEnd) break;
-      const int seen = head_at(g)->seen, tail = head_at(g)->len - head_at(g)->chunk * kTokens;
+      if (head_at(g)->c.flags & kEnd) break;
+      const int copies = head_at(g)->c.copies, tail = head_at(g)->p.len - head_at(g)->c.chunk * kTokens;
       const int item = 2 * g + h, rs = item % S::RAWS, s = item % kSlots;
       if (!wait(&ctl->raw_full[rs], (uint32_t)((item / S::RAWS) & 1))) break;
       if (item >= kSlots && !wait(&ctl->tile_empty[s], (uint32_t)((item / kSlots - 1) & 1))) break;
@@ -251,10 +253,10 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       uint4 x[128 / STEP];
 #pragma unroll
       for (int i = 0; i < 128 / STEP; ++i) x[i] = *reinterpret_cast<const uint4*>(src + i * STEP * D);
-      if (h == 1 && (seen != 0xff || tail < kTokens))      // what no row sees must not meet a zero weight as NaN
+      if (h == 1 && (copies != all_copies || tail < kTokens))      // what no row sees must not meet a zero weight as NaN
 #pragma unroll
         for (int i = 0; i < 128 / STEP; ++i)
-          if (row + i * STEP >= tail || !(seen >> ((row + i * STEP) >> 4) & 1)) x[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (row + i * STEP >= tail || !(copies >> ((row + i * STEP) >> a.w.log_box) & 1)) x[i] = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
       for (int i = 0; i < 128 / STEP; ++i) {
         uint32_t e[8];
@@ -297,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
     };
     // An output is o / sum 2^(m2 - m - 6); zeros for a row before position 0, which sees nothing; NaN where no score leaves a
     // weight.
-    auto store_out = [&](const Head& h, int r, int d, float4 x, float mm, float sum, float mm2) {
+    auto store_out = [&](const Piece& h, int r, int d, float4 x, float mm, float sum, float mm2) {
       const float f = half_power(mm, mm2), inv = sum == 0.f ? NAN : 1.f / sum;
       x = make_float4(x.x * inv * f * f, x.y * inv * f * f, x.z * inv * f * f, x.w * inv * f * f);
       if (h.len - h.tokens + r / G < 0) x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -306,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
     };
     // A piece was handed in and the unit's ticket taken (by thread 0, which looks at it only here): the CTA that took the
     // unit's last one adds the pieces up.
-    Head owed;
+    Piece owed;
     owed.count = 0;
     int ticket = 0;
     auto settle = [&]() {
@@ -382,10 +384,11 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
     for (int g = 0;; ++g) {
       wait(&ctl->head[g % kHeads], (uint32_t)((g / kHeads) & 1));
       if (dead) break;
-      const Head hd = *head_at(g);
-      if (hd.flags & kEnd) break;
+      const Chunk now = head_at(g)->c;
+      if (now.flags & kEnd) break;
+      const Piece hd = head_at(g)->p;
       const int R = hd.tokens * G;
-      if (hd.flags & kFirst) {
+      if (now.flags & kFirst) {
         // ---------------------------------------------------------- queries to tensor memory (the earlier piece's are read)
         float q[D / 2];
         const uint4* src = reinterpret_cast<const uint4*>(c.q + (int64_t)(hd.row0 + row / G) * c.q_stride +
@@ -427,7 +430,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         l = 0.f;
         own = hd.len - hd.tokens + row / G;
       }
-      const float4* sc = reinterpret_cast<const float4*>(sm + S::SC_OFF) + g % kHeads * kGroups + copy * NG;
+      const float4* scales = reinterpret_cast<const float4*>(sm + S::SC_OFF) + now.scales;
+      auto copy_of = [&](int i) { return (copy * NG + i) >> (a.w.log_box - 4); };   // that holds group i of this copy's tokens
       wait(&ctl->sfull[g & 1], (uint32_t)((g >> 1) & 1));
       if (dead) break;
       const uint32_t tS = tbase + lanes + S::S + (uint32_t)((g & 1) * 128 + copy * COLS);
@@ -437,16 +441,16 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
 #pragma unroll
       for (int i = 0; i < COLS / 32; ++i) tm_wait<32>(*reinterpret_cast<float(*)[32]>(&v[i * 32]));
       // the scores; what the row does not see is minus infinity
-      const bool part = hd.seen != 0xff || (hd.chunk + 1) * kTokens > hd.len - hd.tokens + 1;
+      const bool part = now.copies != all_copies || (now.chunk + 1) * kTokens > hd.len - hd.tokens + 1;
       float mt = -INFINITY, mt2 = -INFINITY;
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
-        const float4 s4 = sc[i];
+        const float4 s4 = scales[copy_of(i)];
         const float f = s4.x * back;
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[16 * i + e] *= f;
         if (part) {
-          const int upto = s4.w != 0.f ? own + 1 - hd.chunk * kTokens - copy * COLS - 16 * i : 0;
+          const int upto = now.copies >> copy_of(i) & 1 ? own + 1 - now.chunk * kTokens - copy * COLS - 16 * i : 0;
 #pragma unroll
           for (int e = 0; e < 16; ++e) v[16 * i + e] = e < upto ? v[16 * i + e] : -INFINITY;
         }
@@ -476,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       float pk[COLS / 2];
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
-        const float4 s4 = sc[i];
+        const float4 s4 = scales[copy_of(i)];
         const float f = ex2_approx(up + s4.z) * s4.y;
         const uint64_t f2 = pk2(f, f);
 #pragma unroll
@@ -493,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       // (the tile before this one's weights have been read, and its product added)
       if (g > 0) wait(&ctl->pvdone, (uint32_t)((g - 1) & 1));
       if (dead) break;
-      if (raise && !(hd.flags & kFirst)) {
+      if (raise && !(now.flags & kFirst)) {
 #pragma unroll 1
         for (int i = 0; i < D / 32; ++i) {
           float o[32];
@@ -513,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       tc_fence_before();
       __syncwarp();
       if (lane == 0) tc_mbar_arrive(&ctl->pfull);
-      if (!(hd.flags & kLast)) continue;
+      if (!(now.flags & kLast)) continue;
 
       // ------------------------------------------------------------ the end of a piece: the copies added up, 32 dims at a time
       settle();                                            // (the piece before this one's unit)
@@ -530,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
 #pragma unroll
       for (int i = 0; i < S::COPIES; ++i) sum += stat[i * S::ROWS + row].y * ex2_approx(stat[i * S::ROWS + row].x - mx);
       const float fo = ex2_approx(m2 - mx2);
-      const bool whole = hd.flags & kWhole;
+      const bool whole = now.flags & kWhole;
       const int64_t mine = (int64_t)hd.mine * S::ROWS;
       if (copy == 0) {
         fin[row] = make_float4(mx, sum, mx2, 0.f);

@@ -45,15 +45,16 @@ struct DecodeArgs {
 template <int FMT_, int D_>
 struct DShape {
   static constexpr int FMT = FMT_, D = D_, STAGES = D == 128 ? 3 : 6;
-  static constexpr int TILE = kTokens * D, GROUPS = kGroups;
+  static constexpr int TILE = kTokens * D;
   static constexpr int KV_OFF = 0;                         // [STAGES][K, V]
-  static constexpr int SC_OFF = STAGES * 2 * TILE;         // [STAGES][GROUPS] float4: key factor, mantissa and exponent of vs, seen
-  static constexpr int ST_OFF = SC_OFF + STAGES * GROUPS * 16;  // [W + 1][N] float4: the warps', the piece's
+  static constexpr int SC_OFF = STAGES * 2 * TILE;         // scales of kBatches batches
+  static constexpr int ST_OFF = SC_OFF + kScaleBytes;  // [W + 1][N] float4: the warps', the piece's
   static constexpr int HD_OFF = ST_OFF + (W + 1) * N * 16;      // [STAGES] Head
-  static constexpr int Q_OFF = HD_OFF + STAGES * 48;       // [N][D] queries
+  static constexpr int Q_OFF = HD_OFF + STAGES * 64;       // [N][D] queries
   static constexpr int CTL_OFF = Q_OFF + N * D * 2;
   static constexpr int ALLOC = CTL_OFF + 256 + 1024;       // slack to align the base to 1024 B
   static constexpr int OROW = D + 16;                      // floats between rows of the warps' sums
+  static_assert(STAGES < kBatches, "scales are kept");
   static_assert(kCtas * (ALLOC + 1024) <= 228 * 1024, "shared memory");
   static_assert(W * N * OROW * 4 <= 2 * TILE, "room for the warps' sums in a stage");
 };
@@ -116,49 +117,49 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     };
     const int log_box = a.w.log_box;
     bool ok = work_through(
-        c, a.w, status, lane,
-        [&](const Head& hd) {                              // a piece's queries: one copy a token's heads
+        c, a.w, status, reinterpret_cast<float4*>(sm + S::SC_OFF), lane,
+        [&](const Piece& p) {                              // a piece's queries: one copy a token's heads
           if (pieces > 0 && !wait(&ctl->qempty, (uint32_t)((pieces - 1) & 1))) return false;
           const int bytes = a.G * D * 2;
           if (lane == 0) {
-            tc_mbar_expect_tx(&ctl->qfull, (uint32_t)(hd.tokens * bytes));
+            tc_mbar_expect_tx(&ctl->qfull, (uint32_t)(p.tokens * bytes));
             ctl->q_loads = pieces + 1;
           }
           __syncwarp();
-          if (lane < hd.tokens)
-            bulk_load(sm + S::Q_OFF + lane * bytes, c.q + (int64_t)(hd.row0 + lane) * c.q_stride + (int64_t)hd.kvh * a.G * D,
+          if (lane < p.tokens)
+            bulk_load(sm + S::Q_OFF + lane * bytes, c.q + (int64_t)(p.row0 + lane) * c.q_stride + (int64_t)p.kvh * a.G * D,
                       bytes, &ctl->qfull);
           ++pieces;
           return true;
         },
-        [&](const Head& hd, int id) {
+        [&](const Chunk& ch, const Piece& p, bool mine, int id, int at) {
           if (!free_stage()) return false;
-          const int s = g % S::STAGES, copies = __popc(__ballot_sync(0xffffffffu, id >= 0));
+          const int s = g % S::STAGES;
           if (lane == 0) {
-            tc_mbar_expect_tx(&ctl->full[s], (uint32_t)(copies * 2 * D) << log_box);
+            tc_mbar_expect_tx(&ctl->full[s], (uint32_t)(__popc(ch.copies) * 2 * D) << log_box);
             ctl->loads = g + 1;
           }
           __syncwarp();
-          if (id >= 0) {
-            uint8_t* dst = sm + S::KV_OFF + s * 2 * S::TILE + (lane << log_box) * D;
-            const int y = (hd.chunk * kTokens + (lane << log_box)) & (c.s.page - 1), z = id * Hkv + hd.kvh;
+          if (mine) {
+            uint8_t* dst = sm + S::KV_OFF + s * 2 * S::TILE + (at << log_box) * D;
+            const int y = (ch.chunk * kTokens + (at << log_box)) & (c.s.page - 1), z = id * Hkv + p.kvh;
             tma_load_4d(dst, &kmap, 0, y, z, 0, &ctl->full[s]);
             tma_load_4d(dst + S::TILE, &vmap, 0, y, z, 0, &ctl->full[s]);
           }
           return true;
         },
-        [&](const Head& hd, const float4& sc) {
-          const int s = g % S::STAGES;
-          if (lane < S::GROUPS) reinterpret_cast<float4*>(sm + S::SC_OFF)[s * S::GROUPS + lane] = sc;
-          if (lane == 31) *reinterpret_cast<Head*>(sm + S::HD_OFF + s * 48) = hd;
+        [&](const Chunk& ch, const Piece& p) {
+          Head* hd = reinterpret_cast<Head*>(sm + S::HD_OFF + g % S::STAGES * 64);
+          if (lane == 31) hd->c = ch;
+          if (lane == 31 && (ch.flags & kFirst)) hd->p = p;
           __syncwarp();
-          if (lane == 0) tc_mbar_arrive(&ctl->full[s]);
+          if (lane == 0) tc_mbar_arrive(&ctl->full[g % S::STAGES]);
           ++g;
         });
     if (ok && free_stage()) {
       const int s = g % S::STAGES;
       if (lane == 0) {
-        reinterpret_cast<Head*>(sm + S::HD_OFF + s * 48)->flags = kEnd;
+        reinterpret_cast<Head*>(sm + S::HD_OFF + s * 64)->c.flags = kEnd;
         tc_mbar_arrive(&ctl->full[s]);
         tc_mbar_arrive(&ctl->full[s]);
       }
@@ -183,10 +184,10 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     };
     // An output is o / sum 2^(m2 - m - 6); zeros for a row before position 0, which sees nothing; NaN where no score leaves a
     // weight.
-    auto out_row = [&](const Head& h, int row) {
+    auto out_row = [&](const Piece& h, int row) {
       return c.out + (int64_t)(h.row0 + row / G) * c.out_stride + (int64_t)(h.kvh * G + row % G) * D;
     };
-    auto finish = [&](const Head& h, int row, float4 x, float mm, float sum, float mm2) {
+    auto finish = [&](const Piece& h, int row, float4 x, float mm, float sum, float mm2) {
       const float f = half_power(mm, mm2), inv = sum == 0.f ? NAN : 1.f / sum;
       x = make_float4(x.x * inv * f * f, x.y * inv * f * f, x.z * inv * f * f, x.w * inv * f * f);
       if (h.len - h.tokens + row / G < 0) x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -195,7 +196,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     };
     // A piece was handed in and the unit's ticket taken (by thread 0, which looks at it only here): the CTA that took the
     // unit's last one adds the pieces up.
-    Head owed;
+    Piece owed;
     owed.count = 0;
     int ticket = 0;
     auto settle = [&]() {
@@ -226,6 +227,8 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     uint32_t qf[2 * KS];
     float back[2], o[MB][4], m[2], m2[2], l[2];
     int pos0 = 0, pieces = 0;
+    Piece hd;
+    hd.len = hd.tokens = 0;
     // where this lane's pieces of a key row and of two value rows lie; further rows are whole swizzle periods away
     uint32_t kofs[D / 64], vofs[2];
 #pragma unroll
@@ -237,9 +240,11 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       const int s = g % S::STAGES;
       wait(&ctl->full[s], (uint32_t)((g / S::STAGES) & 1));
       if (dead) break;
-      const Head hd = *reinterpret_cast<const Head*>(sm + S::HD_OFF + s * 48);
-      if (hd.flags & kEnd) break;
-      if (hd.flags & kFirst) {
+      const Head* from = reinterpret_cast<const Head*>(sm + S::HD_OFF + s * 64);
+      const Chunk now = from->c;
+      if (now.flags & kEnd) break;
+      if (now.flags & kFirst) {
+        hd = from->p;
         // ---------------------------------------------------------- queries: row lg, dims D / 4 lr ..
         wait(&ctl->qfull, (uint32_t)(pieces & 1));
         if (dead) break;
@@ -283,11 +288,12 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         pos0 = hd.len - hd.tokens;                         // the first new token's position
       }
       {
-        const int ch = hd.chunk;
+        const int ch = now.chunk;
         const int t0 = ch * kTokens + warp * 32;
-        const float4* scales = reinterpret_cast<const float4*>(sm + S::SC_OFF) + s * S::GROUPS + warp * 2;
-        const float4 sc[2] = {scales[0], scales[1]};
-        const bool in[2] = {sc[0].w != 0.f && t0 < hd.len, sc[1].w != 0.f && t0 + 16 < hd.len};
+        const float4* scales = reinterpret_cast<const float4*>(sm + S::SC_OFF) + now.scales;
+        const int cp[2] = {(warp * 2) >> (a.w.log_box - 4), (warp * 2 + 1) >> (a.w.log_box - 4)};   // the groups' copies
+        const float4 sc[2] = {scales[cp[0]], scales[cp[1]]};
+        const bool in[2] = {(now.copies >> cp[0] & 1) != 0 && t0 < hd.len, (now.copies >> cp[1] & 1) != 0 && t0 + 16 < hd.len};
         if (in[0] || in[1]) {
           const uint8_t* K = sm + S::KV_OFF + s * 2 * S::TILE + warp * 32 * D;
           const uint8_t* V = K + S::TILE;
@@ -412,9 +418,9 @@ __global__ void __launch_bounds__(kThreads, kCtas)
               }
         }
         __syncwarp();
-        if (lane == 0 && !(hd.flags & kLast)) tc_mbar_arrive(&ctl->empty[s]);
+        if (lane == 0 && !(now.flags & kLast)) tc_mbar_arrive(&ctl->empty[s]);
       }
-      if (!(hd.flags & kLast)) continue;
+      if (!(now.flags & kLast)) continue;
       settle();                                            // (the piece before this one's unit)
       // ------------------------------------------------------------ the warps' parts joined, in their order
       // (As few instructions as will do: code that runs once a piece comes from a cold instruction cache.)
@@ -452,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       if (dead) break;
       // ------------------------------------------------------------ outputs, or a piece for the unit's last CTA
       const int R = hd.tokens * G;
-      const bool whole = hd.flags & kWhole;
+      const bool whole = now.flags & kWhole;
       const int64_t mine = (int64_t)hd.mine * N;
 #pragma unroll 1
       for (int e = threadIdx.x; e < R * (D / 4); e += kComputing) {
