@@ -51,10 +51,10 @@ struct Head {
   Piece p;
 };
 static_assert(sizeof(Head) == 64, "four 16-byte accesses");
-// Scales of a batch of 32 copies lie together: key factor, value scale as mantissa and exponent.  As many batches are kept
-// as chunks can be between the warp that loads and those that compute (a batch may hold one chunk alone).
+// Scales of a batch of 32 copies lie together: key factor, value scale as mantissa and exponent.  Of several pieces as many
+// batches are kept as chunks can be between the warp that loads and those that compute (a batch may hold one chunk alone).
 constexpr int kBatches = 8;
-constexpr int kScaleBytes = kBatches * 32 * 16;
+constexpr int scale_bytes(int batches) { return batches * 32 * 16; }
 
 struct Entry {
   int row0, tokens, len, chunks;   // its first row, new tokens, tokens held, chunks of a unit
@@ -88,13 +88,83 @@ struct Runs {
   }
 };
 
-// A whole warp goes through this CTA's chunks.  For each piece it calls piece(p), for each chunk
-//   copies(ch, p, mine, id, at)   lane: whether a copy of the chunk is its own, the copy's page, and its place in the chunk
-//   publish(ch, p)                (after the scales are in place)
-// which say whether to go on; whether all went through.  Little is done a chunk: a warp alone takes 6 cycles an instruction.
+// A whole warp goes through chunks c0 .. c1 - 1 of entry b's key head.  It calls begin() once the first pages are being
+// fetched, and for each chunk
+//   copies(ch, mine, id, at)   lane: whether a copy of the chunk is its own, the copy's page, and its place in the chunk
+//   publish(ch)                (after the scales are in place)
+// of which the first two say whether to go on; whether all went through.  `batch`: how many batches were begun before.  Little
+// is done a chunk: a warp alone takes 6 cycles an instruction.
+template <int BATCHES, typename Begin, typename Copies, typename Publish>
+__device__ __forceinline__ bool load_chunks(const PagedAttnCall& c, const WorkArgs& w, uint32_t* status, float4* held_scales,
+                                            int lane, int& batch, int b, int kvh, int len, int c0, int c1, int flags,
+                                            Begin begin, Copies copies, Publish publish) {
+  // A batch is 32 copies' pages, a lane each: page and scales of the next batch are fetched during this one.
+  const int log_per = 7 - w.log_box, span = 32 >> log_per; // copies a chunk, chunks a batch
+  const int32_t* table = c.s.page_table + (int64_t)b * c.s.max_pages;
+  auto exists = [&](int chunk) {                           // this lane's copy of the batch from `chunk` on
+    return chunk + (lane >> log_per) < c1 && chunk * kTokens + (lane << w.log_box) < len;
+  };
+  auto fetch = [&](int chunk) {
+    return exists(chunk) ? table[(chunk * kTokens + (lane << w.log_box)) >> w.log_page] : -1;
+  };
+  auto check = [&](int chunk, int id) {                    // (a page outside the pool is not seen)
+    if (!exists(chunk)) return -1;
+    if (id >= 0 && id < c.s.num_pages) return id;
+    atomicOr(status, MKV_FLAG_BAD_INDEX);
+    return -1;
+  };
+  auto scales = [&](int id, float& ks, float& vs) {
+    ks = 0.f;
+    vs = 1.f;
+    if (id >= 0) {
+      ks = c.k_scale[(int64_t)id * c.s.Hkv + kvh];
+      vs = c.v_scale[(int64_t)id * c.s.Hkv + kvh];
+    }
+  };
+  int pid = fetch(c0), next = 0;
+  if (!begin()) return false;
+  pid = check(c0, pid);
+  float ks, vs, nks = 0.f, nvs = 1.f;
+  scales(pid, ks, vs);
+  unsigned there = 0;                                      // copies of the batch
+  int at = 0;                                              // its place among the scales
+  for (int ch = c0; ch < c1; ++ch) {
+    const int in = (ch - c0) & (span - 1);
+    if (in == 0 && ch > c0) {
+      pid = next;
+      ks = nks;
+      vs = nvs;
+    }
+    if (in == 0) next = fetch(ch + span);
+    if (in == span / 2) {
+      next = check(ch - in + span, next);
+      scales(next, nks, nvs);
+    }
+    if (in == 0) {
+      there = __ballot_sync(0xffffffffu, pid >= 0);
+      at = batch++ % BATCHES * 32;
+    }
+    Chunk head;
+    head.flags = (ch == c0 ? kFirst : 0) | (ch == c1 - 1 ? kLast : 0) | flags;
+    head.chunk = ch;
+    head.copies = (int)(there >> (in << log_per)) & ((1 << (1 << log_per)) - 1);
+    head.scales = at + (in << log_per);
+    if (!copies(head, pid >= 0 && lane >> log_per == in, pid, lane & ((1 << log_per) - 1))) return false;
+    if (in == 0) {
+      int x;
+      const float mant = frexpf(vs, &x);
+      held_scales[at + lane] = make_float4(ks * w.scale_log2, mant, (float)x, 0.f);
+    }
+    publish(head);
+  }
+  return true;
+}
+
+// A whole warp goes through this CTA's chunks: load_chunks for each piece, with begin(p), copies(ch, p, mine, id, at) and
+// publish(ch, p); whether all went through.
 template <typename Begin, typename Copies, typename Publish>
 __device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkArgs& w, uint32_t* status, float4* held_scales,
-                                             int lane, Begin piece, Copies copies, Publish publish) {
+                                             int lane, Begin begin, Copies copies, Publish publish) {
   const int B = c.s.B, Hkv = c.s.Hkv;
   uint32_t* report = blockIdx.x == 0 ? status : nullptr;
   Entry held = {0, 0, 0, 0};                               // of entry `lane`
@@ -161,9 +231,7 @@ __device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkA
     e.chunks = __shfl_sync(0xffffffffu, held.chunks, i);
     return e;
   };
-  // A batch is 32 copies' pages, a lane each: page and scales of the next batch are fetched during this one.
-  const int log_per = 7 - w.log_box, span = 32 >> log_per; // copies a chunk, chunks a batch
-  int batch = -1;
+  int batch = 0;
   Entry e = entry(b);
   while (cur < end) {
     while (cur >= base + e.chunks * Hkv) {
@@ -173,28 +241,6 @@ __device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkA
     const int kvh = (cur - base) / e.chunks, unit0 = base + kvh * e.chunks;
     const int c0 = cur - unit0, c1 = min(e.chunks, c0 + (end - cur));
     cur += c1 - c0;
-    const int32_t* table = c.s.page_table + (int64_t)b * c.s.max_pages;
-    auto exists = [&](int chunk) {                         // this lane's copy of the batch from `chunk` on
-      return chunk + (lane >> log_per) < c1 && chunk * kTokens + (lane << w.log_box) < e.len;
-    };
-    auto fetch = [&](int chunk) {
-      return exists(chunk) ? table[(chunk * kTokens + (lane << w.log_box)) >> w.log_page] : -1;
-    };
-    auto check = [&](int chunk, int id) {                  // (a page outside the pool is not seen)
-      if (!exists(chunk)) return -1;
-      if (id >= 0 && id < c.s.num_pages) return id;
-      atomicOr(status, MKV_FLAG_BAD_INDEX);
-      return -1;
-    };
-    auto scales = [&](int id, float& ks, float& vs) {
-      ks = 0.f;
-      vs = 1.f;
-      if (id >= 0) {
-        ks = c.k_scale[(int64_t)id * Hkv + kvh];
-        vs = c.v_scale[(int64_t)id * Hkv + kvh];
-      }
-    };
-    int pid = fetch(c0), next = 0;
     const bool whole = c1 - c0 == e.chunks;
     Piece p;
     p.len = e.len;
@@ -203,52 +249,25 @@ __device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkA
     p.kvh = kvh;
     p.row0 = e.row0;
     p.first = p.place0 = p.count = p.mine = 0;
-    if (!piece(p)) return false;
-    pid = check(c0, pid);
-    float ks, vs, nks = 0.f, nvs = 1.f;
-    scales(pid, ks, vs);
-    unsigned there = 0;                                    // copies of the batch
-    for (int ch = c0; ch < c1; ++ch) {
-      const int in = (ch - c0) & (span - 1);
-      if (in == 0 && ch > c0) {
-        pid = next;
-        ks = nks;
-        vs = nvs;
-      }
-      if (in == 0) next = fetch(ch + span);
-      if (in == span / 2) {
-        next = check(ch - in + span, next);
-        scales(next, nks, nvs);
-      }
-      if (in == 0) {
-        there = __ballot_sync(0xffffffffu, pid >= 0);
-        batch = (batch + 1) % kBatches;
-      }
-      Chunk head;
-      head.flags = (ch == c0 ? kFirst : 0) | (ch == c1 - 1 ? kLast : 0) | (whole ? kWhole : 0);
-      head.chunk = ch;
-      head.copies = (int)(there >> (in << log_per)) & ((1 << (1 << log_per)) - 1);
-      head.scales = batch * 32 + (in << log_per);
-      if (!copies(head, p, pid >= 0 && lane >> log_per == in, pid, lane & ((1 << log_per) - 1))) return false;
-      if (in == 0) {
-        int x;
-        const float mant = frexpf(vs, &x);
-        held_scales[batch * 32 + lane] = make_float4(ks * w.scale_log2, mant, (float)x, 0.f);
-      }
-      if (ch == c0 && !whole) {
-        if (even) {
-          p.first = p.unit * w.parts;
-          p.place0 = 2 * p.first;
-          p.count = (chunks0 + part - 1) / part;
-        } else {
-          p.first = rs.of(unit0);
-          p.place0 = 2 * p.first + (rs.start(p.first) < unit0 ? 1 : 0);
-          p.count = rs.of(unit0 + e.chunks - 1) - p.first + 1;
-        }
-        p.mine = r == p.first ? p.place0 : 2 * r;
-      }
-      publish(head, p);
-    }
+    const bool ok = load_chunks<kBatches>(
+        c, w, status, held_scales, lane, batch, b, kvh, e.len, c0, c1, whole ? kWhole : 0, [&]() { return begin(p); },
+        [&](const Chunk& ch, bool mine, int id, int at) { return copies(ch, p, mine, id, at); },
+        [&](const Chunk& ch) {
+          if (ch.chunk == c0 && !whole) {
+            if (even) {
+              p.first = p.unit * w.parts;
+              p.place0 = 2 * p.first;
+              p.count = (chunks0 + part - 1) / part;
+            } else {
+              p.first = rs.of(unit0);
+              p.place0 = 2 * p.first + (rs.start(p.first) < unit0 ? 1 : 0);
+              p.count = rs.of(unit0 + e.chunks - 1) - p.first + 1;
+            }
+            p.mine = r == p.first ? p.place0 : 2 * r;
+          }
+          publish(ch, p);
+        });
+    if (!ok) return false;
   }
   return true;
 }

@@ -54,7 +54,7 @@ struct BShape {
   static constexpr int R_OFF = T_OFF + kSlots * TILE;      // [RAWS] codes
   static constexpr int O_OFF = R_OFF + RAWS * RAW;         // [128][OROW] floats
   static constexpr int SC_OFF = O_OFF + 128 * OROW * 4;    // scales of kBatches batches
-  static constexpr int HD_OFF = SC_OFF + kScaleBytes;
+  static constexpr int HD_OFF = SC_OFF + scale_bytes(kBatches);
   static constexpr int ST_OFF = HD_OFF + kHeads * 64;      // [128] + [ROWS] float4: the lanes', the piece's
   static constexpr int CTL_OFF = ST_OFF + (128 + ROWS) * 16;
   static constexpr int ALLOC = CTL_OFF + 512 + 1024;       // slack to align the base to 1024 B

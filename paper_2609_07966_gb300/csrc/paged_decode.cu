@@ -48,7 +48,7 @@ struct DShape {
   static constexpr int TILE = kTokens * D;
   static constexpr int KV_OFF = 0;                         // [STAGES][K, V]
   static constexpr int SC_OFF = STAGES * 2 * TILE;         // scales of kBatches batches
-  static constexpr int ST_OFF = SC_OFF + kScaleBytes;  // [W + 1][N] float4: the warps', the piece's
+  static constexpr int ST_OFF = SC_OFF + scale_bytes(kBatches);  // [W + 1][N] float4: the warps', the piece's
   static constexpr int HD_OFF = ST_OFF + (W + 1) * N * 16;      // [STAGES] Head
   static constexpr int Q_OFF = HD_OFF + STAGES * 64;       // [N][D] queries
   static constexpr int CTL_OFF = Q_OFF + N * D * 2;

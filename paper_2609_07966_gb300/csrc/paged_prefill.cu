@@ -6,9 +6,11 @@
 // the other is in its softmax.
 //   S_i [128 x 128] = Q_i K^T    fp16 operands in shared memory, accumulator in tensor memory
 //   O_i [128 x D]  += W_i V      W_i (the weights, fp16) from tensor memory, over the S_i they came from
-// The tensor cores have no product of 16-bit queries with 8-bit codes, so one warpgroup widens every tile's codes to fp16
-// (exactly) on their way into shared memory: plain 16-byte loads, eight of the next operand always under way, then the
-// swizzled layout that the products read.  Once a tile serves 256 rows its conversion is an eighth of the products' time.
+// The tensor cores have no product of 16-bit queries with 8-bit codes, so every tile's codes are widened to fp16 (exactly) on
+// their way: one warp loads them (a bulk copy a page) into a ring, one warpgroup reads them there and writes the swizzled
+// layout that the products read.  Once a tile serves 256 rows its conversion is a quarter of the products' time.  (Without
+// the ring, codes in the converting threads' registers eight loads ahead, the loads' latency made it the bottleneck: a
+// prompt of 4096 tokens 156 us.)
 //
 // A tile's pages have scales of their own: within 16 columns both are constant, so a score's is part of the factor of its
 // exponent, the maxima are kept per 16 columns until they are scaled, and a weight is p vs 2^(m - m2 + 6).
@@ -18,7 +20,7 @@
 
 #include <algorithm>
 
-#include "mkv_paged.cuh"
+#include "mkv_paged_work.cuh"
 
 namespace mkv {
 
@@ -28,16 +30,19 @@ constexpr int kBR = 128;            // rows a block, tokens a tile
 constexpr int kRows = 2 * kBR;      // rows a unit
 // Up to this maximum (log2) an unrounded product of score and scale is within a half of the rounded one.
 constexpr float kFused = 16777216.f;
-constexpr int kThreads = 512;       // two softmax warpgroups, one that converts, one whose first warp issues products
-constexpr int kRegsSoftmax = 192, kRegsConvert = 80, kRegsIssue = 48;
-static_assert(2 * kRegsSoftmax + kRegsConvert + kRegsIssue <= 4 * 128, "register shares");
-constexpr int kScales = 4;          // tiles whose scales are held
+constexpr int kThreads = 512;       // two softmax warpgroups, one that converts, one for products and loads (two warps idle)
+constexpr int kRegsSoftmax = 184, kRegsConvert = 72, kRegsOther = 72;
+static_assert(2 * kRegsSoftmax + kRegsConvert + kRegsOther <= 4 * 128, "register shares");
+constexpr int kHeads = 8;           // tiles whose heads and scales are held
+constexpr int kSlots = 3;           // widened tiles (K0 V0 K1 V1 ..)
+constexpr int kHeldBatches = 4;     // (a tile is one of at least four of a batch)
+static_assert(kBR == kTokens && kHeads <= (kHeldBatches - 1) * 4, "tiles are chunks; scales are kept");
 
 struct PrefillArgs {
   PagedAttnCall c;
   uint32_t* status;
   int G;
-  float scale_log2;
+  WorkArgs w;
   int64_t slots;                    // units of all entries, a key head's
   int per;                          // start null: units of an entry
   int splits;                       // parts of a unit's tokens
@@ -49,20 +54,24 @@ template <int FMT_, int D_>
 struct PShape {
   static constexpr int FMT = FMT_, D = D_, KA = D / 64;
   static constexpr int ATOM = kBR * 128, TILE = KA * ATOM, QBLK = TILE;
-  static constexpr int Q_OFF = 0, R_OFF = 2 * QBLK;        // ring: K, V of even tiles, then of odd ones
-  static constexpr int SC_OFF = R_OFF + 4 * TILE;          // [kScales][8] float4: key factor, vs mantissa, exponent, seen
-  static constexpr int QS_OFF = SC_OFF + kScales * 8 * 16; // [256] floats
-  static constexpr int CTL_OFF = QS_OFF + kRows * 4;
-  static constexpr int ALLOC = CTL_OFF + 256 + 1024;
+  static constexpr int RAW = kBR * D, RAWS = 4;            // codes of a tile's keys or values
+  static constexpr int Q_OFF = 0, T_OFF = 2 * QBLK;        // [kSlots] widened tiles
+  static constexpr int R_OFF = T_OFF + kSlots * TILE;      // [RAWS] codes
+  static constexpr int SC_OFF = R_OFF + RAWS * RAW;        // scales of kHeldBatches batches
+  static constexpr int HD_OFF = SC_OFF + scale_bytes(kHeldBatches);   // [kHeads] Chunk
+  static constexpr int QS_OFF = HD_OFF + kHeads * 16;      // [256] exponents that bf16 rows are scaled by
+  static constexpr int CTL_OFF = QS_OFF + kRows;
+  static constexpr int ALLOC = CTL_OFF + 512;
   static_assert(ALLOC <= 227 * 1024, "shared memory");
 };
 
 struct PCtl {
-  uint64_t qfull, drained, kfull[2], kempty[2], vfull[2], vempty[2], sfull[2], pfull[2][2], pvdone[2];
+  uint64_t qfull, drained, raw_full[4], raw_empty[4], tile_full[kSlots], tile_empty[kSlots], head[kHeads], sfull[2], pfull[2][2],
+      pvdone[2];
   uint32_t tslot;
-  int fail;
+  int fail, loads;
 };
-static_assert(sizeof(PCtl) <= 256, "control block");
+static_assert(sizeof(PCtl) <= 512, "control block");
 
 // Units lie entry after entry, enough of them for each entry's rows.
 __device__ __forceinline__ int64_t unit_base(const PrefillArgs& a, int b) {
@@ -108,12 +117,11 @@ __device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
 template <class S, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs a) {
   constexpr int D = S::D;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* sm = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+  extern __shared__ __align__(1024) uint8_t sm[];
   PCtl* ctl = reinterpret_cast<PCtl*>(sm + S::CTL_OFF);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const PagedAttnCall& c = a.c;
-  const int Hkv = c.s.Hkv, page = c.s.page;
+  const int Hkv = c.s.Hkv;
 
   pdl_wait_and_trigger();
   // Launch order: the last rows of the entries first (they see the most), all key heads and parts of a slot together.
@@ -137,42 +145,49 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
   if (threadIdx.x == 0) {
     tc_mbar_init(&ctl->qfull, 8);
     tc_mbar_init(&ctl->drained, 1);
+    for (int s = 0; s < S::RAWS; ++s) {
+      tc_mbar_init(&ctl->raw_full[s], 1);
+      tc_mbar_init(&ctl->raw_empty[s], 4);
+    }
+    for (int s = 0; s < kSlots; ++s) {
+      tc_mbar_init(&ctl->tile_full[s], 4);
+      tc_mbar_init(&ctl->tile_empty[s], 1);
+    }
+    for (int s = 0; s < kHeads; ++s) tc_mbar_init(&ctl->head[s], 1);
     for (int s = 0; s < 2; ++s) {
-      tc_mbar_init(&ctl->kfull[s], 4);
-      tc_mbar_init(&ctl->vfull[s], 4);
-      tc_mbar_init(&ctl->kempty[s], 1);
-      tc_mbar_init(&ctl->vempty[s], 1);
       tc_mbar_init(&ctl->sfull[s], 1);
       tc_mbar_init(&ctl->pfull[s][0], 4);
       tc_mbar_init(&ctl->pfull[s][1], 4);
       tc_mbar_init(&ctl->pvdone[s], 1);
     }
     tc_fence_mbar_init();
-    ctl->fail = 0;
+    ctl->fail = ctl->loads = 0;
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tbase = ctl->tslot;
   volatile int* fail = &ctl->fail;
+  Chunk* heads = reinterpret_cast<Chunk*>(sm + S::HD_OFF);
   uint32_t* status = a.status;
+  const int all_copies = (1 << (kTokens >> a.w.log_box)) - 1;
 
   if (warp >= 12) {
-    regs_down<kRegsIssue>();
+    regs_down<kRegsOther>();
     if (warp == 12 && elect_one()) {
       // ---------------------------------------------------------------- products
       constexpr uint32_t idS = tc_idesc(false, kBR, kBR, false, false);
       constexpr uint32_t idO = tc_idesc(false, kBR, D, false, true);
       const Desc qd = tc_desc_sw128(smem_addr(sm + S::Q_OFF));
-      const Desc kd = tc_desc_sw128(smem_addr(sm + S::R_OFF));
-      const Desc vd = tc_desc_mn<64>(smem_addr(sm + S::R_OFF), S::ATOM);
+      const Desc kd = tc_desc_sw128(smem_addr(sm + S::T_OFF));
+      const Desc vd = tc_desc_mn<64>(smem_addr(sm + S::T_OFF), S::ATOM);
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         const bool ok = wait_or_fail(bar, parity, fail, status);
         tc_fence_after();
         return ok;
       };
       auto scores = [&](int k, int t) {
-        const Desc q0 = qd.at(k * S::QBLK).opaque(), k0 = kd.at((t & 1) * 2 * S::TILE).opaque();
+        const Desc q0 = qd.at(k * S::QBLK).opaque(), k0 = kd.at(2 * t % kSlots * S::TILE).opaque();
 #pragma unroll
         for (int j = 0; j < S::KA * 4; ++j)
           tc_mma_ss(tbase + (uint32_t)(k * kBR), q0.at((j >> 2) * S::ATOM + (j & 3) * 32),
@@ -180,21 +195,22 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         tc_commit(&ctl->sfull[k]);
       };
       auto values = [&](int k, int t, int half) {           // over half of tile t's tokens
-        const Desc v0 = vd.at(((t & 1) * 2 + 1) * S::TILE + half * (kBR / 2) * 128).opaque();
+        const Desc v0 = vd.at((2 * t + 1) % kSlots * S::TILE + half * (kBR / 2) * 128).opaque();
         const uint32_t p0 = tbase + (uint32_t)(k * kBR + half * (kBR / 4));
 #pragma unroll
         for (int kk = 0; kk < kBR / 32; ++kk)
           tc_mma_ts(tbase + (uint32_t)(2 * kBR + k * kBR), p0 + (uint32_t)(kk * 8), v0.at(kk * 2048), idO,
                     t > 0 || half > 0 || kk > 0 ? 1u : 0u);
       };
-      bool ok = wait(&ctl->qfull, 0) && wait(&ctl->kfull[0], 0);
+      bool ok = wait(&ctl->qfull, 0) && wait(&ctl->tile_full[0], 0);
       if (ok) {
         for (int k = 0; k < 2; ++k)
           if (nt[k] > 0) scores(k, 0);
-        tc_commit(&ctl->kempty[0]);
+        tc_commit(&ctl->tile_empty[0]);
       }
       for (int t = 0; ok && t < ntiles; ++t) {
-        ok = wait(&ctl->vfull[t & 1], (uint32_t)((t >> 1) & 1));
+        const int vi = 2 * t + 1, ki = 2 * t + 2;          // places of this tile's values, of the next one's keys
+        ok = wait(&ctl->tile_full[vi % kSlots], (uint32_t)((vi / kSlots) & 1));
         for (int k = 0; ok && k < 2; ++k) {
           if (t < nt[k]) {
             // (the first half's weights arrive while the softmax works on the second)
@@ -206,112 +222,106 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
             values(k, t, 1);
             tc_commit(&ctl->pvdone[k]);
           }
-          if (k == 1) tc_commit(&ctl->vempty[t & 1]);
+          if (k == 1) tc_commit(&ctl->tile_empty[vi % kSlots]);
           if (k == 0 && t + 1 < ntiles) {
-            ok = wait(&ctl->kfull[(t + 1) & 1], (uint32_t)(((t + 1) >> 1) & 1));
+            ok = wait(&ctl->tile_full[ki % kSlots], (uint32_t)((ki / kSlots) & 1));
             if (!ok) break;
           }
           if (t + 1 < nt[k]) scores(k, t + 1);
-          if (k == 1 && t + 1 < ntiles) tc_commit(&ctl->kempty[(t + 1) & 1]);
+          if (k == 1 && t + 1 < ntiles) tc_commit(&ctl->tile_empty[ki % kSlots]);
         }
       }
       tc_commit(&ctl->drained);
+    } else if (warp == 13) {
+      // ---------------------------------------------------------------- loads
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
+      };
+      const int log_box = a.w.log_box;
+      int batch = 0;
+      load_chunks<kHeldBatches>(
+          c, a.w, status, reinterpret_cast<float4*>(sm + S::SC_OFF), lane, batch, u.b, u.kvh, u.len, c0, c1, 0,
+          [&]() { return true; },
+          [&](const Chunk& ch, bool mine, int id, int at) {
+            const uint32_t bytes = (uint32_t)(__popc(ch.copies) * D) << log_box;
+            const int64_t from = (((int64_t)id * Hkv + u.kvh) * c.s.page + ((ch.chunk * kTokens + (at << log_box)) & (c.s.page - 1))) * D;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int item = 2 * (ch.chunk - c0) + h, s = item % S::RAWS;
+              if (item >= S::RAWS && !wait(&ctl->raw_empty[s], (uint32_t)((item / S::RAWS - 1) & 1))) return false;
+              if (lane == 0) {
+                tc_mbar_expect_tx(&ctl->raw_full[s], bytes);
+                ctl->loads = item + 1;
+              }
+              __syncwarp();
+              if (mine)
+                bulk_load(sm + S::R_OFF + s * S::RAW + (at << log_box) * D, (h == 0 ? c.k : c.v) + from, (uint32_t)D << log_box,
+                          &ctl->raw_full[s]);
+            }
+            return true;
+          },
+          [&](const Chunk& ch) {
+            // (its place is free: tile t's codes could only be loaded once tile t - 8 was done with)
+            const int t = ch.chunk - c0;
+            if (lane == 0) heads[t % kHeads] = ch;
+            __syncwarp();
+            if (lane == 0) tc_mbar_arrive(&ctl->head[t % kHeads]);
+          });
     }
   } else if (warp >= 8) {
     regs_down<kRegsConvert>();
     // ---------------------------------------------------------------- codes to fp16
-    // A thread takes one 16-byte piece of STEP rows a tile, rows ROWS apart; eight neighbouring threads two rows of four
-    // pieces, so that their stores meet different banks.
-    constexpr int ROWS = D == 128 ? 16 : 32, STEP = kBR / ROWS;
+    // A thread takes one 16-byte piece of every STEP'th row.  Of eight neighbouring threads four read the first half of one
+    // row and four the second half of the next: different banks, and so are those of the pieces that they store, in an atom
+    // each (two rows of one atom with 64 dims).
+    constexpr int STEP = D == 128 ? 16 : 32;
     const int tid = threadIdx.x - 256;
-    const int piece = D == 128 ? (tid & 3) | (tid >> 3 & 1) << 2 : tid & 3;
-    const int row = D == 128 ? (tid >> 4) * 2 + (tid >> 2 & 1) : tid >> 2;
-    const int32_t* table = c.s.page_table + (int64_t)u.b * c.s.max_pages;
-    // lane g < 8: page of tokens 16 g .. of a tile, -1 where there is none
-    auto fetch = [&](int t) {
-      const int64_t tok = (int64_t)(c0 + t) * kBR + 16 * lane;
-      return lane < 8 && t < ntiles && tok < u.len ? table[tok / page] : -1;
+    const int piece = D == 128 ? tid & 7 : tid & 3;
+    const int row = D == 128 ? (tid >> 4) * 2 + ((tid >> 2 ^ tid >> 3) & 1) : tid >> 2;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
     };
-    auto check = [&](int t, int pid) {
-      const int64_t tok = (int64_t)(c0 + t) * kBR + 16 * lane;
-      if (!(lane < 8 && t < ntiles && tok < u.len)) return -1;
-      if (pid >= 0 && pid < c.s.num_pages) return pid;
-      atomicOr(status, MKV_FLAG_BAD_INDEX);
-      return -1;
-    };
-    // its codes' offset (page and head; -1: none)
-    auto offset = [&](int t, int pid) {
-      const int64_t tok = (int64_t)(c0 + t) * kBR + 16 * lane;
-      return pid < 0 ? (int64_t)-1 : (((int64_t)pid * Hkv + u.kvh) * page + tok % page) * D;
-    };
-    uint4 x[STEP];
-    auto load = [&](int i, int64_t off, const uint8_t* codes) {
-      const int64_t o = __shfl_sync(0xffffffffu, off, D == 128 ? i : 2 * i + (row >> 4));
-      x[i] = o < 0 ? make_uint4(0, 0, 0, 0)
-                   : __ldg(reinterpret_cast<const uint4*>(codes + o + (row & 15) * D + piece * 16));
-    };
-    auto store = [&](int i, uint8_t* tile, bool zero) {
-      const uint32_t w[4] = {zero ? 0u : x[i].x, zero ? 0u : x[i].y, zero ? 0u : x[i].z, zero ? 0u : x[i].w};
-      uint32_t e[8];
+    const uint32_t at0 = (uint32_t)((2 * (piece & 3)) ^ (row & 7)) << 4;
+    for (int item = 0; item < 2 * ntiles; ++item) {
+      const int t = item >> 1, rs = item % S::RAWS, s = item % kSlots;
+      if (!wait(&ctl->raw_full[rs], (uint32_t)((item / S::RAWS) & 1))) break;
+      if (item >= kSlots && !wait(&ctl->tile_empty[s], (uint32_t)((item / kSlots - 1) & 1))) break;
+      const uint8_t* src = sm + S::R_OFF + rs * S::RAW + row * D + piece * 16;
+      uint8_t* dst = sm + S::T_OFF + s * S::TILE + (piece >> 2) * S::ATOM + row * 128;
+      uint4 x[kBR / STEP];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) widen_codes<S::FMT>(w[k], e[2 * k], e[2 * k + 1]);
-      const int r = i * ROWS + row;
-      uint8_t* atom = tile + (piece >> 2) * S::ATOM;
-      *reinterpret_cast<uint4*>(atom + mn_offset<64>(r, 2 * (piece & 3))) = make_uint4(e[0], e[1], e[2], e[3]);
-      *reinterpret_cast<uint4*>(atom + mn_offset<64>(r, 2 * (piece & 3) + 1)) = make_uint4(e[4], e[5], e[6], e[7]);
-    };
-    auto hand_over = [&](uint64_t* bar) {
+      for (int i = 0; i < kBR / STEP; ++i) x[i] = *reinterpret_cast<const uint4*>(src + i * STEP * D);
+      if (item & 1) {                                      // what no row sees must not meet a zero weight as NaN
+        if (!wait(&ctl->head[t % kHeads], (uint32_t)((t / kHeads) & 1))) break;
+        const int copies = heads[t % kHeads].copies, tail = u.len - (c0 + t) * kBR;
+        if (copies != all_copies || tail < kBR)
+#pragma unroll
+          for (int i = 0; i < kBR / STEP; ++i)
+            if (row + i * STEP >= tail || !(copies >> ((row + i * STEP) >> a.w.log_box) & 1)) x[i] = make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+      for (int i = 0; i < kBR / STEP; ++i) {
+        uint32_t e[8];
+        widen_codes<S::FMT>(x[i].x, e[0], e[1]);
+        widen_codes<S::FMT>(x[i].y, e[2], e[3]);
+        widen_codes<S::FMT>(x[i].z, e[4], e[5]);
+        widen_codes<S::FMT>(x[i].w, e[6], e[7]);
+        *reinterpret_cast<uint4*>(dst + i * STEP * 128 + at0) = make_uint4(e[0], e[1], e[2], e[3]);
+        *reinterpret_cast<uint4*>(dst + i * STEP * 128 + (at0 ^ 16u)) = make_uint4(e[4], e[5], e[6], e[7]);
+      }
       fence_async_smem();
       __syncwarp();
-      if (lane == 0) tc_mbar_arrive(bar);
-    };
-    int pid = check(0, fetch(0));
-    int64_t off = offset(0, pid);
-#pragma unroll
-    for (int i = 0; i < STEP; ++i) load(i, off, c.k);
-    bool ok = true;
-    for (int t = 0; ok && t < ntiles; ++t) {
-      const int s = t & 1;
-      uint8_t* tile = sm + S::R_OFF + s * 2 * S::TILE;
-      float ks = 0.f, vs = 1.f;
-      if (warp == 8 && pid >= 0) {
-        ks = c.k_scale[(int64_t)pid * Hkv + u.kvh];
-        vs = c.v_scale[(int64_t)pid * Hkv + u.kvh];
+      if (lane == 0) {
+        tc_mbar_arrive(&ctl->tile_full[s]);
+        tc_mbar_arrive(&ctl->raw_empty[rs]);
       }
-      const int next = fetch(t + 1);
-      if (t > 1) ok = __all_sync(0xffffffffu, wait_or_fail(&ctl->kempty[s], (uint32_t)(((t >> 1) - 1) & 1), fail, status));
-      if (!ok) break;
-#pragma unroll
-      for (int i = 0; i < STEP; ++i) {
-        store(i, tile, false);
-        load(i, off, c.v);
-      }
-      if (warp == 8 && lane < 8) {
-        int e;
-        const float m = frexpf(vs, &e);
-        reinterpret_cast<float4*>(sm + S::SC_OFF)[(t % kScales) * 8 + lane] =
-            make_float4(ks * a.scale_log2, m, (float)e, pid >= 0 ? 1.f : 0.f);
-      }
-      hand_over(&ctl->kfull[s]);
-      pid = check(t + 1, next);
-      off = offset(t + 1, pid);
-      const int tail = u.len - (c0 + t) * kBR;             // rows of the tile that exist
-      if (t > 1) ok = __all_sync(0xffffffffu, wait_or_fail(&ctl->vempty[s], (uint32_t)(((t >> 1) - 1) & 1), fail, status));
-      if (!ok) break;
-#pragma unroll
-      for (int i = 0; i < STEP; ++i) {
-        // (what lies behind the length, whatever it is, must not meet a zero weight as NaN)
-        store(i, tile + S::TILE, i * ROWS + row >= tail);
-        load(i, off, c.k);
-      }
-      hand_over(&ctl->vfull[s]);
     }
   } else {
     regs_up<kRegsSoftmax>();
     const int k = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tbase + lanes + (uint32_t)(k * kBR), tO = tbase + lanes + (uint32_t)(2 * kBR + k * kBR);
-    float* qs = reinterpret_cast<float*>(sm + S::QS_OFF);
+    int8_t* qs = reinterpret_cast<int8_t*>(sm + S::QS_OFF);
     // ---------------------------------------------------------------- queries, D / 8 lanes a row
     {
       constexpr int LN = D / 8, PER = 32 / LN, U = 4;
@@ -342,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] *= f;
             y[q] = narrow8<false>(v);
-            if (ch == 0) qs[r] = power_of_two(-e);
+            if (ch == 0) qs[r] = (int8_t)e;
           }
           *reinterpret_cast<uint4*>(sm + S::Q_OFF + (r / kBR) * S::QBLK + (ch >> 3) * S::ATOM + mn_offset<64>(r % kBR, ch & 7)) =
               y[q];
@@ -364,23 +374,23 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     float back = 1.f;
     if (BF16) {                                            // (all warps' queries are in place)
       wait(&ctl->qfull, 0);
-      back = qs[rin];
+      back = power_of_two(-(int)qs[rin]);
     }
     float m = kNoMax, m2 = kNoMax, l = 0.f;
     for (int t = 0; t < nt[k]; ++t) {
-      if (!wait(&ctl->sfull[k], (uint32_t)(t & 1))) break;
-      const float4* sc = reinterpret_cast<const float4*>(sm + S::SC_OFF) + (t % kScales) * 8;
+      if (!wait(&ctl->head[t % kHeads], (uint32_t)((t / kHeads) & 1)) || !wait(&ctl->sfull[k], (uint32_t)(t & 1))) break;
+      const int copies = heads[t % kHeads].copies, log_group = a.w.log_box - 4;
+      const float4* scales = reinterpret_cast<const float4*>(sm + S::SC_OFF) + heads[t % kHeads].scales;
       float v[kBR];
 #pragma unroll
       for (int i = 0; i < 4; ++i) tm_issue<32>(tS + i * 32, *reinterpret_cast<float(*)[32]>(&v[i * 32]));
 #pragma unroll
       for (int i = 0; i < 4; ++i) tm_wait<32>(*reinterpret_cast<float(*)[32]>(&v[i * 32]));
-      const bool holes = __any_sync(0xffffffffu, sc[lane & 7].w == 0.f);     // a page outside the pool or past the length
-      if (c0 + t >= td || holes) {
+      if (c0 + t >= td || copies != all_copies) {          // (a page outside the pool or past the length)
         const int lim = seen - (c0 + t) * kBR;             // columns of the tile that this row sees
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
-          const int upto = sc[g].w != 0.f ? lim : 0;
+          const int upto = copies >> (g >> log_group) & 1 ? lim : 0;
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[16 * g + i] = 16 * g + i < upto ? v[16 * g + i] : -INFINITY;
         }
@@ -395,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         x0 = fmax3(x0, y[10], y[11]);
         x1 = fmax3(x1, y[12], y[13]);
         x0 = fmax3(fmaxf(x0, x1), y[14], y[15]);
-        const float4 s4 = sc[g];
+        const float4 s4 = scales[g >> log_group];
         x0 *= fmaxf(s4.x * back, 1.17549435e-38f);         // (a factor of zero would make NaN of a masked score)
         mt = fmaxf(mt, x0);
         mt2 = fmaxf(mt2, x0 + s4.z);
@@ -423,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       if (plain) {
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
-          const float f = fmaxf(sc[g].x * back, 1.17549435e-38f);
+          const float f = fmaxf(scales[g >> log_group].x * back, 1.17549435e-38f);
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[16 * g + i] = __fsub_rn(__fmul_rn(v[16 * g + i], f), m);
         }
@@ -436,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         float pk[16];
 #pragma unroll
         for (int g = 2 * h; g < 2 * h + 2; ++g) {
-          const float4 s4 = sc[g];
+          const float4 s4 = scales[g >> log_group];
           const float f = plain ? 1.f : fmaxf(s4.x * back, 1.17549435e-38f), w = ex2_approx(up + s4.z) * s4.y;
           const uint64_t f2 = pk2(f, f), w2 = pk2(w, w);
 #pragma unroll
@@ -491,10 +501,15 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       }
     }
   }
-  // teardown: the products issued are complete (a bounded wait)
+  // teardown: the products issued are complete; after a failure so are the copies (each wait bounded)
   tc_fence_before();
   __syncthreads();
-  if (threadIdx.x == 0) tc_mbar_wait(&ctl->drained, 0, kRoleWaitNs);
+  if (threadIdx.x == 0) {
+    tc_mbar_wait(&ctl->drained, 0, kRoleWaitNs);
+    if (ctl->fail)
+      for (int x = std::max(0, ctl->loads - S::RAWS); x < ctl->loads; ++x)
+        tc_mbar_wait(&ctl->raw_full[x % S::RAWS], (uint32_t)((x / S::RAWS) & 1), kRoleWaitNs);
+  }
   __syncthreads();
   tc_fence_after();
   if (warp == 12) tc_dealloc(tbase, 512);
@@ -596,7 +611,7 @@ cudaError_t launch_paged_prefill(const PagedAttnCall& c, void* ws, cudaStream_t 
   const Plan p = plan_of(c);
   a.c = c;
   a.G = c.s.Hq / c.s.Hkv;
-  a.scale_log2 = c.scale * kLog2e;
+  a.w = work_args(c, kNumSMs);
   a.slots = p.slots;
   a.per = p.per;
   a.splits = p.splits;
