@@ -115,7 +115,7 @@ __device__ __forceinline__ void widen_codes(uint32_t w, uint32_t& lo, uint32_t& 
 // Softmax over 8-bit pages.  Two running maxima a row: m of the scores s (log2), for the sum of the weights p = 2^(s - m),
 // and m2 of s + log2 vs, for the weights p vs 2^(m - m2 + 6) that the tensor cores take in fp16: pages of any value scales
 // then keep full precision.  Either is only raised once a score passes it by 2^8, so accumulators are almost never rescaled
-// and a weight stays below 2^14 (vs is taken as mantissa and exponent, 2^(e - 1) <= vs < 2^e).
+// and a weight stays below 2^14.
 constexpr float kRaise = 8.f;
 constexpr float kOffset = 6.f;      // (full precision in fp16 down to 2^-20 of the maximum)
 constexpr float kNoMax = -3.402823466e+38f;   // the maxima of a row that has seen nothing: no score is below it

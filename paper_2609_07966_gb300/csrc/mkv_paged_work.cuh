@@ -51,10 +51,10 @@ struct Head {
   Piece p;
 };
 static_assert(sizeof(Head) == 64, "four 16-byte accesses");
-// Scales of a batch of 32 copies lie together: key factor, value scale as mantissa and exponent.  Of several pieces as many
+// Scales of a batch of 32 copies lie together: key factor, log2 of the value scale.  Of several pieces as many
 // batches are kept as chunks can be between the warp that loads and those that compute (a batch may hold one chunk alone).
 constexpr int kBatches = 8;
-constexpr int scale_bytes(int batches) { return batches * 32 * 16; }
+constexpr int scale_bytes(int batches) { return batches * 32 * 8; }
 
 struct Entry {
   int row0, tokens, len, chunks;   // its first row, new tokens, tokens held, chunks of a unit
@@ -95,7 +95,7 @@ struct Runs {
 // of which the first two say whether to go on; whether all went through.  `batch`: how many batches were begun before.  Little
 // is done a chunk: a warp alone takes 6 cycles an instruction.
 template <int BATCHES, typename Begin, typename Copies, typename Publish>
-__device__ __forceinline__ bool load_chunks(const PagedAttnCall& c, const WorkArgs& w, uint32_t* status, float4* held_scales,
+__device__ __forceinline__ bool load_chunks(const PagedAttnCall& c, const WorkArgs& w, uint32_t* status, float2* held_scales,
                                             int lane, int& batch, int b, int kvh, int len, int c0, int c1, int flags,
                                             Begin begin, Copies copies, Publish publish) {
   // A batch is 32 copies' pages, a lane each: page and scales of the next batch are fetched during this one.
@@ -151,9 +151,7 @@ __device__ __forceinline__ bool load_chunks(const PagedAttnCall& c, const WorkAr
     head.scales = at + (in << log_per);
     if (!copies(head, pid >= 0 && lane >> log_per == in, pid, lane & ((1 << log_per) - 1))) return false;
     if (in == 0) {
-      int x;
-      const float mant = frexpf(vs, &x);
-      held_scales[at + lane] = make_float4(ks * w.scale_log2, mant, (float)x, 0.f);
+      held_scales[at + lane] = make_float2(ks * w.scale_log2, __log2f(vs));
     }
     publish(head);
   }
@@ -163,7 +161,7 @@ __device__ __forceinline__ bool load_chunks(const PagedAttnCall& c, const WorkAr
 // A whole warp goes through this CTA's chunks: load_chunks for each piece, with begin(p), copies(ch, p, mine, id, at) and
 // publish(ch, p); whether all went through.
 template <typename Begin, typename Copies, typename Publish>
-__device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkArgs& w, uint32_t* status, float4* held_scales,
+__device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkArgs& w, uint32_t* status, float2* held_scales,
                                              int lane, Begin begin, Copies copies, Publish publish) {
   const int B = c.s.B, Hkv = c.s.Hkv;
   uint32_t* report = blockIdx.x == 0 ? status : nullptr;

@@ -18,6 +18,7 @@
 
 #include <algorithm>
 
+#include "mkv_paged_softmax.cuh"
 #include "mkv_paged_work.cuh"
 
 namespace mkv {
@@ -72,12 +73,6 @@ struct BlockCtl {
 };
 static_assert(sizeof(BlockCtl) <= 512, "control block");
 
-__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
 template <class S, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
   constexpr int D = S::D;
@@ -127,7 +122,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
     int g = 0;
     const int log_box = a.w.log_box;
     const bool ok = work_through(
-        c, a.w, status, reinterpret_cast<float4*>(sm + S::SC_OFF), lane, [&](const Piece&) { return true; },
+        c, a.w, status, reinterpret_cast<float2*>(sm + S::SC_OFF), lane, [&](const Piece&) { return true; },
         [&](const Chunk& ch, const Piece& p, bool mine, int id, int at) {
           const uint32_t bytes = (uint32_t)(__popc(ch.copies) * D) << log_box;
           const int64_t from = (((int64_t)id * Hkv + p.kvh) * c.s.page + ((ch.chunk * kTokens + (at << log_box)) & (c.s.page - 1))) * D;
@@ -430,8 +425,9 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         l = 0.f;
         own = hd.len - hd.tokens + row / G;
       }
-      const float4* scales = reinterpret_cast<const float4*>(sm + S::SC_OFF) + now.scales;
+      const float2* scales = reinterpret_cast<const float2*>(sm + S::SC_OFF) + now.scales;
       auto copy_of = [&](int i) { return (copy * NG + i) >> (a.w.log_box - 4); };   // that holds group i of this copy's tokens
+      auto scale = [&](int i) { return scales[copy_of(i)]; };
       wait(&ctl->sfull[g & 1], (uint32_t)((g >> 1) & 1));
       if (dead) break;
       const uint32_t tS = tbase + lanes + S::S + (uint32_t)((g & 1) * 128 + copy * COLS);
@@ -440,30 +436,18 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       for (int i = 0; i < COLS / 32; ++i) tm_issue<32>(tS + i * 32, *reinterpret_cast<float(*)[32]>(&v[i * 32]));
 #pragma unroll
       for (int i = 0; i < COLS / 32; ++i) tm_wait<32>(*reinterpret_cast<float(*)[32]>(&v[i * 32]));
-      // the scores; what the row does not see is minus infinity
+      // what the row does not see is minus infinity
       const bool part = now.copies != all_copies || (now.chunk + 1) * kTokens > hd.len - hd.tokens + 1;
-      float mt = -INFINITY, mt2 = -INFINITY;
+      if (part) {
 #pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const float4 s4 = scales[copy_of(i)];
-        const float f = s4.x * back;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) v[16 * i + e] *= f;
-        if (part) {
+        for (int i = 0; i < NG; ++i) {
           const int upto = now.copies >> copy_of(i) & 1 ? own + 1 - now.chunk * kTokens - copy * COLS - 16 * i : 0;
 #pragma unroll
           for (int e = 0; e < 16; ++e) v[16 * i + e] = e < upto ? v[16 * i + e] : -INFINITY;
         }
-        const float* y = v + 16 * i;
-        float x0 = fmax3(y[0], y[1], y[2]), x1 = fmax3(y[3], y[4], y[5]);
-        x0 = fmax3(x0, y[6], y[7]);
-        x1 = fmax3(x1, y[8], y[9]);
-        x0 = fmax3(x0, y[10], y[11]);
-        x1 = fmax3(x1, y[12], y[13]);
-        x0 = fmax3(fmaxf(x0, x1), y[14], y[15]);
-        mt = fmaxf(mt, x0);
-        mt2 = fmaxf(mt2, x0 + s4.z);
       }
+      float mt = -INFINITY, mt2 = -INFINITY;
+      tile_max<COLS, 16, BF16>(v, back, scale, mt, mt2);
       const bool raise = __any_sync(0xffffffffu, mt > m + kRaise || mt2 > m2 + kRaise);
       float w = 1.f;
       if (raise) {
@@ -473,27 +457,11 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         m = nm;
         m2 = nm2;
       }
-      // weights
-      const uint64_t off2 = pk2(-m, -m);
-      const float up = m - m2 + kOffset;
-      uint64_t sum2[2] = {0ull, 0ull};
       float pk[COLS / 2];
+      tile_weights<COLS, 16, BF16>(v, part, m, m2, back, scale, l, [&](int i, const float(&x)[16]) {
 #pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const float4 s4 = scales[copy_of(i)];
-        const float f = ex2_approx(up + s4.z) * s4.y;
-        const uint64_t f2 = pk2(f, f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float2 y = upk2(fadd2(pk2(v[16 * i + 2 * e], v[16 * i + 2 * e + 1]), off2));
-          const uint64_t p = pk2(ex2_approx(y.x), ex2_approx(y.y));
-          sum2[e & 1] = fadd2(sum2[e & 1], p);
-          const float2 z = upk2(fmul2(p, f2));
-          pk[8 * i + e] = __uint_as_float(pack2<false>(z.x, z.y));
-        }
-      }
-      const float2 s0 = upk2(sum2[0]), s1 = upk2(sum2[1]);
-      l += (s0.x + s0.y) + (s1.x + s1.y);
+        for (int e = 0; e < 16; ++e) pk[16 * i + e] = x[e];
+      });
       // (the tile before this one's weights have been read, and its product added)
       if (g > 0) wait(&ctl->pvdone, (uint32_t)((g - 1) & 1));
       if (dead) break;

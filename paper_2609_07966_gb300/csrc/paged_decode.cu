@@ -20,6 +20,7 @@
 
 #include <algorithm>
 
+#include "mkv_paged_softmax.cuh"
 #include "mkv_paged_work.cuh"
 
 namespace mkv {
@@ -117,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     };
     const int log_box = a.w.log_box;
     bool ok = work_through(
-        c, a.w, status, reinterpret_cast<float4*>(sm + S::SC_OFF), lane,
+        c, a.w, status, reinterpret_cast<float2*>(sm + S::SC_OFF), lane,
         [&](const Piece& p) {                              // a piece's queries: one copy a token's heads
           if (pieces > 0 && !wait(&ctl->qempty, (uint32_t)((pieces - 1) & 1))) return false;
           const int bytes = a.G * D * 2;
@@ -290,9 +291,9 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       {
         const int ch = now.chunk;
         const int t0 = ch * kTokens + warp * 32;
-        const float4* scales = reinterpret_cast<const float4*>(sm + S::SC_OFF) + now.scales;
+        const float2* scales = reinterpret_cast<const float2*>(sm + S::SC_OFF) + now.scales;
         const int cp[2] = {(warp * 2) >> (a.w.log_box - 4), (warp * 2 + 1) >> (a.w.log_box - 4)};   // the groups' copies
-        const float4 sc[2] = {scales[cp[0]], scales[cp[1]]};
+        const float2 sc[2] = {scales[cp[0]], scales[cp[1]]};
         const bool in[2] = {(now.copies >> cp[0] & 1) != 0 && t0 < hd.len, (now.copies >> cp[1] & 1) != 0 && t0 + 16 < hd.len};
         if (in[0] || in[1]) {
           const uint8_t* K = sm + S::KV_OFF + s * 2 * S::TILE + warp * 32 * D;
@@ -365,14 +366,14 @@ __global__ void __launch_bounds__(kThreads, kCtas)
                 if (t0 + 16 * u + lg + 8 > own) x[u][2 + j] = -INFINITY;
               }
               const float t = fmaxf(x[u][j], x[u][2 + j]);
-              over |= t > m[j] + kRaise || t + sc[u].z > m2[j] + kRaise;
+              over |= t > m[j] + kRaise || t + sc[u].y > m2[j] + kRaise;
             }
           }
           if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               float y0 = fmaxf(x[0][j], x[0][2 + j]), y1 = fmaxf(x[1][j], x[1][2 + j]);
-              float t = fmaxf(y0, y1), t2 = fmaxf(y0 + sc[0].z, y1 + sc[1].z);
+              float t = fmaxf(y0, y1), t2 = fmaxf(y0 + sc[0].y, y1 + sc[1].y);
 #pragma unroll
               for (int d = 4; d < 32; d <<= 1) {
                 t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
@@ -396,11 +397,10 @@ __global__ void __launch_bounds__(kThreads, kCtas)
             float w[4];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              const float f = ex2_approx(m[j] - m2[j] + (kOffset + sc[u].z)) * sc[u].y;
-              const float p0 = ex2_approx(x[u][j] - m[j]), p1 = ex2_approx(x[u][2 + j] - m[j]);
-              l[j] += p0 + p1;
-              w[j] = p0 * f;
-              w[2 + j] = p1 * f;
+              const float c2 = weight_shift(m[j], m2[j], sc[u].y);
+              w[j] = ex2_approx(x[u][j] - m[j] + c2);
+              w[2 + j] = ex2_approx(x[u][2 + j] - m[j] + c2);
+              l[j] += (w[j] + w[2 + j]) * ex2_approx(-c2);
             }
             b0[u] = transpose8(pack2<false>(w[0], w[1]));
             b1[u] = transpose8(pack2<false>(w[2], w[3]));

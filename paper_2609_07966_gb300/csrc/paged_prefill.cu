@@ -20,6 +20,7 @@
 
 #include <algorithm>
 
+#include "mkv_paged_softmax.cuh"
 #include "mkv_paged_work.cuh"
 
 namespace mkv {
@@ -28,8 +29,6 @@ namespace {
 
 constexpr int kBR = 128;            // rows a block, tokens a tile
 constexpr int kRows = 2 * kBR;      // rows a unit
-// Up to this maximum (log2) an unrounded product of score and scale is within a half of the rounded one.
-constexpr float kFused = 16777216.f;
 constexpr int kThreads = 512;       // two softmax warpgroups, one that converts, one for products and loads (two warps idle)
 constexpr int kRegsSoftmax = 184, kRegsConvert = 72, kRegsOther = 72;
 static_assert(2 * kRegsSoftmax + kRegsConvert + kRegsOther <= 4 * 128, "register shares");
@@ -50,9 +49,10 @@ struct PrefillArgs {
   float4* part_st;                  // the same without D: m, sum, m2
 };
 
-template <int FMT_, int D_>
+// GC: tokens that share a page's scales for certain
+template <int FMT_, int D_, int GC_>
 struct PShape {
-  static constexpr int FMT = FMT_, D = D_, KA = D / 64;
+  static constexpr int FMT = FMT_, D = D_, GC = GC_, KA = D / 64;
   static constexpr int ATOM = kBR * 128, TILE = KA * ATOM, QBLK = TILE;
   static constexpr int RAW = kBR * D, RAWS = 4;            // codes of a tile's keys or values
   static constexpr int Q_OFF = 0, T_OFF = 2 * QBLK;        // [kSlots] widened tiles
@@ -108,15 +108,9 @@ __device__ __forceinline__ Unit unit_of(const PrefillArgs& a, int64_t slot, int 
   return u;
 }
 
-__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
 template <class S, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs a) {
-  constexpr int D = S::D;
+  constexpr int D = S::D, GC = S::GC;
   extern __shared__ __align__(1024) uint8_t sm[];
   PCtl* ctl = reinterpret_cast<PCtl*>(sm + S::CTL_OFF);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -240,7 +234,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       const int log_box = a.w.log_box;
       int batch = 0;
       load_chunks<kHeldBatches>(
-          c, a.w, status, reinterpret_cast<float4*>(sm + S::SC_OFF), lane, batch, u.b, u.kvh, u.len, c0, c1, 0,
+          c, a.w, status, reinterpret_cast<float2*>(sm + S::SC_OFF), lane, batch, u.b, u.kvh, u.len, c0, c1, 0,
           [&]() { return true; },
           [&](const Chunk& ch, bool mine, int id, int at) {
             const uint32_t bytes = (uint32_t)(__popc(ch.copies) * D) << log_box;
@@ -380,13 +374,15 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     for (int t = 0; t < nt[k]; ++t) {
       if (!wait(&ctl->head[t % kHeads], (uint32_t)((t / kHeads) & 1)) || !wait(&ctl->sfull[k], (uint32_t)(t & 1))) break;
       const int copies = heads[t % kHeads].copies, log_group = a.w.log_box - 4;
-      const float4* scales = reinterpret_cast<const float4*>(sm + S::SC_OFF) + heads[t % kHeads].scales;
+      const float2* scales = reinterpret_cast<const float2*>(sm + S::SC_OFF) + heads[t % kHeads].scales;
       float v[kBR];
 #pragma unroll
       for (int i = 0; i < 4; ++i) tm_issue<32>(tS + i * 32, *reinterpret_cast<float(*)[32]>(&v[i * 32]));
 #pragma unroll
       for (int i = 0; i < 4; ++i) tm_wait<32>(*reinterpret_cast<float(*)[32]>(&v[i * 32]));
-      if (c0 + t >= td || copies != all_copies) {          // (a page outside the pool or past the length)
+      auto scale = [&](int g) { return scales[GC == 16 ? g >> log_group : g >> (log_group - 1)]; };
+      const bool part = c0 + t >= td || copies != all_copies;      // (a page outside the pool or past the length)
+      if (part) {
         const int lim = seen - (c0 + t) * kBR;             // columns of the tile that this row sees
 #pragma unroll
         for (int g = 0; g < 8; ++g) {
@@ -396,20 +392,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         }
       }
       float mt = -INFINITY, mt2 = -INFINITY;
-#pragma unroll
-      for (int g = 0; g < 8; ++g) {
-        const float* y = v + 16 * g;
-        float x0 = fmax3(y[0], y[1], y[2]), x1 = fmax3(y[3], y[4], y[5]);
-        x0 = fmax3(x0, y[6], y[7]);
-        x1 = fmax3(x1, y[8], y[9]);
-        x0 = fmax3(x0, y[10], y[11]);
-        x1 = fmax3(x1, y[12], y[13]);
-        x0 = fmax3(fmaxf(x0, x1), y[14], y[15]);
-        const float4 s4 = scales[g >> log_group];
-        x0 *= fmaxf(s4.x * back, 1.17549435e-38f);         // (a factor of zero would make NaN of a masked score)
-        mt = fmaxf(mt, x0);
-        mt2 = fmaxf(mt2, x0 + s4.z);
-      }
+      tile_max<kBR, GC, BF16>(v, back, scale, mt, mt2);
       if (__any_sync(0xffffffffu, mt > m + kRaise || mt2 > m2 + kRaise)) {
         const float nm = fmaxf(m, mt), nm2 = fmaxf(m2, mt2);
         l *= ex2_approx(m - nm);
@@ -428,36 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
           }
         }
       }
-      // (a maximum so large that its rounding alone passes the exponent's range: the products are rounded as it was)
-      const bool plain = __any_sync(0xffffffffu, fabsf(m) > kFused && m != kNoMax);
-      if (plain) {
-#pragma unroll
-        for (int g = 0; g < 8; ++g) {
-          const float f = fmaxf(scales[g >> log_group].x * back, 1.17549435e-38f);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[16 * g + i] = __fsub_rn(__fmul_rn(v[16 * g + i], f), m);
-        }
-      }
-      const float off = plain ? 0.f : -m, up = m - m2 + kOffset;
-      const uint64_t off2 = pk2(off, off);
-      uint64_t sum2[2] = {0ull, 0ull};
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {                        // 32 columns: two groups
-        float pk[16];
-#pragma unroll
-        for (int g = 2 * h; g < 2 * h + 2; ++g) {
-          const float4 s4 = scales[g >> log_group];
-          const float f = plain ? 1.f : fmaxf(s4.x * back, 1.17549435e-38f), w = ex2_approx(up + s4.z) * s4.y;
-          const uint64_t f2 = pk2(f, f), w2 = pk2(w, w);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float2 y = upk2(ffma2(pk2(v[16 * g + 2 * i], v[16 * g + 2 * i + 1]), f2, off2));
-            const uint64_t p = pk2(ex2_approx(y.x), ex2_approx(y.y));
-            sum2[i & 1] = fadd2(sum2[i & 1], p);
-            const float2 z = upk2(fmul2(p, w2));
-            pk[(g & 1) * 8 + i] = __uint_as_float(pack2<false>(z.x, z.y));
-          }
-        }
+      tile_weights<kBR, GC, BF16>(v, part, m, m2, back, scale, l, [&](int h, const float(&pk)[16]) {
         tm_store<16>(tS + h * 16, pk);
         if (h & 1) {
           tm_store_wait();
@@ -465,9 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
           __syncwarp();
           if (lane == 0) tc_mbar_arrive(&ctl->pfull[k][h >> 1]);
         }
-      }
-      const float2 s0 = upk2(sum2[0]), s1 = upk2(sum2[1]);
-      l += (s0.x + s0.y) + (s1.x + s1.y);
+      });
     }
     // ---------------------------------------------------------------- output
     if (nt[k] > 0) wait(&ctl->pvdone[k], (uint32_t)((nt[k] - 1) & 1));
@@ -516,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
 }
 
 // out = sum_s 2^(m2_s - M2) o_s / sum_s 2^(m_s - M) l_s, a warp a row.
-template <int FMT, int D, bool BF16>
+template <int D, bool BF16>
 __global__ void __launch_bounds__(256) join_kernel(const PrefillArgs a) {
   pdl_wait_and_trigger();
   const int lane = threadIdx.x & 31, Hkv = a.c.s.Hkv;
@@ -587,13 +539,14 @@ cudaError_t launch_shape(const PrefillArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   e = launch_pdl(prefill_kernel<S, BF16>, dim3((unsigned)(units * a.splits)), dim3(kThreads), smem, st, a);
   if (e != cudaSuccess || a.splits == 1) return e;
-  return launch_pdl(join_kernel<S::FMT, S::D, BF16>, dim3((unsigned)(units * (kRows / 8))), dim3(256), 0, st, a);
+  return launch_pdl(join_kernel<S::D, BF16>, dim3((unsigned)(units * (kRows / 8))), dim3(256), 0, st, a);
 }
-template <int FMT>
-cudaError_t launch_f(const PrefillArgs& a, cudaStream_t st) {
+template <int FMT, int D>
+cudaError_t launch_d(const PrefillArgs& a, cudaStream_t st) {
   const bool bf16 = a.c.s.dtype == MKV_BF16;
-  if (a.c.s.D == 128) return bf16 ? launch_shape<PShape<FMT, 128>, true>(a, st) : launch_shape<PShape<FMT, 128>, false>(a, st);
-  return bf16 ? launch_shape<PShape<FMT, 64>, true>(a, st) : launch_shape<PShape<FMT, 64>, false>(a, st);
+  if (a.c.s.page == 16)
+    return bf16 ? launch_shape<PShape<FMT, D, 16>, true>(a, st) : launch_shape<PShape<FMT, D, 16>, false>(a, st);
+  return bf16 ? launch_shape<PShape<FMT, D, 32>, true>(a, st) : launch_shape<PShape<FMT, D, 32>, false>(a, st);
 }
 
 }  // namespace
@@ -618,7 +571,8 @@ cudaError_t launch_paged_prefill(const PagedAttnCall& c, void* ws, cudaStream_t 
   uint8_t* base = static_cast<uint8_t*>(ws) + kCounterBytes;
   a.part_st = reinterpret_cast<float4*>(base);
   a.part_o = reinterpret_cast<float*>(base + align256((size_t)kNumSMs * kRows * sizeof(float4)));
-  return c.s.format == MKV_E4M3 ? launch_f<MKV_E4M3>(a, st) : launch_f<MKV_I8>(a, st);
+  if (c.s.format == MKV_E4M3) return c.s.D == 128 ? launch_d<MKV_E4M3, 128>(a, st) : launch_d<MKV_E4M3, 64>(a, st);
+  return c.s.D == 128 ? launch_d<MKV_I8, 128>(a, st) : launch_d<MKV_I8, 64>(a, st);
 }
 
 }  // namespace mkv
