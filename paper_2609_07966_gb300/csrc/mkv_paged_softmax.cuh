@@ -1,4 +1,4 @@
-// A row's part of the softmax over a tile of 8-bit pages, a thread a row: the tile's maxima, and its weights.
+// A row's part of the softmax over a tile of 8-bit pages, a thread a row or a part of it: the columns' maxima, and weights.
 //
 // GC neighbouring columns (tokens) share a page's scales {kf, lv}: their scores are v kf back, and lv = log2 vs.  A weight as
 // the tensor cores take it is p vs 2^(m - m2 + 6) = 2^(v kf back - m + c) with c = m - m2 + 6 + lv, one exponential; the row's
@@ -32,11 +32,11 @@ __device__ __forceinline__ float max_of(const float* y) {
   return fmax3(x0, x1, fmaxf(y[N - 2], y[N - 1]));         // (N is a multiple of 4: two are left)
 }
 
-// Raises mt and mt2 to the tile's largest score and score + log2 vs.
-template <int COLS, int GC, bool BACK, typename Scale>
-__device__ __forceinline__ void tile_max(const float (&v)[COLS], float back, Scale scale, float& mt, float& mt2) {
+// Raises mt and mt2 to the largest of N columns' scores and scores + log2 vs; GC of them share scale(g).
+template <int N, int GC, bool BACK, typename Scale>
+__device__ __forceinline__ void columns_max(const float (&v)[N], float back, Scale scale, float& mt, float& mt2) {
 #pragma unroll
-  for (int g = 0; g < COLS / GC; ++g) {
+  for (int g = 0; g < N / GC; ++g) {
     const float2 s = scale(g);
     const float x = max_of<GC>(v + GC * g) * score_factor<BACK>(s.x, back);
     mt = fmaxf(mt, x);
@@ -44,48 +44,42 @@ __device__ __forceinline__ void tile_max(const float (&v)[COLS], float back, Sca
   }
 }
 
-// The weights of all columns, 32 at a time to store(i, packed pairs), and the row's sum.  `ends`: the tile is one in which
-// rows end: then the sum takes the weights as they were rounded, so that a row of few tokens is off by less (of one token,
-// not at all).
-template <int COLS, int GC, bool BACK, typename Scale, typename Store>
-__device__ __forceinline__ void tile_weights(float (&v)[COLS], bool ends, float m, float m2, float back, Scale scale, float& l,
-                                             Store store) {
+// The weights of N columns as packed pairs, and their part of the row's sum.  `ends`: rows end among the columns: then the sum
+// takes the weights as they were rounded, so that a row of few tokens is off by less (of one token, not at all).
+template <int N, int GC, bool BACK, typename Scale>
+__device__ __forceinline__ void columns_weights(float (&v)[N], bool ends, float m, float m2, float back, Scale scale, float& l,
+                                                float (&pk)[N / 2]) {
   // (a maximum so large that its rounding alone passes the exponent's range: the products are rounded as it was)
   const bool plain = __any_sync(0xffffffffu, fabsf(m) > kFused && m != kNoMax);
   if (plain) {
 #pragma unroll
-    for (int i = 0; i < COLS; ++i) v[i] = __fsub_rn(__fmul_rn(v[i], score_factor<BACK>(scale(i / GC).x, back)), m);
+    for (int i = 0; i < N; ++i) v[i] = __fsub_rn(__fmul_rn(v[i], score_factor<BACK>(scale(i / GC).x, back)), m);
   }
 #pragma unroll
-  for (int i = 0; i < COLS / 32; ++i) {
-    float pk[16];
+  for (int g = 0; g < N / GC; ++g) {
+    const float2 s = scale(g);
+    const float c = weight_shift(m, m2, s.y), f = plain ? 1.f : score_factor<BACK>(s.x, back), off = plain ? c : c - m;
+    const uint64_t f2 = pk2(f, f), off2 = pk2(off, off);
+    uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-    for (int g = 0; g < 32 / GC; ++g) {
-      const float2 s = scale(i * (32 / GC) + g);
-      const float c = weight_shift(m, m2, s.y), f = plain ? 1.f : score_factor<BACK>(s.x, back), off = plain ? c : c - m;
-      const uint64_t f2 = pk2(f, f), off2 = pk2(off, off);
-      uint64_t sum[2] = {0ull, 0ull};
+    for (int e = 0; e < GC / 2; ++e) {
+      const int at = GC * g + 2 * e;
+      const float2 y = upk2(ffma2(pk2(v[at], v[at + 1]), f2, off2));
+      const float w0 = ex2_approx(y.x), w1 = ex2_approx(y.y);
+      sum[e & 1] = fadd2(sum[e & 1], pk2(w0, w1));
+      pk[GC / 2 * g + e] = __uint_as_float(pack2<false>(w0, w1));
+    }
+    if (ends && c > -kOffset) {                            // (weights of 2^-kOffset or less lose digits in fp16)
+      sum[0] = sum[1] = 0ull;
 #pragma unroll
       for (int e = 0; e < GC / 2; ++e) {
-        const int at = 32 * i + GC * g + 2 * e;
-        const float2 y = upk2(ffma2(pk2(v[at], v[at + 1]), f2, off2));
-        const float w0 = ex2_approx(y.x), w1 = ex2_approx(y.y);
-        sum[e & 1] = fadd2(sum[e & 1], pk2(w0, w1));
-        pk[GC / 2 * g + e] = __uint_as_float(pack2<false>(w0, w1));
+        const uint32_t h = __float_as_uint(pk[GC / 2 * g + e]);
+        const float2 w = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        sum[e & 1] = fadd2(sum[e & 1], pk2(w.x, w.y));
       }
-      if (ends && c > -kOffset) {                          // (weights of 2^-kOffset or less lose digits in fp16)
-        sum[0] = sum[1] = 0ull;
-#pragma unroll
-        for (int e = 0; e < GC / 2; ++e) {
-          const uint32_t h = __float_as_uint(pk[GC / 2 * g + e]);
-          const float2 w = __half22float2(*reinterpret_cast<const __half2*>(&h));
-          sum[e & 1] = fadd2(sum[e & 1], pk2(w.x, w.y));
-        }
-      }
-      const float2 s0 = upk2(sum[0]), s1 = upk2(sum[1]);
-      l += ((s0.x + s0.y) + (s1.x + s1.y)) * ex2_approx(-c);
     }
-    store(i, pk);
+    const float2 s0 = upk2(sum[0]), s1 = upk2(sum[1]);
+    l += ((s0.x + s0.y) + (s1.x + s1.y)) * ex2_approx(-c);
   }
 }
 

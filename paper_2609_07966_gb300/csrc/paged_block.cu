@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         }
       }
       float mt = -INFINITY, mt2 = -INFINITY;
-      tile_max<COLS, 16, BF16>(v, back, scale, mt, mt2);
+      columns_max<COLS, 16, BF16>(v, back, scale, mt, mt2);
       const bool raise = __any_sync(0xffffffffu, mt > m + kRaise || mt2 > m2 + kRaise);
       float w = 1.f;
       if (raise) {
@@ -458,10 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         m2 = nm2;
       }
       float pk[COLS / 2];
-      tile_weights<COLS, 16, BF16>(v, part, m, m2, back, scale, l, [&](int i, const float(&x)[16]) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) pk[16 * i + e] = x[e];
-      });
+      columns_weights<COLS, 16, BF16>(v, part, m, m2, back, scale, l, pk);
       // (the tile before this one's weights have been read, and its product added)
       if (g > 0) wait(&ctl->pvdone, (uint32_t)((g - 1) & 1));
       if (dead) break;

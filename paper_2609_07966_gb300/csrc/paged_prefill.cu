@@ -29,9 +29,10 @@ namespace {
 
 constexpr int kBR = 128;            // rows a block, tokens a tile
 constexpr int kRows = 2 * kBR;      // rows a unit
-constexpr int kThreads = 512;       // two softmax warpgroups, one that converts, one for products and loads (two warps idle)
-constexpr int kRegsSoftmax = 184, kRegsConvert = 72, kRegsOther = 72;
-static_assert(2 * kRegsSoftmax + kRegsConvert + kRegsOther <= 4 * 128, "register shares");
+// Warpgroups: four of softmax (two a block: a row's columns are halved between the threads of two warps, whose chains of
+// instructions then overlap; with one warp a row 156 us for a prompt of 4096 tokens), one that converts, one for products and
+// loads (two warps idle).
+constexpr int kThreads = 768;
 constexpr int kHeads = 8;           // tiles whose heads and scales are held
 constexpr int kSlots = 3;           // widened tiles (K0 V0 K1 V1 ..)
 constexpr int kHeldBatches = 4;     // (a tile is one of at least four of a batch)
@@ -54,13 +55,14 @@ template <int FMT_, int D_, int GC_>
 struct PShape {
   static constexpr int FMT = FMT_, D = D_, GC = GC_, KA = D / 64;
   static constexpr int ATOM = kBR * 128, TILE = KA * ATOM, QBLK = TILE;
-  static constexpr int RAW = kBR * D, RAWS = 4;            // codes of a tile's keys or values
+  static constexpr int RAW = kBR * D, RAWS = 3;            // codes of a tile's keys or values
   static constexpr int Q_OFF = 0, T_OFF = 2 * QBLK;        // [kSlots] widened tiles
   static constexpr int R_OFF = T_OFF + kSlots * TILE;      // [RAWS] codes
   static constexpr int SC_OFF = R_OFF + RAWS * RAW;        // scales of kHeldBatches batches
   static constexpr int HD_OFF = SC_OFF + scale_bytes(kHeldBatches);   // [kHeads] Chunk
   static constexpr int QS_OFF = HD_OFF + kHeads * 16;      // [256] exponents that bf16 rows are scaled by
-  static constexpr int CTL_OFF = QS_OFF + kRows;
+  static constexpr int X_OFF = QS_OFF + kRows;             // [2][256] float2: what the halves of a row tell each other
+  static constexpr int CTL_OFF = X_OFF + 2 * kRows * 8;
   static constexpr int ALLOC = CTL_OFF + 512;
   static_assert(ALLOC <= 227 * 1024, "shared memory");
 };
@@ -135,9 +137,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     return;
   }
 
-  if (warp == 12) tc_alloc(&ctl->tslot, 512);
+  if (warp == 20) tc_alloc(&ctl->tslot, 512);
   if (threadIdx.x == 0) {
-    tc_mbar_init(&ctl->qfull, 8);
+    tc_mbar_init(&ctl->qfull, 16);
     tc_mbar_init(&ctl->drained, 1);
     for (int s = 0; s < S::RAWS; ++s) {
       tc_mbar_init(&ctl->raw_full[s], 1);
@@ -166,9 +168,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
   uint32_t* status = a.status;
   const int all_copies = (1 << (kTokens >> a.w.log_box)) - 1;
 
-  if (warp >= 12) {
-    regs_down<kRegsOther>();
-    if (warp == 12 && elect_one()) {
+  if (warp >= 20) {
+    if (warp == 20 && elect_one()) {
       // ---------------------------------------------------------------- products
       constexpr uint32_t idS = tc_idesc(false, kBR, kBR, false, false);
       constexpr uint32_t idO = tc_idesc(false, kBR, D, false, true);
@@ -190,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       };
       auto values = [&](int k, int t, int half) {           // over half of tile t's tokens
         const Desc v0 = vd.at((2 * t + 1) % kSlots * S::TILE + half * (kBR / 2) * 128).opaque();
-        const uint32_t p0 = tbase + (uint32_t)(k * kBR + half * (kBR / 4));
+        const uint32_t p0 = tbase + (uint32_t)(k * kBR + half * (kBR / 2));
 #pragma unroll
         for (int kk = 0; kk < kBR / 32; ++kk)
           tc_mma_ts(tbase + (uint32_t)(2 * kBR + k * kBR), p0 + (uint32_t)(kk * 8), v0.at(kk * 2048), idO,
@@ -226,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         }
       }
       tc_commit(&ctl->drained);
-    } else if (warp == 13) {
+    } else if (warp == 21) {
       // ---------------------------------------------------------------- loads
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
@@ -262,14 +263,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
             if (lane == 0) tc_mbar_arrive(&ctl->head[t % kHeads]);
           });
     }
-  } else if (warp >= 8) {
-    regs_down<kRegsConvert>();
+  } else if (warp >= 16) {
     // ---------------------------------------------------------------- codes to fp16
     // A thread takes one 16-byte piece of every STEP'th row.  Of eight neighbouring threads four read the first half of one
     // row and four the second half of the next: different banks, and so are those of the pieces that they store, in an atom
     // each (two rows of one atom with 64 dims).
     constexpr int STEP = D == 128 ? 16 : 32;
-    const int tid = threadIdx.x - 256;
+    const int tid = threadIdx.x - 512;
     const int piece = D == 128 ? tid & 7 : tid & 3;
     const int row = D == 128 ? (tid >> 4) * 2 + ((tid >> 2 ^ tid >> 3) & 1) : tid >> 2;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -311,8 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       }
     }
   } else {
-    regs_up<kRegsSoftmax>();
-    const int k = warp >> 2;
+    const int k = warp >> 3, half = warp >> 2 & 1;         // its block; its columns 64 half ..
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tbase + lanes + (uint32_t)(k * kBR), tO = tbase + lanes + (uint32_t)(2 * kBR + k * kBR);
     int8_t* qs = reinterpret_cast<int8_t*>(sm + S::QS_OFF);
@@ -321,11 +320,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       constexpr int LN = D / 8, PER = 32 / LN, U = 4;
       const int ch = lane % LN;
 #pragma unroll 1
-      for (int r0 = warp * PER + lane / LN; r0 < kRows; r0 += 8 * PER * U) {
+      for (int r0 = warp * PER + lane / LN; r0 < kRows; r0 += 16 * PER * U) {
         uint4 y[U];
 #pragma unroll
         for (int q = 0; q < U; ++q) {
-          const int row = base_row + r0 + q * 8 * PER;
+          const int row = base_row + r0 + q * 16 * PER;
           y[q] = make_uint4(0, 0, 0, 0);
           if (row < u.rows)
             y[q] = *reinterpret_cast<const uint4*>(c.q + (u.row0 + row / u.G) * c.q_stride +
@@ -333,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         }
 #pragma unroll
         for (int q = 0; q < U; ++q) {
-          const int r = r0 + q * 8 * PER;
+          const int r = r0 + q * 16 * PER;
           if (BF16) {                                      // a power of two a row (paged_decode.cu)
             float v[8], most = 0.f;
             widen8<true>(y[q], v);
@@ -356,7 +355,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       __syncwarp();
       if (lane == 0) tc_mbar_arrive(&ctl->qfull);
     }
-    bool dead = false;      // this warp's waits ran out: no barrier but mbarriers joins warps here, so it just stops
+    // A warp whose wait ran out stops waiting but still meets its partner, so that neither is left waiting.
+    bool dead = false;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       if (!dead) dead = !__all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status));
       tc_fence_after();
@@ -365,34 +365,55 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     // ---------------------------------------------------------------- softmax: row 32 (warp % 4) + lane of block k
     const int rin = k * kBR + (warp & 3) * 32 + lane, row = base_row + rin, seen = u.seen(row);
     const int td = u.seen(base_row) / kBR;                 // first tile that the unit's first row does not see whole
+    float2* tell = reinterpret_cast<float2*>(sm + S::X_OFF) + half * kRows + rin;
+    const float2* hear = reinterpret_cast<const float2*>(sm + S::X_OFF) + (1 - half) * kRows + rin;
+    auto exchange = [&](float2 x) {                        // with the warp that has the rows' other columns
+      const int pair = 1 + k * 4 + (warp & 3);
+      *tell = x;
+      bar_sync(pair, 64);
+      const float2 y = *hear;
+      bar_sync(pair, 64);
+      return y;
+    };
     float back = 1.f;
     if (BF16) {                                            // (all warps' queries are in place)
       wait(&ctl->qfull, 0);
       back = power_of_two(-(int)qs[rin]);
     }
+    constexpr int HC = kBR / 2;                            // columns of a thread
+    const uint32_t tH = tS + (uint32_t)(half * HC);
+    const int log_group = a.w.log_box - 4;
     float m = kNoMax, m2 = kNoMax, l = 0.f;
     for (int t = 0; t < nt[k]; ++t) {
-      if (!wait(&ctl->head[t % kHeads], (uint32_t)((t / kHeads) & 1)) || !wait(&ctl->sfull[k], (uint32_t)(t & 1))) break;
-      const int copies = heads[t % kHeads].copies, log_group = a.w.log_box - 4;
+      wait(&ctl->head[t % kHeads], (uint32_t)((t / kHeads) & 1));
+      wait(&ctl->sfull[k], (uint32_t)(t & 1));
+      const int copies = heads[t % kHeads].copies;
       const float2* scales = reinterpret_cast<const float2*>(sm + S::SC_OFF) + heads[t % kHeads].scales;
-      float v[kBR];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) tm_issue<32>(tS + i * 32, *reinterpret_cast<float(*)[32]>(&v[i * 32]));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) tm_wait<32>(*reinterpret_cast<float(*)[32]>(&v[i * 32]));
-      auto scale = [&](int g) { return scales[GC == 16 ? g >> log_group : g >> (log_group - 1)]; };
       const bool part = c0 + t >= td || copies != all_copies;      // (a page outside the pool or past the length)
-      if (part) {
-        const int lim = seen - (c0 + t) * kBR;             // columns of the tile that this row sees
+      const int lim = seen - (c0 + t) * kBR - half * HC;   // this thread's columns that its row sees
+      // 32 columns' scores, those that the row does not see minus infinity
+      auto load = [&](int i, float (&v)[32]) {
+        tm_load<32>(tH + (uint32_t)(32 * i), v);
+        if (part) {
 #pragma unroll
-        for (int g = 0; g < 8; ++g) {
-          const int upto = copies >> (g >> log_group) & 1 ? lim : 0;
+          for (int g = 0; g < 2; ++g) {
+            const int upto = copies >> ((4 * half + 2 * i + g) >> log_group) & 1 ? lim - 32 * i : 0;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[16 * g + i] = 16 * g + i < upto ? v[16 * g + i] : -INFINITY;
+            for (int e = 16 * g; e < 16 * g + 16; ++e) v[e] = e < upto ? v[e] : -INFINITY;
+          }
         }
-      }
+      };
+      auto scale_of = [&](int i, int g) { return scales[(4 * half + 2 * i + g * (GC / 16)) >> log_group]; };
       float mt = -INFINITY, mt2 = -INFINITY;
-      tile_max<kBR, GC, BF16>(v, back, scale, mt, mt2);
+#pragma unroll 1
+      for (int i = 0; i < HC / 32; ++i) {
+        float v[32];
+        load(i, v);
+        columns_max<32, GC, BF16>(v, back, [&](int g) { return scale_of(i, g); }, mt, mt2);
+      }
+      const float2 other = exchange(make_float2(mt, mt2));
+      mt = fmaxf(mt, other.x);
+      mt2 = fmaxf(mt2, other.y);
       if (__any_sync(0xffffffffu, mt > m + kRaise || mt2 > m2 + kRaise)) {
         const float nm = fmaxf(m, mt), nm2 = fmaxf(m2, mt2);
         l *= ex2_approx(m - nm);
@@ -400,9 +421,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         m = nm;
         m2 = nm2;
         if (t > 0) {
-          if (!wait(&ctl->pvdone[k], (uint32_t)((t - 1) & 1))) break;
+          wait(&ctl->pvdone[k], (uint32_t)((t - 1) & 1));
 #pragma unroll 1
-          for (int i = 0; i < D / 32; ++i) {
+          for (int i = half * (D / 64); i < (half + 1) * (D / 64); ++i) {
             float o[32];
             tm_load<32>(tO + i * 32, o);
 #pragma unroll
@@ -411,28 +432,31 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
           }
         }
       }
-      tile_weights<kBR, GC, BF16>(v, part, m, m2, back, scale, l, [&](int h, const float(&pk)[16]) {
-        tm_store<16>(tS + h * 16, pk);
-        if (h & 1) {
-          tm_store_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) tc_mbar_arrive(&ctl->pfull[k][h >> 1]);
-        }
-      });
+#pragma unroll 1
+      for (int i = 0; i < HC / 32; ++i) {                  // (weights over scores that were read before)
+        float v[32], pk[16];
+        load(i, v);
+        columns_weights<32, GC, BF16>(v, part, m, m2, back, [&](int g) { return scale_of(i, g); }, l, pk);
+        tm_store<16>(tH + (uint32_t)(16 * i), pk);
+      }
+      tm_store_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc_mbar_arrive(&ctl->pfull[k][half]);
     }
     // ---------------------------------------------------------------- output
     if (nt[k] > 0) wait(&ctl->pvdone[k], (uint32_t)((nt[k] - 1) & 1));
+    l += exchange(make_float2(l, 0.f)).x;
     if (!dead) {
       const bool whole = a.splits == 1;
       // zeros for a row that sees nothing; NaN for one whose scores are all minus infinity
       const float inv = seen <= 0 ? 0.f : l == 0.f ? NAN : 1.f / l, hp = half_power(m, m2);
-      if (!whole) a.part_st[part + rin] = make_float4(m, l, m2, 0.f);
+      if (!whole && half == 0) a.part_st[part + rin] = make_float4(m, l, m2, 0.f);
       uint16_t* dst = c.out + (u.row0 + row / u.G) * c.out_stride + (int64_t)(u.kvh * u.G + row % u.G) * D;
       float* po = a.part_o + (part + rin) * D;
       if (nt[k] > 0) {
 #pragma unroll 1
-        for (int i = 0; i < D / 32; ++i) {
+        for (int i = half * (D / 64); i < (half + 1) * (D / 64); ++i) {
           float o[32];
           tm_load<32>(tO + i * 32, o);
           if (row >= u.rows) continue;
@@ -464,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
   }
   __syncthreads();
   tc_fence_after();
-  if (warp == 12) tc_dealloc(tbase, 512);
+  if (warp == 20) tc_dealloc(tbase, 512);
 }
 
 // out = sum_s 2^(m2_s - M2) o_s / sum_s 2^(m_s - M) l_s, a warp a row.
