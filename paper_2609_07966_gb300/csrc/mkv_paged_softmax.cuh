@@ -32,6 +32,21 @@ __device__ __forceinline__ float max_of(const float* y) {
   return fmax3(x0, x1, fmaxf(y[N - 2], y[N - 1]));         // (N is a multiple of 4: two are left)
 }
 
+// 32 fp32 columns of the thread's tensor-memory lane, load and wait as one statement (as two, the wait names the registers
+// again and the compiler copies them).
+__device__ __forceinline__ void tm_read32(uint32_t addr, float (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+      "tcgen05.wait::ld.sync.aligned;\n"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]),
+        "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), "=f"(v[24]),
+        "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+      : "r"(addr)
+      : "memory");
+}
+
 // Raises mt and mt2 to the largest of N columns' scores and scores + log2 vs; GC of them share scale(g).
 template <int N, int GC, bool BACK, typename Scale>
 __device__ __forceinline__ void columns_max(const float (&v)[N], float back, Scale scale, float& mt, float& mt2) {

@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       const int lim = seen - (c0 + t) * kBR - half * HC;   // this thread's columns that its row sees
       // 32 columns' scores, those that the row does not see minus infinity
       auto load = [&](int i, float (&v)[32]) {
-        tm_load<32>(tH + (uint32_t)(32 * i), v);
+        tm_read32(tH + (uint32_t)(32 * i), v);
         if (part) {
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
