@@ -66,16 +66,22 @@ __device__ __forceinline__ const float2* turn_row(const RopeCall& r, int64_t p, 
 
 // Entry b's rows of the n flattened ones: the first, and how many.
 struct EntryRows {
-  int64_t first, count;
+  int first, count;
 };
 __device__ __forceinline__ EntryRows entry_rows(const PagedShape& s, int b) {
-  if (s.start == nullptr) {
-    const int64_t m = s.n / s.B;
-    return {b * m, m};
-  }
-  const int64_t r0 = min(max((int64_t)s.start[b], (int64_t)0), s.n);
-  return {r0, min(max((int64_t)s.start[b + 1], r0), s.n) - r0};
+  if (s.start == nullptr) return {b * s.each, s.each};
+  const int n = (int)s.n, r0 = min(max(s.start[b], 0), n);
+  return {r0, min(max(s.start[b + 1], r0), n) - r0};
 }
+
+// Division by the heads of a group, G <= 32, of numbers up to 2^26: x ceil(2^32 / G) / 2^32.
+struct Heads {
+  int G;
+  uint32_t inv;                    // (0: G is 1)
+  __host__ __device__ Heads(int g = 1) : G(g), inv(g == 1 ? 0u : (uint32_t)(((1ull << 32) + g - 1) / g)) {}
+  __device__ __forceinline__ int token(int row) const { return inv == 0u ? row : (int)__umulhi((uint32_t)row, inv); }
+  __device__ __forceinline__ int head(int row) const { return row - token(row) * G; }
+};
 
 // The last entry of B that begins at or before what is looked for (`begins(b)`, true up to it; 32 entries at a time, by a
 // whole warp).

@@ -39,7 +39,8 @@ cudaError_t launch_rope_apply(const RopeApplyCall& c, cudaStream_t st);
 // What the append and the attention share of a paged cache.
 struct PagedShape {
   int dtype, format, B, Hq, Hkv, D, page;
-  int64_t n;                       // rows of all entries
+  int64_t n;                       // rows of all entries (fits 32 bits)
+  int each;                        // start null: rows of every entry
   const int32_t* start;            // [B + 1] or null: n / B each
   int64_t num_pages, max_pages;
   const int32_t* page_table;

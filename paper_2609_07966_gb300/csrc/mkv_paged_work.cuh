@@ -62,8 +62,8 @@ struct Entry {
 __device__ __forceinline__ Entry entry_of(const PagedAttnCall& c, const WorkArgs& w, int b, uint32_t* report) {
   const EntryRows r = entry_rows(c.s, b);
   Entry e;
-  e.row0 = (int)r.first;
-  e.tokens = (int)min(r.count, c.max_rows + 1);
+  e.row0 = r.first;
+  e.tokens = (int)min((int64_t)r.count, c.max_rows + 1);
   e.len = (int)min((int64_t)max(c.T_len[b], 0), c.s.max_pages << w.log_page);
   if (e.tokens > c.max_rows) {
     if (report != nullptr) atomicOr(report, MKV_FLAG_BAD_INDEX);

@@ -119,6 +119,7 @@ PagedShape shape_of(const mkv_paged_config* c, int64_t n, const int32_t* start, 
   s.D = c->D;
   s.page = c->page_size;
   s.n = n;
+  s.each = start == nullptr ? (int)(n / c->B) : 0;
   s.start = start;
   if (k != nullptr) {
     s.num_pages = k->num_pages;
@@ -131,6 +132,8 @@ PagedShape shape_of(const mkv_paged_config* c, int64_t n, const int32_t* start, 
 mkv_status check_attention_rows(const mkv_paged_config* c, int64_t n, int64_t max_rows) {
   MKV_REQUIRE(n >= 1 && max_rows >= 1 && max_rows <= n, MKV_ERR_INVALID_ARG, "rows must be 1 <= max_rows <= n");
   MKV_REQUIRE(n <= INT32_MAX, MKV_ERR_UNSUPPORTED, "n = %lld too large", (long long)n);
+  // (a row's token is found by a multiplication that is exact up to there)
+  MKV_REQUIRE(max_rows * (c->Hq / c->Hkv) <= 1 << 26, MKV_ERR_UNSUPPORTED, "max_rows x query heads a key head above %d", 1 << 26);
   return MKV_OK;
 }
 

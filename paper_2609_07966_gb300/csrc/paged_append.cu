@@ -272,9 +272,9 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a) {
   const int t = c.T_len[b];
   const int64_t t0 = max(t, 0);
   bool ok = t >= 0, pages = true;
-  ok = ok && t0 + rows.count <= c.s.max_pages * page;
+  ok = ok && t0 + (int64_t)rows.count <= c.s.max_pages * page;
   if (ok)
-    for (int64_t p = t0 / page + threadIdx.x; p <= (t0 + rows.count - 1) / page; p += kThreads) {
+    for (int64_t p = t0 / page + threadIdx.x; p <= (t0 + (int64_t)rows.count - 1) / page; p += kThreads) {
       const int pid = c.s.page_table[b * c.s.max_pages + p];
       pages = pages && pid >= 0 && pid < c.s.num_pages;
     }
@@ -286,12 +286,12 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a) {
       if (!ok || !pages)
         atomicOr(a.status, ok ? MKV_FLAG_BAD_INDEX : MKV_FLAG_CACHE_FULL);
       else
-        c.T_len[b] = (int)(t0 + rows.count);
+        c.T_len[b] = (int)(t0 + (int64_t)rows.count);
     }
   }
   Slot s;
   const int off = (int)(t0 % page);
-  const int64_t i0 = max((int64_t)0, (int64_t)j * page - off), i1 = min(rows.count, (int64_t)(j + 1) * page - off);
+  const int64_t i0 = max((int64_t)0, (int64_t)j * page - off), i1 = min((int64_t)rows.count, (int64_t)(j + 1) * page - off);
   if (i0 >= i1) return;
   s.row0 = rows.first + i0;
   s.token0 = (int64_t)t + i0;

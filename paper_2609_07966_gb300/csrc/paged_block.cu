@@ -38,7 +38,7 @@ struct BlockArgs {
   PagedAttnCall c;
   WorkArgs w;
   uint32_t* status;
-  int G;
+  Heads heads;
   int* tickets;                     // [B][Hkv], zero between calls
   float* part_o;                    // [kGrid][2][ROWS][D]
   float4* part_st;                  // [kGrid][2][ROWS]: m, sum, m2
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
     regs_up<kRegsSoftmax>();
     // ---------------------------------------------------------------- softmax: lane 32 warp + lane, row `row` of copy `copy`
     constexpr int COLS = S::COLS, NG = S::NG;
-    const int at = warp * 32 + lane, copy = at / S::ROWS, row = at % S::ROWS, G = a.G;
+    const int at = warp * 32 + lane, copy = at / S::ROWS, row = at % S::ROWS, G = a.heads.G;
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const uint32_t tO = tbase + lanes + S::O, tP = tbase + lanes + S::P + (uint32_t)(copy * COLS / 2);
     float* ob = reinterpret_cast<float*>(sm + S::O_OFF);
@@ -297,8 +297,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
     auto store_out = [&](const Piece& h, int r, int d, float4 x, float mm, float sum, float mm2) {
       const float f = half_power(mm, mm2), inv = sum == 0.f ? NAN : 1.f / sum;
       x = make_float4(x.x * inv * f * f, x.y * inv * f * f, x.z * inv * f * f, x.w * inv * f * f);
-      if (h.len - h.tokens + r / G < 0) x = make_float4(0.f, 0.f, 0.f, 0.f);
-      uint16_t* dst = c.out + (int64_t)(h.row0 + r / G) * c.out_stride + (int64_t)(h.kvh * G + r % G) * D + d;
+      if (h.len - h.tokens + a.heads.token(r) < 0) x = make_float4(0.f, 0.f, 0.f, 0.f);
+      uint16_t* dst = c.out + (int64_t)(h.row0 + a.heads.token(r)) * c.out_stride + (int64_t)(h.kvh * G + a.heads.head(r)) * D + d;
       *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<BF16>(x.x, x.y), pack2<BF16>(x.z, x.w));
     };
     // A piece was handed in and the unit's ticket taken (by thread 0, which looks at it only here): the CTA that took the
@@ -386,8 +386,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       if (now.flags & kFirst) {
         // ---------------------------------------------------------- queries to tensor memory (the earlier piece's are read)
         float q[D / 2];
-        const uint4* src = reinterpret_cast<const uint4*>(c.q + (int64_t)(hd.row0 + row / G) * c.q_stride +
-                                                          (int64_t)(hd.kvh * G + row % G) * D);
+        const uint4* src = reinterpret_cast<const uint4*>(c.q + (int64_t)(hd.row0 + a.heads.token(row)) * c.q_stride +
+                                                          (int64_t)(hd.kvh * G + a.heads.head(row)) * D);
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) {
           const uint4 y = row < R ? src[i] : make_uint4(0u, 0u, 0u, 0u);
@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         if (lane == 0) tc_mbar_arrive(&ctl->qfull);
         m = m2 = kNoMax;
         l = 0.f;
-        own = hd.len - hd.tokens + row / G;
+        own = hd.len - hd.tokens + a.heads.token(row);
       }
       const float2* scales = reinterpret_cast<const float2*>(sm + S::SC_OFF) + now.scales;
       auto copy_of = [&](int i) { return (copy * NG + i) >> (a.w.log_box - 4); };   // that holds group i of this copy's tokens
@@ -596,7 +596,7 @@ cudaError_t launch_paged_block(const PagedAttnCall& c, void* ws, cudaStream_t st
   if (e != cudaSuccess) return e;
   a.c = c;
   a.w = work_args(c, kGrid);
-  a.G = c.s.Hq / c.s.Hkv;
+  a.heads = Heads(c.s.Hq / c.s.Hkv);
   uint8_t* base = static_cast<uint8_t*>(ws);
   a.tickets = reinterpret_cast<int*>(base);
   a.part_st = reinterpret_cast<float4*>(base + kCounterBytes);

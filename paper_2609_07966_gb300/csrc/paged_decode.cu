@@ -36,7 +36,7 @@ constexpr int kGrid = kCtas * kNumSMs;
 struct DecodeArgs {
   PagedAttnCall c;
   uint32_t* status;
-  int G;
+  Heads heads;
   WorkArgs w;
   int* tickets;                     // [B][Hkv], zero between calls
   float* part_o;                    // [kGrid][2][N][D]
@@ -121,14 +121,14 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         c, a.w, status, reinterpret_cast<float2*>(sm + S::SC_OFF), lane,
         [&](const Piece& p) {                              // a piece's queries: one copy a token's heads
           if (pieces > 0 && !wait(&ctl->qempty, (uint32_t)((pieces - 1) & 1))) return false;
-          const int bytes = a.G * D * 2;
+          const int bytes = a.heads.G * D * 2;
           if (lane == 0) {
             tc_mbar_expect_tx(&ctl->qfull, (uint32_t)(p.tokens * bytes));
             ctl->q_loads = pieces + 1;
           }
           __syncwarp();
           if (lane < p.tokens)
-            bulk_load(sm + S::Q_OFF + lane * bytes, c.q + (int64_t)(p.row0 + lane) * c.q_stride + (int64_t)p.kvh * a.G * D,
+            bulk_load(sm + S::Q_OFF + lane * bytes, c.q + (int64_t)(p.row0 + lane) * c.q_stride + (int64_t)p.kvh * a.heads.G * D,
                       bytes, &ctl->qfull);
           ++pieces;
           return true;
@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     const int lg = lane >> 2, lr = lane & 3;
     float4* stat = reinterpret_cast<float4*>(sm + S::ST_OFF);
     const bool bf16 = c.s.dtype == MKV_BF16;
-    const int G = a.G;
+    const int G = a.heads.G;
     bool dead = false;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       if (!dead) dead = !__all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status));
@@ -186,12 +186,12 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     // An output is o / sum 2^(m2 - m - 6); zeros for a row before position 0, which sees nothing; NaN where no score leaves a
     // weight.
     auto out_row = [&](const Piece& h, int row) {
-      return c.out + (int64_t)(h.row0 + row / G) * c.out_stride + (int64_t)(h.kvh * G + row % G) * D;
+      return c.out + (int64_t)(h.row0 + a.heads.token(row)) * c.out_stride + (int64_t)(h.kvh * G + a.heads.head(row)) * D;
     };
     auto finish = [&](const Piece& h, int row, float4 x, float mm, float sum, float mm2) {
       const float f = half_power(mm, mm2), inv = sum == 0.f ? NAN : 1.f / sum;
       x = make_float4(x.x * inv * f * f, x.y * inv * f * f, x.z * inv * f * f, x.w * inv * f * f);
-      if (h.len - h.tokens + row / G < 0) x = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (h.len - h.tokens + a.heads.token(row) < 0) x = make_float4(0.f, 0.f, 0.f, 0.f);
       return bf16 ? make_uint2(pack2<true>(x.x, x.y), pack2<true>(x.z, x.w))
                   : make_uint2(pack2<false>(x.x, x.y), pack2<false>(x.z, x.w));
     };
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 
     uint32_t qf[2 * KS];
     float back[2], o[MB][4], m[2], m2[2], l[2];
-    int pos0 = 0, pieces = 0;
+    int pos0 = 0, own[2] = {0, 0}, pieces = 0;              // own: rows' own positions, the last that they see
     Piece hd;
     hd.len = hd.tokens = 0;
     // where this lane's pieces of a key row and of two value rows lie; further rows are whole swizzle periods away
@@ -287,6 +287,8 @@ __global__ void __launch_bounds__(kThreads, kCtas)
           l[j] = 0.f;
         }
         pos0 = hd.len - hd.tokens;                         // the first new token's position
+#pragma unroll
+        for (int j = 0; j < 2; ++j) own[j] = pos0 + a.heads.token(2 * lr + j);
       }
       {
         const int ch = now.chunk;
@@ -361,9 +363,8 @@ __global__ void __launch_bounds__(kThreads, kCtas)
               x[u][j] *= f;
               x[u][2 + j] *= f;
               if (part) {
-                const int own = in[u] ? pos0 + (2 * lr + j) / G : -1;    // the row's own position: the last that it sees
-                if (t0 + 16 * u + lg > own) x[u][j] = -INFINITY;
-                if (t0 + 16 * u + lg + 8 > own) x[u][2 + j] = -INFINITY;
+                if (!in[u] || t0 + 16 * u + lg > own[j]) x[u][j] = -INFINITY;
+                if (!in[u] || t0 + 16 * u + lg + 8 > own[j]) x[u][2 + j] = -INFINITY;
               }
               const float t = fmaxf(x[u][j], x[u][2 + j]);
               over |= t > m[j] + kRaise || t + sc[u].y > m2[j] + kRaise;
@@ -525,7 +526,7 @@ cudaError_t launch_paged_decode(const PagedAttnCall& c, void* ws, cudaStream_t s
   const cudaError_t e = status_word(&a.status);
   if (e != cudaSuccess) return e;
   a.c = c;
-  a.G = c.s.Hq / c.s.Hkv;
+  a.heads = Heads(c.s.Hq / c.s.Hkv);
   a.w = work_args(c, kGrid);
   uint8_t* base = static_cast<uint8_t*>(ws);
   a.tickets = reinterpret_cast<int*>(base);

@@ -41,9 +41,9 @@ static_assert(kBR == kTokens && kHeads <= (kHeldBatches - 1) * 4, "tiles are chu
 struct PrefillArgs {
   PagedAttnCall c;
   uint32_t* status;
-  int G;
+  Heads heads;
   WorkArgs w;
-  int64_t slots;                    // units of all entries, a key head's
+  int slots;                    // units of all entries, a key head's
   int per;                          // start null: units of an entry
   int splits;                       // parts of a unit's tokens
   float* part_o;                    // [slot][Hkv][splits][256][D]
@@ -72,41 +72,44 @@ struct PCtl {
       pvdone[2];
   uint32_t tslot;
   int fail, loads;
+  int b, rb, rows, pos0, len, row0, live, c0, c1, nt[2];   // the unit, and what of it is this CTA's
 };
 static_assert(sizeof(PCtl) <= 512, "control block");
 
 // Units lie entry after entry, enough of them for each entry's rows.
-__device__ __forceinline__ int64_t unit_base(const PrefillArgs& a, int b) {
-  if (a.c.s.start == nullptr) return (int64_t)b * a.per;
-  return (min(max((int64_t)a.c.s.start[b], (int64_t)0), a.c.s.n) * a.G + (int64_t)b * (kRows - 1)) / kRows;
+__device__ __forceinline__ int unit_base(const PrefillArgs& a, int b) {
+  if (a.c.s.start == nullptr) return b * a.per;
+  const int r0 = min(max(a.c.s.start[b], 0), (int)a.c.s.n);
+  return (int)(((int64_t)r0 * a.heads.G + (int64_t)b * (kRows - 1)) / kRows);
 }
 struct Unit {
-  int b, kvh, rb, rows, G, len;    // rows of the entry (tokens x G)
-  int64_t row0;                    // its first token's row
+  int b, kvh, rb, rows, pos0, len; // its block of rows; rows of the entry (tokens x heads of a group), its first new position
+  int row0;                        // its first token's row
   bool live;
-  __device__ __forceinline__ int pos(int row) const { return len - rows / G + row / G; }   // a row's position
   // tokens that a row sees
-  __device__ __forceinline__ int seen(int row) const { return row < rows ? max(0, min(len, pos(row) + 1)) : 0; }
+  __device__ __forceinline__ int seen(const Heads& h, int row) const {
+    return row < rows ? max(0, min(len, pos0 + h.token(row) + 1)) : 0;
+  }
   // tiles of block k: at least one where it has rows, so that they are written
-  __device__ __forceinline__ int tiles(int k) const {
+  __device__ __forceinline__ int tiles(const Heads& h, int k) const {
     const int first = rb * kRows + k * kBR, last = min(first + kBR, rows) - 1;
-    return last >= first ? max(1, (seen(last) + kBR - 1) / kBR) : 0;
+    return last >= first ? max(1, (seen(h, last) + kBR - 1) / kBR) : 0;
   }
 };
-__device__ __forceinline__ Unit unit_of(const PrefillArgs& a, int64_t slot, int kvh, int lane, bool report) {
+__device__ __forceinline__ Unit unit_of(const PrefillArgs& a, int slot, int kvh, int lane, bool report) {
   Unit u;
-  u.b = a.c.s.start == nullptr ? (int)(slot / a.per)
-                               : find_entry(a.c.s.B, lane, [&](int b) { return unit_base(a, b) <= slot; });
+  u.b = a.c.s.start == nullptr ? slot / a.per : find_entry(a.c.s.B, lane, [&](int b) { return unit_base(a, b) <= slot; });
   u.kvh = kvh;
-  u.G = a.G;
-  u.rb = (int)(slot - unit_base(a, u.b));
+  u.rb = slot - unit_base(a, u.b);
   const EntryRows r = entry_rows(a.c.s, u.b);
   u.row0 = r.first;
   u.live = r.count <= a.c.max_rows;
   if (!u.live && report && u.rb == 0 && kvh == 0) atomicOr(a.status, MKV_FLAG_BAD_INDEX);
-  u.rows = (int)min(r.count, a.c.max_rows) * a.G;
+  const int tokens = (int)min((int64_t)r.count, a.c.max_rows);
+  u.rows = tokens * a.heads.G;
   u.live = u.live && u.rb >= 0 && (int64_t)u.rb * kRows < u.rows;
   u.len = (int)min((int64_t)max(a.c.T_len[u.b], 0), a.c.s.max_pages * a.c.s.page);
+  u.pos0 = u.len - tokens;
   return u;
 }
 
@@ -119,26 +122,31 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
   const PagedAttnCall& c = a.c;
   const int Hkv = c.s.Hkv;
 
-  pdl_wait_and_trigger();
   // Launch order: the last rows of the entries first (they see the most), all key heads and parts of a slot together.
-  const int64_t each = (int64_t)Hkv * a.splits, at = blockIdx.x / each;
-  const int in = (int)(blockIdx.x - at * each), split = in / Hkv;
-  const int64_t slot = a.slots - 1 - at;
-  const Unit u = unit_of(a, slot, in % Hkv, lane, true);
-  if (!u.live) return;
-  const int all0 = u.tiles(0), all1 = u.tiles(1), all = max(all0, all1);
-  const int c0 = (int)((int64_t)all * split / a.splits), c1 = (int)((int64_t)all * (split + 1) / a.splits);
-  const int nt[2] = {max(0, min(all0, c1) - c0), max(0, min(all1, c1) - c0)};   // tiles of each block here
-  const int ntiles = c1 - c0;
-  const int base_row = u.rb * kRows;
-  const int64_t part = ((slot * Hkv + u.kvh) * a.splits + split) * kRows;
-  if (ntiles == 0) {                                       // (fewer tiles than parts)
-    for (int r = threadIdx.x; r < kRows; r += kThreads) a.part_st[part + r] = make_float4(kNoMax, 0.f, kNoMax, 0.f);
-    return;
+  const int each = Hkv * a.splits, at = blockIdx.x / each, in = blockIdx.x - at * each, split = in / Hkv, kvh = in - split * Hkv;
+  const int slot = a.slots - 1 - at;
+  pdl_wait_and_trigger();
+  if (warp == 0) {                                         // (one warp finds it out: twenty-four took 5 us a CTA)
+    const Unit u = unit_of(a, slot, kvh, lane, true);
+    const int all0 = u.tiles(a.heads, 0), all1 = u.tiles(a.heads, 1), all = max(all0, all1);
+    const int c0 = a.splits == 1 ? 0 : (int)((int64_t)all * split / a.splits);
+    const int c1 = a.splits == 1 ? all : (int)((int64_t)all * (split + 1) / a.splits);
+    if (lane == 0) {
+      ctl->b = u.b;
+      ctl->rb = u.rb;
+      ctl->rows = u.rows;
+      ctl->pos0 = u.pos0;
+      ctl->len = u.len;
+      ctl->row0 = u.row0;
+      ctl->live = u.live;
+      ctl->c0 = c0;
+      ctl->c1 = c1;
+      ctl->nt[0] = max(0, min(all0, c1) - c0);
+      ctl->nt[1] = max(0, min(all1, c1) - c0);
+    }
   }
-
   if (warp == 20) tc_alloc(&ctl->tslot, 512);
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 32) {
     tc_mbar_init(&ctl->qfull, 16);
     tc_mbar_init(&ctl->drained, 1);
     for (int s = 0; s < S::RAWS; ++s) {
@@ -163,6 +171,22 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
   __syncthreads();
   tc_fence_after();
   const uint32_t tbase = ctl->tslot;
+  Unit u;
+  u.b = ctl->b;
+  u.kvh = kvh;
+  u.rb = ctl->rb;
+  u.rows = ctl->rows;
+  u.pos0 = ctl->pos0;
+  u.len = ctl->len;
+  u.row0 = ctl->row0;
+  const int c0 = ctl->c0, ntiles = ctl->c1 - c0, nt[2] = {ctl->nt[0], ctl->nt[1]}, base_row = u.rb * kRows;
+  const int64_t part = ((int64_t)(slot * Hkv + kvh) * a.splits + split) * kRows;
+  if (!ctl->live || ntiles == 0) {                         // (no such rows; or fewer tiles than parts)
+    if (ctl->live)
+      for (int r = threadIdx.x; r < kRows; r += kThreads) a.part_st[part + r] = make_float4(kNoMax, 0.f, kNoMax, 0.f);
+    if (warp == 20) tc_dealloc(tbase, 512);
+    return;
+  }
   volatile int* fail = &ctl->fail;
   Chunk* heads = reinterpret_cast<Chunk*>(sm + S::HD_OFF);
   uint32_t* status = a.status;
@@ -235,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       const int log_box = a.w.log_box;
       int batch = 0;
       load_chunks<kHeldBatches>(
-          c, a.w, status, reinterpret_cast<float2*>(sm + S::SC_OFF), lane, batch, u.b, u.kvh, u.len, c0, c1, 0,
+          c, a.w, status, reinterpret_cast<float2*>(sm + S::SC_OFF), lane, batch, u.b, u.kvh, u.len, c0, c0 + ntiles, 0,
           [&]() { return true; },
           [&](const Chunk& ch, bool mine, int id, int at) {
             const uint32_t bytes = (uint32_t)(__popc(ch.copies) * D) << log_box;
@@ -317,18 +341,18 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     int8_t* qs = reinterpret_cast<int8_t*>(sm + S::QS_OFF);
     // ---------------------------------------------------------------- queries, D / 8 lanes a row
     {
-      constexpr int LN = D / 8, PER = 32 / LN, U = 4;
+      constexpr int LN = D / 8, PER = 32 / LN, U = kRows / (16 * PER);   // (all of a thread's loads under way together)
       const int ch = lane % LN;
-#pragma unroll 1
-      for (int r0 = warp * PER + lane / LN; r0 < kRows; r0 += 16 * PER * U) {
+      const int r0 = warp * PER + lane / LN;
+      {
         uint4 y[U];
 #pragma unroll
         for (int q = 0; q < U; ++q) {
           const int row = base_row + r0 + q * 16 * PER;
           y[q] = make_uint4(0, 0, 0, 0);
           if (row < u.rows)
-            y[q] = *reinterpret_cast<const uint4*>(c.q + (u.row0 + row / u.G) * c.q_stride +
-                                                   (int64_t)(u.kvh * u.G + row % u.G) * D + ch * 8);
+            y[q] = *reinterpret_cast<const uint4*>(c.q + (u.row0 + a.heads.token(row)) * c.q_stride +
+                                                   (int64_t)(kvh * a.heads.G + a.heads.head(row)) * D + ch * 8);
         }
 #pragma unroll
         for (int q = 0; q < U; ++q) {
@@ -363,8 +387,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       return !dead;
     };
     // ---------------------------------------------------------------- softmax: row 32 (warp % 4) + lane of block k
-    const int rin = k * kBR + (warp & 3) * 32 + lane, row = base_row + rin, seen = u.seen(row);
-    const int td = u.seen(base_row) / kBR;                 // first tile that the unit's first row does not see whole
+    const int rin = k * kBR + (warp & 3) * 32 + lane, row = base_row + rin, seen = u.seen(a.heads, row);
+    const int td = u.seen(a.heads, base_row) / kBR;                 // first tile that the unit's first row does not see whole
     float2* tell = reinterpret_cast<float2*>(sm + S::X_OFF) + half * kRows + rin;
     const float2* hear = reinterpret_cast<const float2*>(sm + S::X_OFF) + (1 - half) * kRows + rin;
     auto exchange = [&](float2 x) {                        // with the warp that has the rows' other columns
@@ -452,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       // zeros for a row that sees nothing; NaN for one whose scores are all minus infinity
       const float inv = seen <= 0 ? 0.f : l == 0.f ? NAN : 1.f / l, hp = half_power(m, m2);
       if (!whole && half == 0) a.part_st[part + rin] = make_float4(m, l, m2, 0.f);
-      uint16_t* dst = c.out + (u.row0 + row / u.G) * c.out_stride + (int64_t)(u.kvh * u.G + row % u.G) * D;
+      uint16_t* dst = c.out + (u.row0 + a.heads.token(row)) * c.out_stride + (int64_t)(kvh * a.heads.G + a.heads.head(row)) * D;
       float* po = a.part_o + (part + rin) * D;
       if (nt[k] > 0) {
 #pragma unroll 1
@@ -496,13 +520,11 @@ template <int D, bool BF16>
 __global__ void __launch_bounds__(256) join_kernel(const PrefillArgs a) {
   pdl_wait_and_trigger();
   const int lane = threadIdx.x & 31, Hkv = a.c.s.Hkv;
-  const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), unit = w / kRows;
-  const int rin = (int)(w - unit * kRows);
-  const int64_t slot = unit / Hkv;
-  const Unit u = unit_of(a, slot, (int)(unit - slot * Hkv), lane, false);
+  const int unit = blockIdx.x / (kRows / 8), rin = blockIdx.x % (kRows / 8) * 8 + (threadIdx.x >> 5), slot = unit / Hkv;
+  const Unit u = unit_of(a, slot, unit - slot * Hkv, lane, false);
   const int row = u.rb * kRows + rin;
   if (!u.live || row >= u.rows) return;
-  const int64_t part = unit * a.splits * kRows + rin;
+  const int64_t part = (int64_t)unit * a.splits * kRows + rin;
   float mx = kNoMax, mx2 = kNoMax;
   const float4 st = lane < a.splits ? a.part_st[part + (int64_t)lane * kRows] : make_float4(kNoMax, 0.f, kNoMax, 0.f);
   mx = st.x;
@@ -530,10 +552,10 @@ __global__ void __launch_bounds__(256) join_kernel(const PrefillArgs a) {
 #pragma unroll
     for (int k = 0; k < VL; ++k) y[k] += f * po[k];
   }
-  const float inv = u.seen(row) <= 0 ? 0.f : sum == 0.f ? NAN : 1.f / sum, hp = half_power(mx, mx2);
+  const float inv = u.seen(a.heads, row) <= 0 ? 0.f : sum == 0.f ? NAN : 1.f / sum, hp = half_power(mx, mx2);
 #pragma unroll
   for (int k = 0; k < VL; ++k) y[k] = inv == 0.f ? 0.f : y[k] * inv * hp * hp;
-  uint16_t* dst = a.c.out + (u.row0 + row / u.G) * a.c.out_stride + (int64_t)(u.kvh * u.G + row % u.G) * D + lane * VL;
+  uint16_t* dst = a.c.out + (u.row0 + a.heads.token(row)) * a.c.out_stride + (int64_t)(u.kvh * a.heads.G + a.heads.head(row)) * D + lane * VL;
   if constexpr (VL == 4)
     *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<BF16>(y[0], y[1]), pack2<BF16>(y[2], y[3]));
   else
@@ -556,7 +578,7 @@ Plan plan_of(const PagedAttnCall& c) {
 
 template <class S, bool BF16>
 cudaError_t launch_shape(const PrefillArgs& a, cudaStream_t st) {
-  const int64_t units = a.slots * a.c.s.Hkv;
+  const int64_t units = (int64_t)a.slots * a.c.s.Hkv;
   if (units * a.splits > INT32_MAX) return cudaErrorInvalidConfiguration;
   constexpr int smem = std::max(S::ALLOC, 116 * 1024);      // one CTA an SM: it takes all of the tensor memory
   cudaError_t e = cudaFuncSetAttribute(prefill_kernel<S, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -587,9 +609,10 @@ cudaError_t launch_paged_prefill(const PagedAttnCall& c, void* ws, cudaStream_t 
   if (e != cudaSuccess) return e;
   const Plan p = plan_of(c);
   a.c = c;
-  a.G = c.s.Hq / c.s.Hkv;
+  a.heads = Heads(c.s.Hq / c.s.Hkv);
   a.w = work_args(c, kNumSMs);
-  a.slots = p.slots;
+  if (p.slots > INT32_MAX) return cudaErrorInvalidConfiguration;
+  a.slots = (int)p.slots;
   a.per = p.per;
   a.splits = p.splits;
   uint8_t* base = static_cast<uint8_t*>(ws) + kCounterBytes;
