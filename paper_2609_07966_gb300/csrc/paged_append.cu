@@ -5,7 +5,8 @@
 //
 // Bound by memory: every row is read once, queries are written in 16 bits and keys and values in 8.  A slot is one page of
 // one entry that the call writes into, with the rows that fall into it; its keys and values are units of one head each.
-// A unit's values stay in registers, in fp32, between its maximum and its codes, so that rows are read and rotated once:
+// A unit's rows stay in registers, as they were read, between its maximum and its codes (rotated twice: held in fp32 they left
+// room for two CTAs an SM, and three prompts of 2-4K tokens took 80 us):
 //   warps   a unit a warp, eight units a CTA: decode steps, and pages of 16 tokens (128 work columns);
 //   blocks  a unit a CTA of 256 threads: larger pages filled by prompts.
 // Other CTAs of the slot rotate its rows' queries, a thread the same dims of several heads.
@@ -49,17 +50,13 @@ __device__ __forceinline__ float least_scale(uint32_t most) {
   return __uint_as_float((uint32_t)(127 + min(max(e, kExpMin), kExpMax)) << 23);
 }
 
-// x / scale rounded to codes (x finite or infinite).  A power of two's reciprocal is exact.
-struct Divide {
-  float scale, inv;
-  __device__ __forceinline__ explicit Divide(float s) : scale(s), inv(0.f) {
-    const uint32_t u = __float_as_uint(s), e = u >> 23;
-    if ((u & 0x7fffffu) == 0 && e >= 1 && e <= 253) inv = __uint_as_float((254u - e) << 23);
-  }
-  __device__ __forceinline__ float operator()(float x) const { return inv != 0.f ? x * inv : __fdiv_rn(x, scale); }
-};
-// Eight codes (rounded to nearest even, the largest ones beyond the range).
-template <int FMT>
+// The reciprocal of a power of two, exact; 0 for other scales (and the ends of the range), which have to be divided by.
+__device__ __forceinline__ float exact_inverse(float s) {
+  const uint32_t u = __float_as_uint(s), e = u >> 23;
+  return (u & 0x7fffffu) == 0 && e >= 1 && e <= 253 ? __uint_as_float((254u - e) << 23) : 0.f;
+}
+// Eight codes, rounded to nearest even; SAFE: the largest ones beyond the range.
+template <int FMT, bool SAFE>
 __device__ __forceinline__ uint2 encode8(const float* x) {
   uint32_t w[2];
 #pragma unroll
@@ -69,11 +66,17 @@ __device__ __forceinline__ uint2 encode8(const float* x) {
       asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x[4 * i + 1]), "f"(x[4 * i]));
       asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x[4 * i + 3]), "f"(x[4 * i + 2]));
       w[i] = (uint32_t)lo | (uint32_t)hi << 16;
-    } else {
+    } else if (SAFE) {
       w[i] = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         w[i] |= ((uint32_t)min(max(__float2int_rn(x[4 * i + k]), -127), 127) & 0xffu) << (8 * k);
+    } else {
+      // (|x| <= 127: at 1.5 2^23 a unit is the last place, so the sum's low byte is x rounded)
+      uint32_t u[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) u[k] = __float_as_uint(__fadd_rn(x[4 * i + k], 12582912.f));
+      w[i] = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
     }
   }
   return make_uint2(w[0], w[1]);
@@ -98,85 +101,117 @@ struct Slot {
   int64_t pid;
 };
 
-// One column of 16 dims of a unit's row: its two runs of eight dims, rotated.
-template <int D, bool BF16>
-__device__ __forceinline__ void load_column(const AppendArgs& a, const Slot& s, bool key, int h, int e, float (&x)[16], int& lo,
-                                            int& hi) {
+// A column of 16 dims of a unit's row: two runs of eight dims, at lo and hi; `turn`: they are rotated.
+struct Column {
+  int i, col, lo, hi;
+  bool turn;
+};
+template <int D>
+__device__ __forceinline__ Column column_of(const AppendArgs& a, bool key, int e) {
   constexpr int kCols = D / 16;
-  const int i = e / kCols, col = e % kCols;
-  const int64_t row = s.row0 + i;
-  const bool turn = key && col < a.c.rope.rot / 16;
-  lo = turn ? turn_lo(col, a.c.rope.pairs) : 16 * col;
-  hi = turn ? turn_hi(col, a.c.rope.rot, a.c.rope.pairs) : 16 * col + 8;
+  Column c;
+  c.i = e / kCols;
+  c.col = e % kCols;
+  c.turn = key && c.col < a.c.rope.rot / 16;
+  c.lo = c.turn ? turn_lo(c.col, a.c.rope.pairs) : 16 * c.col;
+  c.hi = c.turn ? turn_hi(c.col, a.c.rope.rot, a.c.rope.pairs) : 16 * c.col + 8;
+  return c;
+}
+template <int D>
+__device__ __forceinline__ void load_column(const AppendArgs& a, const Slot& s, bool key, int h, int e, uint4& lo, uint4& hi) {
+  const Column c = column_of<D>(a, key, e);
+  const int64_t row = s.row0 + c.i;
   const uint16_t* p = (key ? a.c.k_new + row * a.c.k_stride : a.c.v_new + row * a.c.v_stride) + h * D;
-  const uint4 p0 = *reinterpret_cast<const uint4*>(p + lo), p1 = *reinterpret_cast<const uint4*>(p + hi);
-  Turn8 t;
-  if (turn) t.load(turn_row(a.c.rope, a.c.pos != nullptr ? a.c.pos[row] : s.token0 + i, a.status), 8 * col);
-  widen8<BF16>(p0, x);
-  widen8<BF16>(p1, x + 8);
-  if (turn) rotate16(x, t, a.c.rope.pairs, 1.f);
+  lo = *reinterpret_cast<const uint4*>(p + c.lo);
+  hi = *reinterpret_cast<const uint4*>(p + c.hi);
+}
+// Its values, rotated.
+template <int D, bool BF16>
+__device__ __forceinline__ void turn_column(const AppendArgs& a, const Slot& s, const Column& c, const uint4& lo, const uint4& hi,
+                                            float (&x)[16]) {
+  widen8<BF16>(lo, x);
+  widen8<BF16>(hi, x + 8);
+  if (c.turn) {
+    Turn8 t;
+    t.load(turn_row(a.c.rope, a.c.pos != nullptr ? a.c.pos[s.row0 + c.i] : s.token0 + c.i, a.status), 8 * c.col);
+    rotate16(x, t, a.c.rope.pairs, 1.f);
+  }
 }
 
-template <int FMT, int D>
-__device__ __forceinline__ void store_column(uint8_t* page, const Slot& s, int e, float (&x)[16], int lo, int hi,
-                                             const Divide& div) {
-  constexpr int kCols = D / 16;
-  uint8_t* row = page + (int64_t)(s.at + e / kCols) * D;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = x[i] == x[i] ? div(x[i]) : 0.f;
-  *reinterpret_cast<uint2*>(row + lo) = encode8<FMT>(x);
-  *reinterpret_cast<uint2*>(row + hi) = encode8<FMT>(x + 8);
-}
-
-// GROUP threads (a warp or the CTA) quantize one head's keys or values of a slot.
+// GROUP threads (a warp or the CTA) quantize one head's keys or values of a slot.  `lo`, `hi`: what this thread holds; `was`:
+// the page's scale if it holds tokens.
 template <int FMT, int D, bool BF16, int GROUP>
-__device__ __forceinline__ void quantize_unit(const AppendArgs& a, const Slot& s, bool key, int h) {
+__device__ __forceinline__ void quantize_unit(const AppendArgs& a, const Slot& s, bool key, int h, const uint4 (&lo)[kKeep],
+                                              const uint4 (&hi)[kKeep], float was) {
   constexpr int kCols = D / 16;
   const int tid = threadIdx.x % GROUP, items = s.count * kCols;
   const int64_t head = s.pid * a.c.s.Hkv + h;
-  float* scale = (key ? a.c.k_scale : a.c.v_scale) + head;
   uint8_t* page = (key ? a.c.k : a.c.v) + head * a.c.s.page * D;
-  const float was = s.held > 0 ? *scale : 0.f;
-  float x[kKeep][16];
-  int lo[kKeep], hi[kKeep];
   uint32_t most = 0;
-  bool bad = false;
-  auto measure = [&](const float(&y)[16]) {
+  bool bad = false;                                        // an infinity or NaN
+  auto measure = [&](int e, const uint4& p0, const uint4& p1) {
+    const Column c = column_of<D>(a, key, e);
+    if (c.turn) {
+      float y[16], top = 0.f, zero = 0.f;
+      turn_column<D, BF16>(a, s, c, p0, p1, y);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const uint32_t u = __float_as_uint(y[i]) & 0x7fffffffu;
-      const bool no = u >= 0x7f800000u;
-      bad |= no;
-      most = max(most, no ? 0u : u);
+      for (int i = 0; i < 16; ++i) {
+        top = fmaxf(top, fabsf(y[i]));
+        zero = fmaf(y[i], 0.f, zero);                      // (NaN if any value is not finite)
+      }
+      if (zero == 0.f) {
+        most = max(most, __float_as_uint(top));
+      } else {
+        bad = true;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t u = __float_as_uint(y[i]) & 0x7fffffffu;
+          most = max(most, u < 0x7f800000u ? u : 0u);
+        }
+      }
+    } else {                                               // two values a word, as they are: their order is that of their bits
+      constexpr uint32_t inf = BF16 ? 0x7f80u : 0x7c00u;
+      const uint32_t w[8] = {p0.x, p0.y, p0.z, p0.w, p1.x, p1.y, p1.z, p1.w};
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+      uint32_t top = max(m & 0xffffu, m >> 16);
+      if (top >= inf) {
+        bad = true;
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t x0 = w[i] & 0x7fffu, x1 = w[i] >> 16 & 0x7fffu;
+          top = max(top, max(x0 < inf ? x0 : 0u, x1 < inf ? x1 : 0u));
+        }
+      }
+      most = max(most, __float_as_uint(widen<BF16>((uint16_t)top)));
     }
   };
 #pragma unroll
   for (int k = 0; k < kKeep; ++k)
-    if (tid + k * GROUP < items) {
-      load_column<D, BF16>(a, s, key, h, tid + k * GROUP, x[k], lo[k], hi[k]);
-      measure(x[k]);
-    }
+    if (tid + k * GROUP < items) measure(tid + k * GROUP, lo[k], hi[k]);
   // (warps: more than 16 tokens of an entry that the others do not have; they are read again below)
   if (GROUP == 32)
     for (int e = tid + kKeep * GROUP; e < items; e += GROUP) {
-      float y[16];
-      int l, g;
-      load_column<D, BF16>(a, s, key, h, e, y, l, g);
-      measure(y);
+      uint4 p0, p1;
+      load_column<D>(a, s, key, h, e, p0, p1);
+      measure(e, p0, p1);
     }
   if (bad) atomicOr(a.status, MKV_FLAG_NOT_FINITE);
   most = __reduce_max_sync(0xffffffffu, most);
+  bool safe = __any_sync(0xffffffffu, bad);
   if constexpr (GROUP > 32) {
     __shared__ uint32_t of_warp[GROUP / 32];
     if ((tid & 31) == 0) of_warp[tid >> 5] = most;
-    __syncthreads();
+    safe = __syncthreads_or(bad);
 #pragma unroll
     for (int w = 0; w < GROUP / 32; ++w) most = max(most, of_warp[w]);
   }
   const bool fits = s.held > 0 && __uint_as_float(most) <= top_code<FMT>() * was;
   const float now = fits ? was : least_scale<FMT>(most);
   if (!fits) {
-    if (tid == 0) *scale = now;
+    if (tid == 0) (key ? a.c.k_scale : a.c.v_scale)[head] = now;
     if (s.held > 0) {
       const float less = __fdiv_rn(was, now);
       for (int e = tid; e < s.held * kCols; e += GROUP) {
@@ -189,21 +224,44 @@ __device__ __forceinline__ void quantize_unit(const AppendArgs& a, const Slot& s
         decode4<FMT>(old.w, y + 12);
 #pragma unroll
         for (int i = 0; i < 16; ++i) y[i] *= less;
-        const uint2 n0 = encode8<FMT>(y), n1 = encode8<FMT>(y + 8);
+        const uint2 n0 = encode8<FMT, true>(y), n1 = encode8<FMT, true>(y + 8);
         *p = make_uint4(n0.x, n0.y, n1.x, n1.y);
       }
     }
   }
-  const Divide div(now);
+  safe |= __uint_as_float(most) > top_code<FMT>() * now;   // (beyond the largest scale)
+  const float inv = exact_inverse(now);
+  auto store = [&](int e, const uint4& p0, const uint4& p1) {
+    const Column c = column_of<D>(a, key, e);
+    float y[16];
+    turn_column<D, BF16>(a, s, c, p0, p1, y);
+    uint8_t* row = page + (int64_t)(s.at + c.i) * D;
+    if (inv != 0.f && !safe) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] *= inv;
+      *reinterpret_cast<uint2*>(row + c.lo) = encode8<FMT, false>(y);
+      *reinterpret_cast<uint2*>(row + c.hi) = encode8<FMT, false>(y + 8);
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < 2; ++i) {
+        float z[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float x = i == 0 ? y[k] : y[8 + k];
+          z[k] = x == x ? __fdiv_rn(x, now) : 0.f;
+        }
+        *reinterpret_cast<uint2*>(row + (i == 0 ? c.lo : c.hi)) = encode8<FMT, true>(z);
+      }
+    }
+  };
 #pragma unroll
   for (int k = 0; k < kKeep; ++k)
-    if (tid + k * GROUP < items) store_column<FMT, D>(page, s, tid + k * GROUP, x[k], lo[k], hi[k], div);
+    if (tid + k * GROUP < items) store(tid + k * GROUP, lo[k], hi[k]);
   if (GROUP == 32)
     for (int e = tid + kKeep * GROUP; e < items; e += GROUP) {
-      float y[16];
-      int l, g;
-      load_column<D, BF16>(a, s, key, h, e, y, l, g);
-      store_column<FMT, D>(page, s, e, y, l, g, div);
+      uint4 p0, p1;
+      load_column<D>(a, s, key, h, e, p0, p1);
+      store(e, p0, p1);
     }
 }
 
@@ -222,7 +280,7 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs& a, const Slot& 
     if (turn) t.load(turn_row(c.rope, c.pos != nullptr ? c.pos[row] : s.token0 + i, a.status), 8 * col);
     const uint16_t* x = c.q + row * c.q_stride;
     uint16_t* out = c.q_out + row * c.q_out_stride;
-    constexpr int U = 4;                                  // heads whose loads are under way together
+    constexpr int U = 2;                                  // heads whose loads are under way together
     for (int h = h0 + sh; h < h1; h += U * side) {
       uint4 p0[U], p1[U];
 #pragma unroll
@@ -250,20 +308,23 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs& a, const Slot& 
 }
 
 template <int FMT, int D, bool BF16, int GROUP>
-__global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) append_kernel(const AppendArgs a) {
   pdl_wait_and_trigger();
   const PagedAppendCall& c = a.c;
   const int page = c.s.page;
+  // A slot's CTAs follow one another, so that those of the queries, which bandwidth bounds, run beside those of keys and
+  // values, which latency does (all keys and values first: 65 us for three prompts of 2-4K tokens).
+  const int per = a.kv_ctas + a.q_ctas, slot = blockIdx.x / per, sub = blockIdx.x - slot * per;
   int b, j;                                                // the slot's entry; its page, counted from the entry's first
   int64_t slots;                                           // of the entry
   if (c.s.start == nullptr) {
-    b = blockIdx.x / a.cap;
-    j = blockIdx.x - b * a.cap;
+    b = slot / a.cap;
+    j = slot - b * a.cap;
     slots = a.cap;
   } else {
-    b = find_entry(c.s.B, threadIdx.x & 31, [&](int e) { return slot_base(a, e) <= (int64_t)blockIdx.x; });
+    b = find_entry(c.s.B, threadIdx.x & 31, [&](int e) { return slot_base(a, e) <= slot; });
     const int64_t base = slot_base(a, b);
-    j = (int)((int64_t)blockIdx.x - base);
+    j = (int)(slot - base);
     slots = slot_base(a, b + 1) - base;
     if (j < 0 || j >= slots) return;                       // (behind the last entry's)
   }
@@ -271,49 +332,62 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendArgs a) {
   if (rows.count == 0) return;
   const int t = c.T_len[b];
   const int64_t t0 = max(t, 0);
-  bool ok = t >= 0, pages = true;
-  ok = ok && t0 + (int64_t)rows.count <= c.s.max_pages * page;
+  Slot s;
+  const int off = (int)(t0 & (page - 1)), i0 = max(0, j * page - off), i1 = min(rows.count, (j + 1) * page - off);
+  s.row0 = rows.first + i0;
+  s.token0 = (int64_t)t + i0;
+  s.count = i1 - i0;
+  s.at = j == 0 ? off : 0;
+  s.held = s.at;
+  const int64_t first = t0 / page, last = (t0 + (int64_t)rows.count - 1) / page;
+  const bool ok = t >= 0 && last < c.s.max_pages;
+  const int32_t* table = c.s.page_table + b * c.s.max_pages;
+  const bool here = s.count > 0, keys = sub < a.kv_ctas;
+  const int unit = sub * (kThreads / GROUP) + threadIdx.x / GROUP, h = unit < c.s.Hkv ? unit : unit - c.s.Hkv;
+  const bool mine = here && keys && unit < 2 * c.s.Hkv, key = unit < c.s.Hkv;
+  // what a unit needs is asked for before the entry's other pages are looked at
+  s.pid = here && ok ? table[first + j] : -1;
+  uint4 lo[kKeep], hi[kKeep];
+  float was = 0.f;
+  if (mine) {
+#pragma unroll
+    for (int k = 0; k < kKeep; ++k) {
+      const int e = threadIdx.x % GROUP + k * GROUP;
+      if (e < s.count * (D / 16)) load_column<D>(a, s, key, h, e, lo[k], hi[k]);
+    }
+    if (s.held > 0 && s.pid >= 0 && s.pid < c.s.num_pages) was = (key ? c.k_scale : c.v_scale)[s.pid * c.s.Hkv + h];
+  }
+  bool pages = true;
   if (ok)
-    for (int64_t p = t0 / page + threadIdx.x; p <= (t0 + (int64_t)rows.count - 1) / page; p += kThreads) {
-      const int pid = c.s.page_table[b * c.s.max_pages + p];
+    for (int64_t p = first + threadIdx.x; p <= last; p += kThreads) {
+      const int pid = table[p];
       pages = pages && pid >= 0 && pid < c.s.num_pages;
     }
   pages = __syncthreads_and(pages);
-  if (threadIdx.x == 0) {
-    const int all = (int)(slots * (a.kv_ctas + a.q_ctas));
-    if (atomicAdd(c.tickets + b, 1) == all - 1) {          // every CTA of the entry has read its length
-      c.tickets[b] = 0;
-      if (!ok || !pages)
-        atomicOr(a.status, ok ? MKV_FLAG_BAD_INDEX : MKV_FLAG_CACHE_FULL);
-      else
-        c.T_len[b] = (int)(t0 + (int64_t)rows.count);
-    }
-  }
-  Slot s;
-  const int off = (int)(t0 % page);
-  const int64_t i0 = max((int64_t)0, (int64_t)j * page - off), i1 = min((int64_t)rows.count, (int64_t)(j + 1) * page - off);
-  if (i0 >= i1) return;
-  s.row0 = rows.first + i0;
-  s.token0 = (int64_t)t + i0;
-  s.count = (int)(i1 - i0);
-  s.at = j == 0 ? off : 0;
-  s.held = s.at;
-  if ((int)blockIdx.y >= a.kv_ctas) {
-    const int h0 = ((int)blockIdx.y - a.kv_ctas) * a.q_heads;
+  int ticket = 0;                                          // (looked at below, so that nothing waits for it)
+  if (threadIdx.x == 0) ticket = atomicAdd(c.tickets + b, 1);
+  if (here && !keys) {
+    const int h0 = (sub - a.kv_ctas) * a.q_heads;
     rotate_queries<D, BF16>(a, s, h0, min(h0 + a.q_heads, c.s.Hq));
-    return;
+  } else if (mine && ok && pages) {
+    quantize_unit<FMT, D, BF16, GROUP>(a, s, key, h, lo, hi, was);
   }
-  if (!ok || !pages) return;
-  s.pid = c.s.page_table[b * c.s.max_pages + t0 / page + j];
-  const int unit = blockIdx.y * (kThreads / GROUP) + threadIdx.x / GROUP;
-  if (unit < 2 * c.s.Hkv) quantize_unit<FMT, D, BF16, GROUP>(a, s, unit < c.s.Hkv, unit < c.s.Hkv ? unit : unit - c.s.Hkv);
+  if (threadIdx.x == 0 && ticket == (int)slots * per - 1) {   // every CTA of the entry has read its length
+    c.tickets[b] = 0;
+    if (!ok || !pages)
+      atomicOr(a.status, ok ? MKV_FLAG_BAD_INDEX : MKV_FLAG_CACHE_FULL);
+    else
+      c.T_len[b] = (int)(t0 + rows.count);
+  }
 }
 
 template <int FMT, int D, bool BF16>
 cudaError_t launch_d(const AppendArgs& args, int64_t slots, bool warps, cudaStream_t st) {
   AppendArgs a = args;
   a.kv_ctas = warps ? (int)ceil_div(2 * a.c.s.Hkv, kThreads / 32) : 2 * a.c.s.Hkv;
-  const dim3 grid((unsigned)slots, (unsigned)(a.kv_ctas + a.q_ctas));
+  const int64_t ctas = slots * (a.kv_ctas + a.q_ctas);
+  if (ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
+  const dim3 grid((unsigned)ctas);
   if (warps) return launch_pdl(append_kernel<FMT, D, BF16, 32>, grid, dim3(kThreads), 0, st, a);
   return launch_pdl(append_kernel<FMT, D, BF16, kThreads>, grid, dim3(kThreads), 0, st, a);
 }
