@@ -12,7 +12,7 @@
 //
 // Work is shared out in runs of tiles (mkv_paged_work.cuh).  Roles: one warp finds out its CTA's and loads it (a bulk copy a
 // page), four convert keys and four values (four for both took 1.4 us a tile, twice what its bytes take), one issues products,
-// whichever is ready (a finished tile's second product first), four do the softmax of a tile while the next one's scores are
+// whichever is ready (a finished tile's second product first), four or eight do the softmax of a tile while the next one's scores are
 // computed.
 #include <math.h>
 
@@ -25,13 +25,8 @@ namespace mkv {
 
 namespace {
 
-// Warpgroups: softmax; conversion of keys; of values; loads + products (+ two idle warps).
-constexpr int kThreads = 512, kSoftmax = 128;
-// registers a thread: what a launch of kThreads gets (128), and its split
-constexpr int kRegsSoftmax = 208, kRegsConvert = 104, kRegsOther = 96;
-static_assert(kRegsSoftmax + 2 * kRegsConvert + kRegsOther <= 4 * 128, "register shares");
 constexpr int kHeads = 8;           // tiles whose heads and scales are held
-constexpr int kSlots = 4;           // widened tiles (K0 V0 K1 V1 ..; with three, conversion was part of the products' chain: 50 against 4x us)
+constexpr int kSlots = 4;           // widened tiles (K0 V0 K1 V1 ..; with three, conversion is part of the products' chain: 50 against 45 us)
 constexpr int kGrid = kNumSMs;
 
 struct BlockArgs {
@@ -47,14 +42,24 @@ struct BlockArgs {
 template <int FMT_, int D_, int COPIES_>
 struct BShape {
   static constexpr int FMT = FMT_, D = D_, COPIES = COPIES_;
-  static constexpr int ROWS = 128 / COPIES, COLS = 128 / COPIES, NG = COLS / 16;   // of a copy; groups of 16 tokens
+  static constexpr int ROWS = 128 / COPIES, COLS = 128 / COPIES;   // of a copy
+  // Warpgroups: softmax, conversion of keys, of values, loads + products (two warps idle).  With one copy there are two of
+  // softmax, and a row's columns are halved between the threads of two warps (32 drafted over 8 x 8K 88 -> 71 us; with four
+  // copies, where a thread has 32 columns anyway, 44 -> 49).
+  static constexpr int HALVES = COPIES == 1 ? 2 : 1, SW = 4 * HALVES;      // softmax warps
+  static constexpr int THREADS = 32 * (SW + 12), SOFT = 32 * SW;
+  // registers a thread: what a launch gets, and its split
+  static constexpr int RL = HALVES == 2 ? 96 : 128, RS = HALVES == 2 ? 112 : 208, RC = HALVES == 2 ? 96 : 104,
+                       RO = HALVES == 2 ? 64 : 96;
+  static_assert(HALVES * RS + 2 * RC + RO <= (HALVES + 3) * RL, "register shares");
   static constexpr int KA = D / 64, ATOM = 128 * 128, TILE = KA * ATOM;
   static constexpr int RAW = kTokens * D, RAWS = D == 128 ? 4 : 8;
-  static constexpr int OROW = 36;                          // floats between rows of the join's 32 dims
+  static constexpr int OROW = 20;                          // floats between rows of the join's 16 dims
   static constexpr int T_OFF = 0;                          // [kSlots] widened tiles
   static constexpr int R_OFF = T_OFF + kSlots * TILE;      // [RAWS] codes
-  static constexpr int O_OFF = R_OFF + RAWS * RAW;         // [128][OROW] floats
-  static constexpr int SC_OFF = O_OFF + 128 * OROW * 4;    // scales of kBatches batches
+  static constexpr int O_OFF = R_OFF + RAWS * RAW;         // [HALVES][128][OROW] floats
+  static constexpr int X_OFF = O_OFF + HALVES * 128 * OROW * 4; // [2][2][128] float2: what the halves of a row tell each other
+  static constexpr int SC_OFF = X_OFF + 2 * 2 * 128 * 8;    // scales of kBatches batches
   static constexpr int HD_OFF = SC_OFF + scale_bytes(kBatches);
   static constexpr int ST_OFF = HD_OFF + kHeads * 64;      // [128] + [ROWS] float4: the lanes', the piece's
   static constexpr int CTL_OFF = ST_OFF + (128 + ROWS) * 16;
@@ -67,14 +72,14 @@ struct BShape {
 
 struct BlockCtl {
   uint64_t raw_full[8], raw_empty[8], tile_full[kSlots], tile_empty[kSlots], head[kHeads], sfull[2], pfull, pvdone, qfull, meet,
-      drained;
+      pair[4], drained;
   uint32_t tslot;
   int fail, loads, last;
 };
 static_assert(sizeof(BlockCtl) <= 512, "control block");
 
 template <class S, bool BF16>
-__global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
+__global__ void __launch_bounds__(S::THREADS, 1) block_kernel(const BlockArgs a) {
   constexpr int D = S::D;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
@@ -86,8 +91,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
   uint32_t* status = a.status;
   auto head_at = [&](int g) { return reinterpret_cast<Head*>(sm + S::HD_OFF + g % kHeads * 64); };
 
-  if (warp == 13) tc_alloc(&ctl->tslot, 512);
-  if (threadIdx.x == 384) {
+  if (warp == S::SW + 9) tc_alloc(&ctl->tslot, 512);
+  if (threadIdx.x == S::SOFT + 256) {
     for (int s = 0; s < S::RAWS; ++s) {
       tc_mbar_init(&ctl->raw_full[s], 1);
       tc_mbar_init(&ctl->raw_empty[s], 4);
@@ -98,10 +103,11 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
     }
     for (int s = 0; s < kHeads; ++s) tc_mbar_init(&ctl->head[s], 1);
     for (int s = 0; s < 2; ++s) tc_mbar_init(&ctl->sfull[s], 1);
-    tc_mbar_init(&ctl->pfull, 4);
+    tc_mbar_init(&ctl->pfull, S::SW);
     tc_mbar_init(&ctl->pvdone, 1);
-    tc_mbar_init(&ctl->qfull, 4);
-    tc_mbar_init(&ctl->meet, 4);
+    tc_mbar_init(&ctl->qfull, S::SW);
+    tc_mbar_init(&ctl->meet, S::SW);
+    for (int w = 0; w < 4; ++w) tc_mbar_init(&ctl->pair[w], 2);
     tc_mbar_init(&ctl->drained, 1);
     tc_fence_mbar_init();
     ctl->fail = ctl->loads = 0;
@@ -113,8 +119,8 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
   const uint32_t tbase = ctl->tslot;
   const int all_copies = (1 << (kTokens >> a.w.log_box)) - 1;
 
-  if (warp >= 12) regs_down<kRegsOther>();
-  if (warp == 12) {
+  if (warp >= S::SW + 8) regs_down<S::RO>();
+  if (warp == S::SW + 8) {
     // ---------------------------------------------------------------- loads
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
@@ -157,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         tc_mbar_arrive(&ctl->head[g % kHeads]);
       }
     }
-  } else if (warp == 13) {
+  } else if (warp == S::SW + 9) {
     if (elect_one()) {
       // ---------------------------------------------------------------- products
       constexpr uint32_t idS = tc_idesc(false, 128, 128, false, false);
@@ -222,14 +228,14 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       }
       tc_commit(&ctl->drained);
     }
-  } else if (warp >= 4 && warp < 12) {
-    regs_down<kRegsConvert>();
+  } else if (warp >= S::SW && warp < S::SW + 8) {
+    if (S::RC < S::RL) regs_down<S::RC>();
     // ---------------------------------------------------------------- codes to fp16: keys (h 0), values (h 1)
     // A thread takes one 16-byte piece of every STEP'th row.  Of eight neighbouring threads four read the first half of one
     // row and four the second half of the next: different banks, and so are those of the pieces that they store, in an atom
     // each (two rows of one atom with 64 dims).
     constexpr int STEP = D == 128 ? 16 : 32;
-    const int h = warp >= 8 ? 1 : 0, tid = threadIdx.x - 128 - 128 * h;
+    const int h = warp >= S::SW + 4 ? 1 : 0, tid = threadIdx.x - S::SOFT - 128 * h;
     const int piece = D == 128 ? tid & 7 : tid & 3;
     const int row = D == 128 ? (tid >> 4) * 2 + ((tid >> 2 ^ tid >> 3) & 1) : tid >> 2;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -269,14 +275,17 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         tc_mbar_arrive(&ctl->raw_empty[rs]);
       }
     }
-  } else if (warp < 4) {
-    regs_up<kRegsSoftmax>();
-    // ---------------------------------------------------------------- softmax: lane 32 warp + lane, row `row` of copy `copy`
-    constexpr int COLS = S::COLS, NG = S::NG;
-    const int at = warp * 32 + lane, copy = at / S::ROWS, row = at % S::ROWS, G = a.heads.G;
-    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-    const uint32_t tO = tbase + lanes + S::O, tP = tbase + lanes + S::P + (uint32_t)(copy * COLS / 2);
-    float* ob = reinterpret_cast<float*>(sm + S::O_OFF);
+  } else if (warp < S::SW) {
+    regs_up<S::RS>();
+    // ---------------------------------------------------------------- softmax: lane 32 (warp % 4) + lane, row `row` of copy
+    // `copy`; a thread has the copy's columns or half of them
+    constexpr int HALVES = S::HALVES, HC = S::COLS / HALVES, CW = HALVES == 2 ? 32 : HC;   // its columns; so many at a time
+    constexpr int QD = D / HALVES, OD = D / 32 / HALVES;   // its dims of the queries; 32s of dims of the outputs
+    const int half = warp >> 2, at = (warp & 3) * 32 + lane, copy = at / S::ROWS, row = at % S::ROWS, G = a.heads.G;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const int col0 = copy * S::COLS + half * HC;           // its first column of a tile
+    const uint32_t tO = tbase + lanes + S::O, tP = tbase + lanes + S::P + (uint32_t)(col0 / 2);
+    float* ob = reinterpret_cast<float*>(sm + S::O_OFF) + half * 128 * S::OROW;
     float4* stat = reinterpret_cast<float4*>(sm + S::ST_OFF);
     float4* fin = stat + 128;
     bool dead = false;
@@ -284,13 +293,23 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       if (!dead) dead = !__all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status));
       tc_fence_after();
     };
-    // (a barrier of the four warps whose waits are bounded too)
-    uint32_t met = 0;
+    // (barriers of the softmax warps, and of the two that share rows, whose waits are bounded too)
+    uint32_t met = 0, paired = 0;
     auto meet = [&]() {
       __syncwarp();
       if (lane == 0) tc_mbar_arrive(&ctl->meet);
       wait(&ctl->meet, met);
       met ^= 1;
+    };
+    auto exchange = [&](float2 x) {                        // with the thread that has the row's other columns, if there is one
+      if (HALVES == 1) return x;
+      float2* tell = reinterpret_cast<float2*>(sm + S::X_OFF) + paired * 256;
+      tell[half * 128 + at] = x;
+      __syncwarp();
+      if (lane == 0) tc_mbar_arrive(&ctl->pair[warp & 3]);
+      wait(&ctl->pair[warp & 3], paired);
+      paired ^= 1;
+      return tell[(1 - half) * 128 + at];
     };
     // An output is o / sum 2^(m2 - m - 6); zeros for a row before position 0, which sees nothing; NaN where no score leaves a
     // weight.
@@ -316,7 +335,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       if (dead) return;
       if (ctl->last) {
         const int R = owed.tokens * G;
-        if (at < R) {                                      // a row a thread: what its pieces' statistics come to
+        if (half == 0 && at < R) {                         // a row a thread: what its pieces' statistics come to
           float mx = kNoMax, mx2 = kNoMax, sum = 0.f;
 #pragma unroll 4
           for (int i = 0; i < owed.count; ++i) {
@@ -330,9 +349,9 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         }
         meet();
         if (dead) return;
-        constexpr int U = 8;                               // (so many rows' loads under way together)
+        constexpr int U = 8 / S::HALVES;                   // (so many rows' loads under way together)
 #pragma unroll 1
-        for (int e0 = at; e0 < R * (D / 4); e0 += U * kSoftmax) {   // four dims of a row
+        for (int e0 = threadIdx.x; e0 < R * (D / 4); e0 += U * S::SOFT) {   // four dims of a row
           float4 y[U];
 #pragma unroll
           for (int k = 0; k < U; ++k) y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -342,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
             float4 z[U];
 #pragma unroll
             for (int k = 0; k < U; ++k) {
-              const int e = min(e0 + k * kSoftmax, R * (D / 4) - 1);
+              const int e = min(e0 + k * S::SOFT, R * (D / 4) - 1);
               const int64_t p = (int64_t)owed.place(i) * S::ROWS + e / (D / 4);
               f[k] = __ldcg(a.part_st + p).z - fin[e / (D / 4)].z;
               z[k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + p * D + e % (D / 4) * 4));
@@ -355,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
           }
 #pragma unroll
           for (int k = 0; k < U; ++k) {
-            const int e = e0 + k * kSoftmax;
+            const int e = e0 + k * S::SOFT;
             if (e < R * (D / 4)) {
               const float4 all = fin[e / (D / 4)];
               store_out(owed, e / (D / 4), e % (D / 4) * 4, y[k], all.x, all.y, all.z);
@@ -370,84 +389,99 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       float z[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) z[i] = 0.f;
-      for (int i = 0; i < 4; ++i) tm_store<16>(tbase + lanes + S::P + (uint32_t)(16 * i), z);
-      tm_store_wait();
+      if (half == 0) {
+        for (int i = 0; i < 4; ++i) tm_store<16>(tbase + lanes + S::P + (uint32_t)(16 * i), z);
+        tm_store_wait();
+      }
+      meet();
     }
 
+    const int log_group = a.w.log_box - 4;
     float m = kNoMax, m2 = kNoMax, l = 0.f, back = 1.f;
-    int own = 0;                                           // this row's own position: the last that it sees
-    for (int g = 0;; ++g) {
+    int own = 0, pos0 = 0;                                 // this row's own position, the last that it sees; the first row's
+    Piece hd;
+    hd.tokens = 0;
+    for (int g = 0; !dead; ++g) {
       wait(&ctl->head[g % kHeads], (uint32_t)((g / kHeads) & 1));
       if (dead) break;
       const Chunk now = head_at(g)->c;
       if (now.flags & kEnd) break;
-      const Piece hd = head_at(g)->p;
-      const int R = hd.tokens * G;
       if (now.flags & kFirst) {
+        hd = head_at(g)->p;
         // ---------------------------------------------------------- queries to tensor memory (the earlier piece's are read)
-        float q[D / 2];
+        float q[QD / 2];
         const uint4* src = reinterpret_cast<const uint4*>(c.q + (int64_t)(hd.row0 + a.heads.token(row)) * c.q_stride +
-                                                          (int64_t)(hd.kvh * G + a.heads.head(row)) * D);
+                                                          (int64_t)(hd.kvh * G + a.heads.head(row)) * D + half * QD);
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          const uint4 y = row < R ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; i < QD / 8; ++i) {
+          const uint4 y = row < hd.tokens * G ? src[i] : make_uint4(0u, 0u, 0u, 0u);
           q[4 * i] = __uint_as_float(y.x);
           q[4 * i + 1] = __uint_as_float(y.y);
           q[4 * i + 2] = __uint_as_float(y.z);
           q[4 * i + 3] = __uint_as_float(y.w);
         }
-        back = 1.f;
         if (BF16) {
           float most = 0.f;
 #pragma unroll
-          for (int i = 0; i < D / 2; ++i) {
+          for (int i = 0; i < QD / 2; ++i) {
             const uint32_t y = __float_as_uint(q[i]);
             const float x0 = fabsf(widen<true>((uint16_t)y)), x1 = fabsf(widen<true>((uint16_t)(y >> 16)));
             most = fmax3(most, x0 < INFINITY ? x0 : 0.f, x1 < INFINITY ? x1 : 0.f);
           }
+          most = fmaxf(most, exchange(make_float2(most, 0.f)).x);
           const int e = row_exponent(most);
           const float f = power_of_two(e);
           back = power_of_two(-e);
 #pragma unroll
-          for (int i = 0; i < D / 2; ++i) {
+          for (int i = 0; i < QD / 2; ++i) {
             const uint32_t y = __float_as_uint(q[i]);
             q[i] = __uint_as_float(pack2<false>(widen<true>((uint16_t)y) * f, widen<true>((uint16_t)(y >> 16)) * f));
           }
         }
+        constexpr int QW = QD / 2 < 32 ? QD / 2 : 32;
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i)
-          tm_store<32>(tbase + lanes + S::Q + (uint32_t)(32 * i), *reinterpret_cast<float(*)[32]>(&q[32 * i]));
+        for (int i = 0; i < QD / 2 / QW; ++i)
+          tm_store<QW>(tbase + lanes + S::Q + (uint32_t)(half * (QD / 2) + QW * i), *reinterpret_cast<float(*)[QW]>(&q[QW * i]));
         tm_store_wait();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) tc_mbar_arrive(&ctl->qfull);
         m = m2 = kNoMax;
         l = 0.f;
-        own = hd.len - hd.tokens + a.heads.token(row);
+        pos0 = hd.len - hd.tokens;
+        own = pos0 + a.heads.token(row);
       }
       const float2* scales = reinterpret_cast<const float2*>(sm + S::SC_OFF) + now.scales;
-      auto copy_of = [&](int i) { return (copy * NG + i) >> (a.w.log_box - 4); };   // that holds group i of this copy's tokens
-      auto scale = [&](int i) { return scales[copy_of(i)]; };
       wait(&ctl->sfull[g & 1], (uint32_t)((g >> 1) & 1));
       if (dead) break;
-      const uint32_t tS = tbase + lanes + S::S + (uint32_t)((g & 1) * 128 + copy * COLS);
-      float v[COLS];
+      const uint32_t tS = tbase + lanes + S::S + (uint32_t)((g & 1) * 128 + col0);
+      const bool part = now.copies != all_copies || (now.chunk + 1) * kTokens > pos0 + 1;
+      const int lim = own + 1 - now.chunk * kTokens - col0;       // this thread's columns that its row sees
+      // CW columns' scores, those that the row does not see minus infinity
+      auto load = [&](int i, float (&v)[CW]) {
 #pragma unroll
-      for (int i = 0; i < COLS / 32; ++i) tm_issue<32>(tS + i * 32, *reinterpret_cast<float(*)[32]>(&v[i * 32]));
+        for (int k = 0; k < CW / 32; ++k) tm_issue<32>(tS + (uint32_t)(CW * i + 32 * k), *reinterpret_cast<float(*)[32]>(&v[32 * k]));
 #pragma unroll
-      for (int i = 0; i < COLS / 32; ++i) tm_wait<32>(*reinterpret_cast<float(*)[32]>(&v[i * 32]));
-      // what the row does not see is minus infinity
-      const bool part = now.copies != all_copies || (now.chunk + 1) * kTokens > hd.len - hd.tokens + 1;
-      if (part) {
+        for (int k = 0; k < CW / 32; ++k) tm_wait<32>(*reinterpret_cast<float(*)[32]>(&v[32 * k]));
+        if (part) {
 #pragma unroll
-        for (int i = 0; i < NG; ++i) {
-          const int upto = now.copies >> copy_of(i) & 1 ? own + 1 - now.chunk * kTokens - copy * COLS - 16 * i : 0;
+          for (int g16 = 0; g16 < CW / 16; ++g16) {
+            const int upto = now.copies >> ((col0 / 16 + CW / 16 * i + g16) >> log_group) & 1 ? lim - CW * i : 0;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) v[16 * i + e] = e < upto ? v[16 * i + e] : -INFINITY;
+            for (int e = 16 * g16; e < 16 * g16 + 16; ++e) v[e] = e < upto ? v[e] : -INFINITY;
+          }
         }
+      };
+      auto scale_of = [&](int i, int g16) { return scales[(col0 / 16 + CW / 16 * i + g16) >> log_group]; };
+      float mt = -INFINITY, mt2 = -INFINITY, v[CW];
+#pragma unroll 1
+      for (int i = 0; i < HC / CW; ++i) {
+        load(i, v);
+        columns_max<CW, 16, BF16>(v, back, [&](int g16) { return scale_of(i, g16); }, mt, mt2);
       }
-      float mt = -INFINITY, mt2 = -INFINITY;
-      columns_max<COLS, 16, BF16>(v, back, scale, mt, mt2);
+      const float2 other = exchange(make_float2(mt, mt2));
+      mt = fmaxf(mt, other.x);
+      mt2 = fmaxf(mt2, other.y);
       const bool raise = __any_sync(0xffffffffu, mt > m + kRaise || mt2 > m2 + kRaise);
       float w = 1.f;
       if (raise) {
@@ -457,14 +491,18 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
         m = nm;
         m2 = nm2;
       }
-      float pk[COLS / 2];
-      columns_weights<COLS, 16, BF16>(v, part, m, m2, back, scale, l, pk);
+      // (columns that fit the registers are still there, and their weights need not wait)
+      float pk[CW / 2];
+      auto weights = [&](int i) {
+        columns_weights<CW, 16, BF16>(v, part, m, m2, back, [&](int g16) { return scale_of(i, g16); }, l, pk);
+      };
+      if (HC == CW) weights(0);
       // (the tile before this one's weights have been read, and its product added)
       if (g > 0) wait(&ctl->pvdone, (uint32_t)((g - 1) & 1));
       if (dead) break;
       if (raise && !(now.flags & kFirst)) {
 #pragma unroll 1
-        for (int i = 0; i < D / 32; ++i) {
+        for (int i = half * OD; i < (half + 1) * OD; ++i) {
           float o[32];
           tm_load<32>(tO + i * 32, o);
 #pragma unroll
@@ -472,11 +510,13 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
           tm_store<32>(tO + i * 32, o);
         }
       }
-      if constexpr (COLS == 32) {
-        tm_store<16>(tP, pk);
-      } else {
-#pragma unroll
-        for (int i = 0; i < COLS / 64; ++i) tm_store<32>(tP + i * 32, *reinterpret_cast<float(*)[32]>(&pk[i * 32]));
+#pragma unroll 1
+      for (int i = 0; i < HC / CW; ++i) {
+        if (HC > CW) {
+          load(i, v);
+          weights(i);
+        }
+        tm_store<CW / 2>(tP + (uint32_t)(CW / 2 * i), pk);
       }
       tm_store_wait();
       tc_fence_before();
@@ -484,12 +524,14 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       if (lane == 0) tc_mbar_arrive(&ctl->pfull);
       if (!(now.flags & kLast)) continue;
 
-      // ------------------------------------------------------------ the end of a piece: the copies added up, 32 dims at a time
+      // ------------------------------------------------------------ the end of a piece: the copies added up, 16 dims at a time
       settle();                                            // (the piece before this one's unit)
       wait(&ctl->pvdone, (uint32_t)(g & 1));
-      stat[at] = make_float4(m, l, m2, 0.f);
+      const float both = HALVES == 1 ? l : l + exchange(make_float2(l, 0.f)).x;
+      if (half == 0) stat[at] = make_float4(m, both, m2, 0.f);
       meet();
       if (dead) break;
+      const int R = hd.tokens * G;
       float mx = kNoMax, mx2 = kNoMax, sum = 0.f;
 #pragma unroll
       for (int i = 0; i < S::COPIES; ++i) {
@@ -501,23 +543,23 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
       const float fo = ex2_approx(m2 - mx2);
       const bool whole = now.flags & kWhole;
       const int64_t mine = (int64_t)hd.mine * S::ROWS;
-      if (copy == 0) {
+      if (copy == 0 && half == 0) {
         fin[row] = make_float4(mx, sum, mx2, 0.f);
         if (!whole && row < R) __stcg(a.part_st + mine + row, make_float4(mx, sum, mx2, 0.f));
       }
 #pragma unroll 1
-      for (int i = 0; i < D / 32; ++i) {
-        float o[32];
-        tm_load<32>(tO + i * 32, o);
+      for (int i = half * 2 * OD; i < (half + 1) * 2 * OD; ++i) {
+        float o[16];
+        tm_load<16>(tO + i * 16, o);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < 4; ++e)
           *reinterpret_cast<float4*>(ob + at * S::OROW + 4 * e) =
               make_float4(o[4 * e] * fo, o[4 * e + 1] * fo, o[4 * e + 2] * fo, o[4 * e + 3] * fo);
         meet();
         if (dead) break;
 #pragma unroll 1
-        for (int e = at; e < R * 8; e += kSoftmax) {
-          const int r = e >> 3, d = (e & 7) * 4;
+        for (int e = at; e < R * 4; e += 128) {
+          const int r = e >> 2, d = (e & 3) * 4;
           float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
           for (int k = 0; k < S::COPIES; ++k) {
@@ -526,9 +568,9 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
           }
           if (whole) {
             const float4 st = fin[r];
-            store_out(hd, r, i * 32 + d, x, st.x, st.y, st.z);
+            store_out(hd, r, i * 16 + d, x, st.x, st.y, st.z);
           } else {
-            __stcg(reinterpret_cast<float4*>(a.part_o + (mine + r) * D + i * 32 + d), x);
+            __stcg(reinterpret_cast<float4*>(a.part_o + (mine + r) * D + i * 16 + d), x);
           }
         }
         meet();
@@ -554,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) block_kernel(const BlockArgs a) {
   }
   __syncthreads();
   tc_fence_after();
-  if (warp == 13) tc_dealloc(tbase, 512);
+  if (warp == S::SW + 9) tc_dealloc(tbase, 512);
 }
 
 // ---------------------------------------------------------------- host side
@@ -567,7 +609,7 @@ template <class S, bool BF16>
 cudaError_t launch_shape(const BlockArgs& a, cudaStream_t st) {
   constexpr int smem = std::max(S::ALLOC, 116 * 1024);      // one CTA an SM: it takes all of the tensor memory
   const cudaError_t e = cudaFuncSetAttribute(block_kernel<S, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  return e != cudaSuccess ? e : launch_pdl(block_kernel<S, BF16>, dim3(kGrid), dim3(kThreads), smem, st, a);
+  return e != cudaSuccess ? e : launch_pdl(block_kernel<S, BF16>, dim3(kGrid), dim3(S::THREADS), smem, st, a);
 }
 template <int FMT, int D, bool BF16>
 cudaError_t launch_c(const BlockArgs& a, cudaStream_t st) {
