@@ -61,8 +61,8 @@ struct PShape {
   static constexpr int SC_OFF = R_OFF + RAWS * RAW;        // scales of kHeldBatches batches
   static constexpr int HD_OFF = SC_OFF + scale_bytes(kHeldBatches);   // [kHeads] Chunk
   static constexpr int QS_OFF = HD_OFF + kHeads * 16;      // [256] exponents that bf16 rows are scaled by
-  static constexpr int X_OFF = QS_OFF + kRows;             // [2][256] float2: what the halves of a row tell each other
-  static constexpr int CTL_OFF = X_OFF + 2 * kRows * 8;
+  static constexpr int X_OFF = QS_OFF + kRows;             // [2][2][256] float2: what the halves of a row tell each other
+  static constexpr int CTL_OFF = X_OFF + 2 * 2 * kRows * 8;
   static constexpr int ALLOC = CTL_OFF + 512;
   static_assert(ALLOC <= 227 * 1024, "shared memory");
 };
@@ -302,6 +302,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     const uint32_t at0 = (uint32_t)((2 * (piece & 3)) ^ (row & 7)) << 4;
     for (int item = 0; item < 2 * ntiles; ++item) {
       const int t = item >> 1, rs = item % S::RAWS, s = item % kSlots;
+      if (!(item & 1) && !wait(&ctl->head[t % kHeads], (uint32_t)((t / kHeads) & 1))) break;
       if (!wait(&ctl->raw_full[rs], (uint32_t)((item / S::RAWS) & 1))) break;
       if (item >= kSlots && !wait(&ctl->tile_empty[s], (uint32_t)((item / kSlots - 1) & 1))) break;
       const uint8_t* src = sm + S::R_OFF + rs * S::RAW + row * D + piece * 16;
@@ -310,7 +311,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
 #pragma unroll
       for (int i = 0; i < kBR / STEP; ++i) x[i] = *reinterpret_cast<const uint4*>(src + i * STEP * D);
       if (item & 1) {                                      // what no row sees must not meet a zero weight as NaN
-        if (!wait(&ctl->head[t % kHeads], (uint32_t)((t / kHeads) & 1))) break;
         const int copies = heads[t % kHeads].copies, tail = u.len - (c0 + t) * kBR;
         if (copies != all_copies || tail < kBR)
 #pragma unroll
@@ -389,15 +389,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     // ---------------------------------------------------------------- softmax: row 32 (warp % 4) + lane of block k
     const int rin = k * kBR + (warp & 3) * 32 + lane, row = base_row + rin, seen = u.seen(a.heads, row);
     const int td = u.seen(a.heads, base_row) / kBR;                 // first tile that the unit's first row does not see whole
-    float2* tell = reinterpret_cast<float2*>(sm + S::X_OFF) + half * kRows + rin;
-    const float2* hear = reinterpret_cast<const float2*>(sm + S::X_OFF) + (1 - half) * kRows + rin;
+    int turn = 0;
     auto exchange = [&](float2 x) {                        // with the warp that has the rows' other columns
-      const int pair = 1 + k * 4 + (warp & 3);
-      *tell = x;
-      bar_sync(pair, 64);
-      const float2 y = *hear;
-      bar_sync(pair, 64);
-      return y;
+      float2* tell = reinterpret_cast<float2*>(sm + S::X_OFF) + turn * 2 * kRows + rin;
+      turn ^= 1;                                           // (one place is read until the barrier after the next)
+      tell[half * kRows] = x;
+      bar_sync(1 + k * 4 + (warp & 3), 64);
+      return tell[(1 - half) * kRows];
     };
     float back = 1.f;
     if (BF16) {                                            // (all warps' queries are in place)
@@ -409,8 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     const int log_group = a.w.log_box - 4;
     float m = kNoMax, m2 = kNoMax, l = 0.f;
     for (int t = 0; t < nt[k]; ++t) {
-      wait(&ctl->head[t % kHeads], (uint32_t)((t / kHeads) & 1));
-      wait(&ctl->sfull[k], (uint32_t)(t & 1));
+      wait(&ctl->sfull[k], (uint32_t)(t & 1));             // (the tile's head came before its keys)
       const int copies = heads[t % kHeads].copies;
       const float2* scales = reinterpret_cast<const float2*>(sm + S::SC_OFF) + heads[t % kHeads].scales;
       const bool part = c0 + t >= td || copies != all_copies;      // (a page outside the pool or past the length)
