@@ -407,7 +407,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     const int log_group = a.w.log_box - 4;
     float m = kNoMax, m2 = kNoMax, l = 0.f;
     for (int t = 0; t < nt[k]; ++t) {
-      wait(&ctl->sfull[k], (uint32_t)(t & 1));             // (the tile's head came before its keys)
+      wait(&ctl->head[t % kHeads], (uint32_t)((t / kHeads) & 1));
+      wait(&ctl->sfull[k], (uint32_t)(t & 1));
       const int copies = heads[t % kHeads].copies;
       const float2* scales = reinterpret_cast<const float2*>(sm + S::SC_OFF) + heads[t % kHeads].scales;
       const bool part = c0 + t >= td || copies != all_copies;      // (a page outside the pool or past the length)
