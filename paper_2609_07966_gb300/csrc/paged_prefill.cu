@@ -15,7 +15,9 @@
 // A tile's pages have scales of their own: within 16 columns both are constant, so a score's is part of the factor of its
 // exponent, the maxima are kept per 16 columns until they are scaled, and a weight is p vs 2^(m - m2 + 6).
 //
-// With fewer units (256 rows of a key head) than SMs, the tokens of each are shared out too and join_kernel adds the parts up.
+// A unit is 256 rows of a key head.  With few of them, their tiles lie end to end and are cut into equal runs, one an SM; a
+// run's tiles of one unit are a piece, and join_kernel adds up the pieces of units that several runs share.  Many units are
+// balanced by the order in which they are launched.
 #include <math.h>
 
 #include <algorithm>
@@ -36,6 +38,9 @@ constexpr int kThreads = 768;
 constexpr int kHeads = 8;           // tiles whose heads and scales are held
 constexpr int kSlots = 3;           // widened tiles (K0 V0 K1 V1 ..)
 constexpr int kHeldBatches = 4;     // (a tile is one of at least four of a batch)
+// Up to this many units their tiles are shared out.
+constexpr int kShared = 2 * kNumSMs;
+static_assert(kShared <= kThreads && kShared % 4 == 0, "a slot a thread");
 static_assert(kBR == kTokens && kHeads <= (kHeldBatches - 1) * 4, "tiles are chunks; scales are kept");
 
 struct PrefillArgs {
@@ -43,11 +48,12 @@ struct PrefillArgs {
   uint32_t* status;
   Heads heads;
   WorkArgs w;
-  int slots;                    // units of all entries, a key head's
+  int slots;                        // units of all entries, a key head's
   int per;                          // start null: units of an entry
-  int splits;                       // parts of a unit's tokens
-  float* part_o;                    // [slot][Hkv][splits][256][D]
-  float4* part_st;                  // the same without D: m, sum, m2
+  int runs;                         // CTAs that share all tiles; 0: a CTA a unit
+  float* part_o;                    // [kNumSMs][2][D / 4][256][4]: pieces; of a run the first one's place and the last one's
+  float4* part_st;                  // [kNumSMs][2][256]: m, sum, m2
+  int4* joins;                      // [slot][Hkv]: the unit's first run, its first piece's place, how many pieces, its entry
 };
 
 // GC: tokens that share a page's scales for certain
@@ -62,7 +68,8 @@ struct PShape {
   static constexpr int HD_OFF = SC_OFF + scale_bytes(kHeldBatches);   // [kHeads] Chunk
   static constexpr int QS_OFF = HD_OFF + kHeads * 16;      // [256] exponents that bf16 rows are scaled by
   static constexpr int X_OFF = QS_OFF + kRows;             // [2][2][256] float2: what the halves of a row tell each other
-  static constexpr int CTL_OFF = X_OFF + 2 * 2 * kRows * 8;
+  static constexpr int B_OFF = X_OFF + 2 * 2 * kRows * 8;  // [kShared + 1] where the slots' tiles begin
+  static constexpr int CTL_OFF = B_OFF + (kShared + 4) * 4;
   static constexpr int ALLOC = CTL_OFF + 512;
   static_assert(ALLOC <= 227 * 1024, "shared memory");
 };
@@ -73,6 +80,7 @@ struct PCtl {
   uint32_t tslot;
   int fail, loads;
   int b, rb, rows, pos0, len, row0, live, c0, c1, nt[2];   // the unit, and what of it is this CTA's
+  int kvh, whole, place, sums[kThreads / 32];
 };
 static_assert(sizeof(PCtl) <= 512, "control block");
 
@@ -96,9 +104,9 @@ struct Unit {
     return last >= first ? max(1, (seen(h, last) + kBR - 1) / kBR) : 0;
   }
 };
-__device__ __forceinline__ Unit unit_of(const PrefillArgs& a, int slot, int kvh, int lane, bool report) {
+__device__ __forceinline__ Unit unit_of(const PrefillArgs& a, int b, int slot, int kvh, bool report) {
   Unit u;
-  u.b = a.c.s.start == nullptr ? slot / a.per : find_entry(a.c.s.B, lane, [&](int b) { return unit_base(a, b) <= slot; });
+  u.b = b;
   u.kvh = kvh;
   u.rb = slot - unit_base(a, u.b);
   const EntryRows r = entry_rows(a.c.s, u.b);
@@ -112,8 +120,24 @@ __device__ __forceinline__ Unit unit_of(const PrefillArgs& a, int slot, int kvh,
   u.pos0 = u.len - tokens;
   return u;
 }
+// (a whole warp finds the entry, or every thread its own)
+__device__ __forceinline__ int entry_of_slot(const PrefillArgs& a, int slot, int lane) {
+  return a.c.s.start == nullptr ? slot / a.per : find_entry(a.c.s.B, lane, [&](int b) { return unit_base(a, b) <= slot; });
+}
+__device__ __forceinline__ int entry_of_slot(const PrefillArgs& a, int slot) {
+  if (a.c.s.start == nullptr) return slot / a.per;
+  int lo = 0, hi = a.c.s.B;                                // the last entry that begins at or before the slot
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (unit_base(a, mid) <= slot)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
 
-template <class S, bool BF16>
+template <class S, bool BF16, bool SHARED>
 __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs a) {
   constexpr int D = S::D, GC = S::GC;
   extern __shared__ __align__(1024) uint8_t sm[];
@@ -122,29 +146,78 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
   const PagedAttnCall& c = a.c;
   const int Hkv = c.s.Hkv;
 
-  // Launch order: the last rows of the entries first (they see the most), all key heads and parts of a slot together.
-  const int each = Hkv * a.splits, at = blockIdx.x / each, in = blockIdx.x - at * each, split = in / Hkv, kvh = in - split * Hkv;
-  const int slot = a.slots - 1 - at;
   pdl_wait_and_trigger();
-  if (warp == 0) {                                         // (one warp finds it out: twenty-four took 5 us a CTA)
-    const Unit u = unit_of(a, slot, kvh, lane, true);
-    const int all0 = u.tiles(a.heads, 0), all1 = u.tiles(a.heads, 1), all = max(all0, all1);
-    const int c0 = a.splits == 1 ? 0 : (int)((int64_t)all * split / a.splits);
-    const int c1 = a.splits == 1 ? all : (int)((int64_t)all * (split + 1) / a.splits);
-    if (lane == 0) {
-      ctl->b = u.b;
-      ctl->rb = u.rb;
-      ctl->rows = u.rows;
-      ctl->pos0 = u.pos0;
-      ctl->len = u.len;
-      ctl->row0 = u.row0;
-      ctl->live = u.live;
-      ctl->c0 = c0;
-      ctl->c1 = c1;
-      ctl->nt[0] = max(0, min(all0, c1) - c0);
-      ctl->nt[1] = max(0, min(all1, c1) - c0);
+  // What tiles c0 .. of a unit this CTA takes, told to all threads.
+  auto tell = [&](const Unit& u, int c0, int c1) {
+    const int all0 = u.tiles(a.heads, 0), all1 = u.tiles(a.heads, 1);
+    ctl->b = u.b;
+    ctl->kvh = u.kvh;
+    ctl->rb = u.rb;
+    ctl->rows = u.rows;
+    ctl->pos0 = u.pos0;
+    ctl->len = u.len;
+    ctl->row0 = u.row0;
+    ctl->live = u.live;
+    ctl->c0 = c0;
+    ctl->c1 = c1;
+    ctl->nt[0] = max(0, min(all0, c1) - c0);
+    ctl->nt[1] = max(0, min(all1, c1) - c0);
+  };
+  int* base = reinterpret_cast<int*>(sm + S::B_OFF);
+  int cur = 0, end = 0;                                    // of the run: the next tile, the last one's end
+  if (!SHARED) {
+    // Launch order: the last rows of the entries first (they see the most), all key heads of a slot together.
+    const int slot = a.slots - 1 - blockIdx.x / Hkv;
+    if (warp == 0) {                                       // (one warp finds it out: twenty-four took 5 us a CTA)
+      const Unit u = unit_of(a, entry_of_slot(a, slot, lane), slot, blockIdx.x % Hkv, true);
+      if (lane == 0) {
+        tell(u, 0, max(u.tiles(a.heads, 0), u.tiles(a.heads, 1)));
+        ctl->whole = 1;
+        ctl->place = 0;
+      }
     }
+  } else {
+    // The slots' tiles (of all key heads) end to end: a thread a slot.
+    int own = 0;
+    if (threadIdx.x < a.slots) {
+      const Unit u = unit_of(a, entry_of_slot(a, threadIdx.x), threadIdx.x, 0, blockIdx.x == 0);
+      if (u.live) own = max(u.tiles(a.heads, 0), u.tiles(a.heads, 1)) * Hkv;
+      if (!u.live && blockIdx.x == 0)
+        for (int h = 0; h < Hkv; ++h) a.joins[threadIdx.x * Hkv + h] = make_int4(0, 0, 0, 0);
+    }
+    int upto = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += x;
+    }
+    if (lane == 31) ctl->sums[warp] = upto;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) upto += ctl->sums[w];
+    if (threadIdx.x < a.slots) base[threadIdx.x + 1] = upto;
+    if (threadIdx.x == 0) base[0] = 0;
+    __syncthreads();
   }
+  const Runs rs(SHARED ? base[a.slots] : 0, a.runs);
+  if (SHARED) {
+    if ((int)blockIdx.x >= rs.runs) return;
+    cur = rs.start(blockIdx.x);
+    end = rs.start(blockIdx.x + 1);
+  }
+  // The thread whose slot holds tile `cur` finds out the run's next piece.
+  auto next_piece = [&]() {
+    const int slot = threadIdx.x;
+    if (slot >= a.slots || cur < base[slot] || cur >= base[slot + 1]) return;
+    const int all = (base[slot + 1] - base[slot]) / Hkv, kvh = (cur - base[slot]) / all, unit0 = base[slot] + kvh * all;
+    const Unit u = unit_of(a, entry_of_slot(a, slot), slot, kvh, false);
+    const int c0 = cur - unit0, c1 = min(all, end - unit0);
+    tell(u, c0, c1);
+    ctl->whole = c1 - c0 == all;
+    const int first = rs.of(unit0), place0 = 2 * first + (rs.start(first) < unit0 ? 1 : 0);
+    ctl->place = (int)blockIdx.x == first ? place0 : 2 * (int)blockIdx.x;
+    if (c0 == 0) a.joins[slot * Hkv + kvh] = make_int4(first, place0, rs.of(unit0 + all - 1) - first + 1, u.b);
+  };
+  if (SHARED) next_piece();
   if (warp == 20) tc_alloc(&ctl->tslot, 512);
   if (threadIdx.x == 32) {
     tc_mbar_init(&ctl->qfull, 16);
@@ -171,19 +244,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
   __syncthreads();
   tc_fence_after();
   const uint32_t tbase = ctl->tslot;
-  Unit u;
-  u.b = ctl->b;
-  u.kvh = kvh;
-  u.rb = ctl->rb;
-  u.rows = ctl->rows;
-  u.pos0 = ctl->pos0;
-  u.len = ctl->len;
-  u.row0 = ctl->row0;
-  const int c0 = ctl->c0, ntiles = ctl->c1 - c0, nt[2] = {ctl->nt[0], ctl->nt[1]}, base_row = u.rb * kRows;
-  const int64_t part = ((int64_t)(slot * Hkv + kvh) * a.splits + split) * kRows;
-  if (!ctl->live || ntiles == 0) {                         // (no such rows; or fewer tiles than parts)
-    if (ctl->live)
-      for (int r = threadIdx.x; r < kRows; r += kThreads) a.part_st[part + r] = make_float4(kNoMax, 0.f, kNoMax, 0.f);
+  if (!ctl->live) {                                        // (no such rows)
+    __syncthreads();
     if (warp == 20) tc_dealloc(tbase, 512);
     return;
   }
@@ -191,6 +253,19 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
   Chunk* heads = reinterpret_cast<Chunk*>(sm + S::HD_OFF);
   uint32_t* status = a.status;
   const int all_copies = (1 << (kTokens >> a.w.log_box)) - 1;
+  int before = 0, done0 = 0, done1 = 0, pieces = 0, batch = 0;   // tiles of earlier pieces, of each block, and these
+  for (;;) {
+  Unit u;
+  u.b = ctl->b;
+  u.kvh = ctl->kvh;
+  u.rb = ctl->rb;
+  u.rows = ctl->rows;
+  u.pos0 = ctl->pos0;
+  u.len = ctl->len;
+  u.row0 = ctl->row0;
+  const int c0 = ctl->c0, ntiles = ctl->c1 - c0, nt[2] = {ctl->nt[0], ctl->nt[1]}, base_row = u.rb * kRows, kvh = u.kvh;
+  const bool whole = ctl->whole != 0;
+  const int64_t part = (int64_t)ctl->place * kRows;
 
   if (warp >= 20) {
     if (warp == 20 && elect_one()) {
@@ -206,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         return ok;
       };
       auto scores = [&](int k, int t) {
-        const Desc q0 = qd.at(k * S::QBLK).opaque(), k0 = kd.at(2 * t % kSlots * S::TILE).opaque();
+        const Desc q0 = qd.at(k * S::QBLK).opaque(), k0 = kd.at(2 * (before + t) % kSlots * S::TILE).opaque();
 #pragma unroll
         for (int j = 0; j < S::KA * 4; ++j)
           tc_mma_ss(tbase + (uint32_t)(k * kBR), q0.at((j >> 2) * S::ATOM + (j & 3) * 32),
@@ -214,29 +289,31 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         tc_commit(&ctl->sfull[k]);
       };
       auto values = [&](int k, int t, int half) {           // over half of tile t's tokens
-        const Desc v0 = vd.at((2 * t + 1) % kSlots * S::TILE + half * (kBR / 2) * 128).opaque();
+        const Desc v0 = vd.at((2 * (before + t) + 1) % kSlots * S::TILE + half * (kBR / 2) * 128).opaque();
         const uint32_t p0 = tbase + (uint32_t)(k * kBR + half * (kBR / 2));
 #pragma unroll
         for (int kk = 0; kk < kBR / 32; ++kk)
           tc_mma_ts(tbase + (uint32_t)(2 * kBR + k * kBR), p0 + (uint32_t)(kk * 8), v0.at(kk * 2048), idO,
                     t > 0 || half > 0 || kk > 0 ? 1u : 0u);
       };
-      bool ok = wait(&ctl->qfull, 0) && wait(&ctl->tile_full[0], 0);
+      const int first = 2 * before;
+      bool ok = wait(&ctl->qfull, (uint32_t)(pieces & 1)) &&
+                wait(&ctl->tile_full[first % kSlots], (uint32_t)((first / kSlots) & 1));
       if (ok) {
         for (int k = 0; k < 2; ++k)
           if (nt[k] > 0) scores(k, 0);
-        tc_commit(&ctl->tile_empty[0]);
+        tc_commit(&ctl->tile_empty[first % kSlots]);
       }
       for (int t = 0; ok && t < ntiles; ++t) {
-        const int vi = 2 * t + 1, ki = 2 * t + 2;          // places of this tile's values, of the next one's keys
+        const int vi = 2 * (before + t) + 1, ki = vi + 1;          // places of this tile's values, of the next one's keys
         ok = wait(&ctl->tile_full[vi % kSlots], (uint32_t)((vi / kSlots) & 1));
         for (int k = 0; ok && k < 2; ++k) {
           if (t < nt[k]) {
             // (the first half's weights arrive while the softmax works on the second)
-            ok = wait(&ctl->pfull[k][0], (uint32_t)(t & 1));
+            ok = wait(&ctl->pfull[k][0], (uint32_t)(((k == 0 ? done0 : done1) + t) & 1));
             if (!ok) break;
             values(k, t, 0);
-            ok = wait(&ctl->pfull[k][1], (uint32_t)(t & 1));
+            ok = wait(&ctl->pfull[k][1], (uint32_t)(((k == 0 ? done0 : done1) + t) & 1));
             if (!ok) break;
             values(k, t, 1);
             tc_commit(&ctl->pvdone[k]);
@@ -257,7 +334,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
       };
       const int log_box = a.w.log_box;
-      int batch = 0;
       load_chunks<kHeldBatches>(
           c, a.w, status, reinterpret_cast<float2*>(sm + S::SC_OFF), lane, batch, u.b, u.kvh, u.len, c0, c0 + ntiles, 0,
           [&]() { return true; },
@@ -266,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
             const int64_t from = (((int64_t)id * Hkv + u.kvh) * c.s.page + ((ch.chunk * kTokens + (at << log_box)) & (c.s.page - 1))) * D;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const int item = 2 * (ch.chunk - c0) + h, s = item % S::RAWS;
+              const int item = 2 * (before + ch.chunk - c0) + h, s = item % S::RAWS;
               if (item >= S::RAWS && !wait(&ctl->raw_empty[s], (uint32_t)((item / S::RAWS - 1) & 1))) return false;
               if (lane == 0) {
                 tc_mbar_expect_tx(&ctl->raw_full[s], bytes);
@@ -281,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
           },
           [&](const Chunk& ch) {
             // (its place is free: tile t's codes could only be loaded once tile t - 8 was done with)
-            const int t = ch.chunk - c0;
+            const int t = before + ch.chunk - c0;
             if (lane == 0) heads[t % kHeads] = ch;
             __syncwarp();
             if (lane == 0) tc_mbar_arrive(&ctl->head[t % kHeads]);
@@ -300,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
     };
     const uint32_t at0 = (uint32_t)((2 * (piece & 3)) ^ (row & 7)) << 4;
-    for (int item = 0; item < 2 * ntiles; ++item) {
+    for (int item = 2 * before; item < 2 * (before + ntiles); ++item) {
       const int t = item >> 1, rs = item % S::RAWS, s = item % kSlots;
       if (!(item & 1) && !wait(&ctl->head[t % kHeads], (uint32_t)((t / kHeads) & 1))) break;
       if (!wait(&ctl->raw_full[rs], (uint32_t)((item / S::RAWS) & 1))) break;
@@ -311,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
 #pragma unroll
       for (int i = 0; i < kBR / STEP; ++i) x[i] = *reinterpret_cast<const uint4*>(src + i * STEP * D);
       if (item & 1) {                                      // what no row sees must not meet a zero weight as NaN
-        const int copies = heads[t % kHeads].copies, tail = u.len - (c0 + t) * kBR;
+        const int copies = heads[t % kHeads].copies, tail = u.len - (c0 + t - before) * kBR;
         if (copies != all_copies || tail < kBR)
 #pragma unroll
           for (int i = 0; i < kBR / STEP; ++i)
@@ -336,6 +412,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     }
   } else {
     const int k = warp >> 3, half = warp >> 2 & 1;         // its block; its columns 64 half ..
+    const int ntk = k == 0 ? nt[0] : nt[1], dk = k == 0 ? done0 : done1;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tS = tbase + lanes + (uint32_t)(k * kBR), tO = tbase + lanes + (uint32_t)(2 * kBR + k * kBR);
     int8_t* qs = reinterpret_cast<int8_t*>(sm + S::QS_OFF);
@@ -399,18 +476,19 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     };
     float back = 1.f;
     if (BF16) {                                            // (all warps' queries are in place)
-      wait(&ctl->qfull, 0);
+      wait(&ctl->qfull, (uint32_t)(pieces & 1));
       back = power_of_two(-(int)qs[rin]);
     }
     constexpr int HC = kBR / 2;                            // columns of a thread
     const uint32_t tH = tS + (uint32_t)(half * HC);
     const int log_group = a.w.log_box - 4;
     float m = kNoMax, m2 = kNoMax, l = 0.f;
-    for (int t = 0; t < nt[k]; ++t) {
-      wait(&ctl->head[t % kHeads], (uint32_t)((t / kHeads) & 1));
-      wait(&ctl->sfull[k], (uint32_t)(t & 1));
-      const int copies = heads[t % kHeads].copies;
-      const float2* scales = reinterpret_cast<const float2*>(sm + S::SC_OFF) + heads[t % kHeads].scales;
+    for (int t = 0; t < ntk; ++t) {
+      const int at = (before + t) % kHeads;
+      wait(&ctl->head[at], (uint32_t)(((before + t) / kHeads) & 1));
+      wait(&ctl->sfull[k], (uint32_t)((dk + t) & 1));
+      const int copies = heads[at].copies;
+      const float2* scales = reinterpret_cast<const float2*>(sm + S::SC_OFF) + heads[at].scales;
       const bool part = c0 + t >= td || copies != all_copies;      // (a page outside the pool or past the length)
       const int lim = seen - (c0 + t) * kBR - half * HC;   // this thread's columns that its row sees
       // 32 columns' scores, those that the row does not see minus infinity
@@ -443,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         m = nm;
         m2 = nm2;
         if (t > 0) {
-          wait(&ctl->pvdone[k], (uint32_t)((t - 1) & 1));
+          wait(&ctl->pvdone[k], (uint32_t)((dk + t - 1) & 1));
 #pragma unroll 1
           for (int i = half * (D / 64); i < (half + 1) * (D / 64); ++i) {
             float o[32];
@@ -467,16 +545,15 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       if (lane == 0) tc_mbar_arrive(&ctl->pfull[k][half]);
     }
     // ---------------------------------------------------------------- output
-    if (nt[k] > 0) wait(&ctl->pvdone[k], (uint32_t)((nt[k] - 1) & 1));
+    if (ntk > 0) wait(&ctl->pvdone[k], (uint32_t)((dk + ntk - 1) & 1));
     l += exchange(make_float2(l, 0.f)).x;
     if (!dead) {
-      const bool whole = a.splits == 1;
       // zeros for a row that sees nothing; NaN for one whose scores are all minus infinity
       const float inv = seen <= 0 ? 0.f : l == 0.f ? NAN : 1.f / l, hp = half_power(m, m2);
       if (!whole && half == 0) a.part_st[part + rin] = make_float4(m, l, m2, 0.f);
       uint16_t* dst = c.out + (u.row0 + a.heads.token(row)) * c.out_stride + (int64_t)(kvh * a.heads.G + a.heads.head(row)) * D;
-      float* po = a.part_o + (part + rin) * D;
-      if (nt[k] > 0) {
+      float4* po = reinterpret_cast<float4*>(a.part_o) + part * (D / 4) + rin;
+      if (ntk > 0) {
 #pragma unroll 1
         for (int i = half * (D / 64); i < (half + 1) * (D / 64); ++i) {
           float o[32];
@@ -493,97 +570,116 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
           } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              reinterpret_cast<float4*>(po + i * 32)[e] = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+              __stcg(po + (8 * i + e) * kRows, make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]));
           }
         }
       }
     }
   }
-  // teardown: the products issued are complete; after a failure so are the copies (each wait bounded)
+  // the piece's end: the products issued are complete; after a failure so are the copies (each wait bounded)
+  cur += ntiles;
+  const bool more = cur < end;
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0) {
-    tc_mbar_wait(&ctl->drained, 0, kRoleWaitNs);
+    tc_mbar_wait(&ctl->drained, (uint32_t)(pieces & 1), kRoleWaitNs);
     if (ctl->fail)
       for (int x = std::max(0, ctl->loads - S::RAWS); x < ctl->loads; ++x)
         tc_mbar_wait(&ctl->raw_full[x % S::RAWS], (uint32_t)((x / S::RAWS) & 1), kRoleWaitNs);
   }
   __syncthreads();
   tc_fence_after();
+  if (!SHARED || !more || ctl->fail) break;
+  before += ntiles;
+  done0 += nt[0];
+  done1 += nt[1];
+  ++pieces;
+  next_piece();
+  __syncthreads();
+  }
   if (warp == 20) tc_dealloc(tbase, 512);
 }
 
-// out = sum_s 2^(m2_s - M2) o_s / sum_s 2^(m_s - M) l_s, a warp a row.
+// out = sum_i 2^(m2_i - M2) o_i / sum_i 2^(m_i - M) l_i over a unit's pieces i, four dims of a row a thread.
+template <int D>
+struct JShape {
+  static constexpr int ROWS = 1024 / D, TIMES = 4;         // rows side by side of a CTA, and one after another
+  static constexpr int CTAS = kRows / (ROWS * TIMES);      // of a unit
+};
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256) join_kernel(const PrefillArgs a) {
+  using J = JShape<D>;
   pdl_wait_and_trigger();
-  const int lane = threadIdx.x & 31, Hkv = a.c.s.Hkv;
-  const int unit = blockIdx.x / (kRows / 8), rin = blockIdx.x % (kRows / 8) * 8 + (threadIdx.x >> 5), slot = unit / Hkv;
-  const Unit u = unit_of(a, slot, unit - slot * Hkv, lane, false);
-  const int row = u.rb * kRows + rin;
-  if (!u.live || row >= u.rows) return;
-  const int64_t part = (int64_t)unit * a.splits * kRows + rin;
-  float mx = kNoMax, mx2 = kNoMax;
-  const float4 st = lane < a.splits ? a.part_st[part + (int64_t)lane * kRows] : make_float4(kNoMax, 0.f, kNoMax, 0.f);
-  mx = st.x;
-  mx2 = st.z;
+  const int Hkv = a.c.s.Hkv, unit = blockIdx.x / J::CTAS, slot = unit / Hkv;
+  const int r0 = blockIdx.x % J::CTAS * (J::ROWS * J::TIMES) + threadIdx.x % J::ROWS, d4 = threadIdx.x / J::ROWS;
+  const int4 of = a.joins[unit];
+  if (of.z <= 1) return;                                   // (a whole unit, or none)
+  const Unit u = unit_of(a, of.w, slot, unit - slot * Hkv, false);
+  auto at = [&](int i) { return (int64_t)(i == 0 ? of.y : 2 * (of.x + i)); };
+  float mx[J::TIMES], mx2[J::TIMES], sum[J::TIMES];
+  float4 y[J::TIMES];
 #pragma unroll
-  for (int d = 16; d; d >>= 1) {
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-    mx2 = fmaxf(mx2, __shfl_xor_sync(0xffffffffu, mx2, d));
+  for (int k = 0; k < J::TIMES; ++k) {
+    mx[k] = mx2[k] = kNoMax;
+    sum[k] = 0.f;
+    y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-  float sum = st.y * ex2_approx(st.x - mx);
-  const float w2 = ex2_approx(st.z - mx2);
+  const float4* po = reinterpret_cast<const float4*>(a.part_o);
+#pragma unroll 2
+  for (int i = 0; i < of.z; ++i) {
 #pragma unroll
-  for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  // (a part that met no tile of the row's block wrote no outputs)
-  const unsigned has = __ballot_sync(0xffffffffu, st.z != kNoMax);
-  constexpr int VL = D / 32;
-  float y[VL];
-#pragma unroll
-  for (int k = 0; k < VL; ++k) y[k] = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < a.splits; ++s) {
-    const float f = __shfl_sync(0xffffffffu, w2, s);
-    if (!(has >> s & 1)) continue;
-    const float* po = a.part_o + (part + (int64_t)s * kRows) * D + lane * VL;
-#pragma unroll
-    for (int k = 0; k < VL; ++k) y[k] += f * po[k];
+    for (int k = 0; k < J::TIMES; ++k) {
+      const int r = r0 + k * J::ROWS;
+      const float4 st = __ldcg(a.part_st + at(i) * kRows + r);
+      float4 z = __ldcg(po + (at(i) * (D / 4) + d4) * kRows + r);
+      if (st.z == kNoMax) z = make_float4(0.f, 0.f, 0.f, 0.f);       // (no tile of the row's block: no outputs were written)
+      const float nm = fmaxf(mx[k], st.x), nm2 = fmaxf(mx2[k], st.z), f = ex2_approx(mx2[k] - nm2), g = ex2_approx(st.z - nm2);
+      sum[k] = sum[k] * ex2_approx(mx[k] - nm) + st.y * ex2_approx(st.x - nm);
+      y[k] = make_float4(y[k].x * f + z.x * g, y[k].y * f + z.y * g, y[k].z * f + z.z * g, y[k].w * f + z.w * g);
+      mx[k] = nm;
+      mx2[k] = nm2;
+    }
   }
-  const float inv = u.seen(a.heads, row) <= 0 ? 0.f : sum == 0.f ? NAN : 1.f / sum, hp = half_power(mx, mx2);
 #pragma unroll
-  for (int k = 0; k < VL; ++k) y[k] = inv == 0.f ? 0.f : y[k] * inv * hp * hp;
-  uint16_t* dst = a.c.out + (u.row0 + a.heads.token(row)) * a.c.out_stride + (int64_t)(u.kvh * a.heads.G + a.heads.head(row)) * D + lane * VL;
-  if constexpr (VL == 4)
-    *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<BF16>(y[0], y[1]), pack2<BF16>(y[2], y[3]));
-  else
-    *reinterpret_cast<uint32_t*>(dst) = pack2<BF16>(y[0], y[1]);
+  for (int k = 0; k < J::TIMES; ++k) {
+    const int row = u.rb * kRows + r0 + k * J::ROWS;
+    if (row >= u.rows) continue;
+    // zeros for a row that sees nothing; NaN for one whose scores are all minus infinity
+    const float inv = u.seen(a.heads, row) <= 0 ? 0.f : sum[k] == 0.f ? NAN : 1.f / sum[k], hp = half_power(mx[k], mx2[k]);
+    const float4 x = inv == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                : make_float4(y[k].x * inv * hp * hp, y[k].y * inv * hp * hp, y[k].z * inv * hp * hp, y[k].w * inv * hp * hp);
+    uint16_t* dst = a.c.out + (u.row0 + a.heads.token(row)) * a.c.out_stride + (int64_t)(u.kvh * a.heads.G + a.heads.head(row)) * D + d4 * 4;
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<BF16>(x.x, x.y), pack2<BF16>(x.z, x.w));
+  }
 }
 
 // ---------------------------------------------------------------- host side
 struct Plan {
   int64_t slots;
-  int per, splits;
+  int per, runs;
 };
 Plan plan_of(const PagedAttnCall& c) {
   Plan p{};
   const int64_t G = c.s.Hq / c.s.Hkv, m = ceil_div(c.s.n, c.s.B);
   p.per = (int)ceil_div(m * G, kRows);
   p.slots = c.s.start == nullptr ? (int64_t)c.s.B * p.per : (c.s.n * G + (int64_t)c.s.B * (kRows - 1)) / kRows;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(32, kNumSMs / std::max<int64_t>(1, p.slots * c.s.Hkv)));
+  // (tiles are counted in 32 bits)
+  const int64_t units = p.slots * c.s.Hkv, tiles = c.s.max_pages * c.s.page / kTokens + 1;
+  p.runs = units <= kShared && units * tiles <= INT32_MAX / 2 ? kNumSMs : 0;
   return p;
 }
 
 template <class S, bool BF16>
 cudaError_t launch_shape(const PrefillArgs& a, cudaStream_t st) {
   const int64_t units = (int64_t)a.slots * a.c.s.Hkv;
-  if (units * a.splits > INT32_MAX) return cudaErrorInvalidConfiguration;
+  if (units > INT32_MAX) return cudaErrorInvalidConfiguration;
   constexpr int smem = std::max(S::ALLOC, 116 * 1024);      // one CTA an SM: it takes all of the tensor memory
-  cudaError_t e = cudaFuncSetAttribute(prefill_kernel<S, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  auto* kernel = a.runs != 0 ? prefill_kernel<S, BF16, true> : prefill_kernel<S, BF16, false>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(prefill_kernel<S, BF16>, dim3((unsigned)(units * a.splits)), dim3(kThreads), smem, st, a);
-  if (e != cudaSuccess || a.splits == 1) return e;
-  return launch_pdl(join_kernel<S::D, BF16>, dim3((unsigned)(units * (kRows / 8))), dim3(256), 0, st, a);
+  e = launch_pdl(kernel, dim3((unsigned)(a.runs != 0 ? a.runs : units)), dim3(kThreads), smem, st, a);
+  if (e != cudaSuccess || a.runs == 0) return e;
+  return launch_pdl(join_kernel<S::D, BF16>, dim3((unsigned)(units * JShape<S::D>::CTAS)), dim3(256), 0, st, a);
 }
 template <int FMT, int D>
 cudaError_t launch_d(const PrefillArgs& a, cudaStream_t st) {
@@ -596,9 +692,8 @@ cudaError_t launch_d(const PrefillArgs& a, cudaStream_t st) {
 }  // namespace
 
 size_t paged_prefill_ws_bytes(const PagedAttnCall& c) {
-  // (one part an SM at most, where units have several)
-  const size_t parts = kNumSMs;
-  return kCounterBytes + align256(parts * kRows * sizeof(float4)) + align256(parts * kRows * c.s.D * sizeof(float));
+  const size_t rows = (size_t)kNumSMs * 2 * kRows;
+  return kCounterBytes + align256(kShared * sizeof(int4)) + align256(rows * sizeof(float4)) + align256(rows * c.s.D * sizeof(float));
 }
 
 cudaError_t launch_paged_prefill(const PagedAttnCall& c, void* ws, cudaStream_t st) {
@@ -612,10 +707,11 @@ cudaError_t launch_paged_prefill(const PagedAttnCall& c, void* ws, cudaStream_t 
   if (p.slots > INT32_MAX) return cudaErrorInvalidConfiguration;
   a.slots = (int)p.slots;
   a.per = p.per;
-  a.splits = p.splits;
+  a.runs = p.runs;
   uint8_t* base = static_cast<uint8_t*>(ws) + kCounterBytes;
-  a.part_st = reinterpret_cast<float4*>(base);
-  a.part_o = reinterpret_cast<float*>(base + align256((size_t)kNumSMs * kRows * sizeof(float4)));
+  a.joins = reinterpret_cast<int4*>(base);
+  a.part_st = reinterpret_cast<float4*>(base + align256(kShared * sizeof(int4)));
+  a.part_o = reinterpret_cast<float*>(base + align256(kShared * sizeof(int4)) + align256((size_t)kNumSMs * 2 * kRows * sizeof(float4)));
   if (c.s.format == MKV_E4M3) return c.s.D == 128 ? launch_d<MKV_E4M3, 128>(a, st) : launch_d<MKV_E4M3, 64>(a, st);
   return c.s.D == 128 ? launch_d<MKV_I8, 128>(a, st) : launch_d<MKV_I8, 64>(a, st);
 }
