@@ -33,7 +33,8 @@
  *  - Shapes: B batch entries, Hq query heads, Hkv key/value heads,
  *    G = Hq/Hkv query heads per group, D head dimension.  Supported:
  *    D in {64, 128}; G in {1, 2, 4, 8}; bits in {2, 3, 4}; page_size 16.
- *    Anything else returns MKV_ERR_UNSUPPORTED.
+ *    Anything else returns MKV_ERR_UNSUPPORTED.  (Operators that take more
+ *    say so at their configuration.)
  *  - Layouts are row-major with the last index fastest:
  *      q            [B][Hq][D] fp16 (already rotated by the query position)
  *      out          [B][Hq][D] fp16
@@ -663,8 +664,9 @@ mkv_status mkv_rope_apply(const mkv_rope_config* cfg, int32_t dtype, const void*
  * written. */
 typedef enum {
   MKV_E4M3 = 0,   /* 8-bit floats, largest 448; the two NaN codes are never
-                     written, and are NaN where a token holds them (what lies
-                     behind an entry's last token may be anything)          */
+                     written, and a token that holds one may make NaN of every
+                     row computed beside it (what lies behind an entry's last
+                     token may be anything)                                 */
   MKV_I8 = 1      /* two's complement, -127..127                             */
 } mkv_code_format;
 
@@ -679,17 +681,19 @@ typedef struct {
 } mkv_paged_config;
 
 /* Device memory owned by the caller.  The pages of an entry differ from one
- * another, and those that an append writes into belong to no other entry. */
+ * another, and those that an append writes into belong to no other entry (full
+ * pages may be shared, as those of a common beginning).  num_pages * Hkv and
+ * max_pages * page_size stay below 2^31. */
 typedef struct {
   int64_t num_pages;            /* pages in the pool                          */
   int64_t max_pages;            /* pages an entry may hold                    */
   const int32_t* page_table;    /* int32 [B][max_pages]                       */
   int32_t* T_len;               /* int32 [B]: tokens held                     */
   int32_t* tickets;             /* int32 [B]: zero-filled by the caller once;
-                                   every call leaves them zero                */
+                                   every append leaves them zero              */
   void* k;                      /* codes [num_pages][Hkv][page_size][D],      */
   void* v;                      /*   16-byte aligned                          */
-  float* k_scale;               /* fp32 [num_pages][Hkv], positive and finite */
+  float* k_scale;               /* fp32 [num_pages][Hkv], positive, finite, normal */
   float* v_scale;
 } mkv_paged_cache;
 
@@ -710,9 +714,9 @@ typedef struct {
 } mkv_paged_rows;
 
 /* One launch that rotates the rows' queries and keys (rope, table and T_max as
- * for mkv_rope_apply, rot_dim a multiple of 16; rope NULL: taken as they are),
- * quantizes keys and values into the pages behind T_len[b], and adds the rows
- * to T_len.  A page's scale is the least power of two (2^-100..2^120) with
+ * for mkv_rope_apply, with rope->D the cache's, rot_dim a multiple of 16 and a
+ * 16-byte aligned table; rope NULL: taken as they are), quantizes keys and
+ * values into the pages behind T_len[b], and adds the rows to T_len.  A page's scale is the least power of two (2^-100..2^120) with
  * which its largest magnitude is at most 448 or 127 codes; a page that held
  * tokens keeps its scale if the new ones fit it, else it takes the larger one
  * and the codes that it held are rounded again.  Codes are rounded to nearest
@@ -724,17 +728,25 @@ mkv_status mkv_paged_append(const mkv_paged_config* cfg, const mkv_rope_config* 
                             const mkv_paged_rows* rows, mkv_paged_cache* cache, void* stream);
 
 /* Bytes of workspace mkv_paged_attention needs for n rows, at most max_rows of
- * an entry (laid out as mkv_workspace_size describes).  Host only. */
+ * an entry (laid out as mkv_workspace_size describes): at most 42 MB, and no
+ * less for more rows, so that one of the size for a program's largest call does
+ * for all of them.  Host only. */
 mkv_status mkv_paged_workspace_size(const mkv_paged_config* cfg, int64_t n, int64_t max_rows, size_t* bytes);
 
 /* Causal attention of the entries' newest rows, which the cache holds already:
  * row i of entry b's m is at position T_len[b] - m + i and attends to the
  * tokens up to its own; a row before position 0 gets zeros.  q [n][Hq][D] (row
  * stride q_stride elements; 0: Hq * D), out likewise, 16-byte aligned, strides
- * multiples of 8.  No entry has more than max_rows rows (1..n); one that does
- * is left out and sets MKV_FLAG_BAD_INDEX.  Tokens of a page outside the pool
- * are not seen (MKV_FLAG_BAD_INDEX).  The cache is only read.  ws must be
- * 256-byte aligned. */
+ * multiples of 8; out may be q itself (with the same stride), but must not
+ * overlap it otherwise.  No entry has more than max_rows rows (1..n); one that
+ * does is left out and sets MKV_FLAG_BAD_INDEX.  Tokens of a page outside the
+ * pool are not seen (MKV_FLAG_BAD_INDEX); a row that is left with none gets
+ * NaN.  A T_len above max_pages * page_size is taken as that.  B * Hkv *
+ * max_pages * page_size is at most 2^36, max_rows * Hq / Hkv at most 2^26.  The
+ * cache is only read.  ws must be 256-byte aligned.  The path is chosen by
+ * max_rows, so give the true maximum (1 for a step of single tokens).  After a
+ * bounded wait that ran out (MKV_FLAG_WAIT_TIMEOUT), outputs are not valid and
+ * the counters of ws have to be zeroed again. */
 mkv_status mkv_paged_attention(const mkv_paged_config* cfg, const void* q, int64_t q_stride, const int32_t* start,
                                int64_t n, int64_t max_rows, const mkv_paged_cache* cache, void* out,
                                int64_t out_stride, void* ws, size_t ws_bytes, void* stream);

@@ -39,7 +39,7 @@ mkv_status check_rope(const mkv_rope_config* c) {
   return MKV_OK;
 }
 
-// The table of a rotation that a call takes; `wide`: as the append needs it.
+// A rotation and the table that a call takes.
 mkv_status check_table(const mkv_rope_config* c, const float* table, int64_t T_max) {
   MKV_TRY(check_rope(c));
   MKV_REQUIRE(table != nullptr && T_max >= 1, MKV_ERR_INVALID_ARG, "rope table NULL or empty");
@@ -278,11 +278,12 @@ mkv_status mkv_paged_attention(const mkv_paged_config* cfg, const void* q, int64
   c.out_stride = out_stride;
   MKV_TRY(check_row("q", q, dims, &c.q_stride));
   MKV_TRY(check_row("out", out, dims, &c.out_stride));
+  MKV_REQUIRE(q != out || c.q_stride == c.out_stride, MKV_ERR_INVALID_ARG, "in place, the strides must be the same");
   c.s = shape_of(cfg, n, start, cache);
   c.max_rows = max_rows;
-  // (chunks of 128 tokens are counted in 32 bits)
-  MKV_REQUIRE((int64_t)cfg->B * cfg->Hkv * (cache->max_pages * cfg->page_size / 128 + 1) <= INT32_MAX / 2, MKV_ERR_UNSUPPORTED,
-              "too many tokens (max_pages x B x Hkv) for one call");
+  // (chunks of 128 tokens are counted in 32 bits: 2^29, and one more a unit)
+  MKV_REQUIRE(cache->max_pages * cfg->page_size <= (int64_t(1) << 36) / ((int64_t)cfg->B * cfg->Hkv), MKV_ERR_UNSUPPORTED,
+              "too many tokens (B x Hkv x max_pages x page_size) for one call");
   const size_t need = attention_ws_bytes(c);
   MKV_REQUIRE(ws != nullptr && ws_bytes >= need, MKV_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
   MKV_REQUIRE(aligned(ws, 256), MKV_ERR_INVALID_ARG, "ws must be 256-byte aligned");

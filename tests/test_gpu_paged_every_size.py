@@ -188,3 +188,30 @@ def test_far_offsets(most):
     torch.cuda.synchronize()
     assert mkv.mkv_get_status() == 0
     assert torch.equal(rows(out), want)
+
+
+@every
+def test_short_entries_beside_long_ones(most):
+    """Some entries with hundreds of times the others' tokens: work is shared out in runs that hold several entries."""
+    B = 20
+    lens = [6000 if b in (3, 11) else most + 13 * b for b in range(B)]
+    c = Case("bf16", "e4m3", 8, 2, 64, 16, lens, [most if b % 4 else max(1, most - b) for b in range(B)])
+    c.run()
+    c.check()
+
+
+@every
+def test_one_graph_for_all_lengths(most):
+    """A call captured once, replayed as the entries' lengths change on the device (and with them how work is shared out)."""
+    torch = torch_cuda()
+    c = Case("fp16", "int8", 8, 2, 128, 32, [4000, 300, 2000], [most, most, 1], max_pages=126)
+    g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=side):
+        c.run(torch.cuda.current_stream().cuda_stream)
+    for lens in ([4000, 300, 2000], [most, 90, 1], [0, 0, 0], [129, 4032, 700], [4032, 4032, 4032]):
+        c.hc.lens = np.array(lens, dtype=np.int32)
+        c.hc.cache.t["T_len"].copy_(device(c.hc.lens))
+        c.out[:c.n].fill_(5)
+        g.replay()
+        c.check(what=f"{lens}")

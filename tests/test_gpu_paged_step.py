@@ -158,3 +158,48 @@ def test_two_streams():
         s.check(qkv, new, outs, f"{new}", lengths=False)
     for s in servers:
         assert all(c.t["T_len"].cpu().numpy().tolist() == s.lens.tolist() for c in s.caches)
+
+
+@pytest.mark.parametrize("new", [[1, 3], [200, 90]])
+def test_append_far_offsets(new):
+    """Rows and a pool whose offsets pass 32 bits: bit for bit what the same call writes close together."""
+    torch = torch_cuda()
+    rng, Hq, Hkv, D, page, B = seeded("far", tuple(new)), 8, 2, 128, 64, 2
+    cfg, rope = mkv.paged_config(mkv.MKV_BF16, mkv.MKV_I8, B, Hq, Hkv, D, page), mkv.rope_config(D)
+    table, lens, most, n = caches.rope_table(rope, 512), [70, 0], 5, sum(new)
+    qkv = randn(rng, (n, Hq + 2 * Hkv, D), "bf16")
+    start = device(np.concatenate([[0], np.cumsum(new)]).astype(np.int32))
+    before = (1 << 32) // (Hkv * page * D) + 50
+    got = []
+    for first, stride in ((0, (Hq + 2 * Hkv) * D), (before, (1 << 31) // (n - 1) // 8 * 8 + (Hq + 2 * Hkv) * D)):
+        pools = [torch.zeros((first + B * most, Hkv, page, D), dtype=torch.int8, device="cuda") for _ in range(2)]
+        scales = [torch.ones((first + B * most, Hkv), device="cuda") for _ in range(2)]
+        ids = (torch.arange(B * most, device="cuda") + first).to(torch.int32).reshape(B, most)
+        c = caches.wrap_paged_cache(cfg, ids, device(np.array(lens, np.int32)), *pools, *scales)
+        x, out = (torch.zeros(stride * (n - 1) + (Hq + 2 * Hkv) * D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        x.as_strided(qkv.shape, (stride, D, 1)).copy_(qkv)
+        rows = mkv.paged_rows(n, start=start.data_ptr(), q=x.data_ptr(), q_stride=stride, k=x[Hq * D:].data_ptr(), k_stride=stride,
+                              v=x[(Hq + Hkv) * D:].data_ptr(), v_stride=stride, q_out=out.data_ptr(), q_out_stride=stride)
+        mkv.mkv_paged_append(cfg, rope, table.data_ptr(), 512, rows, c.c)
+        torch.cuda.synchronize()
+        assert mkv.mkv_get_status() == 0
+        got.append([y[first:].clone() for y in pools + scales] + [c.t["T_len"], out.as_strided((n, Hq, D), (stride, D, 1)).clone()])
+    for y, z in zip(*got):
+        assert torch.equal(y, z)
+
+
+def test_rope_far_offsets():
+    torch = torch_cuda()
+    rng, n, heads, D = seeded("far rope"), 9, 5, 128
+    cfg = mkv.rope_config(D)
+    table, pos = caches.rope_table(cfg, 512), device(rng.integers(0, 512, n).astype(np.int32))
+    src = randn(rng, (n, heads, D), "bf16")
+    got = []
+    for stride in (heads * D, (1 << 31) // (n - 1) + heads * D):
+        x, out = (torch.zeros(stride * (n - 1) + heads * D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        x.as_strided(src.shape, (stride, D, 1)).copy_(src)
+        mkv.mkv_rope_apply(cfg, mkv.MKV_BF16, x.data_ptr(), stride, pos.data_ptr(), n, heads, table.data_ptr(), 512, 0, out.data_ptr(),
+                           stride)
+        got.append(out.as_strided(src.shape, (stride, D, 1)).clone())
+    torch.cuda.synchronize()
+    assert mkv.mkv_get_status() == 0 and torch.equal(*got)

@@ -138,3 +138,29 @@ def test_wrapped_caches_are_checked():
         caches.wrap_paged_cache(cfg, **{**good, "k": good["k"][0]})
     with pytest.raises(ValueError):
         caches.wrap_paged_cache(cfg, **good, tickets=torch.zeros(1, dtype=torch.int32))
+
+
+def test_attention_limits(L):
+    def attend(cfg, cache, n=4, most=2, out=2 * P, qs=0, os=0):
+        return L.mkv_paged_attention(by(cfg), P, qs, P, n, most, by(cache), out, os, P, ctypes.c_size_t(16), None)
+    assert attend(_cfg(), _cache()) == WSP                # (all else is in order)
+    assert attend(_cfg(), _cache(), out=P, os=2048) == INV
+    assert attend(_cfg(), _cache(), out=P, qs=2048, os=2048) == WSP
+    # query rows of a key head: 2^26
+    assert attend(_cfg(), _cache(), n=1 << 25, most=(1 << 24)) == WSP
+    assert attend(_cfg(), _cache(), n=1 << 25, most=(1 << 24) + 1) == UNS
+    # tokens of all units: 2^36
+    big = _cfg(B=64, Hq=32, Hkv=32, page_size=128)
+    assert attend(big, _cache(max_pages=1 << 18)) == WSP
+    assert attend(big, _cache(max_pages=(1 << 18) + 1)) == UNS
+
+
+def test_workspace_grows_with_the_rows(L):
+    """Never less for more rows: a workspace for the largest call serves the others; and it does not grow past 42 MB."""
+    size = ctypes.c_size_t(0)
+    for kw in (dict(), dict(D=64, Hq=32, Hkv=1), dict(B=1, Hq=3, Hkv=3)):
+        last = 0
+        for most in (1, 2, 4, 8, 9, 16, 32, 33, 64, 65, 128, 129, 1000, 4096, 100000):
+            assert L.mkv_paged_workspace_size(by(_cfg(**kw)), 1 << 20, most, by(size)) == mkv.MKV_OK
+            assert last <= size.value <= 42 * 10 ** 6, (kw, most)
+            last = size.value
