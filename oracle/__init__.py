@@ -24,6 +24,7 @@ Modules
   order      -- the total orders used for every ranking decision        (O7)
   selector   -- the configuration choice over predicted costs (Section 2.3) (O8)
   latent     -- attention under a visibility pattern, latent attention     (O9)
+  paged      -- rotary positions with scaled frequencies, 8-bit codes and pages (O10)
 
 Parity status: every function is pinned by tests in ``tests/test_oracle_*``
 against closed forms, invariants, brute force or an independent library

@@ -70,8 +70,9 @@ struct PagedAttnCall {
   const uint8_t *k, *v;
   const float *k_scale, *v_scale;
 };
-// By the query rows of a key head (max_rows x heads of a group): up to kPagedFew paged_decode.cu, up to kPagedBlock
-// paged_block.cu, more paged_prefill.cu.
+// By the query rows of a key head (max_rows x heads of a group): up to kPagedFew, what a narrow product takes, paged_decode.cu,
+// up to kPagedBlock, a block of a tcgen05 product, paged_block.cu, more paged_prefill.cu.  Over 8 x 8K tokens, 32 / 8 heads:
+// one token 31 us (by paged_block.cu 51), two 31 (42), eight 44 (by paged_prefill.cu 74), sixteen 56 (74), 32 71 (75).
 constexpr int kPagedFew = 8, kPagedBlock = 128;
 size_t paged_decode_ws_bytes(const PagedAttnCall& c);
 cudaError_t launch_paged_decode(const PagedAttnCall& c, void* ws, cudaStream_t st);

@@ -12,23 +12,25 @@ namespace mkv {
 constexpr int kTokens = 128;        // of a chunk
 constexpr int kGroups = kTokens / 16;
 
-// Up to this many chunks a CTA, equal parts of every unit where entries are equally long; beyond it a CTA's few pieces cost
-// less than the SMs that such a cut leaves without work.
-constexpr int kLongRun = 32;
-
 struct WorkArgs {
   int log_page, log_box;            // a copy's tokens: a page's, a chunk's at most
   int parts;                        // CTAs a unit if each gets as many; 0: not to be done
+  int lost;                         // so many chunks more a CTA are worth it
   int grid;
   float scale_log2;
 };
-// (equal parts that leave more than a fifth of the CTAs without work are not worth it)
-inline WorkArgs work_args(const PagedAttnCall& c, int grid) {
+// Where entries are equally long, every unit may be cut into equal parts, so that no CTA has pieces of two units.  That costs
+// the CTAs that such a cut leaves without work: not taken beyond a fifth of them, or `lost` chunks a CTA.  (One token, where
+// memory is the bound whatever the CTAs: 8 x 8K 32.2 -> 30.8 us, 16 x 32K, 256 of 304 CTAs, 164 -> 161.  Eight drafted tokens,
+// 152 CTAs that are bound themselves: 8 x 8K, 5 chunks lost, 47 -> 44; 8 x 32K, 20 lost, 121 -> 129.)
+constexpr int kAnyLost = 1 << 30;
+inline WorkArgs work_args(const PagedAttnCall& c, int grid, int lost) {
   WorkArgs w{};
   while ((1 << w.log_page) < c.s.page) ++w.log_page;
   w.log_box = w.log_page;           // (pages are of 16 to 128 tokens)
   const int units = c.s.B * c.s.Hkv, parts = grid / units;
   w.parts = parts * units * 5 >= grid * 4 ? parts : 0;
+  w.lost = lost;
   w.grid = grid;
   w.scale_log2 = c.scale * kLog2e;
   return w;
@@ -180,11 +182,10 @@ __device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkA
     for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
   }
   total += upto32;
-  // Entries of one length (and of few chunks): the same parts of every unit, so that no CTA has pieces of two.
   const int chunks0 = __shfl_sync(0xffffffffu, held.chunks, 0);
-  const bool even = B <= 32 && w.parts > 0 && total < w.grid * kLongRun &&
+  const int part = w.parts > 0 ? (chunks0 + w.parts - 1) / w.parts : 0;  // chunks of each
+  const bool even = B <= 32 && w.parts > 0 && part - total / w.grid <= w.lost &&
                     __all_sync(0xffffffffu, lane >= B || held.chunks == chunks0);
-  const int part = even ? (chunks0 + w.parts - 1) / w.parts : 0;         // chunks of each
   Runs rs(total, w.grid);
   if (even) rs.runs = B * Hkv * w.parts;
   const int r = blockIdx.x;

@@ -5,7 +5,7 @@
 // for all of their layers.  Applying it is bound by memory: every value is read and written once.  A thread holds the
 // (cos, sin) of eight pairs and takes those pairs in several heads of its token, so that the table (8 bytes a pair, as
 // much as a head's values) is read once a token rather than once a head; small calls take one head a thread, since they
-// only pay latency.
+// only pay latency.  8192 tokens x 40 heads of 128 dims: 31 us, 0.81 of the measured copy rate; 8 tokens: 2.1 us, the launch.
 #include <algorithm>
 
 #include "mkv_paged.cuh"
@@ -151,7 +151,8 @@ cudaError_t launch_rope_apply(const RopeApplyCall& c, cudaStream_t st) {
   }
   a.turns = c.rope.rot / 16;
   a.cols = a.turns + (c.out == c.x ? 0 : (c.D - c.rope.rot) / 8);
-  // One head a thread until the GPU's threads (2048 an SM) are taken, then up to eight.
+  // One head a thread until the GPU's threads (2048 an SM) are taken, then up to eight.  (8192 tokens x 40 heads: eight 31 us,
+  // one 99; 8 tokens: 3.4 against 2.1; 1001 tokens of 12 heads of 64: 4.3 against 3.8.)
   const int64_t work = c.n * c.heads * a.cols;
   a.loops = (int)std::min<int64_t>(8, std::max<int64_t>(1, work / (2048 * kNumSMs)));
   a.slots = (int)std::min<int64_t>(ceil_div(c.heads, a.loops), kThreads / a.cols);
