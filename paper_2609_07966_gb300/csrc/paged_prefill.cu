@@ -662,6 +662,8 @@ __global__ void __launch_bounds__(256) join_kernel(const PrefillArgs a) {
   const int r0 = blockIdx.x % J::CTAS * (J::ROWS * J::TIMES) + threadIdx.x % J::ROWS, d4 = threadIdx.x / J::ROWS;
   const int4 of = a.joins[unit];
   if (of.z <= 1) return;                                   // (a whole unit, or none)
+  // (lengths that another stream changes under way leave CTAs at odds: then nothing outside the workspace is read)
+  if (of.x < 0 || of.z > kNumSMs - of.x || of.y < 0 || of.y >= 2 * kNumSMs || of.w < 0 || of.w >= a.c.s.B) return;
   const Unit u = unit_of(a, of.w, slot, unit - slot * Hkv, false);
   auto at = [&](int i) { return (int64_t)(i == 0 ? of.y : 2 * (of.x + i)); };
   float mx[J::TIMES], mx2[J::TIMES], sum[J::TIMES];

@@ -203,3 +203,53 @@ def test_rope_far_offsets():
         got.append(out.as_strided(src.shape, (stride, D, 1)).clone())
     torch.cuda.synchronize()
     assert mkv.mkv_get_status() == 0 and torch.equal(*got)
+
+
+@pytest.mark.parametrize("rows", [1, 9, 130])
+def test_as_many_entries_as_there_may_be(rows):
+    """4096 entries: their rows are appended (entries without any among them) and attended to; some of them are checked."""
+    torch = torch_cuda()
+    B, rng = 4096, seeded("many", rows)
+    new = rng.integers(0, rows + 1, B) if rows < 100 else np.where(np.arange(B) % 64 == 5, rows, rng.integers(0, 3, B))
+    new[:2] = rows, 0
+    cfg = mkv.paged_config(mkv.MKV_F16, mkv.MKV_E4M3, B, 2, 1, 64, 16)
+    held, pages, n = rng.integers(0, 20, B), 11, int(new.sum())
+    c = caches.alloc_paged_cache(cfg, B * pages, pages)
+    c.t["page_table"].copy_(torch.arange(B * pages, device="cuda").to(torch.int32).reshape(B, pages))
+    qkv, q = randn(rng, (n + int(held.sum()), 4, 64), "fp16"), torch.empty(n, 2, 64, dtype=torch.float16, device="cuda")
+    ws, nws = caches.paged_workspace(cfg, n, rows)
+
+    def append(x, m):
+        start = device(np.concatenate([[0], np.cumsum(m)]).astype(np.int32))
+        mkv.mkv_paged_append(cfg, None, 0, 0, mkv.paged_rows(len(x), start=start.data_ptr(), k=x[:, 2:].data_ptr(), k_stride=256,
+                                                             v=x[:, 3:].data_ptr(), v_stride=256), c.c)
+        torch.cuda.synchronize()
+        return start
+    append(qkv[n:], held)
+    start = append(qkv[:n], new)
+    q.copy_(qkv[:n, :2])
+    mkv.mkv_paged_attention(cfg, q.data_ptr(), 0, start.data_ptr(), n, rows, c.c, q.data_ptr(), 0, ws.data_ptr(), nws)
+    torch.cuda.synchronize()
+    assert mkv.mkv_get_status() == 0
+    assert c.t["T_len"].cpu().numpy().tolist() == (held + new).tolist()
+    first, before = np.concatenate([[0], np.cumsum(new)]), np.concatenate([[0], np.cumsum(held)]) + n
+    host = f64(qkv)
+    for b in [0, 5, 69, 4095] + list(rng.choice(B, 60)):
+        m, t = int(new[b]), int(held[b] + new[b])
+        tokens = []
+        for i, name in ((2, "k"), (3, "v")):
+            x = np.concatenate([host[before[b]:before[b + 1], i], host[first[b]:first[b + 1], i]])
+            ids = slice(b * pages, b * pages + -(-t // 16))
+            z = P.decode(c.t[name].view(torch.uint8)[ids, 0].cpu().numpy(), "e4m3") * \
+                f64(c.t[name + "_scale"][ids, 0])[:, None, None]
+            z = z.reshape(-1, 64)[:t]
+            # a code is off by half a step, 2^-4 of the value; where its page's scale grew, what fell below the normal range was
+            # rounded again, by half of the least step, 2^-10 of a scale that is at most 2 / 448 of the page's largest value
+            assert (np.abs(z - x) <= 2.0 ** -3 * np.abs(x) + 2.0 ** -9 * np.abs(x).max(initial=0.0)).all(), b
+            tokens.append(z)
+        if m:
+            vis = np.arange(t)[None, :] <= (t - m + np.arange(m))[:, None]
+            ref, mag = attend_visible(host[first[b]:first[b + 1], :2].reshape(2 * m, 64), *tokens, np.repeat(vis, 2, axis=0), 0.125)
+            got = f64(q)[first[b]:first[b + 1]].reshape(2 * m, 64)
+            tol = (U["fp16"] + 2 * SCORE) * mag + U["fp16"] * np.abs(ref) + t * 2.0 ** -31 * np.abs(tokens[1]).max() + TINY["fp16"]
+            assert (np.abs(got - ref) <= tol).all(), b
