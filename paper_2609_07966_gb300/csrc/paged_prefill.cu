@@ -213,9 +213,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     if (threadIdx.x < a.slots) base[threadIdx.x + 1] = upto;
     if (threadIdx.x == 0) base[0] = 0;
     __syncthreads();
-  }
-  if (SHARED) {
-    int cur, end;
+    int cur, end;                                          // of this CTA's run
     int most = 0, least = INT32_MAX, units = 0;
     for (int w = 0; w < (a.slots + 31) / 32; ++w) {
       most = max(most, ctl->most[w]);
@@ -254,8 +252,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     const int c0 = cur - unit0, c1 = min(all, end - unit0);
     tell(u, c0, c1);
     ctl->whole = c1 - c0 == all;
-    if (!ctl->shared) a.joins[slot * Hkv + kvh] = make_int4(0, 0, 0, 0);
-    if (!ctl->shared) return;
+    if (!ctl->shared) {
+      a.joins[slot * Hkv + kvh] = make_int4(0, 0, 0, 0);
+      return;
+    }
     const Runs rs(base[a.slots], a.runs);
     const int first = rs.of(unit0), place0 = 2 * first + (rs.start(first) < unit0 ? 1 : 0);
     ctl->place = (int)blockIdx.x == first ? place0 : 2 * (int)blockIdx.x;
@@ -714,7 +714,7 @@ Plan plan_of(const PagedAttnCall& c) {
   const int64_t G = c.s.Hq / c.s.Hkv, m = ceil_div(c.s.n, c.s.B);
   p.per = (int)ceil_div(m * G, kRows);
   p.slots = c.s.start == nullptr ? (int64_t)c.s.B * p.per : (c.s.n * G + (int64_t)c.s.B * (kRows - 1)) / kRows;
-  // (tiles are counted in 32 bits)
+  // (not with caches that hold fewer tiles than a piece and the join cost; tiles are counted in 32 bits)
   const int64_t units = p.slots * c.s.Hkv, tiles = c.s.max_pages * c.s.page / kTokens + 1;
   p.runs = units <= kShared && tiles > kPieceTiles + kJoinTiles && units * tiles <= INT32_MAX / 2 ? kNumSMs : 0;
   return p;
