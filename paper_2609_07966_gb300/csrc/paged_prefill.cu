@@ -277,8 +277,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
     for (int s = 0; s < kHeads; ++s) tc_mbar_init(&ctl->head[s], 1);
     for (int s = 0; s < 2; ++s) {
       tc_mbar_init(&ctl->sfull[s], 1);
-      tc_mbar_init(&ctl->pfull[s][0], 4);
-      tc_mbar_init(&ctl->pfull[s][1], 4);
+      tc_mbar_init(&ctl->pfull[s][0], 8);                  // (the first half's weights; both halves' outputs are scaled)
+      tc_mbar_init(&ctl->pfull[s][1], 4);                  // (the second half's weights)
       tc_mbar_init(&ctl->pvdone[s], 1);
     }
     tc_fence_mbar_init();
@@ -354,7 +354,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
           ok = wait(&ctl->tile_full[vi % kSlots], (uint32_t)((vi / kSlots) & 1));
           for (int k = 0; ok && k < 2; ++k) {
             if (t < nt[k]) {
-              // (the first half's weights arrive while the softmax works on the second)
+              // (the first half's weights arrive while the softmax works on the second; a product over half of the tokens adds
+              // to all dims of the outputs, so both halves of those have been scaled by then)
               ok = wait(&ctl->pfull[k][0], (uint32_t)(((k == 0 ? done0 : done1) + t) & 1));
               if (!ok) break;
               values(k, t, 0);
@@ -577,6 +578,12 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
               tm_store<32>(tO + i * 32, o);
             }
           }
+        }
+        if (half == 1) {                                     // (the other half's warps arrive there after their weights)
+          tm_store_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) tc_mbar_arrive(&ctl->pfull[k][0]);
         }
 #pragma unroll 1
         for (int i = 0; i < HC / 32; ++i) {                  // (weights over scores that were read before)
