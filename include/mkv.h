@@ -683,7 +683,8 @@ typedef struct {
 /* Device memory owned by the caller.  The pages of an entry differ from one
  * another, and those that an append writes into belong to no other entry (full
  * pages may be shared, as those of a common beginning).  num_pages * Hkv and
- * max_pages * page_size stay below 2^31. */
+ * max_pages * page_size stay below 2^31.  page_table, T_len and a call's start
+ * do not change while the call runs (its own stores to T_len aside). */
 typedef struct {
   int64_t num_pages;            /* pages in the pool                          */
   int64_t max_pages;            /* pages an entry may hold                    */
@@ -745,8 +746,9 @@ mkv_status mkv_paged_workspace_size(const mkv_paged_config* cfg, int64_t n, int6
  * max_pages * page_size is at most 2^36, max_rows * Hq / Hkv at most 2^26.  The
  * cache is only read.  ws must be 256-byte aligned.  The path is chosen by
  * max_rows, so give the true maximum (1 for a step of single tokens).  After a
- * bounded wait that ran out (MKV_FLAG_WAIT_TIMEOUT), outputs are not valid and
- * the counters of ws have to be zeroed again. */
+ * bounded wait that ran out (MKV_FLAG_WAIT_TIMEOUT), or if lengths, start or
+ * pages changed under way (which may set MKV_FLAG_BAD_INDEX), outputs are not
+ * valid and the counters of ws have to be zeroed again. */
 mkv_status mkv_paged_attention(const mkv_paged_config* cfg, const void* q, int64_t q_stride, const int32_t* start,
                                int64_t n, int64_t max_rows, const mkv_paged_cache* cache, void* out,
                                int64_t out_stride, void* ws, size_t ws_bytes, void* stream);

@@ -6,6 +6,7 @@
 #pragma once
 
 #include "mkv_paged.cuh"
+#include "mkv_paged_runs.h"
 
 namespace mkv {
 
@@ -74,21 +75,6 @@ __device__ __forceinline__ Entry entry_of(const PagedAttnCall& c, const WorkArgs
   e.chunks = e.tokens > 0 ? max(1, (e.len + kTokens - 1) / kTokens) : 0;
   return e;
 }
-
-// `total` chunks in `runs` runs, the first total % runs of them one longer.
-struct Runs {
-  int runs, len, longer;
-  __device__ __forceinline__ Runs(int total, int grid) {
-    runs = min(total, grid);
-    len = runs > 0 ? total / runs : 0;
-    longer = total - len * runs;
-  }
-  __device__ __forceinline__ int start(int i) const { return i * len + min(i, longer); }
-  __device__ __forceinline__ int of(int chunk) const {    // the run that holds a chunk
-    const int split = longer * (len + 1);
-    return chunk < split ? chunk / (len + 1) : longer + (chunk - split) / len;
-  }
-};
 
 // A whole warp goes through chunks c0 .. c1 - 1 of entry b's key head.  It calls begin() once the first pages are being
 // fetched, and for each chunk
@@ -232,10 +218,14 @@ __device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkA
   };
   int batch = 0;
   Entry e = entry(b);
+  int of_entry = e.chunks * Hkv;
   while (cur < end) {
-    while (cur >= base + e.chunks * Hkv) {
-      base += e.chunks * Hkv;
-      e = entry(++b);
+    if (!walk_to(cur, B, b, base, of_entry, [&](int i) {
+          e = entry(i);
+          return e.chunks * Hkv;
+        })) {
+      if (lane == 0) atomicOr(status, MKV_FLAG_BAD_INDEX); // (lengths changed under way)
+      return true;
     }
     const int kvh = (cur - base) / e.chunks, unit0 = base + kvh * e.chunks;
     const int c0 = cur - unit0, c1 = min(e.chunks, c0 + (end - cur));
@@ -258,9 +248,10 @@ __device__ __forceinline__ bool work_through(const PagedAttnCall& c, const WorkA
               p.place0 = 2 * p.first;
               p.count = (chunks0 + part - 1) / part;
             } else {
-              p.first = rs.of(unit0);
-              p.place0 = 2 * p.first + (rs.start(p.first) < unit0 ? 1 : 0);
-              p.count = rs.of(unit0 + e.chunks - 1) - p.first + 1;
+              const Shares sh(rs, unit0, e.chunks);
+              p.first = sh.first;
+              p.place0 = sh.place0;
+              p.count = sh.count;
             }
             p.mine = r == p.first ? p.place0 : 2 * r;
           }

@@ -257,9 +257,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       return;
     }
     const Runs rs(base[a.slots], a.runs);
-    const int first = rs.of(unit0), place0 = 2 * first + (rs.start(first) < unit0 ? 1 : 0);
-    ctl->place = (int)blockIdx.x == first ? place0 : 2 * (int)blockIdx.x;
-    if (c0 == 0) a.joins[slot * Hkv + kvh] = make_int4(first, place0, rs.of(unit0 + all - 1) - first + 1, u.b);
+    const Shares sh(rs, unit0, all);
+    ctl->place = (int)blockIdx.x == sh.first ? sh.place0 : 2 * (int)blockIdx.x;
+    if (c0 == 0) a.joins[slot * Hkv + kvh] = make_int4(sh.first, sh.place0, sh.count, u.b);
   };
   if (SHARED) next_piece();
   if (warp == 20) tc_alloc(&ctl->tslot, 512);
