@@ -102,6 +102,7 @@ def append_page(codes, scale, held, new, fmt):
     else:
         now = least_scale(most, fmt)
         if held > 0:
+            now = max(now, np.float32(scale))
             with np.errstate(under="ignore"):
                 less = np.float32(scale) / now
                 codes[:held] = encode(decode(codes[:held], fmt).astype(np.float32) * less, fmt)

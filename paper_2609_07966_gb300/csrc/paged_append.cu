@@ -213,7 +213,7 @@ __device__ __forceinline__ void quantize_unit(const AppendArgs& a, const Slot& s
     for (int w = 0; w < GROUP / 32; ++w) most = max(most, of_warp[w]);
   }
   const bool fits = s.held > 0 && __uint_as_float(most) <= top_code<FMT>() * was;
-  const float now = fits ? was : least_scale<FMT>(most);
+  const float now = fits ? was : fmaxf(was, least_scale<FMT>(most));   // (a caller's scale may be above the largest)
   if (!fits) {
     if (tid == 0) (key ? a.c.k_scale : a.c.v_scale)[head] = now;
     if (s.held > 0) {
