@@ -11,10 +11,9 @@
 namespace mkv {
 
 constexpr int kTokens = 128;        // of a chunk
-constexpr int kGroups = kTokens / 16;
 
 struct WorkArgs {
-  int log_page, log_box;            // a copy's tokens: a page's, a chunk's at most
+  int log_page;                     // of the tokens of a page, which is a copy: 16 to 128, a chunk at most
   int parts;                        // CTAs a unit if each gets as many; 0: not to be done
   int lost;                         // so many chunks more a CTA are worth it
   int grid;
@@ -28,7 +27,6 @@ constexpr int kAnyLost = 1 << 30;
 inline WorkArgs work_args(const PagedAttnCall& c, int grid, int lost) {
   WorkArgs w{};
   while ((1 << w.log_page) < c.s.page) ++w.log_page;
-  w.log_box = w.log_page;           // (pages are of 16 to 128 tokens)
   const int units = c.s.B * c.s.Hkv, parts = grid / units;
   w.parts = parts * units * 5 >= grid * 4 ? parts : 0;
   w.lost = lost;
@@ -87,13 +85,13 @@ __device__ __forceinline__ bool load_chunks(const PagedAttnCall& c, const WorkAr
                                             int lane, int& batch, int b, int kvh, int len, int c0, int c1, int flags,
                                             Begin begin, Copies copies, Publish publish) {
   // A batch is 32 copies' pages, a lane each: page and scales of the next batch are fetched during this one.
-  const int log_per = 7 - w.log_box, span = 32 >> log_per; // copies a chunk, chunks a batch
+  const int log_per = 7 - w.log_page, span = 32 >> log_per; // copies a chunk, chunks a batch
   const int32_t* table = c.s.page_table + (int64_t)b * c.s.max_pages;
   auto exists = [&](int chunk) {                           // this lane's copy of the batch from `chunk` on
-    return chunk + (lane >> log_per) < c1 && chunk * kTokens + (lane << w.log_box) < len;
+    return chunk + (lane >> log_per) < c1 && chunk * kTokens + (lane << w.log_page) < len;
   };
   auto fetch = [&](int chunk) {
-    return exists(chunk) ? table[(chunk * kTokens + (lane << w.log_box)) >> w.log_page] : -1;
+    return exists(chunk) ? table[(chunk << (7 - w.log_page)) + lane] : -1;
   };
   auto check = [&](int chunk, int id) {                    // (a page outside the pool is not seen)
     if (!exists(chunk)) return -1;

@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) block_kernel(const BlockArgs a)
   tc_fence_after();
   pdl_wait_and_trigger();
   const uint32_t tbase = ctl->tslot;
-  const int all_copies = (1 << (kTokens >> a.w.log_box)) - 1;
+  const int all_copies = (1 << (kTokens >> a.w.log_page)) - 1;
 
   if (warp >= S::SW + 8) regs_down<S::RO>();
   if (warp == S::SW + 8) {
@@ -131,12 +131,12 @@ __global__ void __launch_bounds__(S::THREADS, 1) block_kernel(const BlockArgs a)
       return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
     };
     int g = 0;
-    const int log_box = a.w.log_box;
+    const int log_page = a.w.log_page;
     const bool ok = work_through(
         c, a.w, status, reinterpret_cast<float2*>(sm + S::SC_OFF), lane, [&](const Piece&) { return true; },
         [&](const Chunk& ch, const Piece& p, bool mine, int id, int at) {
-          const uint32_t bytes = (uint32_t)(__popc(ch.copies) * D) << log_box;
-          const int64_t from = (((int64_t)id * Hkv + p.kvh) * c.s.page + ((ch.chunk * kTokens + (at << log_box)) & (c.s.page - 1))) * D;
+          const uint32_t bytes = (uint32_t)(__popc(ch.copies) * D) << log_page;
+          const int64_t from = ((int64_t)id * Hkv + p.kvh) * c.s.page * D;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const int item = 2 * g + h, s = item % S::RAWS;
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) block_kernel(const BlockArgs a)
             }
             __syncwarp();
             if (mine)
-              bulk_load(sm + S::R_OFF + s * S::RAW + (at << log_box) * D, (h == 0 ? c.k : c.v) + from, (uint32_t)D << log_box,
+              bulk_load(sm + S::R_OFF + s * S::RAW + (at << log_page) * D, (h == 0 ? c.k : c.v) + from, (uint32_t)D << log_page,
                         &ctl->raw_full[s]);
           }
           return true;
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) block_kernel(const BlockArgs a)
       if (h == 1 && (copies != all_copies || tail < kTokens))      // what no row sees must not meet a zero weight as NaN
 #pragma unroll
         for (int i = 0; i < 128 / STEP; ++i)
-          if (row + i * STEP >= tail || !(copies >> ((row + i * STEP) >> a.w.log_box) & 1)) x[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (row + i * STEP >= tail || !(copies >> ((row + i * STEP) >> a.w.log_page) & 1)) x[i] = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
       for (int i = 0; i < 128 / STEP; ++i) {
         uint32_t e[8];
@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(S::THREADS, 1) block_kernel(const BlockArgs a)
       meet();
     }
 
-    const int log_group = a.w.log_box - 4;
+    const int log_group = a.w.log_page - 4;
     float m = kNoMax, m2 = kNoMax, l = 0.f, back = 1.f;
     int own = 0, pos0 = 0;                                 // this row's own position, the last that it sees; the first row's
     Piece hd;

@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     auto free_stage = [&]() {
       return g < S::STAGES || wait(&ctl->empty[g % S::STAGES], (uint32_t)((g / S::STAGES - 1) & 1));
     };
-    const int log_box = a.w.log_box;
+    const int log_page = a.w.log_page;
     bool ok = work_through(
         c, a.w, status, reinterpret_cast<float2*>(sm + S::SC_OFF), lane,
         [&](const Piece& p) {                              // a piece's queries: one copy a token's heads
@@ -140,15 +140,15 @@ __global__ void __launch_bounds__(kThreads, kCtas)
           if (!free_stage()) return false;
           const int s = g % S::STAGES;
           if (lane == 0) {
-            tc_mbar_expect_tx(&ctl->full[s], (uint32_t)(__popc(ch.copies) * 2 * D) << log_box);
+            tc_mbar_expect_tx(&ctl->full[s], (uint32_t)(__popc(ch.copies) * 2 * D) << log_page);
             ctl->loads = g + 1;
           }
           __syncwarp();
           if (mine) {
-            uint8_t* dst = sm + S::KV_OFF + s * 2 * S::TILE + (at << log_box) * D;
-            const int y = (ch.chunk * kTokens + (at << log_box)) & (c.s.page - 1), z = id * Hkv + p.kvh;
-            tma_load_4d(dst, &kmap, 0, y, z, 0, &ctl->full[s]);
-            tma_load_4d(dst + S::TILE, &vmap, 0, y, z, 0, &ctl->full[s]);
+            uint8_t* dst = sm + S::KV_OFF + s * 2 * S::TILE + (at << log_page) * D;
+            const int z = id * Hkv + p.kvh;
+            tma_load_4d(dst, &kmap, 0, 0, z, 0, &ctl->full[s]);
+            tma_load_4d(dst + S::TILE, &vmap, 0, 0, z, 0, &ctl->full[s]);
           }
           return true;
         },
@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         const int ch = now.chunk;
         const int t0 = ch * kTokens + warp * 32;
         const float2* scales = reinterpret_cast<const float2*>(sm + S::SC_OFF) + now.scales;
-        const int cp[2] = {(warp * 2) >> (a.w.log_box - 4), (warp * 2 + 1) >> (a.w.log_box - 4)};   // the groups' copies
+        const int cp[2] = {(warp * 2) >> (a.w.log_page - 4), (warp * 2 + 1) >> (a.w.log_page - 4)};   // the groups' copies
         const float2 sc[2] = {scales[cp[0]], scales[cp[1]]};
         const bool in[2] = {(now.copies >> cp[0] & 1) != 0 && t0 < hd.len, (now.copies >> cp[1] & 1) != 0 && t0 + 16 < hd.len};
         if (in[0] || in[1]) {

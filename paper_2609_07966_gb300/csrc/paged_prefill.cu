@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
   volatile int* fail = &ctl->fail;
   Chunk* heads = reinterpret_cast<Chunk*>(sm + S::HD_OFF);
   uint32_t* status = a.status;
-  const int all_copies = (1 << (kTokens >> a.w.log_box)) - 1;
+  const int all_copies = (1 << (kTokens >> a.w.log_page)) - 1;
   for (;;) {
     Unit u;
     u.b = ctl->b;
@@ -379,15 +379,14 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
         auto wait = [&](uint64_t* bar, uint32_t parity) {
           return __all_sync(0xffffffffu, wait_or_fail(bar, parity, fail, status)) != 0;
         };
-        const int log_box = a.w.log_box;
+        const int log_page = a.w.log_page;
         int batch = 0;
         load_chunks<kHeldBatches>(
             c, a.w, status, reinterpret_cast<float2*>(sm + S::SC_OFF), lane, batch, u.b, u.kvh, u.len, c0, c0 + ntiles, 0,
             [&]() { return true; },
             [&](const Chunk& ch, bool mine, int id, int at) {
-              const uint32_t bytes = (uint32_t)(__popc(ch.copies) * D) << log_box;
-              const int in_page = (ch.chunk * kTokens + (at << log_box)) & (c.s.page - 1);
-              const int64_t from = (((int64_t)id * Hkv + u.kvh) * c.s.page + in_page) * D;
+              const uint32_t bytes = (uint32_t)(__popc(ch.copies) * D) << log_page;
+              const int64_t from = ((int64_t)id * Hkv + u.kvh) * c.s.page * D;
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
                 const int item = 2 * (before + ch.chunk - c0) + h, s = item % S::RAWS;
@@ -398,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
                 }
                 __syncwarp();
                 if (mine)
-                  bulk_load(sm + S::R_OFF + s * S::RAW + (at << log_box) * D, (h == 0 ? c.k : c.v) + from, (uint32_t)D << log_box,
+                  bulk_load(sm + S::R_OFF + s * S::RAW + (at << log_page) * D, (h == 0 ? c.k : c.v) + from, (uint32_t)D << log_page,
                             &ctl->raw_full[s]);
               }
               return true;
@@ -439,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
           if (copies != all_copies || tail < kBR)
 #pragma unroll
             for (int i = 0; i < kBR / STEP; ++i)
-              if (row + i * STEP >= tail || !(copies >> ((row + i * STEP) >> a.w.log_box) & 1)) x[i] = make_uint4(0u, 0u, 0u, 0u);
+              if (row + i * STEP >= tail || !(copies >> ((row + i * STEP) >> a.w.log_page) & 1)) x[i] = make_uint4(0u, 0u, 0u, 0u);
         }
 #pragma unroll
         for (int i = 0; i < kBR / STEP; ++i) {
@@ -528,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill_kernel(const PrefillArgs 
       }
       constexpr int HC = kBR / 2;                            // columns of a thread
       const uint32_t tH = tS + (uint32_t)(half * HC);
-      const int log_group = a.w.log_box - 4;
+      const int log_group = a.w.log_page - 4;
       float m = kNoMax, m2 = kNoMax, l = 0.f;
       for (int t = 0; t < ntk; ++t) {
         const int at = (before + t) % kHeads;
