@@ -10,7 +10,9 @@
 //   warps   a unit a warp, eight units a CTA: decode steps, and pages of 16 tokens (128 work columns);
 //   blocks  a unit a CTA of 256 threads: larger pages filled by prompts.
 // (One to nine rows of 64 entries: warps 8.9 us, blocks 22; three prompts in pages of 64 tokens: 76 and 63.)  One token of 8
-// entries takes 5 us, its launch and two dependent loads; the three prompts, 10238 rows of 32 + 16 heads, run at 0.55 of the
+// entries takes 5 us, its launch and two dependent loads.  One to nine rows of 64 entries are one wave (408 CTAs, three an SM):
+// latency, a scheduler issues in a third of the cycles and a warp once in 13 (without the queries 8.1 us, without rotations
+// too 6.3, 8 entries 6.7); a warp's unit spills 88 to 92 bytes at the 80 registers that three CTAs leave.  The three prompts, 10238 rows of 32 + 16 heads, run at 0.55 of the
 // measured copy rate: keys and values alone take 30 us, bound by instructions (the maximum, the rotation twice, the codes) and
 // by the latency of a unit's steps, which CTAs of the other kind fill in part.
 // Other CTAs of the slot rotate its rows' queries, a thread the same dims of several heads.

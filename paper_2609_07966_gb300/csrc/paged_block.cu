@@ -53,7 +53,7 @@ struct BShape {
   // copies, where a thread has 32 columns anyway, 44 -> 49).
   static constexpr int HALVES = COPIES == 1 ? 2 : 1, SW = 4 * HALVES;      // softmax warps
   static constexpr int THREADS = 32 * (SW + 12), SOFT = 32 * SW;
-  // registers a thread: what a launch gets, and its split
+  // registers a thread: what a launch gets, and its split (with one copy up to 28 bytes are spilled)
   static constexpr int RL = HALVES == 2 ? 96 : 128, RS = HALVES == 2 ? 112 : 208, RC = HALVES == 2 ? 96 : 104,
                        RO = HALVES == 2 ? 64 : 96;
   static_assert(HALVES * RS + 2 * RC + RO <= (HALVES + 3) * RL, "register shares");

@@ -15,7 +15,7 @@
 // A tile of 128 tokens takes about 3900 cycles for both blocks, of which the products need 2048: a block's scores, softmax and
 // second product follow one another, tensor memory holds one tile of scores a block, and the other block's products fill only
 // a part of the wait.  A unit takes another 10 us: its queries, the pipeline's start, the last tile's chain and the output.
-// 4096 tokens, 32 / 8 heads of 128: 141 us, 0.50 of the measured peak; 511 and 383 over 8K and 6K: 122 us, 0.44.
+// 4096 tokens, 32 / 8 heads of 128: 143 us, 0.50 of the measured peak; 511 and 383 over 8K and 6K: 121 us, 0.44.
 //
 // A tile's pages have scales of their own: within 16 columns both are constant, so a score's is part of the factor of its
 // exponent, the maxima are kept per 16 columns until they are scaled, and a weight is p vs 2^(m - m2 + 6).
@@ -63,7 +63,7 @@ struct PrefillArgs {
   int4* joins;                      // [slot][Hkv]: the unit's first run, its first piece's place, how many pieces, its entry
 };
 
-// GC: tokens that share a page's scales for certain, 16 or (pages of 32 and more) 32: a 4096-token prompt 152 and 141 us.
+// GC: tokens that share a page's scales for certain, 16 or (pages of 32 and more) 32: a 4096-token prompt 154 and 143 us.
 template <int FMT_, int D_, int GC_>
 struct PShape {
   static constexpr int FMT = FMT_, D = D_, GC = GC_, KA = D / 64;
